@@ -293,6 +293,73 @@ lqer_status_t lqer_workspace_init(void* workspace, size_t workspace_bytes, void*
 /* Read the device-side status word of `workspace` (synchronises `stream`). */
 lqer_status_t lqer_poll_status(const void* workspace, void* stream, lqer_status_t* device_status);
 
+/* ---- Between the layers ----
+ * What a program that serves a model needs at the layers' boundary, with the same element types: the norm in front of a layer, the
+ * gated activation in front of a down projection, and the adapters of many requests beside a shared projection.
+ * All are asynchronous on `stream`, need no workspace and allocate nothing; pointers belong to the current device and are 16-byte
+ * aligned (16-bit and 32-bit tensors alike).  An MXINT8 tensor [M,K] is M*K mantissas followed by M*K/16 exponent bytes, in the
+ * format (a_bits, exp_min, exp_max) of `cfg`; cfg may be NULL for the defaults.  M is at most 2^24. */
+
+/* h = X + residual (fp32 sum, rounded to r_dtype), residual_out = h, Y = h * weight / sqrt(mean(h^2) + eps) along the row
+ * (pre-norm transformer block; the paper's Section 2.1 leaves the quantised input of the next layer to its producer).
+ *  - X [M,K] fp32 or bf16; residual and residual_out [M,K] of r_dtype (fp32 or bf16); weight [K] of w_dtype (fp32 or bf16).
+ *    residual may be NULL (h = X rounded to r_dtype), residual_out may be NULL (h is not kept) or may be residual itself, or X if
+ *    it has X's type.
+ *  - Y [M,K] of y_dtype, apart from all inputs: fp32, bf16 (nearest even), or MXINT8 (K a multiple of 16), which is quantised as
+ *    lqer_linear_ex would quantise it, from 64-bit values: mantissas and exponents are those of exact arithmetic on h.
+ *  - K a multiple of 8, at most 2^20; eps >= 0.  One row takes one CTA; rows up to 32768 columns are read once. */
+lqer_status_t lqer_add_rms_norm(const void* X, lqer_dtype_t x_dtype, const void* residual, void* residual_out, lqer_dtype_t r_dtype,
+                                const void* weight, lqer_dtype_t w_dtype, double eps, int M, int K, const lqer_config_t* cfg,
+                                void* Y, lqer_dtype_t y_dtype, void* stream);
+
+/* Y = act(gate) * up, element by element.  gate and up: M rows of N elements of x_dtype (fp32 or bf16), row_stride elements from one row to
+ * the next (N for two dense tensors, 2 N for the halves of one [M, 2 N] tensor; a multiple of 8).  Y [M,N] dense, of y_dtype: fp32,
+ * bf16 or MXINT8 (N a multiple of 16; quantised from 64-bit values as above), apart from the inputs.  N is a multiple of 8, at most 2^22. */
+typedef enum {
+  LQER_SILU = 0,             /* g / (1 + exp(-g)) */
+  LQER_GELU_TANH = 1         /* g / 2 * (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
+} lqer_activation_t;
+lqer_status_t lqer_gated_activation(const void* gate, const void* up, lqer_dtype_t x_dtype, long long row_stride, int M, int N,
+                                    lqer_activation_t act, const lqer_config_t* cfg, void* Y, lqer_dtype_t y_dtype, void* stream);
+
+/* MXINT8 activations as values (exact): Xq [M,K] in the format of cfg, Y [M,K] fp32 or bf16, K a multiple of 16.  For a consumer other than a
+ * layer; the counterpart of lqer_quantize_activations and of LQER_MXINT8 outputs. */
+lqer_status_t lqer_dequantize_activations(const void* Xq, int M, int K, const lqer_config_t* cfg, void* Y, lqer_dtype_t y_dtype,
+                                          void* stream);
+
+/* Adapters of many requests beside one shared projection: Y[m] = Y0[m] + scale_a (X[m] A_a) B_a, where a is the adapter of row m's
+ * request.  The shared projection (lqer_linear*) computes Y0; the adapters are a term of the same shape as the layer's own
+ * (X A_k) B_k (Section 3.1), with other factors for other rows.
+ *
+ * A pool holds n_slots adapters (at most 1024) of one [K,N] projection, each of any rank from 1 to max_rank (at most 256), their factors
+ * in bf16 in the kernel's order.  The struct is the caller's (host); `data` is device memory, 256-byte aligned.
+ *  - lqer_adapter_pool_bytes reads K, N, max_rank, n_slots.  lqer_adapter_pool_init empties all slots.
+ *  - lqer_adapter_load puts A [K,rank] and B [rank,N] (dense, both of `dtype`: fp32, rounded to bf16, or bf16) into a slot, replacing
+ *    what was there; rank 0 empties the slot (A and B are not read).  Stream order decides which calls see which adapter.  */
+typedef struct {
+  void* data;
+  int K, N, max_rank, n_slots;
+} lqer_adapter_pool_t;
+lqer_status_t lqer_adapter_pool_bytes(const lqer_adapter_pool_t* pool, size_t* bytes);
+lqer_status_t lqer_adapter_pool_init(const lqer_adapter_pool_t* pool, size_t pool_bytes, void* stream);
+lqer_status_t lqer_adapter_load(const lqer_adapter_pool_t* pool, int slot, const void* A, const void* B, lqer_dtype_t dtype, int rank,
+                                float scale, void* stream);
+/* The plan of a batch: its rows sorted by slot, for every adapted projection of a step.  slots: DEVICE array of M ints, -1 for a row without
+ * adapter; a value that is neither -1 nor a slot below n_slots counts as -1 and is reported as LQER_ERR_BOUNDS by lqer_poll_status(plan).
+ * plan: device memory of lqer_adapter_plan_bytes, 256-byte aligned.  A captured graph may hold the call: a replay sorts what
+ * `slots` holds then. */
+lqer_status_t lqer_adapter_plan_bytes(int M, int n_slots, size_t* bytes);
+lqer_status_t lqer_adapter_plan(const int* slots, int M, int n_slots, void* plan, size_t plan_bytes, void* stream);
+/* The term itself.  X [M,K] fp32, bf16 or MXINT8 (format of cfg); Y0 and Y [M,N] fp32 or bf16 each (Y may be Y0 if the types agree, and is
+ * apart from everything otherwise).  plan: made by lqer_adapter_plan for the same M and the given plan_slots <= pool->n_slots; its
+ * buffer is only read, but for its status: a plan of another batch size (or none), or a slot that no lqer_adapter_load
+ * or lqer_adapter_pool_init of this pool's shape wrote, is reported there as LQER_ERR_BAD_PACKED, and such rows are not written or
+ * take no adapter.  Rows of an empty slot take none.  K % 16 == 0, N % 8 == 0.  fp32 accumulation; fp32 X and X A are kept to
+ * 24 bits for fp32 Y and to 16 bits for bf16 Y.  A row's result does not depend on the other rows; its last
+ * bits may depend on M. */
+lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lqer_adapter_pool_t* pool, void* plan, int plan_slots,
+                            const void* Y0, lqer_dtype_t y0_dtype, void* Y, lqer_dtype_t y_dtype, const lqer_config_t* cfg, void* stream);
+
 /* Force a kernel path for tests: 0 auto (which alone runs the cluster kernel for 3 to 16 rows), 1 plain CUDA-core
  * reference kernel, 2 small-batch kernels
  * (column-owner kernel for M <= 4, small prologue + small-batch GEMM for M <= 128), 3 tensor-core GEMM behind the
@@ -343,9 +410,9 @@ unsigned long long lqer_launch_count(void);
  * serialise nothing but they do keep consecutive kernels from overlapping, so leave it off
  * when measuring end-to-end time.  lqer_profile_collect waits for the recorded launches,
  * sums launches and elapsed milliseconds per kernel family into *out (host) and forgets them.
- * Families: 0 weight pack, 1 export, 2 stand-alone activation quantiser, 3 activation prologue,
- * 4 CUDA-core reference GEMM, 5 factor preparation (calibration statistics, subspace iteration),
- * 6 tensor-core GEMM (CTA pair per tile), 7 decode kernels. */
+ * Families: 0 weight pack (adapters too), 1 export, 2 stand-alone activation kernels (quantiser and back, norm, gated activation),
+ * 3 activation prologue, 4 CUDA-core reference GEMM, 5 factor preparation (calibration statistics, subspace iteration),
+ * 6 tensor-core GEMM (CTA pair per tile), 7 decode kernels, adapters and their plans. */
 #define LQER_NUM_KERNEL_FAMILIES 8
 typedef struct {
   unsigned long long launches[LQER_NUM_KERNEL_FAMILIES];

@@ -48,6 +48,10 @@ class Call(C.Structure):
     _fields_ = [("X", C.c_void_p), ("M", C.c_int), ("packed", C.c_void_p), ("Y", C.c_void_p)]
 
 
+class _Pool(C.Structure):
+    _fields_ = [("data", C.c_void_p), ("K", C.c_int), ("N", C.c_int), ("max_rank", C.c_int), ("n_slots", C.c_int)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -94,6 +98,15 @@ def lib() -> C.CDLL:
             "lqer_linear_host_batched_bytes": (i, [C.POINTER(Call), i, C.POINTER(sz)]),
             "lqer_linear_host_batched": (i, [C.POINTER(Call), i, vp, sz, vp]),
             "lqer_linear_host_batched_ex": (i, [C.POINTER(Call), i, i, i, vp, sz, vp]),
+            "lqer_add_rms_norm": (i, [vp, i, vp, vp, i, vp, i, C.c_double, i, i, cfgp, vp, i, vp]),
+            "lqer_gated_activation": (i, [vp, vp, i, C.c_longlong, i, i, i, cfgp, vp, i, vp]),
+            "lqer_dequantize_activations": (i, [vp, i, i, cfgp, vp, i, vp]),
+            "lqer_adapter_pool_bytes": (i, [C.POINTER(_Pool), C.POINTER(sz)]),
+            "lqer_adapter_pool_init": (i, [C.POINTER(_Pool), sz, vp]),
+            "lqer_adapter_load": (i, [C.POINTER(_Pool), i, vp, vp, i, i, C.c_float, vp]),
+            "lqer_adapter_plan_bytes": (i, [i, i, C.POINTER(sz)]),
+            "lqer_adapter_plan": (i, [vp, i, i, vp, sz, vp]),
+            "lqer_adapters": (i, [vp, i, i, C.POINTER(_Pool), vp, i, vp, i, vp, i, cfgp, vp]),
             "lqer_workspace_init": (i, [vp, sz, vp]),
             "lqer_poll_status": (i, [vp, vp, C.POINTER(i)]),
             "lqer_set_path": (i, [i]),
@@ -406,6 +419,229 @@ def linear_host_batched_ex(calls, ws: torch.Tensor, x_dtype, y_dtype, stream=Non
     """linear_host_batched with host X of x_dtype and host Y of y_dtype; `calls` from make_host_calls(..., x_dtype, y_dtype)."""
     _check(lib().lqer_linear_host_batched_ex(calls, len(calls), _DTYPES[x_dtype], _DTYPES[y_dtype], ws.data_ptr(), ws.numel(),
                                              _stream(stream)), "lqer_linear_host_batched_ex")
+
+
+# ---- between the layers ----------------------------------------------------------------------------------------------------
+# One small kernel a call: what Python adds in front of the launch counts, so these take the raw stream and one check a tensor.
+
+def _raw_stream(stream, index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
+
+
+def _on(t: torch.Tensor):
+    """The device of t, current while the call runs, if it is another than the current one."""
+    index = t.get_device()
+    if index < 0:
+        raise ValueError("expected CUDA tensors")
+    return None if index == torch.cuda.current_device() else torch.cuda.device(index)
+
+
+def _same(first: torch.Tensor, *others) -> None:
+    """All on the first one's device, dense (None is skipped)."""
+    index = first.get_device()
+    for t in (first, *others):
+        if t is not None and (t.get_device() != index or not t.is_contiguous()):
+            raise ValueError("expected contiguous CUDA tensors of one device")
+
+
+def _stream_here(stream, t: torch.Tensor) -> int:
+    if stream is not None and stream.device != t.device:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return _raw_stream(stream, t.get_device())
+
+
+def _cfg(cfg):
+    return None if cfg is None else C.byref(cfg)
+
+
+def _code(dt, *allowed) -> int:
+    if dt not in allowed:
+        raise ValueError(f"unsupported dtype {dt}")
+    return _DTYPES[dt]
+
+
+_REAL = (torch.float32, torch.bfloat16)
+_ACTS = {"silu": 0, "gelu": 1}
+
+
+def _output(Y, rows: int, cols: int, out_dtype, like: torch.Tensor):
+    """The tensor of a [rows, cols] result of out_dtype, made where none is given, and its type's code."""
+    if Y is not None and Y.dtype != torch.uint8:
+        out_dtype = Y.dtype
+    elif Y is not None:
+        out_dtype = MXINT8
+    code = _code(out_dtype, *_REAL, MXINT8)
+    shape = (mxint8_bytes(rows, cols),) if out_dtype == MXINT8 else (rows, cols)
+    if out_dtype == MXINT8 and cols % 16:
+        raise ValueError("an MXINT8 output has whole blocks of 16 columns")
+    if Y is None:
+        Y = torch.empty(shape, dtype=_tensor_dtype(out_dtype), device=like.device)
+    elif tuple(Y.shape) != shape:
+        raise ValueError(f"expected an output of shape {shape}")
+    return Y, code
+
+
+def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None, out_dtype=MXINT8,
+                 cfg: Config | None = None, residual_out: torch.Tensor | None = None, Y: torch.Tensor | None = None, stream=None):
+    """h = X + residual (in the residual's type), Y = h * weight / sqrt(mean(h^2) + eps) along the rows: (Y, h).
+
+    X [M, K] and residual [M, K] fp32 or bf16, weight [K]; Y of out_dtype (fp32, bf16 or MXINT8).  Without a residual h is X, and
+    is only written where residual_out is given (None is returned otherwise); with one it goes to residual_out (which may be
+    the residual itself) or to a new tensor."""
+    if X.dim() != 2 or weight.dim() != 1 or weight.shape[0] != X.shape[1]:
+        raise ValueError("expected X [M, K] and weight [K]")
+    M, K = X.shape
+    for t in (residual, residual_out):
+        if t is not None and t.shape != X.shape:
+            raise ValueError("the residual has X's shape")
+    if residual is not None and residual_out is not None and residual.dtype != residual_out.dtype:
+        raise ValueError("residual and residual_out are of one type")
+    other = _on(X)
+    if other is not None:
+        with other:
+            return add_rms_norm(X, weight, eps, residual, out_dtype, cfg, residual_out, Y, stream)
+    Y, y_code = _output(Y, M, K, out_dtype, X)
+    if residual is not None and residual_out is None:
+        residual_out = torch.empty_like(residual)
+    _same(X, weight, residual, residual_out, Y)
+    r = residual_out if residual_out is not None else X
+    _check(lib().lqer_add_rms_norm(X.data_ptr(), _code(X.dtype, *_REAL), None if residual is None else residual.data_ptr(),
+                                   None if residual_out is None else residual_out.data_ptr(), _code(r.dtype, *_REAL),
+                                   weight.data_ptr(), _code(weight.dtype, *_REAL), eps, M, K, _cfg(cfg), Y.data_ptr(), y_code,
+                                   _stream_here(stream, X)), "lqer_add_rms_norm")
+    return Y, residual_out
+
+
+def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", out_dtype=MXINT8, cfg: Config | None = None,
+                     Y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """act(gate) * up ("silu", or "gelu" in its tanh form), fp32, bf16 or MXINT8.  gate and up [M, N]: dense, or views with one row
+    stride, as the halves of one [M, 2 N] tensor are."""
+    if gate.dim() != 2 or gate.shape != up.shape or gate.dtype != up.dtype or gate.get_device() != up.get_device():
+        raise ValueError("expected gate and up of one shape [M, N], type and device")
+    M, N = gate.shape
+    if N > 1 and (gate.stride(1) != 1 or up.stride(1) != 1) or M > 1 and gate.stride(0) != up.stride(0):
+        raise ValueError("expected rows of consecutive elements, with one row stride for gate and up")
+    other = _on(gate)
+    if other is not None:
+        with other:
+            return gated_activation(gate, up, act, out_dtype, cfg, Y, stream)
+    if act not in _ACTS:
+        raise ValueError(f"unknown activation {act!r}")
+    Y, y_code = _output(Y, M, N, out_dtype, gate)
+    _same(Y)
+    if Y.get_device() != gate.get_device():
+        raise ValueError("expected tensors of one device")
+    _check(lib().lqer_gated_activation(gate.data_ptr(), up.data_ptr(), _code(gate.dtype, *_REAL), gate.stride(0) if M > 1 else (N + 7) // 8 * 8, M, N, _ACTS[act],
+                                       _cfg(cfg), Y.data_ptr(), y_code, _stream_here(stream, gate)), "lqer_gated_activation")
+    return Y
+
+
+def dequantize_activations(Xq: torch.Tensor, M: int, K: int, out_dtype=torch.float32, cfg: Config | None = None,
+                           Y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """The values of a flat MXINT8 buffer of [M, K] activations (exact in fp32 and in bf16)."""
+    if Xq.dtype != torch.uint8 or K % 16 or Xq.numel() != mxint8_bytes(M, K):
+        raise ValueError("an MXINT8 tensor is a flat uint8 tensor of mxint8_bytes(M, K)")
+    other = _on(Xq)
+    if other is not None:
+        with other:
+            return dequantize_activations(Xq, M, K, out_dtype, cfg, Y, stream)
+    Y, y_code = _output(Y, M, K, _REAL[_code(out_dtype, *_REAL)], Xq)
+    _same(Xq, Y)
+    _check(lib().lqer_dequantize_activations(Xq.data_ptr(), M, K, _cfg(cfg), Y.data_ptr(), y_code, _stream_here(stream, Xq)),
+           "lqer_dequantize_activations")
+    return Y
+
+
+class AdapterPool:
+    """Places for n_slots adapters of one [K, N] projection, of ranks up to max_rank (see include/lqer.h)."""
+
+    def __init__(self, K: int, N: int, max_rank: int, n_slots: int, device):
+        self.K, self.N, self.max_rank, self.n_slots = K, N, max_rank, n_slots
+        self.handle = _Pool(None, K, N, max_rank, n_slots)
+        self.ref = C.byref(self.handle)
+        size = C.c_size_t()
+        _check(lib().lqer_adapter_pool_bytes(self.ref, C.byref(size)), "lqer_adapter_pool_bytes")
+        self.buf = torch.empty(size.value, dtype=torch.uint8, device=device)
+        self.handle.data = self.buf.data_ptr()
+
+
+def new_adapter_pool(K: int, N: int, max_rank: int, n_slots: int, device="cuda", stream=None) -> AdapterPool:
+    pool = AdapterPool(K, N, max_rank, n_slots, device)
+    with torch.cuda.device(pool.buf.device):
+        _check(lib().lqer_adapter_pool_init(pool.ref, pool.buf.numel(), _stream_here(stream, pool.buf)), "lqer_adapter_pool_init")
+    return pool
+
+
+def load_adapter(pool: AdapterPool, slot: int, A: torch.Tensor, B: torch.Tensor, scale: float = 1.0, stream=None) -> None:
+    """Puts A [K, rank] and B [rank, N] (both fp32 or both bf16; kept in bf16) into a slot of the pool."""
+    if A.dim() != 2 or B.dim() != 2 or A.shape[0] != pool.K or B.shape[1] != pool.N or A.shape[1] != B.shape[0] or A.dtype != B.dtype:
+        raise ValueError("expected A [K, rank] and B [rank, N] of one type")
+    if A.shape[1] < 1:
+        raise ValueError("an adapter has a rank of at least 1 (unload_adapter empties a slot)")
+    _same(pool.buf, A, B)
+    with torch.cuda.device(pool.buf.device):
+        _check(lib().lqer_adapter_load(pool.ref, slot, A.data_ptr(), B.data_ptr(), _code(A.dtype, *_REAL), A.shape[1], scale,
+                                       _stream_here(stream, pool.buf)), "lqer_adapter_load")
+
+
+def unload_adapter(pool: AdapterPool, slot: int, stream=None) -> None:
+    """Empties a slot: rows that name it take no adapter."""
+    with torch.cuda.device(pool.buf.device):
+        _check(lib().lqer_adapter_load(pool.ref, slot, None, None, 0, 0, 0.0, _stream_here(stream, pool.buf)), "lqer_adapter_load")
+
+
+@dataclass
+class AdapterPlan:
+    buf: torch.Tensor   # uint8 device buffer; poll_status(buf) tells of slots out of range
+    M: int
+    n_slots: int
+
+
+def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | None = None, stream=None) -> AdapterPlan:
+    """The plan of a batch: slots int32 [M], the slot of each row's adapter in the pools of this step (-1: none).  It serves every pool
+    with as many slots.  `plan`: one of the same sizes to be made again in place."""
+    if slots.dtype != torch.int32 or slots.dim() != 1:
+        raise ValueError("expected int32 slots [M]")
+    other = _on(slots)
+    if other is not None:
+        with other:
+            return adapter_plan(slots, pool, plan, stream)
+    M = slots.shape[0]
+    if plan is None:
+        size = C.c_size_t()
+        _check(lib().lqer_adapter_plan_bytes(M, pool.n_slots, C.byref(size)), "lqer_adapter_plan_bytes")
+        plan = AdapterPlan(torch.empty(size.value, dtype=torch.uint8, device=slots.device), M, pool.n_slots)
+    elif plan.M != M or plan.n_slots != pool.n_slots:
+        raise ValueError("the plan to be made again has other sizes")
+    _same(slots, plan.buf)
+    _check(lib().lqer_adapter_plan(slots.data_ptr(), M, pool.n_slots, plan.buf.data_ptr(), plan.buf.numel(), _stream_here(stream, slots)),
+           "lqer_adapter_plan")
+    return plan
+
+
+def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: torch.Tensor, Y: torch.Tensor | None = None, out_dtype=None,
+                   cfg: Config | None = None, stream=None) -> torch.Tensor:
+    """Y[m] = Y0[m] + scale (X[m] A) B with the adapter of row m.  X [M, K] fp32 or bf16, or a flat MXINT8 buffer; Y0 [M, N] fp32 or
+    bf16, the shared projection's output; Y of out_dtype (Y0's type where it is not given), or the given tensor, Y0 itself included."""
+    M = plan.M
+    if X.dtype == torch.uint8:
+        x_code, fits = 2, X.numel() == mxint8_bytes(M, pool.K)
+    else:
+        x_code, fits = _code(X.dtype, *_REAL), X.shape == (M, pool.K)
+    if not fits or Y0.shape != (M, pool.N):
+        raise ValueError("expected X of the plan's rows and the pool's K columns, and Y0 [M, N]")
+    other = _on(X)
+    if other is not None:
+        with other:
+            return apply_adapters(X, pool, plan, Y0, Y, out_dtype, cfg, stream)
+    if Y is None:
+        Y = torch.empty((M, pool.N), dtype=out_dtype or Y0.dtype, device=X.device)
+    elif Y.shape != (M, pool.N):
+        raise ValueError("expected Y [M, N]")
+    _same(X, Y0, Y, plan.buf, pool.buf)
+    _check(lib().lqer_adapters(X.data_ptr(), x_code, M, pool.ref, plan.buf.data_ptr(), plan.n_slots, Y0.data_ptr(), _code(Y0.dtype, *_REAL),
+                               Y.data_ptr(), _code(Y.dtype, *_REAL), _cfg(cfg), _stream_here(stream, X)), "lqer_adapters")
+    return Y
 
 
 def poll_status(ws: torch.Tensor, stream=None) -> int:

@@ -74,7 +74,7 @@ int sm_count() {
 static bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 static size_t align_up(size_t v, size_t a) { return (v + a - 1) / a * a; }
 
-static lqer_status_t check_config(const lqer_config_t* cfg) {
+lqer_status_t check_config(const lqer_config_t* cfg) {
   if (cfg == nullptr) return LQER_ERR_NULL;
   // activations (and T) take 3 to 8 mantissa bits (Section 4.3 compares W4A8 and W4A6); weights 4 or 2 (Section 4.4: W2A8)
   if ((cfg->w_bits != 4 && cfg->w_bits != 2) || cfg->a_bits < 3 || cfg->a_bits > 8 || cfg->lr_bits != 8 || cfg->block != 16) return LQER_ERR_CONFIG;
@@ -144,7 +144,7 @@ static lqer_status_t lookup(const void* packed, PackedMeta& out) {
   return LQER_OK;
 }
 
-static lqer_status_t check_arch() {
+lqer_status_t check_arch() {
   static std::mutex mu;
   static std::unordered_map<int, int> major_of;
   int dev = 0;

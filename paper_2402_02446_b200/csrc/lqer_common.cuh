@@ -615,4 +615,25 @@ int decode_pre_max_calls();
 cudaError_t launch_decode_pre(const lqer_call_t* calls, const PackedMeta* metas, uint8_t* const* outs, int n, int order,
                               int x_type, cudaStream_t s);
 
+// Between the layers (lqer_boundary.cu): types as kX* / kY*; bits, emin, emax: the format of an MXINT8 tensor.
+cudaError_t launch_add_rms_norm(const void* X, int x_type, const void* res, void* res_out, int r_type, const void* w, int w_type, double eps,
+                                int M, int K, int bits, int emin, int emax, void* Y, int y_type, cudaStream_t s);
+cudaError_t launch_gated_activation(const void* gate, const void* up, int x_type, size_t ld, int M, int N, int act, int bits, int emin,
+                                    int emax, void* Y, int y_type, cudaStream_t s);
+cudaError_t launch_dequantize(const void* Xq, int M, int K, int bits, int emin, int emax, void* Y, int y_type, cudaStream_t s);
+// Adapters of many requests (lqer_adapters.cu).
+constexpr int kAdapterMaxRank = 256, kAdapterMaxSlots = 1024;
+size_t adapter_slot_bytes(int K, int N, int max_rank);
+size_t adapter_plan_bytes(int M, int n_slots);
+cudaError_t launch_adapter_pool_init(void* pool, int K, int N, int max_rank, int n_slots, cudaStream_t s);
+cudaError_t launch_adapter_load(void* pool, int K, int N, int max_rank, int slot, const void* A, const void* B, bool bf16, int rank, float scale,
+                                cudaStream_t s);
+cudaError_t launch_adapter_plan(const int* slots, int M, int n_slots, void* plan, cudaStream_t s);
+cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, int K, int N, int max_rank, void* plan, int plan_slots,
+                            const void* Y0, int y0_type, void* Y, int y_type, int bits, int emin, int emax, cudaStream_t s);
+
+// Argument checks shared by the entry points (lqer_api.cu).
+lqer_status_t check_config(const lqer_config_t* cfg);
+lqer_status_t check_arch();
+
 }  // namespace lqer
