@@ -296,7 +296,7 @@ lqer_status_t lqer_poll_status(const void* workspace, void* stream, lqer_status_
 /* ---- Between the layers ----
  * What a program that serves a model needs at the layers' boundary, with the same element types: the norm in front of a layer, the
  * gated activation in front of a down projection, and the adapters of many requests beside a shared projection.
- * All are asynchronous on `stream`, need no workspace and allocate nothing; pointers belong to the current device and are 16-byte
+ * All are asynchronous on `stream` and allocate nothing; pointers belong to the current device and are 16-byte
  * aligned (16-bit and 32-bit tensors alike).  An MXINT8 tensor [M,K] is M*K mantissas followed by M*K/16 exponent bytes, in the
  * format (a_bits, exp_min, exp_max) of `cfg`; cfg may be NULL for the defaults.  M is at most 2^24. */
 
@@ -355,10 +355,15 @@ lqer_status_t lqer_adapter_plan(const int* slots, int M, int n_slots, void* plan
  * buffer is only read, but for its status: a plan of another batch size (or none), or a slot that no lqer_adapter_load
  * or lqer_adapter_pool_init of this pool's shape wrote, is reported there as LQER_ERR_BAD_PACKED, and such rows are not written or
  * take no adapter.  Rows of an empty slot take none.  K % 16 == 0, N % 8 == 0.  fp32 accumulation; fp32 X and X A are kept to
- * 24 bits for fp32 Y and to 16 bits for bf16 Y.  A row's result does not depend on the other rows; its last
- * bits may depend on M. */
+ * 24 bits for fp32 Y and to 16 bits for bf16 Y.  Up to 512 rows are one launch, and a row's result does not depend on the other rows'
+ * values; more are two, with X A in between in `workspace` (lqer_adapters_workspace_bytes, 256-byte aligned; 0 bytes up to 512
+ * rows, and the workspace may then be NULL; nothing in it has to be kept or cleared between calls, and calls that overlap need one
+ * each).  The sums are taken in an order that M, the plan and the pool's shape decide, so a row's last bits may depend on
+ * them.  A bounded wait that ran out is reported in the plan as LQER_ERR_TIMEOUT. */
+lqer_status_t lqer_adapters_workspace_bytes(int M, const lqer_adapter_pool_t* pool, int plan_slots, size_t* bytes);
 lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lqer_adapter_pool_t* pool, void* plan, int plan_slots,
-                            const void* Y0, lqer_dtype_t y0_dtype, void* Y, lqer_dtype_t y_dtype, const lqer_config_t* cfg, void* stream);
+                            const void* Y0, lqer_dtype_t y0_dtype, void* Y, lqer_dtype_t y_dtype, const lqer_config_t* cfg, void* workspace,
+                            size_t workspace_bytes, void* stream);
 
 /* Force a kernel path for tests: 0 auto (which alone runs the cluster kernel for 3 to 16 rows), 1 plain CUDA-core
  * reference kernel, 2 small-batch kernels

@@ -106,7 +106,8 @@ def lib() -> C.CDLL:
             "lqer_adapter_load": (i, [C.POINTER(_Pool), i, vp, vp, i, i, C.c_float, vp]),
             "lqer_adapter_plan_bytes": (i, [i, i, C.POINTER(sz)]),
             "lqer_adapter_plan": (i, [vp, i, i, vp, sz, vp]),
-            "lqer_adapters": (i, [vp, i, i, C.POINTER(_Pool), vp, i, vp, i, vp, i, cfgp, vp]),
+            "lqer_adapters_workspace_bytes": (i, [i, C.POINTER(_Pool), i, C.POINTER(sz)]),
+            "lqer_adapters": (i, [vp, i, i, C.POINTER(_Pool), vp, i, vp, i, vp, i, cfgp, vp, sz, vp]),
             "lqer_workspace_init": (i, [vp, sz, vp]),
             "lqer_poll_status": (i, [vp, vp, C.POINTER(i)]),
             "lqer_set_path": (i, [i]),
@@ -422,62 +423,57 @@ def linear_host_batched_ex(calls, ws: torch.Tensor, x_dtype, y_dtype, stream=Non
 
 
 # ---- between the layers ----------------------------------------------------------------------------------------------------
-# One small kernel a call: what Python adds in front of the launch counts, so these take the raw stream and one check a tensor.
+# One small kernel a call: what Python adds in front of the launch counts, so these look at a tensor once, take the raw stream,
+# and enter a device only where it is not the current one.
 
-def _raw_stream(stream, index: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(index) if stream is None else stream.cuda_stream
-
-
-def _on(t: torch.Tensor):
-    """The device of t, current while the call runs, if it is another than the current one."""
-    index = t.get_device()
-    if index < 0:
-        raise ValueError("expected CUDA tensors")
-    return None if index == torch.cuda.current_device() else torch.cuda.device(index)
-
-
-def _same(first: torch.Tensor, *others) -> None:
-    """All on the first one's device, dense (None is skipped)."""
-    index = first.get_device()
-    for t in (first, *others):
-        if t is not None and (t.get_device() != index or not t.is_contiguous()):
-            raise ValueError("expected contiguous CUDA tensors of one device")
-
-
-def _stream_here(stream, t: torch.Tensor) -> int:
-    if stream is not None and stream.device != t.device:
-        raise ValueError("the stream belongs to another device than the tensors")
-    return _raw_stream(stream, t.get_device())
-
-
-def _cfg(cfg):
-    return None if cfg is None else C.byref(cfg)
-
-
-def _code(dt, *allowed) -> int:
-    if dt not in allowed:
-        raise ValueError(f"unsupported dtype {dt}")
-    return _DTYPES[dt]
-
-
-_REAL = (torch.float32, torch.bfloat16)
+_REAL_CODE = {torch.float32: 0, torch.bfloat16: 1}
+_OUT_CODE = {torch.float32: 0, torch.bfloat16: 1, MXINT8: 2, torch.uint8: 2}
 _ACTS = {"silu": 0, "gelu": 1}
 
 
-def _output(Y, rows: int, cols: int, out_dtype, like: torch.Tensor):
-    """The tensor of a [rows, cols] result of out_dtype, made where none is given, and its type's code."""
-    if Y is not None and Y.dtype != torch.uint8:
-        out_dtype = Y.dtype
-    elif Y is not None:
-        out_dtype = MXINT8
-    code = _code(out_dtype, *_REAL, MXINT8)
-    shape = (mxint8_bytes(rows, cols),) if out_dtype == MXINT8 else (rows, cols)
-    if out_dtype == MXINT8 and cols % 16:
-        raise ValueError("an MXINT8 output has whole blocks of 16 columns")
-    if Y is None:
-        Y = torch.empty(shape, dtype=_tensor_dtype(out_dtype), device=like.device)
-    elif tuple(Y.shape) != shape:
-        raise ValueError(f"expected an output of shape {shape}")
+def _here(index: int) -> bool:
+    """Whether the device of a call's first tensor is the current one."""
+    if index < 0:
+        raise ValueError("expected CUDA tensors")
+    return index == torch._C._cuda_getDevice()
+
+
+def _ptr(t: torch.Tensor, index: int) -> int:
+    """The address of a dense tensor on that device."""
+    if t.get_device() != index or not t.is_contiguous():
+        raise ValueError("expected contiguous CUDA tensors of one device")
+    return t.data_ptr()
+
+
+def _raw_stream(stream, index: int) -> int:
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(index)
+    if stream.device.index != index:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return stream.cuda_stream
+
+
+def _code(codes, dt) -> int:
+    c = codes.get(dt)
+    if c is None:
+        raise ValueError(f"unsupported dtype {dt}")
+    return c
+
+
+def _output(Y, M: int, N: int, out_dtype, like: torch.Tensor):
+    """The tensor of an [M, N] result (made where none is given; its type goes before out_dtype) and its type's code."""
+    code = _code(_OUT_CODE, out_dtype if Y is None else Y.dtype)
+    if code == 2:
+        if N % 16:
+            raise ValueError("an MXINT8 output has whole blocks of 16 columns")
+        if Y is None:
+            return like.new_empty(mxint8_bytes(M, N), dtype=torch.uint8), code
+        if Y.dim() != 1 or Y.shape[0] != mxint8_bytes(M, N):
+            raise ValueError("an MXINT8 output is a flat uint8 tensor of mxint8_bytes(M, N)")
+    elif Y is None:
+        return like.new_empty((M, N), dtype=out_dtype), code
+    elif Y.shape != (M, N):
+        raise ValueError(f"expected an output of shape {(M, N)}")
     return Y, code
 
 
@@ -488,27 +484,31 @@ def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: to
     X [M, K] and residual [M, K] fp32 or bf16, weight [K]; Y of out_dtype (fp32, bf16 or MXINT8).  Without a residual h is X, and
     is only written where residual_out is given (None is returned otherwise); with one it goes to residual_out (which may be
     the residual itself) or to a new tensor."""
-    if X.dim() != 2 or weight.dim() != 1 or weight.shape[0] != X.shape[1]:
-        raise ValueError("expected X [M, K] and weight [K]")
-    M, K = X.shape
-    for t in (residual, residual_out):
-        if t is not None and t.shape != X.shape:
-            raise ValueError("the residual has X's shape")
-    if residual is not None and residual_out is not None and residual.dtype != residual_out.dtype:
-        raise ValueError("residual and residual_out are of one type")
-    other = _on(X)
-    if other is not None:
-        with other:
+    index = X.get_device()
+    if not _here(index):
+        with torch.cuda.device(index):
             return add_rms_norm(X, weight, eps, residual, out_dtype, cfg, residual_out, Y, stream)
+    shape = X.shape
+    if len(shape) != 2 or weight.shape != shape[1:]:
+        raise ValueError("expected X [M, K] and weight [K]")
+    M, K = shape
+    r_ptr = h_ptr = None
+    r_code = x_code = _code(_REAL_CODE, X.dtype)
+    if residual is not None:
+        if residual.shape != shape:
+            raise ValueError("the residual has X's shape")
+        r_ptr, r_code = _ptr(residual, index), _code(_REAL_CODE, residual.dtype)
+        if residual_out is None:
+            residual_out = torch.empty_like(residual)
+    if residual_out is not None:
+        if residual_out.shape != shape or residual is not None and residual_out.dtype != residual.dtype:
+            raise ValueError("residual_out has X's shape and the residual's type")
+        h_ptr, r_code = _ptr(residual_out, index), _code(_REAL_CODE, residual_out.dtype)
     Y, y_code = _output(Y, M, K, out_dtype, X)
-    if residual is not None and residual_out is None:
-        residual_out = torch.empty_like(residual)
-    _same(X, weight, residual, residual_out, Y)
-    r = residual_out if residual_out is not None else X
-    _check(lib().lqer_add_rms_norm(X.data_ptr(), _code(X.dtype, *_REAL), None if residual is None else residual.data_ptr(),
-                                   None if residual_out is None else residual_out.data_ptr(), _code(r.dtype, *_REAL),
-                                   weight.data_ptr(), _code(weight.dtype, *_REAL), eps, M, K, _cfg(cfg), Y.data_ptr(), y_code,
-                                   _stream_here(stream, X)), "lqer_add_rms_norm")
+    status = lib().lqer_add_rms_norm(_ptr(X, index), x_code, r_ptr, h_ptr, r_code, _ptr(weight, index), _code(_REAL_CODE, weight.dtype), eps, M, K,
+                                     None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code, _raw_stream(stream, index))
+    if status:
+        raise LqerError(status, "lqer_add_rms_norm")
     return Y, residual_out
 
 
@@ -516,39 +516,41 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", ou
                      Y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """act(gate) * up ("silu", or "gelu" in its tanh form), fp32, bf16 or MXINT8.  gate and up [M, N]: dense, or views with one row
     stride, as the halves of one [M, 2 N] tensor are."""
-    if gate.dim() != 2 or gate.shape != up.shape or gate.dtype != up.dtype or gate.get_device() != up.get_device():
-        raise ValueError("expected gate and up of one shape [M, N], type and device")
-    M, N = gate.shape
-    if N > 1 and (gate.stride(1) != 1 or up.stride(1) != 1) or M > 1 and gate.stride(0) != up.stride(0):
-        raise ValueError("expected rows of consecutive elements, with one row stride for gate and up")
-    other = _on(gate)
-    if other is not None:
-        with other:
+    index = gate.get_device()
+    if not _here(index):
+        with torch.cuda.device(index):
             return gated_activation(gate, up, act, out_dtype, cfg, Y, stream)
+    shape = gate.shape
+    if len(shape) != 2 or up.shape != shape or up.dtype != gate.dtype or up.get_device() != index:
+        raise ValueError("expected gate and up of one shape [M, N], type and device")
+    M, N = shape
+    ld, one = gate.stride()
+    if N > 1 and one != 1 or up.stride() != (ld, one):
+        raise ValueError("expected rows of consecutive elements, with one row stride for gate and up")
     if act not in _ACTS:
         raise ValueError(f"unknown activation {act!r}")
     Y, y_code = _output(Y, M, N, out_dtype, gate)
-    _same(Y)
-    if Y.get_device() != gate.get_device():
-        raise ValueError("expected tensors of one device")
-    _check(lib().lqer_gated_activation(gate.data_ptr(), up.data_ptr(), _code(gate.dtype, *_REAL), gate.stride(0) if M > 1 else (N + 7) // 8 * 8, M, N, _ACTS[act],
-                                       _cfg(cfg), Y.data_ptr(), y_code, _stream_here(stream, gate)), "lqer_gated_activation")
+    status = lib().lqer_gated_activation(gate.data_ptr(), up.data_ptr(), _code(_REAL_CODE, gate.dtype), ld if M > 1 else N, M, N, _ACTS[act],
+                                         None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code, _raw_stream(stream, index))
+    if status:
+        raise LqerError(status, "lqer_gated_activation")
     return Y
 
 
 def dequantize_activations(Xq: torch.Tensor, M: int, K: int, out_dtype=torch.float32, cfg: Config | None = None,
                            Y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The values of a flat MXINT8 buffer of [M, K] activations (exact in fp32 and in bf16)."""
+    index = Xq.get_device()
+    if not _here(index):
+        with torch.cuda.device(index):
+            return dequantize_activations(Xq, M, K, out_dtype, cfg, Y, stream)
     if Xq.dtype != torch.uint8 or K % 16 or Xq.numel() != mxint8_bytes(M, K):
         raise ValueError("an MXINT8 tensor is a flat uint8 tensor of mxint8_bytes(M, K)")
-    other = _on(Xq)
-    if other is not None:
-        with other:
-            return dequantize_activations(Xq, M, K, out_dtype, cfg, Y, stream)
-    Y, y_code = _output(Y, M, K, _REAL[_code(out_dtype, *_REAL)], Xq)
-    _same(Xq, Y)
-    _check(lib().lqer_dequantize_activations(Xq.data_ptr(), M, K, _cfg(cfg), Y.data_ptr(), y_code, _stream_here(stream, Xq)),
-           "lqer_dequantize_activations")
+    Y, y_code = _output(Y, M, K, out_dtype, Xq)
+    status = lib().lqer_dequantize_activations(_ptr(Xq, index), M, K, None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code,
+                                               _raw_stream(stream, index))
+    if status:
+        raise LqerError(status, "lqer_dequantize_activations")
     return Y
 
 
@@ -568,7 +570,7 @@ class AdapterPool:
 def new_adapter_pool(K: int, N: int, max_rank: int, n_slots: int, device="cuda", stream=None) -> AdapterPool:
     pool = AdapterPool(K, N, max_rank, n_slots, device)
     with torch.cuda.device(pool.buf.device):
-        _check(lib().lqer_adapter_pool_init(pool.ref, pool.buf.numel(), _stream_here(stream, pool.buf)), "lqer_adapter_pool_init")
+        _check(lib().lqer_adapter_pool_init(pool.ref, pool.buf.numel(), _raw_stream(stream, pool.buf.get_device())), "lqer_adapter_pool_init")
     return pool
 
 
@@ -578,16 +580,17 @@ def load_adapter(pool: AdapterPool, slot: int, A: torch.Tensor, B: torch.Tensor,
         raise ValueError("expected A [K, rank] and B [rank, N] of one type")
     if A.shape[1] < 1:
         raise ValueError("an adapter has a rank of at least 1 (unload_adapter empties a slot)")
-    _same(pool.buf, A, B)
-    with torch.cuda.device(pool.buf.device):
-        _check(lib().lqer_adapter_load(pool.ref, slot, A.data_ptr(), B.data_ptr(), _code(A.dtype, *_REAL), A.shape[1], scale,
-                                       _stream_here(stream, pool.buf)), "lqer_adapter_load")
+    index = pool.buf.get_device()
+    with torch.cuda.device(index):
+        _check(lib().lqer_adapter_load(pool.ref, slot, _ptr(A, index), _ptr(B, index), _code(_REAL_CODE, A.dtype), A.shape[1], scale,
+                                       _raw_stream(stream, index)), "lqer_adapter_load")
 
 
 def unload_adapter(pool: AdapterPool, slot: int, stream=None) -> None:
     """Empties a slot: rows that name it take no adapter."""
-    with torch.cuda.device(pool.buf.device):
-        _check(lib().lqer_adapter_load(pool.ref, slot, None, None, 0, 0, 0.0, _stream_here(stream, pool.buf)), "lqer_adapter_load")
+    index = pool.buf.get_device()
+    with torch.cuda.device(index):
+        _check(lib().lqer_adapter_load(pool.ref, slot, None, None, 0, 0, 0.0, _raw_stream(stream, index)), "lqer_adapter_load")
 
 
 @dataclass
@@ -600,12 +603,12 @@ class AdapterPlan:
 def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | None = None, stream=None) -> AdapterPlan:
     """The plan of a batch: slots int32 [M], the slot of each row's adapter in the pools of this step (-1: none).  It serves every pool
     with as many slots.  `plan`: one of the same sizes to be made again in place."""
+    index = slots.get_device()
+    if not _here(index):
+        with torch.cuda.device(index):
+            return adapter_plan(slots, pool, plan, stream)
     if slots.dtype != torch.int32 or slots.dim() != 1:
         raise ValueError("expected int32 slots [M]")
-    other = _on(slots)
-    if other is not None:
-        with other:
-            return adapter_plan(slots, pool, plan, stream)
     M = slots.shape[0]
     if plan is None:
         size = C.c_size_t()
@@ -613,34 +616,43 @@ def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | Non
         plan = AdapterPlan(torch.empty(size.value, dtype=torch.uint8, device=slots.device), M, pool.n_slots)
     elif plan.M != M or plan.n_slots != pool.n_slots:
         raise ValueError("the plan to be made again has other sizes")
-    _same(slots, plan.buf)
-    _check(lib().lqer_adapter_plan(slots.data_ptr(), M, pool.n_slots, plan.buf.data_ptr(), plan.buf.numel(), _stream_here(stream, slots)),
+    _check(lib().lqer_adapter_plan(_ptr(slots, index), M, pool.n_slots, _ptr(plan.buf, index), plan.buf.numel(), _raw_stream(stream, index)),
            "lqer_adapter_plan")
     return plan
 
 
+def adapters_workspace_bytes(M: int, pool: AdapterPool, plan_slots: int | None = None) -> int:
+    """The workspace that apply_adapters needs for M rows: nothing up to 512."""
+    out = C.c_size_t()
+    _check(lib().lqer_adapters_workspace_bytes(M, pool.ref, plan_slots or pool.n_slots, C.byref(out)), "lqer_adapters_workspace_bytes")
+    return out.value
+
+
 def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: torch.Tensor, Y: torch.Tensor | None = None, out_dtype=None,
-                   cfg: Config | None = None, stream=None) -> torch.Tensor:
+                   cfg: Config | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Y[m] = Y0[m] + scale (X[m] A) B with the adapter of row m.  X [M, K] fp32 or bf16, or a flat MXINT8 buffer; Y0 [M, N] fp32 or
-    bf16, the shared projection's output; Y of out_dtype (Y0's type where it is not given), or the given tensor, Y0 itself included."""
-    M = plan.M
-    if X.dtype == torch.uint8:
-        x_code, fits = 2, X.numel() == mxint8_bytes(M, pool.K)
-    else:
-        x_code, fits = _code(X.dtype, *_REAL), X.shape == (M, pool.K)
-    if not fits or Y0.shape != (M, pool.N):
+    bf16, the shared projection's output; Y of out_dtype (Y0's type where it is not given), or the given tensor, Y0 itself included.
+    ws: a workspace of adapters_workspace_bytes (more than 512 rows need one; made where none is given)."""
+    index = X.get_device()
+    if not _here(index):
+        with torch.cuda.device(index):
+            return apply_adapters(X, pool, plan, Y0, Y, out_dtype, cfg, ws, stream)
+    M, K, N = plan.M, pool.K, pool.N
+    x_code = _code(_OUT_CODE, X.dtype)
+    if X.shape != ((mxint8_bytes(M, K),) if x_code == 2 else (M, K)) or Y0.shape != (M, N):
         raise ValueError("expected X of the plan's rows and the pool's K columns, and Y0 [M, N]")
-    other = _on(X)
-    if other is not None:
-        with other:
-            return apply_adapters(X, pool, plan, Y0, Y, out_dtype, cfg, stream)
     if Y is None:
-        Y = torch.empty((M, pool.N), dtype=out_dtype or Y0.dtype, device=X.device)
-    elif Y.shape != (M, pool.N):
+        Y = torch.empty_like(Y0) if out_dtype is None or out_dtype == Y0.dtype else Y0.new_empty((M, N), dtype=out_dtype)
+    elif Y.shape != (M, N):
         raise ValueError("expected Y [M, N]")
-    _same(X, Y0, Y, plan.buf, pool.buf)
-    _check(lib().lqer_adapters(X.data_ptr(), x_code, M, pool.ref, plan.buf.data_ptr(), plan.n_slots, Y0.data_ptr(), _code(Y0.dtype, *_REAL),
-                               Y.data_ptr(), _code(Y.dtype, *_REAL), _cfg(cfg), _stream_here(stream, X)), "lqer_adapters")
+    _ptr(pool.buf, index)
+    if ws is None and M > 512:
+        ws = X.new_empty(adapters_workspace_bytes(M, pool, plan.n_slots), dtype=torch.uint8)
+    status = lib().lqer_adapters(_ptr(X, index), x_code, M, pool.ref, _ptr(plan.buf, index), plan.n_slots, _ptr(Y0, index), _code(_REAL_CODE, Y0.dtype),
+                                 _ptr(Y, index), _code(_REAL_CODE, Y.dtype), None if cfg is None else C.byref(cfg),
+                                 None if ws is None else _ptr(ws, index), 0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(stream, index))
+    if status:
+        raise LqerError(status, "lqer_adapters")
     return Y
 
 

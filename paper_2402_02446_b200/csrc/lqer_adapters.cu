@@ -2,49 +2,34 @@
 //   Y[m] = Y0[m] + scale_a (X[m] A_a) B_a,   a = the slot of row m (none: Y[m] = Y0[m]).
 // The same kind of term as the layer's own (X A_k) B_k (paper Section 3.1), with factors that differ from row to row.
 //
-// Pool: n_slots places of one size for adapters of a [K, N] projection up to max_rank, bf16 in the order in which mma.sync takes
-// its B fragments, so that a lane reads 16 bytes per fragment pair and a warp 512 consecutive bytes:
-//   A: [K / 32][rank / 8][lane][8]      lane (g, t) = (lane / 4, lane % 4): element i is A[32 kb + 8 t + i][8 n + g]
-//   B: [N / 32][rank / 16][2][lane][8]  element 4 jj + i of half h is B[16 s + 4 t + i][32 nb + 8 (g / 2) + 2 (2 h + jj) + g % 2]
-// The contraction index may be dealt to the MMA's K positions in any order as long as both operands agree, and the
-// output columns to its N positions: dealt like this a lane's activations are 8 consecutive elements of a row, and its
-// outputs 8 consecutive columns, so that X, Y0 and Y go between memory and registers in 16-byte pieces without shared memory.
+// Pool: n_slots places of one size for adapters of a [K, N] projection up to max_rank, bf16, both factors with the contraction index
+// innermost, in the images that the tensor cores read from shared memory (128-byte swizzle: the 16-byte pieces of a row change
+// places by the row's index):
+//   A: [K / 64][rank, padded to 16] rows of 64 K
+//   B: [N / 128][rank / 64][128 columns] rows of 64 ranks (32 or 16 where max_rank is no more: rows of 64 or 32 bytes); column
+//      8 t + 2 j + i of 32 is row 8 j + 2 t + i: of an accumulator's columns, which a lane holds in pairs, it then has 8 neighbours
+// They are read as they lie: by bulk copies for the tcgen05 kernels, and for mma.sync in 16-byte pieces, a lane's eight consecutive
+// elements being its share of two MMA steps (the contraction index may be dealt to the MMA's K positions in any order as long as
+// both operands agree).
 //
 // Plan: the rows sorted by slot (stable) and cut into tiles of at most tile_rows rows of one slot.  It belongs to a batch, not to a
 // layer: a step of a model makes it once and uses it for every projection.
 //
-// A cluster of CTAs takes one tile.  First the CTAs share the contraction over K (each warp 16 rows), then they add up their
-// partial T through distributed shared memory, and then they share the columns of Y.  X, A, B, Y0 and Y are touched once by a
-// tile; T never leaves the chip.  The sums are taken in a fixed order.
+// Few rows (up to 512, few_rows_kernel): a cluster of CTAs takes a tile of up to 8 rows.  The factors are the MMA's 16-row operand, the tokens its 8
+// columns.  First the CTAs share the contraction over K, then each sends its part of T to all (distributed shared memory),
+// and then they share the columns of Y.  T never leaves the chip, and everything is summed in a fixed order.
+// Many rows: lqer_adapters_many.cu.
 //
 // Precision: A, B and MXINT8 or bf16 X are exact in bf16.  fp32 X and T enter the tensor cores as sums of bf16 parts, cut off
 // rather than rounded (no part can overflow): three parts hold all 24 bits, two parts 16 bits (2^-16, against 2^-9 for the
-// bf16 result they are used for).
-#include "lqer_tc_ptx.cuh"
+// bf16 result they are used for).  The tensor cores cut a running sum off where it does not fit, so their chains are kept short - a
+// block of 32 of K, lower parts first - and added up by ordinary fp32 additions.
+#include "lqer_adapters.cuh"
 
 namespace lqer {
 namespace ad {
 
 constexpr int kThreads = 256, kWarps = 8;
-constexpr uint32_t kPoolMagic = 0x4C4F5241u, kPlanMagic = 0x4E414C50u;
-constexpr int kMaxCluster = 8;
-
-struct SlotHead {            // first 32 bytes of a slot
-  uint32_t magic;
-  int K, N, max_rank;
-  int rank;                  // 0: empty
-  float scale;
-  int reserved[2];
-};
-struct PlanHead {            // first 256 bytes of a plan
-  DeviceStatus status;
-  uint32_t magic;
-  int M, n_slots, tile_rows, n_tiles;
-};
-struct Tile { int slot, first, rows, reserved; };
-
-__host__ __device__ inline size_t a_bytes(int K, int rank) { return (size_t)((K + 31) / 32) * ((rank + 7) / 8) * 512; }
-__host__ __device__ inline size_t b_bytes(int N, int rank) { return (size_t)((N + 31) / 32) * ((rank + 15) / 16) * 1024; }
 
 // ---------------------------------------------------------------------------- pool
 __global__ void pool_init_kernel(uint8_t* pool, size_t slot_bytes, int n_slots, int K, int N, int max_rank) {
@@ -61,20 +46,21 @@ __device__ __forceinline__ uint16_t to_bf16(const void* p, bool bf16, size_t i) 
 __global__ void adapter_load_kernel(uint8_t* slot, const void* A, const void* B, bool bf16, int K, int N, int max_rank, int rank, float scale) {
   const size_t stride = (size_t)gridDim.x * blockDim.x, first = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (first == 0) *reinterpret_cast<SlotHead*>(slot) = SlotHead{kPoolMagic, K, N, max_rank, rank, scale, {0, 0}};
-  uint16_t* pa = reinterpret_cast<uint16_t*>(slot + 256);
-  uint16_t* pb = reinterpret_cast<uint16_t*>(slot + 256 + a_bytes(K, max_rank));
-  const int r8 = (rank + 7) / 8, r16 = (rank + 15) / 16;
-  for (size_t e = first; e < a_bytes(K, rank) / 2; e += stride) {
-    const int i = e & 7, lane = (e >> 3) & 31;
-    const size_t blk = e >> 8;
-    const int k = (int)(blk / r8) * 32 + (lane & 3) * 8 + i, r = (int)(blk % r8) * 8 + (lane >> 2);
-    pa[e] = k < K && r < rank ? to_bf16(A, bf16, (size_t)k * rank + r) : (uint16_t)0;
+  uint8_t* pa = slot + 256;
+  uint8_t* pb = slot + 256 + a_bytes(K, max_rank);
+  const int rows = rank16(rank) * 16, pitch = b_pitch(max_rank), wide = pitch / 2, slabs = (rank + 63) / 64;
+  // a thread writes one element; consecutive threads read consecutive ones of A's and B's rows
+  const size_t na = (size_t)((K + 63) / 64) * 64 * rows;
+  for (size_t e = first; e < na; e += stride) {
+    const int r = (int)(e % rows), k = (int)(e / rows);
+    const uint16_t v = k < K && r < rank ? to_bf16(A, bf16, (size_t)k * rank + r) : (uint16_t)0;
+    *reinterpret_cast<uint16_t*>(pa + (size_t)(k / 64) * rows * 128 + swizzled(r, (k % 64) / 8, 128) + (k % 8) * 2) = v;
   }
-  for (size_t e = first; e < b_bytes(N, rank) / 2; e += stride) {
-    const int i = e & 3, jj = (e >> 2) & 1, lane = (e >> 3) & 31, h = (e >> 8) & 1, g = lane >> 2;
-    const size_t blk = e >> 9;
-    const int r = (int)(blk % r16) * 16 + (lane & 3) * 4 + i, n = (int)(blk / r16) * 32 + (g >> 1) * 8 + 2 * (2 * h + jj) + (g & 1);
-    pb[e] = n < N && r < rank ? to_bf16(B, bf16, (size_t)r * N + n) : (uint16_t)0;
+  const size_t cols = (size_t)((N + 127) / 128) * 128, nb = cols * slabs * wide;
+  for (size_t e = first; e < nb; e += stride) {
+    const int n = (int)(e % cols), r = (int)(e / cols);
+    const uint16_t v = n < N && r < rank ? to_bf16(B, bf16, (size_t)r * N + n) : (uint16_t)0;
+    *reinterpret_cast<uint16_t*>(pb + ((size_t)(n / 128) * slabs + r / wide) * 128 * pitch + swizzled(image_row(n % 128), (r % wide) / 8, pitch) + (r % 8) * 2) = v;
   }
 }
 
@@ -82,9 +68,10 @@ __global__ void adapter_load_kernel(uint8_t* slot, const void* A, const void* B,
 // One CTA: a stable counting sort of the rows by slot (key n_slots: no adapter), then the tiles.  Each warp counts and places
 // a stretch of rows of its own, with cursors of its own, so that only the prefix sums in between go over the whole CTA.
 constexpr int kPlanThreads = 1024, kPlanWarps = 32;
+// rows: tile_rows entries a tile, the rows of the batch; places behind a tile's last row name that row again.
 __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restrict__ slots, int M, int n_slots, int tile_rows, PlanHead* head,
-                                                            Tile* tiles, int* order) {
-  extern __shared__ int cursors[];                     // [bins][32 warps], then [bins + 1] tiles before a bin
+                                                            Tile* tiles, int* rows) {
+  extern __shared__ int cursors[];                     // [bins][32 warps], then [bins + 1] tiles before a bin and [bins] rows before it
   const int bins = n_slots + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   int* tile_at = cursors + bins * kPlanWarps;
   __shared__ int bad, sums[kPlanWarps];
@@ -137,337 +124,305 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restric
   int t0 = scan(mine_t);
   for (int b = bfrom; b < bto; ++b) {
     tile_at[b] = t0;
-    const int rows = rows_of(b), first = cursors[b * kPlanWarps];
-    for (int r = 0; r < rows; r += tile_rows) tiles[t0++] = Tile{b < n_slots ? b : -1, first + r, min(tile_rows, rows - r), 0};
+    const int n_rows = rows_of(b);
+    for (int r = 0; r < n_rows; r += tile_rows) tiles[t0++] = Tile{b < n_slots ? b : -1, min(tile_rows, n_rows - r)};
   }
   if (bto == bins && bfrom < bins) tile_at[bins] = t0;
+  int* first_of = tile_at + bins + 1;                  // a bin's first place in the order
+  for (int b = bfrom; b < bto; ++b) first_of[b] = cursors[b * kPlanWarps];
   __syncthreads();
-  if (tid == 0) *head = PlanHead{DeviceStatus{bad ? (int)LQER_ERR_BOUNDS : 0, 801, 0, 0}, kPlanMagic, M, n_slots, tile_rows, tile_at[bins]};
+  if (tid == 0) *head = PlanHead{DeviceStatus{bad ? (int)LQER_ERR_BOUNDS : 0, 801, 0, 0}, kPlanMagic, M, n_slots, tile_rows, tile_at[bins], tile_at[n_slots]};
   for (int at = lo; at < hi; at += 32) {
     const int row = at + lane, key = row < hi ? key_of(row) : -1;
     const unsigned same = __match_any_sync(0xFFFFFFFFu, key);
-    if (key >= 0) order[cursors[key * kPlanWarps + warp] + __popc(same & ((1u << lane) - 1u))] = row;
+    if (key >= 0) {
+      const int place = cursors[key * kPlanWarps + warp] + __popc(same & ((1u << lane) - 1u)) - first_of[key];
+      const int end = (key + 1 < bins ? first_of[key + 1] : M) - first_of[key];
+      int* at_tile = rows + ((size_t)tile_at[key] + place / tile_rows) * tile_rows;
+      at_tile[place % tile_rows] = row;
+      if (place + 1 == end)
+        for (int i = place % tile_rows + 1; i < tile_rows; ++i) at_tile[i] = row;
+    }
     __syncwarp();
     if (key >= 0 && lane == __ffs(same) - 1) cursors[key * kPlanWarps + warp] += __popc(same);
     __syncwarp();
   }
 }
 
-// ---------------------------------------------------------------------------- the operator
-struct Params {
-  const void* X;
-  const uint8_t* pool;
-  PlanHead* plan;
-  const Tile* tiles;
-  const int* order;
-  const void* Y0;
-  void* Y;
-  size_t slot_bytes;
-  int M, K, N, max_rank, plan_slots, tile_rows;
-  int y0_bf16, y_bf16;
-  int bits, emin, emax;      // format of an MXINT8 X
-  size_t y_extent;
-};
-
-// Floats from one row of partial sums to the next: the rows g of a fragment's stores lie 8 banks apart.
-__host__ __device__ inline int part_stride(int max_rank) { return ((max_rank + 15) & ~15) + 8; }
-
-__device__ __forceinline__ uint4 ld16(const void* p) { return __ldg(static_cast<const uint4*>(p)); }
-__device__ __forceinline__ uint4 ld16_once(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ void mma(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
+// ---------------------------------------------------------------------------- few rows
+__device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-      : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
+      : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
-// The upper halves of two fp32 values (their leading bf16 parts, cut off) in one word.
-__device__ __forceinline__ uint32_t top_halves(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
-__device__ __forceinline__ float without_top(float v) {
-  const float r = v - __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);      // exact
-  return fabsf(v) == __uint_as_float(0x7F800000u) ? 0.f : r;                   // an infinity is all in its first part; NaN stays NaN
-}
-// P parts of two values: word p holds part p of both.
-template <int P>
-__device__ __forceinline__ void split(float a, float b, uint32_t (&w)[P]) {
-#pragma unroll
-  for (int p = 0; p < P; ++p) {
-    w[p] = top_halves(a, b);
-    if (p + 1 < P) { a = without_top(a); b = without_top(b); }
-  }
+__device__ __forceinline__ void st_dsmem_f4(float* p, uint32_t cta, const float4& v) {
+  asm volatile("{\n .reg .b32 ra;\n mapa.shared::cluster.u32 ra, %0, %1;\n st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n}\n"
+               ::"r"(tc::smem_u32(p)), "r"(cta), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
 }
 
-// Eight consecutive activations of a row as raw bits, and as P words of bf16 pairs for each of the four pairs.
-template <int XT>
-struct XOct {
-  uint4 a, b;                // fp32: both; bf16: a; MXINT8: a.x, a.y mantissas, a.z exponent byte
-};
-template <int XT>
-__device__ __forceinline__ void load_x(XOct<XT>& o, const Params& p, int row, int col, bool in) {
-  if (!in) {
-    o.a = o.b = make_uint4(0u, 0u, 0u, 0u);
-    if (XT == kXMXINT8) o.a.z = 127u;
-    return;
-  }
-  const size_t idx = (size_t)row * p.K + col;
-  if (XT == kXF32) {
-    const float* x = static_cast<const float*>(p.X) + idx;
-    o.a = ld16_once(x);
-    o.b = ld16_once(x + 4);
-  } else if (XT == kXBF16) {
-    o.a = ld16_once(static_cast<const uint16_t*>(p.X) + idx);
-  } else {
-    const uint8_t* x = static_cast<const uint8_t*>(p.X);
-    const uint2 m = __ldg(reinterpret_cast<const uint2*>(x + idx));
-    o.a = make_uint4(m.x, m.y, __ldg(x + (size_t)p.M * p.K + (size_t)row * (p.K / 16) + (col >> 4)), 0u);
-  }
-}
-template <int XT, int P>
-__device__ __forceinline__ void pairs_of(const XOct<XT>& o, const Params& p, uint32_t (&w)[4][P]) {
-  if (XT == kXF32) {
-    split<P>(__uint_as_float(o.a.x), __uint_as_float(o.a.y), w[0]);
-    split<P>(__uint_as_float(o.a.z), __uint_as_float(o.a.w), w[1]);
-    split<P>(__uint_as_float(o.b.x), __uint_as_float(o.b.y), w[2]);
-    split<P>(__uint_as_float(o.b.z), __uint_as_float(o.b.w), w[3]);
-  } else if (XT == kXBF16) {
-    w[0][0] = o.a.x; w[1][0] = o.a.y; w[2][0] = o.a.z; w[3][0] = o.a.w;
-  } else {
-    const float4 u = mxint_quad_values(o.a.x, o.a.z, p.bits, p.emin, p.emax), v = mxint_quad_values(o.a.y, o.a.z, p.bits, p.emin, p.emax);
-    w[0][0] = top_halves(u.x, u.y); w[1][0] = top_halves(u.z, u.w);
-    w[2][0] = top_halves(v.x, v.y); w[3][0] = top_halves(v.z, v.w);
-  }
-}
+// XP, TP: bf16 parts of X and of T.  PITCH: bytes of a row of B's image.  The MMA's eight columns are tokens;
+// where the tile has so few that the parts fit side by side (two tokens of three parts, four of two) they are tokens and parts, and
+// one MMA takes the place of two or three: column = token + part * 2 (or 4).
+__host__ __device__ constexpr int side_by_side(int parts) { return parts == 1 ? 8 : parts == 2 ? 4 : 2; }
+// Floats from one column of partial sums to the next: a fragment's stores then go to 32 different banks.
+__host__ __device__ inline int part_stride(int max_rank) { return rank16(max_rank) * 16 + 4; }
 
-__device__ __forceinline__ void load_y0(const Params& p, int row, int col, float (&v)[8]) {
-  const size_t idx = (size_t)row * p.N + col;
-  if (p.y0_bf16) {
-    const uint4 u = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Y0) + idx);
-    const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { v[2 * i] = __uint_as_float(w[i] << 16); v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u); }
-  } else {
-    const float4* q = reinterpret_cast<const float4*>(static_cast<const float*>(p.Y0) + idx);
-    const float4 a = q[0], b = q[1];
-    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w; v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-  }
-}
-__device__ __forceinline__ void store_y(const Params& p, int row, int col, const float (&v)[8]) {
-  const size_t idx = (size_t)row * p.N + col;
-  if (!LQER_IN_BOUNDS(&p.plan->status, idx * (p.y_bf16 ? 2 : 4), p.y_bf16 ? 16 : 32, p.y_extent, 802)) return;
-  if (p.y_bf16) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(w[i]) : "f"(v[2 * i + 1]), "f"(v[2 * i]));
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.Y) + idx) = make_uint4(w[0], w[1], w[2], w[3]);
-  } else {
-    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.Y) + idx);
-    q[0] = make_float4(v[0], v[1], v[2], v[3]);
-    q[1] = make_float4(v[4], v[5], v[6], v[7]);
-  }
-}
-__device__ __forceinline__ float4 ld_dsmem_f4(const float* p, uint32_t cta) {
-  float4 v;
-  asm volatile("{\n .reg .b32 ra;\n mapa.shared::cluster.u32 ra, %4, %5;\n ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [ra];\n}\n"
-               : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(tc::smem_u32(p)), "r"(cta) : "memory");
-  return v;
-}
-
-// XP, TP: bf16 parts of X and of T.  WR: warps along the rows (16 each); the other kWarps / WR share the contraction over K, and
-// later the columns.  RC8: octets of the rank that a pass over X takes.
-template <int XT, int XP, int TP, int WR, int RC8>
-__global__ void __launch_bounds__(kThreads, 2) adapters_kernel(const Params p) {
-  constexpr int WK = kWarps / WR, ROWS = 16 * WR;
+template <int XT, int XP, int TP, int PITCH>
+__global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
+  constexpr int RB = PITCH == 32 ? 16 : 32;             // ranks of a step of B
+  constexpr int XS = side_by_side(XP), TS = side_by_side(TP);
+  constexpr int RC = PITCH == 32 ? 1 : PITCH == 64 ? 2 : 4;                  // sixteens of the rank that one pass over X takes
   extern __shared__ __align__(16) uint8_t smem[];
-  __shared__ int rows[ROWS];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, t = lane & 3;
-  const int wr = warp % WR, wk = warp / WR;
   uint32_t c;
   asm volatile("mov.u32 %0, %%cluster_nctaid.x;" : "=r"(c));
   const uint32_t q = tc::cluster_rank();
   const int tile_id = blockIdx.x / c;
   tc::pdl_launch_dependents();
   tc::pdl_wait();
-  // A plan of another batch (or none) has other sizes in its head: nothing is done then, and its status says so.
-  if (p.plan->magic != kPlanMagic || p.plan->M != p.M || p.plan->n_slots != p.plan_slots || p.plan->tile_rows != ROWS) {
-    if (blockIdx.x == 0 && tid == 0) report_error(&p.plan->status, LQER_ERR_BAD_PACKED, 803);
-    return;
-  }
-  if (tile_id >= p.plan->n_tiles) return;               // the whole cluster
+  // nothing here waits for anything else: the tile list is as long as the grid, whatever it holds
+  const PlanHead head = load_head(p.plan);
   const Tile tile = p.tiles[tile_id];
+  const int row_g = p.rows[tile_id * kFewRows + g];
+  const int row_0 = p.rows[tile_id * kFewRows + 2 * t], row_1 = p.rows[tile_id * kFewRows + 2 * t + 1];
+  if (!plan_fits(p, head) || tile_id >= head.n_tiles) return;            // the whole cluster
   const uint8_t* slot = p.pool + (size_t)max(tile.slot, 0) * p.slot_bytes;
-  const SlotHead hd = *reinterpret_cast<const SlotHead*>(slot);
-  const bool known = hd.magic == kPoolMagic && hd.K == p.K && hd.N == p.N && hd.max_rank == p.max_rank && hd.rank >= 0 && hd.rank <= p.max_rank;
-  if (tile.slot >= 0 && !known && q == 0 && tid == 0) report_error(&p.plan->status, LQER_ERR_BAD_PACKED, 804, tile.slot);
-  const int rank = tile.slot >= 0 && known ? hd.rank : 0;
-  if (tid < ROWS) rows[tid] = p.order[tile.first + min(tid, tile.rows - 1)];
-  __syncthreads();
+  const SlotHead hd = load_slot(slot);
+  const int rank = rank_of(p, tile.slot, hd, q == 0 && tid == 0);
   const int NB = (p.N + 31) / 32, nb_lo = NB * q / c, nb_hi = NB * (q + 1) / c;
   if (rank == 0) {                                      // no adapter: the rows as they are
     if (p.Y0 == p.Y) return;
-    const int octets = min(nb_hi * 4, p.N / 8) - nb_lo * 4;
-    for (int i = warp; i < tile.rows; i += kWarps)
-      for (int o = lane; o < octets; o += 32) {
-        float v[8];
-        load_y0(p, rows[i], (nb_lo * 4 + o) * 8, v);
-        store_y(p, rows[i], (nb_lo * 4 + o) * 8, v);
+    const int quads = min(nb_hi * 8, p.N / 4) - nb_lo * 8;
+    const size_t at = (size_t)p.rows[tile_id * kFewRows + warp % kFewRows] * p.N + nb_lo * 32;
+    if (warp % kFewRows < tile.rows)
+      for (int o = lane + warp / kFewRows * 32; o < quads; o += kWarps / kFewRows * 32) {
+        Y0Quad y;
+        y.load(p, at + o * 4);
+        store_y(p, at + o * 4, y.values(p));
       }
     return;
   }
-  const int r8 = (rank + 7) / 8, r16 = (rank + 15) / 16, ld = part_stride(p.max_rank);
-  float* part = reinterpret_cast<float*>(smem);                        // [WK][ROWS][ld]; the first becomes the CTA's sum,
-  uint4* frags = reinterpret_cast<uint4*>(part + (size_t)ROWS * ld);   // the others make room for [WR][rank / 16][TP][lane]
-  const int row_a = rows[wr * 16 + g], row_b = rows[wr * 16 + g + 8];
-
-  // ---- T's share of this CTA: K blocks of 32, dealt to the warps in turn
-  const int KB = (p.K + 31) / 32, kb_lo = KB * q / c, kb_hi = KB * (q + 1) / c;
+  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");    // waited for before the first remote store
+  const int r16 = rank16(rank), ld = part_stride(p.max_rank);
+  float* part = reinterpret_cast<float*>(smem);         // [warp][column][ld], and then [lane][...] the fragments of T
+  float* sums = part + kWarps * 8 * ld;                 // [CTA of the cluster][token][ld]
   const uint8_t* A = slot + 256;
-  for (int n0 = 0; n0 < r8; n0 += RC8) {
-    const int nn = min(RC8, r8 - n0);
-    float acc[RC8][4];
+  const uint8_t* B = slot + 256 + a_bytes(p.K, p.max_rank);
+
+  // ---- T's share of this CTA: K blocks of 32, dealt to the warps in turn.  Factor rows (ranks) g and g + 8 of each sixteen, tokens g.
+  const int KB = (p.K + 31) / 32, kb_lo = KB * q / c, kb_hi = KB * (q + 1) / c;
+  const bool xpack = XP > 1 && tile.rows <= XS;
+  const uint8_t* a_lane = A + g * 128;                  // ranks g and, 1024 bytes on, g + 8; the swizzle's share is the row's index, g
+  const uint32_t piece0 = (t ^ (g & 3)) << 4, flip = (g & 4) << 4;
+  const int x_row = xpack ? __shfl_sync(0xFFFFFFFFu, row_g, (g % XS) * 4) : row_g, x_part = g / XS;
+  for (int n0 = 0; n0 < r16; n0 += RC) {
+    const int nn = min(RC, r16 - n0);
+    float acc[RC][4];
 #pragma unroll
-    for (int j = 0; j < RC8; ++j)
+    for (int j = 0; j < RC; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    XOct<XT> xa, xb;
-    int kb = kb_lo + wk;
-    bool in = kb < kb_hi && kb * 32 + 8 * t < p.K;
-    load_x<XT>(xa, p, row_a, kb * 32 + 8 * t, in);
-    load_x<XT>(xb, p, row_b, kb * 32 + 8 * t, in);
-    for (; kb < kb_hi; kb += WK) {
-      uint4 f[RC8];
+    XOct<XT> x;
+    int kb = kb_lo + warp;
+    x.load(p, x_row, kb * 32 + 8 * t, kb < kb_hi && kb * 32 + 8 * t < p.K);
+    for (; kb < kb_hi; kb += kWarps) {
+      uint4 f0[RC], f1[RC];
+      const uint8_t* a = a_lane + ((size_t)(kb >> 1) * r16 + n0) * 2048 + (piece0 | (flip ^ (kb & 1) << 6));
 #pragma unroll
-      for (int j = 0; j < RC8; ++j)
-        if (j < nn) f[j] = ld16(A + ((size_t)kb * r8 + n0 + j) * 512 + lane * 16);
-      uint32_t wa[4][XP], wb[4][XP];
-      pairs_of<XT, XP>(xa, p, wa);
-      pairs_of<XT, XP>(xb, p, wb);
-      const int next = kb + WK;
-      in = next < kb_hi && next * 32 + 8 * t < p.K;
-      load_x<XT>(xa, p, row_a, next * 32 + 8 * t, in);
-      load_x<XT>(xb, p, row_b, next * 32 + 8 * t, in);
-#pragma unroll
-      for (int j = 0; j < RC8; ++j)
+      for (int j = 0; j < RC; ++j)
         if (j < nn) {
+          f0[j] = ld16(a + j * 2048);
+          f1[j] = ld16(a + j * 2048 + 1024);
+        }
+      uint32_t w[4][XP];
+      x.template pairs<XP>(p, w);
+      const int next = kb + kWarps;
+      x.load(p, x_row, next * 32 + 8 * t, next < kb_hi && next * 32 + 8 * t < p.K);
+      if (xpack) {
 #pragma unroll
-          for (int x = 0; x < XP; ++x) {
-            const uint32_t a0[4] = {wa[0][x], wb[0][x], wa[1][x], wb[1][x]}, a1[4] = {wa[2][x], wb[2][x], wa[3][x], wb[3][x]};
-            mma(acc[j], a0, f[j].x, f[j].y);
-            mma(acc[j], a1, f[j].z, f[j].w);
-          }
+        for (int i = 0; i < 4; ++i) {
+          uint32_t m = 0;
+#pragma unroll
+          for (int k = 0; k < XP; ++k) m = x_part == k ? w[i][k] : m;
+          w[i][0] = m;
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < RC; ++j)
+        if (j < nn) {
+          float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+          for (int k = XP - 1; k >= 0; --k)
+            if (k == 0 || !xpack) {
+              mma(d, f0[j].x, f1[j].x, f0[j].y, f1[j].y, w[0][k], w[1][k]);
+              mma(d, f0[j].z, f1[j].z, f0[j].w, f1[j].w, w[2][k], w[3][k]);
+            }
+#pragma unroll
+          for (int i = 0; i < 4; ++i) acc[j][i] += d[i];
         }
     }
-    float* mine = part + ((size_t)wk * ROWS + wr * 16) * ld + n0 * 8;
+    float* mine = part + (warp * 8 + 2 * t) * ld + n0 * 16 + g;
 #pragma unroll
-    for (int j = 0; j < RC8; ++j)
+    for (int j = 0; j < RC; ++j)
       if (j < nn) {
-        *reinterpret_cast<float2*>(mine + (size_t)g * ld + j * 8 + 2 * t) = make_float2(acc[j][0], acc[j][1]);
-        *reinterpret_cast<float2*>(mine + (size_t)(g + 8) * ld + j * 8 + 2 * t) = make_float2(acc[j][2], acc[j][3]);
+        mine[j * 16] = acc[j][0];
+        mine[ld + j * 16] = acc[j][1];
+        mine[j * 16 + 8] = acc[j][2];
+        mine[ld + j * 16 + 8] = acc[j][3];
       }
-  }
-  __syncthreads();
-  // ---- the CTA's sum, then the cluster's: every CTA reads all of them, in order
-  const int quads = r8 * 2;
-  if (WK > 1) {
-    for (int i = tid; i < ROWS * quads; i += kThreads) {
-      float4* at = reinterpret_cast<float4*>(part + (size_t)(i / quads) * ld) + i % quads;
-      float4 s = *at;
-      for (int w = 1; w < WK; ++w) {
-        const float4 v = *reinterpret_cast<float4*>(reinterpret_cast<float*>(at) + (size_t)w * ROWS * ld);
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-      }
-      *at = s;
-    }
-  }
-  tc::cluster_barrier();
-  // T's element (row, 16 s + 4 t + i) belongs to lane (row % 8, t) of the row's warp: registers row / 8 and 2 + row / 8
-  for (int i = tid; i < ROWS * r16 * 4; i += kThreads) {
-    const int row = i / (r16 * 4), quad = i % (r16 * 4);
-    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
-    if (quad < quads)
-      for (uint32_t k = 0; k < c; ++k) {
-        const float4 v = ld_dsmem_f4(part + (size_t)row * ld + quad * 4, k);
-        s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
-      }
-    // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
-    const int past = quad * 4 + 4 - rank;
-    if (past > 0) { s.w = 0.f; if (past > 1) s.z = 0.f; if (past > 2) s.y = 0.f; if (past > 3) s.x = 0.f; }
-    uint32_t lo[TP], hi[TP];
-    split<TP>(s.x * hd.scale, s.y * hd.scale, lo);
-    split<TP>(s.z * hd.scale, s.w * hd.scale, hi);
-    uint32_t* f = reinterpret_cast<uint32_t*>(frags + ((size_t)(row / 16) * r16 + quad / 4) * TP * 32 + (row % 8) * 4 + quad % 4) + (row / 8) % 2;
-#pragma unroll
-    for (int x = 0; x < TP; ++x) { f[x * 128] = lo[x]; f[x * 128 + 2] = hi[x]; }
-  }
-  // no CTA leaves while its sums may still be read
-  asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");
-  __syncthreads();
-  // ---- the CTA's columns of Y: blocks of 32, dealt to the warps in turn
-  const uint8_t* B = slot + 256 + a_bytes(p.K, p.max_rank);
-  const uint4* fr = frags + (size_t)wr * r16 * TP * 32 + lane;
-  const bool has_a = wr * 16 + g < tile.rows, has_b = wr * 16 + g + 8 < tile.rows;
-  for (int nb = nb_lo + wk; nb < nb_hi; nb += WK) {
-    const int col = nb * 32 + 8 * t;
-    const bool in = col < p.N;
-    float ya[8], yb[8];
-    if (in && has_a) load_y0(p, row_a, col, ya);
-    if (in && has_b) load_y0(p, row_b, col, yb);
-    float acc[4][4];
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    const uint8_t* b = B + (size_t)nb * r16 * 1024 + lane * 16;
-    for (int s = 0; s < r16; ++s) {
-      const uint4 b0 = ld16(b + s * 1024), b1 = ld16(b + s * 1024 + 512);
-#pragma unroll
-      for (int x = 0; x < TP; ++x) {
-        const uint4 v = fr[(s * TP + x) * 32];
-        const uint32_t a[4] = {v.x, v.y, v.z, v.w};
-        mma(acc[0], a, b0.x, b0.y);
-        mma(acc[1], a, b0.z, b0.w);
-        mma(acc[2], a, b1.x, b1.y);
-        mma(acc[3], a, b1.z, b1.w);
-      }
-    }
-    if (in && has_a) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { ya[2 * j] += acc[j][0]; ya[2 * j + 1] += acc[j][1]; }
-      store_y(p, row_a, col, ya);
-    }
-    if (in && has_b) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j) { yb[2 * j] += acc[j][2]; yb[2 * j + 1] += acc[j][3]; }
-      store_y(p, row_b, col, yb);
-    }
   }
   __syncwarp();
-  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");
+  asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // every CTA of the cluster is there to be written to
+  __syncthreads();
+  // ---- the CTA's sum, warps in order (and parts, lower first, where they lie side by side), to every CTA
+  for (int i = tid; i < tile.rows * r16 * 4; i += kThreads) {
+    const int row = i / (r16 * 4), quad = i % (r16 * 4);
+    float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = XP - 1; k >= 0; --k)
+      if (k == 0 || xpack) {
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+          const float4 v = *reinterpret_cast<const float4*>(part + (w * 8 + row + k * XS) * ld + quad * 4);
+          s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
+        }
+      }
+    for (uint32_t k = 0; k < c; ++k) st_dsmem_f4(sums + (q * 8 + row) * ld + quad * 4, k, s);
+  }
+  // ---- what the last phase reads first is on its way while the sums travel
+  const bool tpack = tile.rows <= TS;
+  const int ra = tpack ? (TS == 8 || t * 2 < TS ? 2 * t : 8) : 2 * t;      // this lane's tokens are ra and ra + 1
+  const bool has_a = ra < tile.rows, has_b = ra + 1 < tile.rows;
+  Y0Quad ya, yb;
+  int nb = nb_lo + warp, col = nb * 32 + 4 * g;
+  const size_t at_a = (size_t)row_0 * p.N, at_b = (size_t)row_1 * p.N;
+  if (nb < nb_hi && col < p.N) {
+    if (has_a) ya.load(p, at_a + col);
+    if (has_b) yb.load(p, at_b + col);
+  }
+  __syncwarp();
+  tc::cluster_barrier();
+  // ---- fragments of T: column g, ranks RB / 4 * t ... of a step; one set for each part, or one for all side by side
+  constexpr int RL = RB / 4;                            // ranks of a lane in a step: 8 or 4
+  const int steps = (rank + RB - 1) / RB;
+  uint32_t* frags = reinterpret_cast<uint32_t*>(part);  // [step][part][lane][RL / 2]
+  for (int i = tid; i < steps * 32; i += kThreads) {
+    const int col = (i >> 2) & 7, first = (i >> 5) * RB + (i & 3) * RL, token = tpack ? col % TS : col;
+    float v[RL];
+#pragma unroll
+    for (int k = 0; k < RL; ++k) v[k] = 0.f;
+    if (token < tile.rows && first < r16 * 16) {
+      for (uint32_t k = 0; k < c; ++k)
+#pragma unroll
+        for (int h = 0; h < RL; h += 4) {
+          const float4 u = *reinterpret_cast<const float4*>(sums + (k * 8 + token) * ld + first + h);
+          v[h] += u.x; v[h + 1] += u.y; v[h + 2] += u.z; v[h + 3] += u.w;
+        }
+    }
+    uint32_t w[RL / 2][TP];
+#pragma unroll
+    for (int k = 0; k < RL; k += 2) {
+      // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
+      const float lo = first + k < rank ? v[k] * hd.scale : 0.f, hi = first + k + 1 < rank ? v[k + 1] * hd.scale : 0.f;
+      split<TP>(lo, hi, w[k / 2]);
+    }
+    uint32_t* at = frags + ((size_t)(i >> 5) * TP * 32 + (i & 31)) * (RL / 2);
+#pragma unroll
+    for (int k = 0; k < RL / 2; ++k) {
+      if (tpack) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int x = 0; x < TP; ++x) m = col / TS == x ? w[k][x] : m;
+        at[k] = m;
+      } else {
+#pragma unroll
+        for (int x = 0; x < TP; ++x) at[x * 32 * (RL / 2) + k] = w[k][x];
+      }
+    }
+  }
+  __syncthreads();
+  // ---- the CTA's columns of Y: blocks of 32, dealt to the warps in turn; a lane's four columns 4 g .. 4 g + 3 are rows g and g + 8
+  // of two MMAs
+  constexpr int SC = PITCH == 128 ? 2 : 1;              // steps of a row of B's image: their fragments are on their way together
+  const int slabs = (rank + 63) / 64;
+  const uint32_t* fr = frags + lane * (RL / 2);
+  for (; nb < nb_hi; nb += kWarps, col += kWarps * 32) {
+    const uint8_t* b = B + (size_t)(nb >> 2) * slabs * 128 * PITCH + ((nb & 3) * 32 + 16 * (g & 1) + 2 * (g >> 1)) * PITCH;
+    float acc[2][4];
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
+    for (int s0 = 0; s0 < steps; s0 += SC, b += 128 * PITCH) {
+      uint32_t f[SC][4][RL / 2];
+#pragma unroll
+      for (int h = 0; h < SC; ++h)
+        if (s0 + h < steps) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {                 // column 4 g + i of 32; the swizzle goes by the image's row modulo 8
+            const uint32_t row = 2 * (g >> 1) + (i & 1), at = (8 * (i >> 1) + (i & 1)) * PITCH;
+            if (PITCH > 32) {
+              const uint4 u = ld16(b + at + (((h * 4 + t) ^ (PITCH == 128 ? row : row >> 1)) << 4));
+              f[h][i][0] = u.x; f[h][i][1] = u.y; f[h][i][RL / 2 - 2] = u.z; f[h][i][RL / 2 - 1] = u.w;
+            } else {
+              const uint2 u = __ldg(reinterpret_cast<const uint2*>(b + at + (((t >> 1) ^ (row >> 2)) << 4) + (t & 1) * 8));
+              f[h][i][0] = u.x; f[h][i][1] = u.y;
+            }
+          }
+        }
+#pragma unroll
+      for (int x = TP - 1; x >= 0; --x)
+        if (x == 0 || !tpack) {
+#pragma unroll
+          for (int h = 0; h < SC; ++h)
+            if (s0 + h < steps) {
+              uint32_t w[RL / 2];
+#pragma unroll
+              for (int k = 0; k < RL / 2; ++k) w[k] = fr[((s0 + h) * TP + x) * 32 * (RL / 2) + k];
+#pragma unroll
+              for (int j = 0; j < 2; ++j)
+#pragma unroll
+                for (int k = 0; k < RL / 2; k += 2)
+                  mma(acc[j], f[h][2 * j][k], f[h][2 * j + 1][k], f[h][2 * j][k + 1], f[h][2 * j + 1][k + 1], w[k], w[k + 1]);
+            }
+        }
+    }
+    float4 va = ya.values(p), vb = yb.values(p);
+    const int next = col + kWarps * 32;
+    if (nb + kWarps < nb_hi && next < p.N) {            // the next block's Y0
+      if (has_a) ya.load(p, at_a + next);
+      if (has_b) yb.load(p, at_b + next);
+    }
+    if (tpack && TP > 1) {                              // the parts of a token are in the neighbouring lanes
+#pragma unroll
+      for (int j = 0; j < 2; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (TS == 2) acc[j][i] += __shfl_xor_sync(0xFFFFFFFFu, acc[j][i], 1);
+          acc[j][i] += __shfl_xor_sync(0xFFFFFFFFu, acc[j][i], 2);
+        }
+    }
+    if (col < p.N) {
+      va.x += acc[0][0]; va.y += acc[0][2]; va.z += acc[1][0]; va.w += acc[1][2];
+      vb.x += acc[0][1]; vb.y += acc[0][3]; vb.z += acc[1][1]; vb.w += acc[1][3];
+      if (has_a) store_y(p, at_a + col, va);
+      if (has_b) store_y(p, at_b + col, vb);
+    }
+  }
 }
 
 // ---------------------------------------------------------------------------- host
-inline size_t slot_bytes(int K, int N, int max_rank) { return (256 + a_bytes(K, max_rank) + b_bytes(N, max_rank) + 255) & ~(size_t)255; }
-inline int tile_rows_of(int M) { return M <= 512 ? 16 : 64; }
-// No batch has more tiles than this: one that is not full per slot (and one of rows without), the rest are full.
-inline int max_tiles(int M, int n_slots) {
-  const int rows = tile_rows_of(M), partial = n_slots + 1 < M ? n_slots + 1 : M;
-  const long long t = (long long)partial + M / rows;
-  return (int)(t < M ? t : M);
-}
-
-template <int XT, int XP, int TP, int WR, int RC8>
-static cudaError_t launch(const Params& p, int clusters, int c, cudaStream_t s) {
-  constexpr int WK = kWarps / WR, ROWS = 16 * WR;
-  const size_t sums = (size_t)ROWS * part_stride(p.max_rank) * 4, frags = (size_t)WR * ((p.max_rank + 15) / 16) * TP * 512;
-  const size_t smem = sums + ((WK - 1) * sums > frags ? (WK - 1) * sums : frags);
+template <int XT, int XP, int TP, int PITCH>
+static cudaError_t launch_few(const Params& p, int tiles, int c, cudaStream_t s) {
+  const size_t part = (size_t)kWarps * 8 * part_stride(p.max_rank) * 4;    // the fragments of T fit in the same place
+  const size_t smem = part + (size_t)c * 8 * part_stride(p.max_rank) * 4;
   static OncePerDevice once;
   cudaError_t e = once.run([] {
-    return cudaFuncSetAttribute(adapters_kernel<XT, XP, TP, WR, RC8>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
+    return cudaFuncSetAttribute(few_rows_kernel<XT, XP, TP, PITCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
   });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
-  cfg.gridDim = dim3((unsigned)(clusters * c));
+  cfg.gridDim = dim3((unsigned)(tiles * c));
   cfg.blockDim = dim3(kThreads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
@@ -479,19 +434,21 @@ static cudaError_t launch(const Params& p, int clusters, int c, cudaStream_t s) 
   cfg.attrs = attr;
   cfg.numAttrs = 2;
   LaunchScope scope(kFamDecode, s);
-  return cudaLaunchKernelEx(&cfg, adapters_kernel<XT, XP, TP, WR, RC8>, p);
+  return cudaLaunchKernelEx(&cfg, few_rows_kernel<XT, XP, TP, PITCH>, p);
 }
 template <int XT, int XP, int TP>
-static cudaError_t launch_rows(const Params& p, int clusters, int c, cudaStream_t s) {
-  if (p.tile_rows == 16) return p.max_rank <= 16 ? launch<XT, XP, TP, 1, 2>(p, clusters, c, s) : launch<XT, XP, TP, 1, 8>(p, clusters, c, s);
-  return p.max_rank <= 16 ? launch<XT, XP, TP, 4, 2>(p, clusters, c, s) : launch<XT, XP, TP, 4, 8>(p, clusters, c, s);
+static cudaError_t launch_few_rank(const Params& p, int tiles, int c, cudaStream_t s) {
+  const int pitch = b_pitch(p.max_rank);
+  return pitch == 32   ? launch_few<XT, XP, TP, 32>(p, tiles, c, s)
+         : pitch == 64 ? launch_few<XT, XP, TP, 64>(p, tiles, c, s)
+                       : launch_few<XT, XP, TP, 128>(p, tiles, c, s);
 }
 
 }  // namespace ad
 
 size_t adapter_slot_bytes(int K, int N, int max_rank) { return ad::slot_bytes(K, N, max_rank); }
 size_t adapter_plan_bytes(int M, int n_slots) {
-  return 256 + (((size_t)ad::max_tiles(M, n_slots) * sizeof(ad::Tile) + 255) & ~(size_t)255) + (((size_t)M * 4 + 255) & ~(size_t)255);
+  return 256 + ad::tiles_bytes(M, n_slots) + (((size_t)ad::max_tiles(M, n_slots) * ad::tile_rows_of(M) * 4 + 255) & ~(size_t)255);
 }
 cudaError_t launch_adapter_pool_init(void* pool, int K, int N, int max_rank, int n_slots, cudaStream_t s) {
   LaunchScope scope(kFamPack, s);
@@ -501,15 +458,15 @@ cudaError_t launch_adapter_pool_init(void* pool, int K, int N, int max_rank, int
 cudaError_t launch_adapter_load(void* pool, int K, int N, int max_rank, int slot, const void* A, const void* B, bool bf16, int rank, float scale,
                                 cudaStream_t s) {
   LaunchScope scope(kFamPack, s);
-  ad::adapter_load_kernel<<<rank > 0 ? 2 * sm_count() : 1, 256, 0, s>>>(static_cast<uint8_t*>(pool) + (size_t)slot * ad::slot_bytes(K, N, max_rank), A, B,
+  ad::adapter_load_kernel<<<rank > 0 ? 4 * sm_count() : 1, 256, 0, s>>>(static_cast<uint8_t*>(pool) + (size_t)slot * ad::slot_bytes(K, N, max_rank), A, B,
                                                                        bf16, K, N, max_rank, rank, scale);
   return cudaGetLastError();
 }
 cudaError_t launch_adapter_plan(const int* slots, int M, int n_slots, void* plan, cudaStream_t s) {
   uint8_t* at = static_cast<uint8_t*>(plan);
   ad::Tile* tiles = reinterpret_cast<ad::Tile*>(at + 256);
-  int* order = reinterpret_cast<int*>(at + 256 + (((size_t)ad::max_tiles(M, n_slots) * sizeof(ad::Tile) + 255) & ~(size_t)255));
-  const size_t smem = (size_t)(n_slots + 1) * ad::kPlanWarps * 4 + (size_t)(n_slots + 2) * 4;
+  int* rows = reinterpret_cast<int*>(at + 256 + ad::tiles_bytes(M, n_slots));
+  const size_t smem = (size_t)(n_slots + 1) * ad::kPlanWarps * 4 + (size_t)(2 * n_slots + 3) * 4;
   static OncePerDevice once;
   cudaError_t e = once.run([] { return cudaFuncSetAttribute(ad::plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); });
   if (e != cudaSuccess) return e;
@@ -524,17 +481,20 @@ cudaError_t launch_adapter_plan(const int* slots, int M, int n_slots, void* plan
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   LaunchScope scope(kFamDecode, s);
-  return cudaLaunchKernelEx(&cfg, ad::plan_kernel, slots, M, n_slots, ad::tile_rows_of(M), reinterpret_cast<ad::PlanHead*>(at), tiles, order);
+  return cudaLaunchKernelEx(&cfg, ad::plan_kernel, slots, M, n_slots, ad::tile_rows_of(M), reinterpret_cast<ad::PlanHead*>(at), tiles, rows);
+}
+size_t adapter_scratch_bytes(int M, int plan_slots, int max_rank) {
+  return ad::tile_rows_of(M) > ad::kFewRows ? ad::many_scratch_bytes(M, plan_slots, max_rank) : 0;
 }
 cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, int K, int N, int max_rank, void* plan, int plan_slots,
-                            const void* Y0, int y0_type, void* Y, int y_type, int bits, int emin, int emax, cudaStream_t s) {
+                            const void* Y0, int y0_type, void* Y, int y_type, int bits, int emin, int emax, void* scratch, cudaStream_t s) {
   uint8_t* at = static_cast<uint8_t*>(plan);
   const int most = ad::max_tiles(M, plan_slots);
   ad::Params p;
   p.X = X; p.pool = static_cast<const uint8_t*>(pool);
   p.plan = reinterpret_cast<ad::PlanHead*>(at);
   p.tiles = reinterpret_cast<const ad::Tile*>(at + 256);
-  p.order = reinterpret_cast<const int*>(at + 256 + (((size_t)most * sizeof(ad::Tile) + 255) & ~(size_t)255));
+  p.rows = reinterpret_cast<const int*>(at + 256 + ad::tiles_bytes(M, plan_slots));
   p.Y0 = Y0; p.Y = Y;
   p.slot_bytes = ad::slot_bytes(K, N, max_rank);
   p.M = M; p.K = K; p.N = N; p.max_rank = max_rank; p.plan_slots = plan_slots; p.tile_rows = ad::tile_rows_of(M);
@@ -542,16 +502,16 @@ cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, 
   p.bits = bits; p.emin = emin; p.emax = emax;
   const size_t whole = y_bytes(y_type, M, N), less = debug_y_shrink();
   p.y_extent = whole > less ? whole - less : 0;
-  // CTAs to a tile: as many as give every SM two, but no fewer than one K block and one column block to a warp of each.
-  const int wk = p.tile_rows == 16 ? 8 : 2, full = (M + p.tile_rows - 1) / p.tile_rows;
-  int c = ad::kMaxCluster;
-  while (c > 1 && (p.tile_rows > 16 && full * c > 2 * sm_count())) c /= 2;
-  while (c > 1 && (K + 31) / 32 < c * wk && (N + 31) / 32 < c * wk) c /= 2;
+  if (p.tile_rows > ad::kFewRows) return ad::launch_many(p, x_type, most, scratch, s);
+  // CTAs to a tile: as many, up to eight, as fit two to an SM, but no more than there are blocks of K or of columns for.
+  int c = 8;
+  while (c > 1 && most * c > 2 * sm_count() + sm_count() / 2) c /= 2;
+  while (c > 1 && (K + 31) / 32 < c * ad::kWarps && (N + 31) / 32 < c * ad::kWarps) c /= 2;
   if (x_type == kXF32)
-    return p.y_bf16 ? ad::launch_rows<kXF32, 2, 2>(p, most, c, s) : ad::launch_rows<kXF32, 3, 3>(p, most, c, s);
+    return p.y_bf16 ? ad::launch_few_rank<kXF32, 2, 2>(p, most, c, s) : ad::launch_few_rank<kXF32, 3, 3>(p, most, c, s);
   if (x_type == kXBF16)
-    return p.y_bf16 ? ad::launch_rows<kXBF16, 1, 2>(p, most, c, s) : ad::launch_rows<kXBF16, 1, 3>(p, most, c, s);
-  return p.y_bf16 ? ad::launch_rows<kXMXINT8, 1, 2>(p, most, c, s) : ad::launch_rows<kXMXINT8, 1, 3>(p, most, c, s);
+    return p.y_bf16 ? ad::launch_few_rank<kXBF16, 1, 2>(p, most, c, s) : ad::launch_few_rank<kXBF16, 1, 3>(p, most, c, s);
+  return p.y_bf16 ? ad::launch_few_rank<kXMXINT8, 1, 2>(p, most, c, s) : ad::launch_few_rank<kXMXINT8, 1, 3>(p, most, c, s);
 }
 
 }  // namespace lqer

@@ -1,0 +1,195 @@
+// Adapters of many requests: the layouts of pool and plan, and what the kernels for few and for many rows share (lqer_adapters.cu,
+// lqer_adapters_many.cu; the layouts are described in the former).
+#pragma once
+
+#include "lqer_tc_ptx.cuh"
+
+namespace lqer {
+namespace ad {
+
+constexpr uint32_t kPoolMagic = 0x4C4F5242u, kPlanMagic = 0x4E414C50u;
+constexpr int kFewRows = 8, kManyRows = 128; // rows of a tile of the kernels for few and for many rows
+
+struct SlotHead {            // first 32 bytes of a slot
+  uint32_t magic;
+  int K, N, max_rank;
+  int rank;                  // 0: empty
+  float scale;
+  int reserved[2];
+};
+struct PlanHead {            // first 256 bytes of a plan
+  DeviceStatus status;
+  uint32_t magic;
+  int M, n_slots, tile_rows;
+  int n_tiles, n_adapted;    // tiles; those in front that name a slot
+};
+struct Tile { int slot, rows; };
+
+// Bytes of a row of B's image (also the span of its swizzle).
+__host__ __device__ inline int b_pitch(int max_rank) { return max_rank <= 16 ? 32 : max_rank <= 32 ? 64 : 128; }
+__host__ __device__ inline int rank16(int rank) { return (rank + 15) / 16; }
+__host__ __device__ inline size_t a_bytes(int K, int rank) { return (size_t)((K + 63) / 64) * rank16(rank) * 2048; }
+__host__ __device__ inline size_t b_bytes(int N, int rank, int pitch) { return (size_t)((N + 127) / 128) * ((rank + 63) / 64) * 128 * pitch; }
+// Place of 16-byte piece c of row r in an image of that pitch.
+__host__ __device__ inline uint32_t swizzled(uint32_t r, uint32_t c, uint32_t pitch) {
+  const uint32_t at = r * pitch + c * 16;
+  return at ^ (((at >> 7) & (pitch / 16 - 1)) << 4);
+}
+
+// Row of B's image, among 128, of a column.
+__host__ __device__ inline int image_row(int n) { return (n & ~31) + 8 * ((n & 7) >> 1) + 2 * ((n & 31) >> 3) + (n & 1); }
+
+// ---------------------------------------------------------------------------- what both kinds of kernels share
+struct Params {
+  const void* X;
+  const uint8_t* pool;
+  PlanHead* plan;
+  const Tile* tiles;
+  const int* rows;
+  const void* Y0;
+  void* Y;
+  size_t slot_bytes;
+  int M, K, N, max_rank, plan_slots, tile_rows;
+  int y0_bf16, y_bf16;
+  int bits, emin, emax;      // format of an MXINT8 X
+  size_t y_extent;
+};
+
+__device__ __forceinline__ uint4 ld16(const void* p) { return __ldg(static_cast<const uint4*>(p)); }
+__device__ __forceinline__ uint4 ld16_once(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+// The upper halves of two fp32 values (their leading bf16 parts, cut off) in one word.
+__device__ __forceinline__ uint32_t top_halves(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
+__device__ __forceinline__ float without_top(float v) {
+  const float r = v - __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);      // exact
+  return fabsf(v) == __uint_as_float(0x7F800000u) ? 0.f : r;                   // an infinity is all in its first part; NaN stays NaN
+}
+// P parts of two values: word p holds part p of both.
+template <int P>
+__device__ __forceinline__ void split(float a, float b, uint32_t (&w)[P]) {
+#pragma unroll
+  for (int p = 0; p < P; ++p) {
+    w[p] = top_halves(a, b);
+    if (p + 1 < P) { a = without_top(a); b = without_top(b); }
+  }
+}
+
+// Eight consecutive activations of a row as raw bits, and as P words of bf16 pairs for each of the four pairs.
+template <int XT>
+struct XOct {
+  uint4 a, b;                // fp32: both; bf16: a; MXINT8: a.x, a.y mantissas, a.z exponent byte
+  __device__ __forceinline__ void load(const Params& p, int row, int col, bool in) {
+    if (!in) {
+      a = b = make_uint4(0u, 0u, 0u, 0u);
+      if (XT == kXMXINT8) a.z = 127u;
+      return;
+    }
+    const size_t idx = (size_t)row * p.K + col;
+    if (XT == kXF32) {
+      const float* x = static_cast<const float*>(p.X) + idx;
+      a = ld16_once(x);
+      b = ld16_once(x + 4);
+    } else if (XT == kXBF16) {
+      a = ld16_once(static_cast<const uint16_t*>(p.X) + idx);
+    } else {
+      const uint8_t* x = static_cast<const uint8_t*>(p.X);
+      const uint2 m = __ldg(reinterpret_cast<const uint2*>(x + idx));
+      a = make_uint4(m.x, m.y, __ldg(x + (size_t)p.M * p.K + (size_t)row * (p.K / 16) + (col >> 4)), 0u);
+    }
+  }
+  template <int P>
+  __device__ __forceinline__ void pairs(const Params& p, uint32_t (&w)[4][P]) const {
+    if (XT == kXF32) {
+      split<P>(__uint_as_float(a.x), __uint_as_float(a.y), w[0]);
+      split<P>(__uint_as_float(a.z), __uint_as_float(a.w), w[1]);
+      split<P>(__uint_as_float(b.x), __uint_as_float(b.y), w[2]);
+      split<P>(__uint_as_float(b.z), __uint_as_float(b.w), w[3]);
+    } else if (XT == kXBF16) {
+      w[0][0] = a.x; w[1][0] = a.y; w[2][0] = a.z; w[3][0] = a.w;
+    } else {
+      const float4 u = mxint_quad_values(a.x, a.z, p.bits, p.emin, p.emax), v = mxint_quad_values(a.y, a.z, p.bits, p.emin, p.emax);
+      w[0][0] = top_halves(u.x, u.y); w[1][0] = top_halves(u.z, u.w);
+      w[2][0] = top_halves(v.x, v.y); w[3][0] = top_halves(v.z, v.w);
+    }
+  }
+};
+
+struct Y0Quad {
+  uint4 a;                   // four values of Y0: fp32, or bf16 in a.x and a.y
+  __device__ __forceinline__ void load(const Params& p, size_t idx) {
+    if (p.y0_bf16) {
+      const uint2 u = *reinterpret_cast<const uint2*>(static_cast<const uint16_t*>(p.Y0) + idx);
+      a.x = u.x;
+      a.y = u.y;
+    } else {
+      a = *reinterpret_cast<const uint4*>(static_cast<const float*>(p.Y0) + idx);
+    }
+  }
+  __device__ __forceinline__ float4 values(const Params& p) const {
+    if (p.y0_bf16)
+      return make_float4(__uint_as_float(a.x << 16), __uint_as_float(a.x & 0xFFFF0000u), __uint_as_float(a.y << 16), __uint_as_float(a.y & 0xFFFF0000u));
+    return make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w));
+  }
+};
+__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+__device__ __forceinline__ void store_y(const Params& p, size_t idx, const float4& v) {
+  if (!LQER_IN_BOUNDS(&p.plan->status, idx * (p.y_bf16 ? 2 : 4), p.y_bf16 ? 8 : 16, p.y_extent, 802)) return;
+  if (p.y_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + idx) = make_uint2(round_bf16x2(v.x, v.y), round_bf16x2(v.z, v.w));
+  else *reinterpret_cast<float4*>(static_cast<float*>(p.Y) + idx) = v;
+}
+// Whether the plan is one of this batch.  (A plan of another batch, or none, has other sizes in its head: nothing is done then, and its
+// status says so.)
+__device__ __forceinline__ bool plan_fits(const Params& p, const PlanHead& h) {
+  if (h.magic == kPlanMagic && h.M == p.M && h.n_slots == p.plan_slots && h.tile_rows == p.tile_rows) return true;
+  if (blockIdx.x == 0 && threadIdx.x == 0) report_error(&p.plan->status, LQER_ERR_BAD_PACKED, 803);
+  return false;
+}
+// The rank of a tile's adapter, 0 where the rows take none.
+__device__ __forceinline__ int rank_of(const Params& p, int slot, const SlotHead& hd, bool tell) {
+  if (slot < 0) return 0;
+  if (hd.magic == kPoolMagic && hd.K == p.K && hd.N == p.N && hd.max_rank == p.max_rank && hd.rank >= 0 && hd.rank <= p.max_rank) return hd.rank;
+  if (tell) report_error(&p.plan->status, LQER_ERR_BAD_PACKED, 804, slot);
+  return 0;
+}
+__device__ __forceinline__ PlanHead load_head(const PlanHead* h) {
+  const uint4 a = *reinterpret_cast<const uint4*>(&h->magic);
+  PlanHead r;
+  r.magic = a.x; r.M = (int)a.y; r.n_slots = (int)a.z; r.tile_rows = (int)a.w;
+  const int2 b = *reinterpret_cast<const int2*>(&h->n_tiles);
+  r.n_tiles = b.x;
+  r.n_adapted = b.y;
+  return r;
+}
+__device__ __forceinline__ SlotHead load_slot(const uint8_t* slot) {
+  const uint4 a = *reinterpret_cast<const uint4*>(slot);
+  const uint2 b = *reinterpret_cast<const uint2*>(slot + 16);
+  return SlotHead{a.x, (int)a.y, (int)a.z, (int)a.w, (int)b.x, __uint_as_float(b.y), {0, 0}};
+}
+
+// ---------------------------------------------------------------------------- host
+inline size_t slot_bytes(int K, int N, int max_rank) {
+  return (256 + a_bytes(K, max_rank) + b_bytes(N, max_rank, b_pitch(max_rank)) + 255) & ~(size_t)255;
+}
+inline int tile_rows_of(int M) { return M <= 512 ? kFewRows : kManyRows; }
+// No batch has more tiles than this: one that is not full per slot (and one of rows without), the rest are full.
+inline int max_tiles(int M, int n_slots) {
+  const int rows = tile_rows_of(M), partial = n_slots + 1 < M ? n_slots + 1 : M;
+  const long long t = (long long)partial + M / rows;
+  return (int)(t < M ? t : M);
+}
+inline size_t tiles_bytes(int M, int n_slots) { return ((size_t)max_tiles(M, n_slots) * sizeof(Tile) + 255) & ~(size_t)255; }
+
+
+// The kernels for many rows: two launches, T's partial sums in between in `scratch`.
+size_t many_scratch_bytes(int M, int plan_slots, int max_rank);
+cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s);
+
+}  // namespace ad
+}  // namespace lqer

@@ -128,8 +128,18 @@ lqer_status_t lqer_adapter_plan(const int* slots, int M, int n_slots, void* plan
   return of(launch_adapter_plan(slots, M, n_slots, plan, static_cast<cudaStream_t>(stream)));
 }
 
+lqer_status_t lqer_adapters_workspace_bytes(int M, const lqer_adapter_pool_t* pool, int plan_slots, size_t* bytes) {
+  if (bytes == nullptr) return LQER_ERR_NULL;
+  lqer_status_t st = pool_shape(pool);
+  if (st != LQER_OK) return st;
+  if (!rows_ok(M) || plan_slots < 1 || plan_slots > pool->n_slots) return LQER_ERR_SHAPE;
+  *bytes = adapter_scratch_bytes(M, plan_slots, pool->max_rank);
+  return LQER_OK;
+}
+
 lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lqer_adapter_pool_t* pool, void* plan, int plan_slots,
-                            const void* Y0, lqer_dtype_t y0_dtype, void* Y, lqer_dtype_t y_dtype, const lqer_config_t* cfg, void* stream) {
+                            const void* Y0, lqer_dtype_t y0_dtype, void* Y, lqer_dtype_t y_dtype, const lqer_config_t* cfg, void* workspace,
+                            size_t workspace_bytes, void* stream) {
   if (X == nullptr || plan == nullptr || Y0 == nullptr || Y == nullptr) return LQER_ERR_NULL;
   lqer_status_t st = pool_ready(pool);
   if (st != LQER_OK) return st;
@@ -139,9 +149,15 @@ lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lq
   if (!rows_ok(M) || plan_slots < 1 || plan_slots > pool->n_slots) return LQER_ERR_SHAPE;
   if (misaligned(X) || misaligned(Y0) || misaligned(Y) || misaligned(plan, 256)) return LQER_ERR_ALIGN;
   if (Y == X || (Y == Y0 && y0_dtype != y_dtype)) return LQER_ERR_CONFIG;
+  const size_t need = adapter_scratch_bytes(M, plan_slots, pool->max_rank);
+  if (need > 0) {
+    if (workspace == nullptr) return LQER_ERR_NULL;
+    if (misaligned(workspace, 256)) return LQER_ERR_ALIGN;
+    if (workspace_bytes < need) return LQER_ERR_BUFFER_TOO_SMALL;
+  }
   if ((st = check_arch()) != LQER_OK) return st;
   return of(launch_adapters(X, x_dtype, M, pool->data, pool->K, pool->N, pool->max_rank, plan, plan_slots, Y0, y0_dtype, Y,
-                            y_dtype, f.a_bits, f.exp_min, f.exp_max, static_cast<cudaStream_t>(stream)));
+                            y_dtype, f.a_bits, f.exp_min, f.exp_max, workspace, static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

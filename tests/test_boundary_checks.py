@@ -64,8 +64,8 @@ def test_adapter_refusals():
     for kw in bad_shapes:
         assert lib.lqer_adapter_pool_bytes(_pool(**kw), C.byref(size)) == E("LQER_ERR_SHAPE"), kw
     assert lib.lqer_adapter_pool_bytes(_pool(None), C.byref(size)) == 0            # the size needs no memory
-    # 2 bytes a factor entry at whole octets of the rank (A) and sixteens of the rank by blocks of 32 columns (B), and a head
-    assert size.value == 4 * (256 + 2 * 64 * 16 + 2 * 64 * 16)
+    # a head, and 2 bytes an entry: A by blocks of 64 rows and 16 ranks, B by blocks of 128 columns and 16, 32 or 64 ranks
+    assert size.value == 4 * (256 + 2 * 64 * 16 + 2 * 128 * 16)
     assert lib.lqer_adapter_pool_init(_pool(), size.value - 1, None) == E("LQER_ERR_BUFFER_TOO_SMALL")
     assert lib.lqer_adapter_pool_init(_pool(None), size.value, None) == E("LQER_ERR_NULL")
     assert lib.lqer_adapter_pool_init(_pool(P + 16), size.value, None) == E("LQER_ERR_ALIGN")
@@ -91,8 +91,8 @@ def test_adapter_refusals():
     assert plan(slots=P + 2) == plan(buf=P + 128) == E("LQER_ERR_ALIGN")
     assert plan(nbytes=need - 1) == E("LQER_ERR_BUFFER_TOO_SMALL")
 
-    def apply(X=P, xt=F32, M=4, pool=_pool(), buf=P, n=4, Y0=2 * P, y0t=F32, Y=3 * P, yt=F32, cfg=None):
-        return lib.lqer_adapters(X, xt, M, pool, buf, n, Y0, y0t, Y, yt, cfg, None)
+    def apply(X=P, xt=F32, M=4, pool=_pool(), buf=P, n=4, Y0=2 * P, y0t=F32, Y=3 * P, yt=F32, cfg=None, ws=None, nbytes=0):
+        return lib.lqer_adapters(X, xt, M, pool, buf, n, Y0, y0t, Y, yt, cfg, ws, nbytes, None)
 
     for kw in (dict(X=None), dict(pool=None), dict(buf=None), dict(Y0=None), dict(Y=None), dict(pool=_pool(None))):
         assert apply(**kw) == E("LQER_ERR_NULL"), kw
@@ -102,6 +102,13 @@ def test_adapter_refusals():
         assert apply(**kw) == E("LQER_ERR_ALIGN"), kw
     for kw in (dict(xt=3), dict(y0t=MX), dict(yt=MX), dict(Y=P), dict(Y=2 * P, yt=BF16)):
         assert apply(**kw) == E("LQER_ERR_CONFIG"), kw
+    # more than 512 rows go through a workspace
+    assert lib.lqer_adapters_workspace_bytes(512, _pool(), 4, C.byref(size)) == 0 and size.value == 0
+    assert lib.lqer_adapters_workspace_bytes(513, _pool(), 4, C.byref(size)) == 0 and size.value > 0
+    assert lib.lqer_adapters_workspace_bytes(513, _pool(), 5, C.byref(size)) == lib.lqer_adapters_workspace_bytes(0, _pool(), 4, C.byref(size)) == E("LQER_ERR_SHAPE")
+    assert lib.lqer_adapters_workspace_bytes(513, _pool(), 4, None) == E("LQER_ERR_NULL")
+    assert apply(M=513) == E("LQER_ERR_NULL") and apply(M=513, ws=P + 16, nbytes=1 << 30) == E("LQER_ERR_ALIGN")
+    assert apply(M=513, ws=P, nbytes=size.value - 1) == E("LQER_ERR_BUFFER_TOO_SMALL")
     assert L.launch_count() == 0
 
 
@@ -115,13 +122,13 @@ def test_tensors_on_the_host_are_refused():
 
 
 def test_a_plan_has_room_for_every_batch():
-    # the head, a tile (16 bytes) for every tile that any batch can have, the rows' order
+    # the head, slot and length (8 bytes) of every tile that any batch can have, its rows
     size = C.c_size_t()
-    for M in (1, 2, 15, 16, 17, 100, 512, 513, 4096):
+    for M in (1, 2, 7, 8, 9, 15, 16, 17, 100, 512, 513, 4096):
         for n in (1, 2, 7, 64, 1024):
             assert L.lib().lqer_adapter_plan_bytes(M, n, C.byref(size)) == 0
-            rows = 16 if M <= 512 else 64
+            rows = 8 if M <= 512 else 128
             # the worst batch: as many bins as possible with one row more than a whole number of tiles
             bins = min(n + 1, M)
             worst = sum(-(-r // rows) for r in [1] * (bins - 1) + [M - (bins - 1)])
-            assert size.value >= 256 + 16 * worst + 4 * M
+            assert size.value >= 256 + 8 * worst + 4 * rows * worst
