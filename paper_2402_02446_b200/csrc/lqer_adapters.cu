@@ -499,6 +499,8 @@ cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, 
   p.slot_bytes = ad::slot_bytes(K, N, max_rank);
   p.M = M; p.K = K; p.N = N; p.max_rank = max_rank; p.plan_slots = plan_slots; p.tile_rows = ad::tile_rows_of(M);
   p.y0_bf16 = y0_type == kYBF16; p.y_bf16 = y_type == kYBF16;
+  p.x_wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
+  p.y_wide = reinterpret_cast<uintptr_t>(Y0) % 32 == 0 && reinterpret_cast<uintptr_t>(Y) % 32 == 0;
   p.bits = bits; p.emin = emin; p.emax = emax;
   const size_t whole = y_bytes(y_type, M, N), less = debug_y_shrink();
   p.y_extent = whole > less ? whole - less : 0;

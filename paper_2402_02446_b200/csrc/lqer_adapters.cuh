@@ -51,6 +51,7 @@ struct Params {
   size_t slot_bytes;
   int M, K, N, max_rank, plan_slots, tile_rows;
   int y0_bf16, y_bf16;
+  bool x_wide, y_wide;       // X; Y0 and Y: aligned to 32 bytes
   int bits, emin, emax;      // format of an MXINT8 X
   size_t y_extent;
 };
@@ -61,19 +62,62 @@ __device__ __forceinline__ uint4 ld16_once(const void* p) {
   asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
   return v;
 }
+// 32 bytes in one access (a whole sector), or in two where the tensor is not aligned to 32.
+__device__ __forceinline__ void ld32(const void* p, bool aligned, uint4& a, uint4& b) {
+  if (aligned) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a.x), "=r"(a.y), "=r"(a.z), "=r"(a.w), "=r"(b.x), "=r"(b.y), "=r"(b.z), "=r"(b.w) : "l"(p) : "memory");
+  } else {
+    a = static_cast<const uint4*>(p)[0];
+    b = static_cast<const uint4*>(p)[1];
+  }
+}
+__device__ __forceinline__ void st32(void* p, bool aligned, const uint4& a, const uint4& b) {
+  if (aligned) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(a.x), "r"(a.y), "r"(a.z), "r"(a.w), "r"(b.x), "r"(b.y), "r"(b.z), "r"(b.w) : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = a;
+    static_cast<uint4*>(p)[1] = b;
+  }
+}
 // The upper halves of two fp32 values (their leading bf16 parts, cut off) in one word.
 __device__ __forceinline__ uint32_t top_halves(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
-__device__ __forceinline__ float without_top(float v) {
-  const float r = v - __uint_as_float(__float_as_uint(v) & 0xFFFF0000u);      // exact
-  return fabsf(v) == __uint_as_float(0x7F800000u) ? 0.f : r;                   // an infinity is all in its first part; NaN stays NaN
-}
-// P parts of two values: word p holds part p of both.
+__device__ __forceinline__ float top_half(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
+// P parts of two values: word p holds part p of both.  What is left of an infinity is nothing (it is all in its first part); NaN stays.
 template <int P>
 __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[P]) {
+  const float inf = __uint_as_float(0x7F800000u);
 #pragma unroll
   for (int p = 0; p < P; ++p) {
     w[p] = top_halves(a, b);
-    if (p + 1 < P) { a = without_top(a); b = without_top(b); }
+    if (p + 1 < P) {
+      const float ra = a - top_half(a), rb = b - top_half(b);              // exact
+      a = p == 0 && fabsf(a) == inf ? 0.f : ra;
+      b = p == 0 && fabsf(b) == inf ? 0.f : rb;
+    }
+  }
+}
+// The same of eight values, of which an infinity is rare: one test for all.
+template <int P>
+__device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&w)[4][P]) {
+  float big = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(v[i]));
+  if (big == __uint_as_float(0x7F800000u)) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split<P>(v[2 * i], v[2 * i + 1], w[i]);
+    return;
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    float a = v[2 * i], b = v[2 * i + 1];
+#pragma unroll
+    for (int p = 0; p < P; ++p) {
+      w[i][p] = top_halves(a, b);
+      a -= top_half(a);
+      b -= top_half(b);
+    }
   }
 }
 
@@ -89,9 +133,7 @@ struct XOct {
     }
     const size_t idx = (size_t)row * p.K + col;
     if (XT == kXF32) {
-      const float* x = static_cast<const float*>(p.X) + idx;
-      a = ld16_once(x);
-      b = ld16_once(x + 4);
+      ld32(static_cast<const float*>(p.X) + idx, p.x_wide, a, b);
     } else if (XT == kXBF16) {
       a = ld16_once(static_cast<const uint16_t*>(p.X) + idx);
     } else {
@@ -103,10 +145,9 @@ struct XOct {
   template <int P>
   __device__ __forceinline__ void pairs(const Params& p, uint32_t (&w)[4][P]) const {
     if (XT == kXF32) {
-      split<P>(__uint_as_float(a.x), __uint_as_float(a.y), w[0]);
-      split<P>(__uint_as_float(a.z), __uint_as_float(a.w), w[1]);
-      split<P>(__uint_as_float(b.x), __uint_as_float(b.y), w[2]);
-      split<P>(__uint_as_float(b.z), __uint_as_float(b.w), w[3]);
+      const float v[8] = {__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w),
+                          __uint_as_float(b.x), __uint_as_float(b.y), __uint_as_float(b.z), __uint_as_float(b.w)};
+      split8<P>(v, w);
     } else if (XT == kXBF16) {
       w[0][0] = a.x; w[1][0] = a.y; w[2][0] = a.z; w[3][0] = a.w;
     } else {
@@ -187,7 +228,7 @@ inline int max_tiles(int M, int n_slots) {
 inline size_t tiles_bytes(int M, int n_slots) { return ((size_t)max_tiles(M, n_slots) * sizeof(Tile) + 255) & ~(size_t)255; }
 
 
-// The kernels for many rows: two launches, T's partial sums in between in `scratch`.
+// The kernels for many rows: three launches, T in between in `scratch`.
 size_t many_scratch_bytes(int M, int plan_slots, int max_rank);
 cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s);
 

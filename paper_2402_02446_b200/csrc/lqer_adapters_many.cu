@@ -1,24 +1,25 @@
 // Adapters of many requests, more than 512 rows (see lqer_adapters.cu for the term, its precision and the layouts of pool and plan):
-// two launches on the tcgen05 tensor cores, tiles of 128 rows of one adapter.
+// three launches, tiles of 128 rows of one adapter, the products on the tcgen05 tensor cores.
 //
-// project_kernel: T = X A_a.  The MMA's 128 rows are tokens, its columns the ranks.  Eight warps bring X from its rows, wherever they lie,
+// project_kernel: T = X A_a.  The MMA's 128 rows are tokens, its columns the ranks.  Sixteen warps bring X from its rows, wherever they lie,
 // through registers into the swizzled image (fp32 as bf16 parts, MXINT8 as its values), A's slabs of 64 K come by bulk copies, and
 // the accumulators - one for each part, so that the small ones are not cut off against the large - stay in tensor memory.
-// expand_kernel: Y = Y0 + scale T B_a.  T is the 128-row operand, in parts, written once a tile; B's images come by bulk copies; each
-// block of 128 columns is one accumulator, and two of them take turns, so that the tensor cores work ahead of the warps that
-// add Y0, which is on its way from memory a block ahead.
+// finish_kernel: T from its partial sums, scaled, in bf16 parts, in the swizzled images that the next kernel copies.
+// expand_kernel: Y = Y0 + T B_a.  T is the 128-row operand, copied once a tile, as B's images are; each block of 128 columns is one
+// accumulator, and two of them take turns, so that the tensor cores work ahead of the sixteen warps that add Y0, which is on its
+// way from memory a block ahead (bf16: two).
 //
-// Both are bound by memory: X is read once, Y0 read and Y written once; A and B come from L2 after a tile's first use.  The tiles'
-// number is known on the device only, so the work (tile by tile, its slabs of K or blocks of columns in turn) is cut into equal
-// stretches, one for each CTA of a grid as large as the device.  A stretch of the projection ends where it ends, in the middle of a
-// tile if need be: it leaves its partial sums of T in place (tile + CTA) of the scratch, which no other stretch has, and the
-// expansion adds up a tile's stretches in order.
+// They are bound by memory: X is read once, Y0 read and Y written once; A and B come from L2 after a tile's first use.  The tiles'
+// number is known on the device only.  The projection's work (tile by tile, its slabs of K in turn) is cut into equal stretches, one
+// for each CTA of a grid as large as the device; a stretch ends where it ends, in the middle of a tile if need be: it leaves its
+// partial sums of T in place (tile + CTA) of the scratch, which no other stretch has, and finish_kernel adds up a tile's
+// stretches in order.  The expansion's CTAs draw groups of columns from a counter.
 #include "lqer_adapters.cuh"
 
 namespace lqer {
 namespace ad {
 
-constexpr int kWorkWarps = 8, kCopyWarp = 8, kMmaWarp = 9, kManyThreads = 320;
+constexpr int kWorkWarps = 16, kCopyWarp = 16, kMmaWarp = 17, kManyThreads = 576;
 constexpr int kXImage = 128 * 128;           // bytes of 128 rows of 64 bf16
 constexpr int kMaxStages = 4;
 constexpr int kMaxChain = 32;                // slabs of K that an accumulator takes before it is added to the partial sums
@@ -26,6 +27,8 @@ constexpr int kMaxChain = 32;                // slabs of K that an accumulator t
 struct ManyParams {
   Params p;
   float4* scratch;           // [tile + CTA][rank / 4][128 rows]
+  uint8_t* images;           // T: [tile][part][rank / 64][128 rows x 128 bytes]
+  int* next_group;           // what expand_kernel's CTAs draw from
   int project_ctas, stages;
   int stall;                 // test hook: the first copy never comes
   long long wait_limit;
@@ -64,7 +67,7 @@ __device__ __forceinline__ uint32_t columns_pow2(int n) {
 }
 // Barriers of a CTA, set up by its first thread.
 struct Barriers {
-  unsigned long long full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], ready;
+  unsigned long long full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], t_full, t_empty, drawn[2], taken[2];
 };
 __device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
 __device__ __forceinline__ void init_barriers(Barriers& b) {
@@ -76,8 +79,11 @@ __device__ __forceinline__ void init_barriers(Barriers& b) {
   for (int i = 0; i < 2; ++i) {
     tc::mbar_init(bar_of(b.acc_full[i]), 1);
     tc::mbar_init(bar_of(b.acc_empty[i]), kWorkWarps);
+    tc::mbar_init(bar_of(b.drawn[i]), 1);
+    tc::mbar_init(bar_of(b.taken[i]), kWorkWarps + 1);
   }
-  tc::mbar_init(bar_of(b.ready), kWorkWarps);
+  tc::mbar_init(bar_of(b.t_full), 1);
+  tc::mbar_init(bar_of(b.t_empty), 1);
   tc::fence_barrier_init();
 }
 
@@ -108,6 +114,7 @@ struct RunWalk {
 template <int XT, int XP>
 __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_constant__ ManyParams mp) {
   constexpr int AHEAD = XT == kXF32 ? 2 : 4;            // slabs whose X is on its way
+  constexpr int RW = 128 / kWorkWarps / 4;              // rows of a lane: eight lanes a row
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
@@ -144,19 +151,19 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
     int it = 0, runs = 0;
     const uint32_t piece = lane & 7;
     while (ok && walk.next(p, r)) {
-      int row[4];
-      uint32_t at[4];
+      int row[RW];
+      uint32_t at[RW];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = warp * 16 + i * 4 + (lane >> 3);
+      for (int i = 0; i < RW; ++i) {
+        const int m = (warp * RW + i) * 4 + (lane >> 3);
         row[i] = p.rows[(size_t)r.tile * kManyRows + m];
         at[i] = swizzled(m, piece, 128);
       }
-      XOct<XT> x[AHEAD][4];
-      auto load = [&](XOct<XT> (&o)[4], int s) {
+      XOct<XT> x[AHEAD][RW];
+      auto load = [&](XOct<XT> (&o)[RW], int s) {
         const int col = (r.slab + s) * 64 + piece * 8;
 #pragma unroll
-        for (int i = 0; i < 4; ++i) o[i].load(p, row[i], col, s < r.slabs && col < p.K);
+        for (int i = 0; i < RW; ++i) o[i].load(p, row[i], col, s < r.slabs && col < p.K);
       };
 #pragma unroll
       for (int a = 0; a < AHEAD; ++a) load(x[a], a);
@@ -170,7 +177,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
             if (ok) {
               uint8_t* img = smem + (size_t)st * stage_bytes;
 #pragma unroll
-              for (int i = 0; i < 4; ++i) {
+              for (int i = 0; i < RW; ++i) {
                 uint32_t w[4][XP];
                 x[a][i].template pairs<XP>(p, w);
 #pragma unroll
@@ -190,7 +197,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
       tc::tc_fence_after();
       const int r16 = rank16(r.rank), m = (warp & 3) * 32 + lane;
       float4* out = mp.scratch + (size_t)(r.tile + blockIdx.x) * (partial_floats(p.max_rank) / 4) + m;
-      for (int b = warp >> 2; b < r16; b += 2) {
+      for (int b = warp >> 2; b < r16; b += kWorkWarps / 4) {
         float v[16];
 #pragma unroll
         for (int k = XP - 1; k >= 0; --k) {
@@ -280,18 +287,54 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
   }
 }
 
+// ---------------------------------------------------------------------------- T from its partial sums
+// A CTA takes eight ranks of a tile, a thread one of its rows.
+template <int TP>
+__global__ void __launch_bounds__(128) finish_kernel(const __grid_constant__ ManyParams mp) {
+  const Params& p = mp.p;
+  tc::pdl_launch_dependents();
+  tc::pdl_wait();
+  const int slabs = (p.max_rank + 63) / 64, tile = blockIdx.x / (slabs * 8), e = blockIdx.x % (slabs * 8), m = threadIdx.x;
+  if (blockIdx.x == 0 && m == 0) *mp.next_group = 0;
+  const PlanHead head = load_head(p.plan);
+  const int slot = p.tiles[tile].slot;                  // (the list is as long as the grid asks, whatever it holds)
+  if (!plan_fits(p, head) || tile >= head.n_adapted) return;
+  const SlotHead hd = load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes);
+  const int rank = rank_of(p, slot, hd, m == 0 && e == 0);
+  if (e * 8 >= (rank + 63) / 64 * 64) return;
+  const int KS = (p.K + 63) / 64;
+  const long long units = (long long)head.n_adapted * KS;
+  const int ctas = busy(units, mp.project_ctas), from = holder(units, (long long)tile * KS, ctas), to = holder(units, (long long)(tile + 1) * KS - 1, ctas);
+  const size_t per = partial_floats(p.max_rank) / 4;
+  const float4* src = mp.scratch + (size_t)(tile + from) * per + e * 256 + m;
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (e * 8 < rank) {
+#pragma unroll 4
+    for (int k = 0; k <= to - from; ++k) {
+      const float4 lo = src[k * per], hi = src[k * per + 128];
+      v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
+      v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+    }
+  }
+  uint32_t w[4][TP];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
+    const float lo = e * 8 + 2 * i < rank ? v[2 * i] * hd.scale : 0.f, hi = e * 8 + 2 * i + 1 < rank ? v[2 * i + 1] * hd.scale : 0.f;
+    split<TP>(lo, hi, w[i]);
+  }
+  uint8_t* img = mp.images + ((size_t)tile * TP * slabs + (e >> 3)) * kXImage + swizzled(m, e & 7, 128);
+#pragma unroll
+  for (int k = 0; k < TP; ++k) *reinterpret_cast<uint4*>(img + (size_t)k * slabs * kXImage) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+}
+
 // ---------------------------------------------------------------------------- Y = Y0 + T B
 template <bool BF16>
 struct Oct {
   uint4 a, b;                // eight values: fp32 both, bf16 a
-  __device__ __forceinline__ void load(const void* p, size_t idx) {
-    if (BF16) {
-      a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p) + idx);
-    } else {
-      const uint4* q = reinterpret_cast<const uint4*>(static_cast<const float*>(p) + idx);
-      a = q[0];
-      b = q[1];
-    }
+  __device__ __forceinline__ void load(const Params& p, size_t idx) {
+    if (BF16) a = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Y0) + idx);
+    else ld32(static_cast<const float*>(p.Y0) + idx, p.y_wide, a, b);
   }
   __device__ __forceinline__ void values(float (&v)[8]) const {
     const uint32_t w[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
@@ -313,19 +356,44 @@ __device__ __forceinline__ void store_oct(const Params& p, size_t idx, const flo
     *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.Y) + idx) =
         make_uint4(round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]), round_bf16x2(v[6], v[7]));
   } else {
-    float4* q = reinterpret_cast<float4*>(static_cast<float*>(p.Y) + idx);
-    q[0] = make_float4(v[0], v[1], v[2], v[3]);
-    q[1] = make_float4(v[4], v[5], v[6], v[7]);
+    uint4 a, b;
+    a.x = __float_as_uint(v[0]); a.y = __float_as_uint(v[1]); a.z = __float_as_uint(v[2]); a.w = __float_as_uint(v[3]);
+    b.x = __float_as_uint(v[4]); b.y = __float_as_uint(v[5]); b.z = __float_as_uint(v[6]); b.w = __float_as_uint(v[7]);
+    st32(static_cast<float*>(p.Y) + idx, p.y_wide, a, b);
   }
 }
+
+// The groups of a CTA, one after another: its first is its own number, the others are drawn from a counter by the copying warp, so that
+// CTAs that get at memory faster take more of them (4096 rows of 13824 fp32 columns: equal stretches ended between 64 and 112 us).  A
+// group is 256 columns of a tile; whose work it is changes nothing in the results.
+struct Groups {
+  volatile int* list;        // two places in shared memory
+  Barriers* bars;
+  int k = 0;
+  // The next group (all lanes of a warp, or one thread alone); negative if a wait ran out.
+  template <bool WARP>
+  __device__ __forceinline__ int next(volatile tc::WaitState* ws) {
+    const uint32_t slot = k & 1;
+    bool ok = tc::mbar_wait(bar_of(bars->drawn[slot]), (k >> 1) & 1, ws);
+    if (WARP) ok = __all_sync(0xFFFFFFFFu, ok) != 0;
+    const int g = ok ? list[slot] : -1;
+    if (WARP) __syncwarp();
+    if (!WARP || (threadIdx.x & 31) == 0) tc::mbar_arrive(bar_of(bars->taken[slot]));
+    ++k;
+    return g;
+  }
+};
 
 template <bool Y0B, bool YB>
 __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_constant__ ManyParams mp) {
   constexpr int TP = YB ? 2 : 3;
+  constexpr int CB = Y0B ? 2 : 1;                       // blocks of 128 columns in a turn: 32 KB of Y0 on its way in fp32, 64 in bf16
+  constexpr int TURNS = 2 / CB;                         // of a group
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
   __shared__ tc::WaitState ws;
+  __shared__ volatile int list[2];
   const Params& p = mp.p;
   uint8_t* smem = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -336,7 +404,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
     ws.abort = 0;
     ws.limit = mp.wait_limit;
   }
-  if (warp == kMmaWarp) tc::tmem_alloc(tc::smem_u32(&tmem_at), 256);
+  if (warp == kMmaWarp) tc::tmem_alloc(tc::smem_u32(&tmem_at), 256 * CB);
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
@@ -345,128 +413,133 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   tc::pdl_wait();
   const PlanHead head = load_head(p.plan);
   const bool fits = plan_fits(p, head);
-  const int NC = (p.N + 127) / 128;
-  const long long items = fits ? (long long)(p.Y0 == p.Y ? head.n_adapted : head.n_tiles) * NC : 0;
-  const long long begin = stretch(items, blockIdx.x, gridDim.x), end = stretch(items, blockIdx.x + 1, gridDim.x);
+  const int NG = (p.N + 255) / 256, NC = (p.N + 127) / 128;
+  const int groups = fits ? (p.Y0 == p.Y ? head.n_adapted : head.n_tiles) * NG : 0;
   bool ok = true;
-  int tile_id = -1, rank = 0;
-  Tile tile{-1, 0};
-  SlotHead hd;
-  // the tile of item v, if it is another one than that of the item before
-  auto enter = [&](long long v) {
-    const int t = (int)(v / NC);
-    if (t == tile_id) return false;
-    tile_id = t;
-    tile = p.tiles[t];
-    hd = load_slot(p.pool + (size_t)max(tile.slot, 0) * p.slot_bytes);
-    rank = rank_of(p, tile.slot, hd, tid == 0);
-    return true;
+  Groups mine{list, &bars};
+  auto rank_at = [&](int t, int& slot, bool tell) {
+    slot = p.tiles[t].slot;
+    return rank_of(p, slot, load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes), tell);
   };
   if (warp < kWorkWarps) {
-    const int quarter = (warp & 3) * 32, half = (warp >> 2) * 64, t = lane & 3;
-    int n = 0;                                          // blocks with an accumulator so far
-    size_t at[4];                                       // this lane's rows, quarter + lane / 4 + 8 i, in Y0 and Y
-    bool has[4];
-    Oct<Y0B> y[4][2];
-    auto load_y0 = [&](int i, int c, long long v) {     // rows i, columns 32 c + 8 t of the warp's 64
-      const int col = (int)(v % NC) * 128 + half + c * 32 + 8 * t;
-      if (has[i] && col < p.N) y[i][c].load(p.Y0, at[i] + col);
+    // ---- accumulators and Y0 into Y: a warp has 32 rows and 32 columns of a block, a lane rows lane / 4 + 8 i and columns 8 (lane % 4) ...
+    const int quarter = (warp & 3) * 32, first = (warp >> 2) * 32 + 8 * (lane & 3);
+    int n = 0;                                          // turns with accumulators so far
+    int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the one whose Y0 is on its way
+    Oct<Y0B> y[CB][4];
+    int ahead = -1, rank_ahead = 0;                     // tile of that group
+    auto enter = [&](int g) {                           // the rows of group g's tile
+      const int t = g / NG;
+      if (t == ahead) return;
+      ahead = t;
+      int slot;
+      rank_ahead = rank_at(t, slot, tid == 0);
+      const int rows = p.tiles[t].rows;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = quarter + (lane >> 2) + 8 * i;
+        coming[i] = m < rows ? p.rows[(size_t)t * kManyRows + m] : -1;
+      }
     };
-    for (long long v = begin; v < end && ok; ++v) {
-      if (enter(v)) {
+    auto load_y0 = [&](int g, int turn) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int m = quarter + (lane >> 2) + 8 * i;
-          has[i] = m < tile.rows;
-          at[i] = (size_t)p.rows[(size_t)tile_id * kManyRows + m] * p.N;
+      for (int c = 0; c < CB; ++c) {
+        const int col = (g % NG) * 256 + (turn * CB + c) * 128 + first;
+        if (col < p.N) {
 #pragma unroll
-          for (int c = 0; c < 2; ++c) load_y0(i, c, v);
-        }
-        if (rank > 0) {
-          // T, summed over the stretches that have a part of this tile, into its images.  The last tile's MMAs are done: its last
-          // accumulator was waited for.
-          const int KS = (p.K + 63) / 64, r16 = rank16(rank), m = tid & 127, slabs = (rank + 63) / 64;
-          const long long units = (long long)head.n_adapted * KS;
-          const int ctas = busy(units, mp.project_ctas), from = holder(units, (long long)tile_id * KS, ctas),
-                    to = holder(units, (long long)(tile_id + 1) * KS - 1, ctas);
-          const size_t per = partial_floats(p.max_rank) / 4;
-          const float4* src = mp.scratch + (size_t)(tile_id + from) * per + m;
-          for (int e = tid >> 7; e < slabs * 8; e += 2) {                   // eight ranks
-            float v8[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-            if (e < r16 * 2)
-              for (int k = 0; k <= to - from; ++k) {
-                const float4 lo = src[k * per + e * 256], hi = src[k * per + e * 256 + 128];
-                v8[0] += lo.x; v8[1] += lo.y; v8[2] += lo.z; v8[3] += lo.w;
-                v8[4] += hi.x; v8[5] += hi.y; v8[6] += hi.z; v8[7] += hi.w;
-              }
-            uint32_t w[4][TP];
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-              // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
-              const float lo = e * 8 + 2 * i < rank ? v8[2 * i] * hd.scale : 0.f, hi = e * 8 + 2 * i + 1 < rank ? v8[2 * i + 1] * hd.scale : 0.f;
-              split<TP>(lo, hi, w[i]);
-            }
-            uint8_t* img = smem + (size_t)(e >> 3) * kXImage + swizzled(m, e & 7, 128);
-#pragma unroll
-            for (int k = 0; k < TP; ++k)
-              *reinterpret_cast<uint4*>(img + (size_t)k * max_slabs * kXImage) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
-          }
-          tc::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(bar_of(bars.ready));
+          for (int i = 0; i < 4; ++i)
+            if (coming[i] >= 0) y[c][i].load(p, (size_t)coming[i] * p.N + col);
         }
       }
-      const bool more = v + 1 < end && (int)((v + 1) / NC) == tile_id;
-      const int buf = n & 1;
-      if (rank > 0) {
-        ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
-        ++n;
+    };
+    int g = mine.next<true>(&ws), then = groups;
+    if (g >= 0 && g < groups) {
+      enter(g);
+      load_y0(g, 0);
+    }
+    while (g >= 0 && g < groups && ok) {
+      const int rank = rank_ahead;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) row[i] = coming[i];
+#pragma unroll
+      for (int turn = 0; turn < TURNS; ++turn) {
         if (!ok) break;
-        tc::tc_fence_after();
-      }
+        const bool last = turn + 1 == TURNS;
+        if (last) {
+          then = mine.next<true>(&ws);
+          if (then >= 0 && then < groups) enter(then);
+        }
+        const int buf = n & 1;
+        if (rank > 0) {
+          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
+          ++n;
+          tc::tc_fence_after();
+        }
+        if (!ok) break;
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
+        for (int c = 0; c < CB; ++c) {
+          const int col = (g % NG) * 256 + (turn * CB + c) * 128 + first;
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint32_t u[16];
-#pragma unroll
-          for (int i = 0; i < 16; ++i) u[i] = 0u;
-          if (rank > 0) {
-            tmem_ld_16x32(tmem + ((uint32_t)(quarter + h * 16) << 16) + buf * 128 + half + c * 32, u);
-            tc::tmem_ld_wait();
-          }
-#pragma unroll
-          for (int i = 0; i < 2; ++i) {                 // rows lane / 4 and lane / 4 + 8 of the sixteen
-            const int k = 2 * h + i, col = (int)(v % NC) * 128 + half + c * 32 + 8 * t;
-            float o[8];
-            y[k][c].values(o);
-            if (more) load_y0(k, c, v + 1);
+          for (int h = 0; h < 2; ++h) {                 // sixteen rows
+            uint32_t u[16];
             if (rank > 0) {
+              tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + (buf * CB + c) * 128 + (warp >> 2) * 32, u);
+              tc::tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) u[i] = 0u;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int i = 2 * h + k;
+              float o[8];
+              y[c][i].values(o);
 #pragma unroll
               for (int j = 0; j < 4; ++j) {
-                o[2 * j] += __uint_as_float(u[4 * j + 2 * i]);
-                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * i + 1]);
+                o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
+                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
               }
+              if (row[i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[i] * p.N + col, o);
             }
-            if (has[k] && col < p.N) store_oct<YB>(p, at[k] + col, o);
           }
         }
+        if (rank > 0) {
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
+        }
+        if (!last) load_y0(g, turn + 1);
+        else if (then >= 0 && then < groups) load_y0(then, 0);
       }
-      if (rank > 0) {
-        tc::tc_fence_before();
-        __syncwarp();
-        if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
-      }
+      g = then;
     }
   } else if (warp == kCopyWarp) {
-    // ---- images of B: a stage is 128 columns of up to 64 ranks
+    // ---- draws the groups; copies a tile's images of T, and images of B: a stage is 128 columns of up to 64 ranks
     if (lane == 0) {
-      int it = 0;
-      for (long long v = begin; v < end && ok; ++v) {
-        enter(v);
-        const int slabs = (rank + 63) / 64;
-        const uint8_t* B = p.pool + (size_t)max(tile.slot, 0) * p.slot_bytes + 256 + a_bytes(p.K, p.max_rank) + (size_t)(v % NC) * slabs * image;
-        for (int s = 0; s < slabs && ok; ++s, ++it) {
+      int it = 0, tiles = 0, at = -1;
+      for (int k = 0, g = blockIdx.x, then; ok; g = then, ++k) {
+        ok = tc::mbar_wait(bar_of(bars.taken[k & 1]), ((k >> 1) & 1) ^ 1, &ws);
+        if (!ok) break;
+        list[k & 1] = g;
+        tc::mbar_arrive(bar_of(bars.drawn[k & 1]));
+        if (g >= groups) break;
+        then = (int)gridDim.x + atomicAdd(mp.next_group, 1);
+        int slot;
+        const int t = g / NG, rank = rank_at(t, slot, false), slabs = (rank + 63) / 64;
+        if (rank > 0 && t != at) {
+          at = t;
+          if (tiles > 0) ok = tc::mbar_wait(bar_of(bars.t_empty), (tiles - 1) & 1, &ws);
+          if (!ok) break;
+          ++tiles;
+          tc::mbar_expect_tx(bar_of(bars.t_full), TP * slabs * kXImage);
+          for (int x = 0; x < TP; ++x)
+            for (int s = 0; s < slabs; ++s)
+              tc::bulk_load(tc::smem_u32(smem + (size_t)(x * max_slabs + s) * kXImage), mp.images + ((size_t)(t * TP + x) * max_slabs + s) * kXImage,
+                            kXImage, bar_of(bars.t_full));
+        }
+        const int c0 = (g % NG) * 2, stages = (min(c0 + 2, NC) - c0) * slabs;
+        const uint8_t* B = p.pool + (size_t)max(slot, 0) * p.slot_bytes + 256 + a_bytes(p.K, p.max_rank) + (size_t)c0 * slabs * image;
+        for (int s = 0; s < stages && ok; ++s, ++it) {
           const int st = it % mp.stages, turn = it / mp.stages;
           ok = tc::mbar_wait(bar_of(bars.empty[st]), (turn & 1) ^ 1, &ws);
           if (!ok) break;
@@ -474,39 +547,52 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
           tc::bulk_load(tc::smem_u32(ring + (size_t)st * image), B + (size_t)s * image, image, bar_of(bars.copied[st]));
         }
       }
-      for (int k = 0; k < mp.stages && !ok && k < it; ++k) {                // after a wait that ran out: no copy is left in flight
+      // after a wait that ran out: no copy is left in flight
+      const long long t0 = clock64();
+      if (!ok && tiles > 0)
+        while (!tc::mbar_try_wait(bar_of(bars.t_full), (tiles - 1) & 1) && clock64() - t0 < mp.wait_limit) {}
+      for (int k = 0; k < mp.stages && !ok && k < it; ++k) {
         const int last = it - 1 - k, st = last % mp.stages, turn = last / mp.stages;
-        const long long t0 = clock64();
-        while (!tc::mbar_try_wait(bar_of(bars.copied[st]), turn & 1) && clock64() - t0 < mp.wait_limit) {}
+        while (!tc::mbar_try_wait(bar_of(bars.copied[st]), turn & 1) && clock64() - t0 < 2 * mp.wait_limit) {}
       }
     }
   } else {
     // ---- MMAs
     if (lane == 0) {
       const uint32_t idesc = tc::make_idesc(128, 128);
-      int it = 0, n = 0, tiles = 0;
-      for (long long v = begin; v < end && ok; ++v) {
-        if (enter(v) && rank > 0) ok = tc::mbar_wait(bar_of(bars.ready), tiles++ & 1, &ws);
+      int it = 0, n = 0, tiles = 0, at = -1;
+      for (int g = mine.next<false>(&ws); g >= 0 && g < groups && ok; g = mine.next<false>(&ws)) {
+        int slot;
+        const int t = g / NG, rank = rank_at(t, slot, false), slabs = (rank + 63) / 64, r16 = rank16(rank);
         if (rank == 0) continue;
-        if (ok) ok = tc::mbar_wait(bar_of(bars.acc_empty[n & 1]), ((n >> 1) & 1) ^ 1, &ws);
-        tc::tc_fence_after();
-        const int slabs = (rank + 63) / 64, r16 = rank16(rank);
-        for (int s = 0; s < slabs && ok; ++s, ++it) {
-          const int st = it % mp.stages, turn = it / mp.stages;
-          ok = tc::mbar_wait(bar_of(bars.copied[st]), turn & 1, &ws);
-          if (!ok) break;
-          tc::tc_fence_after();
-          const uint64_t b = image_desc(tc::smem_u32(ring + (size_t)st * image), pitch);
-          const int steps = min(4, r16 - s * 4);
-#pragma unroll
-          for (int k = TP - 1; k >= 0; --k) {
-            const uint64_t a = image_desc(tc::smem_u32(smem + (size_t)(k * max_slabs + s) * kXImage), 128);
-            for (int h = 0; h < steps; ++h) umma(tmem + (n & 1) * 128, a + 2 * h, b + 2 * h, idesc, s > 0 || h > 0 || k < TP - 1 ? 1u : 0u);
-          }
-          tc::umma_commit(bar_of(bars.empty[st]));
+        if (t != at) {
+          at = t;
+          if (tiles > 0) tc::umma_commit(bar_of(bars.t_empty));              // once what was issued so far is done
+          ok = tc::mbar_wait(bar_of(bars.t_full), tiles++ & 1, &ws);
         }
-        if (ok) tc::umma_commit(bar_of(bars.acc_full[n & 1]));
-        ++n;
+        for (int turn = 0; turn < TURNS && ok; ++turn, ++n) {
+          ok = tc::mbar_wait(bar_of(bars.acc_empty[n & 1]), ((n >> 1) & 1) ^ 1, &ws);
+          tc::tc_fence_after();
+          for (int c = 0; c < CB && ok; ++c) {
+            if ((g % NG) * 2 + turn * CB + c >= NC) continue;
+            const uint32_t d = tmem + ((n & 1) * CB + c) * 128;
+            for (int s = 0; s < slabs && ok; ++s, ++it) {
+              const int st = it % mp.stages, round = it / mp.stages;
+              ok = tc::mbar_wait(bar_of(bars.copied[st]), round & 1, &ws);
+              if (!ok) break;
+              tc::tc_fence_after();
+              const uint64_t b = image_desc(tc::smem_u32(ring + (size_t)st * image), pitch);
+              const int steps = min(4, r16 - s * 4);
+#pragma unroll
+              for (int x = TP - 1; x >= 0; --x) {
+                const uint64_t a = image_desc(tc::smem_u32(smem + (size_t)(x * max_slabs + s) * kXImage), 128);
+                for (int h = 0; h < steps; ++h) umma(d, a + 2 * h, b + 2 * h, idesc, s > 0 || h > 0 || x < TP - 1 ? 1u : 0u);
+              }
+              tc::umma_commit(bar_of(bars.empty[st]));
+            }
+          }
+          if (ok) tc::umma_commit(bar_of(bars.acc_full[n & 1]));
+        }
       }
     }
   }
@@ -516,23 +602,26 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   if (tid == 0 && ws.abort != 0) report_error(&p.plan->status, LQER_ERR_TIMEOUT, 811);
   if (warp == kMmaWarp) {
     tc::tc_fence_after();
-    tc::tmem_dealloc(tmem, 256);
+    tc::tmem_dealloc(tmem, 256 * CB);
   }
 }
 
 // ---------------------------------------------------------------------------- host
 constexpr size_t kSmemMost = 226 * 1024;
+// The grids are no larger than kPrologueMaxCtas (launch_many takes fewer CTAs where the device has fewer SMs).
+static size_t partial_bytes(int tiles, int max_rank) { return ((size_t)tiles + kPrologueMaxCtas) * partial_floats(max_rank) * 4; }
+static size_t image_bytes(int tiles, int max_rank) { return (size_t)tiles * 3 * ((max_rank + 63) / 64) * kXImage; }
 size_t many_scratch_bytes(int M, int plan_slots, int max_rank) {
-  // the grids are no larger than this many CTAs (launch_many takes fewer where the device has fewer SMs)
-  return ((size_t)max_tiles(M, plan_slots) + kPrologueMaxCtas) * partial_floats(max_rank) * 4;
+  const int tiles = max_tiles(M, plan_slots);
+  return partial_bytes(tiles, max_rank) + image_bytes(tiles, max_rank) + 256;
 }
 template <class Kernel>
-static cudaError_t launch(Kernel kernel, OncePerDevice& once, const ManyParams& mp, int ctas, size_t smem, cudaStream_t s) {
+static cudaError_t launch(Kernel kernel, OncePerDevice& once, const ManyParams& mp, int ctas, int threads, size_t smem, cudaStream_t s) {
   cudaError_t e = once.run([=] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMost); });
   if (e != cudaSuccess) return e;
   cudaLaunchConfig_t cfg = {};
   cfg.gridDim = dim3((unsigned)ctas);
-  cfg.blockDim = dim3(kManyThreads);
+  cfg.blockDim = dim3(threads);
   cfg.dynamicSmemBytes = smem;
   cfg.stream = s;
   cudaLaunchAttribute attr[1];
@@ -548,7 +637,7 @@ static cudaError_t launch_project(ManyParams mp, cudaStream_t s) {
   const size_t stage = (size_t)XP * kXImage + rank16(mp.p.max_rank) * 2048;
   mp.stages = (int)((kSmemMost - 1024) / stage);
   if (mp.stages > kMaxStages) mp.stages = kMaxStages;
-  return launch(project_kernel<XT, XP>, once, mp, mp.project_ctas, mp.stages * stage + 1024, s);
+  return launch(project_kernel<XT, XP>, once, mp, mp.project_ctas, kManyThreads, mp.stages * stage + 1024, s);
 }
 template <bool Y0B, bool YB>
 static cudaError_t launch_expand(ManyParams mp, int ctas, cudaStream_t s) {
@@ -556,16 +645,21 @@ static cudaError_t launch_expand(ManyParams mp, int ctas, cudaStream_t s) {
   const size_t t = (size_t)(YB ? 2 : 3) * ((mp.p.max_rank + 63) / 64) * kXImage, image = (size_t)128 * b_pitch(mp.p.max_rank);
   mp.stages = (int)((kSmemMost - 1024 - t) / image);
   if (mp.stages > kMaxStages) mp.stages = kMaxStages;
-  return launch(expand_kernel<Y0B, YB>, once, mp, ctas, t + mp.stages * image + 1024, s);
+  return launch(expand_kernel<Y0B, YB>, once, mp, ctas, kManyThreads, t + mp.stages * image + 1024, s);
 }
 cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s) {
-  (void)tiles;
   const int sms = sm_count(), ctas = sms < kPrologueMaxCtas ? sms : kPrologueMaxCtas;
-  ManyParams mp{p, static_cast<float4*>(scratch), ctas, 0, take_stall(kFamDecode) ? 1 : 0, wait_limit_cycles()};
-  LaunchScope scope(kFamDecode, s, 2);
+  uint8_t* images = static_cast<uint8_t*>(scratch) + partial_bytes(tiles, p.max_rank);
+  ManyParams mp{p, static_cast<float4*>(scratch), images, reinterpret_cast<int*>(images + image_bytes(tiles, p.max_rank)), ctas, 0,
+                take_stall(kFamDecode) ? 1 : 0, wait_limit_cycles()};
+  LaunchScope scope(kFamDecode, s, 3);
   cudaError_t e = x_type == kXF32    ? (p.y_bf16 ? launch_project<kXF32, 2>(mp, s) : launch_project<kXF32, 3>(mp, s))
                   : x_type == kXBF16 ? launch_project<kXBF16, 1>(mp, s)
                                      : launch_project<kXMXINT8, 1>(mp, s);
+  if (e != cudaSuccess) return e;
+  static OncePerDevice once[2];
+  const int eights = tiles * ((p.max_rank + 63) / 64) * 8;
+  e = p.y_bf16 ? launch(finish_kernel<2>, once[0], mp, eights, 128, 0, s) : launch(finish_kernel<3>, once[1], mp, eights, 128, 0, s);
   if (e != cudaSuccess) return e;
   return p.y0_bf16 ? (p.y_bf16 ? launch_expand<true, true>(mp, ctas, s) : launch_expand<true, false>(mp, ctas, s))
                    : (p.y_bf16 ? launch_expand<false, true>(mp, ctas, s) : launch_expand<false, false>(mp, ctas, s));
