@@ -28,21 +28,46 @@ struct ManyParams {
   Params p;
   float4* scratch;           // [tile + CTA][rank / 4][128 rows]
   uint8_t* images;           // T: [tile][part][rank / 64][128 rows x 128 bytes]
-  int* next_group;           // what expand_kernel's CTAs draw from
-  int project_ctas, stages;
+  int* drawn;                // groups that expand_kernel's CTAs took beside their first
+  int project_ctas, stages, t_sets;      // t_sets: tiles' T that fit side by side, 1 or 2
   int stall;                 // test hook: the first copy never comes
   long long wait_limit;
 };
 __host__ __device__ inline size_t partial_floats(int max_rank) { return (size_t)rank16(max_rank) * 16 * 128; }
-// CTAs that have work, first unit of CTA i's stretch of `units`, and the CTA whose stretch holds a unit.
-__device__ __forceinline__ int busy(long long units, int ctas) { return (int)min(units, (long long)ctas); }
-__device__ __forceinline__ long long stretch(long long units, int i, int ctas) { return units * i / ctas; }
-__device__ __forceinline__ int holder(long long units, long long u, int ctas) {
-  int i = (int)(u * ctas / units);
-  while (i + 1 < ctas && stretch(units, i + 1, ctas) <= u) ++i;
-  while (stretch(units, i, ctas) > u) --i;
-  return i;
-}
+// The projection's work, KS slabs of each of `tiles` tiles, cut into stretches for up to `most` CTAs.  Either every tile is cut alike
+// (`parts` CTAs, `each` slabs a stretch), or the whole of it is (parts == 0), with stretches that may reach into the next tile.  To
+// change tiles costs a CTA about as much as four slabs, so tiles are cut alike where that makes the longest stretch no more than four
+// slabs longer (2048 rows of 4096 bf16 columns in 17 tiles, 8 against 7.4 slabs: 11.6 -> 9.2 us).
+struct Cut {
+  int KS, ctas, parts, each, rest;      // ctas: those that have work; parts == 0: units = each * ctas + rest
+  __device__ Cut(int tiles, int slabs, int most) : KS(slabs) {
+    const long long units = (long long)max(tiles, 0) * KS;
+    parts = tiles > 0 ? min(most / tiles, KS) : 0;
+    ctas = (int)min(units, (long long)most);
+    each = ctas > 0 ? (int)(units / ctas) : 0;
+    rest = ctas > 0 ? (int)(units - (long long)each * ctas) : 0;
+    if (parts > 0 && (KS + parts - 1) / parts <= each + (rest > 0 ? 1 : 0) + 4) {
+      each = (KS + parts - 1) / parts;
+      parts = (KS + each - 1) / each;
+      ctas = tiles * parts;
+    } else {
+      parts = 0;
+    }
+  }
+  // first unit (tile * KS + slab) of CTA i's stretch; i may be ctas
+  __device__ long long first(int i) const {
+    if (parts > 0) return (long long)(i / parts) * KS + (i % parts) * each;
+    return (long long)each * i + (ctas > 0 ? rest * i / ctas : 0);
+  }
+  // the CTA whose stretch holds a unit
+  __device__ int holder(long long u) const {
+    if (parts > 0) return (int)(u / KS) * parts + (int)(u % KS) / each;
+    int i = min(max((int)((float)u / ((float)each + (float)rest / (float)ctas)), 0), ctas - 1);
+    while (i + 1 < ctas && first(i + 1) <= u) ++i;
+    while (first(i) > u) --i;
+    return i;
+  }
+};
 __device__ __forceinline__ void umma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
   asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
                ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
@@ -67,7 +92,7 @@ __device__ __forceinline__ uint32_t columns_pow2(int n) {
 }
 // Barriers of a CTA, set up by its first thread.
 struct Barriers {
-  unsigned long long full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], t_full, t_empty, drawn[2], taken[2];
+  unsigned long long full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], t_full[2], t_empty[2], drawn[2], taken[2];
 };
 __device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
 __device__ __forceinline__ void init_barriers(Barriers& b) {
@@ -79,41 +104,42 @@ __device__ __forceinline__ void init_barriers(Barriers& b) {
   for (int i = 0; i < 2; ++i) {
     tc::mbar_init(bar_of(b.acc_full[i]), 1);
     tc::mbar_init(bar_of(b.acc_empty[i]), kWorkWarps);
+    tc::mbar_init(bar_of(b.t_full[i]), 1);
+    tc::mbar_init(bar_of(b.t_empty[i]), 1);
     tc::mbar_init(bar_of(b.drawn[i]), 1);
     tc::mbar_init(bar_of(b.taken[i]), kWorkWarps + 1);
   }
-  tc::mbar_init(bar_of(b.t_full), 1);
-  tc::mbar_init(bar_of(b.t_empty), 1);
   tc::fence_barrier_init();
 }
 
 // ---------------------------------------------------------------------------- T = X A
-// A CTA's stretch is walked by all roles alike: runs of slabs of one tile, at most kMaxChain each; tiles without a rank are passed over.
+// A CTA's stretch is walked by all roles alike: runs of slabs of one tile, at most kMaxChain each.  (An empty slot's rank counts as 16
+// here, so that nobody has to know it before X is on its way; finish_kernel knows.)
 struct Run {
-  int tile, slab, slabs, rank;
+  int tile, slab, slabs;
   bool first;                // the first of its tile in this stretch
 };
 struct RunWalk {
   long long u, end, begin;
   int KS;
-  __device__ bool next(const Params& p, Run& r) {
-    while (u < end) {
-      r.tile = (int)(u / KS);
-      r.slab = (int)(u % KS);
-      r.first = u == begin || r.slab == 0;
-      r.slabs = (int)min((long long)min(KS - r.slab, kMaxChain), end - u);
-      const int slot = p.tiles[r.tile].slot;
-      r.rank = rank_of(p, slot, load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes), false);
-      u += r.slabs;
-      if (r.rank > 0) return true;
-    }
-    return false;
+  __device__ bool next(Run& r) {
+    if (u >= end) return false;
+    r.tile = (int)(u / KS);
+    r.slab = (int)(u % KS);
+    r.first = u == begin || r.slab == 0;
+    r.slabs = (int)min((long long)min(KS - r.slab, kMaxChain), end - u);
+    u += r.slabs;
+    return true;
   }
 };
+__device__ __forceinline__ int project_rank16(const Params& p, int tile, int& slot) {
+  slot = max(p.tiles[tile].slot, 0);
+  return max(rank16(rank_of(p, slot, load_slot(p.pool + (size_t)slot * p.slot_bytes), false)), 1);
+}
 
 template <int XT, int XP>
 __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_constant__ ManyParams mp) {
-  constexpr int AHEAD = XT == kXF32 ? 2 : 4;            // slabs whose X is on its way
+  constexpr int AHEAD = XT == kXF32 ? 3 : 6;            // slabs whose X is on its way
   constexpr int RW = 128 / kWorkWarps / 4;              // rows of a lane: eight lanes a row
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
@@ -135,22 +161,21 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_at;
-  tc::pdl_launch_dependents();
   tc::pdl_wait();
+  tc::pdl_launch_dependents();                          // in this order: see expand_kernel
   const PlanHead head = load_head(p.plan);
   RunWalk walk;
   walk.KS = (p.K + 63) / 64;
-  const long long units = plan_fits(p, head) ? (long long)head.n_adapted * walk.KS : 0;
-  const int ctas = busy(units, gridDim.x), cta = min((int)blockIdx.x, ctas);
-  walk.begin = walk.u = ctas > 0 ? stretch(units, cta, ctas) : 0;
-  walk.end = ctas > 0 ? stretch(units, min(cta + 1, ctas), ctas) : 0;
+  const Cut cut(plan_fits(p, head) ? head.n_adapted : 0, walk.KS, gridDim.x);
+  walk.begin = walk.u = cut.first(min((int)blockIdx.x, cut.ctas));
+  walk.end = cut.first(min((int)blockIdx.x + 1, cut.ctas));
   Run r;
   bool ok = true;
   if (warp < kWorkWarps) {
     // ---- X into its images; then, at a run's end, the accumulators into the partial sums
     int it = 0, runs = 0;
     const uint32_t piece = lane & 7;
-    while (ok && walk.next(p, r)) {
+    while (ok && walk.next(r)) {
       int row[RW];
       uint32_t at[RW];
 #pragma unroll
@@ -167,6 +192,8 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
       };
 #pragma unroll
       for (int a = 0; a < AHEAD; ++a) load(x[a], a);
+      int slot;
+      const int r16 = project_rank16(p, r.tile, slot);
       for (int s0 = 0; s0 < r.slabs && ok; s0 += AHEAD) {
 #pragma unroll
         for (int a = 0; a < AHEAD; ++a) {
@@ -195,7 +222,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
       ++runs;
       if (!ok) break;
       tc::tc_fence_after();
-      const int r16 = rank16(r.rank), m = (warp & 3) * 32 + lane;
+      const int m = (warp & 3) * 32 + lane;
       float4* out = mp.scratch + (size_t)(r.tile + blockIdx.x) * (partial_floats(p.max_rank) / 4) + m;
       for (int b = warp >> 2; b < r16; b += kWorkWarps / 4) {
         float v[16];
@@ -227,9 +254,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
     // ---- slabs of A
     if (lane == 0) {
       int it = 0;
-      while (ok && walk.next(p, r)) {
-        const uint32_t bytes = rank16(r.rank) * 2048;
-        const uint8_t* A = p.pool + (size_t)p.tiles[r.tile].slot * p.slot_bytes + 256 + (size_t)r.slab * bytes;
+      while (ok && walk.next(r)) {
+        int slot;
+        const uint32_t bytes = project_rank16(p, r.tile, slot) * 2048;
+        const uint8_t* A = p.pool + (size_t)slot * p.slot_bytes + 256 + (size_t)r.slab * bytes;
         for (int s = 0; s < r.slabs && ok; ++s, ++it) {
           const int st = it % mp.stages, turn = it / mp.stages;
           ok = tc::mbar_wait(bar_of(bars.empty[st]), (turn & 1) ^ 1, &ws);
@@ -251,8 +279,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
     // ---- MMAs
     if (lane == 0) {
       int it = 0, runs = 0;
-      while (ok && walk.next(p, r)) {
-        const int cols = rank16(r.rank) * 16;
+      while (ok && walk.next(r)) {
+        int slot;
+        const int cols = project_rank16(p, r.tile, slot) * 16;
         const uint32_t idesc = tc::make_idesc(128, cols);
         ok = tc::mbar_wait(bar_of(bars.acc_empty[0]), (runs & 1) ^ 1, &ws);
         ++runs;
@@ -288,44 +317,51 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
 }
 
 // ---------------------------------------------------------------------------- T from its partial sums
-// A CTA takes eight ranks of a tile, a thread one of its rows.
+// A CTA takes eight ranks of a tile, a thread four of one of its rows.
 template <int TP>
-__global__ void __launch_bounds__(128) finish_kernel(const __grid_constant__ ManyParams mp) {
+__global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ ManyParams mp) {
   const Params& p = mp.p;
-  tc::pdl_launch_dependents();
-  tc::pdl_wait();
-  const int slabs = (p.max_rank + 63) / 64, tile = blockIdx.x / (slabs * 8), e = blockIdx.x % (slabs * 8), m = threadIdx.x;
-  if (blockIdx.x == 0 && m == 0) *mp.next_group = 0;
+  // plan and pool were there before project_kernel (see expand_kernel); its partial sums have to be waited for
+  const int slabs = (p.max_rank + 63) / 64, tile = blockIdx.x / (slabs * 8), e = blockIdx.x % (slabs * 8), m = threadIdx.x & 127, h = threadIdx.x >> 7;
   const PlanHead head = load_head(p.plan);
   const int slot = p.tiles[tile].slot;                  // (the list is as long as the grid asks, whatever it holds)
-  if (!plan_fits(p, head) || tile >= head.n_adapted) return;
-  const SlotHead hd = load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes);
-  const int rank = rank_of(p, slot, hd, m == 0 && e == 0);
-  if (e * 8 >= (rank + 63) / 64 * 64) return;
-  const int KS = (p.K + 63) / 64;
-  const long long units = (long long)head.n_adapted * KS;
-  const int ctas = busy(units, mp.project_ctas), from = holder(units, (long long)tile * KS, ctas), to = holder(units, (long long)(tile + 1) * KS - 1, ctas);
+  int rank = 0;
+  SlotHead hd;
+  if (plan_fits(p, head) && tile < head.n_adapted) {
+    hd = load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes);
+    rank = rank_of(p, slot, hd, threadIdx.x == 0 && e == 0);
+  }
+  const int KS = (p.K + 63) / 64, first = e * 8 + h * 4;
+  const bool here = e * 8 < (rank + 63) / 64 * 64, filled = here && first < rank;
+  const Cut cut(filled ? head.n_adapted : 0, KS, mp.project_ctas);
+  const int from = filled ? cut.holder((long long)tile * KS) : 0, count = filled ? cut.holder((long long)(tile + 1) * KS - 1) - from + 1 : 0;
   const size_t per = partial_floats(p.max_rank) / 4;
-  const float4* src = mp.scratch + (size_t)(tile + from) * per + e * 256 + m;
-  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-  if (e * 8 < rank) {
-#pragma unroll 4
-    for (int k = 0; k <= to - from; ++k) {
-      const float4 lo = src[k * per], hi = src[k * per + 128];
-      v[0] += lo.x; v[1] += lo.y; v[2] += lo.z; v[3] += lo.w;
-      v[4] += hi.x; v[5] += hi.y; v[6] += hi.z; v[7] += hi.w;
+  const float4* src = mp.scratch + (size_t)(tile + from) * per + (e * 2 + h) * 128 + m;
+  tc::pdl_wait();
+  tc::pdl_launch_dependents();                          // not before: expand_kernel's CTAs would take the places of this kernel's last ones
+  if (blockIdx.x == 0 && threadIdx.x == 0) *mp.drawn = 0;
+  if (!here) return;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  constexpr int TOGETHER = 12;                          // stretches whose sums are on their way together
+  for (int k0 = 0; k0 < count; k0 += TOGETHER) {
+    float4 u[TOGETHER];
+#pragma unroll
+    for (int k = 0; k < TOGETHER; ++k) {
+      u[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (k0 + k < count) u[k] = src[(k0 + k) * per];
     }
-  }
-  uint32_t w[4][TP];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
-    const float lo = e * 8 + 2 * i < rank ? v[2 * i] * hd.scale : 0.f, hi = e * 8 + 2 * i + 1 < rank ? v[2 * i + 1] * hd.scale : 0.f;
-    split<TP>(lo, hi, w[i]);
+    for (int k = 0; k < TOGETHER; ++k) { v[0] += u[k].x; v[1] += u[k].y; v[2] += u[k].z; v[3] += u[k].w; }
   }
-  uint8_t* img = mp.images + ((size_t)tile * TP * slabs + (e >> 3)) * kXImage + swizzled(m, e & 7, 128);
+  // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
 #pragma unroll
-  for (int k = 0; k < TP; ++k) *reinterpret_cast<uint4*>(img + (size_t)k * slabs * kXImage) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
+  for (int i = 0; i < 4; ++i) v[i] = first + i < rank ? v[i] * hd.scale : 0.f;
+  uint32_t lo[TP], hi[TP];
+  split<TP>(v[0], v[1], lo);
+  split<TP>(v[2], v[3], hi);
+  uint8_t* img = mp.images + ((size_t)tile * TP * slabs + (e >> 3)) * kXImage + swizzled(m, e & 7, 128) + h * 8;
+#pragma unroll
+  for (int k = 0; k < TP; ++k) *reinterpret_cast<uint2*>(img + (size_t)k * slabs * kXImage) = make_uint2(lo[k], hi[k]);
 }
 
 // ---------------------------------------------------------------------------- Y = Y0 + T B
@@ -363,20 +399,22 @@ __device__ __forceinline__ void store_oct(const Params& p, size_t idx, const flo
   }
 }
 
-// The groups of a CTA, one after another: its first is its own number, the others are drawn from a counter by the copying warp, so that
-// CTAs that get at memory faster take more of them (4096 rows of 13824 fp32 columns: equal stretches ended between 64 and 112 us).  A
-// group is 256 columns of a tile; whose work it is changes nothing in the results.
+// The groups - 256 columns of a tile - are taken in order, each by the next CTA that is free: some SMs get at memory faster than others,
+// and CTAs that work side by side on neighbouring columns are kind to the memory's pages (4096 rows of 13824 fp32 columns: 88 us, against
+// 112 where every CTA had a stretch of its own).  The copying warp draws them, from a counter in the scratch; whose work a group
+// is changes nothing in the results.  What the other warps see of it:
 struct Groups {
-  volatile int* list;        // two places in shared memory
+  volatile int2* list;       // two places in shared memory: group, rank of its tile's adapter
   Barriers* bars;
   int k = 0;
-  // The next group (all lanes of a warp, or one thread alone); negative if a wait ran out.
+  // the next group (all lanes of a warp, or one thread alone); negative if a wait ran out
   template <bool WARP>
-  __device__ __forceinline__ int next(volatile tc::WaitState* ws) {
+  __device__ __forceinline__ int next(int& rank, volatile tc::WaitState* ws) {
     const uint32_t slot = k & 1;
     bool ok = tc::mbar_wait(bar_of(bars->drawn[slot]), (k >> 1) & 1, ws);
     if (WARP) ok = __all_sync(0xFFFFFFFFu, ok) != 0;
-    const int g = ok ? list[slot] : -1;
+    const int g = ok ? list[slot].x : -1;
+    rank = list[slot].y;
     if (WARP) __syncwarp();
     if (!WARP || (threadIdx.x & 31) == 0) tc::mbar_arrive(bar_of(bars->taken[slot]));
     ++k;
@@ -387,120 +425,109 @@ struct Groups {
 template <bool Y0B, bool YB>
 __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_constant__ ManyParams mp) {
   constexpr int TP = YB ? 2 : 3;
-  constexpr int CB = Y0B ? 2 : 1;                       // blocks of 128 columns in a turn: 32 KB of Y0 on its way in fp32, 64 in bf16
-  constexpr int TURNS = 2 / CB;                         // of a group
+  constexpr int AHEAD = Y0B ? 2 : 1;                    // blocks of 128 columns whose Y0 is on its way: 64 KB a CTA
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
   __shared__ tc::WaitState ws;
-  __shared__ volatile int list[2];
+  __shared__ volatile int2 list[2];
   const Params& p = mp.p;
   uint8_t* smem = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int max_slabs = (p.max_rank + 63) / 64, pitch = b_pitch(p.max_rank), image = 128 * pitch;
-  uint8_t* ring = smem + (size_t)TP * max_slabs * kXImage;
+  const uint32_t t_bytes = TP * max_slabs * kXImage;
+  uint8_t* ring = smem + mp.t_sets * t_bytes;
   if (tid == 0) {
     init_barriers(bars);
     ws.abort = 0;
     ws.limit = mp.wait_limit;
   }
-  if (warp == kMmaWarp) tc::tmem_alloc(tc::smem_u32(&tmem_at), 256 * CB);
+  if (warp == kMmaWarp) tc::tmem_alloc(tc::smem_u32(&tmem_at), 256);
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_at;
   tc::pdl_launch_dependents();
-  tc::pdl_wait();
+  // project_kernel lets the kernels behind it start only once it has waited for all that came before the call, so plan, pool and Y0
+  // may be read here at once; only what finish_kernel writes - the images of T, the counter - has to be waited for, which the
+  // copying warp does.
   const PlanHead head = load_head(p.plan);
   const bool fits = plan_fits(p, head);
   const int NG = (p.N + 255) / 256, NC = (p.N + 127) / 128;
   const int groups = fits ? (p.Y0 == p.Y ? head.n_adapted : head.n_tiles) * NG : 0;
   bool ok = true;
   Groups mine{list, &bars};
-  auto rank_at = [&](int t, int& slot, bool tell) {
-    slot = p.tiles[t].slot;
-    return rank_of(p, slot, load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes), tell);
-  };
   if (warp < kWorkWarps) {
     // ---- accumulators and Y0 into Y: a warp has 32 rows and 32 columns of a block, a lane rows lane / 4 + 8 i and columns 8 (lane % 4) ...
     const int quarter = (warp & 3) * 32, first = (warp >> 2) * 32 + 8 * (lane & 3);
     int n = 0;                                          // turns with accumulators so far
-    int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the one whose Y0 is on its way
-    Oct<Y0B> y[CB][4];
-    int ahead = -1, rank_ahead = 0;                     // tile of that group
+    int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the next one
+    Oct<Y0B> y[AHEAD][4];
+    int ahead = -1, rank = 0, then_rank = 0;            // tile of the next group; ranks of the group at hand and of the next one
     auto enter = [&](int g) {                           // the rows of group g's tile
       const int t = g / NG;
       if (t == ahead) return;
       ahead = t;
-      int slot;
-      rank_ahead = rank_at(t, slot, tid == 0);
       const int rows = p.tiles[t].rows;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const int m = quarter + (lane >> 2) + 8 * i;
-        coming[i] = m < rows ? p.rows[(size_t)t * kManyRows + m] : -1;
+        coming[i] = p.rows[(size_t)t * kManyRows + m];
+        if (m >= rows) coming[i] = -1;
       }
     };
-    auto load_y0 = [&](int g, int turn) {
-#pragma unroll
-      for (int c = 0; c < CB; ++c) {
-        const int col = (g % NG) * 256 + (turn * CB + c) * 128 + first;
-        if (col < p.N) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (coming[i] >= 0) y[c][i].load(p, (size_t)coming[i] * p.N + col);
-        }
-      }
-    };
-    int g = mine.next<true>(&ws), then = groups;
+    int g = mine.next<true>(rank, &ws), then = groups;
     if (g >= 0 && g < groups) {
       enter(g);
-      load_y0(g, 0);
+#pragma unroll
+      for (int a = 0; a < AHEAD; ++a) {
+        const int col = (g % NG) * 256 + a * 128 + first;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (coming[i] >= 0 && col < p.N) y[a][i].load(p, (size_t)coming[i] * p.N + col);
+      }
     }
     while (g >= 0 && g < groups && ok) {
-      const int rank = rank_ahead;
 #pragma unroll
       for (int i = 0; i < 4; ++i) row[i] = coming[i];
+      then = mine.next<true>(then_rank, &ws);
+      const bool more = then >= 0 && then < groups;
+      if (more) enter(then);
 #pragma unroll
-      for (int turn = 0; turn < TURNS; ++turn) {
+      for (int turn = 0; turn < 2; ++turn) {
         if (!ok) break;
-        const bool last = turn + 1 == TURNS;
-        if (last) {
-          then = mine.next<true>(&ws);
-          if (then >= 0 && then < groups) enter(then);
-        }
-        const int buf = n & 1;
+        const int buf = n & 1, col = (g % NG) * 256 + turn * 128 + first;
         if (rank > 0) {
           ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
           ++n;
           tc::tc_fence_after();
         }
         if (!ok) break;
+        Oct<Y0B>(&now)[4] = y[AHEAD == 2 ? turn : 0];
+        // what comes into the same registers: this group's second block, or the next group's
+        const bool own = AHEAD == 1 && turn == 0;
+        const int next_col = own ? col + 128 : more ? (then % NG) * 256 + (AHEAD == 2 ? turn * 128 : 0) + first : p.N;
 #pragma unroll
-        for (int c = 0; c < CB; ++c) {
-          const int col = (g % NG) * 256 + (turn * CB + c) * 128 + first;
+        for (int h = 0; h < 2; ++h) {                   // sixteen rows
+          uint32_t u[16];
+          if (rank > 0) {
+            tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
+            tc::tmem_ld_wait();
+          } else {
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {                 // sixteen rows
-            uint32_t u[16];
-            if (rank > 0) {
-              tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + (buf * CB + c) * 128 + (warp >> 2) * 32, u);
-              tc::tmem_ld_wait();
-            } else {
+            for (int i = 0; i < 16; ++i) u[i] = 0u;
+          }
 #pragma unroll
-              for (int i = 0; i < 16; ++i) u[i] = 0u;
+          for (int k = 0; k < 2; ++k) {
+            const int i = 2 * h + k;
+            float o[8];
+            now[i].values(o);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
+              o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
             }
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const int i = 2 * h + k;
-              float o[8];
-              y[c][i].values(o);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
-                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
-              }
-              if (row[i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[i] * p.N + col, o);
-            }
+            if (row[i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[i] * p.N + col, o);
           }
         }
         if (rank > 0) {
@@ -508,34 +535,48 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
         }
-        if (!last) load_y0(g, turn + 1);
-        else if (then >= 0 && then < groups) load_y0(then, 0);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int r = own ? row[i] : coming[i];
+          if (r >= 0 && next_col < p.N) now[i].load(p, (size_t)r * p.N + next_col);
+        }
       }
       g = then;
+      rank = then_rank;
     }
   } else if (warp == kCopyWarp) {
     // ---- draws the groups; copies a tile's images of T, and images of B: a stage is 128 columns of up to 64 ranks
     if (lane == 0) {
-      int it = 0, tiles = 0, at = -1;
-      for (int k = 0, g = blockIdx.x, then; ok; g = then, ++k) {
+      int it = 0, tiles = 0, at = -1, rank = 0, slot = -1;
+      for (int k = 0, g = blockIdx.x, then = groups; ok; g = then, ++k) {
+        if (g < groups && g / NG != at) {
+          at = g / NG;
+          slot = p.tiles[at].slot;
+          rank = rank_of(p, slot, load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes), true);
+        } else {
+          at = -2 - at;                                 // the same tile
+        }
         ok = tc::mbar_wait(bar_of(bars.taken[k & 1]), ((k >> 1) & 1) ^ 1, &ws);
         if (!ok) break;
-        list[k & 1] = g;
+        list[k & 1].x = g;
+        list[k & 1].y = rank;
         tc::mbar_arrive(bar_of(bars.drawn[k & 1]));
+        if (k == 0) tc::pdl_wait();                     // for the counter and T
         if (g >= groups) break;
-        then = (int)gridDim.x + atomicAdd(mp.next_group, 1);
-        int slot;
-        const int t = g / NG, rank = rank_at(t, slot, false), slabs = (rank + 63) / 64;
-        if (rank > 0 && t != at) {
-          at = t;
-          if (tiles > 0) ok = tc::mbar_wait(bar_of(bars.t_empty), (tiles - 1) & 1, &ws);
+        then = (int)gridDim.x + atomicAdd(mp.drawn, 1);
+        const int slabs = (rank + 63) / 64;
+        if (at < 0) {
+          at = -2 - at;
+        } else if (rank > 0) {
+          const int set = tiles % mp.t_sets, use = tiles / mp.t_sets;
+          if (use > 0) ok = tc::mbar_wait(bar_of(bars.t_empty[set]), (use - 1) & 1, &ws);
           if (!ok) break;
           ++tiles;
-          tc::mbar_expect_tx(bar_of(bars.t_full), TP * slabs * kXImage);
+          tc::mbar_expect_tx(bar_of(bars.t_full[set]), TP * slabs * kXImage);
           for (int x = 0; x < TP; ++x)
             for (int s = 0; s < slabs; ++s)
-              tc::bulk_load(tc::smem_u32(smem + (size_t)(x * max_slabs + s) * kXImage), mp.images + ((size_t)(t * TP + x) * max_slabs + s) * kXImage,
-                            kXImage, bar_of(bars.t_full));
+              tc::bulk_load(tc::smem_u32(smem + set * t_bytes + (size_t)(x * max_slabs + s) * kXImage),
+                            mp.images + ((size_t)(at * TP + x) * max_slabs + s) * kXImage, kXImage, bar_of(bars.t_full[set]));
         }
         const int c0 = (g % NG) * 2, stages = (min(c0 + 2, NC) - c0) * slabs;
         const uint8_t* B = p.pool + (size_t)max(slot, 0) * p.slot_bytes + 256 + a_bytes(p.K, p.max_rank) + (size_t)c0 * slabs * image;
@@ -549,8 +590,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
       }
       // after a wait that ran out: no copy is left in flight
       const long long t0 = clock64();
-      if (!ok && tiles > 0)
-        while (!tc::mbar_try_wait(bar_of(bars.t_full), (tiles - 1) & 1) && clock64() - t0 < mp.wait_limit) {}
+      for (int k = 0; k < mp.t_sets && !ok && k < tiles; ++k) {
+        const int set = (tiles - 1 - k) % mp.t_sets, use = (tiles - 1 - k) / mp.t_sets;
+        while (!tc::mbar_try_wait(bar_of(bars.t_full[set]), use & 1) && clock64() - t0 < mp.wait_limit) {}
+      }
       for (int k = 0; k < mp.stages && !ok && k < it; ++k) {
         const int last = it - 1 - k, st = last % mp.stages, turn = last / mp.stages;
         while (!tc::mbar_try_wait(bar_of(bars.copied[st]), turn & 1) && clock64() - t0 < 2 * mp.wait_limit) {}
@@ -560,36 +603,34 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
     // ---- MMAs
     if (lane == 0) {
       const uint32_t idesc = tc::make_idesc(128, 128);
-      int it = 0, n = 0, tiles = 0, at = -1;
-      for (int g = mine.next<false>(&ws); g >= 0 && g < groups && ok; g = mine.next<false>(&ws)) {
-        int slot;
-        const int t = g / NG, rank = rank_at(t, slot, false), slabs = (rank + 63) / 64, r16 = rank16(rank);
+      int it = 0, n = 0, tiles = 0, at = -1, rank;
+      for (int g = mine.next<false>(rank, &ws); g >= 0 && g < groups && ok; g = mine.next<false>(rank, &ws)) {
+        const int t = g / NG, slabs = (rank + 63) / 64, r16 = rank16(rank);
         if (rank == 0) continue;
         if (t != at) {
           at = t;
-          if (tiles > 0) tc::umma_commit(bar_of(bars.t_empty));              // once what was issued so far is done
-          ok = tc::mbar_wait(bar_of(bars.t_full), tiles++ & 1, &ws);
+          if (tiles > 0) tc::umma_commit(bar_of(bars.t_empty[(tiles - 1) % mp.t_sets]));         // once what was issued so far is done
+          ok = tc::mbar_wait(bar_of(bars.t_full[tiles % mp.t_sets]), tiles / mp.t_sets & 1, &ws);
+          ++tiles;
         }
-        for (int turn = 0; turn < TURNS && ok; ++turn, ++n) {
+        const uint8_t* T = smem + (tiles - 1) % mp.t_sets * t_bytes;
+        for (int turn = 0; turn < 2 && ok; ++turn, ++n) {
           ok = tc::mbar_wait(bar_of(bars.acc_empty[n & 1]), ((n >> 1) & 1) ^ 1, &ws);
           tc::tc_fence_after();
-          for (int c = 0; c < CB && ok; ++c) {
-            if ((g % NG) * 2 + turn * CB + c >= NC) continue;
-            const uint32_t d = tmem + ((n & 1) * CB + c) * 128;
-            for (int s = 0; s < slabs && ok; ++s, ++it) {
-              const int st = it % mp.stages, round = it / mp.stages;
-              ok = tc::mbar_wait(bar_of(bars.copied[st]), round & 1, &ws);
-              if (!ok) break;
-              tc::tc_fence_after();
-              const uint64_t b = image_desc(tc::smem_u32(ring + (size_t)st * image), pitch);
-              const int steps = min(4, r16 - s * 4);
+          const int stages = (g % NG) * 2 + turn < NC ? slabs : 0;
+          for (int s = 0; s < stages && ok; ++s, ++it) {
+            const int st = it % mp.stages, round = it / mp.stages;
+            ok = tc::mbar_wait(bar_of(bars.copied[st]), round & 1, &ws);
+            if (!ok) break;
+            tc::tc_fence_after();
+            const uint64_t b = image_desc(tc::smem_u32(ring + (size_t)st * image), pitch);
+            const int steps = min(4, r16 - s * 4);
 #pragma unroll
-              for (int x = TP - 1; x >= 0; --x) {
-                const uint64_t a = image_desc(tc::smem_u32(smem + (size_t)(x * max_slabs + s) * kXImage), 128);
-                for (int h = 0; h < steps; ++h) umma(d, a + 2 * h, b + 2 * h, idesc, s > 0 || h > 0 || x < TP - 1 ? 1u : 0u);
-              }
-              tc::umma_commit(bar_of(bars.empty[st]));
+            for (int x = TP - 1; x >= 0; --x) {
+              const uint64_t a = image_desc(tc::smem_u32(T + (size_t)(x * max_slabs + s) * kXImage), 128);
+              for (int h = 0; h < steps; ++h) umma(tmem + (n & 1) * 128, a + 2 * h, b + 2 * h, idesc, s > 0 || h > 0 || x < TP - 1 ? 1u : 0u);
             }
+            tc::umma_commit(bar_of(bars.empty[st]));
           }
           if (ok) tc::umma_commit(bar_of(bars.acc_full[n & 1]));
         }
@@ -602,7 +643,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   if (tid == 0 && ws.abort != 0) report_error(&p.plan->status, LQER_ERR_TIMEOUT, 811);
   if (warp == kMmaWarp) {
     tc::tc_fence_after();
-    tc::tmem_dealloc(tmem, 256 * CB);
+    tc::tmem_dealloc(tmem, 256);
   }
 }
 
@@ -643,14 +684,15 @@ template <bool Y0B, bool YB>
 static cudaError_t launch_expand(ManyParams mp, int ctas, cudaStream_t s) {
   static OncePerDevice once;
   const size_t t = (size_t)(YB ? 2 : 3) * ((mp.p.max_rank + 63) / 64) * kXImage, image = (size_t)128 * b_pitch(mp.p.max_rank);
-  mp.stages = (int)((kSmemMost - 1024 - t) / image);
+  mp.t_sets = 2 * t + 2 * image + 1024 <= kSmemMost ? 2 : 1;
+  mp.stages = (int)((kSmemMost - 1024 - mp.t_sets * t) / image);
   if (mp.stages > kMaxStages) mp.stages = kMaxStages;
-  return launch(expand_kernel<Y0B, YB>, once, mp, ctas, kManyThreads, t + mp.stages * image + 1024, s);
+  return launch(expand_kernel<Y0B, YB>, once, mp, ctas, kManyThreads, mp.t_sets * t + mp.stages * image + 1024, s);
 }
 cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s) {
   const int sms = sm_count(), ctas = sms < kPrologueMaxCtas ? sms : kPrologueMaxCtas;
   uint8_t* images = static_cast<uint8_t*>(scratch) + partial_bytes(tiles, p.max_rank);
-  ManyParams mp{p, static_cast<float4*>(scratch), images, reinterpret_cast<int*>(images + image_bytes(tiles, p.max_rank)), ctas, 0,
+  ManyParams mp{p, static_cast<float4*>(scratch), images, reinterpret_cast<int*>(images + image_bytes(tiles, p.max_rank)), ctas, 0, 1,
                 take_stall(kFamDecode) ? 1 : 0, wait_limit_cycles()};
   LaunchScope scope(kFamDecode, s, 3);
   cudaError_t e = x_type == kXF32    ? (p.y_bf16 ? launch_project<kXF32, 2>(mp, s) : launch_project<kXF32, 3>(mp, s))
@@ -659,7 +701,7 @@ cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, c
   if (e != cudaSuccess) return e;
   static OncePerDevice once[2];
   const int eights = tiles * ((p.max_rank + 63) / 64) * 8;
-  e = p.y_bf16 ? launch(finish_kernel<2>, once[0], mp, eights, 128, 0, s) : launch(finish_kernel<3>, once[1], mp, eights, 128, 0, s);
+  e = p.y_bf16 ? launch(finish_kernel<2>, once[0], mp, eights, 256, 0, s) : launch(finish_kernel<3>, once[1], mp, eights, 256, 0, s);
   if (e != cudaSuccess) return e;
   return p.y0_bf16 ? (p.y_bf16 ? launch_expand<true, true>(mp, ctas, s) : launch_expand<true, false>(mp, ctas, s))
                    : (p.y_bf16 ? launch_expand<false, true>(mp, ctas, s) : launch_expand<false, false>(mp, ctas, s));
