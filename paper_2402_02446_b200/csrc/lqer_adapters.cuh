@@ -125,22 +125,36 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&w)[4][P])
 template <int XT>
 struct XOct {
   uint4 a, b;                // fp32: both; bf16: a; MXINT8: a.x, a.y mantissas, a.z exponent byte
-  __device__ __forceinline__ void load(const Params& p, int row, int col, bool in) {
+  struct Place {
+    const uint8_t* x;
+    const uint8_t* e;        // MXINT8: of the exponent byte
+    __device__ __forceinline__ void set(const Params& p, int row, int col) {
+      const size_t idx = (size_t)row * p.K + col;
+      x = static_cast<const uint8_t*>(p.X) + idx * (XT == kXF32 ? 4 : XT == kXBF16 ? 2 : 1);
+      if (XT == kXMXINT8) e = static_cast<const uint8_t*>(p.X) + (size_t)p.M * p.K + (idx >> 4);      // K is a multiple of 16
+    }
+    __device__ __forceinline__ void next_slab() {
+      x += 64 * (XT == kXF32 ? 4 : XT == kXBF16 ? 2 : 1);
+      if (XT == kXMXINT8) e += 4;
+    }
+  };
+  __device__ __forceinline__ void load(const Params& p, const Place& at, bool in) {
     if (!in) {
       a = b = make_uint4(0u, 0u, 0u, 0u);
       if (XT == kXMXINT8) a.z = 127u;
-      return;
-    }
-    const size_t idx = (size_t)row * p.K + col;
-    if (XT == kXF32) {
-      ld32(static_cast<const float*>(p.X) + idx, p.x_wide, a, b);
+    } else if (XT == kXF32) {
+      ld32(at.x, p.x_wide, a, b);
     } else if (XT == kXBF16) {
-      a = ld16_once(static_cast<const uint16_t*>(p.X) + idx);
+      a = ld16_once(at.x);
     } else {
-      const uint8_t* x = static_cast<const uint8_t*>(p.X);
-      const uint2 m = __ldg(reinterpret_cast<const uint2*>(x + idx));
-      a = make_uint4(m.x, m.y, __ldg(x + (size_t)p.M * p.K + (size_t)row * (p.K / 16) + (col >> 4)), 0u);
+      const uint2 m = __ldg(reinterpret_cast<const uint2*>(at.x));
+      a = make_uint4(m.x, m.y, __ldg(at.e), 0u);
     }
+  }
+  __device__ __forceinline__ void load(const Params& p, int row, int col, bool in) {
+    Place at;
+    at.set(p, row, col);
+    load(p, at, in);
   }
   template <int P>
   __device__ __forceinline__ void pairs(const Params& p, uint32_t (&w)[4][P]) const {

@@ -139,7 +139,7 @@ __device__ __forceinline__ int project_rank16(const Params& p, int tile, int& sl
 
 template <int XT, int XP>
 __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_constant__ ManyParams mp) {
-  constexpr int AHEAD = XT == kXF32 ? 3 : 6;            // slabs whose X is on its way
+  constexpr int AHEAD = XT == kXF32 ? 2 : 6;            // slabs whose X is on its way (fp32: more would not fit the registers)
   constexpr int RW = 128 / kWorkWarps / 4;              // rows of a lane: eight lanes a row
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
@@ -176,22 +176,27 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
     int it = 0, runs = 0;
     const uint32_t piece = lane & 7;
     while (ok && walk.next(r)) {
-      int row[RW];
+      typename XOct<XT>::Place from[RW];                // of the octet that is sent for next
       uint32_t at[RW];
+      int col = r.slab * 64 + piece * 8;
+      const int stop = min((r.slab + r.slabs) * 64, p.K);
 #pragma unroll
       for (int i = 0; i < RW; ++i) {
         const int m = (warp * RW + i) * 4 + (lane >> 3);
-        row[i] = p.rows[(size_t)r.tile * kManyRows + m];
+        from[i].set(p, p.rows[(size_t)r.tile * kManyRows + m], col);
         at[i] = swizzled(m, piece, 128);
       }
       XOct<XT> x[AHEAD][RW];
-      auto load = [&](XOct<XT> (&o)[RW], int s) {
-        const int col = (r.slab + s) * 64 + piece * 8;
+      auto load = [&](XOct<XT> (&o)[RW]) {              // the next slab's
 #pragma unroll
-        for (int i = 0; i < RW; ++i) o[i].load(p, row[i], col, s < r.slabs && col < p.K);
+        for (int i = 0; i < RW; ++i) {
+          o[i].load(p, from[i], col < stop);
+          from[i].next_slab();
+        }
+        col += 64;
       };
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) load(x[a], a);
+      for (int a = 0; a < AHEAD; ++a) load(x[a]);
       int slot;
       const int r16 = project_rank16(p, r.tile, slot);
       for (int s0 = 0; s0 < r.slabs && ok; s0 += AHEAD) {
@@ -210,7 +215,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
 #pragma unroll
                 for (int k = 0; k < XP; ++k) *reinterpret_cast<uint4*>(img + k * kXImage + at[i]) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
               }
-              load(x[a], s0 + a + AHEAD);
+              load(x[a]);
               tc::fence_proxy_async_smem();
               __syncwarp();
               if (lane == 0) tc::mbar_arrive(bar_of(bars.full[st]));
@@ -547,7 +552,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   } else if (warp == kCopyWarp) {
     // ---- draws the groups; copies a tile's images of T, and images of B: a stage is 128 columns of up to 64 ranks
     if (lane == 0) {
-      int it = 0, tiles = 0, at = -1, rank = 0, slot = -1;
+      int it = 0, tiles = 0, at = -1, rank = 0, slot = -1, left = 0;
       for (int k = 0, g = blockIdx.x, then = groups; ok; g = then, ++k) {
         if (g < groups && g / NG != at) {
           at = g / NG;
@@ -563,7 +568,15 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
         tc::mbar_arrive(bar_of(bars.drawn[k & 1]));
         if (k == 0) tc::pdl_wait();                     // for the counter and T
         if (g >= groups) break;
-        then = (int)gridDim.x + atomicAdd(mp.drawn, 1);
+        if (left > 0) {
+          --left;
+          then = g + 1;
+        } else {
+          // several neighbours at a time (one T for all) as long as there is much left
+          const int take = g + 16 * (int)gridDim.x < groups ? 4 : g + 6 * (int)gridDim.x < groups ? 2 : 1;
+          then = (int)gridDim.x + atomicAdd(mp.drawn, take);
+          left = take - 1;
+        }
         const int slabs = (rank + 63) / 64;
         if (at < 0) {
           at = -2 - at;
