@@ -155,6 +155,11 @@ __device__ __forceinline__ void mma(float (&d)[4], uint32_t a0, uint32_t a1, uin
       : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
       : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+template <int BYTES>
+__device__ __forceinline__ void copy_async(uint32_t dst, const void* src) {
+  if (BYTES == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+  else asm volatile("cp.async.ca.shared.global [%0], [%1], 8;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void st_dsmem_f4(float* p, uint32_t cta, const float4& v) {
   asm volatile("{\n .reg .b32 ra;\n mapa.shared::cluster.u32 ra, %0, %1;\n st.shared::cluster.v4.f32 [ra], {%2, %3, %4, %5};\n}\n"
                ::"r"(tc::smem_u32(p)), "r"(cta), "f"(v.x), "f"(v.y), "f"(v.z), "f"(v.w) : "memory");
@@ -209,11 +214,57 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
   const uint8_t* A = slot + 256;
   const uint8_t* B = slot + 256 + a_bytes(p.K, p.max_rank);
 
-  // ---- T's share of this CTA: K blocks of 32, dealt to the warps in turn.  Factor rows (ranks) g and g + 8 of each sixteen, tokens g.
+  // ---- The factors' pieces, first of A and then of B, come through a ring of the warp's own in shared memory, AHEAD sets ahead of their
+  // use; a lane reads what it copied itself.  So the first of B are on their way while T is being exchanged.
+  constexpr int SC = PITCH == 128 ? 2 : 1;              // steps of a row of B's image
+  constexpr int AHEAD = PITCH == 128 ? 2 : 4, SET = SC * (PITCH == 32 ? 1024 : 2048);
   const int KB = (p.K + 31) / 32, kb_lo = KB * q / c, kb_hi = KB * (q + 1) / c;
-  const bool xpack = XP > 1 && tile.rows <= XS;
+  const int slabs = (rank + 63) / 64, steps = (rank + RB - 1) / RB;
+  const uint8_t* ring = reinterpret_cast<const uint8_t*>(sums + c * 8 * ld) + warp * AHEAD * SET;
   const uint8_t* a_lane = A + g * 128;                  // ranks g and, 1024 bytes on, g + 8; the swizzle's share is the row's index, g
   const uint32_t piece0 = (t ^ (g & 3)) << 4, flip = (g & 4) << 4;
+  int s_n0 = kb_lo + warp < kb_hi ? 0 : r16, s_kb = kb_lo + warp, s_nb = nb_lo + warp, s_slab = 0, s_set = 0, set = 0;
+  auto send = [&]() {
+    const uint32_t to = tc::smem_u32(ring + s_set * SET);
+    if (s_n0 < r16) {
+      const uint8_t* a = a_lane + ((size_t)(s_kb >> 1) * r16 + s_n0) * 2048 + (piece0 | (flip ^ (s_kb & 1) << 6));
+#pragma unroll
+      for (int j = 0; j < RC; ++j)
+        if (s_n0 + j < r16) {
+          copy_async<16>(to + (2 * j * 32 + lane) * 16, a + j * 2048);
+          copy_async<16>(to + ((2 * j + 1) * 32 + lane) * 16, a + j * 2048 + 1024);
+        }
+      s_kb += kWarps;
+      if (s_kb >= kb_hi) { s_kb = kb_lo + warp; s_n0 += RC; }
+    } else if (s_nb < nb_hi) {
+      // column 4 g + i of 32 of the block; the swizzle goes by the image's row modulo 8
+      const uint8_t* b = B + ((size_t)(s_nb >> 2) * slabs + s_slab) * 128 * PITCH + ((s_nb & 3) * 32 + 16 * (g & 1) + 2 * (g >> 1)) * PITCH;
+#pragma unroll
+      for (int h = 0; h < SC; ++h)
+        if (s_slab * SC + h < steps) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const uint32_t row = 2 * (g >> 1) + (i & 1), at = (8 * (i >> 1) + (i & 1)) * PITCH;
+            if (PITCH > 32) copy_async<16>(to + ((h * 4 + i) * 32 + lane) * 16, b + at + (((h * 4 + t) ^ (PITCH == 128 ? row : row >> 1)) << 4));
+            else copy_async<8>(to + (i * 32 + lane) * 8, b + at + (((t >> 1) ^ (row >> 2)) << 4) + (t & 1) * 8);
+          }
+        }
+      if (++s_slab == slabs) { s_slab = 0; s_nb += kWarps; }
+    }
+    asm volatile("cp.async.commit_group;" ::: "memory");
+    s_set = s_set + 1 == AHEAD ? 0 : s_set + 1;
+  };
+  auto arrived = [&]() {                                // the oldest set under way
+    asm volatile("cp.async.wait_group %0;" ::"n"(AHEAD - 1) : "memory");
+    const uint8_t* at = ring + set * SET;
+    set = set + 1 == AHEAD ? 0 : set + 1;
+    return at;
+  };
+#pragma unroll
+  for (int i = 0; i < AHEAD; ++i) send();
+
+  // ---- T's share of this CTA: K blocks of 32, dealt to the warps in turn.  Factor rows (ranks) g and g + 8 of each sixteen, tokens g.
+  const bool xpack = XP > 1 && tile.rows <= XS;
   const int x_row = xpack ? __shfl_sync(0xFFFFFFFFu, row_g, (g % XS) * 4) : row_g, x_part = g / XS;
   for (int n0 = 0; n0 < r16; n0 += RC) {
     const int nn = min(RC, r16 - n0);
@@ -226,14 +277,6 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
     int kb = kb_lo + warp;
     x.load(p, x_row, kb * 32 + 8 * t, kb < kb_hi && kb * 32 + 8 * t < p.K);
     for (; kb < kb_hi; kb += kWarps) {
-      uint4 f0[RC], f1[RC];
-      const uint8_t* a = a_lane + ((size_t)(kb >> 1) * r16 + n0) * 2048 + (piece0 | (flip ^ (kb & 1) << 6));
-#pragma unroll
-      for (int j = 0; j < RC; ++j)
-        if (j < nn) {
-          f0[j] = ld16(a + j * 2048);
-          f1[j] = ld16(a + j * 2048 + 1024);
-        }
       uint32_t w[4][XP];
       x.template pairs<XP>(p, w);
       const int next = kb + kWarps;
@@ -247,19 +290,22 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
           w[i][0] = m;
         }
       }
+      const uint4* f = reinterpret_cast<const uint4*>(arrived()) + lane;
 #pragma unroll
       for (int j = 0; j < RC; ++j)
         if (j < nn) {
+          const uint4 f0 = f[2 * j * 32], f1 = f[(2 * j + 1) * 32];
           float d[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
           for (int k = XP - 1; k >= 0; --k)
             if (k == 0 || !xpack) {
-              mma(d, f0[j].x, f1[j].x, f0[j].y, f1[j].y, w[0][k], w[1][k]);
-              mma(d, f0[j].z, f1[j].z, f0[j].w, f1[j].w, w[2][k], w[3][k]);
+              mma(d, f0.x, f1.x, f0.y, f1.y, w[0][k], w[1][k]);
+              mma(d, f0.z, f1.z, f0.w, f1.w, w[2][k], w[3][k]);
             }
 #pragma unroll
           for (int i = 0; i < 4; ++i) acc[j][i] += d[i];
         }
+      send();
     }
     float* mine = part + (warp * 8 + 2 * t) * ld + n0 * 16 + g;
 #pragma unroll
@@ -304,7 +350,6 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
   tc::cluster_barrier();
   // ---- fragments of T: column g, ranks RB / 4 * t ... of a step; one set for each part, or one for all side by side
   constexpr int RL = RB / 4;                            // ranks of a lane in a step: 8 or 4
-  const int steps = (rank + RB - 1) / RB;
   uint32_t* frags = reinterpret_cast<uint32_t*>(part);  // [step][part][lane][RL / 2]
   for (int i = tid; i < steps * 32; i += kThreads) {
     const int col = (i >> 2) & 7, first = (i >> 5) * RB + (i & 3) * RL, token = tpack ? col % TS : col;
@@ -343,29 +388,26 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
   __syncthreads();
   // ---- the CTA's columns of Y: blocks of 32, dealt to the warps in turn; a lane's four columns 4 g .. 4 g + 3 are rows g and g + 8
   // of two MMAs
-  constexpr int SC = PITCH == 128 ? 2 : 1;              // steps of a row of B's image: their fragments are on their way together
-  const int slabs = (rank + 63) / 64;
   const uint32_t* fr = frags + lane * (RL / 2);
   for (; nb < nb_hi; nb += kWarps, col += kWarps * 32) {
-    const uint8_t* b = B + (size_t)(nb >> 2) * slabs * 128 * PITCH + ((nb & 3) * 32 + 16 * (g & 1) + 2 * (g >> 1)) * PITCH;
     float acc[2][4];
 #pragma unroll
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    for (int s0 = 0; s0 < steps; s0 += SC, b += 128 * PITCH) {
+    for (int s0 = 0; s0 < steps; s0 += SC) {
+      const uint8_t* at = arrived();
       uint32_t f[SC][4][RL / 2];
 #pragma unroll
       for (int h = 0; h < SC; ++h)
         if (s0 + h < steps) {
 #pragma unroll
-          for (int i = 0; i < 4; ++i) {                 // column 4 g + i of 32; the swizzle goes by the image's row modulo 8
-            const uint32_t row = 2 * (g >> 1) + (i & 1), at = (8 * (i >> 1) + (i & 1)) * PITCH;
+          for (int i = 0; i < 4; ++i) {
             if (PITCH > 32) {
-              const uint4 u = ld16(b + at + (((h * 4 + t) ^ (PITCH == 128 ? row : row >> 1)) << 4));
+              const uint4 u = reinterpret_cast<const uint4*>(at)[(h * 4 + i) * 32 + lane];
               f[h][i][0] = u.x; f[h][i][1] = u.y; f[h][i][RL / 2 - 2] = u.z; f[h][i][RL / 2 - 1] = u.w;
             } else {
-              const uint2 u = __ldg(reinterpret_cast<const uint2*>(b + at + (((t >> 1) ^ (row >> 2)) << 4) + (t & 1) * 8));
+              const uint2 u = reinterpret_cast<const uint2*>(at)[i * 32 + lane];
               f[h][i][0] = u.x; f[h][i][1] = u.y;
             }
           }
@@ -386,6 +428,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
                   mma(acc[j], f[h][2 * j][k], f[h][2 * j + 1][k], f[h][2 * j][k + 1], f[h][2 * j + 1][k + 1], w[k], w[k + 1]);
             }
         }
+      send();
     }
     float4 va = ya.values(p), vb = yb.values(p);
     const int next = col + kWarps * 32;
@@ -415,7 +458,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
 template <int XT, int XP, int TP, int PITCH>
 static cudaError_t launch_few(const Params& p, int tiles, int c, cudaStream_t s) {
   const size_t part = (size_t)kWarps * 8 * part_stride(p.max_rank) * 4;    // the fragments of T fit in the same place
-  const size_t smem = part + (size_t)c * 8 * part_stride(p.max_rank) * 4;
+  const size_t smem = part + (size_t)c * 8 * part_stride(p.max_rank) * 4 + (size_t)kWarps * (PITCH == 128 ? 8192 : PITCH == 64 ? 8192 : 4096);
   static OncePerDevice once;
   cudaError_t e = once.run([] {
     return cudaFuncSetAttribute(few_rows_kernel<XT, XP, TP, PITCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
