@@ -172,6 +172,10 @@ __host__ __device__ constexpr int side_by_side(int parts) { return parts == 1 ? 
 // Floats from one column of partial sums to the next: a fragment's stores then go to 32 different banks.
 __host__ __device__ inline int part_stride(int max_rank) { return rank16(max_rank) * 16 + 4; }
 
+// A warp's ring of the factors' pieces: at rank 128 and eight CTAs to a tile two CTAs still fit an SM.
+__host__ __device__ constexpr int ring_sets(int pitch) { return pitch == 32 ? 4 : 3; }
+__host__ __device__ constexpr int ring_set_bytes(int pitch) { return pitch == 32 ? 1024 : 2048; }
+
 template <int XT, int XP, int TP, int PITCH>
 __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
   constexpr int RB = PITCH == 32 ? 16 : 32;             // ranks of a step of B
@@ -209,47 +213,49 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
   }
   asm volatile("barrier.cluster.arrive.release.aligned;" ::: "memory");    // waited for before the first remote store
   const int r16 = rank16(rank), ld = part_stride(p.max_rank);
-  float* part = reinterpret_cast<float*>(smem);         // [warp][column][ld], and then [lane][...] the fragments of T
-  float* sums = part + kWarps * 8 * ld;                 // [CTA of the cluster][token][ld]
+  float* part = reinterpret_cast<float*>(smem);         // [two warps][column][ld], and then [lane][...] the fragments of T
+  float* sums = part + kWarps / 2 * 8 * ld;              // [CTA of the cluster][token][ld]
   const uint8_t* A = slot + 256;
   const uint8_t* B = slot + 256 + a_bytes(p.K, p.max_rank);
 
   // ---- The factors' pieces, first of A and then of B, come through a ring of the warp's own in shared memory, AHEAD sets ahead of their
   // use; a lane reads what it copied itself.  So the first of B are on their way while T is being exchanged.
-  constexpr int SC = PITCH == 128 ? 2 : 1;              // steps of a row of B's image
-  constexpr int AHEAD = PITCH == 128 ? 2 : 4, SET = SC * (PITCH == 32 ? 1024 : 2048);
+  // A set is a step of B's 32 columns, or two sixteens of A's ranks.
+  constexpr int AHEAD = ring_sets(PITCH), SET = ring_set_bytes(PITCH);
   const int KB = (p.K + 31) / 32, kb_lo = KB * q / c, kb_hi = KB * (q + 1) / c;
   const int slabs = (rank + 63) / 64, steps = (rank + RB - 1) / RB;
   const uint8_t* ring = reinterpret_cast<const uint8_t*>(sums + c * 8 * ld) + warp * AHEAD * SET;
   const uint8_t* a_lane = A + g * 128;                  // ranks g and, 1024 bytes on, g + 8; the swizzle's share is the row's index, g
   const uint32_t piece0 = (t ^ (g & 3)) << 4, flip = (g & 4) << 4;
-  int s_n0 = kb_lo + warp < kb_hi ? 0 : r16, s_kb = kb_lo + warp, s_nb = nb_lo + warp, s_slab = 0, s_set = 0, set = 0;
+  int s_n0 = kb_lo + warp < kb_hi ? 0 : r16, s_j = 0, s_kb = kb_lo + warp, s_nb = nb_lo + warp, s_step = 0, s_set = 0, set = 0;
   auto send = [&]() {
     const uint32_t to = tc::smem_u32(ring + s_set * SET);
     if (s_n0 < r16) {
-      const uint8_t* a = a_lane + ((size_t)(s_kb >> 1) * r16 + s_n0) * 2048 + (piece0 | (flip ^ (s_kb & 1) << 6));
+      const uint8_t* a = a_lane + ((size_t)(s_kb >> 1) * r16 + s_n0 + s_j) * 2048 + (piece0 | (flip ^ (s_kb & 1) << 6));
 #pragma unroll
-      for (int j = 0; j < RC; ++j)
-        if (s_n0 + j < r16) {
+      for (int j = 0; j < (RC > 1 ? 2 : 1); ++j)
+        if (s_n0 + s_j + j < r16) {
           copy_async<16>(to + (2 * j * 32 + lane) * 16, a + j * 2048);
           copy_async<16>(to + ((2 * j + 1) * 32 + lane) * 16, a + j * 2048 + 1024);
         }
-      s_kb += kWarps;
-      if (s_kb >= kb_hi) { s_kb = kb_lo + warp; s_n0 += RC; }
+      s_j += 2;
+      if (s_j >= RC || s_n0 + s_j >= r16) {
+        s_j = 0;
+        s_kb += kWarps;
+        if (s_kb >= kb_hi) { s_kb = kb_lo + warp; s_n0 += RC; }
+      }
     } else if (s_nb < nb_hi) {
       // column 4 g + i of 32 of the block; the swizzle goes by the image's row modulo 8
-      const uint8_t* b = B + ((size_t)(s_nb >> 2) * slabs + s_slab) * 128 * PITCH + ((s_nb & 3) * 32 + 16 * (g & 1) + 2 * (g >> 1)) * PITCH;
+      const int half = PITCH == 128 ? s_step & 1 : 0;
+      const uint8_t* b = B + ((size_t)(s_nb >> 2) * slabs + (PITCH == 128 ? s_step >> 1 : 0)) * 128 * PITCH +
+                         ((s_nb & 3) * 32 + 16 * (g & 1) + 2 * (g >> 1)) * PITCH;
 #pragma unroll
-      for (int h = 0; h < SC; ++h)
-        if (s_slab * SC + h < steps) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            const uint32_t row = 2 * (g >> 1) + (i & 1), at = (8 * (i >> 1) + (i & 1)) * PITCH;
-            if (PITCH > 32) copy_async<16>(to + ((h * 4 + i) * 32 + lane) * 16, b + at + (((h * 4 + t) ^ (PITCH == 128 ? row : row >> 1)) << 4));
-            else copy_async<8>(to + (i * 32 + lane) * 8, b + at + (((t >> 1) ^ (row >> 2)) << 4) + (t & 1) * 8);
-          }
-        }
-      if (++s_slab == slabs) { s_slab = 0; s_nb += kWarps; }
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t row = 2 * (g >> 1) + (i & 1), at = (8 * (i >> 1) + (i & 1)) * PITCH;
+        if (PITCH > 32) copy_async<16>(to + (i * 32 + lane) * 16, b + at + (((half * 4 + t) ^ (PITCH == 128 ? row : row >> 1)) << 4));
+        else copy_async<8>(to + (i * 32 + lane) * 8, b + at + (((t >> 1) ^ (row >> 2)) << 4) + (t & 1) * 8);
+      }
+      if (++s_step == steps) { s_step = 0; s_nb += kWarps; }
     }
     asm volatile("cp.async.commit_group;" ::: "memory");
     s_set = s_set + 1 == AHEAD ? 0 : s_set + 1;
@@ -290,32 +296,43 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
           w[i][0] = m;
         }
       }
-      const uint4* f = reinterpret_cast<const uint4*>(arrived()) + lane;
 #pragma unroll
-      for (int j = 0; j < RC; ++j)
-        if (j < nn) {
-          const uint4 f0 = f[2 * j * 32], f1 = f[(2 * j + 1) * 32];
-          float d[4] = {0.f, 0.f, 0.f, 0.f};
+      for (int j0 = 0; j0 < RC; j0 += 2)
+        if (j0 < nn) {
+          const uint4* f = reinterpret_cast<const uint4*>(arrived()) + lane;
 #pragma unroll
-          for (int k = XP - 1; k >= 0; --k)
-            if (k == 0 || !xpack) {
-              mma(d, f0.x, f1.x, f0.y, f1.y, w[0][k], w[1][k]);
-              mma(d, f0.z, f1.z, f0.w, f1.w, w[2][k], w[3][k]);
+          for (int j = j0; j < j0 + (RC > 1 ? 2 : 1); ++j)
+            if (j < nn) {
+              const uint4 f0 = f[2 * (j - j0) * 32], f1 = f[(2 * (j - j0) + 1) * 32];
+              float d[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+              for (int k = XP - 1; k >= 0; --k)
+                if (k == 0 || !xpack) {
+                  mma(d, f0.x, f1.x, f0.y, f1.y, w[0][k], w[1][k]);
+                  mma(d, f0.z, f1.z, f0.w, f1.w, w[2][k], w[3][k]);
+                }
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[j][i] += d[i];
             }
-#pragma unroll
-          for (int i = 0; i < 4; ++i) acc[j][i] += d[i];
+          send();
         }
-      send();
     }
-    float* mine = part + (warp * 8 + 2 * t) * ld + n0 * 16 + g;
+    // four places of partial sums: the upper four warps add theirs to the lower four's
+    float* mine = part + ((warp & 3) * 8 + 2 * t) * ld + n0 * 16 + g;
 #pragma unroll
-    for (int j = 0; j < RC; ++j)
-      if (j < nn) {
-        mine[j * 16] = acc[j][0];
-        mine[ld + j * 16] = acc[j][1];
-        mine[j * 16 + 8] = acc[j][2];
-        mine[ld + j * 16 + 8] = acc[j][3];
+    for (int turn = 0; turn < 2; ++turn) {
+      if (warp >> 2 == turn) {
+#pragma unroll
+        for (int j = 0; j < RC; ++j)
+          if (j < nn) {
+            mine[j * 16] = turn ? mine[j * 16] + acc[j][0] : acc[j][0];
+            mine[ld + j * 16] = turn ? mine[ld + j * 16] + acc[j][1] : acc[j][1];
+            mine[j * 16 + 8] = turn ? mine[j * 16 + 8] + acc[j][2] : acc[j][2];
+            mine[ld + j * 16 + 8] = turn ? mine[ld + j * 16 + 8] + acc[j][3] : acc[j][3];
+          }
       }
+      if (turn == 0) __syncthreads();
+    }
   }
   __syncwarp();
   asm volatile("barrier.cluster.wait.acquire.aligned;" ::: "memory");      // every CTA of the cluster is there to be written to
@@ -328,7 +345,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
     for (int k = XP - 1; k >= 0; --k)
       if (k == 0 || xpack) {
 #pragma unroll
-        for (int w = 0; w < kWarps; ++w) {
+        for (int w = 0; w < kWarps / 2; ++w) {
           const float4 v = *reinterpret_cast<const float4*>(part + (w * 8 + row + k * XS) * ld + quad * 4);
           s.x += v.x; s.y += v.y; s.z += v.z; s.w += v.w;
         }
@@ -395,38 +412,29 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
     for (int j = 0; j < 2; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) acc[j][i] = 0.f;
-    for (int s0 = 0; s0 < steps; s0 += SC) {
+    for (int s = 0; s < steps; ++s) {
       const uint8_t* at = arrived();
-      uint32_t f[SC][4][RL / 2];
+      uint32_t f[4][RL / 2];
 #pragma unroll
-      for (int h = 0; h < SC; ++h)
-        if (s0 + h < steps) {
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            if (PITCH > 32) {
-              const uint4 u = reinterpret_cast<const uint4*>(at)[(h * 4 + i) * 32 + lane];
-              f[h][i][0] = u.x; f[h][i][1] = u.y; f[h][i][RL / 2 - 2] = u.z; f[h][i][RL / 2 - 1] = u.w;
-            } else {
-              const uint2 u = reinterpret_cast<const uint2*>(at)[i * 32 + lane];
-              f[h][i][0] = u.x; f[h][i][1] = u.y;
-            }
-          }
+      for (int i = 0; i < 4; ++i) {
+        if (PITCH > 32) {
+          const uint4 u = reinterpret_cast<const uint4*>(at)[i * 32 + lane];
+          f[i][0] = u.x; f[i][1] = u.y; f[i][RL / 2 - 2] = u.z; f[i][RL / 2 - 1] = u.w;
+        } else {
+          const uint2 u = reinterpret_cast<const uint2*>(at)[i * 32 + lane];
+          f[i][0] = u.x; f[i][1] = u.y;
         }
+      }
 #pragma unroll
       for (int x = TP - 1; x >= 0; --x)
         if (x == 0 || !tpack) {
+          uint32_t w[RL / 2];
 #pragma unroll
-          for (int h = 0; h < SC; ++h)
-            if (s0 + h < steps) {
-              uint32_t w[RL / 2];
+          for (int k = 0; k < RL / 2; ++k) w[k] = fr[(s * TP + x) * 32 * (RL / 2) + k];
 #pragma unroll
-              for (int k = 0; k < RL / 2; ++k) w[k] = fr[((s0 + h) * TP + x) * 32 * (RL / 2) + k];
+          for (int j = 0; j < 2; ++j)
 #pragma unroll
-              for (int j = 0; j < 2; ++j)
-#pragma unroll
-                for (int k = 0; k < RL / 2; k += 2)
-                  mma(acc[j], f[h][2 * j][k], f[h][2 * j + 1][k], f[h][2 * j][k + 1], f[h][2 * j + 1][k + 1], w[k], w[k + 1]);
-            }
+            for (int k = 0; k < RL / 2; k += 2) mma(acc[j], f[2 * j][k], f[2 * j + 1][k], f[2 * j][k + 1], f[2 * j + 1][k + 1], w[k], w[k + 1]);
         }
       send();
     }
@@ -457,8 +465,8 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
 // ---------------------------------------------------------------------------- host
 template <int XT, int XP, int TP, int PITCH>
 static cudaError_t launch_few(const Params& p, int tiles, int c, cudaStream_t s) {
-  const size_t part = (size_t)kWarps * 8 * part_stride(p.max_rank) * 4;    // the fragments of T fit in the same place
-  const size_t smem = part + (size_t)c * 8 * part_stride(p.max_rank) * 4 + (size_t)kWarps * (PITCH == 128 ? 8192 : PITCH == 64 ? 8192 : 4096);
+  const size_t part = (size_t)kWarps / 2 * 8 * part_stride(p.max_rank) * 4;      // the fragments of T fit in the same place
+  const size_t smem = part + (size_t)c * 8 * part_stride(p.max_rank) * 4 + (size_t)kWarps * ring_sets(PITCH) * ring_set_bytes(PITCH);
   static OncePerDevice once;
   cudaError_t e = once.run([] {
     return cudaFuncSetAttribute(few_rows_kernel<XT, XP, TP, PITCH>, cudaFuncAttributeMaxDynamicSharedMemorySize, 200 * 1024);
