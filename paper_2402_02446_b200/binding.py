@@ -622,7 +622,7 @@ def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | Non
 
 
 def adapters_workspace_bytes(M: int, pool: AdapterPool, plan_slots: int | None = None) -> int:
-    """The workspace that apply_adapters needs for M rows: nothing up to 512."""
+    """The workspace that apply_adapters needs for M rows of a pool: nothing up to 512."""
     out = C.c_size_t()
     _check(lib().lqer_adapters_workspace_bytes(M, pool.ref, plan_slots or pool.n_slots, C.byref(out)), "lqer_adapters_workspace_bytes")
     return out.value
@@ -632,7 +632,7 @@ def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: to
                    cfg: Config | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Y[m] = Y0[m] + scale (X[m] A) B with the adapter of row m.  X [M, K] fp32 or bf16, or a flat MXINT8 buffer; Y0 [M, N] fp32 or
     bf16, the shared projection's output; Y of out_dtype (Y0's type where it is not given), or the given tensor, Y0 itself included.
-    ws: a workspace of adapters_workspace_bytes (more than 512 rows need one; made where none is given)."""
+    ws: a workspace of adapters_workspace_bytes (more than 512 rows may need one; made where none is given)."""
     index = X.get_device()
     if not _here(index):
         with torch.cuda.device(index):

@@ -15,7 +15,7 @@
 // Plan: the rows sorted by slot (stable) and cut into tiles of at most tile_rows rows of one slot.  It belongs to a batch, not to a
 // layer: a step of a model makes it once and uses it for every projection.
 //
-// Few rows (up to 512, few_rows_kernel): a cluster of CTAs takes a tile of up to 8 rows.  The factors are the MMA's 16-row operand, the tokens its 8
+// Few rows (up to 512, and up to 1024 of small products; few_rows_kernel): a cluster of CTAs takes a tile of up to 8 rows.  The factors are the MMA's 16-row operand, the tokens its 8
 // columns.  First the CTAs share the contraction over K, then each sends its part of T to all (distributed shared memory),
 // and then they share the columns of Y.  T never leaves the chip, and everything is summed in a fixed order.
 // Many rows: lqer_adapters_many.cu.
@@ -65,15 +65,22 @@ __global__ void adapter_load_kernel(uint8_t* slot, const void* A, const void* B,
 }
 
 // ---------------------------------------------------------------------------- plan
-// One CTA: a stable counting sort of the rows by slot (key n_slots: no adapter), then the tiles.  Each warp counts and places
-// a stretch of rows of its own, with cursors of its own, so that only the prefix sums in between go over the whole CTA.
+// One CTA: a stable counting sort of the rows by slot (key n_slots: no adapter), cut into tiles twice: of 8 rows and of 128 (either list
+// may be left out).  Each warp counts and places a stretch of rows of its own, with cursors of its own, so that only the prefix
+// sums in between go over the whole CTA.
+struct PlanList {
+  Tile* tiles;
+  int* rows;                 // an entry for each row of each tile; places behind a tile's last row name that row again
+  int tile_rows;             // 0: no such list
+};
 constexpr int kPlanThreads = 1024, kPlanWarps = 32;
-// rows: tile_rows entries a tile, the rows of the batch; places behind a tile's last row name that row again.
-__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restrict__ slots, int M, int n_slots, int tile_rows, PlanHead* head,
-                                                            Tile* tiles, int* rows) {
-  extern __shared__ int cursors[];                     // [bins][32 warps], then [bins + 1] tiles before a bin and [bins] rows before it
+__global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restrict__ slots, int M, int n_slots, PlanHead* head, const PlanList few,
+                                                            const PlanList many) {
+  extern __shared__ int cursors[];                     // [bins][32 warps], then [bins] rows before a bin and, for both lists, [bins + 1] tiles before it
   const int bins = n_slots + 1, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  int* tile_at = cursors + bins * kPlanWarps;
+  int* first_of = cursors + bins * kPlanWarps;
+  int* tile_at[2] = {first_of + bins, first_of + 2 * bins + 1};
+  const PlanList lists[2] = {few, many};
   __shared__ int bad, sums[kPlanWarps];
   tc::pdl_launch_dependents();
   tc::pdl_wait();
@@ -119,29 +126,48 @@ __global__ void __launch_bounds__(kPlanThreads) plan_kernel(const int* __restric
   // tiles: bin b holds rows [cursors[b][0], cursors[b + 1][0]) of the order
   const int brun = (bins + kPlanThreads - 1) / kPlanThreads, bfrom = min(tid * brun, bins), bto = min(bfrom + brun, bins);
   auto rows_of = [&](int b) { return (b + 1 < bins ? cursors[(b + 1) * kPlanWarps] : M) - cursors[b * kPlanWarps]; };
-  int mine_t = 0;
-  for (int b = bfrom; b < bto; ++b) mine_t += (rows_of(b) + tile_rows - 1) / tile_rows;
-  int t0 = scan(mine_t);
-  for (int b = bfrom; b < bto; ++b) {
-    tile_at[b] = t0;
-    const int n_rows = rows_of(b);
-    for (int r = 0; r < n_rows; r += tile_rows) tiles[t0++] = Tile{b < n_slots ? b : -1, min(tile_rows, n_rows - r)};
-  }
-  if (bto == bins && bfrom < bins) tile_at[bins] = t0;
-  int* first_of = tile_at + bins + 1;                  // a bin's first place in the order
   for (int b = bfrom; b < bto; ++b) first_of[b] = cursors[b * kPlanWarps];
+#pragma unroll
+  for (int l = 0; l < 2; ++l) {
+    const int per = lists[l].tile_rows;
+    if (per == 0) continue;
+    int mine_t = 0;
+    for (int b = bfrom; b < bto; ++b) mine_t += (rows_of(b) + per - 1) / per;
+    int t0 = scan(mine_t);
+    for (int b = bfrom; b < bto; ++b) {
+      tile_at[l][b] = t0;
+      const int n_rows = rows_of(b);
+      for (int r = 0; r < n_rows; r += per) lists[l].tiles[t0++] = Tile{b < n_slots ? b : -1, min(per, n_rows - r)};
+    }
+    if (bto == bins && bfrom < bins) tile_at[l][bins] = t0;
+  }
   __syncthreads();
-  if (tid == 0) *head = PlanHead{DeviceStatus{bad ? (int)LQER_ERR_BOUNDS : 0, 801, 0, 0}, kPlanMagic, M, n_slots, tile_rows, tile_at[bins], tile_at[n_slots]};
+  if (tid == 0) {
+    head->status = DeviceStatus{bad ? (int)LQER_ERR_BOUNDS : 0, 801, 0, 0};
+    head->magic = kPlanMagic;
+    head->M = M;
+    head->n_slots = n_slots;
+#pragma unroll
+    for (int l = 0; l < 2; ++l) {
+      head->of[l].n_tiles = lists[l].tile_rows > 0 ? tile_at[l][bins] : 0;
+      head->of[l].n_adapted = lists[l].tile_rows > 0 ? tile_at[l][n_slots] : 0;
+    }
+  }
   for (int at = lo; at < hi; at += 32) {
     const int row = at + lane, key = row < hi ? key_of(row) : -1;
     const unsigned same = __match_any_sync(0xFFFFFFFFu, key);
     if (key >= 0) {
       const int place = cursors[key * kPlanWarps + warp] + __popc(same & ((1u << lane) - 1u)) - first_of[key];
       const int end = (key + 1 < bins ? first_of[key + 1] : M) - first_of[key];
-      int* at_tile = rows + ((size_t)tile_at[key] + place / tile_rows) * tile_rows;
-      at_tile[place % tile_rows] = row;
-      if (place + 1 == end)
-        for (int i = place % tile_rows + 1; i < tile_rows; ++i) at_tile[i] = row;
+#pragma unroll
+      for (int l = 0; l < 2; ++l) {
+        const int per = lists[l].tile_rows;
+        if (per == 0) continue;
+        int* at_tile = lists[l].rows + ((size_t)tile_at[l][key] + place / per) * per;
+        at_tile[place % per] = row;
+        if (place + 1 == end)
+          for (int i = place % per + 1; i < per; ++i) at_tile[i] = row;
+      }
     }
     __syncwarp();
     if (key >= 0 && lane == __ffs(same) - 1) cursors[key * kPlanWarps + warp] += __popc(same);
@@ -190,7 +216,7 @@ __global__ void __launch_bounds__(kThreads, 2) few_rows_kernel(const Params p) {
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   // nothing here waits for anything else: the tile list is as long as the grid, whatever it holds
-  const PlanHead head = load_head(p.plan);
+  const ListHead head = load_head(p.plan, 0);
   const Tile tile = p.tiles[tile_id];
   const int row_g = p.rows[tile_id * kFewRows + g];
   const int row_0 = p.rows[tile_id * kFewRows + 2 * t], row_1 = p.rows[tile_id * kFewRows + 2 * t + 1];
@@ -498,9 +524,7 @@ static cudaError_t launch_few_rank(const Params& p, int tiles, int c, cudaStream
 }  // namespace ad
 
 size_t adapter_slot_bytes(int K, int N, int max_rank) { return ad::slot_bytes(K, N, max_rank); }
-size_t adapter_plan_bytes(int M, int n_slots) {
-  return 256 + ad::tiles_bytes(M, n_slots) + (((size_t)ad::max_tiles(M, n_slots) * ad::tile_rows_of(M) * 4 + 255) & ~(size_t)255);
-}
+size_t adapter_plan_bytes(int M, int n_slots) { return ad::plan_layout(M, n_slots).bytes; }
 cudaError_t launch_adapter_pool_init(void* pool, int K, int N, int max_rank, int n_slots, cudaStream_t s) {
   LaunchScope scope(kFamPack, s);
   ad::pool_init_kernel<<<(n_slots + 255) / 256, 256, 0, s>>>(static_cast<uint8_t*>(pool), ad::slot_bytes(K, N, max_rank), n_slots, K, N, max_rank);
@@ -515,9 +539,12 @@ cudaError_t launch_adapter_load(void* pool, int K, int N, int max_rank, int slot
 }
 cudaError_t launch_adapter_plan(const int* slots, int M, int n_slots, void* plan, cudaStream_t s) {
   uint8_t* at = static_cast<uint8_t*>(plan);
-  ad::Tile* tiles = reinterpret_cast<ad::Tile*>(at + 256);
-  int* rows = reinterpret_cast<int*>(at + 256 + ad::tiles_bytes(M, n_slots));
-  const size_t smem = (size_t)(n_slots + 1) * ad::kPlanWarps * 4 + (size_t)(2 * n_slots + 3) * 4;
+  const ad::PlanLayout l = ad::plan_layout(M, n_slots);
+  auto list = [&](int i) {
+    return ad::PlanList{reinterpret_cast<ad::Tile*>(at + l.tiles_at[i]), reinterpret_cast<int*>(at + l.rows_at[i]),
+                        l.tiles[i] == 0 ? 0 : i == 0 ? ad::kFewRows : ad::kManyRows};
+  };
+  const size_t smem = (size_t)(n_slots + 1) * (ad::kPlanWarps + 3) * 4 + 8;
   static OncePerDevice once;
   cudaError_t e = once.run([] { return cudaFuncSetAttribute(ad::plan_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024); });
   if (e != cudaSuccess) return e;
@@ -532,33 +559,37 @@ cudaError_t launch_adapter_plan(const int* slots, int M, int n_slots, void* plan
   cfg.attrs = attr;
   cfg.numAttrs = 1;
   LaunchScope scope(kFamDecode, s);
-  return cudaLaunchKernelEx(&cfg, ad::plan_kernel, slots, M, n_slots, ad::tile_rows_of(M), reinterpret_cast<ad::PlanHead*>(at), tiles, rows);
+  return cudaLaunchKernelEx(&cfg, ad::plan_kernel, slots, M, n_slots, reinterpret_cast<ad::PlanHead*>(at), list(0), list(1));
 }
-size_t adapter_scratch_bytes(int M, int plan_slots, int max_rank) {
-  return ad::tile_rows_of(M) > ad::kFewRows ? ad::many_scratch_bytes(M, plan_slots, max_rank) : 0;
+size_t adapter_scratch_bytes(int M, int plan_slots, int K, int N, int max_rank) {
+  return ad::takes_few(M, K, N, max_rank) ? 0 : ad::many_scratch_bytes(ad::plan_layout(M, plan_slots).tiles[1], max_rank);
 }
 cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, int K, int N, int max_rank, void* plan, int plan_slots,
                             const void* Y0, int y0_type, void* Y, int y_type, int bits, int emin, int emax, void* scratch, cudaStream_t s) {
   uint8_t* at = static_cast<uint8_t*>(plan);
-  const int most = ad::max_tiles(M, plan_slots);
+  const bool few = ad::takes_few(M, K, N, max_rank);
+  const ad::PlanLayout l = ad::plan_layout(M, plan_slots);
+  const int most = l.tiles[few ? 0 : 1];
   ad::Params p;
   p.X = X; p.pool = static_cast<const uint8_t*>(pool);
   p.plan = reinterpret_cast<ad::PlanHead*>(at);
-  p.tiles = reinterpret_cast<const ad::Tile*>(at + 256);
-  p.rows = reinterpret_cast<const int*>(at + 256 + ad::tiles_bytes(M, plan_slots));
+  p.tiles = reinterpret_cast<const ad::Tile*>(at + l.tiles_at[few ? 0 : 1]);
+  p.rows = reinterpret_cast<const int*>(at + l.rows_at[few ? 0 : 1]);
   p.Y0 = Y0; p.Y = Y;
   p.slot_bytes = ad::slot_bytes(K, N, max_rank);
-  p.M = M; p.K = K; p.N = N; p.max_rank = max_rank; p.plan_slots = plan_slots; p.tile_rows = ad::tile_rows_of(M);
+  p.M = M; p.K = K; p.N = N; p.max_rank = max_rank; p.plan_slots = plan_slots;
   p.y0_bf16 = y0_type == kYBF16; p.y_bf16 = y_type == kYBF16;
   p.x_wide = reinterpret_cast<uintptr_t>(X) % 32 == 0;
   p.y_wide = reinterpret_cast<uintptr_t>(Y0) % 32 == 0 && reinterpret_cast<uintptr_t>(Y) % 32 == 0;
   p.bits = bits; p.emin = emin; p.emax = emax;
   const size_t whole = y_bytes(y_type, M, N), less = debug_y_shrink();
   p.y_extent = whole > less ? whole - less : 0;
-  if (p.tile_rows > ad::kFewRows) return ad::launch_many(p, x_type, most, scratch, s);
-  // CTAs to a tile: as many, up to eight, as fit two to an SM, but no more than there are blocks of K or of columns for.
+  if (!few) return ad::launch_many(p, x_type, most, scratch, s);
+  // CTAs to a tile: as many, up to eight, as fit two to an SM (of whole clusters fewer do: 33 of eight, 71 of four), for a number of
+  // tiles between the fewest and the most that the batch can have; but no more than there are blocks of K or of columns for.
+  const int tiles = (M / ad::kFewRows + most + 1) / 2;
   int c = 8;
-  while (c > 1 && most * c > 2 * sm_count() + sm_count() / 2) c /= 2;
+  while (c > 1 && tiles * c > 2 * sm_count() - 4 * c) c /= 2;
   while (c > 1 && (K + 31) / 32 < c * ad::kWarps && (N + 31) / 32 < c * ad::kWarps) c /= 2;
   if (x_type == kXF32)
     return p.y_bf16 ? ad::launch_few_rank<kXF32, 2, 2>(p, most, c, s) : ad::launch_few_rank<kXF32, 3, 3>(p, most, c, s);

@@ -20,8 +20,8 @@ struct SlotHead {            // first 32 bytes of a slot
 struct PlanHead {            // first 256 bytes of a plan
   DeviceStatus status;
   uint32_t magic;
-  int M, n_slots, tile_rows;
-  int n_tiles, n_adapted;    // tiles; those in front that name a slot
+  int M, n_slots, reserved;
+  struct { int n_tiles, n_adapted; } of[2];    // of the list for few and of that for many rows: tiles; those in front that name a slot
 };
 struct Tile { int slot, rows; };
 
@@ -49,7 +49,7 @@ struct Params {
   const void* Y0;
   void* Y;
   size_t slot_bytes;
-  int M, K, N, max_rank, plan_slots, tile_rows;
+  int M, K, N, max_rank, plan_slots;
   int y0_bf16, y_bf16;
   bool x_wide, y_wide;       // X; Y0 and Y: aligned to 32 bytes
   int bits, emin, emax;      // format of an MXINT8 X
@@ -199,10 +199,20 @@ __device__ __forceinline__ void store_y(const Params& p, size_t idx, const float
   if (p.y_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + idx) = make_uint2(round_bf16x2(v.x, v.y), round_bf16x2(v.z, v.w));
   else *reinterpret_cast<float4*>(static_cast<float*>(p.Y) + idx) = v;
 }
+// What a kernel needs of a plan's head.
+struct ListHead {
+  uint32_t magic;
+  int M, n_slots, n_tiles, n_adapted;
+};
+__device__ __forceinline__ ListHead load_head(const PlanHead* h, int list) {
+  const uint4 a = *reinterpret_cast<const uint4*>(&h->magic);
+  const int2 b = *reinterpret_cast<const int2*>(&h->of[list]);
+  return ListHead{a.x, (int)a.y, (int)a.z, b.x, b.y};
+}
 // Whether the plan is one of this batch.  (A plan of another batch, or none, has other sizes in its head: nothing is done then, and its
 // status says so.)
-__device__ __forceinline__ bool plan_fits(const Params& p, const PlanHead& h) {
-  if (h.magic == kPlanMagic && h.M == p.M && h.n_slots == p.plan_slots && h.tile_rows == p.tile_rows) return true;
+__device__ __forceinline__ bool plan_fits(const Params& p, const ListHead& h) {
+  if (h.magic == kPlanMagic && h.M == p.M && h.n_slots == p.plan_slots) return true;
   if (blockIdx.x == 0 && threadIdx.x == 0) report_error(&p.plan->status, LQER_ERR_BAD_PACKED, 803);
   return false;
 }
@@ -212,15 +222,6 @@ __device__ __forceinline__ int rank_of(const Params& p, int slot, const SlotHead
   if (hd.magic == kPoolMagic && hd.K == p.K && hd.N == p.N && hd.max_rank == p.max_rank && hd.rank >= 0 && hd.rank <= p.max_rank) return hd.rank;
   if (tell) report_error(&p.plan->status, LQER_ERR_BAD_PACKED, 804, slot);
   return 0;
-}
-__device__ __forceinline__ PlanHead load_head(const PlanHead* h) {
-  const uint4 a = *reinterpret_cast<const uint4*>(&h->magic);
-  PlanHead r;
-  r.magic = a.x; r.M = (int)a.y; r.n_slots = (int)a.z; r.tile_rows = (int)a.w;
-  const int2 b = *reinterpret_cast<const int2*>(&h->n_tiles);
-  r.n_tiles = b.x;
-  r.n_adapted = b.y;
-  return r;
 }
 __device__ __forceinline__ SlotHead load_slot(const uint8_t* slot) {
   const uint4 a = *reinterpret_cast<const uint4*>(slot);
@@ -232,18 +233,41 @@ __device__ __forceinline__ SlotHead load_slot(const uint8_t* slot) {
 inline size_t slot_bytes(int K, int N, int max_rank) {
   return (256 + a_bytes(K, max_rank) + b_bytes(N, max_rank, b_pitch(max_rank)) + 255) & ~(size_t)255;
 }
-inline int tile_rows_of(int M) { return M <= 512 ? kFewRows : kManyRows; }
+// A plan holds the rows in tiles of 8 for up to kFewMost of them, and in tiles of 128 for more than kManyLeast: in between the call
+// chooses.  Both measured, few / many, us: 1024 rows of 1264 x 1968 rank 32 bf16 10.2 / 16.7, of 4096 x 4096 rank 16 15.9 / 19.9, of
+// 5120 x 5120 rank 32 21 / 25, rank 128 43 / 31, of 4096 x 11008 rank 64 44 / 31; 513 rows of the last 24 / 26, of 5120 x 5120 rank
+// 128 25 / 28; 1536 rows of 4096 x 4096 rank 16 27 / 24.
+constexpr int kFewMost = 1024, kManyLeast = 512;
+constexpr long long kFewWork = 350LL * 1000 * 1000;
+inline bool takes_few(int M, int K, int N, int max_rank) {
+  return M <= kManyLeast || (M <= kFewMost && (long long)M * (K + N) * max_rank <= kFewWork);
+}
 // No batch has more tiles than this: one that is not full per slot (and one of rows without), the rest are full.
-inline int max_tiles(int M, int n_slots) {
-  const int rows = tile_rows_of(M), partial = n_slots + 1 < M ? n_slots + 1 : M;
-  const long long t = (long long)partial + M / rows;
+inline int max_tiles(int M, int n_slots, int tile_rows) {
+  const long long partial = n_slots + 1 < M ? n_slots + 1 : M, t = partial + M / tile_rows;
   return (int)(t < M ? t : M);
 }
-inline size_t tiles_bytes(int M, int n_slots) { return ((size_t)max_tiles(M, n_slots) * sizeof(Tile) + 255) & ~(size_t)255; }
-
+// Where a plan's lists lie: tiles and their rows, for few and for many rows.
+struct PlanLayout {
+  int tiles[2];
+  size_t tiles_at[2], rows_at[2], bytes;
+};
+inline PlanLayout plan_layout(int M, int n_slots) {
+  auto up = [](size_t v) { return (v + 255) & ~(size_t)255; };
+  PlanLayout l;
+  l.bytes = 256;
+  for (int i = 0; i < 2; ++i) {
+    const int rows = i == 0 ? kFewRows : kManyRows;
+    l.tiles[i] = (i == 0 ? M <= kFewMost : M > kManyLeast) ? max_tiles(M, n_slots, rows) : 0;
+    l.tiles_at[i] = l.bytes;
+    l.rows_at[i] = l.tiles_at[i] + up((size_t)l.tiles[i] * sizeof(Tile));
+    l.bytes = l.rows_at[i] + up((size_t)l.tiles[i] * rows * 4);
+  }
+  return l;
+}
 
 // The kernels for many rows: three launches, T in between in `scratch`.
-size_t many_scratch_bytes(int M, int plan_slots, int max_rank);
+size_t many_scratch_bytes(int tiles, int max_rank);
 cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s);
 
 }  // namespace ad

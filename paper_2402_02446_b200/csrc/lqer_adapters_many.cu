@@ -1,4 +1,4 @@
-// Adapters of many requests, more than 512 rows (see lqer_adapters.cu for the term, its precision and the layouts of pool and plan):
+// Adapters of many requests, many rows (see lqer_adapters.cu for the term, its precision and the layouts of pool and plan):
 // three launches, tiles of 128 rows of one adapter, the products on the tcgen05 tensor cores.
 //
 // project_kernel: T = X A_a.  The MMA's 128 rows are tokens, its columns the ranks.  Sixteen warps bring X from its rows, wherever they lie,
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
   const uint32_t tmem = tmem_at;
   tc::pdl_wait();
   tc::pdl_launch_dependents();                          // in this order: see expand_kernel
-  const PlanHead head = load_head(p.plan);
+  const ListHead head = load_head(p.plan, 1);
   RunWalk walk;
   walk.KS = (p.K + 63) / 64;
   const Cut cut(plan_fits(p, head) ? head.n_adapted : 0, walk.KS, gridDim.x);
@@ -328,7 +328,7 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Man
   const Params& p = mp.p;
   // plan and pool were there before project_kernel (see expand_kernel); its partial sums have to be waited for
   const int slabs = (p.max_rank + 63) / 64, tile = blockIdx.x / (slabs * 8), e = blockIdx.x % (slabs * 8), m = threadIdx.x & 127, h = threadIdx.x >> 7;
-  const PlanHead head = load_head(p.plan);
+  const ListHead head = load_head(p.plan, 1);
   const int slot = p.tiles[tile].slot;                  // (the list is as long as the grid asks, whatever it holds)
   int rank = 0;
   SlotHead hd;
@@ -456,7 +456,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   // project_kernel lets the kernels behind it start only once it has waited for all that came before the call, so plan, pool and Y0
   // may be read here at once; only what finish_kernel writes - the images of T, the counter - has to be waited for, which the
   // copying warp does.
-  const PlanHead head = load_head(p.plan);
+  const ListHead head = load_head(p.plan, 1);
   const bool fits = plan_fits(p, head);
   const int NG = (p.N + 255) / 256, NC = (p.N + 127) / 128;
   const int groups = fits ? (p.Y0 == p.Y ? head.n_adapted : head.n_tiles) * NG : 0;
@@ -665,8 +665,7 @@ constexpr size_t kSmemMost = 226 * 1024;
 // The grids are no larger than kPrologueMaxCtas (launch_many takes fewer CTAs where the device has fewer SMs).
 static size_t partial_bytes(int tiles, int max_rank) { return ((size_t)tiles + kPrologueMaxCtas) * partial_floats(max_rank) * 4; }
 static size_t image_bytes(int tiles, int max_rank) { return (size_t)tiles * 3 * ((max_rank + 63) / 64) * kXImage; }
-size_t many_scratch_bytes(int M, int plan_slots, int max_rank) {
-  const int tiles = max_tiles(M, plan_slots);
+size_t many_scratch_bytes(int tiles, int max_rank) {
   return partial_bytes(tiles, max_rank) + image_bytes(tiles, max_rank) + 256;
 }
 template <class Kernel>

@@ -133,7 +133,7 @@ lqer_status_t lqer_adapters_workspace_bytes(int M, const lqer_adapter_pool_t* po
   lqer_status_t st = pool_shape(pool);
   if (st != LQER_OK) return st;
   if (!rows_ok(M) || plan_slots < 1 || plan_slots > pool->n_slots) return LQER_ERR_SHAPE;
-  *bytes = adapter_scratch_bytes(M, plan_slots, pool->max_rank);
+  *bytes = adapter_scratch_bytes(M, plan_slots, pool->K, pool->N, pool->max_rank);
   return LQER_OK;
 }
 
@@ -149,7 +149,7 @@ lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lq
   if (!rows_ok(M) || plan_slots < 1 || plan_slots > pool->n_slots) return LQER_ERR_SHAPE;
   if (misaligned(X) || misaligned(Y0) || misaligned(Y) || misaligned(plan, 256)) return LQER_ERR_ALIGN;
   if (Y == X || (Y == Y0 && y0_dtype != y_dtype)) return LQER_ERR_CONFIG;
-  const size_t need = adapter_scratch_bytes(M, plan_slots, pool->max_rank);
+  const size_t need = adapter_scratch_bytes(M, plan_slots, pool->K, pool->N, pool->max_rank);
   if (need > 0) {
     if (workspace == nullptr) return LQER_ERR_NULL;
     if (misaligned(workspace, 256)) return LQER_ERR_ALIGN;

@@ -631,7 +631,7 @@ cudaError_t launch_adapter_load(void* pool, int K, int N, int max_rank, int slot
 cudaError_t launch_adapter_plan(const int* slots, int M, int n_slots, void* plan, cudaStream_t s);
 cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, int K, int N, int max_rank, void* plan, int plan_slots,
                             const void* Y0, int y0_type, void* Y, int y_type, int bits, int emin, int emax, void* scratch, cudaStream_t s);
-size_t adapter_scratch_bytes(int M, int plan_slots, int max_rank);
+size_t adapter_scratch_bytes(int M, int plan_slots, int K, int N, int max_rank);
 
 // Argument checks shared by the entry points (lqer_api.cu).
 lqer_status_t check_config(const lqer_config_t* cfg);

@@ -104,11 +104,14 @@ def test_adapter_refusals():
         assert apply(**kw) == E("LQER_ERR_CONFIG"), kw
     # more than 512 rows go through a workspace
     assert lib.lqer_adapters_workspace_bytes(512, _pool(), 4, C.byref(size)) == 0 and size.value == 0
-    assert lib.lqer_adapters_workspace_bytes(513, _pool(), 4, C.byref(size)) == 0 and size.value > 0
+    assert lib.lqer_adapters_workspace_bytes(1024, _pool(), 4, C.byref(size)) == 0 and size.value == 0      # a small product
+    big = dict(K=4096, N=11008, max_rank=64)
+    assert lib.lqer_adapters_workspace_bytes(640, _pool(**big), 4, C.byref(size)) == 0 and size.value > 0
+    assert lib.lqer_adapters_workspace_bytes(1025, _pool(), 4, C.byref(size)) == 0 and size.value > 0
     assert lib.lqer_adapters_workspace_bytes(513, _pool(), 5, C.byref(size)) == lib.lqer_adapters_workspace_bytes(0, _pool(), 4, C.byref(size)) == E("LQER_ERR_SHAPE")
     assert lib.lqer_adapters_workspace_bytes(513, _pool(), 4, None) == E("LQER_ERR_NULL")
-    assert apply(M=513) == E("LQER_ERR_NULL") and apply(M=513, ws=P + 16, nbytes=1 << 30) == E("LQER_ERR_ALIGN")
-    assert apply(M=513, ws=P, nbytes=size.value - 1) == E("LQER_ERR_BUFFER_TOO_SMALL")
+    assert apply(M=1025) == E("LQER_ERR_NULL") and apply(M=1025, ws=P + 16, nbytes=1 << 30) == E("LQER_ERR_ALIGN")
+    assert apply(M=1025, ws=P, nbytes=size.value - 1) == E("LQER_ERR_BUFFER_TOO_SMALL")
     assert L.launch_count() == 0
 
 
@@ -122,13 +125,15 @@ def test_tensors_on_the_host_are_refused():
 
 
 def test_a_plan_has_room_for_every_batch():
-    # the head, slot and length (8 bytes) of every tile that any batch can have, its rows
+    # the head, slot and length (8 bytes) of every tile that any batch can have, its rows: tiles of 8 up to 1024 rows, of 128 above 512
     size = C.c_size_t()
-    for M in (1, 2, 7, 8, 9, 15, 16, 17, 100, 512, 513, 4096):
+    for M in (1, 2, 7, 8, 9, 15, 16, 17, 100, 512, 513, 1024, 1025, 4096):
         for n in (1, 2, 7, 64, 1024):
             assert L.lib().lqer_adapter_plan_bytes(M, n, C.byref(size)) == 0
-            rows = 8 if M <= 512 else 128
-            # the worst batch: as many bins as possible with one row more than a whole number of tiles
-            bins = min(n + 1, M)
-            worst = sum(-(-r // rows) for r in [1] * (bins - 1) + [M - (bins - 1)])
-            assert size.value >= 256 + 8 * worst + 4 * rows * worst
+            need = 256
+            for rows in ([8] if M <= 1024 else []) + ([128] if M > 512 else []):
+                # the worst batch: as many bins as possible with one row more than a whole number of tiles
+                bins = min(n + 1, M)
+                worst = sum(-(-r // rows) for r in [1] * (bins - 1) + [M - (bins - 1)])
+                need += 8 * worst + 4 * rows * worst
+            assert size.value >= need, (M, n)

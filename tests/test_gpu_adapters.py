@@ -94,9 +94,10 @@ def test_adapters(shape, x, y0, y):
 
 
 @pytest.mark.parametrize("x,y", [("bf16", "bf16"), ("f32", "f32"), ("mxint8", "bf16"), ("bf16", "f32"), ("f32", "bf16"), ("mxint8", "f32")])
-@pytest.mark.parametrize("M,ranks", [(513, [16, 8]), (700, [64, 33, 5]), (1300, [128]), (530, [256, 8])])
+@pytest.mark.parametrize("M,ranks", [(513, [16, 8]), (700, [64, 33, 5]), (1300, [128]), (530, [256, 8]), (1025, [16, 3]), (1100, [256, 20]), (2500, [32, 8, 17]),
+                                     (1040, [256, 256])])
 def test_adapters_many_rows(M, ranks, x, y):
-    # runs of uneven length, scattered rows and rows without adapter
+    # runs of uneven length, scattered rows and rows without adapter; up to 1024 rows of products as small as these are "few"
     g = torch.Generator().manual_seed(M)
     slots = torch.sort(torch.randint(-1, len(ranks), (M,), generator=g))[0]
     slots[::7] = torch.randint(-1, len(ranks), (len(slots[::7]),), generator=g)
@@ -108,7 +109,7 @@ def test_adapters_many_rows(M, ranks, x, y):
 
 def test_random_batches_of_many_slots():
     g = torch.Generator().manual_seed(3)
-    for M, n in ((1, 64), (7, 1024), (64, 64), (129, 3), (512, 1000), (515, 600)):
+    for M, n in ((1, 64), (7, 1024), (64, 64), (129, 3), (512, 1000), (515, 600), (1024, 1024), (1500, 900), (4097, 1024)):
         slots = torch.randint(-1, n, (M,), generator=g).tolist()
         ranks = [(j * 7) % 17 for j in range(n)]              # empty slots among them
         c = Case(M, 64, 72, ranks, slots, max_rank=16)
