@@ -252,12 +252,17 @@ __device__ __forceinline__ void zero8(float (&v)[8]) {
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] = 0.f;
 }
-// A CTA takes a row at a time, in registers: OPT octets a thread.  Up to 8192 columns (AHEAD) the next row's elements are on their way
-// while this row's sum is formed and its results are written; a thread then holds two octets where both summands are bf16, and one
-// otherwise, in 64 registers either way.  The sum of squares is kept in fp64: it makes the row's factor good to fp64 (the
-// MXINT borders need that) and holds squares that fp32 cannot.
+// A CTA takes a row at a time, in registers: OPT octets a thread.  Up to 8192 columns (16384 of bf16) the next row's elements are on their
+// way while this row's sum is formed and its results are written (AHEAD); a thread then holds two octets and their weights (bf16) or
+// one.  The sum of squares is kept in fp64: it makes the row's factor good to fp64 (the MXINT borders need that) and holds
+// squares that fp32 cannot.
+// CTAs that are to fit an SM: two octets a thread, their weights and what comes next take 80 registers, four octets and what comes next
+// 128, the other forms 64.
+__host__ __device__ constexpr int norm_ctas(int threads, int opt, bool ahead) {
+  return !ahead || opt == 1 ? 1024 / threads : opt == 2 ? 768 / threads : 1;
+}
 template <bool XB, bool RB, int YT, int OPT, bool AHEAD, int THREADS>
-__global__ void __launch_bounds__(THREADS, 1024 / THREADS) add_rms_norm_kernel(const NormParams p) {
+__global__ void __launch_bounds__(THREADS, norm_ctas(THREADS, OPT, AHEAD)) add_rms_norm_kernel(const NormParams p) {
   __shared__ double slots[2][THREADS / 32];
   tc::pdl_launch_dependents();
   tc::pdl_wait();
@@ -269,12 +274,15 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) add_rms_norm_kernel(c
   RawRow<XB, RB> raw[AHEAD ? OPT : 1];
   size_t idx = (size_t)blockIdx.x * p.K + col0;
   const size_t hop = (size_t)gridDim.x * p.K;
+  constexpr bool KEEP = AHEAD && OPT == 2;            // the weights stay in registers
+  float w[KEEP ? OPT : 1][8];
   if (AHEAD) {
 #pragma unroll
     for (int o = 0; o < OPT; ++o) {
       raw[o].x.clear();
       raw[o].r.clear();
       if (in[o]) raw[o].load(p, idx + o * step);
+      if (KEEP) load_w(p, in[o] ? col0 + o * step : 0, w[o]);
     }
   }
   int turn = 0;
@@ -304,9 +312,8 @@ __global__ void __launch_bounds__(THREADS, 1024 / THREADS) add_rms_norm_kernel(c
     const float inv = (float)inv64;
 #pragma unroll
     for (int o = 0; o < OPT; ++o) {
-      float w[8];                                   // read again for every row: from L1
-      load_w(p, in[o] ? col0 + o * step : 0, w);
-      finish8<YT>(p, idx + o * step, in[o], h[o], w, inv, inv64, qc);
+      if (!KEEP) load_w(p, in[o] ? col0 + o * step : 0, w[0]);              // again for every row: from L1
+      finish8<YT>(p, idx + o * step, in[o], h[o], w[KEEP ? o : 0], inv, inv64, qc);
     }
   }
 }
@@ -372,16 +379,20 @@ static cudaError_t launch_norm(const NormParams& p, cudaStream_t s) {
   const int octets = p.K / 8;
   LaunchScope scope(kFamQuantize, s);
   if (octets > 4096) return launch_after(add_rms_norm_long_kernel<XB, RB, YT>, dim3(p.M), 1024, s, p);
-  constexpr int AHEAD_OPT = XB && RB ? 2 : 1;
-  const bool ahead = octets <= 1024;
-  const int opt = ahead ? AHEAD_OPT : 4;
+  constexpr int AHEAD_OPT = XB && RB ? 2 : 1, LONG = 4;
+  const bool ahead = octets <= 1024, ahead_long = !ahead && XB && RB && octets <= 2048;
+  const int opt = ahead ? AHEAD_OPT : LONG;
   const int threads = ((octets + opt - 1) / opt + 31) / 32 * 32;
-  // as many CTAs as are resident at 64 registers a thread
-  const int per = threads <= 64 ? 16 : 1024 / threads, resident = sm_count() * per, grid = p.M < resident ? p.M : resident;
-  if (!ahead) return launch_after(add_rms_norm_kernel<XB, RB, YT, 4, false, 1024>, dim3(grid), threads, s, p);
-  return threads <= 256   ? launch_after(add_rms_norm_kernel<XB, RB, YT, AHEAD_OPT, true, 256>, dim3(grid), threads, s, p)
-         : threads <= 512 ? launch_after(add_rms_norm_kernel<XB, RB, YT, AHEAD_OPT, true, 512>, dim3(grid), threads, s, p)
-                          : launch_after(add_rms_norm_kernel<XB, RB, YT, AHEAD_OPT, true, 1024>, dim3(grid), threads, s, p);
+  // as many CTAs as are resident
+  const int room = ahead && opt == 2 ? 768 : ahead_long ? 512 : 1024, per = threads <= 64 ? 12 : threads > room ? 1 : room / threads;
+  const int resident = sm_count() * per, grid = p.M < resident ? p.M : resident;
+  if constexpr (XB && RB)
+    if (ahead_long) return launch_after(add_rms_norm_kernel<XB, RB, YT, LONG, true, 512>, dim3(grid), threads, s, p);
+  if (!ahead) return launch_after(add_rms_norm_kernel<XB, RB, YT, LONG, false, 1024>, dim3(grid), threads, s, p);
+  constexpr int MOST = AHEAD_OPT == 2 ? 512 : 1024, MIDDLE = AHEAD_OPT == 2 ? 384 : 512;
+  return threads <= 256      ? launch_after(add_rms_norm_kernel<XB, RB, YT, AHEAD_OPT, true, 256>, dim3(grid), threads, s, p)
+         : threads <= MIDDLE ? launch_after(add_rms_norm_kernel<XB, RB, YT, AHEAD_OPT, true, MIDDLE>, dim3(grid), threads, s, p)
+                             : launch_after(add_rms_norm_kernel<XB, RB, YT, AHEAD_OPT, true, MOST>, dim3(grid), threads, s, p);
 }
 template <bool XB, bool RB>
 static cudaError_t launch_norm_y(const NormParams& p, int y_type, cudaStream_t s) {
@@ -433,7 +444,8 @@ __device__ __forceinline__ void gate8(const float (&g)[8], const float (&u)[8], 
     }
     float t[2], r[2];
     unf2(t2, t[0], t[1]);
-    y = fmaxf(y, fmaxf(t[0], t[1]));
+#pragma unroll
+    for (int k = 0; k < 2; ++k) y = fmaxf(y, ACT == LQER_SILU || t[k] < 128.f ? t[k] : 0.f);         // 2^y beyond fp32: the value is zero, surely
 #pragma unroll
     for (int k = 0; k < 2; ++k) asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(t[k]) : "f"(t[k]));
     const F2 d2 = add2(f2(t[0], t[1]), one2);
@@ -444,6 +456,19 @@ __device__ __forceinline__ void gate8(const float (&g)[8], const float (&u)[8], 
     unf2(v2, v[i], v[i + 1]);
   }
   rel = fmaf(y, ACT == LQER_SILU ? 2.3841858e-7f : 9.5367432e-7f, 7.1525574e-7f);
+}
+// act(gate[at]) * up[at] in fp64: for values in doubt, from memory again, so that nothing has to be kept for them.
+template <bool XB, int ACT>
+__device__ __noinline__ double gate_wide(const void* gate, const void* up, size_t at) {
+  double g, u;
+  if (XB) {
+    g = __uint_as_float((uint32_t)static_cast<const uint16_t*>(gate)[at] << 16);
+    u = __uint_as_float((uint32_t)static_cast<const uint16_t*>(up)[at] << 16);
+  } else {
+    g = static_cast<const float*>(gate)[at];
+    u = static_cast<const float*>(up)[at];
+  }
+  return g / (1.0 + exp(-act_argument<ACT>(g))) * u;
 }
 // Thread t of a CTA's row of threads holds columns 8 t .. 8 t + 7 of the CTA's stretch, of every gridDim.y-th row; the next row's are on
 // their way while this one's are worked on.
@@ -467,6 +492,7 @@ __global__ void __launch_bounds__(128, 8) gated_activation_kernel(const GatePara
     float g[8], u[8], v[8], rel = 0.f;
     rg.values(g);
     ru.values(u);
+    const size_t now = at;
     at += hop;
     if (in && row + (int)gridDim.y < p.M) {
       rg.load(p.gate, at);
@@ -476,13 +502,7 @@ __global__ void __launch_bounds__(128, 8) gated_activation_kernel(const GatePara
     if (YT == kYMXINT8) {
       uint2 m8;
       int e;
-      quantise8(
-          v, qc, rel,
-          [&](int i) {
-            const double gd = pick8(g, i);
-            return gd / (1.0 + exp(-act_argument<ACT>(gd))) * (double)pick8(u, i);
-          },
-          m8, e);
+      quantise8(v, qc, rel, [&](int i) { return in ? gate_wide<XB, ACT>(p.gate, p.up, now + i) : 0.0; }, m8, e);
       if (in) store_mxint8(p.Y, p.Ye, idx, m8, e);
     } else if (in) {
       store8<YT == kYBF16>(p.Y, idx, v);
