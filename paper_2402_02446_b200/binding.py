@@ -460,21 +460,19 @@ def _code(codes, dt) -> int:
     return c
 
 
-def _output(Y, M: int, N: int, out_dtype, like: torch.Tensor):
-    """The tensor of an [M, N] result (made where none is given; its type goes before out_dtype) and its type's code."""
-    code = _code(_OUT_CODE, out_dtype if Y is None else Y.dtype)
-    if code == 2:
-        if N % 16:
-            raise ValueError("an MXINT8 output has whole blocks of 16 columns")
-        if Y is None:
-            return like.new_empty(mxint8_bytes(M, N), dtype=torch.uint8), code
-        if Y.dim() != 1 or Y.shape[0] != mxint8_bytes(M, N):
-            raise ValueError("an MXINT8 output is a flat uint8 tensor of mxint8_bytes(M, N)")
-    elif Y is None:
-        return like.new_empty((M, N), dtype=out_dtype), code
-    elif Y.shape != (M, N):
-        raise ValueError(f"expected an output of shape {(M, N)}")
-    return Y, code
+def _output(Y, M: int, N: int, out_dtype, like: torch.Tensor, index: int):
+    """The tensor of an [M, N] result (made where none is given; its type goes before out_dtype), its type's code and its address."""
+    code = _OUT_CODE.get(out_dtype if Y is None else Y.dtype)
+    if code is None:
+        raise ValueError(f"unsupported output dtype {out_dtype if Y is None else Y.dtype}")
+    if code == 2 and N % 16:
+        raise ValueError("an MXINT8 output has whole blocks of 16 columns")
+    if Y is None:
+        Y = like.new_empty(M * N + M * N // 16, dtype=torch.uint8) if code == 2 else like.new_empty((M, N), dtype=out_dtype)
+        return Y, code, Y.data_ptr()
+    if Y.shape != ((mxint8_bytes(M, N),) if code == 2 else (M, N)):
+        raise ValueError("expected an output [M, N], or a flat uint8 tensor of mxint8_bytes(M, N)")
+    return Y, code, _ptr(Y, index)
 
 
 def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: torch.Tensor | None = None, out_dtype=MXINT8,
@@ -504,9 +502,9 @@ def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: to
         if residual_out.shape != shape or residual is not None and residual_out.dtype != residual.dtype:
             raise ValueError("residual_out has X's shape and the residual's type")
         h_ptr, r_code = _ptr(residual_out, index), _code(_REAL_CODE, residual_out.dtype)
-    Y, y_code = _output(Y, M, K, out_dtype, X)
+    Y, y_code, y_ptr = _output(Y, M, K, out_dtype, X, index)
     status = lib().lqer_add_rms_norm(_ptr(X, index), x_code, r_ptr, h_ptr, r_code, _ptr(weight, index), _code(_REAL_CODE, weight.dtype), eps, M, K,
-                                     None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code, _raw_stream(stream, index))
+                                     None if cfg is None else C.byref(cfg), y_ptr, y_code, _raw_stream(stream, index))
     if status:
         raise LqerError(status, "lqer_add_rms_norm")
     return Y, residual_out
@@ -529,9 +527,9 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", ou
         raise ValueError("expected rows of consecutive elements, with one row stride for gate and up")
     if act not in _ACTS:
         raise ValueError(f"unknown activation {act!r}")
-    Y, y_code = _output(Y, M, N, out_dtype, gate)
+    Y, y_code, y_ptr = _output(Y, M, N, out_dtype, gate, index)
     status = lib().lqer_gated_activation(gate.data_ptr(), up.data_ptr(), _code(_REAL_CODE, gate.dtype), ld if M > 1 else N, M, N, _ACTS[act],
-                                         None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code, _raw_stream(stream, index))
+                                         None if cfg is None else C.byref(cfg), y_ptr, y_code, _raw_stream(stream, index))
     if status:
         raise LqerError(status, "lqer_gated_activation")
     return Y
@@ -546,7 +544,7 @@ def dequantize_activations(Xq: torch.Tensor, M: int, K: int, out_dtype=torch.flo
             return dequantize_activations(Xq, M, K, out_dtype, cfg, Y, stream)
     if Xq.dtype != torch.uint8 or K % 16 or Xq.numel() != mxint8_bytes(M, K):
         raise ValueError("an MXINT8 tensor is a flat uint8 tensor of mxint8_bytes(M, K)")
-    Y, y_code = _output(Y, M, K, out_dtype, Xq)
+    Y, y_code, y_ptr = _output(Y, M, K, out_dtype, Xq, index)
     status = lib().lqer_dequantize_activations(_ptr(Xq, index), M, K, None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code,
                                                _raw_stream(stream, index))
     if status:
@@ -564,6 +562,7 @@ class AdapterPool:
         size = C.c_size_t()
         _check(lib().lqer_adapter_pool_bytes(self.ref, C.byref(size)), "lqer_adapter_pool_bytes")
         self.buf = torch.empty(size.value, dtype=torch.uint8, device=device)
+        self.index = self.buf.get_device()
         self.handle.data = self.buf.data_ptr()
 
 
@@ -599,6 +598,9 @@ class AdapterPlan:
     M: int
     n_slots: int
 
+    def __post_init__(self):
+        self.index, self.ptr = self.buf.get_device(), self.buf.data_ptr()
+
 
 def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | None = None, stream=None) -> AdapterPlan:
     """The plan of a batch: slots int32 [M], the slot of each row's adapter in the pools of this step (-1: none).  It serves every pool
@@ -616,8 +618,9 @@ def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | Non
         plan = AdapterPlan(torch.empty(size.value, dtype=torch.uint8, device=slots.device), M, pool.n_slots)
     elif plan.M != M or plan.n_slots != pool.n_slots:
         raise ValueError("the plan to be made again has other sizes")
-    _check(lib().lqer_adapter_plan(_ptr(slots, index), M, pool.n_slots, _ptr(plan.buf, index), plan.buf.numel(), _raw_stream(stream, index)),
-           "lqer_adapter_plan")
+    if plan.index != index:
+        raise ValueError("expected the plan on the device of the slots")
+    _check(lib().lqer_adapter_plan(_ptr(slots, index), M, pool.n_slots, plan.ptr, plan.buf.numel(), _raw_stream(stream, index)), "lqer_adapter_plan")
     return plan
 
 
@@ -641,15 +644,20 @@ def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: to
     x_code = _code(_OUT_CODE, X.dtype)
     if X.shape != ((mxint8_bytes(M, K),) if x_code == 2 else (M, K)) or Y0.shape != (M, N):
         raise ValueError("expected X of the plan's rows and the pool's K columns, and Y0 [M, N]")
+    if pool.index != index or plan.index != index:
+        raise ValueError("expected pool and plan on the device of X")
+    y0_ptr = _ptr(Y0, index)
     if Y is None:
         Y = torch.empty_like(Y0) if out_dtype is None or out_dtype == Y0.dtype else Y0.new_empty((M, N), dtype=out_dtype)
+        y_ptr = Y.data_ptr()
     elif Y.shape != (M, N):
         raise ValueError("expected Y [M, N]")
-    _ptr(pool.buf, index)
+    else:
+        y_ptr = _ptr(Y, index)
     if ws is None and M > 512:
         ws = X.new_empty(adapters_workspace_bytes(M, pool, plan.n_slots), dtype=torch.uint8)
-    status = lib().lqer_adapters(_ptr(X, index), x_code, M, pool.ref, _ptr(plan.buf, index), plan.n_slots, _ptr(Y0, index), _code(_REAL_CODE, Y0.dtype),
-                                 _ptr(Y, index), _code(_REAL_CODE, Y.dtype), None if cfg is None else C.byref(cfg),
+    status = lib().lqer_adapters(_ptr(X, index), x_code, M, pool.ref, plan.ptr, plan.n_slots, y0_ptr, _code(_REAL_CODE, Y0.dtype),
+                                 y_ptr, _code(_REAL_CODE, Y.dtype), None if cfg is None else C.byref(cfg),
                                  None if ws is None else _ptr(ws, index), 0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(stream, index))
     if status:
         raise LqerError(status, "lqer_adapters")
