@@ -381,7 +381,7 @@ lqer_status_t lqer_set_path(int path);
  * the kernel give up, write LQER_ERR_TIMEOUT to the status word and return, so the context stays usable.
  *  - lqer_set_wait_limit_cycles: the bound in SM clock cycles (default 4e9, about two seconds; 1e3 .. 2^40).
  *  - lqer_inject_stall(family): the next launch of that kernel family (numbering of lqer_kernel_times_t:
- *    3 activation prologue, 6 tensor-core GEMM pair kernel, 7 decode and small-batch kernels) is told to expect one arrival
+ *    3 activation prologue, 6 tensor-core GEMM pair kernel, 7 decode and small-batch kernels, adapters of many rows) is told to expect one arrival
  *    more than will ever come (3, 7) or has its last stage of operands withheld (6), so that its waits run
  *    out; no memory is touched that an ordinary launch would not touch.  -1 disarms.  After such a launch
  *    the outputs are undefined and the workspace needs lqer_workspace_init before its next use. */
@@ -392,6 +392,7 @@ lqer_status_t lqer_inject_stall(int kernel_family);
  * Every global store of the inference kernels and every bulk copy of packed weights first checks its byte range
  * against the extent of the buffer it belongs to; the first violation is written to the status word
  * (LQER_ERR_BOUNDS; lqer_poll_status) and the access is skipped - nothing traps, nothing out of range is touched.
+ * The kernels between the layers check their stores of Y where they have a status word, the adapters' in their plan.
  * It stands in for a memory checker where none can be run.  lqer_debug_bounds_shrink (host, process wide) is its test
  * hook: the declared extent of every Y is made `bytes` smaller for the launches that follow, so that the checks at
  * the end of Y fire (the stores they guard are skipped; Y is then incomplete); 0 restores.  The ordinary build

@@ -523,7 +523,7 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", ou
         raise ValueError("expected gate and up of one shape [M, N], type and device")
     M, N = shape
     ld, one = gate.stride()
-    if N > 1 and one != 1 or up.stride() != (ld, one):
+    if N > 1 and (one != 1 or up.stride(1) != 1) or M > 1 and up.stride(0) != ld:
         raise ValueError("expected rows of consecutive elements, with one row stride for gate and up")
     if act not in _ACTS:
         raise ValueError(f"unknown activation {act!r}")

@@ -5,6 +5,11 @@ Bound of a row's result: with S = scale (|X| |A|) |B| the errors are relative to
 magnitude; a sum of T passes through at most K / 16 MMAs a part and 16 partial sums, one of Y through rank / 16 MMAs a part.  The
 scale and the last addition are rounded (2^-24 each, of S and of the result), and a bf16 result (2^-8).
 """
+import os
+import subprocess
+import sys
+import textwrap
+
 import numpy as np
 import pytest
 import torch
@@ -14,7 +19,8 @@ import paper_2402_02446_b200 as L
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
 TYPES = {"f32": torch.float32, "bf16": torch.bfloat16}
-BAD_PACKED, BOUNDS = 6, 10
+BAD_PACKED, TIMEOUT, BOUNDS = 6, 9, 10
+FAM_DECODE = 7
 
 
 def _randn(shape, seed, dtype=torch.float32):
@@ -238,6 +244,160 @@ def test_streams_graphs_and_two_batches_at_once():
     torch.cuda.synchronize()
     for case, Yk in got:
         case.check(Yk)
+
+
+def _many(seed=0, y="bf16", M=1500, ranks=(64, 16, 0, 40), K=1040, N=1064):
+    """A batch that takes the tensor-core kernels: runs, scattered rows, rows without an adapter and rows of an empty slot."""
+    g = torch.Generator().manual_seed(seed)
+    slots = torch.sort(torch.randint(-1, len(ranks), (M,), generator=g))[0]
+    slots[::9] = torch.randint(-1, len(ranks), (len(slots[::9]),), generator=g)
+    c = Case(M, K, N, list(ranks), slots.tolist(), x=y, y0=y, y=y, seed=seed, max_rank=64)
+    assert L.adapters_workspace_bytes(M, c.pool) > 0
+    return c
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+def test_many_rows_in_place_and_the_same_again(y):
+    c = _many(1, y)
+    Y = c.run()
+    c.check(Y)
+    inplace = c.Y0.clone()
+    L.apply_adapters(c.X, c.pool, c.plan, inplace, Y=inplace)
+    assert torch.equal(inplace, Y)
+    # whichever CTA takes which columns, the results are the same
+    ws = torch.full((L.adapters_workspace_bytes(c.M, c.pool),), 255, dtype=torch.uint8, device=DEV)
+    for _ in range(5):
+        assert torch.equal(L.apply_adapters(c.X, c.pool, c.plan, c.Y0, ws=ws), Y)
+    # tensors that are aligned to 16 bytes only
+    def shifted(t):
+        n = 16 // t.element_size()
+        return torch.empty(t.numel() + 2 * n, dtype=t.dtype, device=DEV)[n:n + t.numel()].view(t.shape).copy_(t)
+    X, Y0, Z = shifted(c.X), shifted(c.Y0), shifted(c.Y0)
+    assert X.data_ptr() % 32 == 16 and torch.equal(L.apply_adapters(X, c.pool, c.plan, Y0, Y=Z), Y)
+
+
+def test_many_rows_without_any_adapter():
+    c = _many(2)
+    c.slots.fill_(-1)
+    assert torch.equal(c.run(), c.Y0)
+    inplace = c.Y0.clone()
+    L.apply_adapters(c.X, c.pool, c.plan, inplace, Y=inplace)
+    assert torch.equal(inplace, c.Y0)
+    for j in range(4):
+        L.unload_adapter(c.pool, j)
+    c.slots[:] = torch.arange(c.M, device=DEV) % 4
+    assert torch.equal(c.run(), c.Y0) and L.poll_status(c.plan.buf) == 0
+    c.pool.buf[:32] = 255                                      # a slot that nobody wrote
+    assert torch.equal(c.run(), c.Y0) and L.poll_status(c.plan.buf) == BAD_PACKED
+
+
+def test_many_rows_next_to_a_row_of_nan():
+    c = _many(3)
+    Y = c.run()
+    c.X[700] = float("nan")
+    c.X[701, 5] = float("inf")
+    Z = c.run()
+    keep = torch.ones(c.M, dtype=torch.bool, device=DEV)
+    keep[700] = keep[701] = False
+    assert torch.equal(Z[keep], Y[keep])
+
+
+def test_many_rows_streams_and_graphs():
+    c, d = _many(4), _many(500, "f32", M=1100)
+    Yc, Yd = c.run(), d.run()
+    slots, X, Z = c.slots.clone(), c.X.clone(), torch.empty_like(Yc)
+    plan = L.adapter_plan(slots, c.pool)
+    ws = torch.empty(L.adapters_workspace_bytes(c.M, c.pool), dtype=torch.uint8, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        L.adapter_plan(slots, c.pool, plan=plan)
+        L.apply_adapters(X, c.pool, plan, c.Y0, Y=Z, ws=ws)
+    graph.replay()
+    assert torch.equal(Z, Yc)
+    slots.copy_(c.slots.flip(0))
+    X.copy_(c.X * 2)
+    graph.replay()
+    graph.replay()
+    old = c.slots, c.X, c.X64
+    c.slots, c.X, c.X64 = slots, X, X.double()
+    c.check(Z)
+    c.slots, c.X, c.X64 = old
+    torch.cuda.synchronize()
+    s1, s2 = torch.cuda.Stream(), torch.cuda.Stream()
+    got = []
+    for _ in range(6):
+        with torch.cuda.stream(s1):
+            got.append((Yc, c.run()))
+        with torch.cuda.stream(s2):
+            got.append((Yd, d.run()))
+    torch.cuda.synchronize()
+    for want, have in got:
+        assert torch.equal(have, want)
+
+
+def test_many_rows_behind_the_kernel_that_makes_their_input():
+    # the kernels overlap their neighbours on the stream: inputs made, used, and made anew without a pause
+    c = _many(6, "f32")
+    want = [L.apply_adapters(c.X * k, c.pool, L.adapter_plan(c.slots, c.pool), c.Y0 * k) for k in (1, 2, 4)]
+    torch.cuda.synchronize()
+    plan, X, Y0 = L.adapter_plan(c.slots, c.pool), torch.empty_like(c.X), torch.empty_like(c.Y0)
+    w = torch.ones(1040, device=DEV)
+    for _ in range(4):
+        got = []
+        for k in (1, 2, 4):
+            L.adapter_plan(c.slots, c.pool, plan=plan)
+            torch.mul(c.X, k, out=X)
+            torch.mul(c.Y0, k, out=Y0)
+            got.append(L.apply_adapters(X, c.pool, plan, Y0))
+            L.add_rms_norm(X, w, 1e-5)
+        for a, b in zip(got, want):
+            assert torch.equal(a, b)
+
+
+def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_fine():
+    c = _many(7)
+    Y = c.run()
+    L.set_wait_limit_cycles(2_000_000)                          # about a millisecond
+    L.inject_stall(FAM_DECODE)
+    try:
+        c.run()
+        torch.cuda.synchronize()
+    finally:
+        L.inject_stall(-1)
+        L.set_wait_limit_cycles(4_000_000_000)
+    assert L.poll_status(c.plan.buf) == TIMEOUT
+    for _ in range(2):
+        assert torch.equal(c.run(), Y) and L.poll_status(c.plan.buf) == 0
+
+
+def test_the_checked_build_keeps_to_the_extent_of_y():
+    code = textwrap.dedent("""
+        import sys, torch
+        sys.path.insert(0, "tests")
+        import test_gpu_adapters as t
+        import paper_2402_02446_b200 as L
+        from paper_2402_02446_b200 import binding
+        assert binding.DEBUG_BOUNDS
+        for y in ("f32", "bf16"):
+            for c in (t.Case(20, 256, 264, [8, 16], [0, 1] * 10, x="bf16", y0=y, y=y), t._many(9, y)):
+                Y = c.run()
+                assert L.poll_status(c.plan.buf) == 0
+                c.check(Y)
+                Z = torch.full_like(Y, 7.0)
+                L.debug_bounds_shrink(400)
+                try:
+                    c.run(Y=Z)
+                    torch.cuda.synchronize()
+                finally:
+                    L.debug_bounds_shrink(0)
+                assert L.poll_status(c.plan.buf) == t.BOUNDS
+                n = 400 // Y.element_size()
+                assert (Z.flatten()[-n:] == 7.0).all() and torch.equal(Z.flatten()[:-n - 16], Y.flatten()[:-n - 16])
+        print("fine")
+    """)
+    r = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))),
+                       env=dict(os.environ, LQER_DEBUG_BOUNDS="1"), capture_output=True, text=True, timeout=600)
+    assert r.returncode == 0 and "fine" in r.stdout, r.stdout[-1500:] + r.stderr[-2500:]
 
 
 def test_a_block_of_layers_with_adapters():
