@@ -64,6 +64,11 @@ __device__ __forceinline__ void store8(void* p, size_t idx, const float (&v)[8])
     q[1] = make_float4(v[4], v[5], v[6], v[7]);
   }
 }
+// 32 bytes, a whole sector, in one access.
+__device__ __forceinline__ void store32(void* p, const uint32_t (&u)[8]) {
+  asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+               ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
+}
 // Two fp32 operations in one instruction.
 struct F2 { unsigned long long w; };
 __device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.w) : "f"(a), "f"(b)); return r; }
@@ -526,17 +531,39 @@ static cudaError_t launch_gate_y(const GateParams& p, int act, int y_type, cudaS
 }
 
 // ---------------------------------------------------------------------------- MXINT activations as values
+// A thread takes whole blocks: 16 bytes of mantissas and an exponent.  wide: the values are aligned to 32 bytes.
 template <int YT>
-__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ Xq, void* Y, size_t octets, Format f) {
+__global__ void __launch_bounds__(256) dequantize_kernel(const uint8_t* __restrict__ Xq, void* Y, size_t blocks, bool wide, Format f) {
   tc::pdl_launch_dependents();
   tc::pdl_wait();
-  const uint8_t* exps = Xq + octets * 8;
-  for (size_t o = (size_t)blockIdx.x * blockDim.x + threadIdx.x; o < octets; o += (size_t)gridDim.x * blockDim.x) {
-    const uint2 m = *reinterpret_cast<const uint2*>(Xq + o * 8);
-    const uint32_t eb = exps[o >> 1];
-    const float4 a = mxint_quad_values(m.x, eb, f.bits, f.emin, f.emax), b = mxint_quad_values(m.y, eb, f.bits, f.emin, f.emax);
-    const float v[8] = {a.x, a.y, a.z, a.w, b.x, b.y, b.z, b.w};
-    store8<YT == kYBF16>(Y, o * 8, v);
+  const uint8_t* exps = Xq + blocks * 16;
+  for (size_t o = (size_t)blockIdx.x * blockDim.x + threadIdx.x; o < blocks; o += (size_t)gridDim.x * blockDim.x) {
+    const uint4 m = reinterpret_cast<const uint4*>(Xq)[o];
+    const uint32_t eb = exps[o];
+    float v[2][8];
+    const uint32_t w[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float4 q = mxint_quad_values(w[i], eb, f.bits, f.emin, f.emax);
+      v[i >> 1][4 * (i & 1)] = q.x; v[i >> 1][4 * (i & 1) + 1] = q.y; v[i >> 1][4 * (i & 1) + 2] = q.z; v[i >> 1][4 * (i & 1) + 3] = q.w;
+    }
+    if (!wide) {
+      store8<YT == kYBF16>(Y, o * 16, v[0]);
+      store8<YT == kYBF16>(Y, o * 16 + 8, v[1]);
+    } else if (YT == kYBF16) {
+      uint32_t u[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = round_bf16x2(v[i >> 2][2 * (i & 3)], v[i >> 2][2 * (i & 3) + 1]);
+      store32(static_cast<uint16_t*>(Y) + o * 16, u);
+    } else {
+#pragma unroll
+      for (int h = 0; h < 2; ++h) {
+        uint32_t u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = __float_as_uint(v[h][i]);
+        store32(static_cast<float*>(Y) + o * 16 + h * 8, u);
+      }
+    }
   }
 }
 
@@ -554,12 +581,13 @@ cudaError_t launch_gated_activation(const void* gate, const void* up, int x_type
   return x_type == kXBF16 ? bd::launch_gate_y<true>(p, act, y_type, s) : bd::launch_gate_y<false>(p, act, y_type, s);
 }
 cudaError_t launch_dequantize(const void* Xq, int M, int K, int bits, int emin, int emax, void* Y, int y_type, cudaStream_t s) {
-  const size_t octets = (size_t)M * K / 8, want = (octets + 255) / 256, most = (size_t)sm_count() * 32;
+  const size_t blocks = (size_t)M * K / 16, want = (blocks + 255) / 256, most = (size_t)sm_count() * 32;
+  const bool wide = reinterpret_cast<uintptr_t>(Y) % 32 == 0;
   const bd::Format f{bits, emin, emax};
   const dim3 grid((unsigned)(want < most ? want : most));
   LaunchScope scope(kFamQuantize, s);
-  return y_type == kYBF16 ? bd::launch_after(bd::dequantize_kernel<kYBF16>, grid, 256, s, static_cast<const uint8_t*>(Xq), Y, octets, f)
-                          : bd::launch_after(bd::dequantize_kernel<kYF32>, grid, 256, s, static_cast<const uint8_t*>(Xq), Y, octets, f);
+  return y_type == kYBF16 ? bd::launch_after(bd::dequantize_kernel<kYBF16>, grid, 256, s, static_cast<const uint8_t*>(Xq), Y, blocks, wide, f)
+                          : bd::launch_after(bd::dequantize_kernel<kYF32>, grid, 256, s, static_cast<const uint8_t*>(Xq), Y, blocks, wide, f);
 }
 
 }  // namespace lqer

@@ -180,6 +180,15 @@ def test_gated_activation_large_negative_gates_keep_their_borders():
         _check(L.gated_activation(g, u, act=act, cfg=cfg), _act64(g.double().cpu().numpy(), act)[0] * u.double().cpu().numpy(), 0, 64, 512, "mxint8", cfg)
 
 
+def test_values_into_a_tensor_aligned_to_16_bytes_only():
+    X = _values((9, 272), 44, torch.float32)
+    Xq = L.to_mxint8(*L.quantize_activations(X))
+    for dt in (torch.float32, torch.bfloat16):
+        n = 16 // torch.empty(0, dtype=dt).element_size()
+        Y = torch.empty(9 * 272 + 2 * n, dtype=dt, device=DEV)[n:n + 9 * 272].view(9, 272)
+        assert Y.data_ptr() % 32 == 16 and torch.equal(L.dequantize_activations(Xq, 9, 272, Y=Y), L.dequantize_activations(Xq, 9, 272, out_dtype=dt))
+
+
 def test_the_layer_takes_the_norms_output_as_its_own():
     # MXINT8 from the norm into the layer equals the fp32 values of that tensor into the layer, bit for bit
     import lqer_inputs as gen
