@@ -39,29 +39,43 @@ __host__ __device__ inline size_t partial_floats(int max_rank) { return (size_t)
 // change tiles costs a CTA about as much as four slabs, so tiles are cut alike where that makes the longest stretch no more than four
 // slabs longer (2048 rows of 4096 bf16 columns in 17 tiles, 8 against 7.4 slabs: 11.6 -> 9.2 us).
 struct Cut {
-  int KS, ctas, parts, each, rest;      // ctas: those that have work; parts == 0: units = each * ctas + rest
+  unsigned KS, each, rest;              // tiles * KS stays below 2^32: no more than 2^24 rows in 2^17 + 1025 tiles, and 2^20 columns
+  int ctas, parts;                      // ctas: those that have work; parts == 0: units = each * ctas + rest
   __device__ Cut(int tiles, int slabs, int most) : KS(slabs) {
-    const long long units = (long long)max(tiles, 0) * KS;
-    parts = tiles > 0 ? min(most / tiles, KS) : 0;
-    ctas = (int)min(units, (long long)most);
-    each = ctas > 0 ? (int)(units / ctas) : 0;
-    rest = ctas > 0 ? (int)(units - (long long)each * ctas) : 0;
-    if (parts > 0 && (KS + parts - 1) / parts <= each + (rest > 0 ? 1 : 0) + 4) {
-      each = (KS + parts - 1) / parts;
-      parts = (KS + each - 1) / each;
-      ctas = tiles * parts;
-    } else {
-      parts = 0;
+    const unsigned units = (unsigned)max(tiles, 0) * KS;
+    parts = tiles > 0 ? min(most / tiles, slabs) : 0;
+    ctas = (int)min(units, (unsigned)most);
+    each = ctas > 0 ? units / (unsigned)ctas : 0;
+    rest = units - each * (unsigned)ctas;
+    if (parts > 0) {
+      const unsigned alike = (KS + parts - 1) / parts;
+      if (alike <= each + (rest > 0 ? 1 : 0) + 4) {
+        each = alike;
+        parts = (KS + each - 1) / each;
+        ctas = tiles * parts;
+        return;
+      }
     }
+    parts = 0;
   }
   // first unit (tile * KS + slab) of CTA i's stretch; i may be ctas
-  __device__ long long first(int i) const {
-    if (parts > 0) return (long long)(i / parts) * KS + (i % parts) * each;
-    return (long long)each * i + (ctas > 0 ? rest * i / ctas : 0);
+  __device__ unsigned first(int i) const {
+    if (parts > 0) return (unsigned)i / (unsigned)parts * KS + (unsigned)i % (unsigned)parts * each;
+    return each * (unsigned)i + (ctas > 0 ? rest * (unsigned)i / (unsigned)ctas : 0u);
   }
-  // the CTA whose stretch holds a unit
-  __device__ int holder(long long u) const {
-    if (parts > 0) return (int)(u / KS) * parts + (int)(u % KS) / each;
+  // the first of the CTAs that have a share of a tile, and how many they are
+  __device__ int first_of(int tile, int& count) const {
+    if (ctas == 0) return count = 0;
+    if (parts > 0) {
+      count = parts;
+      return tile * parts;
+    }
+    const int a = holder((unsigned)tile * KS);
+    count = holder((unsigned)(tile + 1) * KS - 1) - a + 1;
+    return a;
+  }
+  // (parts == 0) the CTA whose stretch holds a unit
+  __device__ int holder(unsigned u) const {
     int i = min(max((int)((float)u / ((float)each + (float)rest / (float)ctas)), 0), ctas - 1);
     while (i + 1 < ctas && first(i + 1) <= u) ++i;
     while (first(i) > u) --i;
@@ -85,6 +99,17 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t (&r)[16])
         "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
       : "r"(taddr) : "memory");
 }
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
+__device__ __forceinline__ uint4 lds16(uint32_t a) {
+  uint4 v;
+  asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "r"(a) : "memory");
+  return v;
+}
 __device__ __forceinline__ uint32_t columns_pow2(int n) {
   uint32_t c = 32;
   while ((int)c < n) c *= 2;
@@ -92,7 +117,7 @@ __device__ __forceinline__ uint32_t columns_pow2(int n) {
 }
 // Barriers of a CTA, set up by its first thread.
 struct Barriers {
-  unsigned long long full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], t_full[2], t_empty[2], drawn[2], taken[2];
+  unsigned long long full[kMaxStages], copied[kMaxStages], empty[kMaxStages], acc_full[2], acc_empty[2], t_full[2], t_empty[2], drawn[4], taken[4];
 };
 __device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
 __device__ __forceinline__ void init_barriers(Barriers& b) {
@@ -106,6 +131,8 @@ __device__ __forceinline__ void init_barriers(Barriers& b) {
     tc::mbar_init(bar_of(b.acc_empty[i]), kWorkWarps);
     tc::mbar_init(bar_of(b.t_full[i]), 1);
     tc::mbar_init(bar_of(b.t_empty[i]), 1);
+  }
+  for (int i = 0; i < 4; ++i) {
     tc::mbar_init(bar_of(b.drawn[i]), 1);
     tc::mbar_init(bar_of(b.taken[i]), kWorkWarps + 1);
   }
@@ -120,14 +147,13 @@ struct Run {
   bool first;                // the first of its tile in this stretch
 };
 struct RunWalk {
-  long long u, end, begin;
-  int KS;
+  unsigned u, end, begin, KS;
   __device__ bool next(Run& r) {
     if (u >= end) return false;
     r.tile = (int)(u / KS);
     r.slab = (int)(u % KS);
     r.first = u == begin || r.slab == 0;
-    r.slabs = (int)min((long long)min(KS - r.slab, kMaxChain), end - u);
+    r.slabs = (int)min(min(KS - r.slab, (unsigned)kMaxChain), end - u);
     u += r.slabs;
     return true;
   }
@@ -336,10 +362,11 @@ __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ Man
     hd = load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes);
     rank = rank_of(p, slot, hd, threadIdx.x == 0 && e == 0);
   }
-  const int KS = (p.K + 63) / 64, first = e * 8 + h * 4;
+  const int first = e * 8 + h * 4;
   const bool here = e * 8 < (rank + 63) / 64 * 64, filled = here && first < rank;
-  const Cut cut(filled ? head.n_adapted : 0, KS, mp.project_ctas);
-  const int from = filled ? cut.holder((long long)tile * KS) : 0, count = filled ? cut.holder((long long)(tile + 1) * KS - 1) - from + 1 : 0;
+  const Cut cut(filled ? head.n_adapted : 0, (p.K + 63) / 64, mp.project_ctas);
+  int count;
+  const int from = cut.first_of(tile, count);
   const size_t per = partial_floats(p.max_rank) / 4;
   const float4* src = mp.scratch + (size_t)(tile + from) * per + (e * 2 + h) * 128 + m;
   tc::pdl_wait();
@@ -409,14 +436,14 @@ __device__ __forceinline__ void store_oct(const Params& p, size_t idx, const flo
 // 112 where every CTA had a stretch of its own).  The copying warp draws them, from a counter in the scratch; whose work a group
 // is changes nothing in the results.  What the other warps see of it:
 struct Groups {
-  volatile int2* list;       // two places in shared memory: group, rank of its tile's adapter
+  volatile int2* list;       // four places in shared memory: group, rank of its tile's adapter
   Barriers* bars;
   int k = 0;
   // the next group (all lanes of a warp, or one thread alone); negative if a wait ran out
   template <bool WARP>
   __device__ __forceinline__ int next(int& rank, volatile tc::WaitState* ws) {
-    const uint32_t slot = k & 1;
-    bool ok = tc::mbar_wait(bar_of(bars->drawn[slot]), (k >> 1) & 1, ws);
+    const uint32_t slot = k & 3;
+    bool ok = tc::mbar_wait(bar_of(bars->drawn[slot]), (k >> 2) & 1, ws);
     if (WARP) ok = __all_sync(0xFFFFFFFFu, ok) != 0;
     const int g = ok ? list[slot].x : -1;
     rank = list[slot].y;
@@ -427,15 +454,17 @@ struct Groups {
   }
 };
 
-template <bool Y0B, bool YB>
+// STAGED: Y0 is on its way two groups (fp32: one) ahead, 128 KB a CTA, by copies into shared memory; otherwise T leaves no room there,
+// and half as much is on its way into registers.
+template <bool Y0B, bool YB, bool STAGED>
 __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_constant__ ManyParams mp) {
   constexpr int TP = YB ? 2 : 3;
-  constexpr int AHEAD = Y0B ? 2 : 1;                    // blocks of 128 columns whose Y0 is on its way: 64 KB a CTA
+  constexpr int FIXED = STAGED && Y0B ? 3 : 2;          // groups of a CTA that need no drawing
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
   __shared__ tc::WaitState ws;
-  __shared__ volatile int2 list[2];
+  __shared__ volatile int2 list[4];
   const Params& p = mp.p;
   uint8_t* smem = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -466,6 +495,115 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
     // ---- accumulators and Y0 into Y: a warp has 32 rows and 32 columns of a block, a lane rows lane / 4 + 8 i and columns 8 (lane % 4) ...
     const int quarter = (warp & 3) * 32, first = (warp >> 2) * 32 + 8 * (lane & 3);
     int n = 0;                                          // turns with accumulators so far
+    auto rows_of = [&](int g, int (&r)[4]) {
+      const int t = g / NG, rows = p.tiles[t].rows;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int m = quarter + (lane >> 2) + 8 * i;
+        r[i] = p.rows[(size_t)t * kManyRows + m];
+        if (m >= rows) r[i] = -1;
+      }
+    };
+    if constexpr (STAGED) {
+      constexpr int A = FIXED - 1, D = 2 * A, WB = Y0B ? 2048 : 4096;      // groups ahead; blocks ahead; bytes of a warp's share of a block
+      const uint32_t yring = tc::smem_u32(ring + (size_t)mp.stages * image) + warp * D * WB;
+      // bf16: a lane sends for what it will need.  fp32: eight lanes send for the 128 bytes of a row, and pairs of rows swap their
+      // 16-byte pieces, so that the lanes that read them meet no bank twice.
+      auto send = [&](int slot, int g, int turn, const int (&r)[4]) {
+        const int col0 = (g % NG) * 256 + turn * 128 + (warp >> 2) * 32;
+        if (Y0B) {
+          const int col = col0 + 8 * (lane & 3);
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (g < groups && r[i] >= 0 && col < p.N)
+              cp_async16(yring + slot * WB + (i * 32 + lane) * 16, static_cast<const uint16_t*>(p.Y0) + (size_t)r[i] * p.N + col);
+        } else {
+          const int col = col0 + 4 * (lane & 7);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const int from = __shfl_sync(0xFFFFFFFFu, r[j >> 1], ((j & 1) * 4 + (lane >> 3)) * 4), m = 4 * j + (lane >> 3);
+            if (g < groups && from >= 0 && col < p.N)
+              cp_async16(yring + slot * WB + m * 128 + (((lane & 7) ^ (m & 1)) << 4), static_cast<const float*>(p.Y0) + (size_t)from * p.N + col);
+          }
+        }
+        cp_async_commit();
+      };
+      int row[A + 1][4], rank[A + 1], g[A + 1];
+#pragma unroll
+      for (int a = 0; a < A; ++a) {
+        g[a] = blockIdx.x + a * gridDim.x;
+        if (g[a] < groups) rows_of(g[a], row[a]);
+        send(2 * a, g[a], 0, row[a]);
+        send(2 * a + 1, g[a], 1, row[a]);
+      }
+#pragma unroll
+      for (int a = 0; a < A; ++a)
+        if (a == 0 || (g[a - 1] >= 0 && g[a - 1] < groups)) g[a] = mine.next<true>(rank[a], &ws);
+      int slot = 0;
+      while (g[0] >= 0 && g[0] < groups && ok) {
+        g[A] = g[A - 1];
+        if (g[A - 1] >= 0 && g[A - 1] < groups) g[A] = mine.next<true>(rank[A], &ws);
+        if (g[A] < 0) break;
+        if (g[A] < groups) rows_of(g[A], row[A]);
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {
+          if (!ok) break;
+          const int buf = n & 1, col = (g[0] % NG) * 256 + turn * 128 + first;
+          if (rank[0] > 0) {
+            ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
+            ++n;
+            tc::tc_fence_after();
+          }
+          cp_async_wait<D - 1>();
+          __syncwarp();
+          if (!ok) break;
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {                 // sixteen rows
+            uint32_t u[16];
+            if (rank[0] > 0) {
+              tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
+              tc::tmem_ld_wait();
+            } else {
+#pragma unroll
+              for (int i = 0; i < 16; ++i) u[i] = 0u;
+            }
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+              const int i = 2 * h + k, m = (lane >> 2) + 8 * i;
+              Oct<Y0B> y;
+              if (Y0B) {
+                y.a = lds16(yring + slot * WB + (i * 32 + lane) * 16);
+              } else {
+                y.a = lds16(yring + slot * WB + m * 128 + (((lane & 3) * 2 ^ (m & 1)) << 4));
+                y.b = lds16(yring + slot * WB + m * 128 + (((lane & 3) * 2 + 1 ^ (m & 1)) << 4));
+              }
+              float o[8];
+              y.values(o);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
+                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
+              }
+              if (row[0][i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[0][i] * p.N + col, o);
+            }
+          }
+          if (rank[0] > 0) tc::tc_fence_before();
+          __syncwarp();
+          if (rank[0] > 0 && lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
+          send(slot, g[A], turn, row[A]);
+          slot = slot + 1 == D ? 0 : slot + 1;
+        }
+#pragma unroll
+        for (int a = 0; a < A; ++a) {
+          g[a] = g[a + 1];
+          rank[a] = rank[a + 1];
+#pragma unroll
+          for (int i = 0; i < 4; ++i) row[a][i] = row[a + 1][i];
+        }
+      }
+      cp_async_wait<0>();
+    } else {
+    constexpr int AHEAD = Y0B ? 2 : 1;                  // blocks of 128 columns whose Y0 is on its way
     int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the next one
     Oct<Y0B> y[AHEAD][4];
     int ahead = -1, rank = 0, then_rank = 0;            // tile of the next group; ranks of the group at hand and of the next one
@@ -473,16 +611,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
       const int t = g / NG;
       if (t == ahead) return;
       ahead = t;
-      const int rows = p.tiles[t].rows;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = quarter + (lane >> 2) + 8 * i;
-        coming[i] = p.rows[(size_t)t * kManyRows + m];
-        if (m >= rows) coming[i] = -1;
-      }
+      rows_of(g, coming);
     };
-    int g = mine.next<true>(rank, &ws), then = groups;
-    if (g >= 0 && g < groups) {
+    int g = blockIdx.x, then = groups;                  // the first group needs no drawing
+    if (g < groups) {
       enter(g);
 #pragma unroll
       for (int a = 0; a < AHEAD; ++a) {
@@ -492,6 +624,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
           if (coming[i] >= 0 && col < p.N) y[a][i].load(p, (size_t)coming[i] * p.N + col);
       }
     }
+    g = mine.next<true>(rank, &ws);
     while (g >= 0 && g < groups && ok) {
 #pragma unroll
       for (int i = 0; i < 4; ++i) row[i] = coming[i];
@@ -534,53 +667,66 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
             }
             if (row[i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[i] * p.N + col, o);
           }
+#pragma unroll
+          for (int i = 2 * h; i < 2 * h + 2; ++i) {
+            const int r = own ? row[i] : coming[i];
+            if (r >= 0 && next_col < p.N) now[i].load(p, (size_t)r * p.N + next_col);
+          }
         }
         if (rank > 0) {
           tc::tc_fence_before();
           __syncwarp();
           if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
         }
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int r = own ? row[i] : coming[i];
-          if (r >= 0 && next_col < p.N) now[i].load(p, (size_t)r * p.N + next_col);
-        }
       }
       g = then;
       rank = then_rank;
     }
+    }
   } else if (warp == kCopyWarp) {
     // ---- draws the groups; copies a tile's images of T, and images of B: a stage is 128 columns of up to 64 ranks
     if (lane == 0) {
-      int it = 0, tiles = 0, at = -1, rank = 0, slot = -1, left = 0;
-      for (int k = 0, g = blockIdx.x, then = groups; ok; g = then, ++k) {
-        if (g < groups && g / NG != at) {
-          at = g / NG;
-          slot = p.tiles[at].slot;
-          rank = rank_of(p, slot, load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes), true);
-        } else {
-          at = -2 - at;                                 // the same tile
+      struct Item { int g, slot, rank; };
+      int it = 0, tiles = 0, at = -1, told = 0, left = 0;
+      Item then{-1, -1, 0};              // the last that was told
+      auto tell = [&](int g) {                          // the next group, to all warps
+        const int before = then.g;
+        then.g = g;
+        if (g < groups && (before < 0 || before / NG != g / NG)) {
+          then.slot = p.tiles[g / NG].slot;
+          then.rank = rank_of(p, then.slot, load_slot(p.pool + (size_t)max(then.slot, 0) * p.slot_bytes), true);
         }
-        ok = tc::mbar_wait(bar_of(bars.taken[k & 1]), ((k >> 1) & 1) ^ 1, &ws);
-        if (!ok) break;
-        list[k & 1].x = g;
-        list[k & 1].y = rank;
-        tc::mbar_arrive(bar_of(bars.drawn[k & 1]));
-        if (k == 0) tc::pdl_wait();                     // for the counter and T
-        if (g >= groups) break;
+        const int slot = told & 3;
+        ok = tc::mbar_wait(bar_of(bars.taken[slot]), ((told >> 2) & 1) ^ 1, &ws);
+        ++told;
+        if (!ok) return;
+        list[slot].x = g;
+        list[slot].y = then.rank;
+        tc::mbar_arrive(bar_of(bars.drawn[slot]));
+      };
+      // The first groups need no drawing, so that their Y0 comes while T is still being made.
+      Item items[FIXED];
+#pragma unroll
+      for (int k = 0; k < FIXED; ++k) {
+        if (k == 0 || then.g < groups) tell(blockIdx.x + k * gridDim.x);
+        items[k] = then;
+      }
+      tc::pdl_wait();                                   // for the counter and T
+      while (items[0].g < groups && ok) {
+        const int g = items[0].g, rank = items[0].rank, slot = items[0].slot;
+        int draw = groups;
         if (left > 0) {
-          --left;
-          then = g + 1;
-        } else {
+          draw = then.g + 1;
+        } else if (then.g < groups) {
           // several neighbours at a time (one T for all) as long as there is much left
-          const int take = g + 16 * (int)gridDim.x < groups ? 4 : g + 6 * (int)gridDim.x < groups ? 2 : 1;
-          then = (int)gridDim.x + atomicAdd(mp.drawn, take);
-          left = take - 1;
+          const int take = then.g + 16 * (int)gridDim.x < groups ? 4 : then.g + 6 * (int)gridDim.x < groups ? 2 : 1;
+          draw = FIXED * (int)gridDim.x + atomicAdd(mp.drawn, take);
+          left = take;
         }
+        --left;
         const int slabs = (rank + 63) / 64;
-        if (at < 0) {
-          at = -2 - at;
-        } else if (rank > 0) {
+        if (g / NG != at && rank > 0) {
+          at = g / NG;
           const int set = tiles % mp.t_sets, use = tiles / mp.t_sets;
           if (use > 0) ok = tc::mbar_wait(bar_of(bars.t_empty[set]), (use - 1) & 1, &ws);
           if (!ok) break;
@@ -600,6 +746,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
           tc::mbar_expect_tx(bar_of(bars.copied[st]), image);
           tc::bulk_load(tc::smem_u32(ring + (size_t)st * image), B + (size_t)s * image, image, bar_of(bars.copied[st]));
         }
+#pragma unroll
+        for (int k = 0; k + 1 < FIXED; ++k) items[k] = items[k + 1];
+        if (ok && then.g < groups) tell(draw);
+        items[FIXED - 1] = then;
       }
       // after a wait that ran out: no copy is left in flight
       const long long t0 = clock64();
@@ -694,12 +844,17 @@ static cudaError_t launch_project(ManyParams mp, cudaStream_t s) {
 }
 template <bool Y0B, bool YB>
 static cudaError_t launch_expand(ManyParams mp, int ctas, cudaStream_t s) {
-  static OncePerDevice once;
+  static OncePerDevice once[2];
   const size_t t = (size_t)(YB ? 2 : 3) * ((mp.p.max_rank + 63) / 64) * kXImage, image = (size_t)128 * b_pitch(mp.p.max_rank);
-  mp.t_sets = 2 * t + 2 * image + 1024 <= kSmemMost ? 2 : 1;
-  mp.stages = (int)((kSmemMost - 1024 - mp.t_sets * t) / image);
+  const size_t staged = 128 * 1024, most = kSmemMost - 1024;
+  const bool fits = t + 2 * image + staged <= most;
+  const size_t room = fits ? most - staged : most;
+  mp.t_sets = 2 * t + 2 * image <= room ? 2 : 1;
+  mp.stages = (int)((room - mp.t_sets * t) / image);
   if (mp.stages > kMaxStages) mp.stages = kMaxStages;
-  return launch(expand_kernel<Y0B, YB>, once, mp, ctas, kManyThreads, mp.t_sets * t + mp.stages * image + 1024, s);
+  const size_t smem = mp.t_sets * t + mp.stages * image + (fits ? staged : 0) + 1024;
+  return fits ? launch(expand_kernel<Y0B, YB, true>, once[0], mp, ctas, kManyThreads, smem, s)
+              : launch(expand_kernel<Y0B, YB, false>, once[1], mp, ctas, kManyThreads, smem, s);
 }
 cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s) {
   const int sms = sm_count(), ctas = sms < kPrologueMaxCtas ? sms : kPrologueMaxCtas;
