@@ -489,6 +489,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   const bool fits = plan_fits(p, head);
   const int NG = (p.N + 255) / 256, NC = (p.N + 127) / 128;
   const int groups = fits ? (p.Y0 == p.Y ? head.n_adapted : head.n_tiles) * NG : 0;
+  // a CTA's first groups: neighbours where all CTAs get as many, so that one T serves them
+  const bool side_by_side = groups >= FIXED * (int)gridDim.x;
+  const int g0 = blockIdx.x * (side_by_side ? FIXED : 1), g_step = side_by_side ? 1 : gridDim.x;
   bool ok = true;
   Groups mine{list, &bars};
   if (warp < kWorkWarps) {
@@ -531,7 +534,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
       int row[A + 1][4], rank[A + 1], g[A + 1];
 #pragma unroll
       for (int a = 0; a < A; ++a) {
-        g[a] = blockIdx.x + a * gridDim.x;
+        g[a] = g0 + a * g_step;
         if (g[a] < groups) rows_of(g[a], row[a]);
         send(2 * a, g[a], 0, row[a]);
         send(2 * a + 1, g[a], 1, row[a]);
@@ -613,7 +616,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
       ahead = t;
       rows_of(g, coming);
     };
-    int g = blockIdx.x, then = groups;                  // the first group needs no drawing
+    int g = g0, then = groups;                          // the first group needs no drawing
     if (g < groups) {
       enter(g);
 #pragma unroll
@@ -708,7 +711,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
       Item items[FIXED];
 #pragma unroll
       for (int k = 0; k < FIXED; ++k) {
-        if (k == 0 || then.g < groups) tell(blockIdx.x + k * gridDim.x);
+        if (k == 0 || then.g < groups) tell(g0 + k * g_step);
         items[k] = then;
       }
       tc::pdl_wait();                                   // for the counter and T
