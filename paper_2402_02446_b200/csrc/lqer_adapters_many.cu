@@ -418,16 +418,16 @@ struct Oct {
   }
 };
 template <bool BF16>
-__device__ __forceinline__ void store_oct(const Params& p, size_t idx, const float (&v)[8]) {
-  if (!LQER_IN_BOUNDS(&p.plan->status, idx * (BF16 ? 2 : 4), BF16 ? 16 : 32, p.y_extent, 812)) return;
+__device__ __forceinline__ void store_oct(const Params& p, uint8_t* to, const float (&v)[8]) {
+  if (!LQER_IN_BOUNDS(&p.plan->status, to - static_cast<uint8_t*>(p.Y), BF16 ? 16 : 32, p.y_extent, 812)) return;
   if (BF16) {
-    *reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.Y) + idx) =
+    *reinterpret_cast<uint4*>(to) =
         make_uint4(round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]), round_bf16x2(v[6], v[7]));
   } else {
     uint4 a, b;
     a.x = __float_as_uint(v[0]); a.y = __float_as_uint(v[1]); a.z = __float_as_uint(v[2]); a.w = __float_as_uint(v[3]);
     b.x = __float_as_uint(v[4]); b.y = __float_as_uint(v[5]); b.z = __float_as_uint(v[6]); b.w = __float_as_uint(v[7]);
-    st32(static_cast<float*>(p.Y) + idx, p.y_wide, a, b);
+    st32(to, p.y_wide, a, b);
   }
 }
 
@@ -435,22 +435,22 @@ __device__ __forceinline__ void store_oct(const Params& p, size_t idx, const flo
 // and CTAs that work side by side on neighbouring columns are kind to the memory's pages (4096 rows of 13824 fp32 columns: 88 us, against
 // 112 where every CTA had a stretch of its own).  The copying warp draws them, from a counter in the scratch; whose work a group
 // is changes nothing in the results.  What the other warps see of it:
+struct Group { int g, rank, tile, part; };       // part: which 256 columns of the tile
 struct Groups {
-  volatile int2* list;       // four places in shared memory: group, rank of its tile's adapter
+  uint32_t list;             // four places in shared memory
   Barriers* bars;
   int k = 0;
-  // the next group (all lanes of a warp, or one thread alone); negative if a wait ran out
+  // the next group (all lanes of a warp, or one thread alone); g is negative if a wait ran out
   template <bool WARP>
-  __device__ __forceinline__ int next(int& rank, volatile tc::WaitState* ws) {
-    const uint32_t slot = k & 3;
-    bool ok = tc::mbar_wait(bar_of(bars->drawn[slot]), (k >> 2) & 1, ws);
+  __device__ __forceinline__ Group next(volatile tc::WaitState* ws) {
+    const uint32_t place = k & 3;
+    bool ok = tc::mbar_wait(bar_of(bars->drawn[place]), (k >> 2) & 1, ws);
     if (WARP) ok = __all_sync(0xFFFFFFFFu, ok) != 0;
-    const int g = ok ? list[slot].x : -1;
-    rank = list[slot].y;
+    const uint4 v = lds16(list + place * 16);
     if (WARP) __syncwarp();
-    if (!WARP || (threadIdx.x & 31) == 0) tc::mbar_arrive(bar_of(bars->taken[slot]));
+    if (!WARP || (threadIdx.x & 31) == 0) tc::mbar_arrive(bar_of(bars->taken[place]));
     ++k;
-    return g;
+    return Group{ok ? (int)v.x : -1, (int)v.y, (int)v.z, (int)v.w};
   }
 };
 
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
   __shared__ tc::WaitState ws;
-  __shared__ volatile int2 list[4];
+  __shared__ int4 list[4];
   const Params& p = mp.p;
   uint8_t* smem = smem_raw + ((1024u - (tc::smem_u32(smem_raw) & 1023u)) & 1023u);
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -493,65 +493,101 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
   const bool side_by_side = groups >= FIXED * (int)gridDim.x;
   const int g0 = blockIdx.x * (side_by_side ? FIXED : 1), g_step = side_by_side ? 1 : gridDim.x;
   bool ok = true;
-  Groups mine{list, &bars};
+  Groups mine{tc::smem_u32(list), &bars};
   if (warp < kWorkWarps) {
     // ---- accumulators and Y0 into Y: a warp has 32 rows and 32 columns of a block, a lane rows lane / 4 + 8 i and columns 8 (lane % 4) ...
     const int quarter = (warp & 3) * 32, first = (warp >> 2) * 32 + 8 * (lane & 3);
     int n = 0;                                          // turns with accumulators so far
-    auto rows_of = [&](int g, int (&r)[4]) {
-      const int t = g / NG, rows = p.tiles[t].rows;
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int m = quarter + (lane >> 2) + 8 * i;
-        r[i] = p.rows[(size_t)t * kManyRows + m];
-        if (m >= rows) r[i] = -1;
-      }
-    };
     if constexpr (STAGED) {
       constexpr int A = FIXED - 1, D = 2 * A, WB = Y0B ? 2048 : 4096;      // groups ahead; blocks ahead; bytes of a warp's share of a block
+      constexpr int SENDS = Y0B ? 4 : 8, ROWS = Y0B ? 8 : 4;               // copies of a lane for a block; rows that one copy of all lanes covers
       const uint32_t yring = tc::smem_u32(ring + (size_t)mp.stages * image) + warp * D * WB;
-      // bf16: a lane sends for what it will need.  fp32: eight lanes send for the 128 bytes of a row, and pairs of rows swap their
-      // 16-byte pieces, so that the lanes that read them meet no bank twice.
-      auto send = [&](int slot, int g, int turn, const int (&r)[4]) {
-        const int col0 = (g % NG) * 256 + turn * 128 + (warp >> 2) * 32;
+      // Of a group: the lane's four rows, those that there are, and, for the copies, rows and places.  bf16: a lane sends for what it will
+      // need.  fp32: eight lanes send for the 128 bytes of a row, and pairs of rows swap their 16-byte pieces, so that the lanes that
+      // read them meet no bank twice.
+      struct Place { int row[4], col; uint32_t there; };
+      const int piece = Y0B ? lane & 3 : lane & 7, send_row = Y0B ? lane >> 2 : lane >> 3;
+      uint32_t send_to[2], get_from[2];                 // of even and odd rows
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        send_to[i] = Y0B ? lane * 16 : (4 * i + send_row) * 128 + ((piece ^ (send_row & 1)) << 4);
+        get_from[i] = Y0B ? lane * 16 : (lane >> 2) * 128 + ((2 * (lane & 3) + i ^ (lane >> 2 & 1)) << 4);
+      }
+      auto place = [&](int tile, int part, Place& q) {
+        const int rows = p.tiles[tile].rows;
+        q.col = part * 256 + first;
+        q.there = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int m = quarter + (lane >> 2) + 8 * i;
+          q.row[i] = p.rows[(size_t)tile * kManyRows + m];
+          if (m < rows) q.there |= 1u << i;
+        }
+      };
+      const uint8_t* from[SENDS];                       // of the group that is sent for
+      uint32_t from_there = 0;
+      int from_col = 0;
+      auto sources = [&](int tile, int part, const Place& q) {
+        constexpr int EB = Y0B ? 2 : 4;
+        from_col = part * 256 + (warp >> 2) * 32 + piece * (Y0B ? 8 : 4);
+        from_there = 0;
         if (Y0B) {
-          const int col = col0 + 8 * (lane & 3);
+          from_there = q.there;
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (g < groups && r[i] >= 0 && col < p.N)
-              cp_async16(yring + slot * WB + (i * 32 + lane) * 16, static_cast<const uint16_t*>(p.Y0) + (size_t)r[i] * p.N + col);
+          for (int j = 0; j < 4; ++j) from[j] = static_cast<const uint8_t*>(p.Y0) + ((size_t)q.row[j] * p.N + from_col) * EB;
         } else {
-          const int col = col0 + 4 * (lane & 7);
+          const int rows = p.tiles[tile].rows;
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const int from = __shfl_sync(0xFFFFFFFFu, r[j >> 1], ((j & 1) * 4 + (lane >> 3)) * 4), m = 4 * j + (lane >> 3);
-            if (g < groups && from >= 0 && col < p.N)
-              cp_async16(yring + slot * WB + m * 128 + (((lane & 7) ^ (m & 1)) << 4), static_cast<const float*>(p.Y0) + (size_t)from * p.N + col);
+          for (int j = 0; j < SENDS; ++j) {
+            const int m = quarter + ROWS * j + send_row;
+            from[j] = static_cast<const uint8_t*>(p.Y0) + ((size_t)p.rows[(size_t)tile * kManyRows + m] * p.N + from_col) * EB;
+            if (m < rows) from_there |= 1u << j;
           }
         }
+      };
+      auto send = [&](int slot, int turn, bool any) {
+        const uint32_t there = any && from_col + turn * 128 < p.N ? from_there : 0u;
+#pragma unroll
+        for (int j = 0; j < SENDS; ++j)
+          if (there & 1u << j)
+            cp_async16(yring + slot * WB + (Y0B ? j * 512 + send_to[0] : (j >> 1) * 1024 + send_to[j & 1]), from[j] + turn * (Y0B ? 256 : 512));
         cp_async_commit();
       };
-      int row[A + 1][4], rank[A + 1], g[A + 1];
+      Place q[A + 1];
+      int rank[A + 1], g[A + 1];
 #pragma unroll
       for (int a = 0; a < A; ++a) {
         g[a] = g0 + a * g_step;
-        if (g[a] < groups) rows_of(g[a], row[a]);
-        send(2 * a, g[a], 0, row[a]);
-        send(2 * a + 1, g[a], 1, row[a]);
+        if (g[a] < groups) {
+          place(g[a] / NG, g[a] % NG, q[a]);
+          sources(g[a] / NG, g[a] % NG, q[a]);
+        }
+        send(2 * a, 0, g[a] < groups);
+        send(2 * a + 1, 1, g[a] < groups);
       }
 #pragma unroll
       for (int a = 0; a < A; ++a)
-        if (a == 0 || (g[a - 1] >= 0 && g[a - 1] < groups)) g[a] = mine.next<true>(rank[a], &ws);
+        if (a == 0 || (g[a - 1] >= 0 && g[a - 1] < groups)) {
+          const Group next = mine.next<true>(&ws);
+          g[a] = next.g;
+          rank[a] = next.rank;
+        }
       int slot = 0;
       while (g[0] >= 0 && g[0] < groups && ok) {
-        g[A] = g[A - 1];
-        if (g[A - 1] >= 0 && g[A - 1] < groups) g[A] = mine.next<true>(rank[A], &ws);
-        if (g[A] < 0) break;
-        if (g[A] < groups) rows_of(g[A], row[A]);
+        Group next{groups, 0, 0, 0};
+        if (g[A - 1] >= 0 && g[A - 1] < groups) next = mine.next<true>(&ws);
+        if (next.g < 0) break;
+        g[A] = next.g;
+        rank[A] = next.rank;
+        const bool more = next.g < groups;
+        if (more) place(next.tile, next.part, q[A]);
+        uint8_t* to[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) to[i] = static_cast<uint8_t*>(p.Y) + ((size_t)q[0].row[i] * p.N + q[0].col) * (YB ? 2 : 4);
 #pragma unroll
         for (int turn = 0; turn < 2; ++turn) {
           if (!ok) break;
-          const int buf = n & 1, col = (g[0] % NG) * 256 + turn * 128 + first;
+          const int buf = n & 1;
           if (rank[0] > 0) {
             ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
             ++n;
@@ -560,6 +596,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
           cp_async_wait<D - 1>();
           __syncwarp();
           if (!ok) break;
+          const uint32_t there = q[0].col + turn * 128 < p.N ? q[0].there : 0u, here = yring + slot * WB;
 #pragma unroll
           for (int h = 0; h < 2; ++h) {                 // sixteen rows
             uint32_t u[16];
@@ -572,14 +609,10 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
             }
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
-              const int i = 2 * h + k, m = (lane >> 2) + 8 * i;
+              const int i = 2 * h + k;
               Oct<Y0B> y;
-              if (Y0B) {
-                y.a = lds16(yring + slot * WB + (i * 32 + lane) * 16);
-              } else {
-                y.a = lds16(yring + slot * WB + m * 128 + (((lane & 3) * 2 ^ (m & 1)) << 4));
-                y.b = lds16(yring + slot * WB + m * 128 + (((lane & 3) * 2 + 1 ^ (m & 1)) << 4));
-              }
+              y.a = lds16(here + i * WB / 4 + get_from[0]);
+              if (!Y0B) y.b = lds16(here + i * WB / 4 + get_from[1]);
               float o[8];
               y.values(o);
 #pragma unroll
@@ -587,104 +620,108 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
                 o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
                 o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
               }
-              if (row[0][i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[0][i] * p.N + col, o);
+              if (there & 1u << i) store_oct<YB>(p, to[i] + turn * (YB ? 256 : 512), o);
             }
           }
           if (rank[0] > 0) tc::tc_fence_before();
           __syncwarp();
           if (rank[0] > 0 && lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
-          send(slot, g[A], turn, row[A]);
+          if (turn == 0 && more) sources(next.tile, next.part, q[A]);
+          send(slot, turn, more);
           slot = slot + 1 == D ? 0 : slot + 1;
         }
 #pragma unroll
         for (int a = 0; a < A; ++a) {
           g[a] = g[a + 1];
           rank[a] = rank[a + 1];
-#pragma unroll
-          for (int i = 0; i < 4; ++i) row[a][i] = row[a + 1][i];
+          q[a] = q[a + 1];
         }
       }
       cp_async_wait<0>();
     } else {
-    constexpr int AHEAD = Y0B ? 2 : 1;                  // blocks of 128 columns whose Y0 is on its way
-    int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the next one
-    Oct<Y0B> y[AHEAD][4];
-    int ahead = -1, rank = 0, then_rank = 0;            // tile of the next group; ranks of the group at hand and of the next one
-    auto enter = [&](int g) {                           // the rows of group g's tile
-      const int t = g / NG;
-      if (t == ahead) return;
-      ahead = t;
-      rows_of(g, coming);
-    };
-    int g = g0, then = groups;                          // the first group needs no drawing
-    if (g < groups) {
-      enter(g);
+      constexpr int AHEAD = Y0B ? 2 : 1;                  // blocks of 128 columns whose Y0 is on its way
+      int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the next one
+      Oct<Y0B> y[AHEAD][4];
+      int ahead = -1;                                     // tile of the next group
+      auto enter = [&](int t) {                           // the rows of a group's tile
+        if (t == ahead) return;
+        ahead = t;
+        const int rows = p.tiles[t].rows;
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) {
-        const int col = (g % NG) * 256 + a * 128 + first;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (coming[i] >= 0 && col < p.N) y[a][i].load(p, (size_t)coming[i] * p.N + col);
-      }
-    }
-    g = mine.next<true>(rank, &ws);
-    while (g >= 0 && g < groups && ok) {
-#pragma unroll
-      for (int i = 0; i < 4; ++i) row[i] = coming[i];
-      then = mine.next<true>(then_rank, &ws);
-      const bool more = then >= 0 && then < groups;
-      if (more) enter(then);
-#pragma unroll
-      for (int turn = 0; turn < 2; ++turn) {
-        if (!ok) break;
-        const int buf = n & 1, col = (g % NG) * 256 + turn * 128 + first;
-        if (rank > 0) {
-          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
-          ++n;
-          tc::tc_fence_after();
+        for (int i = 0; i < 4; ++i) {
+          const int m = quarter + (lane >> 2) + 8 * i;
+          coming[i] = p.rows[(size_t)t * kManyRows + m];
+          if (m >= rows) coming[i] = -1;
         }
-        if (!ok) break;
-        Oct<Y0B>(&now)[4] = y[AHEAD == 2 ? turn : 0];
-        // what comes into the same registers: this group's second block, or the next group's
-        const bool own = AHEAD == 1 && turn == 0;
-        const int next_col = own ? col + 128 : more ? (then % NG) * 256 + (AHEAD == 2 ? turn * 128 : 0) + first : p.N;
+      };
+      if (g0 < groups) {
+        enter(g0 / NG);
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {                   // sixteen rows
-          uint32_t u[16];
+        for (int a = 0; a < AHEAD; ++a) {
+          const int col = g0 % NG * 256 + a * 128 + first;
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (coming[i] >= 0 && col < p.N) y[a][i].load(p, (size_t)coming[i] * p.N + col);
+        }
+      }
+      Group at_hand = mine.next<true>(&ws);
+      while (at_hand.g >= 0 && at_hand.g < groups && ok) {
+        const int rank = at_hand.rank;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) row[i] = coming[i];
+        const Group then = mine.next<true>(&ws);
+        const bool more = then.g >= 0 && then.g < groups;
+        if (more) enter(then.tile);
+#pragma unroll
+        for (int turn = 0; turn < 2; ++turn) {
+          if (!ok) break;
+          const int buf = n & 1, col = at_hand.part * 256 + turn * 128 + first;
           if (rank > 0) {
-            tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
-            tc::tmem_ld_wait();
-          } else {
-#pragma unroll
-            for (int i = 0; i < 16; ++i) u[i] = 0u;
+            ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
+            ++n;
+            tc::tc_fence_after();
           }
+          if (!ok) break;
+          Oct<Y0B>(&now)[4] = y[AHEAD == 2 ? turn : 0];
+          // what comes into the same registers: this group's second block, or the next group's
+          const bool own = AHEAD == 1 && turn == 0;
+          const int next_col = own ? col + 128 : more ? then.part * 256 + (AHEAD == 2 ? turn * 128 : 0) + first : p.N;
 #pragma unroll
-          for (int k = 0; k < 2; ++k) {
-            const int i = 2 * h + k;
-            float o[8];
-            now[i].values(o);
+          for (int h = 0; h < 2; ++h) {                   // sixteen rows
+            uint32_t u[16];
+            if (rank > 0) {
+              tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
+              tc::tmem_ld_wait();
+            } else {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
-              o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
+              for (int i = 0; i < 16; ++i) u[i] = 0u;
             }
-            if (row[i] >= 0 && col < p.N) store_oct<YB>(p, (size_t)row[i] * p.N + col, o);
-          }
 #pragma unroll
-          for (int i = 2 * h; i < 2 * h + 2; ++i) {
-            const int r = own ? row[i] : coming[i];
-            if (r >= 0 && next_col < p.N) now[i].load(p, (size_t)r * p.N + next_col);
+            for (int k = 0; k < 2; ++k) {
+              const int i = 2 * h + k;
+              float o[8];
+              now[i].values(o);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) {
+                o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
+                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
+              }
+              if (row[i] >= 0 && col < p.N) store_oct<YB>(p, static_cast<uint8_t*>(p.Y) + ((size_t)row[i] * p.N + col) * (YB ? 2 : 4), o);
+            }
+#pragma unroll
+            for (int i = 2 * h; i < 2 * h + 2; ++i) {
+              const int r = own ? row[i] : coming[i];
+              if (r >= 0 && next_col < p.N) now[i].load(p, (size_t)r * p.N + next_col);
+            }
+          }
+          if (rank > 0) {
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
           }
         }
-        if (rank > 0) {
-          tc::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
-        }
+        at_hand = then;
       }
-      g = then;
-      rank = then_rank;
-    }
     }
   } else if (warp == kCopyWarp) {
     // ---- draws the groups; copies a tile's images of T, and images of B: a stage is 128 columns of up to 64 ranks
@@ -703,8 +740,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
         ok = tc::mbar_wait(bar_of(bars.taken[slot]), ((told >> 2) & 1) ^ 1, &ws);
         ++told;
         if (!ok) return;
-        list[slot].x = g;
-        list[slot].y = then.rank;
+        list[slot] = make_int4(g, then.rank, g / NG, g % NG);
         tc::mbar_arrive(bar_of(bars.drawn[slot]));
       };
       // The first groups need no drawing, so that their Y0 comes while T is still being made.
@@ -769,9 +805,9 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
     // ---- MMAs
     if (lane == 0) {
       const uint32_t idesc = tc::make_idesc(128, 128);
-      int it = 0, n = 0, tiles = 0, at = -1, rank;
-      for (int g = mine.next<false>(rank, &ws); g >= 0 && g < groups && ok; g = mine.next<false>(rank, &ws)) {
-        const int t = g / NG, slabs = (rank + 63) / 64, r16 = rank16(rank);
+      int it = 0, n = 0, tiles = 0, at = -1;
+      for (Group now = mine.next<false>(&ws); now.g >= 0 && now.g < groups && ok; now = mine.next<false>(&ws)) {
+        const int rank = now.rank, t = now.tile, slabs = (rank + 63) / 64, r16 = rank16(rank);
         if (rank == 0) continue;
         if (t != at) {
           at = t;
@@ -783,7 +819,7 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
         for (int turn = 0; turn < 2 && ok; ++turn, ++n) {
           ok = tc::mbar_wait(bar_of(bars.acc_empty[n & 1]), ((n >> 1) & 1) ^ 1, &ws);
           tc::tc_fence_after();
-          const int stages = (g % NG) * 2 + turn < NC ? slabs : 0;
+          const int stages = now.part * 2 + turn < NC ? slabs : 0;
           for (int s = 0; s < stages && ok; ++s, ++it) {
             const int st = it % mp.stages, round = it / mp.stages;
             ok = tc::mbar_wait(bar_of(bars.copied[st]), round & 1, &ws);
