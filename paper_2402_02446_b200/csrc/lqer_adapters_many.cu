@@ -102,6 +102,9 @@ __device__ __forceinline__ void tmem_ld_16x32(uint32_t taddr, uint32_t (&r)[16])
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src) {
   asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
 }
+__device__ __forceinline__ void cp_async16_or_zeros(uint32_t dst, const void* src, int bytes) {      // bytes: 16, or 0 for zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
 __device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N>
 __device__ __forceinline__ void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
@@ -163,9 +166,10 @@ __device__ __forceinline__ int project_rank16(const Params& p, int tile, int& sl
   return max(rank16(rank_of(p, slot, load_slot(p.pool + (size_t)slot * p.slot_bytes), false)), 1);
 }
 
-template <int XT, int XP>
+// AHEAD: slabs whose X is on its way, 32 KB (fp32) or 16 KB each: fp32 by copies into shared memory, the others into registers.
+template <int XT, int XP, int AHEAD>
 __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_constant__ ManyParams mp) {
-  constexpr int AHEAD = XT == kXF32 ? 2 : 6;            // slabs whose X is on its way (fp32: more would not fit the registers)
+  constexpr bool STAGED = XT == kXF32;
   constexpr int RW = 128 / kWorkWarps / 4;              // rows of a lane: eight lanes a row
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
@@ -202,51 +206,95 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
     int it = 0, runs = 0;
     const uint32_t piece = lane & 7;
     while (ok && walk.next(r)) {
-      typename XOct<XT>::Place from[RW];                // of the octet that is sent for next
       uint32_t at[RW];
-      int col = r.slab * 64 + piece * 8;
-      const int stop = min((r.slab + r.slabs) * 64, p.K);
 #pragma unroll
-      for (int i = 0; i < RW; ++i) {
-        const int m = (warp * RW + i) * 4 + (lane >> 3);
-        from[i].set(p, p.rows[(size_t)r.tile * kManyRows + m], col);
-        at[i] = swizzled(m, piece, 128);
-      }
-      XOct<XT> x[AHEAD][RW];
-      auto load = [&](XOct<XT> (&o)[RW]) {              // the next slab's
+      for (int i = 0; i < RW; ++i) at[i] = swizzled((warp * RW + i) * 4 + (lane >> 3), piece, 128);
+      const int stop = min((r.slab + r.slabs) * 64, p.K);
+      int slot, r16;
+      // one slab's octets into a stage, once it is free; sent: what has to be done as soon as they are in registers
+      auto put = [&](const XOct<XT> (&x)[RW], auto&& sent) {
+        const int st = it % mp.stages, turn = it / mp.stages;
+        ++it;
+        ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[st]), (turn & 1) ^ 1, &ws)) != 0;
+        if (!ok) return;
+        uint8_t* img = smem + (size_t)st * stage_bytes;
 #pragma unroll
         for (int i = 0; i < RW; ++i) {
-          o[i].load(p, from[i], col < stop);
-          from[i].next_slab();
+          uint32_t w[4][XP];
+          x[i].template pairs<XP>(p, w);
+#pragma unroll
+          for (int k = 0; k < XP; ++k) *reinterpret_cast<uint4*>(img + k * kXImage + at[i]) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
         }
-        col += 64;
+        sent();
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar_of(bars.full[st]));
       };
+      if constexpr (STAGED) {
+        // A warp's eight rows of 256 bytes, in 16-byte pieces: sixteen lanes send for a row.  A lane reads two neighbouring pieces of a row;
+        // pieces of a row's second half change places with their neighbours, so that eight lanes meet no bank twice.
+        const uint8_t* from[4];
+        const int c = lane & 15;
+        const uint32_t ring = tc::smem_u32(smem + (size_t)mp.stages * stage_bytes) + warp * 2048;
+        const uint32_t to = (lane >> 4) * 256 + ((c ^ (c >> 3)) << 4), get = (lane >> 3) * 256 + ((2 * piece ^ (piece >> 2)) << 4);
+        int col = r.slab * 64 + c * 4, sent_for = 0, here = 0;
 #pragma unroll
-      for (int a = 0; a < AHEAD; ++a) load(x[a]);
-      int slot;
-      const int r16 = project_rank16(p, r.tile, slot);
-      for (int s0 = 0; s0 < r.slabs && ok; s0 += AHEAD) {
+        for (int j = 0; j < 4; ++j)
+          from[j] = static_cast<const uint8_t*>(p.X) + ((size_t)p.rows[(size_t)r.tile * kManyRows + warp * 8 + 2 * j + (lane >> 4)] * p.K + col) * 4;
+        auto send = [&] {                               // for the next slab
+          if (sent_for < r.slabs) {
+            const int bytes = col < stop ? 16 : 0;      // beyond K: zeros
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-          if (s0 + a < r.slabs && ok) {
-            const int st = it % mp.stages, turn = it / mp.stages;
-            ++it;
-            ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[st]), (turn & 1) ^ 1, &ws)) != 0;
-            if (ok) {
-              uint8_t* img = smem + (size_t)st * stage_bytes;
-#pragma unroll
-              for (int i = 0; i < RW; ++i) {
-                uint32_t w[4][XP];
-                x[a][i].template pairs<XP>(p, w);
-#pragma unroll
-                for (int k = 0; k < XP; ++k) *reinterpret_cast<uint4*>(img + k * kXImage + at[i]) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
-              }
-              load(x[a]);
-              tc::fence_proxy_async_smem();
-              __syncwarp();
-              if (lane == 0) tc::mbar_arrive(bar_of(bars.full[st]));
+            for (int j = 0; j < 4; ++j) {
+              cp_async16_or_zeros(ring + (uint32_t)(sent_for % AHEAD) * (kWorkWarps * 2048) + j * 512 + to, bytes ? from[j] : static_cast<const uint8_t*>(p.X), bytes);
+              from[j] += 256;
             }
           }
+          cp_async_commit();
+          ++sent_for;
+          col += 64;
+        };
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) send();
+        r16 = project_rank16(p, r.tile, slot);
+        for (int s = 0; s < r.slabs && ok; ++s) {
+          cp_async_wait<AHEAD - 1>();
+          __syncwarp();
+          XOct<XT> x[RW];
+          const uint32_t src = ring + (uint32_t)here * (kWorkWarps * 2048) + get;
+#pragma unroll
+          for (int i = 0; i < RW; ++i) {
+            x[i].a = lds16(src + i * 1024);
+            x[i].b = lds16((src + i * 1024) ^ 16);
+          }
+          here = here + 1 == AHEAD ? 0 : here + 1;
+          __syncwarp();
+          send();
+          put(x, [] {});
+        }
+        cp_async_wait<0>();
+        __syncwarp();
+      } else {
+        typename XOct<XT>::Place from[RW];              // of the octet that is sent for next
+        int col = r.slab * 64 + piece * 8;
+#pragma unroll
+        for (int i = 0; i < RW; ++i) from[i].set(p, p.rows[(size_t)r.tile * kManyRows + (warp * RW + i) * 4 + (lane >> 3)], col);
+        XOct<XT> x[AHEAD][RW];
+        auto load = [&](XOct<XT> (&o)[RW]) {            // the next slab's
+#pragma unroll
+          for (int i = 0; i < RW; ++i) {
+            o[i].load(p, from[i], col < stop);
+            from[i].next_slab();
+          }
+          col += 64;
+        };
+#pragma unroll
+        for (int a = 0; a < AHEAD; ++a) load(x[a]);
+        r16 = project_rank16(p, r.tile, slot);
+        for (int s0 = 0; s0 < r.slabs && ok; s0 += AHEAD) {
+#pragma unroll
+          for (int a = 0; a < AHEAD; ++a)
+            if (s0 + a < r.slabs && ok) put(x[a], [&] { load(x[a]); });
         }
       }
       if (ok) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[0]), runs & 1, &ws)) != 0;
@@ -873,13 +921,13 @@ static cudaError_t launch(Kernel kernel, OncePerDevice& once, const ManyParams& 
   cfg.numAttrs = 1;
   return cudaLaunchKernelEx(&cfg, kernel, mp);
 }
-template <int XT, int XP>
+template <int XT, int XP, int AHEAD>
 static cudaError_t launch_project(ManyParams mp, cudaStream_t s) {
   static OncePerDevice once;
-  const size_t stage = (size_t)XP * kXImage + rank16(mp.p.max_rank) * 2048;
-  mp.stages = (int)((kSmemMost - 1024) / stage);
+  const size_t stage = (size_t)XP * kXImage + rank16(mp.p.max_rank) * 2048, ring = XT == kXF32 ? (size_t)AHEAD * 2 * kXImage : 0;
+  mp.stages = (int)((kSmemMost - 1024 - ring) / stage);
   if (mp.stages > kMaxStages) mp.stages = kMaxStages;
-  return launch(project_kernel<XT, XP>, once, mp, mp.project_ctas, kManyThreads, mp.stages * stage + 1024, s);
+  return launch(project_kernel<XT, XP, AHEAD>, once, mp, mp.project_ctas, kManyThreads, mp.stages * stage + ring + 1024, s);
 }
 template <bool Y0B, bool YB>
 static cudaError_t launch_expand(ManyParams mp, int ctas, cudaStream_t s) {
@@ -901,9 +949,12 @@ cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, c
   ManyParams mp{p, static_cast<float4*>(scratch), images, reinterpret_cast<int*>(images + image_bytes(tiles, p.max_rank)), ctas, 0, 1,
                 take_stall(kFamDecode) ? 1 : 0, wait_limit_cycles()};
   LaunchScope scope(kFamDecode, s, 3);
-  cudaError_t e = x_type == kXF32    ? (p.y_bf16 ? launch_project<kXF32, 2>(mp, s) : launch_project<kXF32, 3>(mp, s))
-                  : x_type == kXBF16 ? launch_project<kXBF16, 1>(mp, s)
-                                     : launch_project<kXMXINT8, 1>(mp, s);
+  // fp32: three slabs on their way; two where no more fit beside two stages
+  cudaError_t e = x_type == kXF32    ? (p.y_bf16           ? launch_project<kXF32, 2, 3>(mp, s)
+                                        : p.max_rank <= 128 ? launch_project<kXF32, 3, 3>(mp, s)
+                                                            : launch_project<kXF32, 3, 2>(mp, s))
+                  : x_type == kXBF16 ? launch_project<kXBF16, 1, 6>(mp, s)
+                                     : launch_project<kXMXINT8, 1, 6>(mp, s);
   if (e != cudaSuccess) return e;
   static OncePerDevice once[2];
   const int eights = tiles * ((p.max_rank + 63) / 64) * 8;
