@@ -466,8 +466,9 @@ struct Oct {
   }
 };
 template <bool BF16>
-__device__ __forceinline__ void store_oct(const Params& p, uint8_t* to, const float (&v)[8]) {
-  if (!LQER_IN_BOUNDS(&p.plan->status, to - static_cast<uint8_t*>(p.Y), BF16 ? 16 : 32, p.y_extent, 812)) return;
+__device__ __forceinline__ void store_oct(const Params& p, size_t at, const float (&v)[8]) {
+  if (!LQER_IN_BOUNDS(&p.plan->status, at * (BF16 ? 2 : 4), BF16 ? 16 : 32, p.y_extent, 812)) return;
+  uint8_t* to = static_cast<uint8_t*>(p.Y) + at * (BF16 ? 2 : 4);
   if (BF16) {
     *reinterpret_cast<uint4*>(to) =
         make_uint4(round_bf16x2(v[0], v[1]), round_bf16x2(v[2], v[3]), round_bf16x2(v[4], v[5]), round_bf16x2(v[6], v[7]));
@@ -502,12 +503,14 @@ struct Groups {
   }
 };
 
-// STAGED: Y0 is on its way two groups (fp32: one) ahead, 128 KB a CTA, by copies into shared memory; otherwise T leaves no room there,
-// and half as much is on its way into registers.
+// STAGED: an fp32 Y0 is on its way a group ahead, 128 KB a CTA, by copies into shared memory.  Otherwise - rank beyond 64 (bf16 Y: 128), whose
+// T leaves no room, or bf16 Y0 - it comes into registers, 64 KB a CTA.  4096 rows of 5120 x 13824 rank 64, us: fp32 108 staged, 138 not, to
+// bf16 81 and 118; bf16 needs no more than 64 KB: 2048 rows of 4096 x 11008 39.5 staged, 38.5 not, rank 128 52.7 and 48.8.
 template <bool Y0B, bool YB, bool STAGED>
 __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_constant__ ManyParams mp) {
   constexpr int TP = YB ? 2 : 3;
-  constexpr int FIXED = STAGED && Y0B ? 3 : 2;          // groups of a CTA that need no drawing
+  static_assert(!STAGED || !Y0B, "fp32 Y0 only");
+  constexpr int FIXED = 2;                              // groups of a CTA that need no drawing
   extern __shared__ __align__(1024) uint8_t smem_raw[];
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
@@ -546,229 +549,165 @@ __global__ void __launch_bounds__(kManyThreads, 1) expand_kernel(const __grid_co
     // ---- accumulators and Y0 into Y: a warp has 32 rows and 32 columns of a block, a lane rows lane / 4 + 8 i and columns 8 (lane % 4) ...
     const int quarter = (warp & 3) * 32, first = (warp >> 2) * 32 + 8 * (lane & 3);
     int n = 0;                                          // turns with accumulators so far
-    if constexpr (STAGED) {
-      constexpr int A = FIXED - 1, D = 2 * A, WB = Y0B ? 2048 : 4096;      // groups ahead; blocks ahead; bytes of a warp's share of a block
-      constexpr int SENDS = Y0B ? 4 : 8, ROWS = Y0B ? 8 : 4;               // copies of a lane for a block; rows that one copy of all lanes covers
-      const uint32_t yring = tc::smem_u32(ring + (size_t)mp.stages * image) + warp * D * WB;
-      // Of a group: the lane's four rows, those that there are, and, for the copies, rows and places.  bf16: a lane sends for what it will
-      // need.  fp32: eight lanes send for the 128 bytes of a row, and pairs of rows swap their 16-byte pieces, so that the lanes that
-      // read them meet no bank twice.
-      struct Place { int row[4], col; uint32_t there; };
-      const int piece = Y0B ? lane & 3 : lane & 7, send_row = Y0B ? lane >> 2 : lane >> 3;
-      uint32_t send_to[2], get_from[2];                 // of even and odd rows
+    // Of a group: the places of the lane's first eight columns in its four rows, and which of the rows there are.
+    struct Place { size_t at[4]; int col; uint32_t there; };
+    auto place = [&](int tile, int part, Place& q) {
+      const int rows = p.tiles[tile].rows;
+      q.col = part * 256 + first;
+      q.there = 0;
 #pragma unroll
-      for (int i = 0; i < 2; ++i) {
-        send_to[i] = Y0B ? lane * 16 : (4 * i + send_row) * 128 + ((piece ^ (send_row & 1)) << 4);
-        get_from[i] = Y0B ? lane * 16 : (lane >> 2) * 128 + ((2 * (lane & 3) + i ^ (lane >> 2 & 1)) << 4);
+      for (int i = 0; i < 4; ++i) {
+        const int m = quarter + (lane >> 2) + 8 * i;
+        q.at[i] = (size_t)p.rows[(size_t)tile * kManyRows + m] * p.N + q.col;
+        if (m < rows) q.there |= 1u << i;
       }
-      auto place = [&](int tile, int part, Place& q) {
-        const int rows = p.tiles[tile].rows;
-        q.col = part * 256 + first;
-        q.there = 0;
+    };
+    // eight columns of two rows of an accumulator and of Y0, added up
+    auto put = [&](const Oct<Y0B>& y, const uint32_t (&u)[16], int k, size_t at) {
+      float o[8];
+      y.values(o);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int m = quarter + (lane >> 2) + 8 * i;
-          q.row[i] = p.rows[(size_t)tile * kManyRows + m];
-          if (m < rows) q.there |= 1u << i;
-        }
-      };
-      const uint8_t* from[SENDS];                       // of the group that is sent for
+      for (int j = 0; j < 4; ++j) {
+        o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
+        o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
+      }
+      store_oct<YB>(p, at, o);
+    };
+    // sixteen rows of an accumulator
+    auto take = [&](int rank, int buf, int h, uint32_t (&u)[16]) {
+      if (rank > 0) {
+        tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
+        tc::tmem_ld_wait();
+      } else {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) u[i] = 0u;
+      }
+    };
+    Place q;
+    Group now, then;
+    if constexpr (STAGED) {
+      // Eight lanes send for the 128 bytes of a row; pairs of rows swap their 16-byte pieces, so that the lanes that read them meet no bank twice.
+      const uint32_t here = tc::smem_u32(ring + (size_t)mp.stages * image) + warp * 8192;      // two blocks' shares of 32 rows
+      const int piece = lane & 7, send_row = lane >> 3;
+      const uint32_t to = send_row * 128 + ((piece ^ (send_row & 1)) << 4), get = (lane >> 2) * 128 + ((2 * (lane & 3) ^ (lane >> 2 & 1)) << 4);
+      const uint8_t* from[8];                           // of the group that is sent for
       uint32_t from_there = 0;
       int from_col = 0;
-      auto sources = [&](int tile, int part, const Place& q) {
-        constexpr int EB = Y0B ? 2 : 4;
-        from_col = part * 256 + (warp >> 2) * 32 + piece * (Y0B ? 8 : 4);
+      auto sources = [&](int tile, int part) {
+        const int rows = p.tiles[tile].rows;
+        from_col = part * 256 + (warp >> 2) * 32 + piece * 4;
         from_there = 0;
-        if (Y0B) {
-          from_there = q.there;
 #pragma unroll
-          for (int j = 0; j < 4; ++j) from[j] = static_cast<const uint8_t*>(p.Y0) + ((size_t)q.row[j] * p.N + from_col) * EB;
-        } else {
-          const int rows = p.tiles[tile].rows;
-#pragma unroll
-          for (int j = 0; j < SENDS; ++j) {
-            const int m = quarter + ROWS * j + send_row;
-            from[j] = static_cast<const uint8_t*>(p.Y0) + ((size_t)p.rows[(size_t)tile * kManyRows + m] * p.N + from_col) * EB;
-            if (m < rows) from_there |= 1u << j;
-          }
+        for (int j = 0; j < 8; ++j) {
+          const int m = quarter + 4 * j + send_row;
+          from[j] = static_cast<const uint8_t*>(p.Y0) + ((size_t)p.rows[(size_t)tile * kManyRows + m] * p.N + from_col) * 4;
+          if (m < rows) from_there |= 1u << j;
         }
       };
-      auto send = [&](int slot, int turn, bool any) {
+      auto send = [&](int turn, bool any) {
         const uint32_t there = any && from_col + turn * 128 < p.N ? from_there : 0u;
 #pragma unroll
-        for (int j = 0; j < SENDS; ++j)
-          if (there & 1u << j)
-            cp_async16(yring + slot * WB + (Y0B ? j * 512 + send_to[0] : (j >> 1) * 1024 + send_to[j & 1]), from[j] + turn * (Y0B ? 256 : 512));
+        for (int j = 0; j < 8; ++j)
+          if (there & 1u << j) cp_async16(here + turn * 4096 + j * 512 + to, from[j] + turn * 512);
         cp_async_commit();
       };
-      Place q[A + 1];
-      int rank[A + 1], g[A + 1];
-#pragma unroll
-      for (int a = 0; a < A; ++a) {
-        g[a] = g0 + a * g_step;
-        if (g[a] < groups) {
-          place(g[a] / NG, g[a] % NG, q[a]);
-          sources(g[a] / NG, g[a] % NG, q[a]);
-        }
-        send(2 * a, 0, g[a] < groups);
-        send(2 * a + 1, 1, g[a] < groups);
-      }
-#pragma unroll
-      for (int a = 0; a < A; ++a)
-        if (a == 0 || (g[a - 1] >= 0 && g[a - 1] < groups)) {
-          const Group next = mine.next<true>(&ws);
-          g[a] = next.g;
-          rank[a] = next.rank;
-        }
-      int slot = 0;
-      while (g[0] >= 0 && g[0] < groups && ok) {
-        Group next{groups, 0, 0, 0};
-        if (g[A - 1] >= 0 && g[A - 1] < groups) next = mine.next<true>(&ws);
-        if (next.g < 0) break;
-        g[A] = next.g;
-        rank[A] = next.rank;
-        const bool more = next.g < groups;
-        if (more) place(next.tile, next.part, q[A]);
-        uint8_t* to[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) to[i] = static_cast<uint8_t*>(p.Y) + ((size_t)q[0].row[i] * p.N + q[0].col) * (YB ? 2 : 4);
+      if (g0 < groups) sources(g0 / NG, g0 % NG);
+      send(0, g0 < groups);
+      send(1, g0 < groups);
+      now = mine.next<true>(&ws);
+      while (now.g >= 0 && now.g < groups && ok) {
+        then = mine.next<true>(&ws);
+        if (then.g < 0) break;
+        const bool more = then.g < groups;
+        place(now.tile, now.part, q);
 #pragma unroll
         for (int turn = 0; turn < 2; ++turn) {
           if (!ok) break;
           const int buf = n & 1;
-          if (rank[0] > 0) {
+          if (now.rank > 0) {
             ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
             ++n;
             tc::tc_fence_after();
           }
-          cp_async_wait<D - 1>();
+          cp_async_wait<1>();
           __syncwarp();
           if (!ok) break;
-          const uint32_t there = q[0].col + turn * 128 < p.N ? q[0].there : 0u, here = yring + slot * WB;
+          const uint32_t there = q.col + turn * 128 < p.N ? q.there : 0u;
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {                 // sixteen rows
+          for (int h = 0; h < 2; ++h) {
             uint32_t u[16];
-            if (rank[0] > 0) {
-              tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
-              tc::tmem_ld_wait();
-            } else {
-#pragma unroll
-              for (int i = 0; i < 16; ++i) u[i] = 0u;
-            }
+            take(now.rank, buf, h, u);
 #pragma unroll
             for (int k = 0; k < 2; ++k) {
               const int i = 2 * h + k;
+              const uint32_t src = here + turn * 4096 + i * 1024 + get;
               Oct<Y0B> y;
-              y.a = lds16(here + i * WB / 4 + get_from[0]);
-              if (!Y0B) y.b = lds16(here + i * WB / 4 + get_from[1]);
-              float o[8];
-              y.values(o);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
-                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
-              }
-              if (there & 1u << i) store_oct<YB>(p, to[i] + turn * (YB ? 256 : 512), o);
+              y.a = lds16(src);
+              y.b = lds16(src ^ 16);
+              if (there & 1u << i) put(y, u, k, q.at[i] + turn * 128);
             }
           }
-          if (rank[0] > 0) tc::tc_fence_before();
+          if (now.rank > 0) tc::tc_fence_before();
           __syncwarp();
-          if (rank[0] > 0 && lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
-          if (turn == 0 && more) sources(next.tile, next.part, q[A]);
-          send(slot, turn, more);
-          slot = slot + 1 == D ? 0 : slot + 1;
+          if (now.rank > 0 && lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
+          if (turn == 0 && more) sources(then.tile, then.part);
+          send(turn, more);
         }
-#pragma unroll
-        for (int a = 0; a < A; ++a) {
-          g[a] = g[a + 1];
-          rank[a] = rank[a + 1];
-          q[a] = q[a + 1];
-        }
+        now = then;
       }
       cp_async_wait<0>();
     } else {
-      constexpr int AHEAD = Y0B ? 2 : 1;                  // blocks of 128 columns whose Y0 is on its way
-      int row[4] = {-1, -1, -1, -1}, coming[4];           // this lane's rows of the group at hand and of the next one
+      constexpr int AHEAD = Y0B ? 2 : 1;                // blocks of 128 columns whose Y0 is on its way
+      Place next;
       Oct<Y0B> y[AHEAD][4];
-      int ahead = -1;                                     // tile of the next group
-      auto enter = [&](int t) {                           // the rows of a group's tile
-        if (t == ahead) return;
-        ahead = t;
-        const int rows = p.tiles[t].rows;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int m = quarter + (lane >> 2) + 8 * i;
-          coming[i] = p.rows[(size_t)t * kManyRows + m];
-          if (m >= rows) coming[i] = -1;
-        }
-      };
       if (g0 < groups) {
-        enter(g0 / NG);
+        place(g0 / NG, g0 % NG, next);
 #pragma unroll
-        for (int a = 0; a < AHEAD; ++a) {
-          const int col = g0 % NG * 256 + a * 128 + first;
+        for (int a = 0; a < AHEAD; ++a)
 #pragma unroll
           for (int i = 0; i < 4; ++i)
-            if (coming[i] >= 0 && col < p.N) y[a][i].load(p, (size_t)coming[i] * p.N + col);
-        }
+            if (next.there & 1u << i && next.col + a * 128 < p.N) y[a][i].load(p, next.at[i] + a * 128);
       }
-      Group at_hand = mine.next<true>(&ws);
-      while (at_hand.g >= 0 && at_hand.g < groups && ok) {
-        const int rank = at_hand.rank;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) row[i] = coming[i];
-        const Group then = mine.next<true>(&ws);
+      now = mine.next<true>(&ws);
+      while (now.g >= 0 && now.g < groups && ok) {
+        q = next;
+        then = mine.next<true>(&ws);
         const bool more = then.g >= 0 && then.g < groups;
-        if (more) enter(then.tile);
+        if (more) place(then.tile, then.part, next);
 #pragma unroll
         for (int turn = 0; turn < 2; ++turn) {
           if (!ok) break;
-          const int buf = n & 1, col = at_hand.part * 256 + turn * 128 + first;
-          if (rank > 0) {
+          const int buf = n & 1;
+          if (now.rank > 0) {
             ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.acc_full[buf]), (n >> 1) & 1, &ws)) != 0;
             ++n;
             tc::tc_fence_after();
           }
           if (!ok) break;
-          Oct<Y0B>(&now)[4] = y[AHEAD == 2 ? turn : 0];
+          const uint32_t there = q.col + turn * 128 < p.N ? q.there : 0u;
           // what comes into the same registers: this group's second block, or the next group's
           const bool own = AHEAD == 1 && turn == 0;
-          const int next_col = own ? col + 128 : more ? then.part * 256 + (AHEAD == 2 ? turn * 128 : 0) + first : p.N;
+          const int next_at = AHEAD == 2 || own ? turn * 128 + (own ? 128 : 0) : 0;
+          const uint32_t coming = own ? (q.col + 128 < p.N ? q.there : 0u) : more && next.col + next_at < p.N ? next.there : 0u;
+          Oct<Y0B>(&yt)[4] = y[AHEAD == 2 ? turn : 0];
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {                   // sixteen rows
+          for (int h = 0; h < 2; ++h) {
             uint32_t u[16];
-            if (rank > 0) {
-              tmem_ld_16x32(tmem + ((uint32_t)(quarter + 16 * h) << 16) + buf * 128 + (warp >> 2) * 32, u);
-              tc::tmem_ld_wait();
-            } else {
+            take(now.rank, buf, h, u);
 #pragma unroll
-              for (int i = 0; i < 16; ++i) u[i] = 0u;
-            }
+            for (int i = 2 * h; i < 2 * h + 2; ++i)
+              if (there & 1u << i) put(yt[i], u, i & 1, q.at[i] + turn * 128);
 #pragma unroll
-            for (int k = 0; k < 2; ++k) {
-              const int i = 2 * h + k;
-              float o[8];
-              now[i].values(o);
-#pragma unroll
-              for (int j = 0; j < 4; ++j) {
-                o[2 * j] += __uint_as_float(u[4 * j + 2 * k]);
-                o[2 * j + 1] += __uint_as_float(u[4 * j + 2 * k + 1]);
-              }
-              if (row[i] >= 0 && col < p.N) store_oct<YB>(p, static_cast<uint8_t*>(p.Y) + ((size_t)row[i] * p.N + col) * (YB ? 2 : 4), o);
-            }
-#pragma unroll
-            for (int i = 2 * h; i < 2 * h + 2; ++i) {
-              const int r = own ? row[i] : coming[i];
-              if (r >= 0 && next_col < p.N) now[i].load(p, (size_t)r * p.N + next_col);
-            }
+            for (int i = 2 * h; i < 2 * h + 2; ++i)
+              if (coming & 1u << i) yt[i].load(p, (own ? q.at[i] : next.at[i]) + next_at);
           }
-          if (rank > 0) {
+          if (now.rank > 0) {
             tc::tc_fence_before();
             __syncwarp();
             if (lane == 0) tc::mbar_arrive(bar_of(bars.acc_empty[buf]));
           }
         }
-        at_hand = then;
+        now = then;
       }
     }
   } else if (warp == kCopyWarp) {
@@ -933,15 +872,16 @@ template <bool Y0B, bool YB>
 static cudaError_t launch_expand(ManyParams mp, int ctas, cudaStream_t s) {
   static OncePerDevice once[2];
   const size_t t = (size_t)(YB ? 2 : 3) * ((mp.p.max_rank + 63) / 64) * kXImage, image = (size_t)128 * b_pitch(mp.p.max_rank);
-  const size_t staged = 128 * 1024, most = kSmemMost - 1024;
-  const bool fits = t + 2 * image + staged <= most;
-  const size_t room = fits ? most - staged : most;
+  const size_t ring = 128 * 1024, most = kSmemMost - 1024;
+  const bool staged = !Y0B && t + 2 * image + ring <= most;
+  const size_t room = staged ? most - ring : most;
   mp.t_sets = 2 * t + 2 * image <= room ? 2 : 1;
   mp.stages = (int)((room - mp.t_sets * t) / image);
   if (mp.stages > kMaxStages) mp.stages = kMaxStages;
-  const size_t smem = mp.t_sets * t + mp.stages * image + (fits ? staged : 0) + 1024;
-  return fits ? launch(expand_kernel<Y0B, YB, true>, once[0], mp, ctas, kManyThreads, smem, s)
-              : launch(expand_kernel<Y0B, YB, false>, once[1], mp, ctas, kManyThreads, smem, s);
+  const size_t smem = mp.t_sets * t + mp.stages * image + (staged ? ring : 0) + 1024;
+  if constexpr (!Y0B)
+    if (staged) return launch(expand_kernel<false, YB, true>, once[0], mp, ctas, kManyThreads, smem, s);
+  return launch(expand_kernel<Y0B, YB, false>, once[1], mp, ctas, kManyThreads, smem, s);
 }
 cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, cudaStream_t s) {
   const int sms = sm_count(), ctas = sms < kPrologueMaxCtas ? sms : kPrologueMaxCtas;
