@@ -234,9 +234,10 @@ inline size_t slot_bytes(int K, int N, int max_rank) {
   return (256 + a_bytes(K, max_rank) + b_bytes(N, max_rank, b_pitch(max_rank)) + 255) & ~(size_t)255;
 }
 // A plan holds the rows in tiles of 8 for up to kFewMost of them, and in tiles of 128 for more than kManyLeast: in between the call
-// chooses.  Both measured, few / many, us: 1024 rows of 1264 x 1968 rank 32 bf16 10.2 / 16.7, of 4096 x 4096 rank 16 15.9 / 19.9, of
-// 5120 x 5120 rank 32 21 / 25, rank 128 43 / 31, of 4096 x 11008 rank 64 44 / 31; 513 rows of the last 24 / 26, of 5120 x 5120 rank
-// 128 25 / 28; 1536 rows of 4096 x 4096 rank 16 27 / 24.
+// chooses, by its work.  Both measured in bf16, few / many, us.  1024 rows: of 1264 x 1968 rank 32 9.6 / 14.7, of 4096 x 4096 rank 16
+// 15.9 / 19.5, of 5120 x 5120 rank 32 21.2 / 22.3 (fp32: 29 / 34), of 4096 x 4096 rank 64 22.7 / 21.7, of 5120 x 5120 rank 128 43 / 29, of
+// 4096 x 11008 rank 64 44 / 29.  513 rows: of 4096 x 4096 rank 64 14.3 / 18.5, of 4096 x 11008 rank 64 24.3 / 22.7, of 5120 x 5120 rank 128
+// 24.9 / 22.5.
 constexpr int kFewMost = 1024, kManyLeast = 512;
 constexpr long long kFewWork = 350LL * 1000 * 1000;
 inline bool takes_few(int M, int K, int N, int max_rank) {

@@ -6,14 +6,18 @@
 // the accumulators - one for each part, so that the small ones are not cut off against the large - stay in tensor memory.
 // finish_kernel: T from its partial sums, scaled, in bf16 parts, in the swizzled images that the next kernel copies.
 // expand_kernel: Y = Y0 + T B_a.  T is the 128-row operand, copied once a tile, as B's images are; each block of 128 columns is one
-// accumulator, and two of them take turns, so that the tensor cores work ahead of the sixteen warps that add Y0, which is on its
-// way from memory a block ahead (bf16: two).
+// accumulator, and two of them take turns, so that the tensor cores work ahead of the sixteen warps that add Y0, of which two blocks
+// are on their way from memory (64 KB a CTA in bf16, 128 KB in fp32).
 //
 // They are bound by memory: X is read once, Y0 read and Y written once; A and B come from L2 after a tile's first use.  The tiles'
 // number is known on the device only.  The projection's work (tile by tile, its slabs of K in turn) is cut into equal stretches, one
 // for each CTA of a grid as large as the device; a stretch ends where it ends, in the middle of a tile if need be: it leaves its
 // partial sums of T in place (tile + CTA) of the scratch, which no other stretch has, and finish_kernel adds up a tile's
 // stretches in order.  The expansion's CTAs draw groups of columns from a counter.
+//
+// Measured, all three: 4096 rows of 5120 x 13824 rank 64 in fp32 108 us, 5.0 TB/s: 28 us project, of which 13 would do for X's bytes (the
+// rest goes into the instructions that cut fp32 into three parts), 4 finish, 72 expand at 6.3 TB/s, 4 in between.  2048 rows of
+// 4096 x 11008 rank 64 in bf16 38 us: the bytes would take 17, but about 15 us pass before the first Y can be written.
 #include "lqer_adapters.cuh"
 
 namespace lqer {
@@ -37,7 +41,7 @@ __host__ __device__ inline size_t partial_floats(int max_rank) { return (size_t)
 // The projection's work, KS slabs of each of `tiles` tiles, cut into stretches for up to `most` CTAs.  Either every tile is cut alike
 // (`parts` CTAs, `each` slabs a stretch), or the whole of it is (parts == 0), with stretches that may reach into the next tile.  To
 // change tiles costs a CTA about as much as four slabs, so tiles are cut alike where that makes the longest stretch no more than four
-// slabs longer (2048 rows of 4096 bf16 columns in 17 tiles, 8 against 7.4 slabs: 11.6 -> 9.2 us).
+// slabs longer (2048 rows of 4096 x 11008 rank 64 in bf16, the whole call: 40.6 -> 39.6 us).
 struct Cut {
   unsigned KS, each, rest;              // tiles * KS stays below 2^32: no more than 2^24 rows in 2^17 + 1025 tiles, and 2^20 columns
   int ctas, parts;                      // ctas: those that have work; parts == 0: units = each * ctas + rest
@@ -481,9 +485,9 @@ __device__ __forceinline__ void store_oct(const Params& p, size_t at, const floa
 }
 
 // The groups - 256 columns of a tile - are taken in order, each by the next CTA that is free: some SMs get at memory faster than others,
-// and CTAs that work side by side on neighbouring columns are kind to the memory's pages (4096 rows of 13824 fp32 columns: 88 us, against
-// 112 where every CTA had a stretch of its own).  The copying warp draws them, from a counter in the scratch; whose work a group
-// is changes nothing in the results.  What the other warps see of it:
+// and CTAs that work side by side on neighbouring columns are kind to the memory's pages (4096 rows of 5120 x 13824 rank 64 in fp32, the
+// whole call: 108 us; 112 with every 148th group for a CTA, 114 with a stretch of its own for each).  The copying warp draws them, from
+// a counter in the scratch; whose work a group is changes nothing in the results.  What the other warps see of it:
 struct Group { int g, rank, tile, part; };       // part: which 256 columns of the tile
 struct Groups {
   uint32_t list;             // four places in shared memory
