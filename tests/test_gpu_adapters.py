@@ -276,6 +276,26 @@ def test_many_rows_in_place_and_the_same_again(y):
     assert X.data_ptr() % 32 == 16 and torch.equal(L.apply_adapters(X, c.pool, c.plan, Y0, Y=Z), Y)
 
 
+@pytest.mark.parametrize("x,y0,y", [("f32", "f32", "f32"), ("bf16", "bf16", "bf16"), ("mxint8", "f32", "bf16"), ("bf16", "bf16", "f32")])
+@pytest.mark.parametrize("M,K,N,ranks", [(1500, 272, 11016, [64, 0, 20]), (1500, 272, 11016, [128, 0, 20]), (1100, 48, 20488, [8, 256])])
+def test_many_columns(M, K, N, ranks, x, y0, y):
+    # many groups of columns to a CTA, the first two of them neighbours; an empty slot, rows without adapter
+    c = Case(M, K, N, ranks, [(j // 37) % (len(ranks) + 1) - 1 for j in range(M)], x=x, y0=y0, y=y)
+    Y = c.run()
+    assert L.poll_status(c.plan.buf) == 0
+    c.check(Y)
+
+
+@pytest.mark.parametrize("x", ["f32", "bf16", "mxint8"])
+@pytest.mark.parametrize("M,K,N,rank", [(4500, 10256, 264, 24), (12700, 2064, 136, 16), (2100, 16400, 72, 256)])
+def test_long_projections(M, K, N, rank, x):
+    # stretches of more slabs than an accumulator takes at a time, and stretches that end in the middle of a tile
+    c = Case(M, K, N, [rank, 8], [(j // 300) % 3 - 1 for j in range(M)], x=x, y0="f32", y="f32")
+    Y = c.run()
+    assert L.poll_status(c.plan.buf) == 0
+    c.check(Y)
+
+
 def test_many_rows_without_any_adapter():
     c = _many(2)
     c.slots.fill_(-1)
