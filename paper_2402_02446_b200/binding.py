@@ -438,6 +438,17 @@ def _here(index: int) -> bool:
     return index == torch._C._cuda_getDevice()
 
 
+def _on(stream, index: int):
+    """Where a call's launches, and the tensors that it makes, belong: a given stream, or the device's current one."""
+    if stream is None:
+        return torch.cuda.device(index)
+    if index < 0:
+        raise ValueError("expected CUDA tensors")
+    if stream.device.index != index:
+        raise ValueError("the stream belongs to another device than the tensors")
+    return torch.cuda.stream(stream)
+
+
 def _ptr(t: torch.Tensor, index: int) -> int:
     """The address of a dense tensor on that device."""
     if t.get_device() != index or not t.is_contiguous():
@@ -445,12 +456,8 @@ def _ptr(t: torch.Tensor, index: int) -> int:
     return t.data_ptr()
 
 
-def _raw_stream(stream, index: int) -> int:
-    if stream is None:
-        return torch._C._cuda_getCurrentRawStream(index)
-    if stream.device.index != index:
-        raise ValueError("the stream belongs to another device than the tensors")
-    return stream.cuda_stream
+def _raw_stream(index: int) -> int:
+    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _code(codes, dt) -> int:
@@ -483,9 +490,9 @@ def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: to
     is only written where residual_out is given (None is returned otherwise); with one it goes to residual_out (which may be
     the residual itself) or to a new tensor."""
     index = X.get_device()
-    if not _here(index):
-        with torch.cuda.device(index):
-            return add_rms_norm(X, weight, eps, residual, out_dtype, cfg, residual_out, Y, stream)
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return add_rms_norm(X, weight, eps, residual, out_dtype, cfg, residual_out, Y)
     shape = X.shape
     if len(shape) != 2 or weight.shape != shape[1:]:
         raise ValueError("expected X [M, K] and weight [K]")
@@ -504,7 +511,7 @@ def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: to
         h_ptr, r_code = _ptr(residual_out, index), _code(_REAL_CODE, residual_out.dtype)
     Y, y_code, y_ptr = _output(Y, M, K, out_dtype, X, index)
     status = lib().lqer_add_rms_norm(_ptr(X, index), x_code, r_ptr, h_ptr, r_code, _ptr(weight, index), _code(_REAL_CODE, weight.dtype), eps, M, K,
-                                     None if cfg is None else C.byref(cfg), y_ptr, y_code, _raw_stream(stream, index))
+                                     None if cfg is None else C.byref(cfg), y_ptr, y_code, _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_add_rms_norm")
     return Y, residual_out
@@ -515,9 +522,9 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", ou
     """act(gate) * up ("silu", or "gelu" in its tanh form), fp32, bf16 or MXINT8.  gate and up [M, N]: dense, or views with one row
     stride, as the halves of one [M, 2 N] tensor are."""
     index = gate.get_device()
-    if not _here(index):
-        with torch.cuda.device(index):
-            return gated_activation(gate, up, act, out_dtype, cfg, Y, stream)
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return gated_activation(gate, up, act, out_dtype, cfg, Y)
     shape = gate.shape
     if len(shape) != 2 or up.shape != shape or up.dtype != gate.dtype or up.get_device() != index:
         raise ValueError("expected gate and up of one shape [M, N], type and device")
@@ -529,7 +536,7 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", ou
         raise ValueError(f"unknown activation {act!r}")
     Y, y_code, y_ptr = _output(Y, M, N, out_dtype, gate, index)
     status = lib().lqer_gated_activation(gate.data_ptr(), up.data_ptr(), _code(_REAL_CODE, gate.dtype), ld if M > 1 else N, M, N, _ACTS[act],
-                                         None if cfg is None else C.byref(cfg), y_ptr, y_code, _raw_stream(stream, index))
+                                         None if cfg is None else C.byref(cfg), y_ptr, y_code, _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_gated_activation")
     return Y
@@ -539,14 +546,14 @@ def dequantize_activations(Xq: torch.Tensor, M: int, K: int, out_dtype=torch.flo
                            Y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """The values of a flat MXINT8 buffer of [M, K] activations (exact in fp32 and in bf16)."""
     index = Xq.get_device()
-    if not _here(index):
-        with torch.cuda.device(index):
-            return dequantize_activations(Xq, M, K, out_dtype, cfg, Y, stream)
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return dequantize_activations(Xq, M, K, out_dtype, cfg, Y)
     if Xq.dtype != torch.uint8 or K % 16 or Xq.numel() != mxint8_bytes(M, K):
         raise ValueError("an MXINT8 tensor is a flat uint8 tensor of mxint8_bytes(M, K)")
     Y, y_code, y_ptr = _output(Y, M, K, out_dtype, Xq, index)
-    status = lib().lqer_dequantize_activations(_ptr(Xq, index), M, K, None if cfg is None else C.byref(cfg), _ptr(Y, index), y_code,
-                                               _raw_stream(stream, index))
+    status = lib().lqer_dequantize_activations(_ptr(Xq, index), M, K, None if cfg is None else C.byref(cfg), y_ptr, y_code,
+                                               _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_dequantize_activations")
     return Y
@@ -567,9 +574,13 @@ class AdapterPool:
 
 
 def new_adapter_pool(K: int, N: int, max_rank: int, n_slots: int, device="cuda", stream=None) -> AdapterPool:
+    if stream is not None:
+        device = torch.device(device)
+        with _on(stream, stream.device.index if device.index is None else device.index):
+            return new_adapter_pool(K, N, max_rank, n_slots, stream.device)
     pool = AdapterPool(K, N, max_rank, n_slots, device)
-    with torch.cuda.device(pool.buf.device):
-        _check(lib().lqer_adapter_pool_init(pool.ref, pool.buf.numel(), _raw_stream(stream, pool.buf.get_device())), "lqer_adapter_pool_init")
+    with torch.cuda.device(pool.index):
+        _check(lib().lqer_adapter_pool_init(pool.ref, pool.buf.numel(), _raw_stream(pool.index)), "lqer_adapter_pool_init")
     return pool
 
 
@@ -579,17 +590,17 @@ def load_adapter(pool: AdapterPool, slot: int, A: torch.Tensor, B: torch.Tensor,
         raise ValueError("expected A [K, rank] and B [rank, N] of one type")
     if A.shape[1] < 1:
         raise ValueError("an adapter has a rank of at least 1 (unload_adapter empties a slot)")
-    index = pool.buf.get_device()
-    with torch.cuda.device(index):
+    index = pool.index
+    with _on(stream, index):
         _check(lib().lqer_adapter_load(pool.ref, slot, _ptr(A, index), _ptr(B, index), _code(_REAL_CODE, A.dtype), A.shape[1], scale,
-                                       _raw_stream(stream, index)), "lqer_adapter_load")
+                                       _raw_stream(index)), "lqer_adapter_load")
 
 
 def unload_adapter(pool: AdapterPool, slot: int, stream=None) -> None:
     """Empties a slot: rows that name it take no adapter."""
-    index = pool.buf.get_device()
-    with torch.cuda.device(index):
-        _check(lib().lqer_adapter_load(pool.ref, slot, None, None, 0, 0, 0.0, _raw_stream(stream, index)), "lqer_adapter_load")
+    index = pool.index
+    with _on(stream, index):
+        _check(lib().lqer_adapter_load(pool.ref, slot, None, None, 0, 0, 0.0, _raw_stream(index)), "lqer_adapter_load")
 
 
 @dataclass
@@ -606,9 +617,9 @@ def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | Non
     """The plan of a batch: slots int32 [M], the slot of each row's adapter in the pools of this step (-1: none).  It serves every pool
     with as many slots.  `plan`: one of the same sizes to be made again in place."""
     index = slots.get_device()
-    if not _here(index):
-        with torch.cuda.device(index):
-            return adapter_plan(slots, pool, plan, stream)
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return adapter_plan(slots, pool, plan)
     if slots.dtype != torch.int32 or slots.dim() != 1:
         raise ValueError("expected int32 slots [M]")
     M = slots.shape[0]
@@ -620,7 +631,7 @@ def adapter_plan(slots: torch.Tensor, pool: AdapterPool, plan: AdapterPlan | Non
         raise ValueError("the plan to be made again has other sizes")
     if plan.index != index:
         raise ValueError("expected the plan on the device of the slots")
-    _check(lib().lqer_adapter_plan(_ptr(slots, index), M, pool.n_slots, plan.ptr, plan.buf.numel(), _raw_stream(stream, index)), "lqer_adapter_plan")
+    _check(lib().lqer_adapter_plan(_ptr(slots, index), M, pool.n_slots, plan.ptr, plan.buf.numel(), _raw_stream(index)), "lqer_adapter_plan")
     return plan
 
 
@@ -637,9 +648,9 @@ def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: to
     bf16, the shared projection's output; Y of out_dtype (Y0's type where it is not given), or the given tensor, Y0 itself included.
     ws: a workspace of adapters_workspace_bytes (more than 512 rows may need one; made where none is given)."""
     index = X.get_device()
-    if not _here(index):
-        with torch.cuda.device(index):
-            return apply_adapters(X, pool, plan, Y0, Y, out_dtype, cfg, ws, stream)
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return apply_adapters(X, pool, plan, Y0, Y, out_dtype, cfg, ws)
     M, K, N = plan.M, pool.K, pool.N
     x_code = _code(_OUT_CODE, X.dtype)
     if X.shape != ((mxint8_bytes(M, K),) if x_code == 2 else (M, K)) or Y0.shape != (M, N):
@@ -658,7 +669,7 @@ def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: to
         ws = X.new_empty(adapters_workspace_bytes(M, pool, plan.n_slots), dtype=torch.uint8)
     status = lib().lqer_adapters(_ptr(X, index), x_code, M, pool.ref, plan.ptr, plan.n_slots, y0_ptr, _code(_REAL_CODE, Y0.dtype),
                                  y_ptr, _code(_REAL_CODE, Y.dtype), None if cfg is None else C.byref(cfg),
-                                 None if ws is None else _ptr(ws, index), 0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(stream, index))
+                                 None if ws is None else _ptr(ws, index), 0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_adapters")
     return Y

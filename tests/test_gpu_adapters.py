@@ -355,6 +355,25 @@ def test_many_rows_streams_and_graphs():
         assert torch.equal(have, want)
 
 
+def test_a_given_stream_owns_what_the_calls_make():
+    # workspace and outputs come from the stream that is given: what the current one makes meanwhile lies elsewhere
+    c = _many(8, "f32")
+    Y = c.run()
+    s = torch.cuda.Stream()
+    for _ in range(3):
+        torch.cuda.synchronize()
+        with torch.cuda.stream(s):
+            torch.cuda._sleep(2_000_000)
+        pool = L.new_adapter_pool(1040, 1064, 64, 4, stream=s)
+        plan = L.adapter_plan(c.slots, c.pool, stream=s)
+        Z = L.apply_adapters(c.X, c.pool, plan, c.Y0, stream=s)
+        W = L.apply_adapters(c.X, pool, plan, c.Y0, stream=s)
+        waste = [torch.full((n,), 255, dtype=torch.uint8, device=DEV) for n in (L.adapters_workspace_bytes(c.M, c.pool), plan.buf.numel(), Y.numel() * 4)]
+        s.synchronize()
+        assert torch.equal(Z, Y) and torch.equal(W, c.Y0) and L.poll_status(plan.buf) == 0
+        del waste
+
+
 def test_many_rows_behind_the_kernel_that_makes_their_input():
     # the kernels overlap their neighbours on the stream: inputs made, used, and made anew without a pause
     c = _many(6, "f32")
