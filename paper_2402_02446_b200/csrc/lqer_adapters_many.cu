@@ -15,7 +15,7 @@
 // partial sums of T in place (tile + CTA) of the scratch, which no other stretch has, and finish_kernel adds up a tile's
 // stretches in order.  The expansion's CTAs draw groups of columns from a counter.
 //
-// Measured, all three: 4096 rows of 5120 x 13824 rank 64 in fp32 108 us, 5.0 TB/s: 28 us project, of which 13 would do for X's bytes (the
+// Measured, all three: 4096 rows of 5120 x 13824 rank 64 in fp32 106 us, 5.1 TB/s: 28 us project, of which 13 would do for X's bytes (the
 // rest goes into the instructions that cut fp32 into three parts), 4 finish, 72 expand at 6.3 TB/s, 4 in between.  2048 rows of
 // 4096 x 11008 rank 64 in bf16 38 us: the bytes would take 17, but about 15 us pass before the first Y can be written.
 #include "lqer_adapters.cuh"
@@ -400,52 +400,64 @@ __global__ void __launch_bounds__(kManyThreads, 1) project_kernel(const __grid_c
 }
 
 // ---------------------------------------------------------------------------- T from its partial sums
-// A CTA takes eight ranks of a tile, a thread four of one of its rows.
+// An item is sixteen ranks of a tile, a thread's share eight of one row: half as many CTAs as with four, each with twice the loads on
+// their way (4096 rows of 5120 x 13824 rank 64 in fp32, the whole call: 108.1 -> 105.8 us).  No more CTAs than SMs.
 template <int TP>
 __global__ void __launch_bounds__(256) finish_kernel(const __grid_constant__ ManyParams mp) {
   const Params& p = mp.p;
   // plan and pool were there before project_kernel (see expand_kernel); its partial sums have to be waited for
-  const int slabs = (p.max_rank + 63) / 64, tile = blockIdx.x / (slabs * 8), e = blockIdx.x % (slabs * 8), m = threadIdx.x & 127, h = threadIdx.x >> 7;
+  const int slabs = (p.max_rank + 63) / 64, m = threadIdx.x & 127, h = threadIdx.x >> 7;
   const ListHead head = load_head(p.plan, 1);
-  const int slot = p.tiles[tile].slot;                  // (the list is as long as the grid asks, whatever it holds)
-  int rank = 0;
-  SlotHead hd;
-  if (plan_fits(p, head) && tile < head.n_adapted) {
-    hd = load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes);
-    rank = rank_of(p, slot, hd, threadIdx.x == 0 && e == 0);
-  }
-  const int first = e * 8 + h * 4;
-  const bool here = e * 8 < (rank + 63) / 64 * 64, filled = here && first < rank;
-  const Cut cut(filled ? head.n_adapted : 0, (p.K + 63) / 64, mp.project_ctas);
-  int count;
-  const int from = cut.first_of(tile, count);
+  const int tiles = plan_fits(p, head) ? head.n_adapted : 0;
+  const Cut cut(tiles, (p.K + 63) / 64, mp.project_ctas);
   const size_t per = partial_floats(p.max_rank) / 4;
-  const float4* src = mp.scratch + (size_t)(tile + from) * per + (e * 2 + h) * 128 + m;
-  tc::pdl_wait();
-  tc::pdl_launch_dependents();                          // not before: expand_kernel's CTAs would take the places of this kernel's last ones
-  if (blockIdx.x == 0 && threadIdx.x == 0) *mp.drawn = 0;
-  if (!here) return;
-  float v[4] = {0.f, 0.f, 0.f, 0.f};
-  constexpr int TOGETHER = 12;                          // stretches whose sums are on their way together
-  for (int k0 = 0; k0 < count; k0 += TOGETHER) {
-    float4 u[TOGETHER];
+  bool waited = false;
+  auto wait = [&] {
+    if (waited) return;
+    waited = true;
+    tc::pdl_wait();
+    tc::pdl_launch_dependents();                        // not before: expand_kernel's CTAs would take the places of this kernel's last ones
+    if (blockIdx.x == 0 && threadIdx.x == 0) *mp.drawn = 0;
+  };
+  for (int item = blockIdx.x; item < tiles * slabs * 4; item += gridDim.x) {
+    const int tile = item / (slabs * 4), e = item % (slabs * 4), first = e * 16 + h * 8;
+    const int slot = p.tiles[tile].slot;
+    const SlotHead hd = load_slot(p.pool + (size_t)max(slot, 0) * p.slot_bytes);
+    const int rank = rank_of(p, slot, hd, threadIdx.x == 0 && e == 0);
+    int count;
+    const float4* src = mp.scratch + (size_t)(tile + cut.first_of(tile, count)) * per + (e * 4 + h * 2) * 128 + m;
+    if (first >= rank) count = 0;
+    wait();
+    if (e * 16 >= (rank + 63) / 64 * 64) continue;
+    float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+    constexpr int TOGETHER = 6;                         // stretches whose sums are on their way together
+    for (int k0 = 0; k0 < count; k0 += TOGETHER) {
+      float4 u[TOGETHER][2];
 #pragma unroll
-    for (int k = 0; k < TOGETHER; ++k) {
-      u[k] = make_float4(0.f, 0.f, 0.f, 0.f);
-      if (k0 + k < count) u[k] = src[(k0 + k) * per];
+      for (int k = 0; k < TOGETHER; ++k) {
+        u[k][0] = u[k][1] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (k0 + k < count) {
+          u[k][0] = src[(k0 + k) * per];
+          u[k][1] = src[(k0 + k) * per + 128];
+        }
+      }
+#pragma unroll
+      for (int k = 0; k < TOGETHER; ++k) {
+        v[0] += u[k][0].x; v[1] += u[k][0].y; v[2] += u[k][0].z; v[3] += u[k][0].w;
+        v[4] += u[k][1].x; v[5] += u[k][1].y; v[6] += u[k][1].z; v[7] += u[k][1].w;
+      }
     }
+    // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
 #pragma unroll
-    for (int k = 0; k < TOGETHER; ++k) { v[0] += u[k].x; v[1] += u[k].y; v[2] += u[k].z; v[3] += u[k].w; }
+    for (int i = 0; i < 8; ++i) v[i] = first + i < rank ? v[i] * hd.scale : 0.f;
+    uint32_t w[4][TP];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) split<TP>(v[2 * i], v[2 * i + 1], w[i]);
+    uint8_t* img = mp.images + ((size_t)tile * TP * slabs + (e >> 2)) * kXImage + swizzled(m, (e & 3) * 2 + h, 128);
+#pragma unroll
+    for (int k = 0; k < TP; ++k) *reinterpret_cast<uint4*>(img + (size_t)k * slabs * kXImage) = make_uint4(w[0][k], w[1][k], w[2][k], w[3][k]);
   }
-  // beyond the rank the packed A holds zeros, and an infinite activation times zero is no zero
-#pragma unroll
-  for (int i = 0; i < 4; ++i) v[i] = first + i < rank ? v[i] * hd.scale : 0.f;
-  uint32_t lo[TP], hi[TP];
-  split<TP>(v[0], v[1], lo);
-  split<TP>(v[2], v[3], hi);
-  uint8_t* img = mp.images + ((size_t)tile * TP * slabs + (e >> 3)) * kXImage + swizzled(m, e & 7, 128) + h * 8;
-#pragma unroll
-  for (int k = 0; k < TP; ++k) *reinterpret_cast<uint2*>(img + (size_t)k * slabs * kXImage) = make_uint2(lo[k], hi[k]);
+  wait();
 }
 
 // ---------------------------------------------------------------------------- Y = Y0 + T B
@@ -486,7 +498,7 @@ __device__ __forceinline__ void store_oct(const Params& p, size_t at, const floa
 
 // The groups - 256 columns of a tile - are taken in order, each by the next CTA that is free: some SMs get at memory faster than others,
 // and CTAs that work side by side on neighbouring columns are kind to the memory's pages (4096 rows of 5120 x 13824 rank 64 in fp32, the
-// whole call: 108 us; 112 with every 148th group for a CTA, 114 with a stretch of its own for each).  The copying warp draws them, from
+// whole call, before later steps: 108 us; 112 with every 148th group for a CTA, 114 with a stretch of its own for each).  The copying warp draws them, from
 // a counter in the scratch; whose work a group is changes nothing in the results.  What the other warps see of it:
 struct Group { int g, rank, tile, part; };       // part: which 256 columns of the tile
 struct Groups {
@@ -901,8 +913,8 @@ cudaError_t launch_many(const Params& p, int x_type, int tiles, void* scratch, c
                                      : launch_project<kXMXINT8, 1, 6>(mp, s);
   if (e != cudaSuccess) return e;
   static OncePerDevice once[2];
-  const int eights = tiles * ((p.max_rank + 63) / 64) * 8;
-  e = p.y_bf16 ? launch(finish_kernel<2>, once[0], mp, eights, 256, 0, s) : launch(finish_kernel<3>, once[1], mp, eights, 256, 0, s);
+  const int items = tiles * ((p.max_rank + 63) / 64) * 4, finish_ctas = items < ctas ? items : ctas;
+  e = p.y_bf16 ? launch(finish_kernel<2>, once[0], mp, finish_ctas, 256, 0, s) : launch(finish_kernel<3>, once[1], mp, finish_ctas, 256, 0, s);
   if (e != cudaSuccess) return e;
   return p.y0_bf16 ? (p.y_bf16 ? launch_expand<true, true>(mp, ctas, s) : launch_expand<true, false>(mp, ctas, s))
                    : (p.y_bf16 ? launch_expand<false, true>(mp, ctas, s) : launch_expand<false, false>(mp, ctas, s));
