@@ -306,7 +306,8 @@ lqer_status_t lqer_poll_status(const void* workspace, void* stream, lqer_status_
  *    residual may be NULL (h = X rounded to r_dtype), residual_out may be NULL (h is not kept) or may be residual itself, or X if
  *    it has X's type.
  *  - Y [M,K] of y_dtype, apart from all inputs: fp32, bf16 (nearest even), or MXINT8 (K a multiple of 16), which is quantised as
- *    lqer_linear_ex would quantise it, from 64-bit values: mantissas and exponents are those of exact arithmetic on h.
+ *    lqer_linear_ex would quantise it, from 64-bit values: mantissas and exponents are those of exact arithmetic on h
+ *    (|weight| below 2^60).
  *  - K a multiple of 8, at most 2^20; eps >= 0.  One row takes one CTA; rows up to 32768 columns are read once. */
 lqer_status_t lqer_add_rms_norm(const void* X, lqer_dtype_t x_dtype, const void* residual, void* residual_out, lqer_dtype_t r_dtype,
                                 const void* weight, lqer_dtype_t w_dtype, double eps, int M, int K, const lqer_config_t* cfg,
@@ -314,7 +315,8 @@ lqer_status_t lqer_add_rms_norm(const void* X, lqer_dtype_t x_dtype, const void*
 
 /* Y = act(gate) * up, element by element.  gate and up: M rows of N elements of x_dtype (fp32 or bf16), row_stride elements from one row to
  * the next (N for two dense tensors, 2 N for the halves of one [M, 2 N] tensor; a multiple of 8).  Y [M,N] dense, of y_dtype: fp32,
- * bf16 or MXINT8 (N a multiple of 16; quantised from 64-bit values as above), apart from the inputs.  N is a multiple of 8, at most 2^22. */
+ * bf16 or MXINT8 (N a multiple of 16; quantised from 64-bit values as above, |gate * up| below 2^60), apart from the inputs.  N is a
+ * multiple of 8, at most 2^22.  act comes from fp32 arithmetic: a result below |gate * up| * 2^-126 may be zero. */
 typedef enum {
   LQER_SILU = 0,             /* g / (1 + exp(-g)) */
   LQER_GELU_TANH = 1         /* g / 2 * (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) */
