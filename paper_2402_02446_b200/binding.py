@@ -468,14 +468,20 @@ def _code(codes, dt) -> int:
 
 
 def _output(Y, M: int, N: int, out_dtype, like: torch.Tensor, index: int):
-    """The tensor of an [M, N] result (made where none is given; its type goes before out_dtype), its type's code and its address."""
+    """The tensor of an [M, N] result (made where none is given; its type goes before out_dtype), its type's code and its address.
+    like: an input, [M, N] or flat."""
     code = _OUT_CODE.get(out_dtype if Y is None else Y.dtype)
     if code is None:
         raise ValueError(f"unsupported output dtype {out_dtype if Y is None else Y.dtype}")
     if code == 2 and N % 16:
         raise ValueError("an MXINT8 output has whole blocks of 16 columns")
     if Y is None:
-        Y = like.new_empty(M * N + M * N // 16, dtype=torch.uint8) if code == 2 else like.new_empty((M, N), dtype=out_dtype)
+        if code == 2:
+            Y = like.new_empty(M * N + M * N // 16, dtype=torch.uint8)
+        elif like.is_contiguous() and like.dim() == 2:       # [M, N] itself
+            Y = torch.empty_like(like) if like.dtype == out_dtype else torch.empty_like(like, dtype=out_dtype)
+        else:
+            Y = like.new_empty((M, N), dtype=out_dtype)
         return Y, code, Y.data_ptr()
     if Y.shape != ((mxint8_bytes(M, N),) if code == 2 else (M, N)):
         raise ValueError("expected an output [M, N], or a flat uint8 tensor of mxint8_bytes(M, N)")
@@ -505,7 +511,8 @@ def add_rms_norm(X: torch.Tensor, weight: torch.Tensor, eps: float, residual: to
         r_ptr, r_code = _ptr(residual, index), _code(_REAL_CODE, residual.dtype)
         if residual_out is None:
             residual_out = torch.empty_like(residual)
-    if residual_out is not None:
+            h_ptr = residual_out.data_ptr()
+    if residual_out is not None and h_ptr is None:
         if residual_out.shape != shape or residual is not None and residual_out.dtype != residual.dtype:
             raise ValueError("residual_out has X's shape and the residual's type")
         h_ptr, r_code = _ptr(residual_out, index), _code(_REAL_CODE, residual_out.dtype)
