@@ -356,8 +356,8 @@ lqer_status_t lqer_adapter_plan(const int* slots, int M, int n_slots, void* plan
  * apart from everything otherwise).  plan: made by lqer_adapter_plan for the same M and the given plan_slots <= pool->n_slots; its
  * buffer is only read, but for its status: a plan of another batch size (or none), or a slot that no lqer_adapter_load
  * or lqer_adapter_pool_init of this pool's shape wrote, is reported there as LQER_ERR_BAD_PACKED, and such rows are not written or
- * take no adapter.  Rows of an empty slot take none.  K % 16 == 0, N % 8 == 0.  fp32 accumulation; fp32 X and X A are kept to
- * 24 bits for fp32 Y and to 16 bits for bf16 Y.  Up to 512 rows (1024 of small products) are one launch, and a row's result does not
+ * take no adapter.  Rows of an empty slot take none.  K % 16 == 0, N % 8 == 0.  fp32 accumulation; fp32 X and X A enter the next
+ * product with all 24 bits for fp32 Y, and rounded to nearest within 2^-17 of their value for bf16 Y.  Up to 512 rows (1024 of small products) are one launch, and a row's result does not
  * depend on the other rows' values; more are three, with X A in between in `workspace` (lqer_adapters_workspace_bytes, 256-byte
  * aligned; where that is 0 bytes the workspace may be NULL; nothing in it has to be kept or cleared between calls, and calls
  * that overlap need one each).  The sums are taken in an order that M, the plan and the pool's shape decide, so a row's last bits

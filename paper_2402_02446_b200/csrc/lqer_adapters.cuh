@@ -84,27 +84,43 @@ __device__ __forceinline__ void st32(void* p, bool aligned, const uint4& a, cons
 // The upper halves of two fp32 values (their leading bf16 parts, cut off) in one word.
 __device__ __forceinline__ uint32_t top_halves(float lo, float hi) { return __byte_perm(__float_as_uint(lo), __float_as_uint(hi), 0x7632); }
 __device__ __forceinline__ float top_half(float v) { return __uint_as_float(__float_as_uint(v) & 0xFFFF0000u); }
-// P parts of two values: word p holds part p of both.  What is left of an infinity is nothing (it is all in its first part); NaN stays.
+__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
+  uint32_t d;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
+  return d;
+}
+// P bf16 parts of fp32 values.  Three parts are cut off one after the other and hold all 24 bits.  Two are rounded to nearest: what is left of
+// the first is at most 2^-8 of the value, of the second 2^-17, either way alike (cut off, it would be up to 2^-15, always towards
+// zero).  Either takes as many instructions.  kBf16Max: beyond the largest bf16 a value would be rounded to infinity.
+constexpr float kBf16Max = 3.3895313892515354759e38f;
+// The first part of a pair, and what is left of it.
+template <int P>
+__device__ __forceinline__ uint32_t first_part(float& a, float& b) {
+  const uint32_t w = P == 2 ? round_bf16x2(a, b) : top_halves(a, b);
+  a -= P == 2 ? __uint_as_float(w << 16) : top_half(a);                    // exact
+  b -= P == 2 ? __uint_as_float(w & 0xFFFF0000u) : top_half(b);
+  return w;
+}
+// Any pair: word p holds part p of both.  The first part of a value beyond kBf16Max is cut off; what is left of an infinity is nothing (it is
+// all in its first part); NaN stays.
 template <int P>
 __device__ __forceinline__ void split(float a, float b, uint32_t (&w)[P]) {
   const float inf = __uint_as_float(0x7F800000u);
+  w[0] = top_halves(fabsf(a) > kBf16Max || P != 2 ? a : __uint_as_float(round_bf16x2(a, a) & 0xFFFF0000u),
+                    fabsf(b) > kBf16Max || P != 2 ? b : __uint_as_float(round_bf16x2(b, b) & 0xFFFF0000u));
+  a = fabsf(a) == inf ? 0.f : a - __uint_as_float(w[0] << 16);
+  b = fabsf(b) == inf ? 0.f : b - __uint_as_float(w[0] & 0xFFFF0000u);
 #pragma unroll
-  for (int p = 0; p < P; ++p) {
-    w[p] = top_halves(a, b);
-    if (p + 1 < P) {
-      const float ra = a - top_half(a), rb = b - top_half(b);              // exact
-      a = p == 0 && fabsf(a) == inf ? 0.f : ra;
-      b = p == 0 && fabsf(b) == inf ? 0.f : rb;
-    }
-  }
+  for (int p = 1; p + 1 < P; ++p) w[p] = first_part<P>(a, b);
+  if (P > 1) w[P - 1] = P == 2 ? round_bf16x2(a, b) : top_halves(a, b);
 }
-// The same of eight values, of which an infinity is rare: one test for all.
+// Eight values, of which one beyond kBf16Max is rare: one test for all.
 template <int P>
 __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&w)[4][P]) {
   float big = 0.f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) big = fmaxf(big, fabsf(v[i]));
-  if (big == __uint_as_float(0x7F800000u)) {
+  if (big > kBf16Max) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) split<P>(v[2 * i], v[2 * i + 1], w[i]);
     return;
@@ -113,11 +129,8 @@ __device__ __forceinline__ void split8(const float (&v)[8], uint32_t (&w)[4][P])
   for (int i = 0; i < 4; ++i) {
     float a = v[2 * i], b = v[2 * i + 1];
 #pragma unroll
-    for (int p = 0; p < P; ++p) {
-      w[i][p] = top_halves(a, b);
-      a -= top_half(a);
-      b -= top_half(b);
-    }
+    for (int p = 0; p + 1 < P; ++p) w[i][p] = first_part<P>(a, b);
+    w[i][P - 1] = P == 2 ? round_bf16x2(a, b) : top_halves(a, b);
   }
 }
 
@@ -189,11 +202,6 @@ struct Y0Quad {
     return make_float4(__uint_as_float(a.x), __uint_as_float(a.y), __uint_as_float(a.z), __uint_as_float(a.w));
   }
 };
-__device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
-  uint32_t d;
-  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(hi), "f"(lo));
-  return d;
-}
 __device__ __forceinline__ void store_y(const Params& p, size_t idx, const float4& v) {
   if (!LQER_IN_BOUNDS(&p.plan->status, idx * (p.y_bf16 ? 2 : 4), p.y_bf16 ? 8 : 16, p.y_extent, 802)) return;
   if (p.y_bf16) *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + idx) = make_uint2(round_bf16x2(v.x, v.y), round_bf16x2(v.z, v.w));
