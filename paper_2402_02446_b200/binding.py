@@ -469,7 +469,7 @@ def _code(codes, dt) -> int:
 
 def _output(Y, M: int, N: int, out_dtype, like: torch.Tensor, index: int):
     """The tensor of an [M, N] result (made where none is given; its type goes before out_dtype), its type's code and its address.
-    like: an input, [M, N] or flat."""
+    like: an input of any shape."""
     code = _OUT_CODE.get(out_dtype if Y is None else Y.dtype)
     if code is None:
         raise ValueError(f"unsupported output dtype {out_dtype if Y is None else Y.dtype}")
@@ -478,7 +478,7 @@ def _output(Y, M: int, N: int, out_dtype, like: torch.Tensor, index: int):
     if Y is None:
         if code == 2:
             Y = like.new_empty(M * N + M * N // 16, dtype=torch.uint8)
-        elif like.is_contiguous() and like.dim() == 2:       # [M, N] itself
+        elif like.shape == (M, N) and like.is_contiguous():
             Y = torch.empty_like(like) if like.dtype == out_dtype else torch.empty_like(like, dtype=out_dtype)
         else:
             Y = like.new_empty((M, N), dtype=out_dtype)
@@ -551,13 +551,14 @@ def gated_activation(gate: torch.Tensor, up: torch.Tensor, act: str = "silu", ou
 
 def dequantize_activations(Xq: torch.Tensor, M: int, K: int, out_dtype=torch.float32, cfg: Config | None = None,
                            Y: torch.Tensor | None = None, stream=None) -> torch.Tensor:
-    """The values of a flat MXINT8 buffer of [M, K] activations (exact in fp32 and in bf16)."""
+    """The values of an MXINT8 buffer of [M, K] activations (uint8, mxint8_bytes(M, K) of them in any shape, as linear_ex takes it):
+    [M, K], exact in fp32 and in bf16."""
     index = Xq.get_device()
     if stream is not None or not _here(index):
         with _on(stream, index):
             return dequantize_activations(Xq, M, K, out_dtype, cfg, Y)
     if Xq.dtype != torch.uint8 or K % 16 or Xq.numel() != mxint8_bytes(M, K):
-        raise ValueError("an MXINT8 tensor is a flat uint8 tensor of mxint8_bytes(M, K)")
+        raise ValueError("an MXINT8 tensor is a uint8 tensor of mxint8_bytes(M, K) elements")
     Y, y_code, y_ptr = _output(Y, M, K, out_dtype, Xq, index)
     status = lib().lqer_dequantize_activations(_ptr(Xq, index), M, K, None if cfg is None else C.byref(cfg), y_ptr, y_code,
                                                _raw_stream(index))

@@ -137,3 +137,13 @@ def test_a_plan_has_room_for_every_batch():
                 worst = sum(-(-r // rows) for r in [1] * (bins - 1) + [M - (bins - 1)])
                 need += 8 * worst + 4 * rows * worst
             assert size.value >= need, (M, n)
+
+
+def test_a_result_has_its_own_shape_whatever_its_inputs():
+    # an MXINT8 buffer may come in two dimensions: what is made beside it is [M, K] all the same
+    for shape in ((4, 68), (1, 272), (272,), (2, 136)):
+        for dt in (torch.float32, torch.bfloat16):
+            Y, _, _ = binding._output(None, 4, 64, dt, torch.zeros(shape, dtype=torch.uint8), -1)
+            assert Y.shape == (4, 64) and Y.dtype == dt and Y.is_contiguous()
+    Y, _, _ = binding._output(None, 4, 64, torch.bfloat16, torch.zeros((4, 128))[:, :64], -1)
+    assert Y.shape == (4, 64) and Y.is_contiguous()

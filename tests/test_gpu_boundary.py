@@ -180,6 +180,17 @@ def test_gated_activation_large_negative_gates_keep_their_borders():
         _check(L.gated_activation(g, u, act=act, cfg=cfg), _act64(g.double().cpu().numpy(), act)[0] * u.double().cpu().numpy(), 0, 64, 512, "mxint8", cfg)
 
 
+def test_values_of_a_buffer_in_two_dimensions():
+    M, K = 4, 64
+    Xq = L.to_mxint8(*L.quantize_activations(_values((M, K), 45, torch.float32)))
+    for dt in (torch.float32, torch.bfloat16):
+        want = L.dequantize_activations(Xq, M, K, out_dtype=dt)
+        assert want.shape == (M, K)
+        for shape in ((M, 17 * K // 16), (1, -1), (2, -1)):
+            got = L.dequantize_activations(Xq.view(shape), M, K, out_dtype=dt)
+            assert got.shape == (M, K) and torch.equal(got, want)
+
+
 def test_values_into_a_tensor_aligned_to_16_bytes_only():
     X = _values((9, 272), 44, torch.float32)
     Xq = L.to_mxint8(*L.quantize_activations(X))
