@@ -213,6 +213,17 @@ def test_bad_slots_plans_and_pools_are_reported_and_touch_nothing():
     assert L.poll_status(plan.buf) == BAD_PACKED and torch.equal(Z, c.Y0)
 
 
+@pytest.mark.parametrize("M", [2, 512, 1024, 2000])
+def test_a_shorter_batchs_plan_is_refused_unread(M):
+    # the plan's buffer holds one row's lists and no more; the call would need some hundred times as much
+    c = Case(M, 256, 264, [8, 16, 8, 8], [j % 5 - 1 for j in range(M)])
+    small = L.adapter_plan(c.slots[:1], c.pool)
+    Z = torch.full_like(c.Y0, 5.0)
+    L.apply_adapters(c.X, c.pool, L.AdapterPlan(small.buf, M, 4), c.Y0, Y=Z)
+    assert L.poll_status(small.buf) == BAD_PACKED and (Z == 5.0).all()
+    c.check(c.run())
+
+
 def test_streams_graphs_and_two_batches_at_once():
     c = Case(24, 1040, 520, [16, 64, 8], [j % 4 - 1 for j in range(24)])
     Y = c.run()
