@@ -465,6 +465,11 @@ __device__ __forceinline__ void gate8(const float (&g)[8], const float (&u)[8], 
     const F2 v2 = mul2(mul2(g2, f2(r[0], r[1])), f2(u[i], u[i + 1]));
     unf2(v2, v[i], v[i + 1]);
   }
+  if (ACT == LQER_SILU && !(y < 128.f)) {             // rare (a mask of the type's lowest value): the same without those that are zero
+    y = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) y = fmaxf(y, g[i] * -kLog2e < 128.f ? g[i] * -kLog2e : 0.f);
+  }
   rel = fmaf(y, ACT == LQER_SILU ? 2.3841858e-7f : 9.5367432e-7f, 7.1525574e-7f);
 }
 // act(gate[at]) * up[at] in fp64: for values in doubt, from memory again, so that nothing has to be kept for them.

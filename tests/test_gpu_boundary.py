@@ -180,6 +180,41 @@ def test_gated_activation_large_negative_gates_keep_their_borders():
         _check(L.gated_activation(g, u, act=act, cfg=cfg), _act64(g.double().cpu().numpy(), act)[0] * u.double().cpu().numpy(), 0, 64, 512, "mxint8", cfg)
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_gated_activation_special_values(x, act):
+    # masks of the type's lowest value, infinities and NaN, alone in a block, all over a row, and beside ordinary values
+    N, rows, inf, nan = 272, 16, float("inf"), float("nan")
+    g, u = _values((rows, N), 61, TYPES[x], 2), _values((rows, N), 62, TYPES[x], 2)
+    low = torch.finfo(TYPES[x]).min
+    g[0], u[0] = low, 0.0                        # a masked row
+    g[1] = low
+    g[2, 16:48], u[2, 16:48] = low, 0.0          # masked blocks
+    g[3, ::2] = low
+    g[4], g[5] = -inf, inf
+    g[6, 5], g[7, 21], u[8, 40] = -inf, inf, inf
+    g[9, 3], u[10, 4], g[11, 64:80] = nan, nan, nan
+    g[12, 7], u[12, 7] = 0.0, -inf
+    g[13], u[13, ::2] = -200.0, 0.0
+    g[14], u[14] = -1000.0, 2.0 ** 20
+    g[15, ::3] = -90.0
+    with np.errstate(all="ignore"):
+        g64, u64 = g.double().cpu().numpy(), u.double().cpu().numpy()
+        z = g64 if act == "silu" else 2.0 * math.sqrt(2.0 / math.pi) * (g64 + 0.044715 * g64 ** 3)
+        want = g64 / (1.0 + np.exp(-z)) * u64
+        tail = np.where(np.isfinite(g64 * u64), np.abs(g64 * u64) * 2.0 ** -126, 0.0) + 2.0 ** -126      # what may come out as zero
+    rel = (10 + 7 * 90) * U
+    for cfg in (_cfg(), _cfg(6, -40, 3)):
+        _check(L.gated_activation(g, u, act=act, cfg=cfg), want, 0, rows, N, "mxint8", cfg)
+    for y in ("f32", "bf16"):
+        got = L.gated_activation(g, u, act=act, out_dtype=TYPES[y]).double().cpu().numpy()
+        assert np.array_equal(np.isnan(got), np.isnan(want))
+        assert np.array_equal(np.isinf(got), np.isinf(want)) and np.array_equal(np.sign(got[np.isinf(got)]), np.sign(want[np.isinf(want)]))
+        at = np.isfinite(want)
+        bound = np.abs(want[at]) * (rel + (2.0 ** -8 if y == "bf16" else 0.0) * (1 + rel)) + tail[at]
+        assert (np.abs(got[at] - want[at]) <= bound).all()
+
+
 def test_values_of_a_buffer_in_two_dimensions():
     M, K = 4, 64
     Xq = L.to_mxint8(*L.quantize_activations(_values((M, K), 45, torch.float32)))
