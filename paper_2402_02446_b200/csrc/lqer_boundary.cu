@@ -210,6 +210,11 @@ struct RawRow {              // a lane's octet of X and of the residual
     }
   }
 };
+// h * inv * w in fp64, rounded to 48 bits.  Borders have nine, so a value that lies on one exactly (rows of one magnitude, eps 0) gets back on it,
+// from which the inverse root, a unit or two off, and the products have taken it; none gets across.
+__device__ __forceinline__ double norm_wide(float h, double inv, float w) {
+  return __longlong_as_double((__double_as_longlong((double)h * inv * (double)w) + 16) & ~31LL);
+}
 // One row's octet of Y.  Bound on the fp32 values' error: the inverse root, its product with h and the product with w are
 // rounded once each, 3 * 2^-24 < 2^-22; an inverse root near the end of fp32's range has no such bound.
 template <int YT>
@@ -222,7 +227,7 @@ __device__ __forceinline__ void finish8(const NormParams& p, size_t idx, bool in
   if (YT == kYMXINT8) {
     uint2 m8;
     int e;
-    quantise8(v, qc, inv > 1e-30f ? 2.3841858e-7f : 1.0f, [&](int i) { return (double)pick8(h, i) * inv64 * (double)pick8(w, i); }, m8, e);
+    quantise8(v, qc, inv > 1e-30f ? 2.3841858e-7f : 1.0f, [&](int i) { return norm_wide(pick8(h, i), inv64, pick8(w, i)); }, m8, e);
     if (in) store_mxint8(p.Y, p.Ye, idx, m8, e);
   } else if (in) {
     store8<YT == kYBF16>(p.Y, idx, v);

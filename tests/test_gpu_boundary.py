@@ -133,6 +133,24 @@ def test_add_rms_norm_special_values():
     assert (Y == 0).all()
 
 
+@pytest.mark.parametrize("K", [256, 4096, 4112, 8208, 16400, 33024])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_add_rms_norm_rows_that_lie_on_a_border(x, K):
+    # rows of one magnitude: h / rms is +-1, the lower border of an exponent, whatever the magnitude
+    c = torch.arange(1, 128, device=DEV, dtype=torch.float32)[:, None]
+    sign = torch.randint(0, 2, (127, K), generator=torch.Generator(device=DEV).manual_seed(71), device=DEV) * 2 - 1
+    h = (c * sign).to(TYPES[x])
+    res = (h.float() * 0.5 if x == "f32" else torch.zeros_like(h)).to(TYPES[x])
+    w = torch.exp2(torch.arange(K, device=DEV).float() // 16 % 3)
+    m, e = L.split_mxint8(L.add_rms_norm(h - res, w, 0.0, residual=res)[0], 127, K)
+    assert (m == 64 * sign).all() and (e.int() - 127 == torch.arange(K // 16, device=DEV) % 3).all()
+    # half of each row a, half 7 a: rms 5 a; 7 / 5 * 1.25 is a value with seven bits, 1 / 5 * 1.25 a power of two
+    h = torch.where(torch.arange(K, device=DEV) % 2 == 0, c, 7 * c)
+    h = h[(7 * c[:, 0]).to(TYPES[x]) == 7 * c[:, 0]].to(TYPES[x])
+    m, e = L.split_mxint8(L.add_rms_norm(h, torch.full((K,), 1.25, device=DEV), 0.0)[0], h.shape[0], K)
+    assert (m[:, 1::2] == 112).all() and (m[:, ::2] == 16).all() and (e == 127).all()
+
+
 def _act64(g, act):
     with np.errstate(over="ignore"):
         z = g if act == "silu" else 2.0 * math.sqrt(2.0 / math.pi) * (g + 0.044715 * g ** 3)
