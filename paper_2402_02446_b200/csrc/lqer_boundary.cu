@@ -229,8 +229,12 @@ __device__ __forceinline__ void finish8(const NormParams& p, size_t idx, bool in
     int e;
     quantise8(v, qc, inv > 1e-30f ? 2.3841858e-7f : 1.0f, [&](int i) { return norm_wide(pick8(h, i), inv64, pick8(w, i)); }, m8, e);
     if (in) store_mxint8(p.Y, p.Ye, idx, m8, e);
-  } else if (in) {
-    store8<YT == kYBF16>(p.Y, idx, v);
+  } else {
+    if (!(inv > 1e-37f && inv < 1e37f)) {             // the whole row's; not a normal fp32 number
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = (float)((double)h[i] * inv64 * (double)w[i]);
+    }
+    if (in) store8<YT == kYBF16>(p.Y, idx, v);
   }
 }
 // The sum over the CTA, in every thread: warps first, then one value a warp.  Two calls in a row need two sets of slots.

@@ -151,6 +151,19 @@ def test_add_rms_norm_rows_that_lie_on_a_border(x, K):
     assert (m[:, 1::2] == 112).all() and (m[:, ::2] == 16).all() and (e == 127).all()
 
 
+@pytest.mark.parametrize("K", [264, 4104, 8200, 16392, 33024])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+def test_add_rms_norm_rows_near_the_ends_of_the_range(x, K):
+    # the inverse root of such rows is beyond fp32, or not a normal number there; their norms are ordinary numbers
+    size = torch.tensor([1e-40, 4e-39, 1.3e-38, 1e-36, 1e-30, 1e30, 1e36, 2e37, 8e37, 1.6e38], dtype=torch.float64, device=DEV)
+    X = (size[:, None] * (0.5 + 1.5 * torch.rand((len(size), K), generator=torch.Generator(device=DEV).manual_seed(72), device=DEV).double())).to(TYPES[x])
+    w = 1.0 + 0.2 * _values((K,), 73, torch.float32, 0)
+    want = _norm64(X, w, 0.0)
+    for y in ("f32", "bf16"):
+        Y, _ = L.add_rms_norm(X, w, 0.0, out_dtype=TYPES[y])
+        _check(Y, want, 3 * U * (1 + 4 * U), len(size), K, y, None)
+
+
 def _act64(g, act):
     with np.errstate(over="ignore"):
         z = g if act == "silu" else 2.0 * math.sqrt(2.0 / math.pi) * (g + 0.044715 * g ** 3)
