@@ -420,6 +420,25 @@ def test_a_wait_that_runs_out_is_reported_and_the_next_call_is_fine():
         assert torch.equal(c.run(), Y) and L.poll_status(c.plan.buf) == 0
 
 
+@pytest.mark.parametrize("y", ["f32", "bf16"])
+def test_waits_that_run_out_anywhere_leave_nothing_under_way(y):
+    # bounds around the time that ordinary waits take: now one role gives up, now another, with copies and products on their way;
+    # the calls that follow own the same shared and tensor memory
+    c = _many(11, y, M=3000, N=2056)
+    Y = c.run()
+    c.check(Y)
+    for limit in (1000, 1500, 2500, 4000, 6000, 10000, 20000) * 3:
+        L.set_wait_limit_cycles(limit)
+        try:
+            Z = c.run()
+            torch.cuda.synchronize()
+        finally:
+            L.set_wait_limit_cycles(4_000_000_000)
+        status = L.poll_status(c.plan.buf)
+        assert status in (0, TIMEOUT) and (status != 0 or torch.equal(Z, Y))
+        assert torch.equal(c.run(), Y) and L.poll_status(c.plan.buf) == 0
+
+
 def test_the_checked_build_keeps_to_the_extent_of_y():
     code = textwrap.dedent("""
         import sys, torch
