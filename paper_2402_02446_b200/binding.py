@@ -431,11 +431,20 @@ _OUT_CODE = {torch.float32: 0, torch.bfloat16: 1, MXINT8: 2, torch.uint8: 2}
 _ACTS = {"silu": 0, "gelu": 1}
 
 
+def _public_raw_stream(index: int) -> int:
+    return torch.cuda.current_stream(index).cuda_stream
+
+
+# torch's own short ways (a microsecond a call less), or its public ones where a release has no such names
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", _public_raw_stream)
+
+
 def _here(index: int) -> bool:
     """Whether the device of a call's first tensor is the current one."""
     if index < 0:
         raise ValueError("expected CUDA tensors")
-    return index == torch._C._cuda_getDevice()
+    return index == _current_device()
 
 
 def _on(stream, index: int):
@@ -454,10 +463,6 @@ def _ptr(t: torch.Tensor, index: int) -> int:
     if t.get_device() != index or not t.is_contiguous():
         raise ValueError("expected contiguous CUDA tensors of one device")
     return t.data_ptr()
-
-
-def _raw_stream(index: int) -> int:
-    return torch._C._cuda_getCurrentRawStream(index)
 
 
 def _code(codes, dt) -> int:

@@ -13,6 +13,7 @@ import torch
 
 import paper_2402_02446_b200 as L
 from oracle import mxint
+from paper_2402_02446_b200 import binding
 
 pytestmark = pytest.mark.gpu
 DEV = "cuda:0"
@@ -306,3 +307,15 @@ def test_streams_and_graphs():
         graph.replay()
         Y1, out1 = L.add_rms_norm(X * k, w, 1e-5, residual=res)
         assert torch.equal(Yg, Y1) and torch.equal(h, out1) and torch.equal(Zg, L.gated_activation(out1, X * k))
+
+
+def test_the_public_ways_to_device_and_stream_say_the_same(monkeypatch):
+    s = torch.cuda.Stream()
+    for stream in (torch.cuda.current_stream(), s):
+        with torch.cuda.stream(stream):
+            assert binding._public_raw_stream(0) == binding._raw_stream(0) == stream.cuda_stream
+    X, w = _values((3, 256), 81, torch.float32), torch.ones(256, device=DEV)
+    Y, _ = L.add_rms_norm(X, w, 1e-5)
+    monkeypatch.setattr(binding, "_raw_stream", binding._public_raw_stream)
+    monkeypatch.setattr(binding, "_current_device", torch.cuda.current_device)
+    assert torch.equal(L.add_rms_norm(X, w, 1e-5)[0], Y)
