@@ -319,3 +319,60 @@ def test_the_public_ways_to_device_and_stream_say_the_same(monkeypatch):
     monkeypatch.setattr(binding, "_raw_stream", binding._public_raw_stream)
     monkeypatch.setattr(binding, "_current_device", torch.cuda.current_device)
     assert torch.equal(L.add_rms_norm(X, w, 1e-5)[0], Y)
+
+
+# ---- batches of prompt size: more rows than there are CTAs, so that a CTA works on one row with the next one on its way ----
+
+@pytest.mark.parametrize("y", ["f32", "bf16", "mxint8"])
+@pytest.mark.parametrize("r", ["f32", "bf16"])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("M,K", [(5000, 48), (2500, 1040), (700, 4112), (601, 8208), (400, 16400)])
+def test_add_rms_norm_of_a_prompt(M, K, x, r, y):
+    X, res = _values((M, K), 91, TYPES[x], 3), _values((M, K), 92, TYPES[r], 3)
+    w = 1.0 + 0.2 * _values((K,), 93, torch.float32, 0)
+    out_dtype = L.MXINT8 if y == "mxint8" else TYPES[y]
+    h = (X.float() + res.float()).to(TYPES[r])
+    Y, out = L.add_rms_norm(X, w, 1e-5, residual=res, out_dtype=out_dtype)
+    assert torch.equal(out, h)
+    _check(Y, _norm64(h, w, 1e-5), 3 * U * (1 + 4 * U), M, K, y, _cfg())
+    # the sum in the residual's place, or in X's: a row is written while the next one is on its way
+    own = res.clone()
+    Z, out = L.add_rms_norm(X, w, 1e-5, residual=own, residual_out=own, out_dtype=out_dtype)
+    assert out is own and torch.equal(own, h) and torch.equal(Z, Y)
+    if x == r:
+        own = X.clone()
+        Z, out = L.add_rms_norm(own, w, 1e-5, residual=res, residual_out=own, out_dtype=out_dtype)
+        assert out is own and torch.equal(own, h) and torch.equal(Z, Y)
+    # no residual, h not kept
+    Z, out = L.add_rms_norm(h, w, 1e-5, out_dtype=out_dtype)
+    assert out is None and torch.equal(Z, Y)
+
+
+@pytest.mark.parametrize("y", ["f32", "bf16", "mxint8"])
+@pytest.mark.parametrize("act", ["silu", "gelu"])
+@pytest.mark.parametrize("x", ["f32", "bf16"])
+@pytest.mark.parametrize("M,N,joined", [(2500, 272, True), (1500, 2064, False), (1301, 2064, True), (601, 11008, False), (250, 13824, True)])
+def test_gated_activation_of_a_prompt(M, N, joined, x, act, y):
+    if joined:
+        both = _values((M, 2 * N), 94, TYPES[x], 3)
+        gate, up = both[:, :N], both[:, N:]
+    else:
+        gate, up = _values((M, N), 94, TYPES[x], 3), _values((M, N), 95, TYPES[x], 3)
+    cfg = _cfg(6 if M == 1301 else 8)
+    Y = L.gated_activation(gate, up, act=act, out_dtype=L.MXINT8 if y == "mxint8" else TYPES[y], cfg=cfg)
+    g = gate.double()
+    z = g if act == "silu" else 2.0 * math.sqrt(2.0 / math.pi) * (g + 0.044715 * g ** 3)
+    want = g / (1.0 + torch.exp(-z)) * up.double()
+    zs = 0.0 if act == "silu" else z.abs().cpu().numpy()
+    _check(Y, want.cpu().numpy(), (10 + 7 * zs) * U * (1 + 1e-5), M, N, y, cfg, tiny=2.0 ** -102)
+
+
+def test_values_of_a_prompt():
+    M, K = 2300, 11008                           # more blocks than the grid has threads
+    g = torch.Generator(device=DEV).manual_seed(96)
+    m = torch.randint(-127, 128, (M, K), generator=g, device=DEV, dtype=torch.int8)
+    e = torch.randint(127 - 56, 127 + 56, (M, K // 16), generator=g, device=DEV, dtype=torch.uint8)
+    want = m.double() * torch.exp2(e.double() - 127 - 6).repeat_interleave(16, 1)
+    for dt in (torch.float32, torch.bfloat16):
+        got = L.dequantize_activations(L.to_mxint8(m, e), M, K, out_dtype=dt)
+        assert torch.equal(got.double(), want)
