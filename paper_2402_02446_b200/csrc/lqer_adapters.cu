@@ -18,17 +18,20 @@
 // Few rows (up to 512, and up to 1024 of small products; few_rows_kernel): a cluster of CTAs takes a tile of up to 8 rows.  The factors are the MMA's 16-row operand, the tokens its 8
 // columns.  First the CTAs share the contraction over K, then each sends its part of T to all (distributed shared memory),
 // and then they share the columns of Y.  T never leaves the chip, and everything is summed in a fixed order.
-// Measured: one row of 4096 x 4096 rank 16 5.0 us, 64 rows of 24 adapters of 5120 x 5120 rank 16 in bf16 7.4 us, 16 rows of as many
-// adapters of 4096 x 11008 rank 64 (MXINT8 to fp32) 12.5 us, 1.3 TB/s.  What bounds them is the chain of a tile: plan, slot, A and
-// X, the exchange of T, B - some six trips to memory one after the other - and not bytes (2.5 us of the 12.5) or instructions (a fifth of
-// the issue slots).  The plan, one CTA: 3.7 us for 64 rows, 7.5 us for 4096.
+// Measured: one row of 4096 x 4096 rank 16 5.1 us, 64 rows of 24 adapters of 5120 x 5120 rank 16 in bf16 7.5 us, 16 rows of as many
+// adapters of 4096 x 11008 rank 64 (MXINT8 to fp32) 12.1 us, 1.3 TB/s.  What bounds them is the chain of a tile: plan, slot, A and
+// X, the exchange of T, B - some seven trips to memory one after the other - and not bytes (2.5 us of the 12.1) or instructions (a fifth of
+// the issue slots).  With more tiles than fit the device at once it is the tiles of eight rows, each of which reads its adapter whole:
+// 256 rows of 4 adapters of 4096 x 11008 rank 64 in bf16 21.6 us, 512 rows 31.7.  The plan, one CTA: 3.7 us for 64 rows, 7.5 us for 4096.
 // Many rows: lqer_adapters_many.cu.
 //
 // Precision: A, B and MXINT8 or bf16 X are exact in bf16.  fp32 X and T (summed in fp32) enter the tensor cores as sums of bf16 parts:
 // for fp32 Y three, which hold all 24 bits, for bf16 Y two, rounded to nearest (2^-17 of each value, against 2^-8 for the bf16 result;
 // three there as well: 2048 rows of 4096 x 11008 rank 64 in bf16 38.0 -> 40.8 us, rank 128 47.7 -> 58.3, 201 rows of 4112 x 10992 rank 20
-// fp32 to bf16 12.6 -> 14.2).  The tensor cores cut a running sum off where it does not fit, so their chains are kept short - a
-// block of 32 of K, lower parts first - and added up by ordinary fp32 additions.
+// fp32 to bf16 12.6 -> 14.2).  The tensor cores cut a running sum off where it does not fit, so their chains are kept
+// short, lower parts first, and added up by ordinary fp32 additions.  A chain is, for few rows: 32 of K and the parts of X (then fp32 additions),
+// all ranks and parts of T; for many rows: up to 2048 of K and one part of X - all three parts of an fp32 X where the rank is beyond 160,
+// for which tensor memory has no room apart - and all ranks and parts of T.
 #include "lqer_adapters.cuh"
 
 namespace lqer {
@@ -48,6 +51,8 @@ __device__ __forceinline__ uint16_t to_bf16(const void* p, bool bf16, size_t i) 
   asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(d) : "f"(0.f), "f"(v));
   return (uint16_t)d;
 }
+// (A thread writes two bytes at a time, wherever they belong: loading is not on a step's path.  Rank 16 of 4096 x 4096 3 us, rank 64 of
+// 4096 x 11008 11.8 us, rank 256 of 5120 x 13824 45 us.)
 __global__ void adapter_load_kernel(uint8_t* slot, const void* A, const void* B, bool bf16, int K, int N, int max_rank, int rank, float scale) {
   const size_t stride = (size_t)gridDim.x * blockDim.x, first = (size_t)blockIdx.x * blockDim.x + threadIdx.x;
   if (first == 0) *reinterpret_cast<SlotHead*>(slot) = SlotHead{kPoolMagic, K, N, max_rank, rank, scale, {0, 0}};

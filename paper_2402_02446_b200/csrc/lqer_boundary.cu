@@ -10,10 +10,11 @@
 // again from fp64 values.  About one warp in thirty goes that way, so fp64 throughput does not matter.
 // What it costs beside that is instructions, so two elements share one where they can.
 //
-// Measured, and what bounds them.  Norm with residual, 2048 x 4096 bf16 to MXINT8: 12.7 us, 4.7 TB/s; 59 % of the issue slots are taken,
-// memory a third; 4096 x 5120 to bf16, where there is less to compute: 27.7 us, 6.1 TB/s.  Gate, 2048 x 11008 bf16 to MXINT8: 25.9 us,
-// 4.4 TB/s, 64 % of the issue slots (the exponential, the borders); to bf16 24.0 us, 5.6 TB/s; fp32 2048 x 13824 to fp32 54.5 us,
-// 6.2 TB/s.  MXINT8 to bf16, 2048 x 11008: 12.0 us, 5.7 TB/s, memory.  One row of the first two: 2.2 and 1.4 us, a launch and a trip to memory.
+// Measured, and what bounds them.  Norm with residual, 2048 x 4096 bf16 to MXINT8: 12.8 us, 4.6 TB/s (to bf16 12.7); 59 % of the issue slots are
+// taken, memory a third: its 24 warps an SM wait for fixed latencies and for the barrier of each row, and 2048 rows are five turns of 444 CTAs
+// for 4.6.  4096 x 5120 to bf16: 27.7 us, 6.1 TB/s.  Gate, 2048 x 11008 bf16 to MXINT8: SiLU 26.2 us, 4.4 TB/s, 64 % of the issue slots
+// (the exponential, the borders), GELU 32.5; of fp32 34.5 and 36.4, 5.9 TB/s; bf16 to bf16 23.8 us with either, 5.7 TB/s; fp32 2048 x 13824 to
+// fp32 55 us, 6.2 TB/s.  MXINT8 to bf16, 2048 x 11008: 12.0 us, 5.7 TB/s, memory.  One row of the first two: 2.2 and 1.4 us, a launch and a trip to memory.
 #include "lqer_tc_ptx.cuh"
 
 namespace lqer {
@@ -436,7 +437,8 @@ template <int ACT, class T>
 __device__ __forceinline__ T act_argument(T g) {
   return ACT == LQER_SILU ? g : (T)1.5957691216057307117597842397375 * (g + (T)0.044715 * g * g * g);
 }
-// Eight values of the result, and a bound on their relative error.  fp32 results take expf.  Narrower ones take the special
+// Eight values of the result, and a bound on their relative error.  fp32 results take expf and the quick quotient, two units in
+// the last place off (bf16 to fp32, 2048 x 11008: 30.1 us, with an exactly rounded one 44.0).  Narrower ones take the special
 // function unit's 2^x of -z log2(e): beside the units of 2^-23 of ex2 (2), of the reciprocal (1), of the sum and of two products (1/2
 // each) an error of z counts |z| times where exp(-z) rules the denominator, z < 0: one rounding and that of the constant for
 // SiLU (2^-23 |z|), five more for GELU (2^-21 |z|); the bound allows twice that, and 6 units for the rest, that of z > 0
@@ -496,7 +498,7 @@ __device__ __noinline__ double gate_wide(const void* gate, const void* up, size_
 }
 // Thread t of a CTA's row of threads holds columns 8 t .. 8 t + 7 of the CTA's stretch, of every gridDim.y-th row; the next row's are on
 // their way while this one's are worked on.  Eight CTAs of 64 registers fit an SM: the values in doubt come from memory again, since with all
-// inputs kept for them registers were spilled (2048 x 11008, fp32 39.9 us against 34.4, GELU 58 against 33).
+// inputs kept for them registers were spilled (2048 x 11008 to MXINT8, SiLU of fp32 39.9 us against 34.4, GELU of bf16 58 against 32.5).
 template <bool XB, int YT, int ACT>
 __global__ void __launch_bounds__(128, 8) gated_activation_kernel(const GateParams p) {
   tc::pdl_launch_dependents();
