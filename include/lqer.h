@@ -337,7 +337,8 @@ lqer_status_t lqer_dequantize_activations(const void* Xq, int M, int K, const lq
  * in bf16 in the kernel's order.  The struct is the caller's (host); `data` is device memory, 256-byte aligned.
  *  - lqer_adapter_pool_bytes reads K, N, max_rank, n_slots.  lqer_adapter_pool_init empties all slots.
  *  - lqer_adapter_load puts A [K,rank] and B [rank,N] (dense, both of `dtype`: fp32, rounded to bf16, or bf16) into a slot, replacing
- *    what was there; rank 0 empties the slot (A and B are not read).  Stream order decides which calls see which adapter.  */
+ *    what was there; rank 0 empties the slot (A and B are not read).  Stream order decides which calls see which adapter.  Factors
+ *    are finite in bf16: an infinite one gives NaN also where the product would be infinite.  */
 typedef struct {
   void* data;
   int K, N, max_rank, n_slots;

@@ -169,6 +169,30 @@ def test_in_place_and_given_outputs():
         c.check(Y)
 
 
+@pytest.mark.parametrize("M", [3, 40, 1100])
+def test_activations_of_another_format(M):
+    # six bits, a window that saturates large blocks and drops small ones: the values are those that the layer would take
+    cfg = L.default_config()
+    cfg.a_bits, cfg.exp_min, cfg.exp_max = 6, -3, 1
+    c = Case(M, 528, 264, [16, 40], [j % 3 - 1 for j in range(M)])
+    X = _randn((M, 528), 31) * torch.exp2(torch.arange(33, device=DEV) % 9 - 6.0).repeat_interleave(16)
+    Xq = L.to_mxint8(*L.quantize_activations(X, cfg=cfg))
+    c.X64, c.kinds = L.dequantize_activations(Xq, M, 528, cfg=cfg).double(), ("mxint8", "f32", "f32")
+    plan = L.adapter_plan(c.slots, c.pool)
+    c.check(L.apply_adapters(Xq, c.pool, plan, c.Y0, cfg=cfg))
+
+
+@pytest.mark.parametrize("x,y", [("f32", "f32"), ("bf16", "bf16"), ("mxint8", "f32")])
+def test_few_rows_of_tensors_aligned_to_16_bytes_only(x, y):
+    def shifted(t):
+        n = 16 // t.element_size()
+        return torch.empty(t.numel() + 2 * n, dtype=t.dtype, device=DEV)[n:n + t.numel()].view(t.shape).copy_(t)
+    c = Case(21, 528, 264, [16, 40], [j % 3 - 1 for j in range(21)], x=x, y0=y, y=y)
+    Y = c.run()
+    X, Y0, Z = shifted(c.X), shifted(c.Y0), shifted(c.Y0)
+    assert X.data_ptr() % 32 == 16 and torch.equal(L.apply_adapters(X, c.pool, c.plan, Y0, Y=Z), Y)
+
+
 def test_fp32_factors_are_rounded_to_bf16_and_slots_are_replaced():
     c = Case(5, 256, 256, [16, 8], [0, 1, 0, 1, 0], load=torch.float32)
     c.check(c.run())
