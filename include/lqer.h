@@ -368,6 +368,73 @@ lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lq
                             const void* Y0, lqer_dtype_t y0_dtype, void* Y, lqer_dtype_t y_dtype, const lqer_config_t* cfg, void* workspace,
                             size_t workspace_bytes, void* stream);
 
+/* ---- Keys and values of past tokens ----
+ * What stands between a block's query, key and value projections and its output projection in serving: a paged cache of keys and values, its tables
+ * from step to step, and the attention of new tokens over it.  As above, all calls are asynchronous on `stream` and allocate nothing.
+ *
+ * A cache holds n_pages pages of `page` tokens (16, 32, 64 or 128) of one layer: keys and values are [n_pages, kv_heads, page, head_dim] each
+ * (head_dim 64 or 128; n_pages * page < 2^31), bf16, or MXINT8 in the format of cfg (the mantissas in that order, then an exponent byte for every
+ * 16 of them along head_dim).  lqer_kv_cache_bytes: the size of either.  Its memory may hold anything where no token was put. */
+typedef struct {
+  void* keys;
+  void* values;
+  int n_pages, page, kv_heads, head_dim;   /* kv_heads at most 1024 */
+  lqer_dtype_t dtype;                      /* LQER_BF16 or LQER_MXINT8 */
+} lqer_kv_cache_t;
+lqer_status_t lqer_kv_cache_bytes(const lqer_kv_cache_t* cache, size_t* bytes);
+
+/* Tables of up to 16384 requests that share the pages (of all layers' caches alike): row r of `tables` lists the pages of request r in the order of
+ * its tokens; only the first ceil(tokens / page) entries mean anything.  free_pages is a ring of n_pages entries: the free ones are the
+ * entries ring[0] .. ring[1] - 1 (both count up, entry i stands at i mod n_pages). */
+typedef struct {
+  int* tables;       /* [n_requests, max_pages]; n_requests * max_pages < 2^31, max_pages * page <= 2^30 */
+  int* free_pages;   /* [n_pages] */
+  int n_requests, max_pages, n_pages, page;
+} lqer_page_table_t;
+/* One step of the batch.  Request r holds lengths[r] tokens and takes added[r] more (0: none; below 0: it loses its last -added[r], or all that it has;
+ * drafts that were refused, a request that has ended).  The pages that get free join the ring's end, those that are needed come from its
+ * front (what has just come back included), in the order of the requests and of their tokens.
+ *  - lengths_out [n_requests] and ring_out [2] get what holds after the step; they may be lengths and ring themselves (as a captured graph that
+ *    steps wants it).  Otherwise the step may be taken again: tables and free_pages, changed in place, then get the same entries.
+ *  - The rows of the step's tensors [M, ..] belong to the requests in order, max(added[r], 0) each; slots and positions [M] get every
+ *    row's slot (page * tokens a page + place in the page; what lqer_append_kv takes) and the token's place in its request (what a
+ *    rotary embedding takes), and -1 for rows behind the last.
+ *  - step (lqer_cache_step_bytes, 256-byte aligned) gets the plan that lqer_paged_attention reads.  max_added: what no added[r] exceeds.
+ *  - What only the device can see is reported in step (lqer_poll_status): LQER_ERR_BUFFER_TOO_SMALL where too few pages are free, from the
+ *    first request that finds too few on for all that need any; LQER_ERR_BOUNDS for a request whose length is out of the tables' range before or
+ *    after, that takes more than max_added, or whose rows do not fit M, for a ring that cannot be (every request that needs or
+ *    frees pages is refused then), and for a table entry that is no page (such a token has slot -1).  A refused request stays as it was: its length and pages, its rows
+ *    with slot -1; the others take their step. */
+lqer_status_t lqer_cache_step_bytes(int n_requests, size_t* bytes);
+lqer_status_t lqer_cache_step(const lqer_page_table_t* table, const int* lengths, const int* added, const long long* ring, int M, int max_added,
+                              int* lengths_out, long long* ring_out, int* slots, int* positions, void* step, size_t step_bytes, void* stream);
+
+/* Puts rows of keys and values into their slots: K and V have M rows of kv_heads * head_dim elements of x_dtype (fp32 or bf16), k_stride and v_stride
+ * elements from one row to the next (multiples of 8: both may be parts of one projection's rows).  A bf16 cache gets them rounded to nearest
+ * even, an MXINT8 cache quantised as lqer_quantize_activations would, in the format of cfg.  A row whose slot is -1, or none of the cache, is left out;
+ * the slots of a call are different. */
+lqer_status_t lqer_append_kv(const void* K, const void* V, lqer_dtype_t x_dtype, long long k_stride, long long v_stride, int M, const int* slots,
+                             const lqer_kv_cache_t* cache, const lqer_config_t* cfg, void* stream);
+
+/* Causal attention of a step's new tokens over the cache, in which their own keys and values are already:
+ *   Y[m, h] = sum_j softmax_j(scale Q[m, h] . K[j, h / g]) V[j, h / g],   g = q_heads / kv_heads,
+ * over the tokens j of row m's request up to its own position p, and with window > 0 only those with j > p - window or j < sinks.
+ *  - Q: M rows of q_heads * head_dim bf16 elements, q_stride elements from row to row (a multiple of 8); Y [M, q_heads, head_dim] bf16, dense, apart
+ *    from everything else.  q_heads is a multiple of kv_heads, at most 1024.
+ *  - step: made by lqer_cache_step for the same M and a table of these sizes; max_added: at least the step's (kernels are chosen
+ *    by it).  The plan is only read, but for its status: one of another batch or table (or none) is reported there as LQER_ERR_BAD_PACKED and
+ *    nothing is written; a table entry that is no page as LQER_ERR_BOUNDS (the rows of that request then hold anything).  Rows behind the last token
+ *    and those of refused requests are left as they are.
+ *  - Scores, their maxima and all sums are fp32; the weights of the values are rounded to bf16.  What a row does not see may hold anything where no
+ *    row of the step sees it; an infinite or NaN value that some rows of a request see and others do not may reach those, too.
+ *  - workspace: lqer_attention_workspace_bytes, 256-byte aligned; nothing in it has to be kept or cleared, and calls that overlap need one each.
+ *    Sums are taken in an order that depends on the whole batch's lengths, so a row's last bits may; for one batch they are always the same. */
+lqer_status_t lqer_attention_workspace_bytes(int M, int q_heads, const lqer_kv_cache_t* cache, const lqer_page_table_t* table, int max_added,
+                                             size_t* bytes);
+lqer_status_t lqer_paged_attention(const void* Q, long long q_stride, int M, int q_heads, const lqer_kv_cache_t* cache, const lqer_page_table_t* table,
+                                   void* step, int max_added, int window, int sinks, double scale, const lqer_config_t* cfg, void* Y, void* workspace,
+                                   size_t workspace_bytes, void* stream);
+
 /* Force a kernel path for tests: 0 auto (which alone runs the cluster kernel for 3 to 16 rows), 1 plain CUDA-core
  * reference kernel, 2 small-batch kernels
  * (column-owner kernel for M <= 4, small prologue + small-batch GEMM for M <= 128), 3 tensor-core GEMM behind the

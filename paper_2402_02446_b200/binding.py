@@ -52,6 +52,16 @@ class _Pool(C.Structure):
     _fields_ = [("data", C.c_void_p), ("K", C.c_int), ("N", C.c_int), ("max_rank", C.c_int), ("n_slots", C.c_int)]
 
 
+class _Cache(C.Structure):
+    _fields_ = [("keys", C.c_void_p), ("values", C.c_void_p), ("n_pages", C.c_int), ("page", C.c_int), ("kv_heads", C.c_int), ("head_dim", C.c_int),
+                ("dtype", C.c_int)]
+
+
+class _Table(C.Structure):
+    _fields_ = [("tables", C.c_void_p), ("free_pages", C.c_void_p), ("n_requests", C.c_int), ("max_pages", C.c_int), ("n_pages", C.c_int),
+                ("page", C.c_int)]
+
+
 def lib_path() -> str:
     return _LIB_PATH
 
@@ -108,6 +118,12 @@ def lib() -> C.CDLL:
             "lqer_adapter_plan": (i, [vp, i, i, vp, sz, vp]),
             "lqer_adapters_workspace_bytes": (i, [i, C.POINTER(_Pool), i, C.POINTER(sz)]),
             "lqer_adapters": (i, [vp, i, i, C.POINTER(_Pool), vp, i, vp, i, vp, i, cfgp, vp, sz, vp]),
+            "lqer_kv_cache_bytes": (i, [C.POINTER(_Cache), C.POINTER(sz)]),
+            "lqer_cache_step_bytes": (i, [i, C.POINTER(sz)]),
+            "lqer_cache_step": (i, [C.POINTER(_Table), vp, vp, vp, i, i, vp, vp, vp, vp, vp, sz, vp]),
+            "lqer_append_kv": (i, [vp, vp, i, C.c_longlong, C.c_longlong, i, vp, C.POINTER(_Cache), cfgp, vp]),
+            "lqer_attention_workspace_bytes": (i, [i, i, C.POINTER(_Cache), C.POINTER(_Table), i, C.POINTER(sz)]),
+            "lqer_paged_attention": (i, [vp, C.c_longlong, i, i, C.POINTER(_Cache), C.POINTER(_Table), vp, i, i, i, C.c_double, cfgp, vp, vp, sz, vp]),
             "lqer_workspace_init": (i, [vp, sz, vp]),
             "lqer_poll_status": (i, [vp, vp, C.POINTER(i)]),
             "lqer_set_path": (i, [i]),
@@ -685,6 +701,174 @@ def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: to
                                  None if ws is None else _ptr(ws, index), 0 if ws is None else ws.numel() * ws.element_size(), _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_adapters")
+    return Y
+
+
+# ---- keys and values of past tokens ----------------------------------------------------------------------------------------
+
+class KVCache:
+    """Pages of one layer's keys and values (see include/lqer.h).  bf16: keys and values are tensors [n_pages, kv_heads, page, head_dim]; MXINT8:
+    flat uint8 tensors, the mantissas in that order, then the exponent bytes (mxint8_bytes(n_pages * kv_heads * page, head_dim))."""
+
+    def __init__(self, n_pages: int, page: int, kv_heads: int, head_dim: int, dtype, device):
+        code = _OUT_CODE.get(dtype)
+        if code not in (1, 2):
+            raise ValueError("a cache holds torch.bfloat16 or MXINT8")
+        self.n_pages, self.page, self.kv_heads, self.head_dim = n_pages, page, kv_heads, head_dim
+        self.dtype = MXINT8 if code == 2 else torch.bfloat16
+        self.handle = _Cache(None, None, n_pages, page, kv_heads, head_dim, code)
+        self.ref = C.byref(self.handle)
+        size = C.c_size_t()
+        _check(lib().lqer_kv_cache_bytes(self.ref, C.byref(size)), "lqer_kv_cache_bytes")
+        if code == 2:
+            self.keys, self.values = (torch.zeros(size.value, dtype=torch.uint8, device=device) for _ in range(2))
+        else:
+            self.keys, self.values = (torch.zeros((n_pages, kv_heads, page, head_dim), dtype=torch.bfloat16, device=device) for _ in range(2))
+        self.index = self.keys.get_device()
+        self.handle.keys, self.handle.values = self.keys.data_ptr(), self.values.data_ptr()
+
+
+def new_kv_cache(n_pages: int, page: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda", stream=None) -> KVCache:
+    """A cache of zeros: n_pages pages of `page` tokens (16, 32, 64 or 128), head_dim 64 or 128, torch.bfloat16 or MXINT8."""
+    if stream is not None:
+        with _on(stream, stream.device.index if torch.device(device).index is None else torch.device(device).index):
+            return KVCache(n_pages, page, kv_heads, head_dim, dtype, stream.device)
+    return KVCache(n_pages, page, kv_heads, head_dim, dtype, device)
+
+
+class PageTable:
+    """Which pages the requests of a batch hold, for the caches of all layers: tables int32 [n_requests, max_pages], lengths int32 [n_requests] (the
+    tokens that each holds), free int32 [n_pages] and ring int64 [2] (the free pages are entries ring[0] .. ring[1] - 1, modulo n_pages)."""
+
+    def __init__(self, n_requests: int, max_pages: int, n_pages: int, page: int, device):
+        self.n_requests, self.max_pages, self.n_pages, self.page = n_requests, max_pages, n_pages, page
+        size = C.c_size_t()
+        _check(lib().lqer_cache_step_bytes(n_requests, C.byref(size)), "lqer_cache_step_bytes")
+        self.step_bytes = size.value
+        self.tables = torch.full((n_requests, max_pages), -1, dtype=torch.int32, device=device)
+        self.free = torch.arange(n_pages, dtype=torch.int32, device=device)
+        self.lengths = torch.zeros(n_requests, dtype=torch.int32, device=device)
+        self.ring = torch.tensor([0, n_pages], dtype=torch.int64, device=device)
+        self.index = self.tables.get_device()
+        self.handle = _Table(self.tables.data_ptr(), self.free.data_ptr(), n_requests, max_pages, n_pages, page)
+        self.ref = C.byref(self.handle)
+
+
+def new_page_table(n_requests: int, max_pages: int, n_pages: int, page: int, device="cuda", stream=None) -> PageTable:
+    """The tables of n_requests empty requests of up to max_pages pages, with all n_pages pages free."""
+    if stream is not None:
+        with _on(stream, stream.device.index if torch.device(device).index is None else torch.device(device).index):
+            return PageTable(n_requests, max_pages, n_pages, page, stream.device)
+    return PageTable(n_requests, max_pages, n_pages, page, device)
+
+
+class CacheStep:
+    """A step of a batch: slots and positions int32 [M] of its rows (-1 behind the last), lengths [n_requests] and ring [2] as they are after it, and the
+    plan for paged_attention in buf (poll_status(buf) tells of requests that were refused)."""
+
+    def __init__(self, pages: PageTable, M: int, max_added: int):
+        new = pages.tables.new_empty
+        self.M, self.max_added, self.n_requests, self.index = M, max_added, pages.n_requests, pages.index
+        self.buf = new(pages.step_bytes, dtype=torch.uint8)
+        self.slots, self.positions = new(M), new(M)
+        self.lengths, self.ring = new(pages.n_requests), new(2, dtype=torch.int64)
+        self.own_lengths, self.own_ring = self.lengths, self.ring
+
+
+def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | None = None, step: CacheStep | None = None, commit: bool = True,
+               stream=None) -> CacheStep:
+    """Takes the batch one step further: request r takes added[r] tokens (int32 [n_requests]), or loses -added[r]; pages are given out and taken back.
+    M: rows of the step's tensors, those of the requests in order and any padding behind them.  max_added: what no added[r] exceeds (M if not given); 1 tells
+    that this is a decoding step.  step: one of the same sizes to be made again in place.  commit: pages.lengths and pages.ring step on too (in place);
+    otherwise they stay, and the step's own hold what would be."""
+    index = added.get_device()
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return cache_step(pages, added, M, max_added, step, commit)
+    if added.dtype != torch.int32 or added.shape != (pages.n_requests,):
+        raise ValueError("expected added int32 [n_requests]")
+    if pages.index != index:
+        raise ValueError("expected the page table on the device of added")
+    max_added = M if max_added is None else max_added
+    if step is None:
+        if M < 1:
+            raise ValueError("a step has at least one row")
+        step = CacheStep(pages, M, max_added)
+    elif step.M != M or step.n_requests != pages.n_requests or step.index != index:
+        raise ValueError("the step to be made again has other sizes")
+    lengths, ring = (pages.lengths, pages.ring) if commit else (step.own_lengths, step.own_ring)
+    status = lib().lqer_cache_step(pages.ref, pages.lengths.data_ptr(), _ptr(added, index), pages.ring.data_ptr(), M, max_added, lengths.data_ptr(),
+                                   ring.data_ptr(), step.slots.data_ptr(), step.positions.data_ptr(), step.buf.data_ptr(), step.buf.numel(),
+                                   _raw_stream(index))
+    if status:
+        raise LqerError(status, "lqer_cache_step")
+    step.max_added, step.lengths, step.ring = max_added, lengths, ring
+    return step
+
+
+def _head_rows(t: torch.Tensor, heads: int, dim: int, index: int):
+    """Row stride and address of [M, heads, dim] or [M, heads * dim] on that device, the rows dense and any distance apart."""
+    shape, stride = t.shape, t.stride()
+    if shape[1:] != (heads, dim) and shape[1:] != (heads * dim,) or t.get_device() != index:
+        raise ValueError(f"expected [M, {heads}, {dim}] or [M, {heads * dim}] on the device of the others")
+    if stride[-1] != 1 or len(shape) == 3 and heads > 1 and stride[1] != dim:
+        raise ValueError("expected rows of consecutive elements")
+    return (stride[0] if shape[0] > 1 else heads * dim), t.data_ptr()
+
+
+def append_kv(K: torch.Tensor, V: torch.Tensor, cache: KVCache, slots: torch.Tensor, cfg: Config | None = None, stream=None) -> None:
+    """Puts keys and values [M, kv_heads, head_dim] (or [M, kv_heads * head_dim]; fp32 or bf16, any row stride, as parts of a joint projection have)
+    into their slots (int32 [M], of a step): rounded to bf16, or quantised to MXINT8 in the format of cfg."""
+    index = K.get_device()
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return append_kv(K, V, cache, slots, cfg)
+    M = K.shape[0]
+    if V.shape[0] != M or V.dtype != K.dtype or slots.dtype != torch.int32 or slots.shape != (M,) or cache.index != index:
+        raise ValueError("expected K and V of M rows and one type, slots int32 [M], and the cache on their device")
+    k_stride, k_ptr = _head_rows(K, cache.kv_heads, cache.head_dim, index)
+    v_stride, v_ptr = _head_rows(V, cache.kv_heads, cache.head_dim, index)
+    status = lib().lqer_append_kv(k_ptr, v_ptr, _code(_REAL_CODE, K.dtype), k_stride, v_stride, M, _ptr(slots, index), cache.ref,
+                                  None if cfg is None else C.byref(cfg), _raw_stream(index))
+    if status:
+        raise LqerError(status, "lqer_append_kv")
+
+
+def attention_workspace_bytes(M: int, q_heads: int, cache: KVCache, pages: PageTable, max_added: int) -> int:
+    """The workspace that paged_attention needs for steps of M rows with up to max_added tokens a request."""
+    out = C.c_size_t()
+    _check(lib().lqer_attention_workspace_bytes(M, q_heads, cache.ref, pages.ref, max_added, C.byref(out)), "lqer_attention_workspace_bytes")
+    return out.value
+
+
+def paged_attention(Q: torch.Tensor, cache: KVCache, pages: PageTable, step: CacheStep, window: int = 0, sinks: int = 0, scale: float | None = None,
+                    cfg: Config | None = None, Y: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
+    """Causal attention of a step's new tokens over the cache, their own keys and values included: bf16 [M, q_heads, head_dim].  Q [M, q_heads, head_dim]
+    bf16, any row stride.  window: a token sees only the last `window` tokens (itself among them) and the first `sinks`; 0: all.  scale: of the scores,
+    head_dim ** -0.5 if not given.  Rows behind the last token are left as they are in Y (undefined where none is given).  ws: a workspace of
+    attention_workspace_bytes, made where none is given."""
+    index = Q.get_device()
+    if stream is not None or not _here(index):
+        with _on(stream, index):
+            return paged_attention(Q, cache, pages, step, window, sinks, scale, cfg, Y, ws)
+    shape, D = Q.shape, cache.head_dim
+    if Q.dtype != torch.bfloat16 or len(shape) != 3 or shape[0] != step.M or shape[2] != D:
+        raise ValueError("expected Q bf16 [rows of the step, q_heads, head_dim]")
+    if cache.index != index or pages.index != index or step.index != index:
+        raise ValueError("expected cache, page table and step on the device of Q")
+    M, heads = shape[0], shape[1]
+    q_stride, q_ptr = _head_rows(Q, heads, D, index)
+    if Y is None:
+        Y = Q.new_empty(shape)
+    elif Y.shape != shape or Y.dtype != torch.bfloat16:
+        raise ValueError("expected Y bf16 [M, q_heads, head_dim]")
+    if ws is None:
+        ws = Q.new_empty(attention_workspace_bytes(M, heads, cache, pages, step.max_added), dtype=torch.uint8)
+    status = lib().lqer_paged_attention(q_ptr, q_stride, M, heads, cache.ref, pages.ref, step.buf.data_ptr(), step.max_added, window, sinks,
+                                        D ** -0.5 if scale is None else scale, None if cfg is None else C.byref(cfg), _ptr(Y, index), _ptr(ws, index),
+                                        ws.numel() * ws.element_size(), _raw_stream(index))
+    if status:
+        raise LqerError(status, "lqer_paged_attention")
     return Y
 
 

@@ -1,0 +1,505 @@
+// Attention of a few new tokens of each request over the paged cache, split over its length and joined.
+//
+// Row i of head h of a request sees key j <= position, and under a window only the last `window` of them and the first `sinks`:
+//   y = sum_j p_j v_j / sum_j p_j,  p_j = exp2(s_j - m),  s_j = scale log2(e) q . k_j,  m = the largest s_j so far.
+// (m, sum p, sum p v) of two sets of keys join to that of their union: with M = max(m1, m2), each side counts 2^(m_i - M).
+//
+// The rows of the query heads that share a key head, of all of a request's new tokens, go together (a row tile of 8 NT): the keys
+// and values are read once for them.  Bound: those bytes.  The products are far from any limit, so they are mma.sync m16n8k16 with the keys (and
+// the values' columns) on the 16-row side and the row tile on the 8-column side, which wastes least of it, and the operands come straight
+// from memory to registers: within a dot product the order of the elements is free, so a lane takes 16 consecutive bytes of a key, and
+// of four keys' values, and both sides use the order that this gives.  No shared memory, no barrier between the keys.
+//
+// Work is counted in chunks of 64 keys of a (request, key head, row tile), all in one row; each CTA takes an equal run of them, wherever that begins
+// and ends, so lengths may differ as they like.  The four warps take 16 keys of every chunk and join at the end of a run's part; what is not a
+// whole row's part goes to the workspace, and a second kernel joins those parts, in the order of the keys.
+#include "lqer_cache.cuh"
+
+namespace lqer {
+namespace kv {
+
+constexpr int kChunk = 64, kWarps = 4, kSplitThreads = 32 * kWarps;
+constexpr int kMinChunks = 2;                // of a CTA's run
+
+// What a CTA leaves for the join: the (request, key head, row tile) that begins in its run and goes on behind it, if any.
+struct Span { int request, head, tile, parts; };
+struct Split {
+  Attention a;
+  Span* spans;                               // [CTAs]
+  float* parts;                              // [CTAs][2][8 NT][D + 2]: part 0 continues a row, part 1 begins one; sums, then m and l
+  int few;                                   // requests of more rows than this are left alone
+  size_t y_extent;
+};
+
+struct Visible { int sink_chunks, first_chunk, chunks; };     // chunks [0, sink_chunks) and [first_chunk, ..), as many as chunks together
+__device__ __forceinline__ Visible visible(const Attention& p, int n, int len) {
+  Visible v = {0, 0, (len + kChunk - 1) / kChunk};
+  if (p.window > 0) {
+    v.first_chunk = max(0, len - n - p.window + 1) / kChunk;
+    v.sink_chunks = min((min(p.sinks, len) + kChunk - 1) / kChunk, v.first_chunk);
+    v.chunks += v.sink_chunks - v.first_chunk;
+  }
+  return v;
+}
+__device__ __forceinline__ int row_tiles(const Attention& p, int n, int few, int per) {
+  const long long rows = (long long)n * p.group;
+  return n > 0 && rows <= few ? (int)((rows + per - 1) / per) : 0;
+}
+// Where a CTA's run lies: chunks of all requests, chunks a CTA, the request in which the run begins and the chunks before that request.
+struct Run { long long total, per, before; int request; };
+__device__ __forceinline__ Run find_run(const Split& s, int per_tile, Run* shared) {
+  const Attention& p = s.a;
+  const StepRequest* reqs = requests_of(p.step);
+  __shared__ long long sums[kWarps];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  const int q = (p.R + kSplitThreads - 1) / kSplitThreads, from = min(tid * q, p.R), to = min(from + q, p.R);
+  auto chunks_of = [&](int r) {
+    const int4 w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+    const int t = row_tiles(p, w.y, s.few, per_tile);
+    return t == 0 ? 0LL : (long long)t * p.hkv * visible(p, w.y, w.z).chunks;
+  };
+  long long mine = 0;
+  for (int r = from; r < to; ++r) mine += chunks_of(r);
+  long long x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const long long y = __shfl_up_sync(0xFFFFFFFFu, x, o); if (lane >= o) x += y; }
+  if (lane == 31) sums[warp] = x;
+  __syncthreads();
+  long long before = 0, total = 0;
+#pragma unroll
+  for (int w = 0; w < kWarps; ++w) { if (w < warp) before += sums[w]; total += sums[w]; }
+  before += x - mine;
+  const long long per = max((total + gridDim.x - 1) / gridDim.x, (long long)kMinChunks), u0 = per * blockIdx.x;
+  if (tid == 0) *shared = Run{total, per, 0, -1};
+  __syncthreads();
+  if (u0 >= before && u0 < before + mine) {          // one thread
+    int r = from;
+    for (;; ++r) {
+      const long long c = chunks_of(r);
+      if (u0 < before + c) break;
+      before += c;
+    }
+    shared->request = r;
+    shared->before = before;
+  }
+  __syncthreads();
+  return *shared;
+}
+
+__device__ __forceinline__ void mma(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+  asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+               : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3]) : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ uint32_t transposed(uint32_t w) {
+  uint32_t d;
+  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(w));
+  return d;
+}
+__device__ __forceinline__ uint4 once16(const void* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint2 once8(const void* p) {
+  uint2 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
+  return v;
+}
+__device__ __forceinline__ uint32_t byte_of(uint2 w, int i) { return ((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xFFu; }
+
+// Eight elements of a key or of a value: bf16, or mantissas until they are used.
+template <bool MX> struct Oct { uint4 w; };
+template <> struct Oct<true> { uint2 w; };
+// A warp's 16 keys: of key lane / 4 (+ 8) the octets at 8 (lane % 4) + 32 j.
+template <int D, bool MX>
+struct Keys {
+  Oct<MX> k[2][D / 32];
+  uint2 e[MX ? 2 : 1];         // the keys' exponent bytes
+  __device__ __forceinline__ void load(const Attention& p, size_t row, int lane) {      // row: of the first key, in a [.., D] tensor
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const size_t at = (row + lane / 4 + 8 * i) * D + 8 * (lane & 3);
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        if constexpr (MX) k[i][j].w = once8(static_cast<const uint8_t*>(p.keys) + at + 32 * j);
+        else k[i][j].w = once16(static_cast<const uint16_t*>(p.keys) + at + 32 * j);
+      }
+      if constexpr (MX) {
+        const uint8_t* x = p.key_exps + (row + lane / 4 + 8 * i) * (D / 16);
+        if (D == 128) e[i] = __ldg(reinterpret_cast<const uint2*>(x));
+        else e[i] = make_uint2(__ldg(reinterpret_cast<const uint32_t*>(x)), 0u);
+      }
+    }
+  }
+  __device__ __forceinline__ uint4 octet(const Attention& p, int i, int j, int lane) const {
+    if constexpr (MX) return mantissas8(k[i][j].w, mantissa_scale(byte_of(e[i], 2 * j + ((lane & 3) >> 1)), p.emin + 127, p.emax + 127, p.bits - 2));
+    else return k[i][j].w;
+  }
+};
+// Of keys 2 (lane % 4) + {0, 1, 8, 9} the values of columns 8 (lane / 4) .. + 7, and of those 64 further on.
+template <int D, bool MX>
+struct Values {
+  static constexpr int H = D / 64;
+  Oct<MX> v[4][H];
+  uint2 e[MX ? 4 : 1];
+  __device__ __forceinline__ void load(const Attention& p, size_t row, int lane) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const size_t key = row + 2 * (lane & 3) + (i & 1) + 8 * (i >> 1), at = key * D + 8 * (lane >> 2);
+#pragma unroll
+      for (int h = 0; h < H; ++h) {
+        if constexpr (MX) v[i][h].w = once8(static_cast<const uint8_t*>(p.values) + at + 64 * h);
+        else v[i][h].w = once16(static_cast<const uint16_t*>(p.values) + at + 64 * h);
+      }
+      if constexpr (MX) {
+        const uint8_t* x = p.value_exps + key * (D / 16);
+        if (D == 128) e[i] = __ldg(reinterpret_cast<const uint2*>(x));
+        else e[i] = make_uint2(__ldg(reinterpret_cast<const uint32_t*>(x)), 0u);
+      }
+    }
+  }
+  __device__ __forceinline__ void clear(int i) {
+#pragma unroll
+    for (int h = 0; h < H; ++h) {
+      if constexpr (MX) v[i][h].w = make_uint2(0u, 0u);
+      else v[i][h].w = make_uint4(0u, 0u, 0u, 0u);
+    }
+  }
+  __device__ __forceinline__ uint4 octet(const Attention& p, int i, int h, int lane) const {
+    if constexpr (MX) return mantissas8(v[i][h].w, mantissa_scale(byte_of(e[i], 4 * h + (lane >> 3)), p.emin + 127, p.emax + 127, p.bits - 2));
+    else return v[i][h].w;
+  }
+};
+__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+
+template <int D, bool MX, int NT>
+__global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(const Split s) {
+  constexpr int ROWS = 8 * NT, T = D / 16;               // T: tiles of 16 columns of the output
+  __shared__ float sm_o[kWarps][ROWS][D + 4];
+  __shared__ float sm_m[kWarps][ROWS], sm_l[kWarps][ROWS];
+  __shared__ Run sm_run;
+  const Attention& p = s.a;
+  tc::pdl_launch_dependents();
+  tc::pdl_wait();
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
+  if (tid == 0) s.spans[blockIdx.x] = Span{0, 0, 0, 0};
+  if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
+  const Run run = find_run(s, ROWS, &sm_run);
+  long long u = run.per * blockIdx.x;
+  const long long end = min(u + run.per, run.total);
+  if (u >= end) return;
+  const StepRequest* reqs = requests_of(p.step);
+  int r = run.request;
+  long long before = run.before;
+  while (u < end) {
+    const int4 req = __ldg(reinterpret_cast<const int4*>(reqs + r));
+    const int row0 = req.x, n = req.y, len = req.z;
+    const int tiles = row_tiles(p, n, s.few, ROWS);
+    const Visible vis = visible(p, n, len);
+    const long long mine = tiles == 0 ? 0 : (long long)tiles * p.hkv * vis.chunks;
+    if (u >= before + mine) { before += mine; ++r; continue; }
+    const long long local = u - before, which = local / vis.chunks;
+    const int h = (int)(which / tiles), tile = (int)(which % tiles), c0 = (int)(local - which * vis.chunks);
+    const int c1 = (int)min((long long)vis.chunks, c0 + (end - u));
+    const int rows = min(ROWS, n * p.group - tile * ROWS), first_pos = len - n;
+    // the row tile's queries, in the order in which a lane holds a key
+    uint4 q[NT][D / 32];
+    int pos[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+      const int x = tile * ROWS + 8 * t + g;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        q[t][j] = make_uint4(0u, 0u, 0u, 0u);
+        if (8 * t + g < rows)
+          q[t][j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + (size_t)(row0 + x / p.group) * p.q_stride +
+                                                         (size_t)(h * p.group + x % p.group) * D + 8 * c + 32 * j));
+      }
+#pragma unroll
+      for (int i = 0; i < 2; ++i) pos[t][i] = first_pos + (tile * ROWS + 8 * t + 2 * c + i) / p.group;
+    }
+    const int last_pos = len - 1, seen_from = p.window > 0 ? max(0, first_pos - p.window + 1) : 0;
+    float o[NT][T][4], m[NT][2], l[NT][2];
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int i = 0; i < T; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
+      m[t][0] = m[t][1] = -INFINITY;
+      l[t][0] = l[t][1] = 0.f;
+    }
+    // chunk of the run -> first of the warp's keys
+    auto key_of = [&](int chunk) { return ((chunk < vis.sink_chunks ? chunk : vis.first_chunk + chunk - vis.sink_chunks)) * kChunk + warp * 16; };
+    const int* table = p.tables + (size_t)r * p.max_pages;
+    auto entry_of = [&](int chunk) {
+      const int key = key_of(chunk);
+      return chunk < c1 && key < len ? __ldg(table + (key >> p.page_shift)) : 0;
+    };
+    auto row_of = [&](int chunk, int entry) {
+      const int key = key_of(chunk);
+      return (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (key & (p.page - 1));
+    };
+    Keys<D, MX> K;
+    Values<D, MX> V;
+    int entry = entry_of(c0), next_entry = entry_of(c0 + 1);
+    if (key_of(c0) < len) {
+      const size_t at = row_of(c0, entry);
+      K.load(p, at, lane);
+      V.load(p, at, lane);
+    }
+    for (int chunk = c0; chunk < c1; ++chunk) {
+      const int key0 = key_of(chunk);
+      if (key0 >= len) break;                           // the last chunk's end
+      float sc[NT][4];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+#pragma unroll
+      for (int j = 0; j < D / 32; ++j) {
+        const uint4 a = K.octet(p, 0, j, lane), b = K.octet(p, 1, j, lane);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) {
+          mma(sc[t], a.x, b.x, a.y, b.y, q[t][j].x, q[t][j].y);
+          mma(sc[t], a.z, b.z, a.w, b.w, q[t][j].z, q[t][j].w);
+        }
+      }
+      const bool more = chunk + 1 < c1 && key_of(chunk + 1) < len;
+      size_t next_at = 0;
+      if (more) {
+        next_at = row_of(chunk + 1, next_entry);
+        K.load(p, next_at, lane);
+        next_entry = entry_of(chunk + 2);
+      }
+      const bool masked = key0 + 15 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) sc[t][i] *= p.scale_log2;
+        if (masked) {
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            const int key = key0 + g + 8 * (i >> 1), at = pos[t][i & 1];
+            if (key > at || (p.window > 0 && key <= at - p.window && key >= p.sinks)) sc[t][i] = -INFINITY;
+          }
+        }
+      }
+      if (masked) {
+        // values that no row sees may be anything: 0 times that has to be 0
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const int key = key0 + 2 * c + (i & 1) + 8 * (i >> 1);
+          if (key >= len || (key < seen_from && key >= p.sinks)) V.clear(i);
+        }
+      }
+      uint32_t pb[NT][2];
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+        float big[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          big[i] = fmaxf(sc[t][i], sc[t][i + 2]);
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) big[i] = fmaxf(big[i], __shfl_xor_sync(0xFFFFFFFFu, big[i], x));
+        }
+        if (__any_sync(0xFFFFFFFFu, big[0] > m[t][0] || big[1] > m[t][1])) {
+          float f[2];
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float to = fmaxf(m[t][i], big[i]);
+            f[i] = m[t][i] == to ? 1.f : exp2_fast(m[t][i] - to);
+            m[t][i] = to;
+            l[t][i] *= f[i];
+          }
+#pragma unroll
+          for (int i = 0; i < T; ++i) {
+            o[t][i][0] *= f[0]; o[t][i][1] *= f[1];
+            o[t][i][2] *= f[0]; o[t][i][3] *= f[1];
+          }
+        }
+        const float base[2] = {m[t][0] == -INFINITY ? 0.f : m[t][0], m[t][1] == -INFINITY ? 0.f : m[t][1]};
+        float e[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) e[i] = exp2_fast(sc[t][i] - base[i & 1]);
+        l[t][0] += e[0] + e[2];
+        l[t][1] += e[1] + e[3];
+        // the weights enter the product rounded to bf16, 2^-9 either way, as the values do that they weigh; their sum does not
+        pb[t][0] = transposed(round_bf16x2(e[0], e[1]));
+        pb[t][1] = transposed(round_bf16x2(e[2], e[3]));
+      }
+      uint4 v[4][D / 64];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int k = 0; k < D / 64; ++k) v[i][k] = V.octet(p, i, k, lane);
+#pragma unroll
+      for (int i = 0; i < T; ++i) {
+        // column i (of eight) of both halves; heads of 64: i and i + 4
+        constexpr int H = D / 64 - 1;
+        const int lo = i, hi = D == 128 ? i : i + 4;
+        const uint32_t pick_lo = lo & 1 ? 0x7632 : 0x5410, pick_hi = hi & 1 ? 0x7632 : 0x5410;
+        const uint32_t a0 = __byte_perm(word_of(v[0][0], lo / 2), word_of(v[1][0], lo / 2), pick_lo);
+        const uint32_t a1 = __byte_perm(word_of(v[0][H], hi / 2), word_of(v[1][H], hi / 2), pick_hi);
+        const uint32_t a2 = __byte_perm(word_of(v[2][0], lo / 2), word_of(v[3][0], lo / 2), pick_lo);
+        const uint32_t a3 = __byte_perm(word_of(v[2][H], hi / 2), word_of(v[3][H], hi / 2), pick_hi);
+#pragma unroll
+        for (int t = 0; t < NT; ++t) mma(o[t][i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
+      }
+      if (more) V.load(p, next_at, lane);
+    }
+    // the four warps' parts
+#pragma unroll
+    for (int t = 0; t < NT; ++t) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+#pragma unroll
+        for (int x = 4; x < 32; x <<= 1) l[t][i] += __shfl_xor_sync(0xFFFFFFFFu, l[t][i], x);
+        const int row = 8 * t + 2 * c + i;
+        if (g == 0) { sm_m[warp][row] = m[t][i]; sm_l[warp][row] = l[t][i]; }
+        float* to = sm_o[warp][row];
+        if (D == 128) {
+          float4* a = reinterpret_cast<float4*>(to + 8 * g);
+          a[0] = make_float4(o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]);
+          a[1] = make_float4(o[t][T > 4 ? 4 : 0][i], o[t][T > 4 ? 5 : 0][i], o[t][T > 4 ? 6 : 0][i], o[t][T > 4 ? 7 : 0][i]);
+          float4* b = reinterpret_cast<float4*>(to + D / 2 + 8 * g);
+          b[0] = make_float4(o[t][0][i + 2], o[t][1][i + 2], o[t][2][i + 2], o[t][3][i + 2]);
+          b[1] = make_float4(o[t][T > 4 ? 4 : 0][i + 2], o[t][T > 4 ? 5 : 0][i + 2], o[t][T > 4 ? 6 : 0][i + 2], o[t][T > 4 ? 7 : 0][i + 2]);
+        } else {
+          float4* a = reinterpret_cast<float4*>(to + 8 * g);
+          a[0] = make_float4(o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]);
+          a[1] = make_float4(o[t][0][i + 2], o[t][1][i + 2], o[t][2][i + 2], o[t][3][i + 2]);
+        }
+      }
+    }
+    __syncthreads();
+    const bool whole = c0 == 0 && c1 == vis.chunks;
+    float* part = s.parts + (size_t)(2 * blockIdx.x + (c0 > 0 ? 0 : 1)) * ROWS * (D + 2);
+    for (int i = tid; i < rows * (D / 4); i += kSplitThreads) {
+      const int row = i / (D / 4), d = 4 * (i % (D / 4));
+      float big = -INFINITY;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) big = fmaxf(big, sm_m[w][row]);
+      const float base = big == -INFINITY ? 0.f : big;
+      float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+      float all = 0.f;
+#pragma unroll
+      for (int w = 0; w < kWarps; ++w) {
+        const float f = exp2_fast(sm_m[w][row] - base);
+        const float4 x = *reinterpret_cast<const float4*>(&sm_o[w][row][d]);
+        sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
+        all += f * sm_l[w][row];
+      }
+      if (whole) {
+        const float inv = all == 0.f ? 0.f : 1.f / all;
+        const int x = tile * ROWS + row;
+        const size_t at = ((size_t)(row0 + x / p.group) * p.hq + h * p.group + x % p.group) * D + d;
+        if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 60))
+          *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
+      } else {
+        *reinterpret_cast<float4*>(part + row * D + d) = sum;
+        if (d == 0) { part[ROWS * D + row] = big; part[ROWS * D + ROWS + row] = all; }
+      }
+    }
+    if (!whole && c0 == 0 && tid == 0) {
+      const long long stop = u + vis.chunks;             // where the row tile ends
+      s.spans[blockIdx.x] = Span{r, h, tile, (int)((stop - 1) / run.per) - (int)blockIdx.x + 1};
+    }
+    u += c1 - c0;
+    __syncthreads();
+  }
+}
+
+// Joins the parts of the row tile that begins in a CTA's run: blockIdx.y takes one row.
+template <int D, int NT>
+__global__ void __launch_bounds__(D) join_kernel(const Split s) {
+  constexpr int ROWS = 8 * NT;
+  const Attention& p = s.a;
+  tc::pdl_launch_dependents();
+  tc::pdl_wait();
+  const Span span = s.spans[blockIdx.x];
+  if (span.parts == 0) return;
+  const int4 req = __ldg(reinterpret_cast<const int4*>(requests_of(p.step) + span.request));
+  const int row = blockIdx.y, x = span.tile * ROWS + row, d = threadIdx.x;
+  if (x >= req.y * p.group) return;
+  auto part = [&](int i) { return s.parts + (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * ROWS * (D + 2); };
+  float big = -INFINITY;
+  for (int i = 0; i < span.parts; ++i) big = fmaxf(big, part(i)[ROWS * D + row]);
+  const float base = big == -INFINITY ? 0.f : big;
+  float sum = 0.f, all = 0.f;
+#pragma unroll 4
+  for (int i = 0; i < span.parts; ++i) {
+    const float* a = part(i);
+    const float f = exp2_fast(a[ROWS * D + row] - base);
+    sum += f * a[row * D + d];
+    all += f * a[ROWS * D + ROWS + row];
+  }
+  const float y = all == 0.f ? 0.f : sum / all;
+  const size_t at = ((size_t)(req.x + x / p.group) * p.hq + span.head * p.group + x % p.group) * D + d;
+  if (LQER_IN_BOUNDS(&p.step->status, at * 2, 2, s.y_extent, 61)) {
+    const uint32_t w = round_bf16x2(y, y);
+    static_cast<uint16_t*>(p.Y)[at] = (uint16_t)w;
+  }
+}
+
+static int split_grid(const Attention& p, int few, int rows_per) {
+  const long long most_rows = (long long)(few < p.M * (long long)p.group ? few : p.M * (long long)p.group);
+  const long long tiles = (most_rows + rows_per - 1) / rows_per, chunks = ((long long)p.max_pages * p.page + kChunk - 1) / kChunk;
+  const long long units = (long long)(p.R < p.M ? p.R : p.M) * tiles * p.hkv * chunks;
+  const long long per_sm = rows_per == 8 ? 3 : 2, most = (long long)sm_count() * per_sm;
+  const long long want = (units + kMinChunks - 1) / kMinChunks;
+  return (int)(want < most ? want : most);
+}
+static int rows_per_tile(const Attention& p) { return p.max_added * (long long)p.group <= 8 ? 8 : 16; }
+
+template <int D, bool MX, int NT>
+static cudaError_t launch_split(const Split& s, int grid, cudaStream_t stream) {
+  LaunchScope scope(kFamDecode, stream, 2);
+  cudaError_t e = launch_after(split_kernel<D, MX, NT>, dim3(grid), kSplitThreads, 0, stream, s);
+  if (e != cudaSuccess) return e;
+  return launch_after(join_kernel<D, NT>, dim3(grid, 8 * NT), D, 0, stream, s);
+}
+
+}  // namespace kv
+
+static kv::Attention attention_params(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
+  kv::Attention p = {};
+  p.M = M; p.R = t.n_requests; p.max_pages = t.max_pages; p.n_pages = t.n_pages; p.page = t.page;
+  p.page_shift = 0;
+  while ((1 << p.page_shift) < t.page) ++p.page_shift;
+  p.max_added = max_added;
+  p.hq = hq; p.hkv = c.kv_heads; p.group = hq / c.kv_heads;
+  const size_t elements = (size_t)c.n_pages * c.kv_heads * c.page * c.head_dim;
+  p.keys = c.keys; p.values = c.values;
+  p.key_exps = static_cast<const uint8_t*>(c.keys) + elements;
+  p.value_exps = static_cast<const uint8_t*>(c.values) + elements;
+  return p;
+}
+static size_t spans_bytes() { return ((size_t)3 * sm_count() * sizeof(kv::Span) + 255) & ~(size_t)255; }
+
+size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
+  const kv::Attention p = attention_params(c, t, M, hq, max_added);
+  const int rows = kv::rows_per_tile(p);
+  return spans_bytes() + (size_t)kv::split_grid(p, 1 << 30, rows) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+}
+cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
+                                   int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
+                                   cudaStream_t s) {
+  kv::Split k = {};
+  k.a = attention_params(c, t, M, hq, max_added);
+  k.a.Q = Q; k.a.Y = Y; k.a.q_stride = q_stride;
+  k.a.tables = t.tables; k.a.step = static_cast<kv::StepHead*>(step);
+  k.a.window = window; k.a.sinks = window > 0 ? sinks : 0;
+  k.a.scale_log2 = (float)(scale * 1.4426950408889634);
+  k.a.bits = bits; k.a.emin = emin; k.a.emax = emax;
+  k.few = 1 << 30;
+  k.spans = static_cast<kv::Span*>(scratch);
+  k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + spans_bytes());
+  const size_t whole = (size_t)M * hq * c.head_dim * 2, less = debug_y_shrink();
+  k.y_extent = whole > less ? whole - less : 0;
+  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows);
+  const bool mx = c.dtype == LQER_MXINT8;
+  if (c.head_dim == 128)
+    return rows == 8 ? (mx ? kv::launch_split<128, true, 1>(k, grid, s) : kv::launch_split<128, false, 1>(k, grid, s))
+                     : (mx ? kv::launch_split<128, true, 2>(k, grid, s) : kv::launch_split<128, false, 2>(k, grid, s));
+  return rows == 8 ? (mx ? kv::launch_split<64, true, 1>(k, grid, s) : kv::launch_split<64, false, 1>(k, grid, s))
+                   : (mx ? kv::launch_split<64, true, 2>(k, grid, s) : kv::launch_split<64, false, 2>(k, grid, s));
+}
+
+}  // namespace lqer
