@@ -19,6 +19,7 @@ namespace lqer {
 namespace kv {
 
 constexpr int kChunk = 64, kWarps = 4, kSplitThreads = 32 * kWarps;
+constexpr int kFewRows = 32;                 // of a request; more go to lqer_attention_tiles.cu
 constexpr int kMinChunks = 2;                // of a CTA's run
 
 // What a CTA leaves for the join: the (request, key head, row tile) that begins in its run and goes on behind it, if any.
@@ -476,7 +477,7 @@ static size_t spans_bytes() { return ((size_t)3 * sm_count() * sizeof(kv::Span) 
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
   const int rows = kv::rows_per_tile(p);
-  return spans_bytes() + (size_t)kv::split_grid(p, 1 << 30, rows) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+  return spans_bytes() + (size_t)kv::split_grid(p, kv::kFewRows, rows) * 2 * rows * (c.head_dim + 2) * sizeof(float);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
                                    int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
@@ -488,11 +489,16 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
   k.a.window = window; k.a.sinks = window > 0 ? sinks : 0;
   k.a.scale_log2 = (float)(scale * 1.4426950408889634);
   k.a.bits = bits; k.a.emin = emin; k.a.emax = emax;
-  k.few = 1 << 30;
+  k.few = kv::kFewRows;
   k.spans = static_cast<kv::Span*>(scratch);
   k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + spans_bytes());
   const size_t whole = (size_t)M * hq * c.head_dim * 2, less = debug_y_shrink();
   k.y_extent = whole > less ? whole - less : 0;
+  if (max_added * (long long)k.a.group > k.few) {
+    // a single request goes there whatever it turns out to bring
+    const cudaError_t e = kv::launch_tiles(k.a, t.n_requests == 1 ? 0 : k.few, k.y_extent, c, s);
+    if (e != cudaSuccess || t.n_requests == 1) return e;
+  }
   const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows);
   const bool mx = c.dtype == LQER_MXINT8;
   if (c.head_dim == 128)

@@ -1,0 +1,558 @@
+// Attention of prompts over the paged cache: tiles of 128 rows against tiles of 128 keys on tcgen05.
+//
+// The formulas are those of lqer_attention.cu.  The rows of a key head are its query heads' rows, token by token (row i * group + g), and a CTA takes
+// 256 neighbours of them as two tiles, A and B: S = Q K^T (128 x 128, fp32, tensor memory), weights P (bf16, over S in tensor memory), O += P V.
+// While one tile's weights are formed, the tensor cores work for the other.  Bound: the products are 4 D flops a pair at the tensor cores' rate,
+// an exponential a pair at 16 a clock and SM; for heads of 128 both take the same time, so either is the limit.
+//
+//   warps 0-3, 4-7   tile A, tile B: a thread owns a row: scores from tensor memory, maximum, weights back to tensor memory; no exchange
+//                    between threads.  The row's maximum is let lag by up to 2^8 before what is summed up is scaled anew (the sum
+//                    and the values carry the same factor, so nothing is lost), which after the first tiles is rare.
+//   copies           bf16: one warp, a lane a page: TMA brings pages into swizzled tiles.  MXINT8: four warps read the mantissas, form the exact bf16
+//                    values and store them into the same tiles.
+//   issuer           one lane: per key tile and row tile, O += P V of the last key tile, then S of the next.
+// Keys and values share a ring of tiles.  Every wait is bounded.
+#include "lqer_cache.cuh"
+
+namespace lqer {
+namespace kv {
+
+constexpr int kRows = 128, kKeys = 128;      // of a tile
+
+template <int D, bool MX>
+struct Shape {
+  static constexpr int TILE = 128 * D * 2, HALF = 128 * 128;               // bytes: a tile, and its part of 64 columns
+  static constexpr int STAGES = D == 128 ? 5 : 8;
+  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE;
+  static constexpr int COPY_WARPS = MX ? 4 : 1, COPY0 = 8, ISSUER = COPY0 + COPY_WARPS;
+  static constexpr int THREADS = MX ? 512 : 384;
+  static constexpr int S_COL = 0, O_COL = 256;                              // tensor memory: S of A and B, O of A and B
+  static constexpr int BLOCKS = D / 16;                                     // of 16 elements of a row
+};
+struct Tiles {
+  Attention a;
+  int few;                     // requests of more rows than this are taken
+  int negate;                  // the scale is negative: S = -Q K^T, and a.scale_log2 is its absolute value
+  int stall;
+  long long wait_limit;
+  size_t y_extent;
+};
+struct Barriers {
+  unsigned long long full[8], empty[8], s_full[2], p_full[2], o_done[2], q_full, drained;
+};
+__device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
+
+// On the way out after a wait ran out: what the CTA has under way may still write its memory.
+constexpr long long kDrainCycles = 2000000;
+__device__ __forceinline__ void drain(uint32_t bar, uint32_t parity) {
+  const long long t0 = clock64();
+  while (!tc::mbar_try_wait(bar, parity) && clock64() - t0 < kDrainCycles) {}
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, int x, int y, int z, int w, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+               ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
+}
+// Descriptor of the values as the MMA's second operand: columns along memory, 64 to a swizzled row; 8 keys are 1024 bytes, the next 64 columns a half
+// tile away.
+__device__ __forceinline__ uint64_t values_desc(uint32_t saddr, int half) {
+  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(half >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+}
+__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
+               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
+               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
+               ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
+                 "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+__device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  return r;
+}
+
+// What a CTA works on: 256 rows of a request's key head from `base` on.
+struct Item { int request, head, row0, n, len, base, rows; };      // rows: n * group
+// The key tiles that its two row tiles see: sink tiles, then [start, ..), `count` together; a row tile sees those of them in [from, end) and the sinks'.
+struct Plan {
+  int sinks, sink_tiles, start, count;
+  int from[2], end[2], first_pos[2], last_pos[2];
+  __device__ __forceinline__ int tile(int j) const { return j < sinks ? j : start + j - sinks; }
+  __device__ __forceinline__ bool sees(int t, int kv) const { return kv < (t ? end[1] : end[0]) && (kv >= (t ? from[1] : from[0]) || kv < sink_tiles); }
+};
+__device__ __forceinline__ Plan plan_of(const Attention& p, const Item& it) {
+  Plan q;
+  const int first = it.len - it.n;
+  q.sink_tiles = p.window > 0 ? (min(p.sinks, it.len) + kKeys - 1) / kKeys : 0;
+#pragma unroll
+  for (int t = 0; t < 2; ++t) {
+    const int lo = it.base + t * kRows, hi = min(lo + kRows, it.rows);
+    const bool live = lo < hi;
+    q.first_pos[t] = live ? first + lo / p.group : 0;
+    q.last_pos[t] = live ? first + (hi - 1) / p.group : -1;
+    q.end[t] = live ? q.last_pos[t] / kKeys + 1 : 0;
+    q.from[t] = p.window > 0 ? max(0, q.first_pos[t] - p.window + 1) / kKeys : 0;
+  }
+  q.start = q.from[0];
+  q.sinks = min(q.sink_tiles, q.start);
+  q.count = q.sinks + max(q.end[0], q.end[1]) - q.start;
+  return q;
+}
+// The CTA's item; heavy ones (a request's last) first.  False: there is none.
+__device__ __forceinline__ bool find_item(const Tiles& s, Item& it) {
+  const Attention& p = s.a;
+  const StepRequest* reqs = requests_of(p.step);
+  __shared__ int sums[16];
+  __shared__ Item found;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
+  const int per = (p.R + blockDim.x - 1) / blockDim.x, from = min(tid * per, p.R), to = min(from + per, p.R);
+  auto items_of = [&](const int4& w) {
+    const long long rows = (long long)w.y * p.group;
+    return w.y > 0 && rows > s.few ? (int)((rows + 2 * kRows - 1) / (2 * kRows)) : 0;
+  };
+  int mine = 0;
+  for (int r = from; r < to; ++r) mine += items_of(__ldg(reinterpret_cast<const int4*>(reqs + r)));
+  int x = mine;
+#pragma unroll
+  for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xFFFFFFFFu, x, o); if (lane >= o) x += y; }
+  if (lane == 31) sums[warp] = x;
+  __syncthreads();
+  int before = x - mine, total = 0;
+  for (int w = 0; w < warps; ++w) { if (w < warp) before += sums[w]; total += sums[w]; }
+  const int index = total - 1 - (int)(blockIdx.x / p.hkv);
+  if (index < 0) return false;
+  if (index >= before && index < before + mine) {
+    for (int r = from;; ++r) {
+      const int4 w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+      const int c = items_of(w);
+      if (index < before + c) {
+        found = Item{r, (int)(blockIdx.x % p.hkv), w.x, w.y, w.z, (index - before) * 2 * kRows, w.y * p.group};
+        break;
+      }
+      before += c;
+    }
+  }
+  __syncthreads();
+  it = found;
+  return true;
+}
+
+template <int D, bool MX>
+__global__ void __launch_bounds__(Shape<D, MX>::THREADS, 1)
+tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const __grid_constant__ CUtensorMap value_map) {
+  using SH = Shape<D, MX>;
+  extern __shared__ uint8_t dynamic[];
+  __shared__ Barriers bars;
+  __shared__ uint32_t tmem_at;
+  __shared__ tc::WaitState ws;
+  const Attention& p = s.a;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  tc::pdl_launch_dependents();
+  tc::pdl_wait();
+  if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
+  Item it;
+  if (!find_item(s, it)) return;
+  const uint32_t q_at = (tc::smem_u32(dynamic) + 1023u) & ~1023u, ring_at = q_at + 2 * SH::TILE;
+  uint8_t* const q_mem = dynamic + (q_at - tc::smem_u32(dynamic));
+  uint8_t* const ring_mem = q_mem + 2 * SH::TILE;
+  if (tid == 0) {
+    for (int i = 0; i < SH::STAGES; ++i) {
+      tc::mbar_init(bar_of(bars.full[i]), SH::COPY_WARPS);
+      tc::mbar_init(bar_of(bars.empty[i]), 1);
+    }
+    for (int t = 0; t < 2; ++t) {
+      tc::mbar_init(bar_of(bars.s_full[t]), 1);
+      tc::mbar_init(bar_of(bars.p_full[t]), 4);
+      tc::mbar_init(bar_of(bars.o_done[t]), 1);
+    }
+    tc::mbar_init(bar_of(bars.q_full), 8 + (s.stall && blockIdx.x == 0 ? 1 : 0));
+    tc::mbar_init(bar_of(bars.drained), 1);
+    tc::fence_barrier_init();
+    ws.abort = 0;
+    ws.limit = s.wait_limit;
+  }
+  if (warp == SH::ISSUER) tc::tmem_alloc(tc::smem_u32(&tmem_at), 512);
+  tc::tc_fence_before();
+  __syncthreads();
+  tc::tc_fence_after();
+  const uint32_t tmem = tmem_at;
+  const Plan plan = plan_of(p, it);
+  const int* table = p.tables + (size_t)it.request * p.max_pages;
+  // keys that no row of the step sees: from the end on, and between the first tokens and the window
+  const int seen_from = p.window > 0 ? max(0, it.len - it.n - p.window + 1) : 0;
+  auto unseen = [&](int key) { return key >= it.len || (key < seen_from && key >= p.sinks); };
+  auto has_unseen = [&](int key0) { return key0 + kKeys > it.len || (key0 < seen_from && key0 + kKeys > p.sinks); };
+  int copies = 0;
+  bool ok = true;
+
+  if (warp < 8) {
+    // ---- a row tile
+    // registers: what the launch gave, 128 x 512 or 168 x 384, shared out anew: 2 x 192 + 96 + 32 = 4 x 128, 2 x 216 + 72 = 3 x 168
+    if constexpr (MX) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    else asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
+    const int t = warp >> 2, row = tid & 127;
+    const uint32_t lanes = (uint32_t)(warp & 3) << 21;
+    const uint32_t s_at = tmem + lanes + SH::S_COL + t * 128, o_at = tmem + lanes + SH::O_COL + t * D;
+    const int x = it.base + t * kRows + row;                      // of the request's rows of this key head
+    {
+      // queries, as the MMA reads them; 16 bytes a thread, the tile's rows in turn
+      constexpr int PER = D / 8, STEP = 128 / PER;
+      uint8_t* const to = q_mem + t * SH::TILE;
+      const int c = row % PER, r0 = row / PER;
+      uint4 v[PER];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int y = it.base + t * kRows + r0 + i * STEP;
+        v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (y < it.rows)
+          v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + (size_t)(it.row0 + y / p.group) * p.q_stride +
+                                                      (size_t)(it.head * p.group + y % p.group) * D + 8 * c));
+      }
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int r = r0 + i * STEP;
+        *reinterpret_cast<uint4*>(to + (c >> 3) * SH::HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar_of(bars.q_full));
+    }
+    const int first_pos = t ? plan.first_pos[1] : plan.first_pos[0], last_pos = t ? plan.last_pos[1] : plan.last_pos[0];
+    const int pos = it.len - it.n + min(x, it.rows - 1) / p.group;
+    const float c = p.scale_log2;
+    float m = -INFINITY, l0 = 0.f, l1 = 0.f;
+    int n = 0;                                                     // key tiles so far
+    for (int j = 0; j < plan.count && ok; ++j) {
+      const int kv = plan.tile(j), key0 = kv * kKeys;
+      if (!plan.sees(t, kv)) continue;
+      ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.s_full[t]), n & 1, &ws)) != 0;
+      if (!ok) break;
+      tc::tc_fence_after();
+      float v[128];
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t (&part)[32] = *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]);
+        tc::tmem_ld32(s_at + 32 * k, part);
+      }
+      tc::tmem_ld_wait();
+      if (key0 + kKeys - 1 > first_pos || (p.window > 0 && key0 <= last_pos - p.window)) {
+        const int last = pos - key0, from = p.window > 0 ? last - p.window : -1, sink = p.sinks - key0;
+#pragma unroll
+        for (int i = 0; i < 128; ++i)
+          if (i > last || (i <= from && i >= sink)) v[i] = -INFINITY;
+      }
+      float big = -INFINITY;
+      {
+        float b[4] = {v[0], v[1], v[2], v[3]};
+#pragma unroll
+        for (int i = 4; i < 124; i += 8) {
+#pragma unroll
+          for (int k = 0; k < 4; ++k) b[k] = max3(b[k], v[i + k], v[i + 4 + k]);
+        }
+#pragma unroll
+        for (int k = 0; k < 4; ++k) b[k] = fmaxf(b[k], v[124 + k]);
+        big = fmaxf(max3(b[0], b[1], b[2]), b[3]);
+      }
+      const bool up = (big - m) * c > 8.f || (m == -INFINITY && big > -INFINITY);
+      if (__any_sync(0xFFFFFFFFu, up)) {
+        const float f = up ? exp2_fast((m - big) * c) : 1.f;
+        if (up) m = big;
+        if (n > 0) {
+          l0 *= f;
+          l1 *= f;
+          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
+          if (!ok) break;
+          tc::tc_fence_after();
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k) {
+            uint32_t o[16];
+            tc::tmem_ld16(o_at + 16 * k, o);
+            tc::tmem_ld_wait();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * f);
+            tmem_st16(o_at + 16 * k, o);
+          }
+        }
+      }
+      const float base = m == -INFINITY ? 0.f : m * c;
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        uint32_t w[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const float a = exp2_fast(fmaf(v[32 * k + 2 * i], c, -base)), b = exp2_fast(fmaf(v[32 * k + 2 * i + 1], c, -base));
+          l0 += a;
+          l1 += b;
+          w[i] = round_bf16x2(a, b);                              // as in lqer_attention.cu: the weights are rounded, their sum is not
+        }
+        tmem_st16(s_at + 16 * k, w);
+      }
+      if constexpr (!MX) {
+        if (has_unseen(key0)) {
+          // values that no row sees may be anything: 0 times that has to be 0
+          const int at = 2 * j + 1;
+          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.full[at % SH::STAGES]), at / SH::STAGES & 1, &ws)) != 0;
+          if (!ok) break;
+          if (unseen(key0 + row)) {
+            uint4* to = reinterpret_cast<uint4*>(ring_mem + (at % SH::STAGES) * SH::TILE + row * 128);
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) to[h * (SH::HALF / 16) + i] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          tc::fence_proxy_async_smem();
+        }
+      }
+      tmem_st_wait();
+      tc::tc_fence_before();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar_of(bars.p_full[t]));
+      ++n;
+    }
+    if (ok && n > 0) {
+      ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
+      tc::tc_fence_after();
+      const float all = l0 + l1, inv = all == 0.f ? 0.f : 1.f / all;
+      const size_t at = ((size_t)(it.row0 + x / p.group) * p.hq + it.head * p.group + x % p.group) * D;
+      const bool mine = x < it.rows && ok && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
+#pragma unroll
+      for (int k = 0; k < D / 32; ++k) {
+        uint32_t o[32];
+        tc::tmem_ld32(o_at + 32 * k, o);
+        tc::tmem_ld_wait();
+        if (mine) {
+          uint4* to = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.Y) + at + 32 * k);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            uint32_t w[4];
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              w[e] = round_bf16x2(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
+            to[i] = make_uint4(w[0], w[1], w[2], w[3]);
+          }
+        }
+      }
+    }
+  } else if (warp < SH::ISSUER) {
+    if constexpr (!MX) {
+      // ---- copies: a lane a page
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+      const int pages = kKeys >> p.page_shift;
+      for (int j = 0; j < plan.count && ok; ++j) {
+        const int key0 = plan.tile(j) * kKeys, key = key0 + (lane << p.page_shift);
+        const bool mine = lane < pages && key < it.len;
+        const int id = mine ? checked_page(p, __ldg(table + (key >> p.page_shift)), it.request) : 0;
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine)) * (uint32_t)(p.page * D * 2);
+        for (int which = 0; which < 2; ++which, ++copies) {
+          const int at = copies % SH::STAGES;
+          if (copies >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (copies / SH::STAGES - 1) & 1, &ws)) != 0;
+          if (!ok) break;
+          if (lane == 0) tc::mbar_expect_tx(bar_of(bars.full[at]), bytes);
+          __syncwarp();
+          if (mine) {
+            const uint32_t to = ring_at + at * SH::TILE + (uint32_t)(lane << p.page_shift) * 128;
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h)
+              tma_load_4d(to + h * SH::HALF, which ? &value_map : &key_map, 64 * h, 0, it.head, id, bar_of(bars.full[at]));
+          }
+        }
+      }
+    } else {
+      // ---- copies: mantissas into bf16 values; a lane a block of 16, the block's row's neighbours beside it
+      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+      constexpr int B = SH::BLOCKS, N = B, STEP = 128 / B;         // a thread's blocks of a tile, and the rows between them
+      const int k = tid - 256, b = k % B, r0 = k / B, lo = p.emin + 127, hi = p.emax + 127, shift = p.bits - 2;
+      uint4 m[N];
+      uint32_t e[N];
+      int ids[N];
+      auto pages_of = [&](int j) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          const int key = plan.tile(j) * kKeys + r0 + i * STEP;
+          ids[i] = unseen(key) ? -1 : checked_page(p, __ldg(table + (key >> p.page_shift)), it.request);
+        }
+      };
+      auto load = [&](int j, int which) {
+        const uint8_t* x = static_cast<const uint8_t*>(which ? p.values : p.keys);
+        const uint8_t* y = which ? p.value_exps : p.key_exps;
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+          m[i] = make_uint4(0u, 0u, 0u, 0u);
+          e[i] = 127;
+          if (ids[i] >= 0) {
+            const int key = plan.tile(j) * kKeys + r0 + i * STEP;
+            const size_t at = ((((size_t)ids[i] * p.hkv + it.head) << p.page_shift) + (key & (p.page - 1))) * B + b;
+            m[i] = __ldg(reinterpret_cast<const uint4*>(x) + at);
+            e[i] = __ldg(y + at);
+          }
+        }
+      };
+      pages_of(0);
+      load(0, 0);
+      for (int j = 0; j < plan.count && ok; ++j) {
+        for (int which = 0; which < 2; ++which, ++copies) {
+          const int at = copies % SH::STAGES;
+          if (copies >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (copies / SH::STAGES - 1) & 1, &ws)) != 0;
+          if (!ok) break;
+          uint8_t* const to = ring_mem + at * SH::TILE;
+#pragma unroll
+          for (int i = 0; i < N; ++i) {
+            const int r = r0 + i * STEP;
+            const uint32_t sc = mantissa_scale(e[i], lo, hi, shift);
+            const uint4 w[2] = {mantissas8(make_uint2(m[i].x, m[i].y), sc), mantissas8(make_uint2(m[i].z, m[i].w), sc)};
+            // the two halves' columns lie on the same banks: their lanes store their chunks in opposite order
+            const int turn = D == 128 ? b >> 2 : 0;
+            uint8_t* const row = to + (b >> 2) * SH::HALF + r * 128;
+            const int c = 2 * (b & 3);
+            *reinterpret_cast<uint4*>(row + (((c + turn) ^ (r & 7)) << 4)) = turn ? w[1] : w[0];
+            *reinterpret_cast<uint4*>(row + (((c + 1 - turn) ^ (r & 7)) << 4)) = turn ? w[0] : w[1];
+          }
+          tc::fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(bar_of(bars.full[at]));
+          if (which == 0) {
+            load(j, 1);
+          } else if (j + 1 < plan.count) {
+            pages_of(j + 1);
+            load(j + 1, 0);
+          }
+        }
+      }
+    }
+  } else if (warp == SH::ISSUER) {
+    if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (lane == 0) {
+      const uint32_t s_idesc = tc::make_idesc(128, 128) | (s.negate ? 1u << 13 : 0u), o_idesc = tc::make_idesc(128, D) | 1u << 16;
+      int n[2] = {0, 0};                                           // key tiles whose O is under way
+      ok = tc::mbar_wait(bar_of(bars.q_full), 0, &ws);
+      for (int j = 0; j <= plan.count && ok; ++j) {
+        const int v_at = (2 * j - 1) % SH::STAGES, k_at = 2 * j % SH::STAGES;
+        if (j > 0) ok = tc::mbar_wait(bar_of(bars.full[v_at]), (2 * j - 1) / SH::STAGES & 1, &ws);
+        bool keys_there = false;
+#pragma unroll
+        for (int t = 0; t < 2; ++t) {
+          if (!ok) break;
+          if (j > 0 && plan.sees(t, plan.tile(j - 1))) {
+            ok = tc::mbar_wait(bar_of(bars.p_full[t]), n[t] & 1, &ws);
+            if (!ok) break;
+            tc::tc_fence_after();
+#pragma unroll
+            for (int k = 0; k < kKeys / 16; ++k)
+              mma_ts(tmem + SH::O_COL + t * D, tmem + SH::S_COL + t * 128 + 8 * k, values_desc(ring_at + v_at * SH::TILE + k * 2048, SH::HALF), o_idesc,
+                     n[t] > 0 || k > 0 ? 1u : 0u);
+            tc::umma_commit(bar_of(bars.o_done[t]));
+            ++n[t];
+          }
+          if (j < plan.count) {
+            if (!keys_there) {
+              ok = tc::mbar_wait(bar_of(bars.full[k_at]), 2 * j / SH::STAGES & 1, &ws);
+              if (!ok) break;
+              tc::tc_fence_after();
+              keys_there = true;
+            }
+            if (plan.sees(t, plan.tile(j))) {
+#pragma unroll
+              for (int k = 0; k < D / 16; ++k) {
+                const uint32_t off = (k >> 2) * SH::HALF + (k & 3) * 32;
+                mma_ss(tmem + SH::S_COL + t * 128, tc::make_desc(q_at + t * SH::TILE + off), tc::make_desc(ring_at + k_at * SH::TILE + off), s_idesc,
+                       k > 0 ? 1u : 0u);
+              }
+              tc::umma_commit(bar_of(bars.s_full[t]));
+            }
+          }
+        }
+        if (!ok) break;
+        if (j > 0) tc::umma_commit(bar_of(bars.empty[v_at]));
+        if (j < plan.count) tc::umma_commit(bar_of(bars.empty[k_at]));
+      }
+    }
+  } else {
+    if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+  }
+  __syncwarp();
+  tc::tc_fence_before();
+  __syncthreads();
+  if (ws.abort != 0) {
+    if (tid == 0) report_error(&p.step->status, LQER_ERR_TIMEOUT, 820);
+    if (!MX && warp == SH::COPY0 && lane == 0)
+      for (int k = 0; k < SH::STAGES && k < copies; ++k) {
+        const int last = copies - 1 - k;
+        drain(bar_of(bars.full[last % SH::STAGES]), last / SH::STAGES & 1);
+      }
+    if (warp == SH::ISSUER && lane == 0) {
+      tc::umma_commit(bar_of(bars.drained));
+      drain(bar_of(bars.drained), 0);
+    }
+    __syncthreads();
+  }
+  if (warp == SH::ISSUER) {
+    tc::tc_fence_after();
+    tc::tmem_dealloc(tmem, 512);
+  }
+}
+
+typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
+                                  const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
+static EncodeTiledFn encode_fn() {
+  static EncodeTiledFn fn = [] {
+    void* f = nullptr;
+    cudaDriverEntryPointQueryResult q;
+    if (cudaGetDriverEntryPointByVersion("cuTensorMapEncodeTiled", &f, 12000, cudaEnableDefault, &q) != cudaSuccess || q != cudaDriverEntryPointSuccess)
+      f = nullptr;
+    return reinterpret_cast<EncodeTiledFn>(f);
+  }();
+  return fn;
+}
+// 64 columns of a page of one head; x is 0 or 64, so a copy starts on a 128-byte boundary.
+static bool page_map(CUtensorMap* map, const void* base, const lqer_kv_cache_t& c) {
+  const EncodeTiledFn fn = encode_fn();
+  if (fn == nullptr) return false;
+  const cuuint64_t row = (cuuint64_t)c.head_dim * 2;
+  const cuuint64_t dims[4] = {(cuuint64_t)c.head_dim, (cuuint64_t)c.page, (cuuint64_t)c.kv_heads, (cuuint64_t)c.n_pages};
+  const cuuint64_t strides[3] = {row, row * c.page, row * c.page * c.kv_heads};
+  const cuuint32_t box[4] = {64, (cuuint32_t)c.page, 1, 1}, ones[4] = {1, 1, 1, 1};
+  return fn(map, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(base), dims, strides, box, ones, CU_TENSOR_MAP_INTERLEAVE_NONE,
+            CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+template <int D, bool MX>
+static cudaError_t launch_shape(const Tiles& k, int ctas, const lqer_kv_cache_t& c, cudaStream_t s) {
+  using SH = Shape<D, MX>;
+  static OncePerDevice once;
+  cudaError_t e = once.run([] { return cudaFuncSetAttribute(tiles_kernel<D, MX>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::SMEM); });
+  if (e != cudaSuccess) return e;
+  CUtensorMap maps[2] = {};
+  if (!MX && (!page_map(&maps[0], c.keys, c) || !page_map(&maps[1], c.values, c))) return cudaErrorInvalidValue;
+  LaunchScope scope(kFamDecode, s);
+  return launch_after(tiles_kernel<D, MX>, dim3(ctas), SH::THREADS, SH::SMEM, s, k, maps[0], maps[1]);
+}
+cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, cudaStream_t s) {
+  Tiles k = {};
+  k.a = a;
+  k.few = few;
+  k.negate = a.scale_log2 < 0.f;
+  if (k.negate) k.a.scale_log2 = -a.scale_log2;
+  // what is hidden is minus infinity before the scale comes in, and has to stay that: a scale of 0 is one that is as good as 0 for any score
+  if (k.a.scale_log2 < 1e-40f) k.a.scale_log2 = 1e-40f;
+  k.stall = take_stall(kFamDecode) ? 1 : 0;
+  k.wait_limit = wait_limit_cycles();
+  k.y_extent = y_extent;
+  // no more items than this: whole ones, and one that is not for every request that has enough rows to be taken
+  const long long rows = (long long)a.M * a.group, most = rows / (few + 1);
+  const long long items = rows / (2 * kRows) + (most < a.R ? most : a.R);
+  if (items * a.hkv > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  const int ctas = (int)(items * a.hkv);
+  if (c.dtype == LQER_MXINT8) return c.head_dim == 128 ? launch_shape<128, true>(k, ctas, c, s) : launch_shape<64, true>(k, ctas, c, s);
+  return c.head_dim == 128 ? launch_shape<128, false>(k, ctas, c, s) : launch_shape<64, false>(k, ctas, c, s);
+}
+
+}  // namespace kv
+}  // namespace lqer

@@ -90,6 +90,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
   return y;
 }
 
+// Requests of more than `few` rows (tokens times heads that share a key head) on tcgen05 (lqer_attention_tiles.cu).
+cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, cudaStream_t s);
+
 // Launches with the programmatic attribute: the kernels wait for their predecessor before they touch memory.
 template <class... P, class... A>
 static cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
