@@ -420,7 +420,7 @@ lqer_status_t lqer_append_kv(const void* K, const void* V, lqer_dtype_t x_dtype,
  *   Y[m, h] = sum_j softmax_j(scale Q[m, h] . K[j, h / g]) V[j, h / g],   g = q_heads / kv_heads,
  * over the tokens j of row m's request up to its own position p, and with window > 0 only those with j > p - window or j < sinks.
  *  - Q: M rows of q_heads * head_dim bf16 elements, q_stride elements from row to row (a multiple of 8); Y [M, q_heads, head_dim] bf16, dense, apart
- *    from everything else.  q_heads is a multiple of kv_heads, at most 1024.
+ *    from everything else.  q_heads is a multiple of kv_heads, at most 1024; M * q_heads < 2^31.
  *  - step: made by lqer_cache_step for the same M and a table of these sizes; max_added: at least the step's (kernels are chosen
  *    by it).  The plan is only read, but for its status: one of another batch or table (or none) is reported there as LQER_ERR_BAD_PACKED and
  *    nothing is written; a table entry that is no page as LQER_ERR_BOUNDS (the rows of that request then hold anything).  Rows behind the last token

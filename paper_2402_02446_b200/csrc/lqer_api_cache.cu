@@ -43,6 +43,7 @@ lqer_status_t activation_format(const lqer_config_t* cfg, lqer_config_t* out) {
 }
 lqer_status_t attention_shape(int M, int q_heads, const lqer_kv_cache_t* c, const lqer_page_table_t* t, int max_added) {
   if (!rows_ok(M) || max_added < 1 || q_heads < 1 || q_heads > kKvMaxHeads || q_heads % c->kv_heads != 0) return LQER_ERR_SHAPE;
+  if ((long long)M * q_heads > 0x7FFFFFFF) return LQER_ERR_SHAPE;
   return t->page == c->page && t->n_pages == c->n_pages ? LQER_OK : LQER_ERR_SHAPE;
 }
 

@@ -22,23 +22,25 @@ constexpr int kRows = 128, kKeys = 128;      // of a tile
 template <int D, bool MX>
 struct Shape {
   static constexpr int TILE = 128 * D * 2, HALF = 128 * 128;               // bytes: a tile, and its part of 64 columns
-  static constexpr int STAGES = D == 128 ? 5 : 8;
-  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE;
-  static constexpr int COPY_WARPS = MX ? 4 : 1, COPY0 = 8, ISSUER = COPY0 + COPY_WARPS;
+  static constexpr int BLOCKS = D / 16;                                     // of 16 elements of a row
+  static constexpr int STAGES = MX ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);
+  static constexpr int RAW_STAGES = MX ? (D == 128 ? 3 : 6) : 0, RAW_EXPS = 128 * D, RAW = 128 * D + 128 * BLOCKS;   // an MXINT8 tile as it lies in the cache
+  static constexpr int SMEM = 1024 + (2 + STAGES) * TILE + RAW_STAGES * RAW;
+  static constexpr int COPY_WARPS = MX ? 4 : 1, COPY0 = 8, ISSUER = COPY0 + COPY_WARPS, RAW_WARP = MX ? ISSUER + 1 : -1;
   static constexpr int THREADS = MX ? 512 : 384;
   static constexpr int S_COL = 0, O_COL = 256;                              // tensor memory: S of A and B, O of A and B
-  static constexpr int BLOCKS = D / 16;                                     // of 16 elements of a row
 };
 struct Tiles {
   Attention a;
   int few;                     // requests of more rows than this are taken
   int negate;                  // the scale is negative: S = -Q K^T, and a.scale_log2 is its absolute value
+  uint32_t group_inv;          // 2^32 / group rounded up (a group of 1: 0), for quotients of rows below 2^20 / group
   int stall;
   long long wait_limit;
   size_t y_extent;
 };
 struct Barriers {
-  unsigned long long full[8], empty[8], s_full[2], p_full[2], o_done[2], q_full, drained;
+  unsigned long long full[8], empty[8], raw_full[6], raw_empty[6], s_full[2], p_half[2], p_full[2], o_done[2], q_full, drained;
 };
 __device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
 
@@ -77,8 +79,39 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-// What a CTA works on: 256 rows of a request's key head from `base` on.
-struct Item { int request, head, row0, n, len, base, rows; };      // rows: n * group
+// Two fp32 operations in one instruction.
+struct F2 { unsigned long long w; };
+__device__ __forceinline__ F2 f2(float a, float b) { F2 r; asm("mov.b64 %0, {%1, %2};" : "=l"(r.w) : "f"(a), "f"(b)); return r; }
+__device__ __forceinline__ void unf2(F2 v, float& a, float& b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v.w)); }
+__device__ __forceinline__ F2 fma2(F2 a, F2 b, F2 c) { F2 r; asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r.w) : "l"(a.w), "l"(b.w), "l"(c.w)); return r; }
+__device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r.w) : "l"(a.w), "l"(b.w)); return r; }
+// 2^x of two values on the arithmetic units, which have time to spare where the exponential unit has not: x = n + f, n the nearest integer, and a
+// polynomial of third degree in f that is nowhere in [-1/2, 1/2] more than 7.5e-5 of 2^f off (the minimax one, by Remez' exchange).
+// Below 2^-125 it stays 2^-125: no more beside a row's largest weight, which is 2^-8 or more of the sums' scale, than nothing.
+__device__ __forceinline__ void exp2_poly(F2 x, float& a, float& b) {
+  float lo, hi;
+  unf2(x, lo, hi);
+  x = f2(fmaxf(lo, -125.f), fmaxf(hi, -125.f));
+  const F2 round = f2(12582912.f, 12582912.f), minus = f2(-1.f, -1.f);      // 1.5 * 2^23: the sum's low bits are n
+  const F2 r = add2(x, round), n = add2(r, f2(-12582912.f, -12582912.f)), f = fma2(n, minus, x);
+  F2 q = fma2(f, f2(0.05517166853f, 0.05517166853f), f2(0.24261112511f, 0.24261112511f));
+  q = fma2(q, f, f2(0.69326096773f, 0.69326096773f));
+  q = fma2(q, f, f2(0.99992805719f, 0.99992805719f));
+  float ra, rb, qa, qb;
+  unf2(r, ra, rb);
+  unf2(q, qa, qb);
+  a = __uint_as_float((__float_as_uint(ra) << 23) + __float_as_uint(qa));
+  b = __uint_as_float((__float_as_uint(rb) << 23) + __float_as_uint(qb));
+}
+
+// What a CTA works on: 256 rows of a request's key head from `base` on, the first of them head `head0` of the group of token `token0`.
+struct Item { int request, head, row0, n, len, base, rows, token0, head0; };      // rows: n * group
+// Row z of an item: its token, and its head within the group.
+__device__ __forceinline__ void row_of(const Tiles& s, const Item& it, int z, int& token, int& head) {
+  const uint32_t x = (uint32_t)(z + it.head0), q = s.a.group == 1 ? x : __umulhi(x, s.group_inv);
+  token = it.token0 + (int)q;
+  head = (int)(x - q * s.a.group);
+}
 // The key tiles that its two row tiles see: sink tiles, then [start, ..), `count` together; a row tile sees those of them in [from, end) and the sinks'.
 struct Plan {
   int sinks, sink_tiles, start, count;
@@ -86,16 +119,20 @@ struct Plan {
   __device__ __forceinline__ int tile(int j) const { return j < sinks ? j : start + j - sinks; }
   __device__ __forceinline__ bool sees(int t, int kv) const { return kv < (t ? end[1] : end[0]) && (kv >= (t ? from[1] : from[0]) || kv < sink_tiles); }
 };
-__device__ __forceinline__ Plan plan_of(const Attention& p, const Item& it) {
+__device__ __forceinline__ Plan plan_of(const Tiles& s, const Item& it) {
+  const Attention& p = s.a;
   Plan q;
   const int first = it.len - it.n;
   q.sink_tiles = p.window > 0 ? (min(p.sinks, it.len) + kKeys - 1) / kKeys : 0;
 #pragma unroll
   for (int t = 0; t < 2; ++t) {
-    const int lo = it.base + t * kRows, hi = min(lo + kRows, it.rows);
+    const int lo = t * kRows, hi = min(lo + kRows, it.rows - it.base);
     const bool live = lo < hi;
-    q.first_pos[t] = live ? first + lo / p.group : 0;
-    q.last_pos[t] = live ? first + (hi - 1) / p.group : -1;
+    int a, b, h;
+    row_of(s, it, lo, a, h);
+    row_of(s, it, max(hi - 1, 0), b, h);
+    q.first_pos[t] = live ? first + a : 0;
+    q.last_pos[t] = live ? first + b : -1;
     q.end[t] = live ? q.last_pos[t] / kKeys + 1 : 0;
     q.from[t] = p.window > 0 ? max(0, q.first_pos[t] - p.window + 1) / kKeys : 0;
   }
@@ -113,26 +150,31 @@ __device__ __forceinline__ bool find_item(const Tiles& s, Item& it) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int per = (p.R + blockDim.x - 1) / blockDim.x, from = min(tid * per, p.R), to = min(from + per, p.R);
   auto items_of = [&](const int4& w) {
-    const long long rows = (long long)w.y * p.group;
-    return w.y > 0 && rows > s.few ? (int)((rows + 2 * kRows - 1) / (2 * kRows)) : 0;
+    const int rows = w.y * p.group;
+    return w.y > 0 && rows > s.few ? (rows + 2 * kRows - 1) / (2 * kRows) : 0;
   };
+  int4 w = make_int4(0, 0, 0, 0);
   int mine = 0;
-  for (int r = from; r < to; ++r) mine += items_of(__ldg(reinterpret_cast<const int4*>(reqs + r)));
+  for (int r = from; r < to; ++r) {
+    w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+    mine += items_of(w);
+  }
   int x = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xFFFFFFFFu, x, o); if (lane >= o) x += y; }
   if (lane == 31) sums[warp] = x;
   __syncthreads();
   int before = x - mine, total = 0;
-  for (int w = 0; w < warps; ++w) { if (w < warp) before += sums[w]; total += sums[w]; }
+  for (int k = 0; k < warps; ++k) { if (k < warp) before += sums[k]; total += sums[k]; }
   const int index = total - 1 - (int)(blockIdx.x / p.hkv);
   if (index < 0) return false;
   if (index >= before && index < before + mine) {
     for (int r = from;; ++r) {
-      const int4 w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+      if (per > 1) w = __ldg(reinterpret_cast<const int4*>(reqs + r));
       const int c = items_of(w);
       if (index < before + c) {
-        found = Item{r, (int)(blockIdx.x % p.hkv), w.x, w.y, w.z, (index - before) * 2 * kRows, w.y * p.group};
+        const int base = (index - before) * 2 * kRows, token = base / p.group;
+        found = Item{r, (int)(blockIdx.x % p.hkv), w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group};
         break;
       }
       before += c;
@@ -141,6 +183,13 @@ __device__ __forceinline__ bool find_item(const Tiles& s, Item& it) {
   __syncthreads();
   it = found;
   return true;
+}
+// The columns of a key tile from key0 on that the row at `pos` sees, 32 to a word.
+__device__ __forceinline__ uint32_t upto(int n) { return n < 0 ? 0u : n >= 31 ? 0xFFFFFFFFu : (2u << n) - 1u; }       // bits 0 .. n
+__device__ __forceinline__ uint32_t seen_columns(const Attention& p, int pos, int key0, int k) {
+  uint32_t w = upto(pos - key0 - 32 * k);
+  if (p.window > 0) w &= ~upto(pos - p.window - key0 - 32 * k) | upto(p.sinks - 1 - key0 - 32 * k);
+  return w;
 }
 
 template <int D, bool MX>
@@ -153,21 +202,22 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   __shared__ tc::WaitState ws;
   const Attention& p = s.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  tc::pdl_launch_dependents();
-  tc::pdl_wait();
-  if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
-  Item it;
-  if (!find_item(s, it)) return;
-  const uint32_t q_at = (tc::smem_u32(dynamic) + 1023u) & ~1023u, ring_at = q_at + 2 * SH::TILE;
+  const uint32_t q_at = (tc::smem_u32(dynamic) + 1023u) & ~1023u, ring_at = q_at + 2 * SH::TILE, raw_at = ring_at + SH::STAGES * SH::TILE;
   uint8_t* const q_mem = dynamic + (q_at - tc::smem_u32(dynamic));
   uint8_t* const ring_mem = q_mem + 2 * SH::TILE;
+  tc::pdl_launch_dependents();
   if (tid == 0) {
     for (int i = 0; i < SH::STAGES; ++i) {
       tc::mbar_init(bar_of(bars.full[i]), SH::COPY_WARPS);
       tc::mbar_init(bar_of(bars.empty[i]), 1);
     }
+    for (int i = 0; i < SH::RAW_STAGES; ++i) {
+      tc::mbar_init(bar_of(bars.raw_full[i]), 1);
+      tc::mbar_init(bar_of(bars.raw_empty[i]), SH::COPY_WARPS);
+    }
     for (int t = 0; t < 2; ++t) {
       tc::mbar_init(bar_of(bars.s_full[t]), 1);
+      tc::mbar_init(bar_of(bars.p_half[t]), 4);
       tc::mbar_init(bar_of(bars.p_full[t]), 4);
       tc::mbar_init(bar_of(bars.o_done[t]), 1);
     }
@@ -176,13 +226,21 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     tc::fence_barrier_init();
     ws.abort = 0;
     ws.limit = s.wait_limit;
+    if (!MX) {
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&key_map)) : "memory");
+      asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&value_map)) : "memory");
+    }
   }
+  tc::pdl_wait();
+  if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
+  Item it;
+  if (!find_item(s, it)) return;
   if (warp == SH::ISSUER) tc::tmem_alloc(tc::smem_u32(&tmem_at), 512);
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_at;
-  const Plan plan = plan_of(p, it);
+  const Plan plan = plan_of(s, it);
   const int* table = p.tables + (size_t)it.request * p.max_pages;
   // keys that no row of the step sees: from the end on, and between the first tokens and the window
   const int seen_from = p.window > 0 ? max(0, it.len - it.n - p.window + 1) : 0;
@@ -199,20 +257,21 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const int t = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t s_at = tmem + lanes + SH::S_COL + t * 128, o_at = tmem + lanes + SH::O_COL + t * D;
-    const int x = it.base + t * kRows + row;                      // of the request's rows of this key head
+    const int left = it.rows - it.base - t * kRows;               // rows from the tile's first on
     {
       // queries, as the MMA reads them; 16 bytes a thread, the tile's rows in turn
       constexpr int PER = D / 8, STEP = 128 / PER;
       uint8_t* const to = q_mem + t * SH::TILE;
       const int c = row % PER, r0 = row / PER;
+      const uint16_t* from = static_cast<const uint16_t*>(p.Q) + (size_t)it.row0 * p.q_stride + (size_t)(it.head * p.group) * D + 8 * c;
       uint4 v[PER];
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
-        const int y = it.base + t * kRows + r0 + i * STEP;
+        const int r = r0 + i * STEP;
+        int token, head;
+        row_of(s, it, t * kRows + r, token, head);
         v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (y < it.rows)
-          v[i] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + (size_t)(it.row0 + y / p.group) * p.q_stride +
-                                                      (size_t)(it.head * p.group + y % p.group) * D + 8 * c));
+        if (r < left) v[i] = __ldg(reinterpret_cast<const uint4*>(from + (size_t)token * p.q_stride + head * D));
       }
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -224,9 +283,13 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       if (lane == 0) tc::mbar_arrive(bar_of(bars.q_full));
     }
     const int first_pos = t ? plan.first_pos[1] : plan.first_pos[0], last_pos = t ? plan.last_pos[1] : plan.last_pos[0];
-    const int pos = it.len - it.n + min(x, it.rows - 1) / p.group;
+    int token, head;
+    row_of(s, it, t * kRows + max(min(row, left - 1), 0), token, head);
+    const int pos = it.len - it.n + token;
     const float c = p.scale_log2;
-    float m = -INFINITY, l0 = 0.f, l1 = 0.f;
+    const F2 c2 = f2(c, c);
+    float m = -INFINITY;
+    F2 la = f2(0.f, 0.f), lb = f2(0.f, 0.f);                       // sums of weights, four to a row
     int n = 0;                                                     // key tiles so far
     for (int j = 0; j < plan.count && ok; ++j) {
       const int kv = plan.tile(j), key0 = kv * kKeys;
@@ -236,16 +299,32 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       tc::tc_fence_after();
       float v[128];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t (&part)[32] = *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]);
-        tc::tmem_ld32(s_at + 32 * k, part);
+      for (int k = 0; k < 4; ++k) tc::tmem_ld32(s_at + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]));
+      if constexpr (!MX) {
+        if (has_unseen(key0)) {
+          // values that no row sees may be anything: 0 times that has to be 0
+          const int at = 2 * j + 1;
+          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.full[at % SH::STAGES]), at / SH::STAGES & 1, &ws)) != 0;
+          if (!ok) break;
+          if (unseen(key0 + row)) {
+            uint4* to = reinterpret_cast<uint4*>(ring_mem + (at % SH::STAGES) * SH::TILE + row * 128);
+#pragma unroll
+            for (int h = 0; h < D / 64; ++h)
+#pragma unroll
+              for (int i = 0; i < 8; ++i) to[h * (SH::HALF / 16) + i] = make_uint4(0u, 0u, 0u, 0u);
+          }
+          tc::fence_proxy_async_smem();
+        }
       }
       tc::tmem_ld_wait();
-      if (key0 + kKeys - 1 > first_pos || (p.window > 0 && key0 <= last_pos - p.window)) {
-        const int last = pos - key0, from = p.window > 0 ? last - p.window : -1, sink = p.sinks - key0;
+      const bool masked = key0 + kKeys - 1 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
+      if (masked) {
 #pragma unroll
-        for (int i = 0; i < 128; ++i)
-          if (i > last || (i <= from && i >= sink)) v[i] = -INFINITY;
+        for (int k = 0; k < 4; ++k) {
+          const uint32_t seen = seen_columns(p, pos, key0, k);
+#pragma unroll
+          for (int i = 0; i < 32; ++i) v[32 * k + i] = seen & (1u << i) ? v[32 * k + i] : -INFINITY;
+        }
       }
       float big = -INFINITY;
       {
@@ -264,12 +343,12 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         const float f = up ? exp2_fast((m - big) * c) : 1.f;
         if (up) m = big;
         if (n > 0) {
-          l0 *= f;
-          l1 *= f;
+          la = fma2(la, f2(f, f), f2(0.f, 0.f));
+          lb = fma2(lb, f2(f, f), f2(0.f, 0.f));
           ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
           if (!ok) break;
           tc::tc_fence_after();
-#pragma unroll
+#pragma unroll 1
           for (int k = 0; k < D / 16; ++k) {
             uint32_t o[16];
             tc::tmem_ld16(o_at + 16 * k, o);
@@ -280,47 +359,46 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           }
         }
       }
-      const float base = m == -INFINITY ? 0.f : m * c;
+      const float base = m == -INFINITY ? 0.f : -m * c;
+      const F2 base2 = f2(base, base);
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
         uint32_t w[16];
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-          const float a = exp2_fast(fmaf(v[32 * k + 2 * i], c, -base)), b = exp2_fast(fmaf(v[32 * k + 2 * i + 1], c, -base));
-          l0 += a;
-          l1 += b;
+          const F2 x = fma2(f2(v[32 * k + 2 * i], v[32 * k + 2 * i + 1]), c2, base2);
+          float a, b;
+          if (i % 4 == 3 && !masked) {
+            exp2_poly(x, a, b);
+          } else {
+            unf2(x, a, b);
+            a = exp2_fast(a);
+            b = exp2_fast(b);
+          }
+          if (i % 2) lb = add2(lb, f2(a, b));
+          else la = add2(la, f2(a, b));
           w[i] = round_bf16x2(a, b);                              // as in lqer_attention.cu: the weights are rounded, their sum is not
         }
         tmem_st16(s_at + 16 * k, w);
-      }
-      if constexpr (!MX) {
-        if (has_unseen(key0)) {
-          // values that no row sees may be anything: 0 times that has to be 0
-          const int at = 2 * j + 1;
-          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.full[at % SH::STAGES]), at / SH::STAGES & 1, &ws)) != 0;
-          if (!ok) break;
-          if (unseen(key0 + row)) {
-            uint4* to = reinterpret_cast<uint4*>(ring_mem + (at % SH::STAGES) * SH::TILE + row * 128);
-#pragma unroll
-            for (int h = 0; h < D / 64; ++h)
-#pragma unroll
-              for (int i = 0; i < 8; ++i) to[h * (SH::HALF / 16) + i] = make_uint4(0u, 0u, 0u, 0u);
-          }
-          tc::fence_proxy_async_smem();
+        if (k % 2) {
+          // the issuer may begin with the first half
+          tmem_st_wait();
+          tc::tc_fence_before();
+          __syncwarp();
+          if (lane == 0) tc::mbar_arrive(bar_of(k == 1 ? bars.p_half[t] : bars.p_full[t]));
         }
       }
-      tmem_st_wait();
-      tc::tc_fence_before();
-      __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bar_of(bars.p_full[t]));
       ++n;
     }
     if (ok && n > 0) {
       ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
       tc::tc_fence_after();
-      const float all = l0 + l1, inv = all == 0.f ? 0.f : 1.f / all;
-      const size_t at = ((size_t)(it.row0 + x / p.group) * p.hq + it.head * p.group + x % p.group) * D;
-      const bool mine = x < it.rows && ok && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
+      float l[4];
+      unf2(la, l[0], l[1]);
+      unf2(lb, l[2], l[3]);
+      const float all = (l[0] + l[1]) + (l[2] + l[3]), inv = all == 0.f ? 0.f : 1.f / all;
+      const size_t at = ((size_t)(it.row0 + token) * p.hq + it.head * p.group + head) * D;
+      const bool mine = row < left && ok && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) {
         uint32_t o[32];
@@ -364,64 +442,46 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         }
       }
     } else {
-      // ---- copies: mantissas into bf16 values; a lane a block of 16, the block's row's neighbours beside it
+      // ---- mantissas, as they lie in the cache, into swizzled bf16 values; a lane a block of 16, its row's other blocks beside it
       asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
       constexpr int B = SH::BLOCKS, N = B, STEP = 128 / B;         // a thread's blocks of a tile, and the rows between them
       const int k = tid - 256, b = k % B, r0 = k / B, lo = p.emin + 127, hi = p.emax + 127, shift = p.bits - 2;
-      uint4 m[N];
-      uint32_t e[N];
-      int ids[N];
-      auto pages_of = [&](int j) {
+      const uint8_t* const raw_mem = ring_mem + SH::STAGES * SH::TILE;
+      // the two halves' columns lie on the same banks: their lanes store their chunks in opposite order
+      const int turn = D == 128 ? b >> 2 : 0, c = 2 * (b & 3);
+      const uint32_t to0 = (b >> 2) * SH::HALF + r0 * 128 + (((c + turn) ^ (r0 & 7)) << 4), to1 = (b >> 2) * SH::HALF + r0 * 128 + (((c + 1 - turn) ^ (r0 & 7)) << 4);
+      for (int x = 0; x < 2 * plan.count && ok; ++x) {
+        const int at = x % SH::STAGES, raw = x % SH::RAW_STAGES, key0 = plan.tile(x >> 1) * kKeys;
+        ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.raw_full[raw]), x / SH::RAW_STAGES & 1, &ws)) != 0;
+        if (!ok) break;
+        const uint8_t* const from = raw_mem + raw * SH::RAW;
+        uint4 m[N];
+        uint32_t e[N];
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const int key = plan.tile(j) * kKeys + r0 + i * STEP;
-          ids[i] = unseen(key) ? -1 : checked_page(p, __ldg(table + (key >> p.page_shift)), it.request);
+          m[i] = *reinterpret_cast<const uint4*>(from + (r0 + i * STEP) * D + b * 16);
+          e[i] = from[SH::RAW_EXPS + (r0 + i * STEP) * B + b];
         }
-      };
-      auto load = [&](int j, int which) {
-        const uint8_t* x = static_cast<const uint8_t*>(which ? p.values : p.keys);
-        const uint8_t* y = which ? p.value_exps : p.key_exps;
+        if (has_unseen(key0)) {
+#pragma unroll
+          for (int i = 0; i < N; ++i)
+            if (unseen(key0 + r0 + i * STEP)) m[i] = make_uint4(0u, 0u, 0u, 0u);
+        }
+        if (x >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (x / SH::STAGES - 1) & 1, &ws)) != 0;
+        if (!ok) break;
+        uint8_t* const to = ring_mem + at * SH::TILE;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          m[i] = make_uint4(0u, 0u, 0u, 0u);
-          e[i] = 127;
-          if (ids[i] >= 0) {
-            const int key = plan.tile(j) * kKeys + r0 + i * STEP;
-            const size_t at = ((((size_t)ids[i] * p.hkv + it.head) << p.page_shift) + (key & (p.page - 1))) * B + b;
-            m[i] = __ldg(reinterpret_cast<const uint4*>(x) + at);
-            e[i] = __ldg(y + at);
-          }
+          const uint32_t sc = mantissa_scale(e[i], lo, hi, shift);
+          const uint4 w0 = mantissas8(make_uint2(m[i].x, m[i].y), sc), w1 = mantissas8(make_uint2(m[i].z, m[i].w), sc);
+          *reinterpret_cast<uint4*>(to + to0 + i * STEP * 128) = turn ? w1 : w0;          // (STEP is a multiple of 8: the swizzle stays)
+          *reinterpret_cast<uint4*>(to + to1 + i * STEP * 128) = turn ? w0 : w1;
         }
-      };
-      pages_of(0);
-      load(0, 0);
-      for (int j = 0; j < plan.count && ok; ++j) {
-        for (int which = 0; which < 2; ++which, ++copies) {
-          const int at = copies % SH::STAGES;
-          if (copies >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (copies / SH::STAGES - 1) & 1, &ws)) != 0;
-          if (!ok) break;
-          uint8_t* const to = ring_mem + at * SH::TILE;
-#pragma unroll
-          for (int i = 0; i < N; ++i) {
-            const int r = r0 + i * STEP;
-            const uint32_t sc = mantissa_scale(e[i], lo, hi, shift);
-            const uint4 w[2] = {mantissas8(make_uint2(m[i].x, m[i].y), sc), mantissas8(make_uint2(m[i].z, m[i].w), sc)};
-            // the two halves' columns lie on the same banks: their lanes store their chunks in opposite order
-            const int turn = D == 128 ? b >> 2 : 0;
-            uint8_t* const row = to + (b >> 2) * SH::HALF + r * 128;
-            const int c = 2 * (b & 3);
-            *reinterpret_cast<uint4*>(row + (((c + turn) ^ (r & 7)) << 4)) = turn ? w[1] : w[0];
-            *reinterpret_cast<uint4*>(row + (((c + 1 - turn) ^ (r & 7)) << 4)) = turn ? w[0] : w[1];
-          }
-          tc::fence_proxy_async_smem();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(bar_of(bars.full[at]));
-          if (which == 0) {
-            load(j, 1);
-          } else if (j + 1 < plan.count) {
-            pages_of(j + 1);
-            load(j + 1, 0);
-          }
+        tc::fence_proxy_async_smem();
+        __syncwarp();
+        if (lane == 0) {
+          tc::mbar_arrive(bar_of(bars.full[at]));
+          tc::mbar_arrive(bar_of(bars.raw_empty[raw]));
         }
       }
     }
@@ -440,13 +500,17 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         for (int t = 0; t < 2; ++t) {
           if (!ok) break;
           if (j > 0 && plan.sees(t, plan.tile(j - 1))) {
-            ok = tc::mbar_wait(bar_of(bars.p_full[t]), n[t] & 1, &ws);
-            if (!ok) break;
-            tc::tc_fence_after();
 #pragma unroll
-            for (int k = 0; k < kKeys / 16; ++k)
-              mma_ts(tmem + SH::O_COL + t * D, tmem + SH::S_COL + t * 128 + 8 * k, values_desc(ring_at + v_at * SH::TILE + k * 2048, SH::HALF), o_idesc,
-                     n[t] > 0 || k > 0 ? 1u : 0u);
+            for (int half = 0; half < 2; ++half) {
+              ok = tc::mbar_wait(bar_of(half ? bars.p_full[t] : bars.p_half[t]), n[t] & 1, &ws);
+              if (!ok) break;
+              tc::tc_fence_after();
+#pragma unroll
+              for (int k = 4 * half; k < 4 * half + 4; ++k)
+                mma_ts(tmem + SH::O_COL + t * D, tmem + SH::S_COL + t * 128 + 8 * k, values_desc(ring_at + v_at * SH::TILE + k * 2048, SH::HALF), o_idesc,
+                       n[t] > 0 || k > 0 ? 1u : 0u);
+            }
+            if (!ok) break;
             tc::umma_commit(bar_of(bars.o_done[t]));
             ++n[t];
           }
@@ -476,17 +540,42 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   } else {
     if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
+    if (warp == SH::RAW_WARP) {
+      // ---- copies of an MXINT8 cache: a lane a page
+      const int pages = kKeys >> p.page_shift;
+      for (int j = 0; j < plan.count && ok; ++j) {
+        const int key0 = plan.tile(j) * kKeys, key = key0 + (lane << p.page_shift);
+        const bool mine = lane < pages && key < it.len;
+        const int id = mine ? checked_page(p, __ldg(table + (key >> p.page_shift)), it.request) : 0;
+        const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine)) * (uint32_t)(p.page * (D + D / 16));
+        const size_t block = ((((size_t)id * p.hkv + it.head) << p.page_shift)) * SH::BLOCKS;      // of 16 elements
+        for (int which = 0; which < 2; ++which, ++copies) {
+          const int at = copies % SH::RAW_STAGES;
+          if (copies >= SH::RAW_STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.raw_empty[at]), (copies / SH::RAW_STAGES - 1) & 1, &ws)) != 0;
+          if (!ok) break;
+          if (lane == 0) tc::mbar_expect_tx(bar_of(bars.raw_full[at]), bytes);
+          __syncwarp();
+          if (mine) {
+            const uint32_t to = raw_at + at * SH::RAW, place = lane << p.page_shift;
+            tc::bulk_load(to + place * D, static_cast<const uint8_t*>(which ? p.values : p.keys) + block * 16, p.page * D, bar_of(bars.raw_full[at]));
+            tc::bulk_load(to + SH::RAW_EXPS + place * SH::BLOCKS, (which ? p.value_exps : p.key_exps) + block, p.page * SH::BLOCKS, bar_of(bars.raw_full[at]));
+          }
+        }
+      }
+    }
   }
   __syncwarp();
   tc::tc_fence_before();
   __syncthreads();
   if (ws.abort != 0) {
     if (tid == 0) report_error(&p.step->status, LQER_ERR_TIMEOUT, 820);
-    if (!MX && warp == SH::COPY0 && lane == 0)
-      for (int k = 0; k < SH::STAGES && k < copies; ++k) {
+    if (warp == (MX ? SH::RAW_WARP : SH::COPY0) && lane == 0) {
+      constexpr int PLACES = MX ? SH::RAW_STAGES : SH::STAGES;
+      for (int k = 0; k < PLACES && k < copies; ++k) {
         const int last = copies - 1 - k;
-        drain(bar_of(bars.full[last % SH::STAGES]), last / SH::STAGES & 1);
+        drain(bar_of(MX ? bars.raw_full[last % PLACES] : bars.full[last % PLACES]), last / PLACES & 1);
       }
+    }
     if (warp == SH::ISSUER && lane == 0) {
       tc::umma_commit(bar_of(bars.drained));
       drain(bar_of(bars.drained), 0);
@@ -542,6 +631,7 @@ cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqe
   if (k.negate) k.a.scale_log2 = -a.scale_log2;
   // what is hidden is minus infinity before the scale comes in, and has to stay that: a scale of 0 is one that is as good as 0 for any score
   if (k.a.scale_log2 < 1e-40f) k.a.scale_log2 = 1e-40f;
+  k.group_inv = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   k.stall = take_stall(kFamDecode) ? 1 : 0;
   k.wait_limit = wait_limit_cycles();
   k.y_extent = y_extent;

@@ -99,9 +99,10 @@ def attention64(Q, K, V, n, window, sinks, scale):
 def tolerance(y, weighed, most, D, length):
     """Bound on |Y - y|.  The result is rounded to bf16 (2^-8 of it), and so are the weights (2^-8 of each; their sum is not).  The scores: D products
     summed in fp32, whose additions may cut off instead of rounding (2^-23 of the sums so far each), and three roundings more, an error of a score
-    is one of its weight; exp2 is good to 2^-22.  Weights and sums over the tokens: 2^-23 for each addition, the joining of parts among them, as
+    is one of its weight; exp2 is good to 2^-22, or, where a polynomial of third degree takes its
+    place (prompts), to 7.5e-5: the largest |q(f) / 2^f - 1| over [-1/2, 1/2], with a few roundings of 2^-24.  Weights and sums over the tokens: 2^-23 for each addition, the joining of parts among them, as
     many again.  Errors of the weights count twice, in the sum of values and in the sum of weights."""
-    weight = (D + 3) * 2.0 ** -23 * most + 2.0 ** -22
+    weight = (D + 3) * 2.0 ** -23 * most + 7.6e-5
     return 2.0 ** -8 * y.abs() * 1.01 + (2.0 ** -8 + 2 * weight + 2 * length * 2.0 ** -23) * weighed * 1.01 + 2.0 ** -126
 
 
