@@ -54,18 +54,19 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
   asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
                ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w) : "memory");
 }
-// Descriptor of the values as the MMA's second operand: columns along memory, 64 to a swizzled row; 8 keys are 1024 bytes, the next 64 columns a half
-// tile away.
-__device__ __forceinline__ uint64_t values_desc(uint32_t saddr, int half) {
-  return (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(half >> 4) << 16 | (uint64_t)(1024 >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)2 << 61;
+// Descriptors in halves: of an MMA's operands only the low words, with the addresses, change from MMA to MMA.  Queries and keys: rows along the
+// contraction, 128 bytes of it swizzled, 8 rows 1024 bytes apart.  Values as the second operand: their columns along memory, 64 to a swizzled row; 8 keys
+// are 1024 bytes, and the next 64 columns lie a half tile on.
+constexpr uint32_t kDescHigh = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ __forceinline__ uint32_t rows_desc(uint32_t saddr) { return ((saddr & 0x3FFFFu) >> 4) | 1u << 16; }
+__device__ __forceinline__ uint32_t values_desc(uint32_t saddr, int half) { return ((saddr & 0x3FFFFu) >> 4) | (uint32_t)(half >> 4) << 16; }
+__device__ __forceinline__ void mma_ss(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 a, b;\n setp.ne.b32 p, %5, 0;\n mov.b64 a, {%1, %3};\n mov.b64 b, {%2, %3};\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %4, p;\n}\n" ::"r"(d), "r"(a), "r"(b), "r"(kDescHigh), "r"(idesc), "r"(acc) : "memory");
 }
-__device__ __forceinline__ void mma_ss(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n"
-               ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
-}
-__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n"
-               ::"r"(d), "r"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+__device__ __forceinline__ void mma_ts(uint32_t d, uint32_t a, uint32_t b, uint32_t idesc, uint32_t acc) {
+  asm volatile("{\n .reg .pred p;\n .reg .b64 b;\n setp.ne.b32 p, %5, 0;\n mov.b64 b, {%2, %3};\n"
+               " tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], b, %4, p;\n}\n" ::"r"(d), "r"(a), "r"(b), "r"(kDescHigh), "r"(idesc), "r"(acc) : "memory");
 }
 __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
@@ -103,6 +104,9 @@ __device__ __forceinline__ void exp2_poly(F2 x, float& a, float& b) {
   a = __uint_as_float((__float_as_uint(ra) << 23) + __float_as_uint(qa));
   b = __uint_as_float((__float_as_uint(rb) << 23) + __float_as_uint(qb));
 }
+
+template <int N> struct Every { static constexpr int value = N; };
+constexpr int kPolyEvery = 4;
 
 // What a CTA works on: 256 rows of a request's key head from `base` on, the first of them head `head0` of the group of token `token0`.
 struct Item { int request, head, row0, n, len, base, rows, token0, head0; };      // rows: n * group
@@ -361,32 +365,40 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       }
       const float base = m == -INFINITY ? 0.f : -m * c;
       const F2 base2 = f2(base, base);
+      // weights of columns 64 h .. + 63, and word to the issuer, which may begin with the first half; POLY: every POLY-th pair by the polynomial
+      auto weights = [&](auto every, int h) {
+        constexpr int POLY = decltype(every)::value;
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        uint32_t w[16];
+        for (int k = 2 * h; k < 2 * h + 2; ++k) {
+          uint32_t w[16];
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const F2 x = fma2(f2(v[32 * k + 2 * i], v[32 * k + 2 * i + 1]), c2, base2);
-          float a, b;
-          if (i % 4 == 3 && !masked) {
-            exp2_poly(x, a, b);
-          } else {
-            unf2(x, a, b);
-            a = exp2_fast(a);
-            b = exp2_fast(b);
+          for (int i = 0; i < 16; ++i) {
+            const F2 x = fma2(f2(v[32 * k + 2 * i], v[32 * k + 2 * i + 1]), c2, base2);
+            float a, b;
+            if (POLY > 0 && i % (POLY > 0 ? POLY : 1) == POLY - 1) {
+              exp2_poly(x, a, b);
+            } else {
+              unf2(x, a, b);
+              a = exp2_fast(a);
+              b = exp2_fast(b);
+            }
+            if (i % 2) lb = add2(lb, f2(a, b));
+            else la = add2(la, f2(a, b));
+            w[i] = round_bf16x2(a, b);                            // as in lqer_attention.cu: the weights are rounded, their sum is not
           }
-          if (i % 2) lb = add2(lb, f2(a, b));
-          else la = add2(la, f2(a, b));
-          w[i] = round_bf16x2(a, b);                              // as in lqer_attention.cu: the weights are rounded, their sum is not
+          tmem_st16(s_at + 16 * k, w);
         }
-        tmem_st16(s_at + 16 * k, w);
-        if (k % 2) {
-          // the issuer may begin with the first half
-          tmem_st_wait();
-          tc::tc_fence_before();
-          __syncwarp();
-          if (lane == 0) tc::mbar_arrive(bar_of(k == 1 ? bars.p_half[t] : bars.p_full[t]));
-        }
+        tmem_st_wait();
+        tc::tc_fence_before();
+        __syncwarp();
+        if (lane == 0) tc::mbar_arrive(bar_of(h == 0 ? bars.p_half[t] : bars.p_full[t]));
+      };
+      if (masked) {
+        weights(Every<0>{}, 0);
+        weights(Every<0>{}, 1);
+      } else {
+        weights(Every<kPolyEvery>{}, 0);
+        weights(Every<kPolyEvery>{}, 1);
       }
       ++n;
     }
@@ -488,54 +500,64 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   } else if (warp == SH::ISSUER) {
     if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
-    if (lane == 0) {
-      const uint32_t s_idesc = tc::make_idesc(128, 128) | (s.negate ? 1u << 13 : 0u), o_idesc = tc::make_idesc(128, D) | 1u << 16;
-      int n[2] = {0, 0};                                           // key tiles whose O is under way
-      ok = tc::mbar_wait(bar_of(bars.q_full), 0, &ws);
-      for (int j = 0; j <= plan.count && ok; ++j) {
-        const int v_at = (2 * j - 1) % SH::STAGES, k_at = 2 * j % SH::STAGES;
-        if (j > 0) ok = tc::mbar_wait(bar_of(bars.full[v_at]), (2 * j - 1) / SH::STAGES & 1, &ws);
-        bool keys_there = false;
+    // The whole warp walks along, so that addresses stay in uniform registers; one lane issues.
+    const bool leader = tc::elect_one();
+    const uint32_t s_idesc = tc::make_idesc(128, 128) | (s.negate ? 1u << 13 : 0u), o_idesc = tc::make_idesc(128, D) | 1u << 16;
+    const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
+    auto all = [&](bool got) { ok = __all_sync(0xFFFFFFFFu, got) != 0; return ok; };
+    int n[2] = {0, 0};                                             // key tiles whose O is under way
+    int at = 0;                                                    // place in the ring, and how often it has been round: of K(j), V(j - 1) before it
+    uint32_t phase = 0;
+    all(tc::mbar_wait(bar_of(bars.q_full), 0, &ws));
+    for (int j = 0; j <= plan.count && ok; ++j) {
+      const int v_at = at;
+      if (j > 0) {
+        if (!all(tc::mbar_wait(bar_of(bars.full[v_at]), phase, &ws))) break;
+        if (++at == SH::STAGES) { at = 0; phase ^= 1; }
+      }
+      const int k_at = at;
+      const uint32_t k_phase = phase;
+      bool keys_there = false;
 #pragma unroll
-        for (int t = 0; t < 2; ++t) {
-          if (!ok) break;
-          if (j > 0 && plan.sees(t, plan.tile(j - 1))) {
+      for (int t = 0; t < 2; ++t) {
+        if (j > 0 && plan.sees(t, plan.tile(j - 1))) {
 #pragma unroll
-            for (int half = 0; half < 2; ++half) {
-              ok = tc::mbar_wait(bar_of(half ? bars.p_full[t] : bars.p_half[t]), n[t] & 1, &ws);
-              if (!ok) break;
-              tc::tc_fence_after();
+          for (int half = 0; half < 2; ++half) {
+            if (!all(tc::mbar_wait(bar_of(half ? bars.p_full[t] : bars.p_half[t]), n[t] & 1, &ws))) break;
+            tc::tc_fence_after();
+            if (leader) {
 #pragma unroll
               for (int k = 4 * half; k < 4 * half + 4; ++k)
-                mma_ts(tmem + SH::O_COL + t * D, tmem + SH::S_COL + t * 128 + 8 * k, values_desc(ring_at + v_at * SH::TILE + k * 2048, SH::HALF), o_idesc,
-                       n[t] > 0 || k > 0 ? 1u : 0u);
+                mma_ts(base + SH::O_COL + t * D, base + SH::S_COL + t * 128 + 8 * k, values_desc(ring_at + v_at * SH::TILE, SH::HALF) + k * 128, o_idesc,
+                       k > 0 ? 1u : n[t] > 0 ? 1u : 0u);
+              if (half) tc::umma_commit(bar_of(bars.o_done[t]));
             }
-            if (!ok) break;
-            tc::umma_commit(bar_of(bars.o_done[t]));
-            ++n[t];
           }
-          if (j < plan.count) {
-            if (!keys_there) {
-              ok = tc::mbar_wait(bar_of(bars.full[k_at]), 2 * j / SH::STAGES & 1, &ws);
-              if (!ok) break;
-              tc::tc_fence_after();
-              keys_there = true;
-            }
-            if (plan.sees(t, plan.tile(j))) {
+          if (!ok) break;
+          ++n[t];
+        }
+        if (j < plan.count) {
+          if (!keys_there) {
+            if (!all(tc::mbar_wait(bar_of(bars.full[k_at]), k_phase, &ws))) break;
+            tc::tc_fence_after();
+            keys_there = true;
+          }
+          if (plan.sees(t, plan.tile(j)) && leader) {
 #pragma unroll
-              for (int k = 0; k < D / 16; ++k) {
-                const uint32_t off = (k >> 2) * SH::HALF + (k & 3) * 32;
-                mma_ss(tmem + SH::S_COL + t * 128, tc::make_desc(q_at + t * SH::TILE + off), tc::make_desc(ring_at + k_at * SH::TILE + off), s_idesc,
-                       k > 0 ? 1u : 0u);
-              }
-              tc::umma_commit(bar_of(bars.s_full[t]));
+            for (int k = 0; k < D / 16; ++k) {
+              const uint32_t off = (k >> 2) * (SH::HALF >> 4) + (k & 3) * 2;
+              mma_ss(base + SH::S_COL + t * 128, rows_desc(q_at + t * SH::TILE) + off, rows_desc(ring_at + k_at * SH::TILE) + off, s_idesc, k > 0 ? 1u : 0u);
             }
+            tc::umma_commit(bar_of(bars.s_full[t]));
           }
         }
-        if (!ok) break;
+      }
+      if (!ok) break;
+      if (leader) {
         if (j > 0) tc::umma_commit(bar_of(bars.empty[v_at]));
         if (j < plan.count) tc::umma_commit(bar_of(bars.empty[k_at]));
       }
+      if (++at == SH::STAGES) { at = 0; phase ^= 1; }
     }
   } else {
     if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
@@ -576,7 +598,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         drain(bar_of(MX ? bars.raw_full[last % PLACES] : bars.full[last % PLACES]), last / PLACES & 1);
       }
     }
-    if (warp == SH::ISSUER && lane == 0) {
+    if (warp == SH::ISSUER && tc::elect_one()) {
       tc::umma_commit(bar_of(bars.drained));
       drain(bar_of(bars.drained), 0);
     }
