@@ -6,9 +6,10 @@
 //
 // The rows of the query heads that share a key head, of all of a request's new tokens, go together (a row tile of 8 NT): the keys
 // and values are read once for them.  Bound: those bytes.  The products are far from any limit, so they are mma.sync m16n8k16 with the keys (and
-// the values' columns) on the 16-row side and the row tile on the 8-column side, which wastes least of it, and the operands come straight
-// from memory to registers: within a dot product the order of the elements is free, so a lane takes 16 consecutive bytes of a key, and
-// of four keys' values, and both sides use the order that this gives.  No shared memory, no barrier between the keys.
+// the values' columns) on the 16-row side and the row tile on the 8-column side, which wastes least of it.  Within a dot product the order of the
+// elements is free, so a lane takes 16 consecutive bytes of a key (8 of an MXINT8 one), and of four keys' values, and both sides use the order that this gives.
+// Each warp has a ring of its own in shared memory, which asynchronous copies fill ahead of it: no barrier between the keys, and what is on its way
+// takes no registers.  Of MXINT8 the mantissas become bf16 on their way from there (exact), two at a time.
 //
 // Work is counted in chunks of 64 keys of a (request, key head, row tile), all in one row; each CTA takes an equal run of them, wherever that begins
 // and ends, so lengths may differ as they like.  The four warps take 16 keys of every chunk and join at the end of a run's part; what is not a
@@ -96,88 +97,59 @@ __device__ __forceinline__ uint32_t transposed(uint32_t w) {
   asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(d) : "r"(w));
   return d;
 }
-__device__ __forceinline__ uint4 once16(const void* p) {
-  uint4 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint2 once8(const void* p) {
-  uint2 v;
-  asm volatile("ld.global.nc.L1::no_allocate.v2.u32 {%0, %1}, [%2];" : "=r"(v.x), "=r"(v.y) : "l"(p));
-  return v;
-}
-__device__ __forceinline__ uint32_t byte_of(uint2 w, int i) { return ((i < 4 ? w.x : w.y) >> (8 * (i & 3))) & 0xFFu; }
+__device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(from) : "memory"); }
+__device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// Eight elements of a key or of a value: bf16, or mantissas until they are used.
-template <bool MX> struct Oct { uint4 w; };
-template <> struct Oct<true> { uint2 w; };
-// A warp's 16 keys: of key lane / 4 (+ 8) the octets at 8 (lane % 4) + 32 j.
-template <int D, bool MX>
-struct Keys {
-  Oct<MX> k[2][D / 32];
-  uint2 e[MX ? 2 : 1];         // the keys' exponent bytes
-  __device__ __forceinline__ void load(const Attention& p, size_t row, int lane) {      // row: of the first key, in a [.., D] tensor
+template <bool MX> struct OctOf { using type = uint4; };
+template <> struct OctOf<true> { using type = uint2; };
+// A warp's ring: stages of 16 keys and their values as they lie in the cache (and their exponents behind each), their 16-byte pieces moved within a row so
+// that no two lanes that read together meet on a bank.
+template <int D, bool MX, int NT>
+struct Ring {
+  static constexpr int ROWS = 8 * NT, ROW = MX ? D : 2 * D, PIECES = ROW / 16, SET = 16 * ROW, EXPS = MX ? D : 0, STAGE = 2 * (SET + EXPS);
+  static constexpr int STAGES = MX ? 4 : 2, WARP = STAGES * STAGE;
+  static constexpr int OUT = ROWS * (D + 4);                          // floats of a warp's sums, then its maxima and sums of weights: over its ring at the end
+  static constexpr int CTAS = D == 64 ? 4 : 3;
+  static_assert((OUT + 2 * ROWS) * 4 <= WARP, "a warp's sums fit its ring");
+  __device__ static __forceinline__ int key_swizzle(int row) { return MX ? (D == 128 ? (row & 3) << 1 : ((row >> 1) & 1) << 1) : (row & 1) << 2 | ((row >> 1) & 3); }
+  __device__ static __forceinline__ int value_swizzle(int row) { return MX && D == 64 ? ((row >> 1) & 1) << 1 : ((row >> 1) & 3) << 1; }
+  // Sends a stage on its way: 16 rows from `row` on of the [.., D] tensors, which lie one after the other.
+  __device__ static __forceinline__ void fill(const Attention& p, uint32_t at, size_t row, int lane) {
+    const uint8_t* k = static_cast<const uint8_t*>(p.keys) + row * ROW + 16 * lane;
+    const uint8_t* v = static_cast<const uint8_t*>(p.values) + row * ROW + 16 * lane;
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const size_t at = (row + lane / 4 + 8 * i) * D + 8 * (lane & 3);
-#pragma unroll
-      for (int j = 0; j < D / 32; ++j) {
-        if constexpr (MX) k[i][j].w = once8(static_cast<const uint8_t*>(p.keys) + at + 32 * j);
-        else k[i][j].w = once16(static_cast<const uint16_t*>(p.keys) + at + 32 * j);
-      }
-      if constexpr (MX) {
-        const uint8_t* x = p.key_exps + (row + lane / 4 + 8 * i) * (D / 16);
-        if (D == 128) e[i] = __ldg(reinterpret_cast<const uint2*>(x));
-        else e[i] = make_uint2(__ldg(reinterpret_cast<const uint32_t*>(x)), 0u);
-      }
+    for (int i = 0; i < SET / 512; ++i) {
+      const int x = lane + 32 * i, r = x / PIECES, c = x % PIECES;
+      copy16(at + r * ROW + ((c ^ key_swizzle(r)) << 4), k + 512 * i);
+      copy16(at + SET + EXPS + r * ROW + ((c ^ value_swizzle(r)) << 4), v + 512 * i);
     }
-  }
-  __device__ __forceinline__ uint4 octet(const Attention& p, int i, int j, int lane) const {
-    if constexpr (MX) return mantissas8(k[i][j].w, mantissa_scale(byte_of(e[i], 2 * j + ((lane & 3) >> 1)), p.emin + 127, p.emax + 127, p.bits - 2));
-    else return k[i][j].w;
+    if (MX && lane < 2 * EXPS / 16) {
+      const int which = lane >= EXPS / 16, x = lane - which * (EXPS / 16);
+      copy16(at + SET + which * (SET + EXPS) + 16 * x, (which ? p.value_exps : p.key_exps) + row * (D / 16) + 16 * x);
+    }
   }
 };
-// Of keys 2 (lane % 4) + {0, 1, 8, 9} the values of columns 8 (lane / 4) .. + 7, and of those 64 further on.
+// The eight elements of a key's octet j of a lane as pairs; MXINT8: pairs (0, 2), (1, 3), (4, 6), (5, 7), the other way without permutes.
 template <int D, bool MX>
-struct Values {
-  static constexpr int H = D / 64;
-  Oct<MX> v[4][H];
-  uint2 e[MX ? 4 : 1];
-  __device__ __forceinline__ void load(const Attention& p, size_t row, int lane) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const size_t key = row + 2 * (lane & 3) + (i & 1) + 8 * (i >> 1), at = key * D + 8 * (lane >> 2);
-#pragma unroll
-      for (int h = 0; h < H; ++h) {
-        if constexpr (MX) v[i][h].w = once8(static_cast<const uint8_t*>(p.values) + at + 64 * h);
-        else v[i][h].w = once16(static_cast<const uint16_t*>(p.values) + at + 64 * h);
-      }
-      if constexpr (MX) {
-        const uint8_t* x = p.value_exps + key * (D / 16);
-        if (D == 128) e[i] = __ldg(reinterpret_cast<const uint2*>(x));
-        else e[i] = make_uint2(__ldg(reinterpret_cast<const uint32_t*>(x)), 0u);
-      }
-    }
+__device__ __forceinline__ uint4 key_octet(const uint8_t* keys, int row, int j, int lane, int swizzle, uint2 exps, int shift) {
+  const int c = lane & 3;
+  if constexpr (MX) {
+    const uint2 w = *reinterpret_cast<const uint2*>(keys + row * D + (((2 * j + (c >> 1)) ^ swizzle) << 4) + 8 * (c & 1));
+    const MantissaScale s = mantissa_scale(((j & 2 ? exps.y : exps.x) >> (16 * (j & 1) + 8 * (c >> 1))) & 0xFFu, shift);
+    return make_uint4(mantissas_bf16x2(w.x, s), mantissas_bf16x2(byte_down(w.x), s), mantissas_bf16x2(w.y, s), mantissas_bf16x2(byte_down(w.y), s));
+  } else {
+    return *reinterpret_cast<const uint4*>(keys + row * 2 * D + (((4 * j + c) ^ swizzle) << 4));
   }
-  __device__ __forceinline__ void clear(int i) {
-#pragma unroll
-    for (int h = 0; h < H; ++h) {
-      if constexpr (MX) v[i][h].w = make_uint2(0u, 0u);
-      else v[i][h].w = make_uint4(0u, 0u, 0u, 0u);
-    }
-  }
-  __device__ __forceinline__ uint4 octet(const Attention& p, int i, int h, int lane) const {
-    if constexpr (MX) return mantissas8(v[i][h].w, mantissa_scale(byte_of(e[i], 4 * h + (lane >> 3)), p.emin + 127, p.emax + 127, p.bits - 2));
-    else return v[i][h].w;
-  }
-};
+}
 __device__ __forceinline__ uint32_t word_of(const uint4& v, int i) { return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w; }
+__device__ __forceinline__ uint32_t word_of(const uint2& v, int i) { return i == 0 ? v.x : v.y; }
 
 template <int D, bool MX, int NT>
-__global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(const Split s) {
-  constexpr int ROWS = 8 * NT, T = D / 16;               // T: tiles of 16 columns of the output
-  __shared__ float sm_o[kWarps][ROWS][D + 4];
-  __shared__ float sm_m[kWarps][ROWS], sm_l[kWarps][ROWS];
+__global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_kernel(const Split s) {
+  using R = Ring<D, MX, NT>;
+  constexpr int ROWS = 8 * NT, T = D / 16, H = D / 64;   // T: tiles of 16 columns of the output; H: octets of values a lane takes of a key
+  extern __shared__ __align__(128) uint8_t rings[];
   __shared__ Run sm_run;
   const Attention& p = s.a;
   tc::pdl_launch_dependents();
@@ -189,7 +161,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
   long long u = run.per * blockIdx.x;
   const long long end = min(u + run.per, run.total);
   if (u >= end) return;
+  uint8_t* const ring = rings + warp * R::WARP;
+  const uint32_t ring_at = tc::smem_u32(ring);
   const StepRequest* reqs = requests_of(p.step);
+  const int shift = p.bits - 2;
   int r = run.request;
   long long before = run.before;
   while (u < end) {
@@ -203,6 +178,23 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
     const int h = (int)(which / tiles), tile = (int)(which % tiles), c0 = (int)(local - which * vis.chunks);
     const int c1 = (int)min((long long)vis.chunks, c0 + (end - u));
     const int rows = min(ROWS, n * p.group - tile * ROWS), first_pos = len - n;
+    // chunk of the run -> first of the warp's keys
+    auto key_of = [&](int chunk) { return ((chunk < vis.sink_chunks ? chunk : vis.first_chunk + chunk - vis.sink_chunks)) * kChunk + warp * 16; };
+    const int* table = p.tables + (size_t)r * p.max_pages;
+    auto entry_of = [&](int chunk) {
+      const int key = key_of(chunk);
+      return chunk < c1 && key < len ? __ldg(table + (key >> p.page_shift)) : 0;
+    };
+    int entry = entry_of(c0);                             // of the chunk that is sent next
+    auto send = [&](int chunk) {
+      const int key = key_of(chunk);
+      if (chunk < c1 && key < len)
+        R::fill(p, ring_at + (chunk - c0) % R::STAGES * R::STAGE, (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (key & (p.page - 1)), lane);
+      copies_sent();
+      entry = entry_of(chunk + 1);
+    };
+#pragma unroll
+    for (int i = 0; i < R::STAGES - 1; ++i) send(c0 + i);
     // the row tile's queries, in the order in which a lane holds a key
     uint4 q[NT][D / 32];
     int pos[NT][2];
@@ -215,6 +207,10 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
         if (8 * t + g < rows)
           q[t][j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + (size_t)(row0 + x / p.group) * p.q_stride +
                                                          (size_t)(h * p.group + x % p.group) * D + 8 * c + 32 * j));
+        if (MX) {
+          const uint4 w = q[t][j];
+          q[t][j] = make_uint4(__byte_perm(w.x, w.y, 0x5410), __byte_perm(w.x, w.y, 0x7632), __byte_perm(w.z, w.w, 0x5410), __byte_perm(w.z, w.w, 0x7632));
+        }
       }
 #pragma unroll
       for (int i = 0; i < 2; ++i) pos[t][i] = first_pos + (tile * ROWS + 8 * t + 2 * c + i) / p.group;
@@ -228,46 +224,35 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
       m[t][0] = m[t][1] = -INFINITY;
       l[t][0] = l[t][1] = 0.f;
     }
-    // chunk of the run -> first of the warp's keys
-    auto key_of = [&](int chunk) { return ((chunk < vis.sink_chunks ? chunk : vis.first_chunk + chunk - vis.sink_chunks)) * kChunk + warp * 16; };
-    const int* table = p.tables + (size_t)r * p.max_pages;
-    auto entry_of = [&](int chunk) {
-      const int key = key_of(chunk);
-      return chunk < c1 && key < len ? __ldg(table + (key >> p.page_shift)) : 0;
-    };
-    auto row_of = [&](int chunk, int entry) {
-      const int key = key_of(chunk);
-      return (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (key & (p.page - 1));
-    };
-    Keys<D, MX> K;
-    Values<D, MX> V;
-    int entry = entry_of(c0), next_entry = entry_of(c0 + 1);
-    if (key_of(c0) < len) {
-      const size_t at = row_of(c0, entry);
-      K.load(p, at, lane);
-      V.load(p, at, lane);
-    }
     for (int chunk = c0; chunk < c1; ++chunk) {
       const int key0 = key_of(chunk);
-      if (key0 >= len) break;                           // the last chunk's end
+      if (key0 >= len) break;                             // the last chunk's end
+      send(chunk + R::STAGES - 1);
+      copies_wait<R::STAGES - 1>();
+      __syncwarp();
+      const uint8_t* const keys = ring + (chunk - c0) % R::STAGES * R::STAGE;
+      const uint8_t* const values = keys + R::SET + R::EXPS;
       float sc[NT][4];
 #pragma unroll
       for (int t = 0; t < NT; ++t) sc[t][0] = sc[t][1] = sc[t][2] = sc[t][3] = 0.f;
+      uint2 ke[2] = {make_uint2(0u, 0u), make_uint2(0u, 0u)};
+      if constexpr (MX) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          const uint8_t* x = keys + R::SET + (g + 8 * i) * (D / 16);
+          if (D == 128) ke[i] = *reinterpret_cast<const uint2*>(x);
+          else ke[i].x = *reinterpret_cast<const uint32_t*>(x);
+        }
+      }
 #pragma unroll
       for (int j = 0; j < D / 32; ++j) {
-        const uint4 a = K.octet(p, 0, j, lane), b = K.octet(p, 1, j, lane);
+        const uint4 a = key_octet<D, MX>(keys, g, j, lane, R::key_swizzle(g), ke[0], shift);
+        const uint4 b = key_octet<D, MX>(keys, g + 8, j, lane, R::key_swizzle(g + 8), ke[1], shift);
 #pragma unroll
         for (int t = 0; t < NT; ++t) {
           mma(sc[t], a.x, b.x, a.y, b.y, q[t][j].x, q[t][j].y);
           mma(sc[t], a.z, b.z, a.w, b.w, q[t][j].z, q[t][j].w);
         }
-      }
-      const bool more = chunk + 1 < c1 && key_of(chunk + 1) < len;
-      size_t next_at = 0;
-      if (more) {
-        next_at = row_of(chunk + 1, next_entry);
-        K.load(p, next_at, lane);
-        next_entry = entry_of(chunk + 2);
       }
       const bool masked = key0 + 15 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
 #pragma unroll
@@ -280,14 +265,6 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
             const int key = key0 + g + 8 * (i >> 1), at = pos[t][i & 1];
             if (key > at || (p.window > 0 && key <= at - p.window && key >= p.sinks)) sc[t][i] = -INFINITY;
           }
-        }
-      }
-      if (masked) {
-        // values that no row sees may be anything: 0 times that has to be 0
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int key = key0 + 2 * c + (i & 1) + 8 * (i >> 1);
-          if (key >= len || (key < seen_from && key >= p.sinks)) V.clear(i);
         }
       }
       uint32_t pb[NT][2];
@@ -321,31 +298,69 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
         for (int i = 0; i < 4; ++i) e[i] = exp2_fast(sc[t][i] - base[i & 1]);
         l[t][0] += e[0] + e[2];
         l[t][1] += e[1] + e[3];
-        // the weights enter the product rounded to bf16, 2^-9 either way, as the values do that they weigh; their sum does not
+        // the weights enter the product rounded to bf16, 2^-8 of each at most, as the values do that they weigh; their sum does not
         pb[t][0] = transposed(round_bf16x2(e[0], e[1]));
         pb[t][1] = transposed(round_bf16x2(e[2], e[3]));
       }
-      uint4 v[4][D / 64];
+      // of keys 2 c + {0, 1, 8, 9} the values of columns 8 g .. + 7, and of those 64 further on
+      using Oct = typename OctOf<MX>::type;
+      Oct v[4][H];
+      uint2 ve[4] = {};
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
+      for (int i = 0; i < 4; ++i) {
+        const int row = 2 * c + (i & 1) + 8 * (i >> 1);
 #pragma unroll
-        for (int k = 0; k < D / 64; ++k) v[i][k] = V.octet(p, i, k, lane);
+        for (int k = 0; k < H; ++k) {
+          const int piece = MX ? (g >> 1) + 4 * k : g + 8 * k;
+          v[i][k] = *reinterpret_cast<const Oct*>(values + row * R::ROW + ((piece ^ R::value_swizzle(row)) << 4) + (MX ? 8 * (g & 1) : 0));
+        }
+        if constexpr (MX) {
+          const uint8_t* x = values + R::SET + row * (D / 16);
+          if (D == 128) ve[i] = *reinterpret_cast<const uint2*>(x);
+          else ve[i].x = *reinterpret_cast<const uint32_t*>(x);
+        }
+        if (masked) {
+          // values that no row sees may be anything: 0 times that has to be 0
+          const int key = key0 + row;
+          if (key >= len || (key < seen_from && key >= p.sinks)) {
+#pragma unroll
+            for (int k = 0; k < H; ++k) v[i][k] = Oct{};
+            ve[i] = make_uint2(0x7F7F7F7Fu, 0x7F7F7F7Fu);
+          }
+        }
+      }
+      MantissaScale vs[2][H];                             // MXINT8: the scales of a pair of keys
+      if constexpr (MX) {
+        const uint32_t pick = (uint32_t)(g >> 1) * 0x1111u + 0x4400u;
+#pragma unroll
+        for (int k = 0; k < H; ++k)
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            vs[i][k] = mantissa_scales(__byte_perm(word_of(ve[2 * i], k), word_of(ve[2 * i + 1], k), pick) & 0x00FF00FFu, shift);
+      }
+      // column x (of the eight of octet k) of keys 2 c + 8 i and the next one
+      auto pair_of = [&](int i, int k, int x) {
+        if constexpr (MX) {
+          const uint32_t two = __byte_perm(word_of(v[2 * i][k], x >> 2), word_of(v[2 * i + 1][k], x >> 2), x & 2 ? 0x7632 : 0x5410);
+          return mantissas_bf16x2(x & 1 ? byte_down(two) : two, vs[i][k]);
+        } else {
+          return __byte_perm(word_of(v[2 * i][k], x >> 1), word_of(v[2 * i + 1][k], x >> 1), x & 1 ? 0x7632 : 0x5410);
+        }
+      };
 #pragma unroll
       for (int i = 0; i < T; ++i) {
-        // column i (of eight) of both halves; heads of 64: i and i + 4
-        constexpr int H = D / 64 - 1;
-        const int lo = i, hi = D == 128 ? i : i + 4;
-        const uint32_t pick_lo = lo & 1 ? 0x7632 : 0x5410, pick_hi = hi & 1 ? 0x7632 : 0x5410;
-        const uint32_t a0 = __byte_perm(word_of(v[0][0], lo / 2), word_of(v[1][0], lo / 2), pick_lo);
-        const uint32_t a1 = __byte_perm(word_of(v[0][H], hi / 2), word_of(v[1][H], hi / 2), pick_hi);
-        const uint32_t a2 = __byte_perm(word_of(v[2][0], lo / 2), word_of(v[3][0], lo / 2), pick_lo);
-        const uint32_t a3 = __byte_perm(word_of(v[2][H], hi / 2), word_of(v[3][H], hi / 2), pick_hi);
+        // column i of both halves; heads of 64: i and i + 4
+        const int hi = D == 128 ? i : i + 4;
+        const uint32_t a0 = pair_of(0, 0, i), a1 = pair_of(0, H - 1, hi), a2 = pair_of(1, 0, i), a3 = pair_of(1, H - 1, hi);
 #pragma unroll
         for (int t = 0; t < NT; ++t) mma(o[t][i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
       }
-      if (more) V.load(p, next_at, lane);
+      __syncwarp();                                       // the stage may be filled again
     }
+    copies_wait<0>();
+    __syncwarp();
     // the four warps' parts
+    float* const out = reinterpret_cast<float*>(ring);
 #pragma unroll
     for (int t = 0; t < NT; ++t) {
 #pragma unroll
@@ -353,17 +368,16 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
 #pragma unroll
         for (int x = 4; x < 32; x <<= 1) l[t][i] += __shfl_xor_sync(0xFFFFFFFFu, l[t][i], x);
         const int row = 8 * t + 2 * c + i;
-        if (g == 0) { sm_m[warp][row] = m[t][i]; sm_l[warp][row] = l[t][i]; }
-        float* to = sm_o[warp][row];
-        if (D == 128) {
-          float4* a = reinterpret_cast<float4*>(to + 8 * g);
+        if (g == 0) { out[R::OUT + row] = m[t][i]; out[R::OUT + ROWS + row] = l[t][i]; }
+        float* to = out + row * (D + 4) + 8 * g;
+        float4* a = reinterpret_cast<float4*>(to);
+        if constexpr (D == 128) {
+          float4* b = reinterpret_cast<float4*>(to + 64);
           a[0] = make_float4(o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]);
-          a[1] = make_float4(o[t][T > 4 ? 4 : 0][i], o[t][T > 4 ? 5 : 0][i], o[t][T > 4 ? 6 : 0][i], o[t][T > 4 ? 7 : 0][i]);
-          float4* b = reinterpret_cast<float4*>(to + D / 2 + 8 * g);
+          a[1] = make_float4(o[t][4][i], o[t][5][i], o[t][6][i], o[t][7][i]);
           b[0] = make_float4(o[t][0][i + 2], o[t][1][i + 2], o[t][2][i + 2], o[t][3][i + 2]);
-          b[1] = make_float4(o[t][T > 4 ? 4 : 0][i + 2], o[t][T > 4 ? 5 : 0][i + 2], o[t][T > 4 ? 6 : 0][i + 2], o[t][T > 4 ? 7 : 0][i + 2]);
+          b[1] = make_float4(o[t][4][i + 2], o[t][5][i + 2], o[t][6][i + 2], o[t][7][i + 2]);
         } else {
-          float4* a = reinterpret_cast<float4*>(to + 8 * g);
           a[0] = make_float4(o[t][0][i], o[t][1][i], o[t][2][i], o[t][3][i]);
           a[1] = make_float4(o[t][0][i + 2], o[t][1][i + 2], o[t][2][i + 2], o[t][3][i + 2]);
         }
@@ -372,20 +386,21 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
     __syncthreads();
     const bool whole = c0 == 0 && c1 == vis.chunks;
     float* part = s.parts + (size_t)(2 * blockIdx.x + (c0 > 0 ? 0 : 1)) * ROWS * (D + 2);
+    auto of_warp = [&](int w) { return reinterpret_cast<const float*>(rings + w * R::WARP); };
     for (int i = tid; i < rows * (D / 4); i += kSplitThreads) {
       const int row = i / (D / 4), d = 4 * (i % (D / 4));
       float big = -INFINITY;
 #pragma unroll
-      for (int w = 0; w < kWarps; ++w) big = fmaxf(big, sm_m[w][row]);
+      for (int w = 0; w < kWarps; ++w) big = fmaxf(big, of_warp(w)[R::OUT + row]);
       const float base = big == -INFINITY ? 0.f : big;
       float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
       float all = 0.f;
 #pragma unroll
       for (int w = 0; w < kWarps; ++w) {
-        const float f = exp2_fast(sm_m[w][row] - base);
-        const float4 x = *reinterpret_cast<const float4*>(&sm_o[w][row][d]);
+        const float f = exp2_fast(of_warp(w)[R::OUT + row] - base);
+        const float4 x = *reinterpret_cast<const float4*>(of_warp(w) + row * (D + 4) + d);
         sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
-        all += f * sm_l[w][row];
+        all += f * of_warp(w)[R::OUT + ROWS + row];
       }
       if (whole) {
         const float inv = all == 0.f ? 0.f : 1.f / all;
@@ -407,43 +422,81 @@ __global__ void __launch_bounds__(kSplitThreads, NT == 1 ? 3 : 2) split_kernel(c
   }
 }
 
-// Joins the parts of the row tile that begins in a CTA's run: blockIdx.y takes one row.
+// Joins the parts of the row tile that begins in a CTA's run.  A thread takes four columns of a row, and where the rows leave threads over, several take a
+// share of the parts each, in order; few CTAs with much to do each, for most have nothing.
+constexpr int kJoinThreads = 512;
 template <int D, int NT>
-__global__ void __launch_bounds__(D) join_kernel(const Split s) {
-  constexpr int ROWS = 8 * NT;
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(const Split s) {
+  constexpr int ROWS = 8 * NT, QUADS = D / 4;
+  __shared__ float4 sums[kJoinThreads];
+  __shared__ float2 tops[kJoinThreads];                  // a thread's maximum, and its sum of weights
   const Attention& p = s.a;
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   const Span span = s.spans[blockIdx.x];
   if (span.parts == 0) return;
   const int4 req = __ldg(reinterpret_cast<const int4*>(requests_of(p.step) + span.request));
-  const int row = blockIdx.y, x = span.tile * ROWS + row, d = threadIdx.x;
-  if (x >= req.y * p.group) return;
+  const int rows = min(ROWS, req.y * p.group - span.tile * ROWS), items = rows * QUADS, shares = kJoinThreads / items;
+  const int tid = threadIdx.x, share = tid / items, item = tid - share * items, row = item / QUADS, d = 4 * (item - row * QUADS);
+  const int per = (span.parts + shares - 1) / shares, from = share * per, to = share < shares ? min(from + per, span.parts) : from;
   auto part = [&](int i) { return s.parts + (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * ROWS * (D + 2); };
-  float big = -INFINITY;
-  for (int i = 0; i < span.parts; ++i) big = fmaxf(big, part(i)[ROWS * D + row]);
-  const float base = big == -INFINITY ? 0.f : big;
-  float sum = 0.f, all = 0.f;
-#pragma unroll 4
-  for (int i = 0; i < span.parts; ++i) {
-    const float* a = part(i);
-    const float f = exp2_fast(a[ROWS * D + row] - base);
-    sum += f * a[row * D + d];
-    all += f * a[ROWS * D + ROWS + row];
+  float big = -INFINITY, all = 0.f;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int at = from; at < to; at += 4) {                // four parts on their way
+    float m[4], l[4];
+    float4 x[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+      x[i] = make_float4(0.f, 0.f, 0.f, 0.f);
+      if (at + i < to) {
+        const float* a = part(at + i);
+        m[i] = a[ROWS * D + row];
+        l[i] = a[ROWS * D + ROWS + row];
+        x[i] = *reinterpret_cast<const float4*>(a + row * D + d);
+      }
+    }
+    const float top = fmaxf(fmaxf(fmaxf(m[0], m[1]), fmaxf(m[2], m[3])), big), base = top == -INFINITY ? 0.f : top;
+    const float f0 = exp2_fast(big - base);
+    sum.x *= f0; sum.y *= f0; sum.z *= f0; sum.w *= f0;
+    all *= f0;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float f = exp2_fast(m[i] - base);
+      sum.x += f * x[i].x; sum.y += f * x[i].y; sum.z += f * x[i].z; sum.w += f * x[i].w;
+      all += f * l[i];
+    }
+    big = top;
   }
-  const float y = all == 0.f ? 0.f : sum / all;
+  if (shares > 1) {
+    sums[tid] = sum;
+    tops[tid] = make_float2(big, all);
+    __syncthreads();
+    if (share == 0) {
+      for (int k = 1; k < shares; ++k) {
+        const float2 t = tops[item + k * items];
+        const float4 x = sums[item + k * items];
+        const float top = fmaxf(big, t.x), base = top == -INFINITY ? 0.f : top, f = exp2_fast(big - base), g = exp2_fast(t.x - base);
+        sum.x = f * sum.x + g * x.x; sum.y = f * sum.y + g * x.y; sum.z = f * sum.z + g * x.z; sum.w = f * sum.w + g * x.w;
+        all = f * all + g * t.y;
+        big = top;
+      }
+    }
+  }
+  if (share > 0) return;
+  const float inv = all == 0.f ? 0.f : 1.f / all;
+  const int x = span.tile * ROWS + row;
   const size_t at = ((size_t)(req.x + x / p.group) * p.hq + span.head * p.group + x % p.group) * D + d;
-  if (LQER_IN_BOUNDS(&p.step->status, at * 2, 2, s.y_extent, 61)) {
-    const uint32_t w = round_bf16x2(y, y);
-    static_cast<uint16_t*>(p.Y)[at] = (uint16_t)w;
-  }
+  if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 61))
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
 }
 
-static int split_grid(const Attention& p, int few, int rows_per) {
+static int split_grid(const Attention& p, int few, int rows_per, int dim) {
   const long long most_rows = (long long)(few < p.M * (long long)p.group ? few : p.M * (long long)p.group);
   const long long tiles = (most_rows + rows_per - 1) / rows_per, chunks = ((long long)p.max_pages * p.page + kChunk - 1) / kChunk;
   const long long units = (long long)(p.R < p.M ? p.R : p.M) * tiles * p.hkv * chunks;
-  const long long per_sm = rows_per == 8 ? 3 : 2, most = (long long)sm_count() * per_sm;
+  const long long per_sm = dim == 64 ? 4 : 3, most = (long long)sm_count() * per_sm;
   const long long want = (units + kMinChunks - 1) / kMinChunks;
   return (int)(want < most ? want : most);
 }
@@ -451,10 +504,14 @@ static int rows_per_tile(const Attention& p) { return p.max_added * (long long)p
 
 template <int D, bool MX, int NT>
 static cudaError_t launch_split(const Split& s, int grid, cudaStream_t stream) {
-  LaunchScope scope(kFamDecode, stream, 2);
-  cudaError_t e = launch_after(split_kernel<D, MX, NT>, dim3(grid), kSplitThreads, 0, stream, s);
+  constexpr int SMEM = kWarps * Ring<D, MX, NT>::WARP;
+  static OncePerDevice once;
+  cudaError_t e = once.run([] { return cudaFuncSetAttribute(split_kernel<D, MX, NT>, cudaFuncAttributeMaxDynamicSharedMemorySize, SMEM); });
   if (e != cudaSuccess) return e;
-  return launch_after(join_kernel<D, NT>, dim3(grid, 8 * NT), D, 0, stream, s);
+  LaunchScope scope(kFamDecode, stream, 2);
+  e = launch_after(split_kernel<D, MX, NT>, dim3(grid), kSplitThreads, SMEM, stream, s);
+  if (e != cudaSuccess) return e;
+  return launch_after(join_kernel<D, NT>, dim3(grid), kJoinThreads, 0, stream, s);
 }
 
 }  // namespace kv
@@ -472,12 +529,12 @@ static kv::Attention attention_params(const lqer_kv_cache_t& c, const lqer_page_
   p.value_exps = static_cast<const uint8_t*>(c.values) + elements;
   return p;
 }
-static size_t spans_bytes() { return ((size_t)3 * sm_count() * sizeof(kv::Span) + 255) & ~(size_t)255; }
+static size_t spans_bytes() { return ((size_t)4 * sm_count() * sizeof(kv::Span) + 255) & ~(size_t)255; }
 
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
   const int rows = kv::rows_per_tile(p);
-  return spans_bytes() + (size_t)kv::split_grid(p, kv::kFewRows, rows) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+  return spans_bytes() + (size_t)kv::split_grid(p, kv::kFewRows, rows, c.head_dim) * 2 * rows * (c.head_dim + 2) * sizeof(float);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
                                    int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
@@ -499,7 +556,7 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
     const cudaError_t e = kv::launch_tiles(k.a, t.n_requests == 1 ? 0 : k.few, k.y_extent, c, s);
     if (e != cudaSuccess || t.n_requests == 1) return e;
   }
-  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows);
+  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows, c.head_dim);
   const bool mx = c.dtype == LQER_MXINT8;
   if (c.head_dim == 128)
     return rows == 8 ? (mx ? kv::launch_split<128, true, 1>(k, grid, s) : kv::launch_split<128, false, 1>(k, grid, s))

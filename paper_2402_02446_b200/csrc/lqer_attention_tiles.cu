@@ -303,7 +303,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       tc::tc_fence_after();
       float v[128];
 #pragma unroll
-      for (int k = 0; k < 4; ++k) tc::tmem_ld32(s_at + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]));
+      for (int k = 0; k < 2; ++k) tc::tmem_ld32(s_at + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]));
       if constexpr (!MX) {
         if (has_unseen(key0)) {
           // values that no row sees may be anything: 0 times that has to be 0
@@ -320,28 +320,37 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           tc::fence_proxy_async_smem();
         }
       }
-      tc::tmem_ld_wait();
       const bool masked = key0 + kKeys - 1 > first_pos || (p.window > 0 && key0 <= last_pos - p.window);
-      if (masked) {
+      // the second half of the scores is on its way while the first half's maximum is taken
+      float bigs[8];
 #pragma unroll
-        for (int k = 0; k < 4; ++k) {
-          const uint32_t seen = seen_columns(p, pos, key0, k);
+      for (int h = 0; h < 2; ++h) {
+        tc::tmem_ld_wait();
+        if (h == 0) {
 #pragma unroll
-          for (int i = 0; i < 32; ++i) v[32 * k + i] = seen & (1u << i) ? v[32 * k + i] : -INFINITY;
+          for (int k = 2; k < 4; ++k) tc::tmem_ld32(s_at + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]));
+        }
+        if (masked) {
+#pragma unroll
+          for (int k = 2 * h; k < 2 * h + 2; ++k) {
+            const uint32_t seen = seen_columns(p, pos, key0, k);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[32 * k + i] = seen & (1u << i) ? v[32 * k + i] : -INFINITY;
+          }
+        }
+        float* const x = v + 64 * h;
+#pragma unroll
+        for (int k = 0; k < 8; ++k) bigs[k] = h == 0 ? max3(x[k], x[k + 8], x[k + 16]) : max3(bigs[k], x[k], x[k + 8]);
+#pragma unroll
+        for (int i = 24 - 8 * h; i < 56; i += 16)
+#pragma unroll
+          for (int k = 0; k < 8; ++k) bigs[k] = max3(bigs[k], x[i + k], x[i + k + 8]);
+        if (h == 0) {
+#pragma unroll
+          for (int k = 0; k < 8; ++k) bigs[k] = fmaxf(bigs[k], x[56 + k]);
         }
       }
-      float big = -INFINITY;
-      {
-        float b[4] = {v[0], v[1], v[2], v[3]};
-#pragma unroll
-        for (int i = 4; i < 124; i += 8) {
-#pragma unroll
-          for (int k = 0; k < 4; ++k) b[k] = max3(b[k], v[i + k], v[i + 4 + k]);
-        }
-#pragma unroll
-        for (int k = 0; k < 4; ++k) b[k] = fmaxf(b[k], v[124 + k]);
-        big = fmaxf(max3(b[0], b[1], b[2]), b[3]);
-      }
+      float big = fmaxf(max3(max3(bigs[0], bigs[1], bigs[2]), bigs[3], bigs[4]), max3(bigs[5], bigs[6], bigs[7]));
       const bool up = (big - m) * c > 8.f || (m == -INFINITY && big > -INFINITY);
       if (__any_sync(0xFFFFFFFFu, up)) {
         const float f = up ? exp2_fast((m - big) * c) : 1.f;
@@ -365,11 +374,11 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       }
       const float base = m == -INFINITY ? 0.f : -m * c;
       const F2 base2 = f2(base, base);
-      // weights of columns 64 h .. + 63, and word to the issuer, which may begin with the first half; POLY: every POLY-th pair by the polynomial
-      auto weights = [&](auto every, int h) {
+      // the weights, and word to the issuer, which may begin with the first half; POLY: every POLY-th pair by the polynomial
+      auto weights = [&](auto every) {
         constexpr int POLY = decltype(every)::value;
 #pragma unroll
-        for (int k = 2 * h; k < 2 * h + 2; ++k) {
+        for (int k = 0; k < 4; ++k) {
           uint32_t w[16];
 #pragma unroll
           for (int i = 0; i < 16; ++i) {
@@ -386,20 +395,21 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
             else la = add2(la, f2(a, b));
             w[i] = round_bf16x2(a, b);                            // as in lqer_attention.cu: the weights are rounded, their sum is not
           }
+          if (k == 2) {                                           // (by now the first half has arrived, so this waits for nothing)
+            tmem_st_wait();
+            tc::tc_fence_before();
+            __syncwarp();
+            if (lane == 0) tc::mbar_arrive(bar_of(bars.p_half[t]));
+          }
           tmem_st16(s_at + 16 * k, w);
         }
         tmem_st_wait();
         tc::tc_fence_before();
         __syncwarp();
-        if (lane == 0) tc::mbar_arrive(bar_of(h == 0 ? bars.p_half[t] : bars.p_full[t]));
+        if (lane == 0) tc::mbar_arrive(bar_of(bars.p_full[t]));
       };
-      if (masked) {
-        weights(Every<0>{}, 0);
-        weights(Every<0>{}, 1);
-      } else {
-        weights(Every<kPolyEvery>{}, 0);
-        weights(Every<kPolyEvery>{}, 1);
-      }
+      if (masked) weights(Every<0>{});
+      else weights(Every<kPolyEvery>{});
       ++n;
     }
     if (ok && n > 0) {
@@ -457,7 +467,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       // ---- mantissas, as they lie in the cache, into swizzled bf16 values; a lane a block of 16, its row's other blocks beside it
       asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
       constexpr int B = SH::BLOCKS, N = B, STEP = 128 / B;         // a thread's blocks of a tile, and the rows between them
-      const int k = tid - 256, b = k % B, r0 = k / B, lo = p.emin + 127, hi = p.emax + 127, shift = p.bits - 2;
+      const int k = tid - 256, b = k % B, r0 = k / B, shift = p.bits - 2;
       const uint8_t* const raw_mem = ring_mem + SH::STAGES * SH::TILE;
       // the two halves' columns lie on the same banks: their lanes store their chunks in opposite order
       const int turn = D == 128 ? b >> 2 : 0, c = 2 * (b & 3);
@@ -477,14 +487,14 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         if (has_unseen(key0)) {
 #pragma unroll
           for (int i = 0; i < N; ++i)
-            if (unseen(key0 + r0 + i * STEP)) m[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (unseen(key0 + r0 + i * STEP)) { m[i] = make_uint4(0u, 0u, 0u, 0u); e[i] = 127; }
         }
         if (x >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (x / SH::STAGES - 1) & 1, &ws)) != 0;
         if (!ok) break;
         uint8_t* const to = ring_mem + at * SH::TILE;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-          const uint32_t sc = mantissa_scale(e[i], lo, hi, shift);
+          const MantissaScale sc = mantissa_scale(e[i], shift);
           const uint4 w0 = mantissas8(make_uint2(m[i].x, m[i].y), sc), w1 = mantissas8(make_uint2(m[i].z, m[i].w), sc);
           *reinterpret_cast<uint4*>(to + to0 + i * STEP * 128) = turn ? w1 : w0;          // (STEP is a multiple of 8: the swizzle stays)
           *reinterpret_cast<uint4*>(to + to1 + i * STEP * 128) = turn ? w0 : w1;

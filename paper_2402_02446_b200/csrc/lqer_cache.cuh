@@ -61,23 +61,31 @@ __device__ __forceinline__ int checked_page(const Attention& p, int id, int r) {
   return 0;
 }
 
-// Two int8 mantissas (in the low bytes of the halves of `b`, the rest zero) as bf16, times s (a power of two, twice): exact.
-// 0x4300 | low seven bits is 128 + them; taken from it are 128, or 256 where the sign bit is set.
-__device__ __forceinline__ uint32_t mantissas_bf16x2(uint32_t b, uint32_t s) {
-  uint32_t d;
-  asm("sub.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"((b & 0x007F007Fu) | 0x43004300u), "r"((b & 0x00800080u) | 0x43004300u));
-  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(d) : "r"(d), "r"(s));
-  return d;
+// Two int8 mantissas m (in the low bytes of the halves of `b`) as bf16 values m s, exact.  With the sign bit turned over the byte is u = m + 128, and 0x4300 + u
+// the bf16 number y = 128 + u up to u = 127 and 2 u from there on: z = (y - 256) s is m s below zero and 2 m s above, and half of
+// what is positive of it too much.  All but the first step are multiply-adds: the integer units are what bounds the kernels that do this.
+struct MantissaScale { uint32_t s, c; };       // bf16 pairs: s, and -256 s
+__device__ __forceinline__ uint32_t mantissas_bf16x2(uint32_t b, const MantissaScale& k) {
+  const uint32_t y = (b & 0x00FF00FFu) ^ 0x43804380u;
+  uint32_t z, t;
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(z) : "r"(y), "r"(k.s), "r"(k.c));
+  asm("fma.rn.relu.bf16x2 %0, %1, %2, %3;" : "=r"(t) : "r"(y), "r"(k.s), "r"(k.c));
+  asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(z) : "r"(t), "r"(0xBF00BF00u), "r"(z));
+  return z;
 }
-// The bf16 pair of 2^(e - (bits - 2)) for an exponent byte; lo, hi: the window's ends as bytes.
-__device__ __forceinline__ uint32_t mantissa_scale(uint32_t byte, int lo, int hi, int shift) {
-  const uint32_t s = (uint32_t)(min(max((int)byte, lo), hi) - shift) << 7;
-  return s | (s << 16);
+// The scale 2^(e - (bits - 2)) of two blocks from their exponent bytes (in the low bytes of the halves of `e`; within the format's window), shift = bits - 2.
+__device__ __forceinline__ MantissaScale mantissa_scales(uint32_t e, int shift) {
+  return {e * 128u - (uint32_t)shift * 0x00800080u, e * 128u + (0x80008000u + (uint32_t)(8 - shift) * 0x00800080u)};
 }
-// Eight mantissas as four pairs.
-__device__ __forceinline__ uint4 mantissas8(uint2 m, uint32_t s) {
-  return make_uint4(mantissas_bf16x2(__byte_perm(m.x, 0u, 0x4140), s), mantissas_bf16x2(__byte_perm(m.x, 0u, 0x4342), s),
-                    mantissas_bf16x2(__byte_perm(m.y, 0u, 0x4140), s), mantissas_bf16x2(__byte_perm(m.y, 0u, 0x4342), s));
+__device__ __forceinline__ MantissaScale mantissa_scale(uint32_t e, int shift) {
+  return {e * 0x00800080u - (uint32_t)shift * 0x00800080u, e * 0x00800080u + (0x80008000u + (uint32_t)(8 - shift) * 0x00800080u)};
+}
+// A word right by a byte (as a multiplication, where there is room, it takes longer: 40 heads, MXINT8, 171 -> 185 us).
+__device__ __forceinline__ uint32_t byte_down(uint32_t w) { return w >> 8; }
+// Eight mantissas as four pairs in order.
+__device__ __forceinline__ uint4 mantissas8(uint2 m, const MantissaScale& k) {
+  return make_uint4(mantissas_bf16x2(__byte_perm(m.x, 0u, 0x4140), k), mantissas_bf16x2(__byte_perm(m.x, 0u, 0x4342), k),
+                    mantissas_bf16x2(__byte_perm(m.y, 0u, 0x4140), k), mantissas_bf16x2(__byte_perm(m.y, 0u, 0x4342), k));
 }
 __device__ __forceinline__ uint32_t round_bf16x2(float lo, float hi) {
   uint32_t d;
