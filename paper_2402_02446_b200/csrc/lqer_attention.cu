@@ -165,7 +165,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
   const uint32_t ring_at = tc::smem_u32(ring);
   const StepRequest* reqs = requests_of(p.step);
   const int shift = p.bits - 2;
-  int r = run.request;
+  int r = run.request, turn = 0;
   long long before = run.before;
   while (u < end) {
     const int4 req = __ldg(reinterpret_cast<const int4*>(reqs + r));
@@ -178,23 +178,32 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
     const int h = (int)(which / tiles), tile = (int)(which % tiles), c0 = (int)(local - which * vis.chunks);
     const int c1 = (int)min((long long)vis.chunks, c0 + (end - u));
     const int rows = min(ROWS, n * p.group - tile * ROWS), first_pos = len - n;
-    // chunk of the run -> first of the warp's keys
-    auto key_of = [&](int chunk) { return ((chunk < vis.sink_chunks ? chunk : vis.first_chunk + chunk - vis.sink_chunks)) * kChunk + warp * 16; };
-    const int* table = p.tables + (size_t)r * p.max_pages;
-    auto entry_of = [&](int chunk) {
-      const int key = key_of(chunk);
-      return chunk < c1 && key < len ? __ldg(table + (key >> p.page_shift)) : 0;
+    const bool whole = c0 == 0 && c1 == vis.chunks;
+    // Where a run holds many short rows, a warp takes a whole one, and nobody waits for anybody (256 requests of up to 120 tokens, 32/32 heads: @ us).
+    const bool alone = whole && run.per >= 12 * vis.chunks;
+    const long long next = u + (c1 - c0);
+    if (alone && (turn++ & 3) != warp) { u = next; continue; }
+    // a warp's step -> its first key: 16 keys of every chunk, or of a row of its own all
+    const int x0 = alone ? 0 : c0, x1 = alone ? 4 * vis.chunks : c1;
+    auto key_of = [&](int x) {
+      const int chunk = alone ? x >> 2 : x;
+      return (chunk < vis.sink_chunks ? chunk : vis.first_chunk + chunk - vis.sink_chunks) * kChunk + (alone ? x & 3 : warp) * 16;
     };
-    int entry = entry_of(c0);                             // of the chunk that is sent next
-    auto send = [&](int chunk) {
-      const int key = key_of(chunk);
-      if (chunk < c1 && key < len)
-        R::fill(p, ring_at + (chunk - c0) % R::STAGES * R::STAGE, (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (key & (p.page - 1)), lane);
+    const int* table = p.tables + (size_t)r * p.max_pages;
+    auto entry_of = [&](int x) {
+      const int key = key_of(x);
+      return x < x1 && key < len ? __ldg(table + (key >> p.page_shift)) : 0;
+    };
+    int entry = entry_of(x0);                             // of the step that is sent next
+    auto send = [&](int x) {
+      const int key = key_of(x);
+      if (x < x1 && key < len)
+        R::fill(p, ring_at + (x - x0) % R::STAGES * R::STAGE, (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (key & (p.page - 1)), lane);
       copies_sent();
-      entry = entry_of(chunk + 1);
+      entry = entry_of(x + 1);
     };
 #pragma unroll
-    for (int i = 0; i < R::STAGES - 1; ++i) send(c0 + i);
+    for (int i = 0; i < R::STAGES - 1; ++i) send(x0 + i);
     // the row tile's queries, in the order in which a lane holds a key
     uint4 q[NT][D / 32];
     int pos[NT][2];
@@ -224,13 +233,13 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
       m[t][0] = m[t][1] = -INFINITY;
       l[t][0] = l[t][1] = 0.f;
     }
-    for (int chunk = c0; chunk < c1; ++chunk) {
-      const int key0 = key_of(chunk);
+    for (int x = x0; x < x1; ++x) {
+      const int key0 = key_of(x);
       if (key0 >= len) break;                             // the last chunk's end
-      send(chunk + R::STAGES - 1);
+      send(x + R::STAGES - 1);
       copies_wait<R::STAGES - 1>();
       __syncwarp();
-      const uint8_t* const keys = ring + (chunk - c0) % R::STAGES * R::STAGE;
+      const uint8_t* const keys = ring + (x - x0) % R::STAGES * R::STAGE;
       const uint8_t* const values = keys + R::SET + R::EXPS;
       float sc[NT][4];
 #pragma unroll
@@ -359,6 +368,32 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
     }
     copies_wait<0>();
     __syncwarp();
+    u = next;
+    if (alone) {
+#pragma unroll
+      for (int t = 0; t < NT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+#pragma unroll
+          for (int x = 4; x < 32; x <<= 1) l[t][i] += __shfl_xor_sync(0xFFFFFFFFu, l[t][i], x);
+          const int row = 8 * t + 2 * c + i;
+          if (row >= rows) continue;
+          const float inv = l[t][i] == 0.f ? 0.f : 1.f / l[t][i];
+          const int x = tile * ROWS + row;
+          const size_t at = ((size_t)(row0 + x / p.group) * p.hq + h * p.group + x % p.group) * D + 8 * g;
+          auto two = [&](int k, int half) { return round_bf16x2(o[t][k][i + 2 * half] * inv, o[t][k + 1][i + 2 * half] * inv); };
+          uint16_t* const y = static_cast<uint16_t*>(p.Y) + at;
+          if (!LQER_IN_BOUNDS(&p.step->status, at * 2, D == 128 ? 144 : 16, s.y_extent, 63)) continue;
+          if constexpr (D == 128) {
+            *reinterpret_cast<uint4*>(y) = make_uint4(two(0, 0), two(2, 0), two(4, 0), two(6, 0));
+            *reinterpret_cast<uint4*>(y + 64) = make_uint4(two(0, 1), two(2, 1), two(4, 1), two(6, 1));
+          } else {
+            *reinterpret_cast<uint4*>(y) = make_uint4(two(0, 0), two(2, 0), two(0, 1), two(2, 1));
+          }
+        }
+      }
+      continue;
+    }
     // the four warps' parts
     float* const out = reinterpret_cast<float*>(ring);
 #pragma unroll
@@ -384,7 +419,6 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
       }
     }
     __syncthreads();
-    const bool whole = c0 == 0 && c1 == vis.chunks;
     float* part = s.parts + (size_t)(2 * blockIdx.x + (c0 > 0 ? 0 : 1)) * ROWS * (D + 2);
     auto of_warp = [&](int w) { return reinterpret_cast<const float*>(rings + w * R::WARP); };
     for (int i = tid; i < rows * (D / 4); i += kSplitThreads) {
@@ -414,10 +448,9 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
       }
     }
     if (!whole && c0 == 0 && tid == 0) {
-      const long long stop = u + vis.chunks;             // where the row tile ends
+      const long long stop = before + (which + 1) * vis.chunks;      // where the row tile ends
       s.spans[blockIdx.x] = Span{r, h, tile, (int)((stop - 1) / run.per) - (int)blockIdx.x + 1};
     }
-    u += c1 - c0;
     __syncthreads();
   }
 }
