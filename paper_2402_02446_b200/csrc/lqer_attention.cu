@@ -20,7 +20,15 @@ namespace lqer {
 namespace kv {
 
 constexpr int kChunk = 64, kWarps = 4, kSplitThreads = 32 * kWarps;
-constexpr int kFewRows = 32;                 // of a request; more go to lqer_attention_tiles.cu
+// Requests of up to this many rows of a key head (tokens times heads that share it) are taken here, of more by lqer_attention_tiles.cu.  There a request's
+// time is that of its keys (some 14 ns each, 256 rows at a time), as long as the requests' key heads are fewer than the SMs; here it is shared by all
+// SMs, but grows with the rows, 16 at a time (some 12 ns a key, over the SMs).  Both sides measured, here / there, 32/8 heads, us: one request, 8 tokens
+// behind 8000: 24 / 105, 64 behind 4000: 46 / 64; two, 40 tokens: 63 / 120; 8, 20 tokens behind 2000: 36 / 36; 64, 8 tokens: 418 / 318, 20: 200 / 106.
+constexpr int kLeast = 16;
+inline int few_rows(const Attention& p) {
+  const long long heads = (long long)(p.R < p.M ? p.R : p.M) * p.hkv, few = 2900 / heads;
+  return few < kLeast ? kLeast : (int)few;
+}
 constexpr int kMinChunks = 2;                // of a CTA's run
 
 // What a CTA leaves for the join: the (request, key head, row tile) that begins in its run and goes on behind it, if any.
@@ -567,7 +575,7 @@ static size_t spans_bytes() { return ((size_t)4 * sm_count() * sizeof(kv::Span) 
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
   const int rows = kv::rows_per_tile(p);
-  return spans_bytes() + (size_t)kv::split_grid(p, kv::kFewRows, rows, c.head_dim) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+  return spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, c.head_dim) * 2 * rows * (c.head_dim + 2) * sizeof(float);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
                                    int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
@@ -579,14 +587,16 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
   k.a.window = window; k.a.sinks = window > 0 ? sinks : 0;
   k.a.scale_log2 = (float)(scale * 1.4426950408889634);
   k.a.bits = bits; k.a.emin = emin; k.a.emax = emax;
-  k.few = kv::kFewRows;
+  k.few = kv::few_rows(k.a);
   k.spans = static_cast<kv::Span*>(scratch);
   k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + spans_bytes());
   const size_t whole = (size_t)M * hq * c.head_dim * 2, less = debug_y_shrink();
   k.y_extent = whole > less ? whole - less : 0;
   if (max_added * (long long)k.a.group > k.few) {
-    // a single request goes there whatever it turns out to bring
-    const cudaError_t e = kv::launch_tiles(k.a, t.n_requests == 1 ? 0 : k.few, k.y_extent, c, s);
+    // A single request goes there whatever it turns out to bring; beside one that has to, only those of few rows stay (three prompts of 42 to 97 tokens,
+    // 16/4 heads: 18.4 us where the smaller ones stayed, 11.7).
+    k.few = t.n_requests == 1 ? 0 : kv::kLeast;
+    const cudaError_t e = kv::launch_tiles(k.a, k.few, k.y_extent, c, s);
     if (e != cudaSuccess || t.n_requests == 1) return e;
   }
   const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows, c.head_dim);

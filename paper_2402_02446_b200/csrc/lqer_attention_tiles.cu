@@ -11,9 +11,7 @@
 //   copies           bf16: one warp, a lane a page: TMA brings pages into swizzled tiles.  MXINT8: four warps read the mantissas, form the exact bf16
 //                    values and store them into the same tiles.
 //   issuer           one lane: per key tile and row tile, O += P V of the last key tile, then S of the next.
-//   lister           says what the CTA works on next, long rows of keys first, by turns over the CTAs; there is one CTA to an SM.
-// Keys and values share a ring of tiles, which is filled across the ends of items; queries of the next item are on their way from when the last S of the
-// one before is there.  Every wait is bounded.
+// Keys and values share a ring of tiles.  Every wait is bounded.
 #include "lqer_cache.cuh"
 
 namespace lqer {
@@ -28,8 +26,7 @@ struct Shape {
   static constexpr int STAGES = MX ? (D == 128 ? 3 : 6) : (D == 128 ? 5 : 8);
   static constexpr int RAW_STAGES = MX ? (D == 128 ? 3 : 6) : 0, RAW_EXPS = 128 * D, RAW = 128 * D + 128 * BLOCKS;   // an MXINT8 tile as it lies in the cache
   static constexpr int SMEM = 1024 + (2 + STAGES) * TILE + RAW_STAGES * RAW;
-  static constexpr int COPY_WARPS = MX ? 4 : 1, COPY0 = 8, ISSUER = COPY0 + COPY_WARPS, RAW_WARP = MX ? ISSUER + 1 : -1, LISTER = ISSUER + (MX ? 2 : 1);
-  static constexpr int READERS = 8 + COPY_WARPS + (MX ? 2 : 1);              // warps that are told what comes next
+  static constexpr int COPY_WARPS = MX ? 4 : 1, COPY0 = 8, ISSUER = COPY0 + COPY_WARPS, RAW_WARP = MX ? ISSUER + 1 : -1;
   static constexpr int THREADS = MX ? 512 : 384;
   static constexpr int S_COL = 0, O_COL = 256;                              // tensor memory: S of A and B, O of A and B
 };
@@ -41,9 +38,10 @@ struct Tiles {
   int stall;
   long long wait_limit;
   size_t y_extent;
+  bool y_wide;                 // Y: aligned to 32 bytes
 };
 struct Barriers {
-  unsigned long long full[8], empty[8], raw_full[6], raw_empty[6], s_full[2], p_half[2], p_full[2], o_done[2], item_full[2], item_empty[2], q_full[2], drained;
+  unsigned long long full[8], empty[8], raw_full[6], raw_empty[6], s_full[2], p_half[2], p_full[2], o_done[2], q_full, drained;
 };
 __device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
 
@@ -75,6 +73,16 @@ __device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16
   asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};"
                ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]),
                  "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+// 32 bytes in one access (a whole sector), or in two where the tensor is not aligned to 32.
+__device__ __forceinline__ void store32(void* p, bool aligned, const uint32_t* u) {
+  if (aligned) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};"
+                 ::"l"(p), "r"(u[0]), "r"(u[1]), "r"(u[2]), "r"(u[3]), "r"(u[4]), "r"(u[5]), "r"(u[6]), "r"(u[7]) : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(u[0], u[1], u[2], u[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(u[4], u[5], u[6], u[7]);
+  }
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
 __device__ __forceinline__ float max3(float a, float b, float c) {
@@ -148,25 +156,23 @@ __device__ __forceinline__ Plan plan_of(const Tiles& s, const Item& it) {
   q.count = q.sinks + max(q.end[0], q.end[1]) - q.start;
   return q;
 }
-__device__ __forceinline__ int items_of(const Tiles& s, const int4& w) {
-  const int rows = w.y * s.a.group;
-  return w.y > 0 && rows > s.few ? (rows + 2 * kRows - 1) / (2 * kRows) : 0;
-}
-// Items of all requests (each key head has as many), and of the CTA's first one the request and the items before that.  Work goes by falling item
-// number, a request's last ones, with the most keys, first, and all key heads of one before the next.
-struct Start { int total, request, before; };
-__device__ __forceinline__ Start find_start(const Tiles& s) {
+// The CTA's item; heavy ones (a request's last) first.  False: there is none.
+__device__ __forceinline__ bool find_item(const Tiles& s, Item& it) {
   const Attention& p = s.a;
   const StepRequest* reqs = requests_of(p.step);
   __shared__ int sums[16];
-  __shared__ Start found;
+  __shared__ Item found;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int per = (p.R + blockDim.x - 1) / blockDim.x, from = min(tid * per, p.R), to = min(from + per, p.R);
+  auto items_of = [&](const int4& w) {
+    const int rows = w.y * p.group;
+    return w.y > 0 && rows > s.few ? (rows + 2 * kRows - 1) / (2 * kRows) : 0;
+  };
   int4 w = make_int4(0, 0, 0, 0);
   int mine = 0;
   for (int r = from; r < to; ++r) {
     w = __ldg(reinterpret_cast<const int4*>(reqs + r));
-    mine += items_of(s, w);
+    mine += items_of(w);
   }
   int x = mine;
 #pragma unroll
@@ -176,17 +182,22 @@ __device__ __forceinline__ Start find_start(const Tiles& s) {
   int before = x - mine, total = 0;
   for (int k = 0; k < warps; ++k) { if (k < warp) before += sums[k]; total += sums[k]; }
   const int index = total - 1 - (int)(blockIdx.x / p.hkv);
-  if (index < 0) return Start{0, 0, 0};
+  if (index < 0) return false;
   if (index >= before && index < before + mine) {
     for (int r = from;; ++r) {
       if (per > 1) w = __ldg(reinterpret_cast<const int4*>(reqs + r));
-      const int c = items_of(s, w);
-      if (index < before + c) { found = Start{total, r, before}; break; }
+      const int c = items_of(w);
+      if (index < before + c) {
+        const int base = (index - before) * 2 * kRows, token = base / p.group;
+        found = Item{r, (int)(blockIdx.x % p.hkv), w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group};
+        break;
+      }
       before += c;
     }
   }
   __syncthreads();
-  return found;
+  it = found;
+  return true;
 }
 // The columns of a key tile from key0 on that the row at `pos` sees, 32 to a word.
 __device__ __forceinline__ uint32_t upto(int n) { return n < 0 ? 0u : n >= 31 ? 0xFFFFFFFFu : (2u << n) - 1u; }       // bits 0 .. n
@@ -204,7 +215,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   __shared__ Barriers bars;
   __shared__ uint32_t tmem_at;
   __shared__ tc::WaitState ws;
-  __shared__ Item items[2];
   const Attention& p = s.a;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const uint32_t q_at = (tc::smem_u32(dynamic) + 1023u) & ~1023u, ring_at = q_at + 2 * SH::TILE, raw_at = ring_at + SH::STAGES * SH::TILE;
@@ -225,10 +235,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       tc::mbar_init(bar_of(bars.p_half[t]), 4);
       tc::mbar_init(bar_of(bars.p_full[t]), 4);
       tc::mbar_init(bar_of(bars.o_done[t]), 1);
-      tc::mbar_init(bar_of(bars.q_full[t]), 4 + (s.stall && blockIdx.x == 0 ? 1 : 0));
-      tc::mbar_init(bar_of(bars.item_full[t]), 1);
-      tc::mbar_init(bar_of(bars.item_empty[t]), SH::READERS);
     }
+    tc::mbar_init(bar_of(bars.q_full), 8 + (s.stall && blockIdx.x == 0 ? 1 : 0));
     tc::mbar_init(bar_of(bars.drained), 1);
     tc::fence_barrier_init();
     ws.abort = 0;
@@ -240,32 +248,21 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   }
   tc::pdl_wait();
   if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
-  const Start start = find_start(s);
-  if (start.total == 0) return;
+  Item it;
+  if (!find_item(s, it)) return;
   if (warp == SH::ISSUER) tc::tmem_alloc(tc::smem_u32(&tmem_at), 512);
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_at;
+  const Plan plan = plan_of(s, it);
+  const int* table = p.tables + (size_t)it.request * p.max_pages;
+  // keys that no row of the step sees: from the end on, and between the first tokens and the window
+  const int seen_from = p.window > 0 ? max(0, it.len - it.n - p.window + 1) : 0;
+  auto unseen = [&](int key) { return key >= it.len || (key < seen_from && key >= p.sinks); };
+  auto has_unseen = [&](int key0) { return key0 + kKeys > it.len || (key0 < seen_from && key0 + kKeys > p.sinks); };
   int copies = 0;
   bool ok = true;
-  // every lane of a warp goes on, or none
-  auto wait = [&](unsigned long long& bar, uint32_t parity) {
-    ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bar), parity, &ws)) != 0;
-    return ok;
-  };
-  // item number `k` of the CTA, once it is known; false where there is none any more.  A warp that has it says so, unless it will look again.
-  auto item_of = [&](int k, Item& it, bool again) {
-    if (!wait(bars.item_full[k & 1], k >> 1 & 1)) return false;
-    it = items[k & 1];
-    __syncwarp();
-    if (!again && lane == 0) tc::mbar_arrive(bar_of(bars.item_empty[k & 1]));
-    return it.request >= 0;
-  };
-  // keys that no row of the step sees: from the end on, and between the first tokens and the window
-  auto seen_from = [&](const Item& it) { return p.window > 0 ? max(0, it.len - it.n - p.window + 1) : 0; };
-  auto unseen = [&](const Item& it, int key) { return key >= it.len || (key < seen_from(it) && key >= p.sinks); };
-  auto has_unseen = [&](const Item& it, int key0) { return key0 + kKeys > it.len || (key0 < seen_from(it) && key0 + kKeys > p.sinks); };
 
   if (warp < 8) {
     // ---- a row tile
@@ -275,62 +272,57 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const int t = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
     const uint32_t s_at = tmem + lanes + SH::S_COL + t * 128, o_at = tmem + lanes + SH::O_COL + t * D;
-    // Queries of an item, as the MMA reads them: 16 bytes a thread, the tile's rows in turn.
-    auto send_queries = [&](const Item& it) {
+    const int left = it.rows - it.base - t * kRows;               // rows from the tile's first on
+    {
+      // queries, as the MMA reads them; 16 bytes a thread, the tile's rows in turn
       constexpr int PER = D / 8, STEP = 128 / PER;
-      const int c = row % PER, r0 = row / PER, left = it.rows - it.base - t * kRows;
-      const uint32_t to = q_at + t * SH::TILE + (c >> 3) * SH::HALF;
+      uint8_t* const to = q_mem + t * SH::TILE;
+      const int c = row % PER, r0 = row / PER;
       const uint16_t* from = static_cast<const uint16_t*>(p.Q) + (size_t)it.row0 * p.q_stride + (size_t)(it.head * p.group) * D + 8 * c;
-#pragma unroll 4
+      uint4 v[PER];
+#pragma unroll
       for (int i = 0; i < PER; ++i) {
         const int r = r0 + i * STEP;
         int token, head;
         row_of(s, it, t * kRows + r, token, head);
-        const bool there = r < left;
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(to + r * 128 + (((c & 7) ^ (r & 7)) << 4)),
-                     "l"(there ? from + (size_t)token * p.q_stride + head * D : from), "r"(there ? 16 : 0) : "memory");
+        v[i] = make_uint4(0u, 0u, 0u, 0u);
+        if (r < left) v[i] = __ldg(reinterpret_cast<const uint4*>(from + (size_t)token * p.q_stride + head * D));
       }
-    };
-    const float c = p.scale_log2;
-    const F2 c2 = f2(c, c);
-    int at = 0;                                                    // place of the item's first keys in the ring's order
-    uint32_t turn = 0;                                             // key tiles so far, of all items
-    Item it;
-    if (item_of(0, it, true)) send_queries(it);
-    for (int k = 0; ok && item_of(k, it, false); ++k) {
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    tc::fence_proxy_async_smem();
-    __syncwarp();
-    const Plan plan = plan_of(s, it);
-    const int left = it.rows - it.base - t * kRows;               // rows from the tile's first on
-    if (left > 0 && lane == 0) tc::mbar_arrive(bar_of(bars.q_full[t]));
-    const int first_pos = t ? plan.first_pos[1] : plan.first_pos[0], last_pos = t ? plan.last_pos[1] : plan.last_pos[0], end = t ? plan.end[1] : plan.end[0];
+#pragma unroll
+      for (int i = 0; i < PER; ++i) {
+        const int r = r0 + i * STEP;
+        *reinterpret_cast<uint4*>(to + (c >> 3) * SH::HALF + r * 128 + (((c & 7) ^ (r & 7)) << 4)) = v[i];
+      }
+      tc::fence_proxy_async_smem();
+      __syncwarp();
+      if (lane == 0) tc::mbar_arrive(bar_of(bars.q_full));
+    }
+    const int first_pos = t ? plan.first_pos[1] : plan.first_pos[0], last_pos = t ? plan.last_pos[1] : plan.last_pos[0];
     int token, head;
     row_of(s, it, t * kRows + max(min(row, left - 1), 0), token, head);
     const int pos = it.len - it.n + token;
-    auto next_queries = [&]() {
-      Item next;
-      if (item_of(k + 1, next, true)) send_queries(next);
-    };
-    if (left <= 0) next_queries();
+    const float c = p.scale_log2;
+    const F2 c2 = f2(c, c);
     float m = -INFINITY;
     F2 la = f2(0.f, 0.f), lb = f2(0.f, 0.f);                       // sums of weights, four to a row
     int n = 0;                                                     // key tiles so far
     for (int j = 0; j < plan.count && ok; ++j) {
       const int kv = plan.tile(j), key0 = kv * kKeys;
       if (!plan.sees(t, kv)) continue;
-      if (!wait(bars.s_full[t], turn & 1)) break;
+      ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.s_full[t]), n & 1, &ws)) != 0;
+      if (!ok) break;
       tc::tc_fence_after();
       float v[128];
 #pragma unroll
       for (int k = 0; k < 2; ++k) tc::tmem_ld32(s_at + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]));
       if constexpr (!MX) {
-        if (has_unseen(it, key0)) {
+        if (has_unseen(key0)) {
           // values that no row sees may be anything: 0 times that has to be 0
-          const int place = at + 2 * j + 1;
-          if (!wait(bars.full[place % SH::STAGES], place / SH::STAGES & 1)) break;
-          if (unseen(it, key0 + row)) {
-            uint4* to = reinterpret_cast<uint4*>(ring_mem + (place % SH::STAGES) * SH::TILE + row * 128);
+          const int at = 2 * j + 1;
+          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.full[at % SH::STAGES]), at / SH::STAGES & 1, &ws)) != 0;
+          if (!ok) break;
+          if (unseen(key0 + row)) {
+            uint4* to = reinterpret_cast<uint4*>(ring_mem + (at % SH::STAGES) * SH::TILE + row * 128);
 #pragma unroll
             for (int h = 0; h < D / 64; ++h)
 #pragma unroll
@@ -369,8 +361,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           for (int k = 0; k < 8; ++k) bigs[k] = fmaxf(bigs[k], x[56 + k]);
         }
       }
-      if (kv == end - 1) next_queries();                           // the last S is there, so these queries have been read
-      if (!ok) break;
       float big = fmaxf(max3(max3(bigs[0], bigs[1], bigs[2]), bigs[3], bigs[4]), max3(bigs[5], bigs[6], bigs[7]));
       const bool up = (big - m) * c > 8.f || (m == -INFINITY && big > -INFINITY);
       if (__any_sync(0xFFFFFFFFu, up)) {
@@ -379,7 +369,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         if (n > 0) {
           la = fma2(la, f2(f, f), f2(0.f, 0.f));
           lb = fma2(lb, f2(f, f), f2(0.f, 0.f));
-          if (!wait(bars.o_done[t], (turn - 1) & 1)) break;
+          ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
+          if (!ok) break;
           tc::tc_fence_after();
 #pragma unroll 1
           for (int k = 0; k < D / 16; ++k) {
@@ -429,48 +420,37 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         if (lane == 0) tc::mbar_arrive(bar_of(bars.p_full[t]));
       };
       if (masked) weights(Every<0>{});
-      else weights(Every<kPolyEvery>{});
+      else weights(Every<MX ? 0 : kPolyEvery>{});
       ++n;
-      ++turn;
     }
-    at += 2 * plan.count;
-    if (ok && n > 0 && wait(bars.o_done[t], (turn - 1) & 1)) {
+    if (ok && n > 0) {
+      ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
       tc::tc_fence_after();
       float l[4];
       unf2(la, l[0], l[1]);
       unf2(lb, l[2], l[3]);
       const float all = (l[0] + l[1]) + (l[2] + l[3]), inv = all == 0.f ? 0.f : 1.f / all;
-      const size_t y_at = ((size_t)(it.row0 + token) * p.hq + it.head * p.group + head) * D;
-      const bool mine = row < left && LQER_IN_BOUNDS(&p.step->status, y_at * 2, D * 2, s.y_extent, 62);
+      const size_t at = ((size_t)(it.row0 + token) * p.hq + it.head * p.group + head) * D;
+      const bool mine = row < left && ok && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) {
-        uint32_t o[32];
+        uint32_t o[32], w[16];
         tc::tmem_ld32(o_at + 32 * k, o);
         tc::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 16; ++i) w[i] = round_bf16x2(__uint_as_float(o[2 * i]) * inv, __uint_as_float(o[2 * i + 1]) * inv);
         if (mine) {
-          uint4* to = reinterpret_cast<uint4*>(static_cast<uint16_t*>(p.Y) + y_at + 32 * k);
-#pragma unroll
-          for (int i = 0; i < 4; ++i) {
-            uint32_t w[4];
-#pragma unroll
-            for (int e = 0; e < 4; ++e)
-              w[e] = round_bf16x2(__uint_as_float(o[8 * i + 2 * e]) * inv, __uint_as_float(o[8 * i + 2 * e + 1]) * inv);
-            to[i] = make_uint4(w[0], w[1], w[2], w[3]);
-          }
+          uint16_t* const to = static_cast<uint16_t*>(p.Y) + at + 32 * k;
+          store32(to, s.y_wide, w);
+          store32(to + 16, s.y_wide, w + 8);
         }
       }
-      tc::tc_fence_before();
-    }
     }
   } else if (warp < SH::ISSUER) {
     if constexpr (!MX) {
       // ---- copies: a lane a page
       asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
       const int pages = kKeys >> p.page_shift;
-      Item it;
-      for (int k = 0; ok && item_of(k, it, false); ++k) {
-      const Plan plan = plan_of(s, it);
-      const int* table = p.tables + (size_t)it.request * p.max_pages;
       for (int j = 0; j < plan.count && ok; ++j) {
         const int key0 = plan.tile(j) * kKeys, key = key0 + (lane << p.page_shift);
         const bool mine = lane < pages && key < it.len;
@@ -478,7 +458,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine)) * (uint32_t)(p.page * D * 2);
         for (int which = 0; which < 2; ++which, ++copies) {
           const int at = copies % SH::STAGES;
-          if (copies >= SH::STAGES && !wait(bars.empty[at], (copies / SH::STAGES - 1) & 1)) break;
+          if (copies >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (copies / SH::STAGES - 1) & 1, &ws)) != 0;
+          if (!ok) break;
           if (lane == 0) tc::mbar_expect_tx(bar_of(bars.full[at]), bytes);
           __syncwarp();
           if (mine) {
@@ -489,7 +470,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           }
         }
       }
-      }
     } else {
       // ---- mantissas, as they lie in the cache, into swizzled bf16 values; a lane a block of 16, its row's other blocks beside it
       asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
@@ -499,13 +479,10 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       // the two halves' columns lie on the same banks: their lanes store their chunks in opposite order
       const int turn = D == 128 ? b >> 2 : 0, c = 2 * (b & 3);
       const uint32_t to0 = (b >> 2) * SH::HALF + r0 * 128 + (((c + turn) ^ (r0 & 7)) << 4), to1 = (b >> 2) * SH::HALF + r0 * 128 + (((c + 1 - turn) ^ (r0 & 7)) << 4);
-      Item it;
-      int x = 0;                                                   // tiles so far
-      for (int item = 0; ok && item_of(item, it, false); ++item) {
-      const Plan plan = plan_of(s, it);
-      for (int y = 0; y < 2 * plan.count && ok; ++y, ++x) {
-        const int at = x % SH::STAGES, raw = x % SH::RAW_STAGES, key0 = plan.tile(y >> 1) * kKeys;
-        if (!wait(bars.raw_full[raw], x / SH::RAW_STAGES & 1)) break;
+      for (int x = 0; x < 2 * plan.count && ok; ++x) {
+        const int at = x % SH::STAGES, raw = x % SH::RAW_STAGES, key0 = plan.tile(x >> 1) * kKeys;
+        ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.raw_full[raw]), x / SH::RAW_STAGES & 1, &ws)) != 0;
+        if (!ok) break;
         const uint8_t* const from = raw_mem + raw * SH::RAW;
         uint4 m[N];
         uint32_t e[N];
@@ -514,12 +491,13 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           m[i] = *reinterpret_cast<const uint4*>(from + (r0 + i * STEP) * D + b * 16);
           e[i] = from[SH::RAW_EXPS + (r0 + i * STEP) * B + b];
         }
-        if (has_unseen(it, key0)) {
+        if (has_unseen(key0)) {
 #pragma unroll
           for (int i = 0; i < N; ++i)
-            if (unseen(it, key0 + r0 + i * STEP)) { m[i] = make_uint4(0u, 0u, 0u, 0u); e[i] = 127; }
+            if (unseen(key0 + r0 + i * STEP)) { m[i] = make_uint4(0u, 0u, 0u, 0u); e[i] = 127; }
         }
-        if (x >= SH::STAGES && !wait(bars.empty[at], (x / SH::STAGES - 1) & 1)) break;
+        if (x >= SH::STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.empty[at]), (x / SH::STAGES - 1) & 1, &ws)) != 0;
+        if (!ok) break;
         uint8_t* const to = ring_mem + at * SH::TILE;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
@@ -535,7 +513,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           tc::mbar_arrive(bar_of(bars.raw_empty[raw]));
         }
       }
-      }
     }
   } else if (warp == SH::ISSUER) {
     if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
@@ -544,20 +521,15 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const bool leader = tc::elect_one();
     const uint32_t s_idesc = tc::make_idesc(128, 128) | (s.negate ? 1u << 13 : 0u), o_idesc = tc::make_idesc(128, D) | 1u << 16;
     const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
-    uint32_t turn[2] = {0, 0}, tiles[2] = {0, 0};                  // key tiles, and row tiles, so far
+    auto all = [&](bool got) { ok = __all_sync(0xFFFFFFFFu, got) != 0; return ok; };
+    int n[2] = {0, 0};                                             // key tiles whose O is under way
     int at = 0;                                                    // place in the ring, and how often it has been round: of K(j), V(j - 1) before it
     uint32_t phase = 0;
-    Item it;
-    for (int item = 0; ok && item_of(item, it, false); ++item) {
-    const Plan plan = plan_of(s, it);
-    int n[2] = {0, 0};                                             // key tiles whose O is under way
-#pragma unroll
-    for (int t = 0; t < 2; ++t)
-      if (ok && plan.end[t] > 0) wait(bars.q_full[t], tiles[t]++ & 1);
+    all(tc::mbar_wait(bar_of(bars.q_full), 0, &ws));
     for (int j = 0; j <= plan.count && ok; ++j) {
       const int v_at = at;
       if (j > 0) {
-        if (!wait(bars.full[v_at], phase)) break;
+        if (!all(tc::mbar_wait(bar_of(bars.full[v_at]), phase, &ws))) break;
         if (++at == SH::STAGES) { at = 0; phase ^= 1; }
       }
       const int k_at = at;
@@ -568,7 +540,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         if (j > 0 && plan.sees(t, plan.tile(j - 1))) {
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
-            if (!wait(half ? bars.p_full[t] : bars.p_half[t], turn[t] & 1)) break;
+            if (!all(tc::mbar_wait(bar_of(half ? bars.p_full[t] : bars.p_half[t]), n[t] & 1, &ws))) break;
             tc::tc_fence_after();
             if (leader) {
 #pragma unroll
@@ -580,11 +552,10 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           }
           if (!ok) break;
           ++n[t];
-          ++turn[t];
         }
         if (j < plan.count) {
           if (!keys_there) {
-            if (!wait(bars.full[k_at], k_phase)) break;
+            if (!all(tc::mbar_wait(bar_of(bars.full[k_at]), k_phase, &ws))) break;
             tc::tc_fence_after();
             keys_there = true;
           }
@@ -603,8 +574,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         if (j > 0) tc::umma_commit(bar_of(bars.empty[v_at]));
         if (j < plan.count) tc::umma_commit(bar_of(bars.empty[k_at]));
       }
-      if (j < plan.count && ++at == SH::STAGES) { at = 0; phase ^= 1; }
-    }
+      if (++at == SH::STAGES) { at = 0; phase ^= 1; }
     }
   } else {
     if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
@@ -612,10 +582,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     if (warp == SH::RAW_WARP) {
       // ---- copies of an MXINT8 cache: a lane a page
       const int pages = kKeys >> p.page_shift;
-      Item it;
-      for (int k = 0; ok && item_of(k, it, false); ++k) {
-      const Plan plan = plan_of(s, it);
-      const int* table = p.tables + (size_t)it.request * p.max_pages;
       for (int j = 0; j < plan.count && ok; ++j) {
         const int key0 = plan.tile(j) * kKeys, key = key0 + (lane << p.page_shift);
         const bool mine = lane < pages && key < it.len;
@@ -624,7 +590,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         const size_t block = ((((size_t)id * p.hkv + it.head) << p.page_shift)) * SH::BLOCKS;      // of 16 elements
         for (int which = 0; which < 2; ++which, ++copies) {
           const int at = copies % SH::RAW_STAGES;
-          if (copies >= SH::RAW_STAGES && !wait(bars.raw_empty[at], (copies / SH::RAW_STAGES - 1) & 1)) break;
+          if (copies >= SH::RAW_STAGES) ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.raw_empty[at]), (copies / SH::RAW_STAGES - 1) & 1, &ws)) != 0;
+          if (!ok) break;
           if (lane == 0) tc::mbar_expect_tx(bar_of(bars.raw_full[at]), bytes);
           __syncwarp();
           if (mine) {
@@ -633,40 +600,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
             tc::bulk_load(to + SH::RAW_EXPS + place * SH::BLOCKS, (which ? p.value_exps : p.key_exps) + block, p.page * SH::BLOCKS, bar_of(bars.raw_full[at]));
           }
         }
-      }
-      }
-    } else if (warp == SH::LISTER) {
-      // ---- items: from one to the CTA's next, 32 requests at a step
-      const StepRequest* reqs = requests_of(p.step);
-      int r = start.request, before = start.before;
-      for (int k = 0; ok; ++k) {
-        // by turns, every other one backwards: who had the most keys of a turn has the fewest of the next
-        const long long work = (long long)k * gridDim.x + (k & 1 ? gridDim.x - 1 - blockIdx.x : blockIdx.x);
-        const int index = start.total - 1 - (int)min(work / p.hkv, (long long)start.total);
-        while (index >= 0 && index < before) {
-          const int x = r - 1 - lane;
-          const int mine = x >= 0 ? items_of(s, __ldg(reinterpret_cast<const int4*>(reqs + x))) : 0;
-          int sum = mine;
-#pragma unroll
-          for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xFFFFFFFFu, sum, o); if (lane >= o) sum += y; }
-          const unsigned there = __ballot_sync(0xFFFFFFFFu, before - sum <= index);
-          const int to = there != 0 ? __ffs(there) - 1 : 31;
-          before -= __shfl_sync(0xFFFFFFFFu, sum, to);
-          r -= to + 1;
-        }
-        if (k >= 2 && !wait(bars.item_empty[k & 1], (k >> 1) - 1 & 1)) break;
-        if (lane == 0) {
-          Item it = {-1, 0, 0, 0, 0, 0, 0, 0, 0};
-          if (index >= 0) {
-            const int4 w = __ldg(reinterpret_cast<const int4*>(reqs + r));
-            const int base = (index - before) * 2 * kRows, token = base / p.group;
-            it = Item{r, (int)(work % p.hkv), w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group};
-          }
-          items[k & 1] = it;
-          tc::mbar_arrive(bar_of(bars.item_full[k & 1]));
-        }
-        __syncwarp();
-        if (index < 0) break;
       }
     }
   }
@@ -741,11 +674,12 @@ cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqe
   k.stall = take_stall(kFamDecode) ? 1 : 0;
   k.wait_limit = wait_limit_cycles();
   k.y_extent = y_extent;
+  k.y_wide = reinterpret_cast<uintptr_t>(a.Y) % 32 == 0;
   // no more items than this: whole ones, and one that is not for every request that has enough rows to be taken
   const long long rows = (long long)a.M * a.group, most = rows / (few + 1);
   const long long items = rows / (2 * kRows) + (most < a.R ? most : a.R);
-  const long long work = items * a.hkv;
-  const int ctas = (int)(work < sm_count() ? work : sm_count());
+  if (items * a.hkv > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  const int ctas = (int)(items * a.hkv);
   if (c.dtype == LQER_MXINT8) return c.head_dim == 128 ? launch_shape<128, true>(k, ctas, c, s) : launch_shape<64, true>(k, ctas, c, s);
   return c.head_dim == 128 ? launch_shape<128, false>(k, ctas, c, s) : launch_shape<64, false>(k, ctas, c, s);
 }
