@@ -8,8 +8,9 @@ namespace kv {
 // The step is a chain of sums over the requests (rows before a request, pages wanted before it, pages given back before it) and then lists that
 // are as long as what moves.  One CTA does it: the sums need all requests, everything it reads of what it replaces (lengths, ring) is
 // read before, so they may be replaced in place, and a list's entry finds its request by bisection in shared memory.  What bounds it is latency: about a
-// dozen trips to L2 and barriers.  Beyond kRowsInside rows the slots take a launch of their own over all SMs.
-constexpr int kStepThreads = 1024, kRowsInside = 16384;
+// dozen trips to L2 and barriers.  Beyond kRowsInside rows, where a thread would have several behind one another, the slots take a launch of their own over
+// all SMs.
+constexpr int kStepThreads = 1024, kRowsInside = 4096;
 
 struct StepParams {
   const int* lengths;
@@ -62,31 +63,29 @@ __device__ __forceinline__ T scan(T mine, T* sums, T& total) {
   const T before = __shfl_sync(0xFFFFFFFFu, v, max(warp - 1, 0));
   return x - mine + (warp > 0 ? before : T(0));
 }
-// The last of n ascending entries that is not above `at` (the first one is not).
-__device__ __forceinline__ int last_not_above(const int* first, int n, int at) {
-  int lo = 0, hi = n;
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (first[mid] <= at) lo = mid; else hi = mid;
-  }
+// The last of the CTA's ascending entries that is not above `at` (the first one is not): ten steps without a branch, so that several searches run side by side.
+__device__ __forceinline__ int last_not_above(const int* first, int at) {
+  int lo = 0;
+#pragma unroll
+  for (int step = kStepThreads / 2; step > 0; step >>= 1) lo += first[lo + step] <= at ? step : 0;
   return lo;
 }
 // Slot and position of row i of request r; fail: told of a table entry that is no page.
 template <class Fail>
-__device__ __forceinline__ void put_row(const StepParams& p, int row, int r, int i, int n, int len, Fail fail) {
-  int slot = -1, pos = -1;
-  if (i < n) {
-    const int at = len - n + i, id = p.tables[(size_t)r * p.max_pages + (at >> p.page_shift)];
-    if ((unsigned)id < (unsigned)p.n_pages) {
-      slot = (id << p.page_shift) + (at & (p.page - 1));
-      pos = at;
-    } else {
-      fail(LQER_ERR_BOUNDS);
-    }
+__device__ __forceinline__ void slot_of(const StepParams& p, int r, int i, int n, int len, Fail fail, int& slot, int& pos) {
+  slot = pos = -1;
+  if (i >= n) return;
+  const int at = len - n + i, id = p.tables[(size_t)r * p.max_pages + (at >> p.page_shift)];
+  if ((unsigned)id < (unsigned)p.n_pages) {
+    slot = (id << p.page_shift) + (at & (p.page - 1));
+    pos = at;
+  } else {
+    fail(LQER_ERR_BOUNDS);
   }
-  p.slots[row] = slot;
-  p.positions[row] = pos;
 }
+// Place i of a ring of n entries from `start` on (i below n).
+__device__ __forceinline__ int around(int start, int i, int n) { return i < n - start ? start + i : i - (n - start); }
+constexpr int kBatch = 4;    // list entries that a thread has on their way
 __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, const int rows_inside) {
   __shared__ int first[kStepThreads], from[kStepThreads], row0s[kStepThreads], ns[kStepThreads], lens[kStepThreads];
   __shared__ int sums32[32];
@@ -99,10 +98,12 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   if (tid == 0) { taken = 0; status = LQER_OK; }
   __syncthreads();
   auto fail = [&](int code) { atomicCAS(&status, (int)LQER_OK, code); };
+  const Request q0 = request_at(p, tid);
+  auto request = [&](int base) { return base == 0 ? q0 : request_at(p, base + tid); };
   // pages that come back
   int given = 0, total = 0;
   for (int base = 0; base < p.R; base += kStepThreads) {
-    const Request q = request_at(p, base + tid);
+    const Request q = request(base);
     given += max(q.have - q.want, 0);
   }
   scan(given, sums32, total);
@@ -112,13 +113,23 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   if (ring_ok && all_given > 0) {
     int before = 0;
     for (int base = 0; base < p.R; base += kStepThreads) {
-      const Request q = request_at(p, base + tid);
+      const Request q = request(base);
       first[tid] = scan(max(q.have - q.want, 0), sums32, total);
       from[tid] = q.want;
       __syncthreads();
-      for (int i = tid; i < total; i += kStepThreads) {
-        const int k = last_not_above(first, kStepThreads, i);
-        p.free_pages[(tail + before + i) % p.n_pages] = p.tables[(size_t)(base + k) * p.max_pages + from[k] + i - first[k]];
+      const int start = (int)((tail + before) % p.n_pages);        // (no more than n_pages come back: the ring has room for them)
+      for (int at = tid; at < total; at += kBatch * kStepThreads) {
+        int id[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int i = at + u * kStepThreads, k = last_not_above(first, i);
+          if (i < total) id[u] = p.tables[(size_t)(base + k) * p.max_pages + from[k] + i - first[k]];
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int i = at + u * kStepThreads;
+          if (i < total) p.free_pages[around(start, i, p.n_pages)] = id[u];
+        }
       }
       before += total;
       __syncthreads();
@@ -132,7 +143,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   StepRequest* out = reinterpret_cast<StepRequest*>(reinterpret_cast<uint8_t*>(p.head) + kStepHeadBytes);
   for (int base = 0; base < p.R; base += kStepThreads) {
     const int r = base + tid;
-    const Request q = request_at(p, r);
+    const Request q = request(base);
     long long all_rows;
     const long long row0 = rows_before + scan(q.rows, sums64, all_rows);
     const bool fits = row0 + q.rows <= p.M || q.rows == 0;
@@ -155,19 +166,37 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
       p.lengths_out[r] = ok ? q.next : q.len;
     }
     __syncthreads();
-    for (int i = tid; i < total; i += kStepThreads) {
-      const int k = last_not_above(first, kStepThreads, i);
-      if (from[k] < 0) continue;
-      const int id = p.free_pages[(head + wanted_before + i) % p.n_pages];
-      p.tables[(size_t)(base + k) * p.max_pages + from[k] + i - first[k]] = id;
+    // (whoever is not refused takes pages that are there: fewer than n_pages before them)
+    const int start = ring_ok ? (int)((head + min((long long)wanted_before, avail)) % p.n_pages) : 0;
+    for (int at = tid; at < total; at += kBatch * kStepThreads) {
+      int id[kBatch], entry[kBatch], of[kBatch];
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u) {
+        const int i = at + u * kStepThreads, k = last_not_above(first, i);
+        of[u] = i < total && from[k] >= 0 ? base + k : -1;
+        entry[u] = from[k] + i - first[k];
+        if (of[u] >= 0) id[u] = p.free_pages[around(start, i, p.n_pages)];
+      }
+#pragma unroll
+      for (int u = 0; u < kBatch; ++u)
+        if (of[u] >= 0) p.tables[(size_t)of[u] * p.max_pages + entry[u]] = id[u];
     }
     wanted_before += total;
     __syncthreads();
     if (rows_inside) {
       const int lo = (int)min(rows_before, (long long)p.M), hi = (int)min(rows_before + all_rows, (long long)p.M);
-      for (int row = lo + tid; row < hi; row += kStepThreads) {
-        const int k = last_not_above(row0s, kStepThreads, row);
-        put_row(p, row, base + k, row - row0s[k], ns[k], lens[k], fail);
+      for (int at = lo + tid; at < hi; at += kBatch * kStepThreads) {
+        int slot[kBatch], pos[kBatch];
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int row = at + u * kStepThreads, k = last_not_above(row0s, row);
+          if (row < hi) slot_of(p, base + k, row - row0s[k], ns[k], lens[k], fail, slot[u], pos[u]);
+        }
+#pragma unroll
+        for (int u = 0; u < kBatch; ++u) {
+          const int row = at + u * kStepThreads;
+          if (row < hi) { p.slots[row] = slot[u]; p.positions[row] = pos[u]; }
+        }
       }
       __syncthreads();
     }
@@ -175,7 +204,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   }
   const int rows = (int)min(rows_before, (long long)p.M);
   if (rows_inside)
-    for (int row = rows + tid; row < p.M; row += kStepThreads) put_row(p, row, 0, 0, 0, 0, fail);
+    for (int row = rows + tid; row < p.M; row += kStepThreads) p.slots[row] = p.positions[row] = -1;
   if (tid == 0) {
     p.ring_out[0] = head + taken;
     p.ring_out[1] = ring_ok ? tail + all_given : tail;
@@ -186,20 +215,23 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
     *p.head = h;
   }
 }
-// Slots of many rows: a CTA's 1024 rows, their requests by bisection in the plan.
+// Slots of many rows: a thread a row, its request by bisection in the plan.
 __global__ void __launch_bounds__(256) rows_kernel(const StepParams p) {
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   const StepRequest* reqs = requests_of(p.head);
-  for (int row = blockIdx.x * 1024 + threadIdx.x; row < min(p.M, (int)(blockIdx.x + 1) * 1024); row += 256) {
-    int lo = 0, hi = p.R;
-    while (hi - lo > 1) {
-      const int mid = (lo + hi) >> 1;
-      if (reqs[mid].row0 <= row) lo = mid; else hi = mid;
-    }
-    const StepRequest q = reqs[lo];
-    put_row(p, row, lo, row - q.row0, q.n, q.len, [&](int code) { report_error(&p.head->status, code, 10, lo, row); });
+  const int row = blockIdx.x * 256 + threadIdx.x;
+  if (row >= p.M) return;
+  int lo = 0, hi = p.R;
+  while (hi - lo > 1) {
+    const int mid = (lo + hi) >> 1;
+    if (reqs[mid].row0 <= row) lo = mid; else hi = mid;
   }
+  const StepRequest q = reqs[lo];
+  int slot, pos;
+  slot_of(p, lo, row - q.row0, q.n, q.len, [&](int code) { report_error(&p.head->status, code, 10, lo, row); }, slot, pos);
+  p.slots[row] = slot;
+  p.positions[row] = pos;
 }
 
 // ---------------------------------------------------------------------------- appending
@@ -286,7 +318,7 @@ cudaError_t launch_cache_step(const lqer_page_table_t& t, const int* lengths, co
   LaunchScope scope(kFamDecode, s, inside ? 1 : 2);
   cudaError_t e = kv::launch_after(kv::step_kernel, dim3(1), kv::kStepThreads, 0, s, p, inside ? 1 : 0);
   if (e != cudaSuccess || inside) return e;
-  return kv::launch_after(kv::rows_kernel, dim3((M + 1023) / 1024), 256, 0, s, p);
+  return kv::launch_after(kv::rows_kernel, dim3((M + 255) / 256), 256, 0, s, p);
 }
 cudaError_t launch_append_kv(const void* K, const void* V, int x_type, size_t k_stride, size_t v_stride, int M, const int* slots,
                              const lqer_kv_cache_t& c, int bits, int emin, int emax, cudaStream_t s) {
