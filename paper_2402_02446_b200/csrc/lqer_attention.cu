@@ -109,6 +109,10 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm vola
 __device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
+// CTAs to an SM.  What is on its way is enough with two of four warps; more only divide the work further, unless it is the conversion of mantissas that takes
+// the time (heads of 128, two / three, us: 64 requests, 40/8 heads, bf16 204 / 209; 24 requests, 40/40 heads, MXINT8 183 / 169; 16 rows a tile, 16
+// requests of 4 tokens: 65 / 74).
+__host__ __device__ constexpr int ctas_per_sm(int D, bool MX, int NT) { return D == 64 ? 4 : MX && NT == 1 ? 3 : 2; }
 template <bool MX> struct OctOf { using type = uint4; };
 template <> struct OctOf<true> { using type = uint2; };
 // A warp's ring: stages of 16 keys and their values as they lie in the cache (and their exponents behind each), their 16-byte pieces moved within a row so
@@ -118,19 +122,30 @@ struct Ring {
   static constexpr int ROWS = 8 * NT, ROW = MX ? D : 2 * D, PIECES = ROW / 16, SET = 16 * ROW, EXPS = MX ? D : 0, STAGE = 2 * (SET + EXPS);
   static constexpr int STAGES = MX ? 4 : 2, WARP = STAGES * STAGE;
   static constexpr int OUT = ROWS * (D + 4);                          // floats of a warp's sums, then its maxima and sums of weights: over its ring at the end
-  static constexpr int CTAS = D == 64 ? 4 : 3;
+  static constexpr int CTAS = ctas_per_sm(D, MX, NT);
   static_assert((OUT + 2 * ROWS) * 4 <= WARP, "a warp's sums fit its ring");
   __device__ static __forceinline__ int key_swizzle(int row) { return MX ? (D == 128 ? (row & 3) << 1 : ((row >> 1) & 1) << 1) : (row & 1) << 2 | ((row >> 1) & 3); }
   __device__ static __forceinline__ int value_swizzle(int row) { return MX && D == 64 ? ((row >> 1) & 1) << 1 : ((row >> 1) & 3) << 1; }
+  // Where a lane's pieces of a stage go: those of copy i lie 32 / PIECES rows behind those of copy i - 1, and the swizzles repeat after (at most) four.
+  static constexpr int COPIES = SET / 512, OFFSETS = COPIES < 4 ? COPIES : 4, STEP = 32 / PIECES;
+  static_assert(4 * STEP % 8 == 0 || COPIES <= 4, "the swizzles repeat");
+  uint32_t key_to[OFFSETS], value_to[OFFSETS];
+  __device__ __forceinline__ explicit Ring(int lane) {
+#pragma unroll
+    for (int i = 0; i < OFFSETS; ++i) {
+      const int r = lane / PIECES + i * STEP, c = lane % PIECES;
+      key_to[i] = r * ROW + ((c ^ key_swizzle(r)) << 4);
+      value_to[i] = SET + EXPS + r * ROW + ((c ^ value_swizzle(r)) << 4);
+    }
+  }
   // Sends a stage on its way: 16 rows from `row` on of the [.., D] tensors, which lie one after the other.
-  __device__ static __forceinline__ void fill(const Attention& p, uint32_t at, size_t row, int lane) {
+  __device__ __forceinline__ void fill(const Attention& p, uint32_t at, size_t row, int lane) const {
     const uint8_t* k = static_cast<const uint8_t*>(p.keys) + row * ROW + 16 * lane;
     const uint8_t* v = static_cast<const uint8_t*>(p.values) + row * ROW + 16 * lane;
 #pragma unroll
-    for (int i = 0; i < SET / 512; ++i) {
-      const int x = lane + 32 * i, r = x / PIECES, c = x % PIECES;
-      copy16(at + r * ROW + ((c ^ key_swizzle(r)) << 4), k + 512 * i);
-      copy16(at + SET + EXPS + r * ROW + ((c ^ value_swizzle(r)) << 4), v + 512 * i);
+    for (int i = 0; i < COPIES; ++i) {
+      copy16(at + key_to[i % OFFSETS] + i / OFFSETS * OFFSETS * STEP * ROW, k + 512 * i);
+      copy16(at + value_to[i % OFFSETS] + i / OFFSETS * OFFSETS * STEP * ROW, v + 512 * i);
     }
     if (MX && lane < 2 * EXPS / 16) {
       const int which = lane >= EXPS / 16, x = lane - which * (EXPS / 16);
@@ -171,6 +186,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
   if (u >= end) return;
   uint8_t* const ring = rings + warp * R::WARP;
   const uint32_t ring_at = tc::smem_u32(ring);
+  const R copier(lane);
   const StepRequest* reqs = requests_of(p.step);
   const int shift = p.bits - 2;
   int r = run.request, turn = 0;
@@ -191,27 +207,26 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
     const bool alone = whole && run.per >= 12 * vis.chunks;
     const long long next = u + (c1 - c0);
     if (alone && (turn++ & 3) != warp) { u = next; continue; }
-    // a warp's step -> its first key: 16 keys of every chunk, or of a row of its own all
-    const int x0 = alone ? 0 : c0, x1 = alone ? 4 * vis.chunks : c1;
-    auto key_of = [&](int x) {
-      const int chunk = alone ? x >> 2 : x;
-      return (chunk < vis.sink_chunks ? chunk : vis.first_chunk + chunk - vis.sink_chunks) * kChunk + (alone ? x & 3 : warp) * 16;
-    };
+    // A warp's steps, of 16 keys: of every chunk its own, or of a row of its own all; behind the first tokens' they go on at the window's.
+    const int x0 = alone ? 0 : c0, x1 = alone ? 4 * vis.chunks : c1, hop = alone ? 16 : kChunk, mine_at = alone ? 0 : warp * 16;
+    const int jump_at = alone ? 4 * vis.sink_chunks : vis.sink_chunks, jump_to = vis.first_chunk * kChunk + mine_at;
+    int key0 = x0 < jump_at ? x0 * hop + mine_at : jump_to + (x0 - jump_at) * hop;     // first key of the step
+    auto next_key = [&](int key, int x) { return x + 1 == jump_at ? jump_to : key + hop; };
     const int* table = p.tables + (size_t)r * p.max_pages;
-    auto entry_of = [&](int x) {
-      const int key = key_of(x);
-      return x < x1 && key < len ? __ldg(table + (key >> p.page_shift)) : 0;
-    };
-    int entry = entry_of(x0);                             // of the step that is sent next
-    auto send = [&](int x) {
-      const int key = key_of(x);
-      if (x < x1 && key < len)
-        R::fill(p, ring_at + (x - x0) % R::STAGES * R::STAGE, (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (key & (p.page - 1)), lane);
+    int sent = x0, sent_key = key0, place = 0, sent_place = 0;      // the step that is sent next, its first key and its page
+    auto entry_of = [&]() { return sent < x1 && sent_key < len ? __ldg(table + (sent_key >> p.page_shift)) : 0; };
+    int entry = entry_of();
+    auto send = [&]() {
+      if (sent < x1 && sent_key < len)
+        copier.fill(p, ring_at + sent_place, (((size_t)checked_page(p, entry, r) * p.hkv + h) << p.page_shift) + (sent_key & (p.page - 1)), lane);
       copies_sent();
-      entry = entry_of(x + 1);
+      sent_place = sent_place == (R::STAGES - 1) * R::STAGE ? 0 : sent_place + R::STAGE;
+      sent_key = next_key(sent_key, sent);
+      ++sent;
+      entry = entry_of();
     };
 #pragma unroll
-    for (int i = 0; i < R::STAGES - 1; ++i) send(x0 + i);
+    for (int i = 0; i < R::STAGES - 1; ++i) send();
     // the row tile's queries, in the order in which a lane holds a key
     uint4 q[NT][D / 32];
     int pos[NT][2];
@@ -241,13 +256,11 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
       m[t][0] = m[t][1] = -INFINITY;
       l[t][0] = l[t][1] = 0.f;
     }
-    for (int x = x0; x < x1; ++x) {
-      const int key0 = key_of(x);
-      if (key0 >= len) break;                             // the last chunk's end
-      send(x + R::STAGES - 1);
+    for (int x = x0; x < x1 && key0 < len; key0 = next_key(key0, x), ++x) {      // (the last chunk may end before its warps' keys)
+      send();
       copies_wait<R::STAGES - 1>();
       __syncwarp();
-      const uint8_t* const keys = ring + (x - x0) % R::STAGES * R::STAGE;
+      const uint8_t* const keys = ring + place;
       const uint8_t* const values = keys + R::SET + R::EXPS;
       float sc[NT][4];
 #pragma unroll
@@ -373,6 +386,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
         for (int t = 0; t < NT; ++t) mma(o[t][i], a0, a1, a2, a3, pb[t][0], pb[t][1]);
       }
       __syncwarp();                                       // the stage may be filled again
+      place = place == (R::STAGES - 1) * R::STAGE ? 0 : place + R::STAGE;
     }
     copies_wait<0>();
     __syncwarp();
@@ -533,11 +547,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Split s) {
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
 }
 
-static int split_grid(const Attention& p, int few, int rows_per, int dim) {
+static int split_grid(const Attention& p, int few, int rows_per, int dim, bool mx) {
   const long long most_rows = (long long)(few < p.M * (long long)p.group ? few : p.M * (long long)p.group);
   const long long tiles = (most_rows + rows_per - 1) / rows_per, chunks = ((long long)p.max_pages * p.page + kChunk - 1) / kChunk;
   const long long units = (long long)(p.R < p.M ? p.R : p.M) * tiles * p.hkv * chunks;
-  const long long per_sm = dim == 64 ? 4 : 3, most = (long long)sm_count() * per_sm;
+  const long long most = (long long)sm_count() * ctas_per_sm(dim, mx, rows_per / 8);
   const long long want = (units + kMinChunks - 1) / kMinChunks;
   return (int)(want < most ? want : most);
 }
@@ -575,7 +589,7 @@ static size_t spans_bytes() { return ((size_t)4 * sm_count() * sizeof(kv::Span) 
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
   const int rows = kv::rows_per_tile(p);
-  return spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, c.head_dim) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+  return spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, c.head_dim, c.dtype == LQER_MXINT8) * 2 * rows * (c.head_dim + 2) * sizeof(float);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
                                    int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
@@ -599,8 +613,8 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
     const cudaError_t e = kv::launch_tiles(k.a, k.few, k.y_extent, c, s);
     if (e != cudaSuccess || t.n_requests == 1) return e;
   }
-  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows, c.head_dim);
   const bool mx = c.dtype == LQER_MXINT8;
+  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows, c.head_dim, mx);
   if (c.head_dim == 128)
     return rows == 8 ? (mx ? kv::launch_split<128, true, 1>(k, grid, s) : kv::launch_split<128, false, 1>(k, grid, s))
                      : (mx ? kv::launch_split<128, true, 2>(k, grid, s) : kv::launch_split<128, false, 2>(k, grid, s));
