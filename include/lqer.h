@@ -420,15 +420,17 @@ lqer_status_t lqer_append_kv(const void* K, const void* V, lqer_dtype_t x_dtype,
  *   Y[m, h] = sum_j softmax_j(scale Q[m, h] . K[j, h / g]) V[j, h / g],   g = q_heads / kv_heads,
  * over the tokens j of row m's request up to its own position p, and with window > 0 only those with j > p - window or j < sinks.
  *  - Q: M rows of q_heads * head_dim bf16 elements, q_stride elements from row to row (a multiple of 8); Y [M, q_heads, head_dim] bf16, dense, apart
- *    from everything else.  q_heads is a multiple of kv_heads, at most 1024; M * q_heads < 2^31.
+ *    from everything else.  q_heads is a multiple of kv_heads, at most 1024; M * q_heads < 2^31.  |scale| < 1e30.
  *  - step: made by lqer_cache_step for the same M and a table of these sizes; max_added: at least the step's (kernels are chosen
  *    by it).  The plan is only read, but for its status: one of another batch or table (or none) is reported there as LQER_ERR_BAD_PACKED and
  *    nothing is written; a table entry that is no page as LQER_ERR_BOUNDS (the rows of that request then hold anything).  Rows behind the last token
  *    and those of refused requests are left as they are.
- *  - Scores, their maxima and all sums are fp32; the weights of the values are rounded to bf16.  What a row does not see may hold anything where no
- *    row of the step sees it; an infinite or NaN value that some rows of a request see and others do not may reach those, too.
+ *  - Scores, their maxima and all sums are fp32; the weights of the values are rounded to bf16.  What no row of the step sees may hold anything; an
+ *    infinite or NaN value that some rows of a request see and others do not may reach those, too.  Exponents of an MXINT8 cache that are seen lie
+ *    within the format's window, as lqer_append_kv writes them.
  *  - workspace: lqer_attention_workspace_bytes, 256-byte aligned; nothing in it has to be kept or cleared, and calls that overlap need one each.
- *    Sums are taken in an order that depends on the whole batch's lengths, so a row's last bits may; for one batch they are always the same. */
+ *    Sums are taken in an order that depends on the whole batch's lengths, so a row's last bits may; for one batch they are always the same.
+ *  - Requests of many rows take a kernel with bounded waits; one that ran out is reported in step as LQER_ERR_TIMEOUT. */
 lqer_status_t lqer_attention_workspace_bytes(int M, int q_heads, const lqer_kv_cache_t* cache, const lqer_page_table_t* table, int max_added,
                                              size_t* bytes);
 lqer_status_t lqer_paged_attention(const void* Q, long long q_stride, int M, int q_heads, const lqer_kv_cache_t* cache, const lqer_page_table_t* table,

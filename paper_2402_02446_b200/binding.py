@@ -716,6 +716,7 @@ class KVCache:
             raise ValueError("a cache holds torch.bfloat16 or MXINT8")
         self.n_pages, self.page, self.kv_heads, self.head_dim = n_pages, page, kv_heads, head_dim
         self.dtype = MXINT8 if code == 2 else torch.bfloat16
+        self.key = (n_pages, page, kv_heads, head_dim, code)
         self.handle = _Cache(None, None, n_pages, page, kv_heads, head_dim, code)
         self.ref = C.byref(self.handle)
         size = C.c_size_t()
@@ -742,6 +743,7 @@ class PageTable:
 
     def __init__(self, n_requests: int, max_pages: int, n_pages: int, page: int, device):
         self.n_requests, self.max_pages, self.n_pages, self.page = n_requests, max_pages, n_pages, page
+        self.key = (n_requests, max_pages, n_pages, page)
         size = C.c_size_t()
         _check(lib().lqer_cache_step_bytes(n_requests, C.byref(size)), "lqer_cache_step_bytes")
         self.step_bytes = size.value
@@ -773,6 +775,7 @@ class CacheStep:
         self.slots, self.positions = new(M), new(M)
         self.lengths, self.ring = new(pages.n_requests), new(2, dtype=torch.int64)
         self.own_lengths, self.own_ring = self.lengths, self.ring
+        self.room = {}                 # workspace bytes by heads and cache format, for this M and max_added
 
 
 def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | None = None, step: CacheStep | None = None, commit: bool = True,
@@ -802,7 +805,9 @@ def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | N
                                    _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_cache_step")
-    step.max_added, step.lengths, step.ring = max_added, lengths, ring
+    if step.max_added != max_added:
+        step.max_added, step.room = max_added, {}
+    step.lengths, step.ring = lengths, ring
     return step
 
 
@@ -863,10 +868,17 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, pages: PageTable, step: Cac
     elif Y.shape != shape or Y.dtype != torch.bfloat16:
         raise ValueError("expected Y bf16 [M, q_heads, head_dim]")
     if ws is None:
-        ws = Q.new_empty(attention_workspace_bytes(M, heads, cache, pages, step.max_added), dtype=torch.uint8)
+        key = (heads, cache.key, pages.key)
+        room = step.room.get(key)
+        if room is None:
+            room = step.room[key] = attention_workspace_bytes(M, heads, cache, pages, step.max_added)
+        ws = Q.new_empty(room, dtype=torch.uint8)
+        ws_ptr = ws.data_ptr()
+    else:
+        ws_ptr, room = _ptr(ws, index), ws.numel() * ws.element_size()
     status = lib().lqer_paged_attention(q_ptr, q_stride, M, heads, cache.ref, pages.ref, step.buf.data_ptr(), step.max_added, window, sinks,
-                                        D ** -0.5 if scale is None else scale, None if cfg is None else C.byref(cfg), _ptr(Y, index), _ptr(ws, index),
-                                        ws.numel() * ws.element_size(), _raw_stream(index))
+                                        D ** -0.5 if scale is None else scale, None if cfg is None else C.byref(cfg), _ptr(Y, index), ws_ptr, room,
+                                        _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_paged_attention")
     return Y

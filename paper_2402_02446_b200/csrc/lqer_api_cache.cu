@@ -120,7 +120,7 @@ lqer_status_t lqer_paged_attention(const void* Q, long long q_stride, int M, int
   if (st != LQER_OK) return st;
   lqer_config_t f;
   if ((st = activation_format(cfg, &f)) != LQER_OK) return st;
-  if (!(scale - scale == 0.0)) return LQER_ERR_CONFIG;
+  if (!(scale < 1e30 && scale > -1e30)) return LQER_ERR_CONFIG;
   if ((st = attention_shape(M, q_heads, cache, table, max_added)) != LQER_OK) return st;
   if (q_stride < (long long)q_heads * cache->head_dim || q_stride % 8 != 0 || q_stride > (1LL << 32) || window < 0 || sinks < 0) return LQER_ERR_SHAPE;
   if (misaligned(Q) || misaligned(Y) || misaligned(step, 256) || misaligned(workspace, 256)) return LQER_ERR_ALIGN;

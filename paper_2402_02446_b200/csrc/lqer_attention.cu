@@ -598,7 +598,10 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
   k.a = attention_params(c, t, M, hq, max_added);
   k.a.Q = Q; k.a.Y = Y; k.a.q_stride = q_stride;
   k.a.tables = t.tables; k.a.step = static_cast<kv::StepHead*>(step);
-  k.a.window = window; k.a.sinks = window > 0 ? sinks : 0;
+  // a window as long as the tables hides nothing; and positions are below 2^30, so that no difference of one with either overflows
+  const long long room = (long long)t.max_pages * t.page;
+  k.a.window = window < room ? window : 0;
+  k.a.sinks = k.a.window == 0 ? 0 : sinks < (1 << 30) ? sinks : 1 << 30;
   k.a.scale_log2 = (float)(scale * 1.4426950408889634);
   k.a.bits = bits; k.a.emin = emin; k.a.emax = emax;
   k.few = kv::few_rows(k.a);

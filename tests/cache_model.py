@@ -110,7 +110,7 @@ class Batch:
     """A cache and its tables, filled through the library in two steps: what the requests hold, and their new tokens, with anything where no token is."""
 
     def __init__(self, requests, hq, hkv, D, page, dtype=torch.bfloat16, pad=0, spare=3, x_dtype=torch.bfloat16, cfg=None, seed=0, max_added=None, scale=1.5,
-                 dev="cuda:0"):
+                 dev="cuda:0", shuffle=True):
         self.requests, self.hq, self.hkv, self.D, self.cfg, self.dev = requests, hq, hkv, D, cfg, dev
         R = len(requests)
         pages = [(a + b + page - 1) // page for a, b in requests]
@@ -118,7 +118,8 @@ class Batch:
         g = torch.Generator(device=dev).manual_seed(seed)
         rand = lambda *s: torch.randn(s, generator=g, device=dev)  # noqa: E731
         self.pages = L.new_page_table(R, max_pages, n_pages, page, device=dev)
-        self.pages.free.copy_(torch.randperm(n_pages, generator=g, device=dev, dtype=torch.int32))
+        order = torch.arange(n_pages, device=dev, dtype=torch.int32)
+        self.pages.free.copy_(order[torch.randperm(n_pages, generator=g, device=dev)] if shuffle else order.flip(0))
         self.cache = L.new_kv_cache(n_pages, page, hkv, D, dtype=dtype, device=dev)
         for t in (self.cache.keys, self.cache.values):
             t.fill_(float("nan")) if t.dtype == torch.bfloat16 else t.fill_(0xFF)
@@ -135,17 +136,19 @@ class Batch:
         assert L.poll_status(self.step.buf) == 0
         self.Q = (both[:, :hq * D] * scale).to(torch.bfloat16).view(self.M, hq, D)
 
-    def check(self, Y, window=0, sinks=0, scale=None, left=None, log=None):
-        """Y against 64 bits, row by row; rows behind the last token hold `left` still."""
+    def check(self, Y, window=0, sinks=0, scale=None, left=None, log=None, values=None):
+        """Y against 64 bits, row by row; rows behind the last token hold `left` still.  values: gives pages' keys and values, where not all are wanted."""
         scale = self.D ** -0.5 if scale is None else scale
-        keys, values = cache_values(self.cache, self.cfg)
+        if values is None:
+            whole = cache_values(self.cache, self.cfg)
+            values = lambda ids: tuple(x[ids] for x in whole)  # noqa: E731
         page, row, worst = self.pages.page, 0, 0.0
         for r, (before, n) in enumerate(self.requests):
             if n == 0:
                 continue
             length = before + n
             ids = self.pages.tables[r, :(length + page - 1) // page].long()
-            K, V = (x[ids].transpose(0, 1).flatten(1, 2)[:, :length] for x in (keys, values))
+            K, V = (x.transpose(0, 1).flatten(1, 2)[:, :length] for x in values(ids))
             y, weighed, most = attention64(self.Q[row:row + n].double(), K, V, n, window, sinks, scale)
             off = (Y[row:row + n].double() - y).abs() / tolerance(y, weighed, most, self.D, length)
             assert bool(torch.isfinite(Y[row:row + n]).all()), f"request {r}"

@@ -96,13 +96,13 @@ def test_attention_refusals():
     for kw in (dict(Q=None), dict(Y=None), dict(step=None), dict(k=None), dict(v=None), dict(t=None), dict(ws=None), dict(cache=C.POINTER(binding._Cache)()),
                dict(table=C.POINTER(binding._Table)())):
         assert attend(**kw) == E("LQER_ERR_NULL"), kw
-    for kw in (dict(M=0), dict(M=(1 << 24) + 1), dict(heads=0), dict(heads=3), dict(heads=1026, stride=1 << 17), dict(most=0), dict(stride=248), dict(stride=260),
+    for kw in (dict(M=0), dict(M=(1 << 24) + 1), dict(heads=0), dict(heads=3), dict(heads=1026, stride=1 << 17), dict(M=1 << 24, heads=128, stride=1 << 14), dict(most=0), dict(stride=248), dict(stride=260),
                dict(stride=(1 << 32) + 8), dict(window=-1), dict(sinks=-1), dict(page=8), dict(dim=96), dict(heads_kv=0), dict(R=0), dict(max_pages=0),
                dict(table_pages=9), dict(table_page=32)):
         assert attend(**kw) == E("LQER_ERR_SHAPE"), kw
     for kw in (dict(Q=P + 8), dict(Y=P + 8), dict(step=P + 16), dict(ws=P + 16), dict(k=P + 8), dict(t=P + 2)):
         assert attend(**kw) == E("LQER_ERR_ALIGN"), kw
-    for kw in (dict(Y=3 * P), dict(Y=P), dict(Y=2 * P), dict(scale=float("nan")), dict(scale=float("inf")), dict(dtype=F32), dict(cfg=_bad_cfg())):
+    for kw in (dict(Y=3 * P), dict(Y=P), dict(Y=2 * P), dict(scale=float("nan")), dict(scale=float("inf")), dict(scale=-1e30), dict(dtype=F32), dict(cfg=_bad_cfg())):
         assert attend(**kw) == E("LQER_ERR_CONFIG"), kw
     assert need(4, 4, _cache(), _table(), 1, None) == E("LQER_ERR_NULL")
     assert need(4, 4, None, _table(), 1, C.byref(size)) == need(4, 4, _cache(), None, 1, C.byref(size)) == E("LQER_ERR_NULL")

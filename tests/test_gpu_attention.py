@@ -61,3 +61,146 @@ def test_other_scales(scale, ratio_log):
 def test_a_long_request_beside_many_short_ones(ratio_log):
     _run(Batch([(30000, 1)] + [(3 * i % 40, 1) for i in range(300)], 8, 2, 128, 16), log=ratio_log)
     _run(Batch([(9000, 400), (12, 1), (0, 33)], 4, 2, 128, 64, max_added=400), log=ratio_log)
+
+
+@pytest.mark.parametrize("dtype", [BF16, L.MXINT8])
+@pytest.mark.parametrize("hq,hkv,D", [(8, 8, 64), (16, 8, 128)])
+def test_many_short_requests(hq, hkv, D, dtype, ratio_log):
+    # so many that a warp takes a whole row
+    _run(Batch([(i * 7 % 61, 1 + i % 3) for i in range(1400)], hq, hkv, D, 16, dtype, pad=2), log=ratio_log)
+
+
+def test_narrower_mantissas_and_fp32_rows(ratio_log):
+    cfg = L.default_config()
+    cfg.a_bits, cfg.exp_min, cfg.exp_max = 6, -9, 4
+    for requests in ([(90, 2), (33, 1)], [(90, 200), (0, 40)]):
+        _run(Batch(requests, 8, 4, 128, 16, L.MXINT8, x_dtype=torch.float32, cfg=cfg), 50, 3, log=ratio_log)
+
+
+@pytest.mark.parametrize("requests", [[(700, 1), (3, 1)], [(64, 4), (9, 1)], [(100, 300), (5, 1)]])
+def test_views_streams_and_replays(requests):
+    b = Batch(requests, 8, 2, 128, 16, pad=1)
+    want = _run(b)
+    # rows of a wider tensor, results off a 32-byte boundary, a given workspace
+    wide = torch.zeros((b.M, 8 * 128 + 24), dtype=BF16, device=DEV)
+    Q = wide[:, 8:8 + 8 * 128].unflatten(1, (8, 128))
+    Q.copy_(b.Q)
+    flat = torch.full((b.M * 8 * 128 + 8,), 7.0, dtype=BF16, device=DEV)
+    Y = flat[8:].view(b.M, 8, 128)
+    ws = torch.empty(L.attention_workspace_bytes(b.M, 8, b.cache, b.pages, b.step.max_added), dtype=torch.uint8, device=DEV)
+    ws.fill_(0xFF)
+    assert L.paged_attention(Q, b.cache, b.pages, b.step, Y=Y, ws=ws) is Y
+    assert torch.equal(Y, want) and torch.all(flat[:8] == 7)
+    # another stream
+    s = torch.cuda.Stream(DEV)
+    s.wait_stream(torch.cuda.current_stream())
+    Z = L.paged_attention(b.Q, b.cache, b.pages, b.step, stream=s)
+    torch.cuda.synchronize()
+    n = sum(x for _, x in requests)
+    assert torch.equal(Z[:n], want[:n])
+    # a replay sees what the tensors hold then
+    with torch.cuda.stream(s):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=s):
+            L.paged_attention(Q, b.cache, b.pages, b.step, Y=Y, ws=ws)
+    Q.copy_(-b.Q)
+    torch.cuda.synchronize()
+    graph.replay()
+    torch.cuda.synchronize()
+    other = L.paged_attention(-b.Q, b.cache, b.pages, b.step)
+    assert torch.equal(Y[:n], other[:n]) and not torch.equal(Y[:n], want[:n])
+
+
+def test_generations_as_a_program_runs_them():
+    """Two layers' caches under one table: prompts, decoding, drafts of which some are refused, a request that ends and one that takes its place; all through one
+    captured step where the batch is decoding.  The attention of every step against 64 bits."""
+    hq, hkv, D, page, R = 8, 2, 64, 16, 4
+    pages = L.new_page_table(R, 12, 30, page, device=DEV)
+    caches = [L.new_kv_cache(30, page, hkv, D, dtype=dt, device=DEV) for dt in (BF16, L.MXINT8)]
+    g = torch.Generator(device=DEV).manual_seed(5)
+
+    def step(added, M, most):
+        plan = L.cache_step(pages, torch.tensor(added, dtype=torch.int32, device=DEV), M, max_added=most)
+        for cache in caches:
+            qkv = torch.randn((M, (hq + 2 * hkv) * D), generator=g, device=DEV).to(BF16)
+            L.append_kv(qkv[:, hq * D:(hq + hkv) * D], qkv[:, (hq + hkv) * D:], cache, plan.slots)
+            Q = qkv[:, :hq * D].unflatten(1, (hq, D))
+            Y = L.paged_attention(Q, cache, pages, plan)
+            assert L.poll_status(plan.buf) == 0
+            b = Batch.__new__(Batch)
+            b.requests = [(int(n) - max(a, 0), max(a, 0)) for n, a in zip(pages.lengths.tolist(), added)]
+            b.hq, b.hkv, b.D, b.cfg, b.pages, b.cache, b.Q = hq, hkv, D, None, pages, cache, Q
+            b.check(Y)
+
+    step([40, 7, 0, 100], 150, 100)
+    for _ in range(3):
+        step([1, 1, 0, 1], 4, 1)
+    step([4, 4, 0, 4], 12, 4)
+    step([1, -2, 33, -int(pages.lengths[3])], 40, 33)      # drafts refused, one ends, one begins
+    step([1, 1, 1, 60], 63, 60)                            # and its place is taken
+    step([1, 1, 1, 1], 7, 1)
+    held = sum((n + page - 1) // page for n in pages.lengths.tolist())
+    ring = pages.ring.tolist()
+    assert ring[1] - ring[0] == 30 - held
+    free = [pages.free[i % 30].item() for i in range(ring[0], ring[1])]
+    mine = [p for r in range(R) for p in pages.tables[r, :(pages.lengths[r] + page - 1) // page].tolist()]
+    assert sorted(free + mine) == list(range(30))
+
+
+def test_plans_that_do_not_fit_write_nothing():
+    b, other = Batch([(30, 2), (5, 1)], 8, 2, 64, 16), Batch([(30, 2), (5, 1), (1, 1)], 8, 2, 64, 16)
+    long, wide = Batch([(30, 200), (5, 1)], 8, 2, 64, 16), Batch([(30, 200), (5, 1), (1, 1)], 8, 2, 64, 16)
+    for mine, theirs in ((b, other), (long, wide)):
+        Y = torch.full((mine.M, 8, 64), 7.0, dtype=BF16, device=DEV)
+        theirs.step.M = mine.M                             # the binding is told otherwise: only the device can see
+        L.paged_attention(mine.Q, mine.cache, mine.pages, theirs.step, Y=Y)
+        assert L.poll_status(theirs.step.buf) == E("LQER_ERR_BAD_PACKED") and torch.all(Y == 7)
+
+
+@pytest.mark.parametrize("dtype", [BF16, L.MXINT8])
+@pytest.mark.parametrize("n", [1, 300])
+def test_an_entry_that_is_no_page_is_reported(n, dtype):
+    b = Batch([(40, n), (70, 1)], 8, 2, 64, 16, dtype)
+    want = _run(b)
+    b.pages.tables[0, 1] = 1 << 30
+    Y = L.paged_attention(b.Q, b.cache, b.pages, b.step)
+    assert L.poll_status(b.step.buf) == E("LQER_ERR_BOUNDS")
+    assert torch.equal(Y[n:n + 1], want[n:n + 1])
+
+
+def test_refused_requests_keep_their_rows():
+    b = Batch([(20, 1), (30, 1), (10, 1)], 4, 1, 64, 16, spare=0)
+    added = torch.tensor([1, 400, 1], dtype=torch.int32, device=DEV)
+    step = L.cache_step(b.pages, added, 402)
+    assert L.poll_status(step.buf) in (E("LQER_ERR_BOUNDS"), E("LQER_ERR_BUFFER_TOO_SMALL"))
+    Q = torch.randn((402, 4, 64), device=DEV).to(BF16)
+    Y = torch.full_like(Q, 7.0)
+    L.append_kv(torch.zeros((402, 64), device=DEV), torch.zeros((402, 64), device=DEV), b.cache, step.slots)
+    L.paged_attention(Q, b.cache, b.pages, step, Y=Y)
+    assert torch.all(Y[1:401] == 7) and not torch.any(Y[0] == 7) and not torch.any(Y[401] == 7)
+
+
+@pytest.mark.parametrize("dtype", [BF16, L.MXINT8])
+def test_a_wait_that_runs_out(dtype):
+    b = Batch([(100, 300), (0, 150)], 8, 2, 128, 16, dtype)
+    want = _run(b)
+    try:
+        L.set_wait_limit_cycles(1_000_000)
+        L.inject_stall(7)
+        L.paged_attention(b.Q, b.cache, b.pages, b.step)
+        assert L.poll_status(b.step.buf) == E("LQER_ERR_TIMEOUT")
+    finally:
+        L.inject_stall(-1)
+        L.set_wait_limit_cycles(4_000_000_000)
+    b.step.buf[:16].zero_()
+    assert torch.equal(L.paged_attention(b.Q, b.cache, b.pages, b.step), want)
+
+
+def test_results_are_the_same_every_time():
+    for requests in ([(3000, 1), (17, 1), (900, 1)], [(3000, 3), (40, 1)], [(800, 300), (0, 77)]):
+        b = Batch(requests, 16, 2, 128, 16)
+        first = L.paged_attention(b.Q, b.cache, b.pages, b.step, window=700, sinks=2)
+        for _ in range(5):
+            assert torch.equal(L.paged_attention(b.Q, b.cache, b.pages, b.step, window=700, sinks=2), first)
+    # a window that hides nothing is none
+    assert torch.equal(L.paged_attention(b.Q, b.cache, b.pages, b.step, window=2 ** 31 - 1, sinks=2 ** 31 - 1), L.paged_attention(b.Q, b.cache, b.pages, b.step))
