@@ -109,10 +109,10 @@ __device__ __forceinline__ void copy16(uint32_t to, const void* from) { asm vola
 __device__ __forceinline__ void copies_sent() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ __forceinline__ void copies_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-// CTAs to an SM.  What is on its way is enough with two of four warps; more only divide the work further, unless it is the conversion of mantissas that takes
-// the time (heads of 128, two / three, us: 64 requests, 40/8 heads, bf16 204 / 209; 24 requests, 40/40 heads, MXINT8 183 / 169; 16 rows a tile, 16
-// requests of 4 tokens: 65 / 74).
-__host__ __device__ constexpr int ctas_per_sm(int D, bool MX, int NT) { return D == 64 ? 4 : MX && NT == 1 ? 3 : 2; }
+// CTAs to an SM: more warps hide more of one another's latency, fewer divide the work less and leave a warp its registers.  Heads of 128, three / two to an SM,
+// us: 64 requests of up to 8191 tokens, 40/8 heads, bf16 209 / 204, 256 of up to 120, 32/32 heads, 71 / 80, one of 16000 16.4 / 17.6; 24 requests, 40/40 heads,
+// MXINT8 169 / 183; 16 rows a tile, 16 requests of 4 tokens 74 / 65.
+__host__ __device__ constexpr int ctas_per_sm(int D, int NT) { return D == 64 ? 4 : NT == 1 ? 3 : 2; }
 template <bool MX> struct OctOf { using type = uint4; };
 template <> struct OctOf<true> { using type = uint2; };
 // A warp's ring: stages of 16 keys and their values as they lie in the cache (and their exponents behind each), their 16-byte pieces moved within a row so
@@ -122,7 +122,7 @@ struct Ring {
   static constexpr int ROWS = 8 * NT, ROW = MX ? D : 2 * D, PIECES = ROW / 16, SET = 16 * ROW, EXPS = MX ? D : 0, STAGE = 2 * (SET + EXPS);
   static constexpr int STAGES = MX ? 4 : 2, WARP = STAGES * STAGE;
   static constexpr int OUT = ROWS * (D + 4);                          // floats of a warp's sums, then its maxima and sums of weights: over its ring at the end
-  static constexpr int CTAS = ctas_per_sm(D, MX, NT);
+  static constexpr int CTAS = ctas_per_sm(D, NT);
   static_assert((OUT + 2 * ROWS) * 4 <= WARP, "a warp's sums fit its ring");
   __device__ static __forceinline__ int key_swizzle(int row) { return MX ? (D == 128 ? (row & 3) << 1 : ((row >> 1) & 1) << 1) : (row & 1) << 2 | ((row >> 1) & 3); }
   __device__ static __forceinline__ int value_swizzle(int row) { return MX && D == 64 ? ((row >> 1) & 1) << 1 : ((row >> 1) & 3) << 1; }
@@ -547,11 +547,11 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Split s) {
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
 }
 
-static int split_grid(const Attention& p, int few, int rows_per, int dim, bool mx) {
+static int split_grid(const Attention& p, int few, int rows_per, int dim) {
   const long long most_rows = (long long)(few < p.M * (long long)p.group ? few : p.M * (long long)p.group);
   const long long tiles = (most_rows + rows_per - 1) / rows_per, chunks = ((long long)p.max_pages * p.page + kChunk - 1) / kChunk;
   const long long units = (long long)(p.R < p.M ? p.R : p.M) * tiles * p.hkv * chunks;
-  const long long most = (long long)sm_count() * ctas_per_sm(dim, mx, rows_per / 8);
+  const long long most = (long long)sm_count() * ctas_per_sm(dim, rows_per / 8);
   const long long want = (units + kMinChunks - 1) / kMinChunks;
   return (int)(want < most ? want : most);
 }
@@ -589,7 +589,7 @@ static size_t spans_bytes() { return ((size_t)4 * sm_count() * sizeof(kv::Span) 
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
   const int rows = kv::rows_per_tile(p);
-  return spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, c.head_dim, c.dtype == LQER_MXINT8) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+  return spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, c.head_dim) * 2 * rows * (c.head_dim + 2) * sizeof(float);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
                                    int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
@@ -617,7 +617,7 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
     if (e != cudaSuccess || t.n_requests == 1) return e;
   }
   const bool mx = c.dtype == LQER_MXINT8;
-  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows, c.head_dim, mx);
+  const int rows = kv::rows_per_tile(k.a), grid = kv::split_grid(k.a, k.few, rows, c.head_dim);
   if (c.head_dim == 128)
     return rows == 8 ? (mx ? kv::launch_split<128, true, 1>(k, grid, s) : kv::launch_split<128, false, 1>(k, grid, s))
                      : (mx ? kv::launch_split<128, true, 2>(k, grid, s) : kv::launch_split<128, false, 2>(k, grid, s));
