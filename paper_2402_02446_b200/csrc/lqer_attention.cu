@@ -32,7 +32,7 @@ inline int few_rows(const Attention& p) {
 constexpr int kMinChunks = 2;                // of a CTA's run
 
 // What a CTA leaves for the join: the (request, key head, row tile) that begins in its run and goes on behind it, if any.
-struct Span { int request, head, tile, parts; };
+struct Span { int row0, rows, head, tile, parts, unused[3]; };   // row0: the request's first row
 struct Split {
   Attention a;
   Span* spans;                               // [CTAs]
@@ -178,7 +178,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-  if (tid == 0) s.spans[blockIdx.x] = Span{0, 0, 0, 0};
+  if (tid == 0) s.spans[blockIdx.x].parts = 0;
   if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
   const Run run = find_run(s, ROWS, &sm_run);
   long long u = run.per * blockIdx.x;
@@ -471,7 +471,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
     }
     if (!whole && c0 == 0 && tid == 0) {
       const long long stop = before + (which + 1) * vis.chunks;      // where the row tile ends
-      s.spans[blockIdx.x] = Span{r, h, tile, (int)((stop - 1) / run.per) - (int)blockIdx.x + 1};
+      s.spans[blockIdx.x] = Span{row0, rows, h, tile, (int)((stop - 1) / run.per) - (int)blockIdx.x + 1, {}};
     }
     __syncthreads();
   }
@@ -490,8 +490,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Split s) {
   tc::pdl_wait();
   const Span span = s.spans[blockIdx.x];
   if (span.parts == 0) return;
-  const int4 req = __ldg(reinterpret_cast<const int4*>(requests_of(p.step) + span.request));
-  const int rows = min(ROWS, req.y * p.group - span.tile * ROWS), items = rows * QUADS, shares = kJoinThreads / items;
+  const int rows = span.rows, items = rows * QUADS, shares = kJoinThreads / items;
   const int tid = threadIdx.x, share = tid / items, item = tid - share * items, row = item / QUADS, d = 4 * (item - row * QUADS);
   const int per = (span.parts + shares - 1) / shares, from = share * per, to = share < shares ? min(from + per, span.parts) : from;
   auto part = [&](int i) { return s.parts + (size_t)(2 * (blockIdx.x + i) + (i == 0 ? 1 : 0)) * ROWS * (D + 2); };
@@ -542,7 +541,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Split s) {
   if (share > 0) return;
   const float inv = all == 0.f ? 0.f : 1.f / all;
   const int x = span.tile * ROWS + row;
-  const size_t at = ((size_t)(req.x + x / p.group) * p.hq + span.head * p.group + x % p.group) * D + d;
+  const size_t at = ((size_t)(span.row0 + x / p.group) * p.hq + span.head * p.group + x % p.group) * D + d;
   if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 61))
     *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
 }
