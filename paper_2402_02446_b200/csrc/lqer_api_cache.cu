@@ -128,8 +128,8 @@ lqer_status_t lqer_paged_attention(const void* Q, long long q_stride, int M, int
   if (workspace == nullptr) return LQER_ERR_NULL;
   if (workspace_bytes < attention_scratch_bytes(*cache, *table, M, q_heads, max_added)) return LQER_ERR_BUFFER_TOO_SMALL;
   if ((st = check_arch()) != LQER_OK) return st;
-  return of(launch_paged_attention(Q, (size_t)q_stride, M, q_heads, *cache, *table, step, max_added, window, sinks, scale, f.a_bits, f.exp_min,
-                                   f.exp_max, Y, workspace, static_cast<cudaStream_t>(stream)));
+  return of(launch_paged_attention(Q, (size_t)q_stride, M, q_heads, *cache, *table, step, max_added, window, sinks, scale, f.a_bits, Y, workspace,
+                                   static_cast<cudaStream_t>(stream)));
 }
 
 }  // extern "C"

@@ -14,20 +14,27 @@
 // Work is counted in chunks of 64 keys of a (request, key head, row tile), all in one row; each CTA takes an equal run of them, wherever that begins
 // and ends, so lengths may differ as they like.  The four warps take 16 keys of every chunk and join at the end of a run's part; what is not a
 // whole row's part goes to the workspace, and a second kernel joins those parts, in the order of the keys.
+//
+// Measured (GPU time): 64 requests of up to 8191 tokens, 40/8 heads of 128, bf16: 209 us, 6.4 TB/s, what a copy reaches; 24 of up to 4099, 40/40 heads, MXINT8: 168 us,
+// 4.1 TB/s, bound by instructions (some 600 for a warp's 16 keys, more than half of them for the mantissas); eight long ones, four drafted tokens, 32/8 heads under a
+// window of 4096: 34 us, 3.9 TB/s (of it 5 before the first keys are there and 3 for the joining); one of 1021 tokens 9.3 us, of 16000 16, of
+// 100000 73: launches and a chain of trips to memory, then the bytes.  Tried: the CTA that brings a row's last part joins them (a launch less, 2 us on the host,
+// but 1 to 3 us more on the GPU where parts are many); mantissas' low bytes by multiplication (slower); more or deeper stages (none).
 #include "lqer_cache.cuh"
 
 namespace lqer {
 namespace kv {
 
 constexpr int kChunk = 64, kWarps = 4, kSplitThreads = 32 * kWarps;
-// Requests of up to this many rows of a key head (tokens times heads that share it) are taken here, of more by lqer_attention_tiles.cu.  There a request's
-// time is that of its keys (some 14 ns each, 256 rows at a time), as long as the requests' key heads are fewer than the SMs; here it is shared by all
-// SMs, but grows with the rows, 16 at a time (some 12 ns a key, over the SMs).  Both sides measured, here / there, 32/8 heads, us: one request, 8 tokens
-// behind 8000: 24 / 105, 64 behind 4000: 46 / 64; two, 40 tokens: 63 / 120; 8, 20 tokens behind 2000: 36 / 36; 64, 8 tokens: 418 / 318, 20: 200 / 106.
-constexpr int kLeast = 16;
+// Requests of up to this many rows of a key head (tokens times heads that share it) are taken here, of more by lqer_attention_tiles.cu.  There a tile of
+// keys costs what it costs for 256 rows, and where few requests leave SMs without work a request's keys are divided among them, for some 8 us; here
+// the time is shared by all SMs from the start, but grows with the rows, 16 at a time (some 12 ns a key and head, over the SMs).  Both sides measured, here /
+// there, 32/8 heads, us: one request, 64 rows behind 1000: 12 / 19, behind 4000: 19 / 27, behind 16000: 43 / 37; 128 rows: 14 / 19, 28 / 28, 69 / 40;
+// two, 64 rows: 16 / 22, 24 / 31, 54 / 51; 128 rows: 18 / 24, 34 / 32, 87 / 52; 8, 80 rows behind 2000: 36 / 36; 64, 32 rows: 418 / 318, 80: 200 / 106.
+constexpr int kLeast = 16, kMost = 96;
 inline int few_rows(const Attention& p) {
   const long long heads = (long long)(p.R < p.M ? p.R : p.M) * p.hkv, few = 2900 / heads;
-  return few < kLeast ? kLeast : (int)few;
+  return few < kLeast ? kLeast : few > kMost ? kMost : (int)few;
 }
 constexpr int kMinChunks = 2;                // of a CTA's run
 
@@ -585,24 +592,32 @@ static kv::Attention attention_params(const lqer_kv_cache_t& c, const lqer_page_
 }
 static size_t spans_bytes() { return ((size_t)4 * sm_count() * sizeof(kv::Span) + 255) & ~(size_t)255; }
 
+// Parts of few rows, and behind them those of tiles.
+static size_t few_bytes(const kv::Attention& p, int head_dim) {
+  const int rows = kv::rows_per_tile(p);
+  const size_t bytes = spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, head_dim) * 2 * rows * (head_dim + 2) * sizeof(float);
+  return (bytes + 255) & ~(size_t)255;
+}
+// A window as long as the tables hides nothing; and positions are below 2^30, so that no difference of one with either overflows.
+static void set_window(kv::Attention& p, int window, int sinks) {
+  p.window = window < (long long)p.max_pages * p.page ? window : 0;
+  p.sinks = p.window == 0 ? 0 : sinks < (1 << 30) ? sinks : 1 << 30;
+}
+// The most that a call takes, whatever its window.
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
-  const int rows = kv::rows_per_tile(p);
-  return spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, c.head_dim) * 2 * rows * (c.head_dim + 2) * sizeof(float);
+  return few_bytes(p, c.head_dim) + (max_added * (long long)p.group > kv::few_rows(p) ? kv::tiles_scratch_bytes(p, c.head_dim) : 0);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
-                                   int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
+                                   int max_added, int window, int sinks, double scale, int bits, void* Y, void* scratch,
                                    cudaStream_t s) {
   kv::Split k = {};
   k.a = attention_params(c, t, M, hq, max_added);
   k.a.Q = Q; k.a.Y = Y; k.a.q_stride = q_stride;
   k.a.tables = t.tables; k.a.step = static_cast<kv::StepHead*>(step);
-  // a window as long as the tables hides nothing; and positions are below 2^30, so that no difference of one with either overflows
-  const long long room = (long long)t.max_pages * t.page;
-  k.a.window = window < room ? window : 0;
-  k.a.sinks = k.a.window == 0 ? 0 : sinks < (1 << 30) ? sinks : 1 << 30;
+  set_window(k.a, window, sinks);
   k.a.scale_log2 = (float)(scale * 1.4426950408889634);
-  k.a.bits = bits; k.a.emin = emin; k.a.emax = emax;
+  k.a.bits = bits;
   k.few = kv::few_rows(k.a);
   k.spans = static_cast<kv::Span*>(scratch);
   k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + spans_bytes());
@@ -612,7 +627,7 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
     // A single request goes there whatever it turns out to bring; beside one that has to, only those of few rows stay (three prompts of 42 to 97 tokens,
     // 16/4 heads: 18.4 us where the smaller ones stayed, 11.7).
     k.few = t.n_requests == 1 ? 0 : kv::kLeast;
-    const cudaError_t e = kv::launch_tiles(k.a, k.few, k.y_extent, c, s);
+    const cudaError_t e = kv::launch_tiles(k.a, k.few, k.y_extent, c, static_cast<uint8_t*>(scratch) + few_bytes(k.a, c.head_dim), s);
     if (e != cudaSuccess || t.n_requests == 1) return e;
   }
   const bool mx = c.dtype == LQER_MXINT8;

@@ -8,10 +8,23 @@
 //   warps 0-3, 4-7   tile A, tile B: a thread owns a row: scores from tensor memory, maximum, weights back to tensor memory; no exchange
 //                    between threads.  The row's maximum is let lag by up to 2^8 before what is summed up is scaled anew (the sum
 //                    and the values carry the same factor, so nothing is lost), which after the first tiles is rare.
-//   copies           bf16: one warp, a lane a page: TMA brings pages into swizzled tiles.  MXINT8: four warps read the mantissas, form the exact bf16
+//   copies           bf16: one warp, a lane a page: TMA brings pages into swizzled tiles.  MXINT8: one warp copies pages as they lie, four form the exact bf16
 //                    values and store them into the same tiles.
-//   issuer           one lane: per key tile and row tile, O += P V of the last key tile, then S of the next.
+//   issuer           one lane: per key tile and row tile, O += P V of the last key tile, in two halves as the weights come, then S of the next.
 // Keys and values share a ring of tiles.  Every wait is bounded.
+//
+// Measured, 32/8 heads of 128, GPU time: a prompt of 8192 tokens 455 us (1.21 PFLOP/s of what a causal row sees, 0.72 of a long GEMM's burst rate; 545 us when
+// it runs without a pause and the power cap lowers the clock), from MXINT8 520, heads of 64 410; windows of 1024, 32/32 heads, MXINT8, 7682 tokens 218.  A key
+// tile takes a CTA 3300 clocks: 16 MMAs for each row tile at some 85 clocks (64 by the rate; S reads both operands from shared memory, 128 bytes a
+// clock), 2100 from S to the last weights, and the issuer's way between.  What a CTA does before its first and behind its last key tile takes
+// about five more.  Tried, and not faster under a full load: CTAs that stay and take items by turns, with the next queries under way (460 -> 470 us);
+// weights by the old maximum with the new one beside them, which takes 800 of the 2100 clocks away but not the total; two threads a row; an issuer for
+// each row tile (574); short loops over 32 columns (480 to 515).
+//
+// Where the items of 256 rows leave a last turn of CTAs half empty or more (few requests, short pieces of long prompts), that turn's items are divided over
+// their keys, up to 16 CTAs to one, and a second kernel joins the parts.  Whole / divided, us: 2048 tokens behind 10240, 40/8 heads (320 items) 480 / 412, MXINT8
+// 542 / 487; 512 behind 15488, 32/8 heads 222 / 135; 300 of 4000, two requests 69 / 53.  It is a kernel of its own: what it needs beside costs registers
+// that those without it miss (8192 tokens 455 -> 490 us, MXINT8 520 -> 610).
 #include "lqer_cache.cuh"
 
 namespace lqer {
@@ -39,6 +52,9 @@ struct Tiles {
   long long wait_limit;
   size_t y_extent;
   bool y_wide;                 // Y: aligned to 32 bytes
+  int sms;                     // items beyond whole turns of so many CTAs may be divided over their keys; 0: none is
+  struct Divided* divided;     // [1 + sms / 2]: their number (request of the first entry), and what they are
+  float* parts;                // [sms][256][D + 2]: rows' sums, then maxima and sums of weights
 };
 struct Barriers {
   unsigned long long full[8], empty[8], raw_full[6], raw_empty[6], s_full[2], p_half[2], p_full[2], o_done[2], q_full, drained;
@@ -85,9 +101,9 @@ __device__ __forceinline__ void store32(void* p, bool aligned, const uint32_t* u
   }
 }
 __device__ __forceinline__ void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-__device__ __forceinline__ float max3(float a, float b, float c) {
+__device__ __forceinline__ float max3(float a, float b, float c) {     // NaN if one is
   float r;
-  asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
+  asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
 
@@ -103,7 +119,7 @@ __device__ __forceinline__ F2 add2(F2 a, F2 b) { F2 r; asm("add.rn.f32x2 %0, %1,
 __device__ __forceinline__ void exp2_poly(F2 x, float& a, float& b) {
   float lo, hi;
   unf2(x, lo, hi);
-  x = f2(fmaxf(lo, -125.f), fmaxf(hi, -125.f));
+  x = f2(fmaxf(lo, -125.f), fmaxf(hi, -125.f));                           // (NaN gets lost here: the row's other weights are NaN then, too)
   const F2 round = f2(12582912.f, 12582912.f), minus = f2(-1.f, -1.f);      // 1.5 * 2^23: the sum's low bits are n
   const F2 r = add2(x, round), n = add2(r, f2(-12582912.f, -12582912.f)), f = fma2(n, minus, x);
   F2 q = fma2(f, f2(0.05517166853f, 0.05517166853f), f2(0.24261112511f, 0.24261112511f));
@@ -117,10 +133,15 @@ __device__ __forceinline__ void exp2_poly(F2 x, float& a, float& b) {
 }
 
 template <int N> struct Every { static constexpr int value = N; };
+// Pairs between two that take the polynomial, bf16 (8192 tokens, heads of 128 / 64, us: none 478 / 423, every eighth 472 / 411, fourth 465 / 405, third 478 / 405, second
+// 506 / 440).  Beside the conversion of MXINT8, which takes the same units, there are none (530 against 542).
 constexpr int kPolyEvery = 4;
 
-// What a CTA works on: 256 rows of a request's key head from `base` on, the first of them head `head0` of the group of token `token0`.
-struct Item { int request, head, row0, n, len, base, rows, token0, head0; };      // rows: n * group
+// What a CTA works on: 256 rows of a request's key head from `base` on, the first of them head `head0` of the group of token `token0`; of its key tiles
+// part `part` of `parts`, the `slot`-th item that is divided at all.
+struct Item { int request, head, row0, n, len, base, rows, token0, head0, slot, part, parts; };      // rows: n * group
+struct Divided { int request, head, row0, rows, token0, head0, base, parts; };
+constexpr int kMostParts = 16;
 // Row z of an item: its token, and its head within the group.
 __device__ __forceinline__ void row_of(const Tiles& s, const Item& it, int z, int& token, int& head) {
   const uint32_t x = (uint32_t)(z + it.head0), q = s.a.group == 1 ? x : __umulhi(x, s.group_inv);
@@ -128,15 +149,20 @@ __device__ __forceinline__ void row_of(const Tiles& s, const Item& it, int z, in
   head = (int)(x - q * s.a.group);
 }
 // The key tiles that its two row tiles see: sink tiles, then [start, ..), `count` together; a row tile sees those of them in [from, end) and the sinks'.
+template <bool DIVIDED>
 struct Plan {
-  int sinks, sink_tiles, start, count;
+  int sinks, sink_tiles, start, count, skip;         // skip: turns of the parts before (DIVIDED)
   int from[2], end[2], first_pos[2], last_pos[2];
-  __device__ __forceinline__ int tile(int j) const { return j < sinks ? j : start + j - sinks; }
+  __device__ __forceinline__ int tile(int j) const {
+    if (DIVIDED) j += skip;
+    return j < sinks ? j : start + j - sinks;
+  }
   __device__ __forceinline__ bool sees(int t, int kv) const { return kv < (t ? end[1] : end[0]) && (kv >= (t ? from[1] : from[0]) || kv < sink_tiles); }
 };
-__device__ __forceinline__ Plan plan_of(const Tiles& s, const Item& it) {
+template <bool DIVIDED>
+__device__ __forceinline__ Plan<DIVIDED> plan_of(const Tiles& s, const Item& it) {
   const Attention& p = s.a;
-  Plan q;
+  Plan<DIVIDED> q;
   const int first = it.len - it.n;
   q.sink_tiles = p.window > 0 ? (min(p.sinks, it.len) + kKeys - 1) / kKeys : 0;
 #pragma unroll
@@ -154,14 +180,15 @@ __device__ __forceinline__ Plan plan_of(const Tiles& s, const Item& it) {
   q.start = q.from[0];
   q.sinks = min(q.sink_tiles, q.start);
   q.count = q.sinks + max(q.end[0], q.end[1]) - q.start;
+  q.skip = 0;
   return q;
 }
-// The CTA's item; heavy ones (a request's last) first.  False: there is none.
-__device__ __forceinline__ bool find_item(const Tiles& s, Item& it) {
+// The CTA's item, to where all threads find it; heavy ones (a request's last) first.  False: there is none.
+template <bool DIVIDED>
+__device__ __forceinline__ bool find_item(const Tiles& s, Item& found) {
   const Attention& p = s.a;
   const StepRequest* reqs = requests_of(p.step);
   __shared__ int sums[16];
-  __shared__ Item found;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
   const int per = (p.R + blockDim.x - 1) / blockDim.x, from = min(tid * per, p.R), to = min(from + per, p.R);
   auto items_of = [&](const int4& w) {
@@ -181,22 +208,28 @@ __device__ __forceinline__ bool find_item(const Tiles& s, Item& it) {
   __syncthreads();
   int before = x - mine, total = 0;
   for (int k = 0; k < warps; ++k) { if (k < warp) before += sums[k]; total += sums[k]; }
-  const int index = total - 1 - (int)(blockIdx.x / p.hkv);
-  if (index < 0) return false;
+  // All but the last turn of CTAs take an item each; what is left, if it would keep no more than half of them busy, is divided.
+  const long long all = (long long)total * p.hkv;
+  const int left = DIVIDED ? (int)(all % s.sms) : 0, parts = left > 0 ? min(s.sms / left, kMostParts) : 1;
+  const long long undivided = parts > 1 ? all - left : all;
+  if (DIVIDED && blockIdx.x == 0 && tid == 0) s.divided[0].request = parts > 1 ? left : 0;
+  const long long beyond = (long long)blockIdx.x - undivided, number = beyond < 0 ? blockIdx.x : undivided + beyond / parts;
+  if (number >= all) return false;
+  const int index = total - 1 - (int)(number / p.hkv);
   if (index >= before && index < before + mine) {
     for (int r = from;; ++r) {
       if (per > 1) w = __ldg(reinterpret_cast<const int4*>(reqs + r));
       const int c = items_of(w);
       if (index < before + c) {
         const int base = (index - before) * 2 * kRows, token = base / p.group;
-        found = Item{r, (int)(blockIdx.x % p.hkv), w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group};
+        found = Item{r, (int)(number % p.hkv), w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group, beyond < 0 ? -1 : (int)(beyond / parts),
+                     beyond < 0 ? 0 : (int)(beyond % parts), beyond < 0 ? 1 : parts};
         break;
       }
       before += c;
     }
   }
   __syncthreads();
-  it = found;
   return true;
 }
 // The columns of a key tile from key0 on that the row at `pos` sees, 32 to a word.
@@ -207,7 +240,7 @@ __device__ __forceinline__ uint32_t seen_columns(const Attention& p, int pos, in
   return w;
 }
 
-template <int D, bool MX>
+template <int D, bool MX, bool DIVIDED>
 __global__ void __launch_bounds__(Shape<D, MX>::THREADS, 1)
 tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const __grid_constant__ CUtensorMap value_map) {
   using SH = Shape<D, MX>;
@@ -247,15 +280,30 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     }
   }
   tc::pdl_wait();
-  if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
-  Item it;
-  if (!find_item(s, it)) return;
+  if (!step_fits(p, blockIdx.x == 0 && tid == 0)) {
+    if (DIVIDED && blockIdx.x == 0 && tid == 0) s.divided[0].request = 0;
+    return;
+  }
+  __shared__ Item item;
+  if (!find_item<DIVIDED>(s, item)) return;
+  const Item it = item;
+  Plan<DIVIDED> plan = plan_of<DIVIDED>(s, it);
+  int parts = 1;
+  if constexpr (DIVIDED) {
+    if (it.slot >= 0) {
+      // a part has two key tiles or more; an item with fewer has fewer parts
+      parts = min(it.parts, max((plan.count + 1) / 2, 1));
+      if (it.part == 0 && tid == 0) s.divided[1 + it.slot] = Divided{it.request, it.head, it.row0, it.rows, it.token0, it.head0, it.base, parts};
+      if (it.part >= parts) return;
+      plan.skip = (int)((long long)plan.count * it.part / parts);
+      plan.count = (int)((long long)plan.count * (it.part + 1) / parts) - plan.skip;
+    }
+  }
   if (warp == SH::ISSUER) tc::tmem_alloc(tc::smem_u32(&tmem_at), 512);
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
   const uint32_t tmem = tmem_at;
-  const Plan plan = plan_of(s, it);
   const int* table = p.tables + (size_t)it.request * p.max_pages;
   // keys that no row of the step sees: from the end on, and between the first tokens and the window
   const int seen_from = p.window > 0 ? max(0, it.len - it.n - p.window + 1) : 0;
@@ -267,7 +315,9 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   if (warp < 8) {
     // ---- a row tile
     // registers: what the launch gave, 128 x 512 or 168 x 384, shared out anew: 2 x 192 + 96 + 32 = 4 x 128, 2 x 216 + 72 = 3 x 168
-    if constexpr (MX) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
+    // (what the warps take together is what the block was launched with: 4 warpgroups of 128)
+    if constexpr (MX && DIVIDED) asm volatile("setmaxnreg.inc.sync.aligned.u32 184;");
+    else if constexpr (MX) asm volatile("setmaxnreg.inc.sync.aligned.u32 192;");
     else asm volatile("setmaxnreg.inc.sync.aligned.u32 216;");
     const int t = warp >> 2, row = tid & 127;
     const uint32_t lanes = (uint32_t)(warp & 3) << 21;
@@ -358,11 +408,11 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           for (int k = 0; k < 8; ++k) bigs[k] = max3(bigs[k], x[i + k], x[i + k + 8]);
         if (h == 0) {
 #pragma unroll
-          for (int k = 0; k < 8; ++k) bigs[k] = fmaxf(bigs[k], x[56 + k]);
+          for (int k = 0; k < 8; ++k) bigs[k] = max3(bigs[k], x[56 + k], x[56 + k]);
         }
       }
-      float big = fmaxf(max3(max3(bigs[0], bigs[1], bigs[2]), bigs[3], bigs[4]), max3(bigs[5], bigs[6], bigs[7]));
-      const bool up = (big - m) * c > 8.f || (m == -INFINITY && big > -INFINITY);
+      const float big = max3(max3(bigs[0], bigs[1], bigs[2]), max3(bigs[3], bigs[4], bigs[5]), max3(bigs[6], bigs[7], bigs[7]));
+      const bool up = !((big - m) * c <= 8.f) && big != -INFINITY;     // (from nothing, and for NaN, too)
       if (__any_sync(0xFFFFFFFFu, up)) {
         const float f = up ? exp2_fast((m - big) * c) : 1.f;
         if (up) m = big;
@@ -383,7 +433,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           }
         }
       }
-      const float base = m == -INFINITY ? 0.f : -m * c;
+      // a maximum that is infinite or NaN makes all weights NaN; the polynomial alone would hide it
+      const float base = m == -INFINITY ? 0.f : fmaf(-m, c, m - m);
       const F2 base2 = f2(base, base);
       // the weights, and word to the issuer, which may begin with the first half; POLY: every POLY-th pair by the polynomial
       auto weights = [&](auto every) {
@@ -426,12 +477,31 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     if (ok && n > 0) {
       ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.o_done[t]), (n - 1) & 1, &ws)) != 0;
       tc::tc_fence_after();
-      float l[4];
-      unf2(la, l[0], l[1]);
-      unf2(lb, l[2], l[3]);
-      const float all = (l[0] + l[1]) + (l[2] + l[3]), inv = all == 0.f ? 0.f : 1.f / all;
+    }
+    float l[4];
+    unf2(la, l[0], l[1]);
+    unf2(lb, l[2], l[3]);
+    const float all = (l[0] + l[1]) + (l[2] + l[3]);
+    if (DIVIDED && parts > 1) {
+      // a part's sums as they are; where it saw nothing, only that it did not
+      float* const part = s.parts + (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2) + (size_t)(t * kRows + row) * D;
+      float* const marks = s.parts + (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + t * kRows + row;
+      if (ok && left > 0) {
+        marks[0] = n > 0 && m != -INFINITY ? m * c : -INFINITY;
+        marks[2 * kRows] = all;
+      }
+#pragma unroll 1
+      for (int k = 0; k < D / 32 && ok && n > 0; ++k) {
+        uint32_t o[32];
+        tc::tmem_ld32(o_at + 32 * k, o);
+        tc::tmem_ld_wait();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) store32(part + 32 * k + 8 * i, true, o + 8 * i);
+      }
+    } else if (ok && n > 0) {
+      const float inv = all == 0.f ? 0.f : 1.f / all;
       const size_t at = ((size_t)(it.row0 + token) * p.hq + it.head * p.group + head) * D;
-      const bool mine = row < left && ok && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
+      const bool mine = row < left && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
 #pragma unroll
       for (int k = 0; k < D / 32; ++k) {
         uint32_t o[32], w[16];
@@ -472,7 +542,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       }
     } else {
       // ---- mantissas, as they lie in the cache, into swizzled bf16 values; a lane a block of 16, its row's other blocks beside it
-      asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
+      if constexpr (DIVIDED) asm volatile("setmaxnreg.dec.sync.aligned.u32 88;");
+      else asm volatile("setmaxnreg.dec.sync.aligned.u32 96;");
       constexpr int B = SH::BLOCKS, N = B, STEP = 128 / B;         // a thread's blocks of a tile, and the rows between them
       const int k = tid - 256, b = k % B, r0 = k / B, shift = p.bits - 2;
       const uint8_t* const raw_mem = ring_mem + SH::STAGES * SH::TILE;
@@ -515,7 +586,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       }
     }
   } else if (warp == SH::ISSUER) {
-    if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if constexpr (MX && DIVIDED) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    else if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     // The whole warp walks along, so that addresses stay in uniform registers; one lane issues.
     const bool leader = tc::elect_one();
@@ -577,7 +649,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       if (++at == SH::STAGES) { at = 0; phase ^= 1; }
     }
   } else {
-    if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
+    if constexpr (MX && DIVIDED) asm volatile("setmaxnreg.dec.sync.aligned.u32 56;");
+    else if constexpr (MX) asm volatile("setmaxnreg.dec.sync.aligned.u32 32;");
     else asm volatile("setmaxnreg.dec.sync.aligned.u32 72;");
     if (warp == SH::RAW_WARP) {
       // ---- copies of an MXINT8 cache: a lane a page
@@ -627,6 +700,47 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   }
 }
 
+// Joins the parts of the items that were divided, in the order of the keys: blockIdx.x is an item, blockIdx.y 32 of its rows, a thread four columns.
+template <int D>
+__global__ void __launch_bounds__(256) join_tiles_kernel(const Tiles s) {
+  tc::pdl_launch_dependents();
+  tc::pdl_wait();
+  const Attention& p = s.a;
+  if ((int)blockIdx.x >= s.divided[0].request) return;
+  const Divided q = s.divided[1 + blockIdx.x];
+  if (q.parts < 2) return;
+  // places of the parts go by how many the items were to have
+  const int planned = min(s.sms / s.divided[0].request, kMostParts);
+  const float* const first = s.parts + (size_t)blockIdx.x * planned * 2 * kRows * (D + 2);
+  for (int i = threadIdx.x; i < 32 * D / 4; i += 256) {
+    const int row = blockIdx.y * 32 + i / (D / 4), d = 4 * (i % (D / 4));
+    if (row >= q.rows - q.base) return;
+    float m[kMostParts], big = -INFINITY, all = 0.f;
+#pragma unroll
+    for (int k = 0; k < kMostParts; ++k) {
+      m[k] = k < q.parts ? first[(size_t)k * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + row] : -INFINITY;
+      big = fmaxf(big, m[k]);
+    }
+    const float base = big == -INFINITY ? 0.f : big;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int k = 0; k < kMostParts; ++k) {
+      const float l = k >= q.parts ? 0.f : first[(size_t)k * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + 2 * kRows + row];
+      if (l == 0.f) continue;                                      // (nothing is there, or nothing of weight)
+      const float* const part = first + (size_t)k * 2 * kRows * (D + 2);
+      const float f = exp2_fast(m[k] - base);
+      const float4 x = *reinterpret_cast<const float4*>(part + (size_t)row * D + d);
+      sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
+      all += f * l;
+    }
+    const float inv = all == 0.f ? 0.f : 1.f / all;
+    const uint32_t z = (uint32_t)(row + q.head0), token = p.group == 1 ? z : __umulhi(z, s.group_inv), head = z - token * p.group;
+    const size_t at = ((size_t)(q.row0 + q.token0 + token) * p.hq + q.head * p.group + head) * D + d;
+    if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 64))
+      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
+  }
+}
+
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
                                   const cuuint32_t*, CUtensorMapInterleave, CUtensorMapSwizzle, CUtensorMapL2promotion, CUtensorMapFloatOOBfill);
 static EncodeTiledFn encode_fn() {
@@ -651,19 +765,41 @@ static bool page_map(CUtensorMap* map, const void* base, const lqer_kv_cache_t& 
             CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
 
-template <int D, bool MX>
+template <int D, bool MX, bool DIVIDED>
 static cudaError_t launch_shape(const Tiles& k, int ctas, const lqer_kv_cache_t& c, cudaStream_t s) {
   using SH = Shape<D, MX>;
   static OncePerDevice once;
-  cudaError_t e = once.run([] { return cudaFuncSetAttribute(tiles_kernel<D, MX>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::SMEM); });
+  cudaError_t e = once.run([] { return cudaFuncSetAttribute(tiles_kernel<D, MX, DIVIDED>, cudaFuncAttributeMaxDynamicSharedMemorySize, SH::SMEM); });
   if (e != cudaSuccess) return e;
   CUtensorMap maps[2] = {};
   if (!MX && (!page_map(&maps[0], c.keys, c) || !page_map(&maps[1], c.values, c))) return cudaErrorInvalidValue;
-  LaunchScope scope(kFamDecode, s);
-  return launch_after(tiles_kernel<D, MX>, dim3(ctas), SH::THREADS, SH::SMEM, s, k, maps[0], maps[1]);
+  LaunchScope scope(kFamDecode, s, DIVIDED ? 2 : 1);
+  e = launch_after(tiles_kernel<D, MX, DIVIDED>, dim3(ctas), SH::THREADS, SH::SMEM, s, k, maps[0], maps[1]);
+  if (e != cudaSuccess || !DIVIDED) return e;
+  return launch_after(join_tiles_kernel<D>, dim3(k.sms / 2, 2 * kRows / 32), 256, 0, s, k);
 }
-cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, cudaStream_t s) {
+// Whether items may be divided: a division costs a launch and the way of the parts through memory, some 8 us, and gains what the last turn of CTAs leaves of it, if the
+// rows are where they can be, and the keys as many (some 1.8 us for 128).
+static bool may_divide(const Attention& a) {
+  const int sms = sm_count();
+  if (sms < 2) return false;
+  const long long rows = (long long)a.M * a.group, items = (rows + 2 * kRows - 1) / (2 * kRows) * a.hkv, left = items % sms;
+  if (left == 0 || left > sms / 2) return false;
+  const long long room = (long long)a.max_pages * a.page, keys = a.window > 0 && a.window + 2 * kRows < room ? a.window + 2 * kRows : room;
+  const double turn = 1.8 * (double)((keys + kKeys - 1) / kKeys), parts = (double)(sms / left < kMostParts ? sms / left : kMostParts);
+  return turn * (1.0 - 1.0 / parts) > 10.0;
+}
+static size_t divided_bytes() { return ((size_t)(1 + sm_count() / 2) * sizeof(Divided) + 255) & ~(size_t)255; }
+size_t tiles_scratch_bytes(const Attention& a, int head_dim) {
+  return may_divide(a) ? divided_bytes() + (size_t)sm_count() * 2 * kRows * (head_dim + 2) * sizeof(float) : 0;
+}
+cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, void* scratch, cudaStream_t s) {
   Tiles k = {};
+  if (may_divide(a)) {
+    k.sms = sm_count();
+    k.divided = static_cast<Divided*>(scratch);
+    k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + divided_bytes());
+  }
   k.a = a;
   k.few = few;
   k.negate = a.scale_log2 < 0.f;
@@ -678,10 +814,15 @@ cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqe
   // no more items than this: whole ones, and one that is not for every request that has enough rows to be taken
   const long long rows = (long long)a.M * a.group, most = rows / (few + 1);
   const long long items = rows / (2 * kRows) + (most < a.R ? most : a.R);
-  if (items * a.hkv > 0x7FFFFFFF) return cudaErrorInvalidValue;
-  const int ctas = (int)(items * a.hkv);
-  if (c.dtype == LQER_MXINT8) return c.head_dim == 128 ? launch_shape<128, true>(k, ctas, c, s) : launch_shape<64, true>(k, ctas, c, s);
-  return c.head_dim == 128 ? launch_shape<128, false>(k, ctas, c, s) : launch_shape<64, false>(k, ctas, c, s);
+  if (items * a.hkv + k.sms > 0x7FFFFFFF) return cudaErrorInvalidValue;
+  const int ctas = (int)(items * a.hkv) + k.sms;                  // (parts are never more than the SMs)
+  auto launch = [&](auto dim, auto mx) {
+    constexpr int D = decltype(dim)::value;
+    constexpr bool MX = decltype(mx)::value != 0;
+    return k.sms > 0 ? launch_shape<D, MX, true>(k, ctas, c, s) : launch_shape<D, MX, false>(k, ctas, c, s);
+  };
+  if (c.dtype == LQER_MXINT8) return c.head_dim == 128 ? launch(Every<128>{}, Every<1>{}) : launch(Every<64>{}, Every<1>{});
+  return c.head_dim == 128 ? launch(Every<128>{}, Every<0>{}) : launch(Every<64>{}, Every<0>{});
 }
 
 }  // namespace kv

@@ -40,7 +40,7 @@ struct Attention {
   int hq, hkv, group;
   int window, sinks;           // window 0: none
   float scale_log2;            // of the scores, times log2(e)
-  int bits, emin, emax;        // format of an MXINT8 cache
+  int bits;                    // of the mantissas of an MXINT8 cache
 };
 __device__ __forceinline__ const StepRequest* requests_of(const StepHead* h) {
   return reinterpret_cast<const StepRequest*>(reinterpret_cast<const uint8_t*>(h) + kStepHeadBytes);
@@ -73,7 +73,7 @@ __device__ __forceinline__ uint32_t mantissas_bf16x2(uint32_t b, const MantissaS
   asm("fma.rn.bf16x2 %0, %1, %2, %3;" : "=r"(z) : "r"(t), "r"(0xBF00BF00u), "r"(z));
   return z;
 }
-// The scale 2^(e - (bits - 2)) of two blocks from their exponent bytes (in the low bytes of the halves of `e`; within the format's window), shift = bits - 2.
+// The scale 2^(e - (bits - 2)) of two blocks from their exponent bytes (in the low bytes of the halves of `e`; within the format's window), or of one; shift = bits - 2.
 __device__ __forceinline__ MantissaScale mantissa_scales(uint32_t e, int shift) {
   return {e * 128u - (uint32_t)shift * 0x00800080u, e * 128u + (0x80008000u + (uint32_t)(8 - shift) * 0x00800080u)};
 }
@@ -99,7 +99,8 @@ __device__ __forceinline__ float exp2_fast(float x) {
 }
 
 // Requests of more than `few` rows (tokens times heads that share a key head) on tcgen05 (lqer_attention_tiles.cu).
-cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, cudaStream_t s);
+cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, void* scratch, cudaStream_t s);
+size_t tiles_scratch_bytes(const Attention& a, int head_dim);
 
 // Launches with the programmatic attribute: the kernels wait for their predecessor before they touch memory.
 template <class... P, class... A>

@@ -633,7 +633,7 @@ cudaError_t launch_adapters(const void* X, int x_type, int M, const void* pool, 
                             const void* Y0, int y0_type, void* Y, int y_type, int bits, int emin, int emax, void* scratch, cudaStream_t s);
 size_t adapter_scratch_bytes(int M, int plan_slots, int K, int N, int max_rank);
 
-// Keys and values of past tokens (lqer_cache.cu) and the attention over them (lqer_attention.cu).
+// Keys and values of past tokens (lqer_cache.cu) and the attention over them (lqer_attention.cu, lqer_attention_tiles.cu).
 constexpr int kKvMaxHeads = 1024, kKvMaxRequests = 16384;
 size_t cache_step_bytes(int R);
 cudaError_t launch_cache_step(const lqer_page_table_t& t, const int* lengths, const int* added, const long long* ring, int M, int max_added,
@@ -642,8 +642,7 @@ cudaError_t launch_append_kv(const void* K, const void* V, int x_type, size_t k_
                              const lqer_kv_cache_t& c, int bits, int emin, int emax, cudaStream_t s);
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added);
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
-                                   int max_added, int window, int sinks, double scale, int bits, int emin, int emax, void* Y, void* scratch,
-                                   cudaStream_t s);
+                                   int max_added, int window, int sinks, double scale, int bits, void* Y, void* scratch, cudaStream_t s);
 
 // Argument checks shared by the entry points (lqer_api.cu).
 lqer_status_t check_config(const lqer_config_t* cfg);

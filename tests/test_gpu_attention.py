@@ -4,7 +4,7 @@ import pytest
 import torch
 
 import paper_2402_02446_b200 as L
-from cache_model import Batch
+from cache_model import Batch, attention64, tolerance
 from paper_2402_02446_b200 import binding
 
 pytestmark = pytest.mark.gpu
@@ -61,6 +61,16 @@ def test_other_scales(scale, ratio_log):
 def test_a_long_request_beside_many_short_ones(ratio_log):
     _run(Batch([(30000, 1)] + [(3 * i % 40, 1) for i in range(300)], 8, 2, 128, 16), log=ratio_log)
     _run(Batch([(9000, 400), (12, 1), (0, 33)], 4, 2, 128, 64, max_added=400), log=ratio_log)
+
+
+@pytest.mark.parametrize("dtype", [BF16, L.MXINT8])
+@pytest.mark.parametrize("window,sinks", [(0, 0), (1500, 300)])
+@pytest.mark.parametrize("requests,hq,hkv,D", [([(6000, 500), (0, 300), (9, 1)], 4, 2, 128), ([(3000, 1300)], 32, 8, 64), ([(2500, 700), (100, 620)], 20, 4, 128)])
+def test_items_that_are_divided_over_their_keys(requests, hq, hkv, D, window, sinks, dtype, ratio_log):
+    b = Batch(requests, hq, hkv, D, 32, dtype, pad=2)
+    Y = _run(b, window, sinks, log=ratio_log)
+    for _ in range(3):
+        assert torch.equal(L.paged_attention(b.Q, b.cache, b.pages, b.step, window=window, sinks=sinks, Y=Y.clone()), Y)
 
 
 @pytest.mark.parametrize("dtype", [BF16, L.MXINT8])
@@ -204,3 +214,27 @@ def test_results_are_the_same_every_time():
             assert torch.equal(L.paged_attention(b.Q, b.cache, b.pages, b.step, window=700, sinks=2), first)
     # a window that hides nothing is none
     assert torch.equal(L.paged_attention(b.Q, b.cache, b.pages, b.step, window=2 ** 31 - 1, sinks=2 ** 31 - 1), L.paged_attention(b.Q, b.cache, b.pages, b.step))
+
+
+@pytest.mark.parametrize("bad", [float("nan"), float("inf")])
+@pytest.mark.parametrize("requests", [[(700, 1)], [(5000, 3)], [(300, 130)], [(1500, 140)]])
+@pytest.mark.parametrize("D", [64, 128])
+def test_scores_that_are_no_numbers_reach_the_rows_that_see_them(D, requests, bad):
+    # in every column of a tile once: 16 heads times 8 tokens
+    b = Batch(requests, 16, 16, D, 16)
+    (before, n), = requests
+    ids = b.pages.tables[0, :(before + n + 15) // 16].long()
+    for k in range(8):
+        keys = b.cache.keys.clone()
+        for h in range(16):
+            token = 16 * k + h
+            b.cache.keys[ids[token // 16], h, token % 16, 0] = bad
+        Y = L.paged_attention(b.Q, b.cache, b.pages, b.step).double()
+        K, V = (x.double()[ids].transpose(0, 1).flatten(1, 2)[:, :before + n] for x in (b.cache.keys, b.cache.values))
+        y = attention64(b.Q.double(), K, V, n, 0, 0, D ** -0.5)[0]
+        assert torch.equal(torch.isnan(Y), torch.isnan(y)) and bool(torch.isnan(y).any())
+        # an infinite score that is negative weighs nothing
+        _, weighed, most = attention64(b.Q.double(), K.nan_to_num(0.0, 0.0, 0.0), V, n, 0, 0, D ** -0.5)
+        good = ~torch.isnan(y)
+        assert bool(((Y - y).abs() <= tolerance(y, weighed, most, D, before + n))[good].all())
+        b.cache.keys.copy_(keys)

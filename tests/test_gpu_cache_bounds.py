@@ -30,9 +30,9 @@ def test_a_short_extent_is_reported_and_nothing_beyond_it_is_written():
         from paper_2402_02446_b200 import binding
         assert binding.DEBUG_BOUNDS and L.lib_path().endswith("liblqer_dbg.so")
         E = binding.STATUS_NAMES.index
-        # a row by one CTA, a row by several, a warp a row, tiles of rows (bf16 and MXINT8)
+        # a row by one CTA, a row by several, a warp a row, tiles of rows (bf16 and MXINT8), tiles divided over their keys
         for requests, dtype in (([(20, 1), (30, 1)], torch.bfloat16), ([(20, 1), (3000, 1)], torch.bfloat16), ([(9, 1)] * 1400, torch.bfloat16),
-                                ([(20, 200), (30, 250)], torch.bfloat16), ([(20, 200), (30, 250)], L.MXINT8)):
+                                ([(20, 200), (30, 250)], torch.bfloat16), ([(20, 200), (30, 250)], L.MXINT8), ([(20, 40), (4000, 600)], torch.bfloat16)):
             b = Batch(requests, 16, 8, 64, 16, dtype)
             good = L.paged_attention(b.Q, b.cache, b.pages, b.step)
             assert L.poll_status(b.step.buf) == 0
