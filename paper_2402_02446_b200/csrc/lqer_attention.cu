@@ -27,14 +27,15 @@ namespace kv {
 
 constexpr int kChunk = 64, kWarps = 4, kSplitThreads = 32 * kWarps;
 // Requests of up to this many rows of a key head (tokens times heads that share it) are taken here, of more by lqer_attention_tiles.cu.  There a tile of
-// keys costs what it costs for 256 rows, and where few requests leave SMs without work a request's keys are divided among them, for some 8 us; here
-// the time is shared by all SMs from the start, but grows with the rows, 16 at a time (some 12 ns a key and head, over the SMs).  Both sides measured, here /
-// there, 32/8 heads, us: one request, 64 rows behind 1000: 12 / 19, behind 4000: 19 / 27, behind 16000: 43 / 37; 128 rows: 14 / 19, 28 / 28, 69 / 40;
-// two, 64 rows: 16 / 22, 24 / 31, 54 / 51; 128 rows: 18 / 24, 34 / 32, 87 / 52; 8, 80 rows behind 2000: 36 / 36; 64, 32 rows: 418 / 318, 80: 200 / 106.
-constexpr int kLeast = 16, kMost = 96;
+// keys costs what it costs for 256 rows, and where few requests leave SMs without work a request's keys are divided among them, for some 5 us; here
+// the time is shared by all SMs from the start, but grows with the rows, 16 at a time (some 12 ns a key and head, over the SMs).  So long tables, which
+// are what the host knows of the lengths, leave less to it.  Both sides measured, here / there, 32/8 heads, us: one request, 64 rows behind 1000: 12 / 16,
+// behind 4000: 19 / 17, behind 16000: 44 / 27 (MXINT8 56 / 30); two, 64 rows: 16 / 20, 24 / 24, 54 / 44; four, 32 rows: 16 / 21, 24 / 31, 59 / 74, 64 rows:
+// 18 / 21, 31 / 31, 81 / 75; 8, 80 rows behind 2000: 36 / 36; 64, 32 rows: 418 / 318, 80: 200 / 106.
+constexpr int kLeast = 16;
 inline int few_rows(const Attention& p) {
-  const long long heads = (long long)(p.R < p.M ? p.R : p.M) * p.hkv, few = 2900 / heads;
-  return few < kLeast ? kLeast : few > kMost ? kMost : (int)few;
+  const long long heads = (long long)(p.R < p.M ? p.R : p.M) * p.hkv, few = 2900 / heads, most = (long long)p.max_pages * p.page > 4096 ? 48 : 96;
+  return few < kLeast ? kLeast : (int)(few < most ? few : most);
 }
 constexpr int kMinChunks = 2;                // of a CTA's run
 

@@ -23,7 +23,7 @@
 //
 // Where the items of 256 rows leave a last turn of CTAs half empty or more (few requests, short pieces of long prompts), that turn's items are divided over
 // their keys, up to 16 CTAs to one, and a second kernel joins the parts.  Whole / divided, us: 2048 tokens behind 10240, 40/8 heads (320 items) 480 / 412, MXINT8
-// 542 / 487; 512 behind 15488, 32/8 heads 222 / 135; 300 of 4000, two requests 69 / 53.  It is a kernel of its own: what it needs beside costs registers
+// 542 / 487; 512 behind 15488, 32/8 heads 221 / 137; 300 of 4000, two requests 69 / 54.  It is a kernel of its own: what it needs beside costs registers
 // that those without it miss (8192 tokens 455 -> 490 us, MXINT8 520 -> 610).
 #include "lqer_cache.cuh"
 
@@ -141,7 +141,7 @@ constexpr int kPolyEvery = 4;
 // part `part` of `parts`, the `slot`-th item that is divided at all.
 struct Item { int request, head, row0, n, len, base, rows, token0, head0, slot, part, parts; };      // rows: n * group
 struct Divided { int request, head, row0, rows, token0, head0, base, parts; };
-constexpr int kMostParts = 16;
+constexpr int kMostParts = 16, kAtOnce = 8;
 // Row z of an item: its token, and its head within the group.
 __device__ __forceinline__ void row_of(const Tiles& s, const Item& it, int z, int& token, int& head) {
   const uint32_t x = (uint32_t)(z + it.head0), q = s.a.group == 1 ? x : __umulhi(x, s.group_inv);
@@ -700,9 +700,10 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   }
 }
 
-// Joins the parts of the items that were divided, in the order of the keys: blockIdx.x is an item, blockIdx.y 32 of its rows, a thread four columns.
+// Joins the parts of the items that were divided, in the order of the keys: blockIdx.x is an item, blockIdx.y 1024 / D of its rows, a thread four columns of one.
+// (32 rows to a CTA, and the parts one behind the other, made 64 rows behind 4000 31 us instead of 23; all 16 at once 512 behind 15488 141 instead of 137.)
 template <int D>
-__global__ void __launch_bounds__(256) join_tiles_kernel(const Tiles s) {
+__global__ void __launch_bounds__(256, 4) join_tiles_kernel(const Tiles s) {
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   const Attention& p = s.a;
@@ -712,33 +713,44 @@ __global__ void __launch_bounds__(256) join_tiles_kernel(const Tiles s) {
   // places of the parts go by how many the items were to have
   const int planned = min(s.sms / s.divided[0].request, kMostParts);
   const float* const first = s.parts + (size_t)blockIdx.x * planned * 2 * kRows * (D + 2);
-  for (int i = threadIdx.x; i < 32 * D / 4; i += 256) {
-    const int row = blockIdx.y * 32 + i / (D / 4), d = 4 * (i % (D / 4));
-    if (row >= q.rows - q.base) return;
-    float m[kMostParts], big = -INFINITY, all = 0.f;
+  const int row = blockIdx.y * (1024 / D) + threadIdx.x / (D / 4), d = 4 * (threadIdx.x % (D / 4));
+  if (row >= q.rows - q.base) return;
+  float big = -INFINITY, all = 0.f;
+  float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int at = 0; at < q.parts; at += kAtOnce) {                  // what so many parts say is all asked for before any of it is used
+    float m[kAtOnce], l[kAtOnce];
+    float4 x[kAtOnce];
 #pragma unroll
-    for (int k = 0; k < kMostParts; ++k) {
-      m[k] = k < q.parts ? first[(size_t)k * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + row] : -INFINITY;
-      big = fmaxf(big, m[k]);
+    for (int k = 0; k < kAtOnce; ++k) {
+      const float* const part = first + (size_t)(at + k) * 2 * kRows * (D + 2);
+      m[k] = -INFINITY;
+      l[k] = 0.f;
+      if (at + k < q.parts) {
+        m[k] = part[(size_t)2 * kRows * D + row];
+        l[k] = part[(size_t)2 * kRows * D + 2 * kRows + row];
+        x[k] = *reinterpret_cast<const float4*>(part + (size_t)row * D + d);
+      }
     }
-    const float base = big == -INFINITY ? 0.f : big;
-    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+    float top = big;
 #pragma unroll
-    for (int k = 0; k < kMostParts; ++k) {
-      const float l = k >= q.parts ? 0.f : first[(size_t)k * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + 2 * kRows + row];
-      if (l == 0.f) continue;                                      // (nothing is there, or nothing of weight)
-      const float* const part = first + (size_t)k * 2 * kRows * (D + 2);
+    for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, m[k]);
+    const float base = top == -INFINITY ? 0.f : top, f0 = exp2_fast(big - base);
+    sum.x *= f0; sum.y *= f0; sum.z *= f0; sum.w *= f0;
+    all *= f0;
+    big = top;
+#pragma unroll
+    for (int k = 0; k < kAtOnce; ++k) {
+      if (l[k] == 0.f) continue;                                   // nothing was put there, or nothing of weight
       const float f = exp2_fast(m[k] - base);
-      const float4 x = *reinterpret_cast<const float4*>(part + (size_t)row * D + d);
-      sum.x += f * x.x; sum.y += f * x.y; sum.z += f * x.z; sum.w += f * x.w;
-      all += f * l;
+      sum.x += f * x[k].x; sum.y += f * x[k].y; sum.z += f * x[k].z; sum.w += f * x[k].w;
+      all += f * l[k];
     }
-    const float inv = all == 0.f ? 0.f : 1.f / all;
-    const uint32_t z = (uint32_t)(row + q.head0), token = p.group == 1 ? z : __umulhi(z, s.group_inv), head = z - token * p.group;
-    const size_t at = ((size_t)(q.row0 + q.token0 + token) * p.hq + q.head * p.group + head) * D + d;
-    if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 64))
-      *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
   }
+  const float inv = all == 0.f ? 0.f : 1.f / all;
+  const uint32_t z = (uint32_t)(row + q.head0), token = p.group == 1 ? z : __umulhi(z, s.group_inv), head = z - token * p.group;
+  const size_t at = ((size_t)(q.row0 + q.token0 + token) * p.hq + q.head * p.group + head) * D + d;
+  if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 64))
+    *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
 }
 
 typedef CUresult (*EncodeTiledFn)(CUtensorMap*, CUtensorMapDataType, cuuint32_t, void*, const cuuint64_t*, const cuuint64_t*, const cuuint32_t*,
@@ -776,10 +788,11 @@ static cudaError_t launch_shape(const Tiles& k, int ctas, const lqer_kv_cache_t&
   LaunchScope scope(kFamDecode, s, DIVIDED ? 2 : 1);
   e = launch_after(tiles_kernel<D, MX, DIVIDED>, dim3(ctas), SH::THREADS, SH::SMEM, s, k, maps[0], maps[1]);
   if (e != cudaSuccess || !DIVIDED) return e;
-  return launch_after(join_tiles_kernel<D>, dim3(k.sms / 2, 2 * kRows / 32), 256, 0, s, k);
+  return launch_after(join_tiles_kernel<D>, dim3(k.sms / 2, 2 * kRows * D / 1024), 256, 0, s, k);
 }
-// Whether items may be divided: a division costs a launch and the way of the parts through memory, some 8 us, and gains what the last turn of CTAs leaves of it, if the
-// rows are where they can be, and the keys as many (some 1.8 us for 128).
+// Whether items may be divided: a division costs a launch and the way of the parts through memory, some 5 us, and gains what the last turn of CTAs leaves of it, if the
+// rows are where they can be, and the keys as many (some 1.8 us for 128).  Not divided / divided, us: 300 tokens, 32/8 heads: 15 / 20, of 600: 19 / 25, of 1300 32 / 27,
+// of 16000, 512 tokens: 221 / 137.
 static bool may_divide(const Attention& a) {
   const int sms = sm_count();
   if (sms < 2) return false;
