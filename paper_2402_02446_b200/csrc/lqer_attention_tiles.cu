@@ -253,7 +253,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   const uint32_t q_at = (tc::smem_u32(dynamic) + 1023u) & ~1023u, ring_at = q_at + 2 * SH::TILE, raw_at = ring_at + SH::STAGES * SH::TILE;
   uint8_t* const q_mem = dynamic + (q_at - tc::smem_u32(dynamic));
   uint8_t* const ring_mem = q_mem + 2 * SH::TILE;
-  tc::pdl_launch_dependents();
   if (tid == 0) {
     for (int i = 0; i < SH::STAGES; ++i) {
       tc::mbar_init(bar_of(bars.full[i]), SH::COPY_WARPS);
@@ -303,6 +302,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   tc::tc_fence_before();
   __syncthreads();
   tc::tc_fence_after();
+  tc::pdl_launch_dependents();         // not before: a CTA of the next kernel could take tensor memory on this SM first, and then wait for this kernel to end
   const uint32_t tmem = tmem_at;
   const int* table = p.tables + (size_t)it.request * p.max_pages;
   // keys that no row of the step sees: from the end on, and between the first tokens and the window

@@ -1,5 +1,6 @@
 """Attention over the paged cache against 64-bit arithmetic (the bound is derived in cache_model.tolerance), through tables and cache as a serving
 program keeps them.  The cache holds NaN (bf16) or the largest numbers (MXINT8) wherever no token is."""
+import numpy as np
 import pytest
 import torch
 
@@ -155,6 +156,31 @@ def test_generations_as_a_program_runs_them():
     free = [pages.free[i % 30].item() for i in range(ring[0], ring[1])]
     mine = [p for r in range(R) for p in pages.tables[r, :(pages.lengths[r] + page - 1) // page].tolist()]
     assert sorted(free + mine) == list(range(30))
+
+
+@pytest.mark.parametrize("requests", [[(0, 130)], [(900, 100)], [(40, 1000), (3, 60)], [(300, 24)]])
+@pytest.mark.parametrize("dtype", [BF16, L.MXINT8])
+def test_the_output_projection_right_behind(dtype, requests):
+    # the layer's kernels start while the attention's are still running, and use tensor memory of their own
+    import lqer_inputs as gen
+    spec = gen.LayerSpec("output", M=8, K=512, N=264, k=16, calib_rows=32, outlier_frac=0.01, outlier_scale=20.0, seed=78)
+    A, B = gen.make_random_factors(spec)
+    P = L.prepare_weights(*(torch.from_numpy(np.ascontiguousarray(v)).to(DEV) for v in (gen.make_weight(spec), A, B)))
+    b = Batch(requests, 8, 8, 64, 16, dtype)
+    ws = L.new_workspace(b.M, P)
+    room = torch.empty(L.attention_workspace_bytes(b.M, 8, b.cache, b.pages, b.step.max_added), dtype=torch.uint8, device=DEV)
+    Y = torch.empty((b.M, 8, 64), dtype=BF16, device=DEV)
+    many = []
+    for _ in range(20):
+        L.paged_attention(b.Q, b.cache, b.pages, b.step, Y=Y, ws=room)
+        many.append(L.linear_ex(Y.view(b.M, 512), P, ws))
+    torch.cuda.synchronize()
+    b.check(Y)
+    want = L.linear_ex(Y.view(b.M, 512), P, ws)
+    torch.cuda.synchronize()
+    assert L.poll_status(b.step.buf) == 0 and L.poll_status(ws) == 0
+    assert all(torch.equal(x, want) for x in many)
+    P.release()
 
 
 def test_plans_that_do_not_fit_write_nothing():
