@@ -108,7 +108,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   }
   scan(given, sums32, total);
   const int all_given = total;
-  const bool ring_ok = head >= 0 && tail >= head && tail - head + all_given <= p.n_pages;
+  const bool ring_ok = head >= 0 && tail >= head && tail < (1LL << 62) && tail - head + all_given <= p.n_pages;     // (so that no sum overflows)
   if (!ring_ok && tid == 0) fail(LQER_ERR_BOUNDS);
   if (ring_ok && all_given > 0) {
     int before = 0;

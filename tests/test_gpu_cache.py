@@ -92,6 +92,18 @@ def test_a_ring_that_cannot_be_refuses_what_moves_pages(ring):
     _compare(model, pages, L.cache_step(pages, _int(added), 30), model.step(added, 30, 30))
 
 
+@pytest.mark.parametrize("tail", [2 ** 63 - 1, 2 ** 62])
+def test_a_ring_at_the_end_of_its_type_is_one_that_cannot_be(tail):
+    pages = L.new_page_table(2, 4, 8, 16, device=DEV)
+    pages.lengths.copy_(_int([20, 20]))
+    pages.ring.copy_(_int([tail - 4, tail], torch.int64))
+    tables, free = pages.tables.clone(), pages.free.clone()
+    step = L.cache_step(pages, _int([-20, 20]), 20)
+    assert L.poll_status(step.buf) == E("LQER_ERR_BOUNDS")
+    assert step.lengths.tolist() == [20, 20] and step.ring.tolist() == [tail - 4, tail]
+    assert torch.equal(pages.tables, tables) and torch.equal(pages.free, free)
+
+
 def test_entries_that_are_no_page_and_lengths_that_cannot_be():
     pages = L.new_page_table(3, 4, 8, 16, device=DEV)
     pages.lengths.copy_(_int([5, -1, 65]))
