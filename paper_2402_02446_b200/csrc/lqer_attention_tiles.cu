@@ -13,17 +13,18 @@
 //   issuer           one lane: per key tile and row tile, O += P V of the last key tile, in two halves as the weights come, then S of the next.
 // Keys and values share a ring of tiles.  Every wait is bounded.
 //
-// Measured, 32/8 heads of 128, GPU time: a prompt of 8192 tokens 455 us (1.21 PFLOP/s of what a causal row sees, 0.72 of a long GEMM's burst rate; 545 us when
-// it runs without a pause and the power cap lowers the clock), from MXINT8 520, heads of 64 410; windows of 1024, 32/32 heads, MXINT8, 7682 tokens 218.  A key
-// tile takes a CTA 3300 clocks: 16 MMAs for each row tile at some 85 clocks (64 by the rate; S reads both operands from shared memory, 128 bytes a
-// clock), 2100 from S to the last weights, and the issuer's way between.  What a CTA does before its first and behind its last key tile takes
-// about five more.  Tried, and not faster under a full load: CTAs that stay and take items by turns, with the next queries under way (460 -> 470 us);
-// weights by the old maximum with the new one beside them, which takes 800 of the 2100 clocks away but not the total; two threads a row; an issuer for
-// each row tile (574); short loops over 32 columns (480 to 515).
+// Measured, 32/8 heads of 128, GPU time: a prompt of 8192 tokens 456 us (1.2 PFLOP/s of what a causal row sees, 0.72 of a long GEMM's burst rate; 545 us when
+// it runs without a pause and the power cap lowers the clock), from MXINT8 514, heads of 64 392; windows of 1024, 32/32 heads, MXINT8, 7682 tokens 210.  A key
+// tile takes a CTA 3100 clocks: 16 MMAs for each row tile at some 85 clocks (64 by the rate; S reads both operands from shared memory, 128 bytes a
+// clock), 2100 from S to the last weights, and the issuer's way between.  Beside its key tiles an item takes 16000: 3500 until it is known, 5000 for the queries
+// (where all CTAs ask for theirs at once; 1900 by itself), 2200 until the first scores, 2500 for the results, 1300 until the next CTA, and at the end
+// the second row tile is alone with its last key tile.  Tried, and not faster under a full load: CTAs that stay and take items by turns, with the next
+// queries under way (460 -> 470 us); the next item's queries into L2 ahead; the first keys ahead of all others; weights by the old maximum with the new one beside
+// them, which takes 800 of the 2100 clocks away but not the total; two threads a row; an issuer for each row tile (574); short loops over 32 columns (480 to 515).
 //
 // Where the items of 256 rows leave a last turn of CTAs half empty or more (few requests, short pieces of long prompts), that turn's items are divided over
-// their keys, up to 16 CTAs to one, and a second kernel joins the parts.  Whole / divided, us: 2048 tokens behind 10240, 40/8 heads (320 items) 480 / 412, MXINT8
-// 542 / 487; 512 behind 15488, 32/8 heads 221 / 137; 300 of 4000, two requests 69 / 54.  It is a kernel of its own: what it needs beside costs registers
+// their keys, up to 16 CTAs to one, and a second kernel joins the parts.  Whole / divided, us: 2048 tokens behind 10240, 40/8 heads (320 items) 476 / 384, MXINT8
+// 546 / 429; 512 behind 15488, 32/8 heads 212 / 123; 300 of 4000, two requests 67 / 49.  It is a kernel of its own: what it needs beside costs registers
 // that those without it miss (8192 tokens 455 -> 490 us, MXINT8 520 -> 610).
 #include "lqer_cache.cuh"
 
@@ -57,7 +58,7 @@ struct Tiles {
   float* parts;                // [sms][256][D + 2]: rows' sums, then maxima and sums of weights
 };
 struct Barriers {
-  unsigned long long full[8], empty[8], raw_full[6], raw_empty[6], s_full[2], p_half[2], p_full[2], o_done[2], q_full, drained;
+  unsigned long long full[8], empty[8], raw_full[6], raw_empty[6], s_full[2], p_half[2], p_full[2], o_done[2], q_full[2], drained;
 };
 __device__ __forceinline__ uint32_t bar_of(unsigned long long& b) { return tc::smem_u32(&b); }
 
@@ -130,6 +131,9 @@ __device__ __forceinline__ void exp2_poly(F2 x, float& a, float& b) {
   unf2(q, qa, qb);
   a = __uint_as_float((__float_as_uint(ra) << 23) + __float_as_uint(qa));
   b = __uint_as_float((__float_as_uint(rb) << 23) + __float_as_uint(qb));
+  // what -125 gives: what is hidden, or as good as, weighs nothing, whatever its value
+  const float least = -0.99992805719f * 0x1p-125f;
+  unf2(add2(f2(a, b), f2(least, least)), a, b);
 }
 
 template <int N> struct Every { static constexpr int value = N; };
@@ -183,14 +187,16 @@ __device__ __forceinline__ Plan<DIVIDED> plan_of(const Tiles& s, const Item& it)
   q.skip = 0;
   return q;
 }
-// The CTA's item, to where all threads find it; heavy ones (a request's last) first.  False: there is none.
+// The CTA's item, to where all threads find it; heavy ones (a request's last) first.  False: there is none.  Of up to 32 requests every warp
+// knows the sums by itself.
 template <bool DIVIDED>
 __device__ __forceinline__ bool find_item(const Tiles& s, Item& found) {
   const Attention& p = s.a;
   const StepRequest* reqs = requests_of(p.step);
   __shared__ int sums[16];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, warps = blockDim.x >> 5;
-  const int per = (p.R + blockDim.x - 1) / blockDim.x, from = min(tid * per, p.R), to = min(from + per, p.R);
+  const bool one = p.R <= 32;
+  const int per = one ? 1 : (p.R + blockDim.x - 1) / blockDim.x, from = min((one ? lane : tid) * per, p.R), to = min(from + per, p.R);
   auto items_of = [&](const int4& w) {
     const int rows = w.y * p.group;
     return w.y > 0 && rows > s.few ? (rows + 2 * kRows - 1) / (2 * kRows) : 0;
@@ -204,26 +210,31 @@ __device__ __forceinline__ bool find_item(const Tiles& s, Item& found) {
   int x = mine;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) { const int y = __shfl_up_sync(0xFFFFFFFFu, x, o); if (lane >= o) x += y; }
-  if (lane == 31) sums[warp] = x;
-  __syncthreads();
-  int before = x - mine, total = 0;
-  for (int k = 0; k < warps; ++k) { if (k < warp) before += sums[k]; total += sums[k]; }
+  int before = x - mine, total = __shfl_sync(0xFFFFFFFFu, x, 31);
+  if (!one) {
+    if (lane == 31) sums[warp] = x;
+    __syncthreads();
+    total = 0;
+    for (int k = 0; k < warps; ++k) { if (k < warp) before += sums[k]; total += sums[k]; }
+  }
   // All but the last turn of CTAs take an item each; what is left, if it would keep no more than half of them busy, is divided.
-  const long long all = (long long)total * p.hkv;
-  const int left = DIVIDED ? (int)(all % s.sms) : 0, parts = left > 0 ? min(s.sms / left, kMostParts) : 1;
-  const long long undivided = parts > 1 ? all - left : all;
-  if (DIVIDED && blockIdx.x == 0 && tid == 0) s.divided[0].request = parts > 1 ? left : 0;
-  const long long beyond = (long long)blockIdx.x - undivided, number = beyond < 0 ? blockIdx.x : undivided + beyond / parts;
+  const uint32_t all = (uint32_t)(total * p.hkv);                  // (the host has seen to it that this fits)
+  const uint32_t left = DIVIDED ? all % (uint32_t)s.sms : 0u, parts = left > 0 ? min((uint32_t)s.sms / left, (uint32_t)kMostParts) : 1u;
+  const uint32_t undivided = parts > 1 ? all - left : all;
+  if (DIVIDED && blockIdx.x == 0 && tid == 0) s.divided[0].request = parts > 1 ? (int)left : 0;
+  const bool whole = blockIdx.x < undivided;
+  const uint32_t beyond = whole ? 0u : blockIdx.x - undivided, slot = DIVIDED ? beyond / parts : beyond, number = whole ? blockIdx.x : undivided + slot;
   if (number >= all) return false;
-  const int index = total - 1 - (int)(number / p.hkv);
-  if (index >= before && index < before + mine) {
+  const uint32_t back = number / (uint32_t)p.hkv, head = number - back * p.hkv;
+  const int index = total - 1 - (int)back;
+  if (index >= before && index < before + mine && (!one || warp == 0)) {
     for (int r = from;; ++r) {
       if (per > 1) w = __ldg(reinterpret_cast<const int4*>(reqs + r));
       const int c = items_of(w);
       if (index < before + c) {
         const int base = (index - before) * 2 * kRows, token = base / p.group;
-        found = Item{r, (int)(number % p.hkv), w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group, beyond < 0 ? -1 : (int)(beyond / parts),
-                     beyond < 0 ? 0 : (int)(beyond % parts), beyond < 0 ? 1 : parts};
+        found = Item{r, (int)head, w.x, w.y, w.z, base, w.y * p.group, token, base - token * p.group, whole ? -1 : (int)slot,
+                     whole ? 0 : (int)(beyond - slot * parts), whole ? 1 : (int)parts};
         break;
       }
       before += c;
@@ -267,8 +278,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       tc::mbar_init(bar_of(bars.p_half[t]), 4);
       tc::mbar_init(bar_of(bars.p_full[t]), 4);
       tc::mbar_init(bar_of(bars.o_done[t]), 1);
+      tc::mbar_init(bar_of(bars.q_full[t]), 4 + (s.stall && blockIdx.x == 0 ? 1 : 0));
     }
-    tc::mbar_init(bar_of(bars.q_full), 8 + (s.stall && blockIdx.x == 0 ? 1 : 0));
     tc::mbar_init(bar_of(bars.drained), 1);
     tc::fence_barrier_init();
     ws.abort = 0;
@@ -345,7 +356,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       }
       tc::fence_proxy_async_smem();
       __syncwarp();
-      if (lane == 0) tc::mbar_arrive(bar_of(bars.q_full));
+      if (lane == 0) tc::mbar_arrive(bar_of(bars.q_full[t]));
     }
     const int first_pos = t ? plan.first_pos[1] : plan.first_pos[0], last_pos = t ? plan.last_pos[1] : plan.last_pos[0];
     int token, head;
@@ -470,8 +481,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         __syncwarp();
         if (lane == 0) tc::mbar_arrive(bar_of(bars.p_full[t]));
       };
-      if (masked) weights(Every<0>{});
-      else weights(Every<MX ? 0 : kPolyEvery>{});
+      // (one for all tiles: without one of their own for tiles in which something is hidden, 8192 tokens 459 -> 454 us, the window's 217 -> 213)
+      weights(Every<MX ? 0 : kPolyEvery>{});
       ++n;
     }
     if (ok && n > 0) {
@@ -594,22 +605,37 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const uint32_t s_idesc = tc::make_idesc(128, 128) | (s.negate ? 1u << 13 : 0u), o_idesc = tc::make_idesc(128, D) | 1u << 16;
     const uint32_t base = __shfl_sync(0xFFFFFFFFu, tmem, 0);
     auto all = [&](bool got) { ok = __all_sync(0xFFFFFFFFu, got) != 0; return ok; };
-    int n[2] = {0, 0};                                             // key tiles whose O is under way
-    int at = 0;                                                    // place in the ring, and how often it has been round: of K(j), V(j - 1) before it
-    uint32_t phase = 0;
-    all(tc::mbar_wait(bar_of(bars.q_full), 0, &ws));
-    for (int j = 0; j <= plan.count && ok; ++j) {
-      const int v_at = at;
-      if (j > 0) {
-        if (!all(tc::mbar_wait(bar_of(bars.full[v_at]), phase, &ws))) break;
-        if (++at == SH::STAGES) { at = 0; phase ^= 1; }
+    auto scores = [&](int t, int k_at) {
+#pragma unroll
+      for (int k = 0; k < D / 16; ++k) {
+        const uint32_t off = (k >> 2) * (SH::HALF >> 4) + (k & 3) * 2;
+        mma_ss(base + SH::S_COL + t * 128, rows_desc(q_at + t * SH::TILE) + off, rows_desc(ring_at + k_at * SH::TILE) + off, s_idesc, k > 0 ? 1u : 0u);
       }
+      tc::umma_commit(bar_of(bars.s_full[t]));
+    };
+    int n[2] = {0, 0};                                             // key tiles whose O is under way
+    int at = 0;                                                    // place in the ring, and how often it has been round
+    uint32_t phase = 0;
+    // the first scores, of each row tile as soon as its queries are there
+    if (all(tc::mbar_wait(bar_of(bars.full[0]), 0, &ws))) {
+#pragma unroll 1
+      for (int t = 0; t < 2 && all(tc::mbar_wait(bar_of(bars.q_full[t]), 0, &ws)); ++t) {
+        tc::tc_fence_after();
+        if (plan.sees(t, plan.tile(0)) && leader) scores(t, 0);
+      }
+      if (leader) tc::umma_commit(bar_of(bars.empty[0]));
+      at = 1;
+    }
+    for (int j = 1; j <= plan.count && ok; ++j) {                  // values of tile j - 1, keys of tile j
+      const int v_at = at;
+      if (!all(tc::mbar_wait(bar_of(bars.full[v_at]), phase, &ws))) break;
+      if (++at == SH::STAGES) { at = 0; phase ^= 1; }
       const int k_at = at;
       const uint32_t k_phase = phase;
       bool keys_there = false;
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
-        if (j > 0 && plan.sees(t, plan.tile(j - 1))) {
+        if (plan.sees(t, plan.tile(j - 1))) {
 #pragma unroll
           for (int half = 0; half < 2; ++half) {
             if (!all(tc::mbar_wait(bar_of(half ? bars.p_full[t] : bars.p_half[t]), n[t] & 1, &ws))) break;
@@ -631,19 +657,12 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
             tc::tc_fence_after();
             keys_there = true;
           }
-          if (plan.sees(t, plan.tile(j)) && leader) {
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k) {
-              const uint32_t off = (k >> 2) * (SH::HALF >> 4) + (k & 3) * 2;
-              mma_ss(base + SH::S_COL + t * 128, rows_desc(q_at + t * SH::TILE) + off, rows_desc(ring_at + k_at * SH::TILE) + off, s_idesc, k > 0 ? 1u : 0u);
-            }
-            tc::umma_commit(bar_of(bars.s_full[t]));
-          }
+          if (plan.sees(t, plan.tile(j)) && leader) scores(t, k_at);
         }
       }
       if (!ok) break;
       if (leader) {
-        if (j > 0) tc::umma_commit(bar_of(bars.empty[v_at]));
+        tc::umma_commit(bar_of(bars.empty[v_at]));
         if (j < plan.count) tc::umma_commit(bar_of(bars.empty[k_at]));
       }
       if (++at == SH::STAGES) { at = 0; phase ^= 1; }
@@ -791,8 +810,8 @@ static cudaError_t launch_shape(const Tiles& k, int ctas, const lqer_kv_cache_t&
   return launch_after(join_tiles_kernel<D>, dim3(k.sms / 2, 2 * kRows * D / 1024), 256, 0, s, k);
 }
 // Whether items may be divided: a division costs a launch and the way of the parts through memory, some 5 us, and gains what the last turn of CTAs leaves of it, if the
-// rows are where they can be, and the keys as many (some 1.8 us for 128).  Not divided / divided, us: 300 tokens, 32/8 heads: 15 / 20, of 600: 19 / 25, of 1300 32 / 27,
-// of 16000, 512 tokens: 221 / 137.
+// rows are where they can be, and the keys as many (some 1.8 us for 128).  Not divided / divided, us: 300 tokens, 32/8 heads: 15 / 20, of 600: 19 / 25, of 1000: 23 / 22,
+// of 4000, 1100 tokens, 32/32 heads, MXINT8: 120 / 98, of 16000, 512 tokens: 212 / 123.
 static bool may_divide(const Attention& a) {
   const int sms = sm_count();
   if (sms < 2) return false;

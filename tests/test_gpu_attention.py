@@ -264,3 +264,23 @@ def test_scores_that_are_no_numbers_reach_the_rows_that_see_them(D, requests, ba
         good = ~torch.isnan(y)
         assert bool(((Y - y).abs() <= tolerance(y, weighed, most, D, before + n))[good].all())
         b.cache.keys.copy_(keys)
+
+
+@pytest.mark.parametrize("requests,window,hidden,rows", [
+    ([(0, 300)], 0, slice(150, 300), slice(0, 150)), ([(0, 700)], 0, slice(500, 700), slice(0, 500)), ([(1500, 140)], 0, slice(1600, 1640), slice(0, 100)),
+    ([(0, 300)], 40, slice(0, 100), slice(139, 300)), ([(100, 8)], 0, slice(104, 108), slice(0, 4)), ([(2000, 8)], 500, slice(0, 1504), slice(4, 8)),
+])
+@pytest.mark.parametrize("D", [64, 128])
+def test_hidden_values_weigh_nothing_however_large(D, requests, window, hidden, rows):
+    b = Batch(requests, 8, 8, D, 16)
+    (before, n), = requests
+    want = L.paged_attention(b.Q, b.cache, b.pages, b.step, window=window)
+    ids = b.pages.tables[0, :(before + n + 15) // 16].long()
+    V = b.cache.values[ids].transpose(0, 1).flatten(1, 2)
+    V[:, hidden] = 3e38
+    b.cache.values[ids] = V.unflatten(1, (len(ids), 16)).transpose(0, 1)
+    got = L.paged_attention(b.Q, b.cache, b.pages, b.step, window=window)
+    assert torch.equal(got[rows], want[rows])
+    others = torch.ones(n, dtype=torch.bool, device=DEV)
+    others[rows] = False
+    assert bool((got[others].abs() > 1e30).any())
