@@ -37,6 +37,8 @@ inline int few_rows(const Attention& p) {
   const long long heads = (long long)(p.R < p.M ? p.R : p.M) * p.hkv, few = 2900 / heads, most = (long long)p.max_pages * p.page > 4096 ? 48 : 96;
   return few < kLeast ? kLeast : (int)(few < most ? few : most);
 }
+// The most rows of a key head that a request can have; a step may be told of more tokens than the batch has rows.
+inline long long most_rows(const Attention& p) { return (long long)(p.max_added < p.M ? p.max_added : p.M) * p.group; }
 constexpr int kMinChunks = 2;                // of a CTA's run
 
 // What a CTA leaves for the join: the (request, key head, row tile) that begins in its run and goes on behind it, if any.
@@ -562,7 +564,7 @@ static int split_grid(const Attention& p, int few, int rows_per, int dim) {
   const long long want = (units + kMinChunks - 1) / kMinChunks;
   return (int)(want < most ? want : most);
 }
-static int rows_per_tile(const Attention& p) { return p.max_added * (long long)p.group <= 8 ? 8 : 16; }
+static int rows_per_tile(const Attention& p) { return most_rows(p) <= 8 ? 8 : 16; }
 
 template <int D, bool MX, int NT>
 static cudaError_t launch_split(const Split& s, int grid, cudaStream_t stream) {
@@ -607,7 +609,7 @@ static void set_window(kv::Attention& p, int window, int sinks) {
 // The most that a call takes, whatever its window.
 size_t attention_scratch_bytes(const lqer_kv_cache_t& c, const lqer_page_table_t& t, int M, int hq, int max_added) {
   const kv::Attention p = attention_params(c, t, M, hq, max_added);
-  return few_bytes(p, c.head_dim) + (max_added * (long long)p.group > kv::few_rows(p) ? kv::tiles_scratch_bytes(p, c.head_dim) : 0);
+  return few_bytes(p, c.head_dim) + (kv::most_rows(p) > kv::few_rows(p) ? kv::tiles_scratch_bytes(p, c.head_dim) : 0);
 }
 cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq, const lqer_kv_cache_t& c, const lqer_page_table_t& t, void* step,
                                    int max_added, int window, int sinks, double scale, int bits, void* Y, void* scratch,
@@ -624,7 +626,7 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
   k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + spans_bytes());
   const size_t whole = (size_t)M * hq * c.head_dim * 2, less = debug_y_shrink();
   k.y_extent = whole > less ? whole - less : 0;
-  if (max_added * (long long)k.a.group > k.few) {
+  if (kv::most_rows(k.a) > k.few) {                                // (then there are items of more than kLeast rows, or a single request's)
     // A single request goes there whatever it turns out to bring; beside one that has to, only those of few rows stay (three prompts of 42 to 97 tokens,
     // 16/4 heads: 18.4 us where the smaller ones stayed, 11.7).
     k.few = t.n_requests == 1 ? 0 : kv::kLeast;

@@ -284,3 +284,9 @@ def test_hidden_values_weigh_nothing_however_large(D, requests, window, hidden, 
     others = torch.ones(n, dtype=torch.bool, device=DEV)
     others[rows] = False
     assert bool((got[others].abs() > 1e30).any())
+
+
+@pytest.mark.parametrize("requests,hq,hkv", [([(5, 1), (90, 1)], 8, 2), ([(300, 1), (20, 2), (0, 5)], 32, 32), ([(700, 1)], 16, 2), ([(40, 8), (3, 8)], 1, 1)])
+@pytest.mark.parametrize("most", [100, 5000])
+def test_fewer_rows_than_a_request_might_bring(most, requests, hq, hkv, ratio_log):
+    _run(Batch(requests, hq, hkv, 64, 16, max_added=most), log=ratio_log)
