@@ -425,7 +425,8 @@ lqer_status_t lqer_append_kv(const void* K, const void* V, lqer_dtype_t x_dtype,
  *    by it).  The plan is only read, but for its status: one of another batch or table (or none) is reported there as LQER_ERR_BAD_PACKED and
  *    nothing is written; a table entry that is no page as LQER_ERR_BOUNDS (the rows of that request then hold anything).  Rows behind the last token
  *    and those of refused requests are left as they are.
- *  - Scores, their maxima and all sums are fp32; the weights of the values are rounded to bf16.  What no row of the step sees may hold anything; an
+ *  - Scores, their maxima and all sums are fp32 (scale log2(e) Q . K has to be in its range: a row with one that is not may be NaN); the weights of the
+ *    values are rounded to bf16.  What no row of the step sees may hold anything; an
  *    infinite or NaN value that some rows of a request see and others do not may reach those, too.  Exponents of an MXINT8 cache that are seen lie
  *    within the format's window, as lqer_append_kv writes them.
  *  - workspace: lqer_attention_workspace_bytes, 256-byte aligned; nothing in it has to be kept or cleared, and calls that overlap need one each.

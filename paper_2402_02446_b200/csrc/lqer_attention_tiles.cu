@@ -32,6 +32,7 @@ namespace lqer {
 namespace kv {
 
 constexpr int kRows = 128, kKeys = 128;      // of a tile
+constexpr float kNear = 512.f;               // largest exponent of a row's maximum that is rounded by itself: half of its last place is 2^-16, 1.1e-5 of a weight
 
 template <int D, bool MX>
 struct Shape {
@@ -364,7 +365,11 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const int pos = it.len - it.n + token;
     const float c = p.scale_log2;
     const F2 c2 = f2(c, c);
-    float m = -INFINITY;
+    // Exponents are s c - m c in one operation, with m c rounded once.  That is off by 2^-24 of m c, the same for the whole row, and no more than the
+    // polynomial is up to kNear.  Of larger ones, in any row of the warp, the difference is taken first: from 2^30 on the rounding alone would leave the range
+    // of an exponent.  There a maximum that is infinite or NaN makes all weights NaN, too; the polynomial alone would hide it.
+    float m = -INFINITY, base = 0.f;
+    bool far = false;
     F2 la = f2(0.f, 0.f), lb = f2(0.f, 0.f);                       // sums of weights, four to a row
     int n = 0;                                                     // key tiles so far
     for (int j = 0; j < plan.count && ok; ++j) {
@@ -427,6 +432,9 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       if (__any_sync(0xFFFFFFFFu, up)) {
         const float f = up ? exp2_fast((m - big) * c) : 1.f;
         if (up) m = big;
+        base = m == -INFINITY ? 0.f : -m * c;
+        far = __any_sync(0xFFFFFFFFu, !(fabsf(base) <= kNear));
+        if (far) base = 0.f;
         if (n > 0) {
           la = fma2(la, f2(f, f), f2(0.f, 0.f));
           lb = fma2(lb, f2(f, f), f2(0.f, 0.f));
@@ -444,8 +452,12 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
           }
         }
       }
-      // a maximum that is infinite or NaN makes all weights NaN; the polynomial alone would hide it
-      const float base = m == -INFINITY ? 0.f : fmaf(-m, c, m - m);
+      if (far) {
+        const float top = m == -INFINITY ? 0.f : m, less = (top - top) - top;
+        const F2 less2 = f2(less, less);
+#pragma unroll
+        for (int i = 0; i < 128; i += 2) unf2(add2(f2(v[i], v[i + 1]), less2), v[i], v[i + 1]);
+      }
       const F2 base2 = f2(base, base);
       // the weights, and word to the issuer, which may begin with the first half; POLY: every POLY-th pair by the polynomial
       auto weights = [&](auto every) {
@@ -498,7 +510,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       float* const part = s.parts + (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2) + (size_t)(t * kRows + row) * D;
       float* const marks = s.parts + (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + t * kRows + row;
       if (ok && left > 0) {
-        marks[0] = n > 0 && m != -INFINITY ? m * c : -INFINITY;
+        marks[0] = n > 0 ? m : -INFINITY;                          // (of the scores as they are: the join scales differences, too)
         marks[2 * kRows] = all;
       }
 #pragma unroll 1
@@ -753,14 +765,14 @@ __global__ void __launch_bounds__(256, 4) join_tiles_kernel(const Tiles s) {
     float top = big;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) top = fmaxf(top, m[k]);
-    const float base = top == -INFINITY ? 0.f : top, f0 = exp2_fast(big - base);
+    const float base = top == -INFINITY ? 0.f : top, f0 = exp2_fast((big - base) * p.scale_log2);
     sum.x *= f0; sum.y *= f0; sum.z *= f0; sum.w *= f0;
     all *= f0;
     big = top;
 #pragma unroll
     for (int k = 0; k < kAtOnce; ++k) {
       if (l[k] == 0.f) continue;                                   // nothing was put there, or nothing of weight
-      const float f = exp2_fast(m[k] - base);
+      const float f = exp2_fast((m[k] - base) * p.scale_log2);
       sum.x += f * x[k].x; sum.y += f * x[k].y; sum.z += f * x[k].z; sum.w += f * x[k].w;
       all += f * l[k];
     }
