@@ -848,8 +848,9 @@ cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqe
   k.few = few;
   k.negate = a.scale_log2 < 0.f;
   if (k.negate) k.a.scale_log2 = -a.scale_log2;
-  // what is hidden is minus infinity before the scale comes in, and has to stay that: a scale of 0 is one that is as good as 0 for any score
-  if (k.a.scale_log2 < 1e-40f) k.a.scale_log2 = 1e-40f;
+  // what is hidden is minus infinity before the scale comes in, and has to stay that: a scale of 0 is the least number that there is, 2^-149, which makes 2^-20 of the
+  // largest difference of two scores
+  if (k.a.scale_log2 == 0.f) k.a.scale_log2 = 0x1p-149f;
   k.group_inv = a.group == 1 ? 0u : (uint32_t)(((1ull << 32) + a.group - 1) / a.group);
   k.stall = take_stall(kFamDecode) ? 1 : 0;
   k.wait_limit = wait_limit_cycles();
