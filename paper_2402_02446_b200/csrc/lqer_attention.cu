@@ -3,6 +3,7 @@
 // Row i of head h of a request sees key j <= position, and under a window only the last `window` of them and the first `sinks`:
 //   y = sum_j p_j v_j / sum_j p_j,  p_j = exp2(s_j - m),  s_j = scale log2(e) q . k_j,  m = the largest s_j so far.
 // (m, sum p, sum p v) of two sets of keys join to that of their union: with M = max(m1, m2), each side counts 2^(m_i - M).
+// A row sees itself at least, so its sum is 0 only where all of its scores are minus infinity: 0 / 0, NaN, as the formula says.
 //
 // The rows of the query heads that share a key head, of all of a request's new tokens, go together (a row tile of 8 NT): the keys
 // and values are read once for them.  Bound: those bytes.  The products are far from any limit, so they are mma.sync m16n8k16 with the keys (and
@@ -410,7 +411,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
           for (int x = 4; x < 32; x <<= 1) l[t][i] += __shfl_xor_sync(0xFFFFFFFFu, l[t][i], x);
           const int row = 8 * t + 2 * c + i;
           if (row >= rows) continue;
-          const float inv = l[t][i] == 0.f ? 0.f : 1.f / l[t][i];
+          const float inv = 1.f / l[t][i];
           const int x = tile * ROWS + row;
           const size_t at = ((size_t)(row0 + x / p.group) * p.hq + h * p.group + x % p.group) * D + 8 * g;
           auto two = [&](int k, int half) { return round_bf16x2(o[t][k][i + 2 * half] * inv, o[t][k + 1][i + 2 * half] * inv); };
@@ -469,7 +470,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
         all += f * of_warp(w)[R::OUT + ROWS + row];
       }
       if (whole) {
-        const float inv = all == 0.f ? 0.f : 1.f / all;
+        const float inv = 1.f / all;
         const int x = tile * ROWS + row;
         const size_t at = ((size_t)(row0 + x / p.group) * p.hq + h * p.group + x % p.group) * D + d;
         if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 60))
@@ -549,7 +550,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(const Split s) {
     }
   }
   if (share > 0) return;
-  const float inv = all == 0.f ? 0.f : 1.f / all;
+  const float inv = 1.f / all;
   const int x = span.tile * ROWS + row;
   const size_t at = ((size_t)(span.row0 + x / p.group) * p.hq + span.head * p.group + x % p.group) * D + d;
   if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 61))

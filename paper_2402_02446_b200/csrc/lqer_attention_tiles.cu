@@ -522,7 +522,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         for (int i = 0; i < 4; ++i) store32(part + 32 * k + 8 * i, true, o + 8 * i);
       }
     } else if (ok && n > 0) {
-      const float inv = all == 0.f ? 0.f : 1.f / all;
+      const float inv = 1.f / all;
       const size_t at = ((size_t)(it.row0 + token) * p.hq + it.head * p.group + head) * D;
       const bool mine = row < left && LQER_IN_BOUNDS(&p.step->status, at * 2, D * 2, s.y_extent, 62);
 #pragma unroll
@@ -777,7 +777,7 @@ __global__ void __launch_bounds__(256, 4) join_tiles_kernel(const Tiles s) {
       all += f * l[k];
     }
   }
-  const float inv = all == 0.f ? 0.f : 1.f / all;
+  const float inv = 1.f / all;
   const uint32_t z = (uint32_t)(row + q.head0), token = p.group == 1 ? z : __umulhi(z, s.group_inv), head = z - token * p.group;
   const size_t at = ((size_t)(q.row0 + q.token0 + token) * p.hq + q.head * p.group + head) * D + d;
   if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 64))
