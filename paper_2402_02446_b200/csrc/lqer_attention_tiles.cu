@@ -365,6 +365,9 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const int pos = it.len - it.n + token;
     const float c = p.scale_log2;
     const F2 c2 = f2(c, c);
+    // Of the key tiles that have something that no row sees the first row tile clears the values of those that it sees, the second those beyond, which are behind the
+    // window: so nobody writes what is being read (products are issued for the first row tile first, and not before its weights are there).
+    const int clear_end = max(it.len - kKeys + 1, t ? plan.end[0] * kKeys : 0), clear_seen = t ? 0 : seen_from;
     // Exponents are s c - m c in one operation, with m c rounded once.  That is off by 2^-24 of m c, the same for the whole row, and no more than the
     // polynomial is up to kNear.  Of larger ones, in any row of the warp, the difference is taken first: from 2^30 on the rounding alone would leave the range
     // of an exponent.  There a maximum that is infinite or NaN makes all weights NaN, too; the polynomial alone would hide it.
@@ -382,7 +385,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
 #pragma unroll
       for (int k = 0; k < 2; ++k) tc::tmem_ld32(s_at + 32 * k, *reinterpret_cast<uint32_t(*)[32]>(&v[32 * k]));
       if constexpr (!MX) {
-        if (has_unseen(key0)) {
+        if (key0 >= clear_end || (key0 < clear_seen && key0 + kKeys > p.sinks)) {
           // values that no row sees may be anything: 0 times that has to be 0
           const int at = 2 * j + 1;
           ok = __all_sync(0xFFFFFFFFu, tc::mbar_wait(bar_of(bars.full[at % SH::STAGES]), at / SH::STAGES & 1, &ws)) != 0;
