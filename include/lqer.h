@@ -400,6 +400,8 @@ typedef struct {
  *    row's slot (page * tokens a page + place in the page; what lqer_append_kv takes) and the token's place in its request (what a
  *    rotary embedding takes), and -1 for rows behind the last.
  *  - step (lqer_cache_step_bytes, 256-byte aligned) gets the plan that lqer_paged_attention reads.  max_added: what no added[r] exceeds.
+ *    Its last bytes are the step's own lengths (n_requests ints, 16-byte aligned) and, in the last 16 of lqer_cache_step_bytes, its ring, the same as in lengths_out
+ *    and ring_out (which may be these).
  *  - What only the device can see is reported in step (lqer_poll_status): LQER_ERR_BUFFER_TOO_SMALL where too few pages are free, from the
  *    first request that finds too few on for all that need any; LQER_ERR_BOUNDS for a request whose length is out of the tables' range before or
  *    after, that takes more than max_added, or whose rows do not fit M, for a ring that cannot be (every request that needs or

@@ -765,16 +765,17 @@ def new_page_table(n_requests: int, max_pages: int, n_pages: int, page: int, dev
 
 
 class CacheStep:
-    """A step of a batch: slots and positions int32 [M] of its rows (-1 behind the last), lengths [n_requests] and ring [2] as they are after it, and the
-    plan for paged_attention in buf (poll_status(buf) tells of requests that were refused)."""
+    """A step of a batch: slots and positions int32 [M] of its rows (-1 behind the last), lengths [n_requests] and ring [2] as they are after it (the step's own,
+    which later steps leave alone), and the plan for paged_attention in buf (poll_status(buf) tells of requests that were refused)."""
 
     def __init__(self, pages: PageTable, M: int, max_added: int):
         new = pages.tables.new_empty
         self.M, self.max_added, self.n_requests, self.index = M, max_added, pages.n_requests, pages.index
         self.buf = new(pages.step_bytes, dtype=torch.uint8)
         self.slots, self.positions = new(M), new(M)
-        self.lengths, self.ring = new(pages.n_requests), new(2, dtype=torch.int64)
-        self.own_lengths, self.own_ring = self.lengths, self.ring
+        end = pages.step_bytes                             # where the plan ends, and with it lengths and ring
+        at = end - 16 - (4 * pages.n_requests + 15) // 16 * 16
+        self.lengths, self.ring = self.buf[at:at + 4 * pages.n_requests].view(torch.int32), self.buf[end - 16:end].view(torch.int64)
         self.room = {}                 # workspace bytes by heads and cache format, for this M and max_added
 
 
@@ -783,7 +784,7 @@ def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | N
     """Takes the batch one step further: request r takes added[r] tokens (int32 [n_requests]), or loses -added[r]; pages are given out and taken back.
     M: rows of the step's tensors, those of the requests in order and any padding behind them.  max_added: what no added[r] exceeds (M if not given); 1 tells
     that this is a decoding step.  step: one of the same sizes to be made again in place.  commit: pages.lengths and pages.ring step on too (in place);
-    otherwise they stay, and the step's own hold what would be."""
+    otherwise they stay, and only the step's own hold what would be."""
     index = added.get_device()
     if stream is not None or not _here(index):
         with _on(stream, index):
@@ -799,7 +800,7 @@ def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | N
         step = CacheStep(pages, M, max_added)
     elif step.M != M or step.n_requests != pages.n_requests or step.index != index:
         raise ValueError("the step to be made again has other sizes")
-    lengths, ring = (pages.lengths, pages.ring) if commit else (step.own_lengths, step.own_ring)
+    lengths, ring = (pages.lengths, pages.ring) if commit else (step.lengths, step.ring)
     status = lib().lqer_cache_step(pages.ref, pages.lengths.data_ptr(), _ptr(added, index), pages.ring.data_ptr(), M, max_added, lengths.data_ptr(),
                                    ring.data_ptr(), step.slots.data_ptr(), step.positions.data_ptr(), step.buf.data_ptr(), step.buf.numel(),
                                    _raw_stream(index))
@@ -807,7 +808,6 @@ def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | N
         raise LqerError(status, "lqer_cache_step")
     if step.max_added != max_added:
         step.max_added, step.room = max_added, {}
-    step.lengths, step.ring = lengths, ring
     return step
 
 

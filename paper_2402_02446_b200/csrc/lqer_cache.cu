@@ -140,7 +140,9 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   const long long avail = ring_ok ? tail + all_given - head : 0;
   long long rows_before = 0;
   int wanted_before = 0;
-  StepRequest* out = reinterpret_cast<StepRequest*>(reinterpret_cast<uint8_t*>(p.head) + kStepHeadBytes);
+  uint8_t* const plan = reinterpret_cast<uint8_t*>(p.head);
+  StepRequest* out = reinterpret_cast<StepRequest*>(plan + kStepHeadBytes);
+  int* const lengths = reinterpret_cast<int*>(plan + step_lengths_at(p.R));
   for (int base = 0; base < p.R; base += kStepThreads) {
     const int r = base + tid;
     const Request q = request(base);
@@ -163,7 +165,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
     lens[tid] = ok ? q.next : q.bad ? 0 : q.len;
     if (r < p.R) {
       out[r] = StepRequest{row0s[tid], ns[tid], lens[tid], 0};
-      p.lengths_out[r] = ok ? q.next : q.len;
+      p.lengths_out[r] = lengths[r] = ok ? q.next : q.len;
     }
     __syncthreads();
     // (whoever is not refused takes pages that are there: fewer than n_pages before them)
@@ -206,8 +208,9 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   if (rows_inside)
     for (int row = rows + tid; row < p.M; row += kStepThreads) p.slots[row] = p.positions[row] = -1;
   if (tid == 0) {
-    p.ring_out[0] = head + taken;
-    p.ring_out[1] = ring_ok ? tail + all_given : tail;
+    long long* const ring = reinterpret_cast<long long*>(plan + step_ring_at(p.R));
+    p.ring_out[0] = ring[0] = head + taken;
+    p.ring_out[1] = ring[1] = ring_ok ? tail + all_given : tail;
     StepHead h = {};
     h.magic = kStepMagic;
     h.R = p.R; h.M = p.M; h.page = p.page; h.max_pages = p.max_pages; h.n_pages = p.n_pages; h.max_added = p.max_added; h.rows = rows;

@@ -23,7 +23,10 @@ struct StepRequest {           // one per request, behind the head
   int row0, n, len, reserved;  // first row, rows (0: none, or refused), tokens that it holds once they are in
 };
 constexpr size_t kStepHeadBytes = 256;
-inline size_t step_bytes(int R) { return kStepHeadBytes + (size_t)R * sizeof(StepRequest); }
+// Behind the requests: lengths and ring as they are after the step, for whoever keeps the step when the tables' own go on.
+__host__ __device__ constexpr size_t step_lengths_at(int R) { return kStepHeadBytes + (size_t)R * sizeof(StepRequest); }
+__host__ __device__ constexpr size_t step_ring_at(int R) { return step_lengths_at(R) + ((size_t)R * sizeof(int) + 15) / 16 * 16; }
+inline size_t step_bytes(int R) { return step_ring_at(R) + 2 * sizeof(long long); }
 
 // What the attention kernels read.
 struct Attention {
