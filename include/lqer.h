@@ -374,7 +374,8 @@ lqer_status_t lqer_adapters(const void* X, lqer_dtype_t x_dtype, int M, const lq
  *
  * A cache holds n_pages pages of `page` tokens (16, 32, 64 or 128) of one layer: keys and values are [n_pages, kv_heads, page, head_dim] each
  * (head_dim 64 or 128; n_pages * page < 2^31), bf16, or MXINT8 in the format of cfg (the mantissas in that order, then an exponent byte for every
- * 16 of them along head_dim).  lqer_kv_cache_bytes: the size of either.  Its memory may hold anything where no token was put. */
+ * 16 of them along head_dim; the bits of its mantissas are not kept in it, so what writes it and what reads it are given the same cfg).
+ * lqer_kv_cache_bytes: the size of either.  Its memory may hold anything where no token was put. */
 typedef struct {
   void* keys;
   void* values;

@@ -708,15 +708,17 @@ def apply_adapters(X: torch.Tensor, pool: AdapterPool, plan: AdapterPlan, Y0: to
 
 class KVCache:
     """Pages of one layer's keys and values (see include/lqer.h).  bf16: keys and values are tensors [n_pages, kv_heads, page, head_dim]; MXINT8:
-    flat uint8 tensors, the mantissas in that order, then the exponent bytes (mxint8_bytes(n_pages * kv_heads * page, head_dim))."""
+    flat uint8 tensors, the mantissas in that order, then the exponent bytes (mxint8_bytes(n_pages * kv_heads * page, head_dim)), in the format
+    of cfg: that of the first append_kv where none was given."""
 
-    def __init__(self, n_pages: int, page: int, kv_heads: int, head_dim: int, dtype, device):
+    def __init__(self, n_pages: int, page: int, kv_heads: int, head_dim: int, dtype, device, cfg: Config | None = None):
         code = _OUT_CODE.get(dtype)
         if code not in (1, 2):
             raise ValueError("a cache holds torch.bfloat16 or MXINT8")
         self.n_pages, self.page, self.kv_heads, self.head_dim = n_pages, page, kv_heads, head_dim
         self.dtype = MXINT8 if code == 2 else torch.bfloat16
         self.key = (n_pages, page, kv_heads, head_dim, code)
+        self.cfg = None if cfg is None or code != 2 else Config.from_buffer_copy(cfg)
         self.handle = _Cache(None, None, n_pages, page, kv_heads, head_dim, code)
         self.ref = C.byref(self.handle)
         size = C.c_size_t()
@@ -728,13 +730,23 @@ class KVCache:
         self.index = self.keys.get_device()
         self.handle.keys, self.handle.values = self.keys.data_ptr(), self.values.data_ptr()
 
+    def format(self, cfg: Config | None) -> Config | None:
+        """The format of a call: that of the cache where none is given, and no other one.  (Exponents mean the same in all, mantissas go by their bits.)"""
+        own = self.cfg
+        if cfg is None or own is None:
+            return own if cfg is None else cfg
+        if cfg.a_bits != own.a_bits:
+            raise ValueError(f"the cache holds another format: mantissas of {own.a_bits} bits, not {cfg.a_bits}")
+        return cfg
 
-def new_kv_cache(n_pages: int, page: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda", stream=None) -> KVCache:
-    """A cache of zeros: n_pages pages of `page` tokens (16, 32, 64 or 128), head_dim 64 or 128, torch.bfloat16 or MXINT8."""
+
+def new_kv_cache(n_pages: int, page: int, kv_heads: int, head_dim: int, dtype=torch.bfloat16, device="cuda", stream=None, cfg: Config | None = None) -> KVCache:
+    """A cache of zeros: n_pages pages of `page` tokens (16, 32, 64 or 128), head_dim 64 or 128, torch.bfloat16 or MXINT8 (in the format of cfg, or, where none
+    is given, in that in which it is written first)."""
     if stream is not None:
         with _on(stream, stream.device.index if torch.device(device).index is None else torch.device(device).index):
-            return KVCache(n_pages, page, kv_heads, head_dim, dtype, stream.device)
-    return KVCache(n_pages, page, kv_heads, head_dim, dtype, device)
+            return KVCache(n_pages, page, kv_heads, head_dim, dtype, stream.device, cfg)
+    return KVCache(n_pages, page, kv_heads, head_dim, dtype, device, cfg)
 
 
 class PageTable:
@@ -823,7 +835,8 @@ def _head_rows(t: torch.Tensor, heads: int, dim: int, index: int):
 
 def append_kv(K: torch.Tensor, V: torch.Tensor, cache: KVCache, slots: torch.Tensor, cfg: Config | None = None, stream=None) -> None:
     """Puts keys and values [M, kv_heads, head_dim] (or [M, kv_heads * head_dim]; fp32 or bf16, any row stride, as parts of a joint projection have)
-    into their slots (int32 [M], of a step): rounded to bf16, or quantised to MXINT8 in the format of cfg."""
+    into their slots (int32 [M], of a step): rounded to bf16, or quantised to MXINT8 in the format of cfg, which is the cache's own if not given and has to have
+    its mantissas' bits otherwise."""
     index = K.get_device()
     if stream is not None or not _here(index):
         with _on(stream, index):
@@ -833,10 +846,13 @@ def append_kv(K: torch.Tensor, V: torch.Tensor, cache: KVCache, slots: torch.Ten
         raise ValueError("expected K and V of M rows and one type, slots int32 [M], and the cache on their device")
     k_stride, k_ptr = _head_rows(K, cache.kv_heads, cache.head_dim, index)
     v_stride, v_ptr = _head_rows(V, cache.kv_heads, cache.head_dim, index)
+    cfg = cache.format(cfg)
     status = lib().lqer_append_kv(k_ptr, v_ptr, _code(_REAL_CODE, K.dtype), k_stride, v_stride, M, _ptr(slots, index), cache.ref,
                                   None if cfg is None else C.byref(cfg), _raw_stream(index))
     if status:
         raise LqerError(status, "lqer_append_kv")
+    if cache.cfg is None and cache.key[-1] == 2:
+        cache.cfg = default_config() if cfg is None else Config.from_buffer_copy(cfg)
 
 
 def attention_workspace_bytes(M: int, q_heads: int, cache: KVCache, pages: PageTable, max_added: int) -> int:
@@ -850,7 +866,7 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, pages: PageTable, step: Cac
                     cfg: Config | None = None, Y: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Causal attention of a step's new tokens over the cache, their own keys and values included: bf16 [M, q_heads, head_dim].  Q [M, q_heads, head_dim]
     bf16, any row stride.  window: a token sees only the last `window` tokens (itself among them) and the first `sinks`; 0: all.  scale: of the scores,
-    head_dim ** -0.5 if not given.  Rows behind the last token are left as they are in Y (undefined where none is given).  ws: a workspace of
+    head_dim ** -0.5 if not given.  cfg: the format of an MXINT8 cache, its own if not given.  Rows behind the last token are left as they are in Y (undefined where none is given).  ws: a workspace of
     attention_workspace_bytes, made where none is given."""
     index = Q.get_device()
     if stream is not None or not _here(index):
@@ -861,7 +877,7 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, pages: PageTable, step: Cac
         raise ValueError("expected Q bf16 [rows of the step, q_heads, head_dim]")
     if cache.index != index or pages.index != index or step.index != index:
         raise ValueError("expected cache, page table and step on the device of Q")
-    M, heads = shape[0], shape[1]
+    M, heads, cfg = shape[0], shape[1], cache.format(cfg)
     q_stride, q_ptr = _head_rows(Q, heads, D, index)
     if Y is None:
         Y = Q.new_empty(shape)
