@@ -406,7 +406,8 @@ typedef struct {
  *  - What only the device can see is reported in step (lqer_poll_status): LQER_ERR_BUFFER_TOO_SMALL where too few pages are free, from the
  *    first request that finds too few on for all that need any; LQER_ERR_BOUNDS for a request whose length is out of the tables' range before or
  *    after, that takes more than max_added, or whose rows do not fit M, for a ring that cannot be (every request that needs or
- *    frees pages is refused then), and for a table entry that is no page (such a token has slot -1).  A refused request stays as it was: its length and pages, its rows
+ *    frees pages is refused then), and for a table entry that is no page (such a token has slot -1; one
+ *    that comes back joins the ring as it is).  A refused request stays as it was: its length and pages, its rows
  *    with slot -1; the others take their step. */
 lqer_status_t lqer_cache_step_bytes(int n_requests, size_t* bytes);
 lqer_status_t lqer_cache_step(const lqer_page_table_t* table, const int* lengths, const int* added, const long long* ring, int M, int max_added,

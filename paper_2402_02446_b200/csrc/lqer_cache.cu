@@ -128,7 +128,9 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
           const int i = at + u * kStepThreads;
-          if (i < total) p.free_pages[around(start, i, p.n_pages)] = id[u];
+          if (i >= total) continue;
+          p.free_pages[around(start, i, p.n_pages)] = id[u];
+          if ((unsigned)id[u] >= (unsigned)p.n_pages) fail(LQER_ERR_BOUNDS);
         }
       }
       before += total;
