@@ -75,7 +75,7 @@ __device__ __forceinline__ Run find_run(const Split& s, int per_tile, Run* share
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const int q = (p.R + kSplitThreads - 1) / kSplitThreads, from = min(tid * q, p.R), to = min(from + q, p.R);
   auto chunks_of = [&](int r) {
-    const int4 w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+    const int4 w = *reinterpret_cast<const int4*>(reqs + r);
     const int t = row_tiles(p, w.y, s.few, per_tile);
     return t == 0 ? 0LL : (long long)t * p.hkv * visible(p, w.y, w.z).chunks;
   };
@@ -203,7 +203,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
   int r = run.request, turn = 0;
   long long before = run.before;
   while (u < end) {
-    const int4 req = __ldg(reinterpret_cast<const int4*>(reqs + r));
+    const int4 req = *reinterpret_cast<const int4*>(reqs + r);
     const int row0 = req.x, n = req.y, len = req.z;
     const int tiles = row_tiles(p, n, s.few, ROWS);
     const Visible vis = visible(p, n, len);
@@ -225,7 +225,7 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
     auto next_key = [&](int key, int x) { return x + 1 == jump_at ? jump_to : key + hop; };
     const int* table = p.tables + (size_t)r * p.max_pages;
     int sent = x0, sent_key = key0, place = 0, sent_place = 0;      // the step that is sent next, its first key and its page
-    auto entry_of = [&]() { return sent < x1 && sent_key < len ? __ldg(table + (sent_key >> p.page_shift)) : 0; };
+    auto entry_of = [&]() { return sent < x1 && sent_key < len ? table[sent_key >> p.page_shift] : 0; };
     int entry = entry_of();
     auto send = [&]() {
       if (sent < x1 && sent_key < len)
@@ -248,8 +248,8 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
       for (int j = 0; j < D / 32; ++j) {
         q[t][j] = make_uint4(0u, 0u, 0u, 0u);
         if (8 * t + g < rows)
-          q[t][j] = __ldg(reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + (size_t)(row0 + x / p.group) * p.q_stride +
-                                                         (size_t)(h * p.group + x % p.group) * D + 8 * c + 32 * j));
+          q[t][j] = *reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(p.Q) + (size_t)(row0 + x / p.group) * p.q_stride +
+                                                     (size_t)(h * p.group + x % p.group) * D + 8 * c + 32 * j);
         if (MX) {
           const uint4 w = q[t][j];
           q[t][j] = make_uint4(__byte_perm(w.x, w.y, 0x5410), __byte_perm(w.x, w.y, 0x7632), __byte_perm(w.z, w.w, 0x5410), __byte_perm(w.z, w.w, 0x7632));

@@ -205,7 +205,7 @@ __device__ __forceinline__ bool find_item(const Tiles& s, Item& found) {
   int4 w = make_int4(0, 0, 0, 0);
   int mine = 0;
   for (int r = from; r < to; ++r) {
-    w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+    w = *reinterpret_cast<const int4*>(reqs + r);
     mine += items_of(w);
   }
   int x = mine;
@@ -230,7 +230,7 @@ __device__ __forceinline__ bool find_item(const Tiles& s, Item& found) {
   const int index = total - 1 - (int)back;
   if (index >= before && index < before + mine && (!one || warp == 0)) {
     for (int r = from;; ++r) {
-      if (per > 1) w = __ldg(reinterpret_cast<const int4*>(reqs + r));
+      if (per > 1) w = *reinterpret_cast<const int4*>(reqs + r);
       const int c = items_of(w);
       if (index < before + c) {
         const int base = (index - before) * 2 * kRows, token = base / p.group;
@@ -348,7 +348,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         int token, head;
         row_of(s, it, t * kRows + r, token, head);
         v[i] = make_uint4(0u, 0u, 0u, 0u);
-        if (r < left) v[i] = __ldg(reinterpret_cast<const uint4*>(from + (size_t)token * p.q_stride + head * D));
+        if (r < left) v[i] = *reinterpret_cast<const uint4*>(from + (size_t)token * p.q_stride + head * D);
       }
 #pragma unroll
       for (int i = 0; i < PER; ++i) {
@@ -550,7 +550,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       for (int j = 0; j < plan.count && ok; ++j) {
         const int key0 = plan.tile(j) * kKeys, key = key0 + (lane << p.page_shift);
         const bool mine = lane < pages && key < it.len;
-        const int id = mine ? checked_page(p, __ldg(table + (key >> p.page_shift)), it.request) : 0;
+        const int id = mine ? checked_page(p, table[key >> p.page_shift], it.request) : 0;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine)) * (uint32_t)(p.page * D * 2);
         for (int which = 0; which < 2; ++which, ++copies) {
           const int at = copies % SH::STAGES;
@@ -692,7 +692,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       for (int j = 0; j < plan.count && ok; ++j) {
         const int key0 = plan.tile(j) * kKeys, key = key0 + (lane << p.page_shift);
         const bool mine = lane < pages && key < it.len;
-        const int id = mine ? checked_page(p, __ldg(table + (key >> p.page_shift)), it.request) : 0;
+        const int id = mine ? checked_page(p, table[key >> p.page_shift], it.request) : 0;
         const uint32_t bytes = (uint32_t)__popc(__ballot_sync(0xFFFFFFFFu, mine)) * (uint32_t)(p.page * (D + D / 16));
         const size_t block = ((((size_t)id * p.hkv + it.head) << p.page_shift)) * SH::BLOCKS;      // of 16 elements
         for (int which = 0; which < 2; ++which, ++copies) {

@@ -264,7 +264,7 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendParams p) {
   for (size_t i = blockIdx.x * (size_t)256 + threadIdx.x; i < items; i += (size_t)gridDim.x * 256) {
     const int row = (int)(i / per_row), rest = (int)(i - (size_t)row * per_row);
     const int which = rest >= p.hkv * p.blocks, at = rest - which * p.hkv * p.blocks, h = at / p.blocks, b = at - h * p.blocks;
-    const int slot = __ldg(p.slots + row);
+    const int slot = p.slots[row];
     if (slot < 0 || slot >= p.capacity) continue;
     const size_t x = (size_t)row * (which ? p.v_stride : p.k_stride) + (size_t)at * 16;
     const size_t y = ((((size_t)(slot >> p.page_shift) * p.hkv + h) << p.page_shift) + (slot & (p.page - 1))) * (size_t)p.blocks + b;   // in blocks
@@ -273,12 +273,12 @@ __global__ void __launch_bounds__(256) append_kernel(const AppendParams p) {
     uint4 raw[4];
     if (XB) {
       const uint4* src = reinterpret_cast<const uint4*>(static_cast<const uint16_t*>(X) + x);
-      raw[0] = __ldg(src);
-      raw[1] = __ldg(src + 1);
+      raw[0] = src[0];
+      raw[1] = src[1];
     } else {
       const uint4* src = reinterpret_cast<const uint4*>(static_cast<const float*>(X) + x);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) raw[k] = __ldg(src + k);
+      for (int k = 0; k < 4; ++k) raw[k] = src[k];
     }
     if (XB && !MX) {
       uint4* dst = static_cast<uint4*>(C) + 2 * y;

@@ -105,7 +105,9 @@ __device__ __forceinline__ float exp2_fast(float x) {
 cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqer_kv_cache_t& c, void* scratch, cudaStream_t s);
 size_t tiles_scratch_bytes(const Attention& a, int head_dim);
 
-// Launches with the programmatic attribute: the kernels wait for their predecessor before they touch memory.
+// Launches with the programmatic attribute: the kernels wait for their predecessor before they touch memory.  What it may have written while they were
+// there already (plan, tables, slots, queries, keys, values) is read by ordinary loads: those that are marked read-only promise that nobody writes during the
+// kernel's whole life, and could find what a kernel before the predecessor left in the SM's cache.
 template <class... P, class... A>
 static cudaError_t launch_after(void (*kernel)(P...), dim3 grid, int threads, size_t smem, cudaStream_t s, A... args) {
   cudaLaunchConfig_t cfg = {};
