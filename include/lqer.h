@@ -469,9 +469,10 @@ lqer_status_t lqer_inject_stall(int kernel_family);
  * Every global store of the inference kernels and every bulk copy of packed weights first checks its byte range
  * against the extent of the buffer it belongs to; the first violation is written to the status word
  * (LQER_ERR_BOUNDS; lqer_poll_status) and the access is skipped - nothing traps, nothing out of range is touched.
- * The kernels between the layers check their stores of Y where they have a status word, the adapters' in their plan.
+ * The kernels between the layers check their stores of Y where they have a status word, the adapters' in their plan; a step of the cache tables checks all
+ * of its stores and the attention those of Y and of its workspace, in the step.  Appending has no status word: it looks at every slot in either build.
  * It stands in for a memory checker where none can be run.  lqer_debug_bounds_shrink (host, process wide) is its test
- * hook: the declared extent of every Y is made `bytes` smaller for the launches that follow, so that the checks at
+ * hook: the declared extent of every Y, and of a step's slots and positions, is made `bytes` smaller for the launches that follow, so that the checks at
  * the end of Y fire (the stores they guard are skipped; Y is then incomplete); 0 restores.  The ordinary build
  * returns LQER_ERR_CONFIG. */
 lqer_status_t lqer_debug_bounds_shrink(long long bytes);

@@ -49,7 +49,7 @@ struct Split {
   Span* spans;                               // [CTAs]
   float* parts;                              // [CTAs][2][8 NT][D + 2]: part 0 continues a row, part 1 begins one; sums, then m and l
   int few;                                   // requests of more rows than this are left alone
-  size_t y_extent;
+  size_t y_extent, spans_extent, parts_extent;
 };
 
 struct Visible { int sink_chunks, first_chunk, chunks; };     // chunks [0, sink_chunks) and [first_chunk, ..), as many as chunks together
@@ -189,7 +189,8 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, g = lane >> 2, c = lane & 3;
-  if (tid == 0) s.spans[blockIdx.x].parts = 0;
+  const bool span_fits = LQER_IN_BOUNDS(&p.step->status, blockIdx.x * sizeof(Span), sizeof(Span), s.spans_extent, 65);
+  if (tid == 0 && span_fits) s.spans[blockIdx.x].parts = 0;
   if (!step_fits(p, blockIdx.x == 0 && tid == 0)) return;
   const Run run = find_run(s, ROWS, &sm_run);
   long long u = run.per * blockIdx.x;
@@ -475,12 +476,12 @@ __global__ void __launch_bounds__(kSplitThreads, Ring<D, MX, NT>::CTAS) split_ke
         const size_t at = ((size_t)(row0 + x / p.group) * p.hq + h * p.group + x % p.group) * D + d;
         if (LQER_IN_BOUNDS(&p.step->status, at * 2, 8, s.y_extent, 60))
           *reinterpret_cast<uint2*>(static_cast<uint16_t*>(p.Y) + at) = make_uint2(round_bf16x2(sum.x * inv, sum.y * inv), round_bf16x2(sum.z * inv, sum.w * inv));
-      } else {
+      } else if (LQER_IN_BOUNDS(&p.step->status, (size_t)(part - s.parts) * 4, (size_t)ROWS * (D + 2) * 4, s.parts_extent, 66)) {
         *reinterpret_cast<float4*>(part + row * D + d) = sum;
         if (d == 0) { part[ROWS * D + row] = big; part[ROWS * D + ROWS + row] = all; }
       }
     }
-    if (!whole && c0 == 0 && tid == 0) {
+    if (!whole && c0 == 0 && tid == 0 && span_fits) {
       const long long stop = before + (which + 1) * vis.chunks;      // where the row tile ends
       s.spans[blockIdx.x] = Span{row0, rows, h, tile, (int)((stop - 1) / run.per) - (int)blockIdx.x + 1, {}};
     }
@@ -597,11 +598,11 @@ static kv::Attention attention_params(const lqer_kv_cache_t& c, const lqer_page_
 static size_t spans_bytes() { return ((size_t)4 * sm_count() * sizeof(kv::Span) + 255) & ~(size_t)255; }
 
 // Parts of few rows, and behind them those of tiles.
-static size_t few_bytes(const kv::Attention& p, int head_dim) {
+static size_t few_parts_bytes(const kv::Attention& p, int head_dim) {
   const int rows = kv::rows_per_tile(p);
-  const size_t bytes = spans_bytes() + (size_t)kv::split_grid(p, kv::few_rows(p), rows, head_dim) * 2 * rows * (head_dim + 2) * sizeof(float);
-  return (bytes + 255) & ~(size_t)255;
+  return (size_t)kv::split_grid(p, kv::few_rows(p), rows, head_dim) * 2 * rows * (head_dim + 2) * sizeof(float);
 }
+static size_t few_bytes(const kv::Attention& p, int head_dim) { return (spans_bytes() + few_parts_bytes(p, head_dim) + 255) & ~(size_t)255; }
 // A window as long as the tables hides nothing; and positions are below 2^30, so that no difference of one with either overflows.
 static void set_window(kv::Attention& p, int window, int sinks) {
   p.window = window < (long long)p.max_pages * p.page ? window : 0;
@@ -627,6 +628,7 @@ cudaError_t launch_paged_attention(const void* Q, size_t q_stride, int M, int hq
   k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + spans_bytes());
   const size_t whole = (size_t)M * hq * c.head_dim * 2, less = debug_y_shrink();
   k.y_extent = whole > less ? whole - less : 0;
+  if (kDebugBounds) { k.spans_extent = spans_bytes(); k.parts_extent = few_parts_bytes(k.a, c.head_dim); }
   if (kv::most_rows(k.a) > k.few) {                                // (then there are items of more than kLeast rows, or a single request's)
     // A single request goes there whatever it turns out to bring; beside one that has to, only those of few rows stay (three prompts of 42 to 97 tokens,
     // 16/4 heads: 18.4 us where the smaller ones stayed, 11.7).

@@ -56,6 +56,7 @@ struct Tiles {
   bool y_wide;                 // Y: aligned to 32 bytes
   int sms;                     // items beyond whole turns of so many CTAs may be divided over their keys; 0: none is
   struct Divided* divided;     // [1 + sms / 2]: their number (request of the first entry), and what they are
+  size_t divided_extent, parts_extent;
   float* parts;                // [sms][256][D + 2]: rows' sums, then maxima and sums of weights
 };
 struct Barriers {
@@ -304,7 +305,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     if (it.slot >= 0) {
       // a part has two key tiles or more; an item with fewer has fewer parts
       parts = min(it.parts, max((plan.count + 1) / 2, 1));
-      if (it.part == 0 && tid == 0) s.divided[1 + it.slot] = Divided{it.request, it.head, it.row0, it.rows, it.token0, it.head0, it.base, parts};
+      if (it.part == 0 && tid == 0 && LQER_IN_BOUNDS(&p.step->status, (size_t)(1 + it.slot) * sizeof(Divided), sizeof(Divided), s.divided_extent, 67))
+        s.divided[1 + it.slot] = Divided{it.request, it.head, it.row0, it.rows, it.token0, it.head0, it.base, parts};
       if (it.part >= parts) return;
       plan.skip = (int)((long long)plan.count * it.part / parts);
       plan.count = (int)((long long)plan.count * (it.part + 1) / parts) - plan.skip;
@@ -510,9 +512,11 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
     const float all = (l[0] + l[1]) + (l[2] + l[3]);
     if (DIVIDED && parts > 1) {
       // a part's sums as they are; where it saw nothing, only that it did not
-      float* const part = s.parts + (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2) + (size_t)(t * kRows + row) * D;
-      float* const marks = s.parts + (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2) + (size_t)2 * kRows * D + t * kRows + row;
-      if (ok && left > 0) {
+      const size_t part_at = (size_t)(it.slot * it.parts + it.part) * 2 * kRows * (D + 2);
+      float* const part = s.parts + part_at + (size_t)(t * kRows + row) * D;
+      float* const marks = s.parts + part_at + (size_t)2 * kRows * D + t * kRows + row;
+      const bool fits = LQER_IN_BOUNDS(&p.step->status, part_at * 4, (size_t)2 * kRows * (D + 2) * 4, s.parts_extent, 68);
+      if (ok && left > 0 && fits) {
         marks[0] = n > 0 ? m : -INFINITY;                          // (of the scores as they are: the join scales differences, too)
         marks[2 * kRows] = all;
       }
@@ -522,7 +526,8 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
         tc::tmem_ld32(o_at + 32 * k, o);
         tc::tmem_ld_wait();
 #pragma unroll
-        for (int i = 0; i < 4; ++i) store32(part + 32 * k + 8 * i, true, o + 8 * i);
+        for (int i = 0; i < 4; ++i)
+          if (fits) store32(part + 32 * k + 8 * i, true, o + 8 * i);
       }
     } else if (ok && n > 0) {
       const float inv = 1.f / all;
@@ -844,6 +849,8 @@ cudaError_t launch_tiles(const Attention& a, int few, size_t y_extent, const lqe
   Tiles k = {};
   if (may_divide(a)) {
     k.sms = sm_count();
+    k.divided_extent = divided_bytes();
+    k.parts_extent = (size_t)k.sms * 2 * kRows * (c.head_dim + 2) * sizeof(float);
     k.divided = static_cast<Divided*>(scratch);
     k.parts = reinterpret_cast<float*>(static_cast<uint8_t*>(scratch) + divided_bytes());
   }

@@ -24,6 +24,7 @@ struct StepParams {
   int* positions;
   StepHead* head;
   int R, M, max_pages, n_pages, page, page_shift, max_added;
+  size_t rows_extent;        // bytes of slots, and of positions
 };
 struct Request {
   int len, next;             // tokens before and after
@@ -83,6 +84,11 @@ __device__ __forceinline__ void slot_of(const StepParams& p, int r, int i, int n
     fail(LQER_ERR_BOUNDS);
   }
 }
+// The checked build's view of the step's stores: entry i of a list of n, and of the rows' slots and positions.
+__device__ __forceinline__ bool entry_fits(DeviceStatus* st, size_t i, size_t n, int site) { return LQER_IN_BOUNDS(st, i * sizeof(int), sizeof(int), n * sizeof(int), site); }
+__device__ __forceinline__ bool row_fits(const StepParams& p, DeviceStatus* st, int row) {
+  return LQER_IN_BOUNDS(st, (size_t)row * sizeof(int), sizeof(int), p.rows_extent, 11);
+}
 // Place i of a ring of n entries from `start` on (i below n).
 __device__ __forceinline__ int around(int start, int i, int n) { return i < n - start ? start + i : i - (n - start); }
 constexpr int kBatch = 4;    // list entries that a thread has on their way
@@ -90,14 +96,15 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   __shared__ int first[kStepThreads], from[kStepThreads], row0s[kStepThreads], ns[kStepThreads], lens[kStepThreads];
   __shared__ int sums32[32];
   __shared__ long long sums64[32];
-  __shared__ int taken, status;
+  __shared__ int taken;
+  __shared__ DeviceStatus status;
   tc::pdl_launch_dependents();
   tc::pdl_wait();
   const int tid = threadIdx.x;
   const long long head = p.ring[0], tail = p.ring[1];
-  if (tid == 0) { taken = 0; status = LQER_OK; }
+  if (tid == 0) { taken = 0; status = DeviceStatus{LQER_OK, 0, 0, 0}; }
   __syncthreads();
-  auto fail = [&](int code) { atomicCAS(&status, (int)LQER_OK, code); };
+  auto fail = [&](int code) { report_error(&status, code, 10); };
   const Request q0 = request_at(p, tid);
   auto request = [&](int base) { return base == 0 ? q0 : request_at(p, base + tid); };
   // pages that come back
@@ -129,7 +136,8 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
         for (int u = 0; u < kBatch; ++u) {
           const int i = at + u * kStepThreads;
           if (i >= total) continue;
-          p.free_pages[around(start, i, p.n_pages)] = id[u];
+          const int at = around(start, i, p.n_pages);
+          if (entry_fits(&status, at, p.n_pages, 12)) p.free_pages[at] = id[u];
           if ((unsigned)id[u] >= (unsigned)p.n_pages) fail(LQER_ERR_BOUNDS);
         }
       }
@@ -166,8 +174,10 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
     ns[tid] = ok ? (int)q.rows : 0;
     lens[tid] = ok ? q.next : q.bad ? 0 : q.len;
     if (r < p.R) {
-      out[r] = StepRequest{row0s[tid], ns[tid], lens[tid], 0};
-      p.lengths_out[r] = lengths[r] = ok ? q.next : q.len;
+      if (entry_fits(&status, r, p.R, 13)) {
+        out[r] = StepRequest{row0s[tid], ns[tid], lens[tid], 0};
+        p.lengths_out[r] = lengths[r] = ok ? q.next : q.len;
+      }
     }
     __syncthreads();
     // (whoever is not refused takes pages that are there: fewer than n_pages before them)
@@ -183,7 +193,8 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
       }
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
-        if (of[u] >= 0) p.tables[(size_t)of[u] * p.max_pages + entry[u]] = id[u];
+        if (of[u] >= 0 && entry_fits(&status, (size_t)of[u] * p.max_pages + entry[u], (size_t)p.R * p.max_pages, 14))
+          p.tables[(size_t)of[u] * p.max_pages + entry[u]] = id[u];
     }
     wanted_before += total;
     __syncthreads();
@@ -199,7 +210,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
 #pragma unroll
         for (int u = 0; u < kBatch; ++u) {
           const int row = at + u * kStepThreads;
-          if (row < hi) { p.slots[row] = slot[u]; p.positions[row] = pos[u]; }
+          if (row < hi && row_fits(p, &status, row)) { p.slots[row] = slot[u]; p.positions[row] = pos[u]; }
         }
       }
       __syncthreads();
@@ -208,7 +219,9 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
   }
   const int rows = (int)min(rows_before, (long long)p.M);
   if (rows_inside)
-    for (int row = rows + tid; row < p.M; row += kStepThreads) p.slots[row] = p.positions[row] = -1;
+    for (int row = rows + tid; row < p.M; row += kStepThreads)
+      if (row_fits(p, &status, row)) p.slots[row] = p.positions[row] = -1;
+  if (kDebugBounds) __syncthreads();
   if (tid == 0) {
     long long* const ring = reinterpret_cast<long long*>(plan + step_ring_at(p.R));
     p.ring_out[0] = ring[0] = head + taken;
@@ -216,7 +229,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
     StepHead h = {};
     h.magic = kStepMagic;
     h.R = p.R; h.M = p.M; h.page = p.page; h.max_pages = p.max_pages; h.n_pages = p.n_pages; h.max_added = p.max_added; h.rows = rows;
-    h.status.code = status;
+    h.status = status;
     *p.head = h;
   }
 }
@@ -235,8 +248,7 @@ __global__ void __launch_bounds__(256) rows_kernel(const StepParams p) {
   const StepRequest q = reqs[lo];
   int slot, pos;
   slot_of(p, lo, row - q.row0, q.n, q.len, [&](int code) { report_error(&p.head->status, code, 10, lo, row); }, slot, pos);
-  p.slots[row] = slot;
-  p.positions[row] = pos;
+  if (row_fits(p, &p.head->status, row)) { p.slots[row] = slot; p.positions[row] = pos; }
 }
 
 // ---------------------------------------------------------------------------- appending
@@ -319,7 +331,9 @@ size_t cache_step_bytes(int R) { return kv::step_bytes(R); }
 cudaError_t launch_cache_step(const lqer_page_table_t& t, const int* lengths, const int* added, const long long* ring, int M, int max_added,
                               int* lengths_out, long long* ring_out, int* slots, int* positions, void* step, cudaStream_t s) {
   kv::StepParams p = {lengths, added, t.tables, t.free_pages, ring, lengths_out, ring_out, slots, positions, static_cast<kv::StepHead*>(step),
-                      t.n_requests, M, t.max_pages, t.n_pages, t.page, log2_of(t.page), max_added};
+                      t.n_requests, M, t.max_pages, t.n_pages, t.page, log2_of(t.page), max_added, 0};
+  const size_t rows = (size_t)M * sizeof(int), less = debug_y_shrink();
+  p.rows_extent = rows > less ? rows - less : 0;
   const bool inside = M <= kv::kRowsInside;
   LaunchScope scope(kFamDecode, s, inside ? 1 : 2);
   cudaError_t e = kv::launch_after(kv::step_kernel, dim3(1), kv::kStepThreads, 0, s, p, inside ? 1 : 0);
