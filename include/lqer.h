@@ -458,7 +458,8 @@ lqer_status_t lqer_set_path(int path);
  * the kernel give up, write LQER_ERR_TIMEOUT to the status word and return, so the context stays usable.
  *  - lqer_set_wait_limit_cycles: the bound in SM clock cycles (default 4e9, about two seconds; 1e3 .. 2^40).
  *  - lqer_inject_stall(family): the next launch of that kernel family (numbering of lqer_kernel_times_t:
- *    3 activation prologue, 6 tensor-core GEMM pair kernel, 7 decode and small-batch kernels, adapters of many rows) is told to expect one arrival
+ *    3 activation prologue, 6 tensor-core GEMM pair kernel, 7 decode and small-batch kernels, adapters of many rows, attention of many rows; launches of
+ *    a family that have no waits, as the adapters' and the attention's of few rows, leave it for the next one that has) is told to expect one arrival
  *    more than will ever come (3, 7) or has its last stage of operands withheld (6), so that its waits run
  *    out; no memory is touched that an ordinary launch would not touch.  -1 disarms.  After such a launch
  *    the outputs are undefined and the workspace needs lqer_workspace_init before its next use. */

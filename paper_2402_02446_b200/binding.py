@@ -834,7 +834,7 @@ def _head_rows(t: torch.Tensor, heads: int, dim: int, index: int):
 
 
 def append_kv(K: torch.Tensor, V: torch.Tensor, cache: KVCache, slots: torch.Tensor, cfg: Config | None = None, stream=None) -> None:
-    """Puts keys and values [M, kv_heads, head_dim] (or [M, kv_heads * head_dim]; fp32 or bf16, any row stride, as parts of a joint projection have)
+    """Puts keys and values [M, kv_heads, head_dim] (or [M, kv_heads * head_dim]; fp32 or bf16, rows any multiple of 8 elements apart, as parts of a joint projection are)
     into their slots (int32 [M], of a step): rounded to bf16, or quantised to MXINT8 in the format of cfg, which is the cache's own if not given and has to have
     its mantissas' bits otherwise."""
     index = K.get_device()
@@ -865,7 +865,7 @@ def attention_workspace_bytes(M: int, q_heads: int, cache: KVCache, pages: PageT
 def paged_attention(Q: torch.Tensor, cache: KVCache, pages: PageTable, step: CacheStep, window: int = 0, sinks: int = 0, scale: float | None = None,
                     cfg: Config | None = None, Y: torch.Tensor | None = None, ws: torch.Tensor | None = None, stream=None) -> torch.Tensor:
     """Causal attention of a step's new tokens over the cache, their own keys and values included: bf16 [M, q_heads, head_dim].  Q [M, q_heads, head_dim]
-    bf16, any row stride.  window: a token sees only the last `window` tokens (itself among them) and the first `sinks`; 0: all.  scale: of the scores,
+    bf16, rows any multiple of 8 elements apart.  window: a token sees only the last `window` tokens (itself among them) and the first `sinks`; 0: all.  scale: of the scores,
     head_dim ** -0.5 if not given.  cfg: the format of an MXINT8 cache, its own if not given.  Rows behind the last token are left as they are in Y (undefined where none is given).  ws: a workspace of
     attention_workspace_bytes, made where none is given."""
     index = Q.get_device()

@@ -303,7 +303,7 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
   int parts = 1;
   if constexpr (DIVIDED) {
     if (it.slot >= 0) {
-      // a part has two key tiles or more; an item with fewer has fewer parts
+      // a part has two key tiles or so (of an odd count one has a single one); an item with few has fewer parts
       parts = min(it.parts, max((plan.count + 1) / 2, 1));
       if (it.part == 0 && tid == 0 && LQER_IN_BOUNDS(&p.step->status, (size_t)(1 + it.slot) * sizeof(Divided), sizeof(Divided), s.divided_extent, 67))
         s.divided[1 + it.slot] = Divided{it.request, it.head, it.row0, it.rows, it.token0, it.head0, it.base, parts};

@@ -228,7 +228,7 @@ __global__ void __launch_bounds__(kStepThreads) step_kernel(const StepParams p, 
     p.ring_out[1] = ring[1] = ring_ok ? tail + all_given : tail;
     StepHead h = {};
     h.magic = kStepMagic;
-    h.R = p.R; h.M = p.M; h.page = p.page; h.max_pages = p.max_pages; h.n_pages = p.n_pages; h.max_added = p.max_added; h.rows = rows;
+    h.R = p.R; h.M = p.M; h.page = p.page; h.max_pages = p.max_pages; h.n_pages = p.n_pages; h.max_added = p.max_added;
     h.status = status;
     *p.head = h;
   }

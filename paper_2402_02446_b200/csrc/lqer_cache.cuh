@@ -12,12 +12,11 @@ namespace lqer {
 namespace kv {
 
 constexpr uint32_t kStepMagic = 0x50455453u;
-constexpr int kMaxRequests = 16384;
 
 struct StepHead {              // first 256 bytes of a step's plan
   DeviceStatus status;
   uint32_t magic;
-  int R, M, page, max_pages, n_pages, max_added, rows;     // rows: of all requests together
+  int R, M, page, max_pages, n_pages, max_added;
 };
 struct StepRequest {           // one per request, behind the head
   int row0, n, len, reserved;  // first row, rows (0: none, or refused), tokens that it holds once they are in
