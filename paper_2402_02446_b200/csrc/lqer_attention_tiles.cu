@@ -437,9 +437,6 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
       if (__any_sync(0xFFFFFFFFu, up)) {
         const float f = up ? exp2_fast((m - big) * c) : 1.f;
         if (up) m = big;
-        base = m == -INFINITY ? 0.f : -m * c;
-        far = __any_sync(0xFFFFFFFFu, !(fabsf(base) <= kNear));
-        if (far) base = 0.f;
         if (n > 0) {
           la = fma2(la, f2(f, f), f2(0.f, 0.f));
           lb = fma2(lb, f2(f, f), f2(0.f, 0.f));
@@ -456,6 +453,9 @@ tiles_kernel(const Tiles s, const __grid_constant__ CUtensorMap key_map, const _
             tmem_st16(o_at + 16 * k, o);
           }
         }
+        base = m == -INFINITY ? 0.f : -m * c;
+        far = __any_sync(0xFFFFFFFFu, !(fabsf(base) <= kNear));
+        if (far) base = 0.f;
       }
       if (far) {
         const float top = m == -INFINITY ? 0.f : m, less = (top - top) - top;
