@@ -399,7 +399,7 @@ typedef struct {
  *    steps wants it).  Otherwise the step may be taken again: tables and free_pages, changed in place, then get the same entries.
  *  - The rows of the step's tensors [M, ..] belong to the requests in order, max(added[r], 0) each; slots and positions [M] get every
  *    row's slot (page * tokens a page + place in the page; what lqer_append_kv takes) and the token's place in its request (what a
- *    rotary embedding takes), and -1 for rows behind the last.
+ *    rotary embedding takes), and -1 for rows behind the last.  A step that brings no rows has M 0, and NULL for both.
  *  - step (lqer_cache_step_bytes, 256-byte aligned) gets the plan that lqer_paged_attention reads.  max_added: what no added[r] exceeds.
  *    Its last bytes are the step's own lengths (n_requests ints, 16-byte aligned) and, in the last 16 of lqer_cache_step_bytes, its ring, the same as in lengths_out
  *    and ring_out (which may be these).

@@ -794,7 +794,8 @@ class CacheStep:
 def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | None = None, step: CacheStep | None = None, commit: bool = True,
                stream=None) -> CacheStep:
     """Takes the batch one step further: request r takes added[r] tokens (int32 [n_requests]), or loses -added[r]; pages are given out and taken back.
-    M: rows of the step's tensors, those of the requests in order and any padding behind them.  max_added: what no added[r] exceeds (M if not given); 1 tells
+    M: rows of the step's tensors, those of the requests in order and any padding behind them (0: none brings any).  max_added: what no added[r] exceeds (M if not
+    given, 1 at least); 1 tells
     that this is a decoding step.  step: one of the same sizes to be made again in place.  commit: pages.lengths and pages.ring step on too (in place);
     otherwise they stay, and only the step's own hold what would be."""
     index = added.get_device()
@@ -805,10 +806,10 @@ def cache_step(pages: PageTable, added: torch.Tensor, M: int, max_added: int | N
         raise ValueError("expected added int32 [n_requests]")
     if pages.index != index:
         raise ValueError("expected the page table on the device of added")
-    max_added = M if max_added is None else max_added
+    max_added = max(M, 1) if max_added is None else max_added
     if step is None:
-        if M < 1:
-            raise ValueError("a step has at least one row")
+        if M < 0:
+            raise ValueError("a step has no fewer rows than none")
         step = CacheStep(pages, M, max_added)
     elif step.M != M or step.n_requests != pages.n_requests or step.index != index:
         raise ValueError("the step to be made again has other sizes")
@@ -847,6 +848,8 @@ def append_kv(K: torch.Tensor, V: torch.Tensor, cache: KVCache, slots: torch.Ten
     k_stride, k_ptr = _head_rows(K, cache.kv_heads, cache.head_dim, index)
     v_stride, v_ptr = _head_rows(V, cache.kv_heads, cache.head_dim, index)
     cfg = cache.format(cfg)
+    if M == 0:
+        return
     status = lib().lqer_append_kv(k_ptr, v_ptr, _code(_REAL_CODE, K.dtype), k_stride, v_stride, M, _ptr(slots, index), cache.ref,
                                   None if cfg is None else C.byref(cfg), _raw_stream(index))
     if status:
@@ -883,6 +886,8 @@ def paged_attention(Q: torch.Tensor, cache: KVCache, pages: PageTable, step: Cac
         Y = Q.new_empty(shape)
     elif Y.shape != shape or Y.dtype != torch.bfloat16:
         raise ValueError("expected Y bf16 [M, q_heads, head_dim]")
+    if M == 0:
+        return Y
     if ws is None:
         key = (heads, cache.key, pages.key)
         room = step.room.get(key)

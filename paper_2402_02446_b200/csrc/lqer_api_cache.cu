@@ -69,17 +69,18 @@ lqer_status_t lqer_cache_step_bytes(int n_requests, size_t* bytes) {
 
 lqer_status_t lqer_cache_step(const lqer_page_table_t* table, const int* lengths, const int* added, const long long* ring, int M, int max_added,
                               int* lengths_out, long long* ring_out, int* slots, int* positions, void* step, size_t step_bytes, void* stream) {
-  if (lengths == nullptr || added == nullptr || ring == nullptr || lengths_out == nullptr || ring_out == nullptr || slots == nullptr || positions == nullptr ||
-      step == nullptr)
+  const bool empty = M == 0 && slots == nullptr && positions == nullptr;       // a step without rows has no lists of them
+  if (lengths == nullptr || added == nullptr || ring == nullptr || lengths_out == nullptr || ring_out == nullptr || step == nullptr ||
+      (!empty && (slots == nullptr || positions == nullptr)))
     return LQER_ERR_NULL;
   lqer_status_t st = table_ready(table, true);
   if (st != LQER_OK) return st;
-  if (!rows_ok(M) || max_added < 1) return LQER_ERR_SHAPE;
+  if ((!empty && !rows_ok(M)) || max_added < 1) return LQER_ERR_SHAPE;
   if (misaligned(lengths, 4) || misaligned(added, 4) || misaligned(ring, 8) || misaligned(lengths_out, 4) || misaligned(ring_out, 8) || misaligned(slots, 4) ||
       misaligned(positions, 4) || misaligned(step, 256))
     return LQER_ERR_ALIGN;
   if (step_bytes < cache_step_bytes(table->n_requests)) return LQER_ERR_BUFFER_TOO_SMALL;
-  if (lengths_out == added || slots == positions || table->tables == table->free_pages) return LQER_ERR_CONFIG;
+  if (lengths_out == added || (!empty && slots == positions) || table->tables == table->free_pages) return LQER_ERR_CONFIG;
   if ((st = check_arch()) != LQER_OK) return st;
   return of(launch_cache_step(*table, lengths, added, ring, M, max_added, lengths_out, ring_out, slots, positions, step, static_cast<cudaStream_t>(stream)));
 }
