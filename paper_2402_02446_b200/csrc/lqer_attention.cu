@@ -18,7 +18,7 @@
 //
 // Measured (GPU time): 64 requests of up to 8191 tokens, 40/8 heads of 128, bf16: 209 us, 6.4 TB/s, what a copy reaches; 24 of up to 4099, 40/40 heads, MXINT8: 168 us,
 // 4.1 TB/s, bound by instructions (some 600 for a warp's 16 keys, more than half of them for the mantissas); eight long ones, four drafted tokens, 32/8 heads under a
-// window of 4096: 34 us, 3.9 TB/s (of it 5 before the first keys are there and 3 for the joining); one of 1021 tokens 9.3 us, of 16000 16, of
+// window of 4096: 34 us, 3.9 TB/s (of it 5 before the first keys are there and 3 for the joining); 64 requests of up to 8191, 32/8 heads of 64: 110, from MXINT8 111; one of 1021 tokens 9.5 us, of 16000 16, of
 // 100000 73: launches and a chain of trips to memory, then the bytes.  Tried: the CTA that brings a row's last part joins them (a launch less, 2 us on the host,
 // but 1 to 3 us more on the GPU where parts are many); mantissas' low bytes by multiplication (slower); more or deeper stages (none).
 #include "lqer_cache.cuh"
@@ -32,7 +32,8 @@ constexpr int kChunk = 64, kWarps = 4, kSplitThreads = 32 * kWarps;
 // the time is shared by all SMs from the start, but grows with the rows, 16 at a time (some 12 ns a key and head, over the SMs).  So long tables, which
 // are what the host knows of the lengths, leave less to it.  Both sides measured, here / there, 32/8 heads, us: one request, 64 rows behind 1000: 12 / 16,
 // behind 4000: 19 / 17, behind 16000: 44 / 27 (MXINT8 56 / 30); two, 64 rows: 16 / 20, 24 / 24, 54 / 44; four, 32 rows: 16 / 21, 24 / 31, 59 / 74, 64 rows:
-// 18 / 21, 31 / 31, 81 / 75; 8, 80 rows behind 2000: 36 / 36; 64, 32 rows: 418 / 318, 80: 200 / 106.
+// 18 / 21, 31 / 31, 81 / 75; 8, 80 rows behind 2000: 36 / 36; 64, 32 rows: 418 / 318, 80: 200 / 106.  The constants below are where the two sides cross in these
+// cases.  Tables that are much wider than the requests are long take the other side sooner than they should: 64 rows behind 1000, tables for 32768: 14.6 instead of 13.0.
 constexpr int kLeast = 16;
 inline int few_rows(const Attention& p) {
   const long long heads = (long long)(p.R < p.M ? p.R : p.M) * p.hkv, few = 2900 / heads, most = (long long)p.max_pages * p.page > 4096 ? 48 : 96;

@@ -13,8 +13,8 @@
 //   issuer           one lane: per key tile and row tile, O += P V of the last key tile, in two halves as the weights come, then S of the next.
 // Keys and values share a ring of tiles.  Every wait is bounded.
 //
-// Measured, 32/8 heads of 128, GPU time: a prompt of 8192 tokens 456 us (1.2 PFLOP/s of what a causal row sees, 0.72 of a long GEMM's burst rate; 545 us when
-// it runs without a pause and the power cap lowers the clock), from MXINT8 514, heads of 64 392; windows of 1024, 32/32 heads, MXINT8, 7682 tokens 210.  A key
+// Measured, 32/8 heads of 128, GPU time in bursts: a prompt of 8192 tokens 465 us (1.18 PFLOP/s of what a causal row sees, 0.71 of a long GEMM's burst rate; 530 us when
+// it runs without a pause and the power cap lowers the clock), from MXINT8 536, heads of 64 408; windows of 1024, 32/32 heads, 7682 tokens 189, from MXINT8 219.  A key
 // tile takes a CTA 3100 clocks: 16 MMAs for each row tile at some 85 clocks (64 by the rate; S reads both operands from shared memory, 128 bytes a
 // clock), 2100 from S to the last weights, and the issuer's way between.  Beside its key tiles an item takes 16000: 3500 until it is known, 5000 for the queries
 // (where all CTAs ask for theirs at once; 1900 by itself), 2200 until the first scores, 2500 for the results, 1300 until the next CTA, and at the end
@@ -23,8 +23,8 @@
 // them, which takes 800 of the 2100 clocks away but not the total; two threads a row; an issuer for each row tile (574); short loops over 32 columns (480 to 515).
 //
 // Where the items of 256 rows leave a last turn of CTAs half empty or more (few requests, short pieces of long prompts), that turn's items are divided over
-// their keys, up to 16 CTAs to one, and a second kernel joins the parts.  Whole / divided, us: 2048 tokens behind 10240, 40/8 heads (320 items) 476 / 384, MXINT8
-// 546 / 429; 512 behind 15488, 32/8 heads 212 / 123; 300 of 4000, two requests 67 / 49.  It is a kernel of its own: what it needs beside costs registers
+// their keys, up to 16 CTAs to one, and a second kernel joins the parts.  Whole / divided, us: 2048 tokens behind 10240, 40/8 heads (320 items) 483 / 397, MXINT8
+// 594 / 486; 512 behind 15488, 32/8 heads 212 / 123; 300 of 4000, two requests 67 / 49.  It is a kernel of its own: what it needs beside costs registers
 // that those without it miss (8192 tokens 455 -> 490 us, MXINT8 520 -> 610).
 #include "lqer_cache.cuh"
 
@@ -831,7 +831,8 @@ static cudaError_t launch_shape(const Tiles& k, int ctas, const lqer_kv_cache_t&
 }
 // Whether items may be divided: a division costs a launch and the way of the parts through memory, some 5 us, and gains what the last turn of CTAs leaves of it, if the
 // rows are where they can be, and the keys as many (some 1.8 us for 128).  Not divided / divided, us: 300 tokens, 32/8 heads: 15 / 20, of 600: 19 / 25, of 1000: 23 / 22,
-// of 4000, 1100 tokens, 32/32 heads, MXINT8: 120 / 98, of 16000, 512 tokens: 212 / 123.
+// of 4000, 1100 tokens, 32/32 heads, MXINT8: 120 / 98, of 16000, 512 tokens: 212 / 123.  Where the rows begin is not known here: the last turn's items of a whole prompt are its
+// first rows, which see few keys, so that nothing gets divided and the variant is taken for nothing (4096 tokens, 32/8 heads: 138 / 154, MXINT8 161 / 175; 7680: 414 / 436).
 static bool may_divide(const Attention& a) {
   const int sms = sm_count();
   if (sms < 2) return false;

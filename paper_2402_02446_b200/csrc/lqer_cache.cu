@@ -9,7 +9,7 @@ namespace kv {
 // are as long as what moves.  One CTA does it: the sums need all requests, everything it reads of what it replaces (lengths, ring) is
 // read before, so they may be replaced in place, and a list's entry finds its request by bisection in shared memory.  What bounds it is latency: about a
 // dozen trips to L2 and barriers.  Beyond kRowsInside rows, where a thread would have several behind one another, the slots take a launch of their own over
-// all SMs.  Measured: 64 requests of a token each 7 us, 512 that bring 13000 rows, end and lose drafts 13 (7000 pages move, two launches).
+// all SMs.  Measured: 64 requests of a token each 7 us, 512 that bring 13000 rows, end and lose drafts 14 (7000 pages move, two launches).
 constexpr int kStepThreads = 1024, kRowsInside = 4096;
 
 struct StepParams {
@@ -253,8 +253,8 @@ __global__ void __launch_bounds__(256) rows_kernel(const StepParams p) {
 
 // ---------------------------------------------------------------------------- appending
 // A thread takes 16 consecutive elements of a head, of keys or of values: 32 or 64 bytes in, 32 (bf16) or 16 and an exponent byte
-// (MXINT8) out, in one pass.  Bound: memory from some hundred rows on, a launch below: 64 rows of 8 heads of 128 1.8 us, 4096 5.1 (4.6 TB/s, much of it
-// L2's), 4100 of 16 heads of 64 from fp32 to bf16 7.7.
+// (MXINT8) out, in one pass.  Bound: memory from some hundred rows on, a launch below: 64 rows of 8 heads of 128 1.8 us, 4096 in a row 5.1 (4.6 TB/s, much of it
+// L2's), in any order 6.7, to MXINT8 6.6, from fp32 8.0 and 7.5.
 struct AppendParams {
   const void* K;
   const void* V;
